@@ -9,6 +9,9 @@
  *                            protected block mask (Eq. 9) as ascending per-row column lists
  *   avsa_sparse_self_attn    video self-attention under that mask (Eq. 10 / Eq. 11)
  *
+ * A generation that continues a clip keeps keys and values in a paged cache (avsa_cache_*), which the candidates of a
+ * continuation share as far as they begin alike, and attends to it with avsa_prefix_attn.
+ *
  * Conventions for every call
  *   - All data pointers are DEVICE pointers unless a parameter says "host".  The caller owns every
  *     buffer.  The library allocates no device memory, never synchronises the stream (except
@@ -68,7 +71,9 @@ typedef enum {
   AVSA_ERR_WORKSPACE = 3,    /* ws is NULL or smaller than *_workspace_bytes() */
   AVSA_ERR_CUDA = 4,         /* a CUDA runtime / driver call failed */
   AVSA_ERR_TIMEOUT = 5,      /* device: a bounded wait expired (read with avsa_read_status) */
-  AVSA_ERR_BAD_MASK = 6      /* device: a column list entry was out of range or not ascending */
+  AVSA_ERR_BAD_MASK = 6,     /* device: a column list entry was out of range or not ascending */
+  AVSA_ERR_BAD_TABLE = 7,    /* device: a sequence, a page of a sequence or a length of a paged cache is out of range */
+  AVSA_ERR_NO_PAGES = 8      /* device: a paged cache has too few free pages, or a sequence's row of the table is full */
 } avsa_status;
 
 /* Size of the status record area at the start of every workspace. */
@@ -79,6 +84,34 @@ typedef struct {
   const void* ptr;
   int64_t stride_b, stride_h, stride_n;
 } avsa_bf16_4d;
+
+/*
+ * Paged K/V cache of a generation.  The keys and values of `seqs` sequences live in `pages` pages of `page` tokens;
+ * token t of sequence s is in page table[s*width + t / page] at place t % page.  A page may belong to several
+ * sequences that begin alike (avsa_cache_fork).  All arrays are contiguous device memory:
+ *   table   int32 [seqs,width]  pages of each sequence in order, -1 behind its last one
+ *   length  int32 [seqs]        tokens of each sequence, 0 = an empty place
+ *   ref     int32 [pages]       sequences that hold the page, 0 = free
+ * A call reads table, length and ref and writes the state behind it to table_out, length_out and ref_out: the same
+ * pointers (in place) or arrays that overlap none of those read.  `page` is 16, 32, 64 or 128 tokens.
+ */
+typedef struct {
+  const int32_t* table;
+  const int32_t* length;
+  const int32_t* ref;
+  int32_t* table_out;
+  int32_t* length_out;
+  int32_t* ref_out;
+  int seqs, width, pages, page;
+} avsa_cache;
+
+/* The memory of the pages, `planes` times over (2 x layers: keys and values of each): page p of plane i is page_bytes
+ * bytes at ptr + i*stride_plane + p*stride_page.  All of them multiples of 16 bytes. */
+typedef struct {
+  void* ptr;
+  int planes;
+  int64_t page_bytes, stride_plane, stride_page;
+} avsa_pages;
 
 /* flags of avsa_build_block_mask */
 #define AVSA_PROTECT_ROWS 1u            /* Eq. 9: a protected query block keeps every key block */
@@ -232,11 +265,64 @@ AVSA_API int avsa_build_block_mask_static(int B, int H, int N, int d, int blk, a
                                           float softmax_scale, float* block_scores, int32_t* col_idx,
                                           int32_t* col_cnt, uint8_t* prot_tok, uint8_t* prot_blk, void* stream);
 
+/*
+ * (6) Attention of a batch that shares a long beginning, over a paged cache.
+ *
+ *   o[b,h,i,:] = sum_{t < lim} softmax_t(q[b,h,i,:] . k_t * softmax_scale) v_t          -> o bf16, strides of q
+ *   lse[b,h,i] = natural-log log-sum-exp of the row                                      -> lse fp32 [B,H,L], optional
+ *
+ * for the keys k_t and values v_t of sequence s = seq[b] (seq NULL: s = b), key/value head h / (H/Hkv), with
+ * lim = length[s], or with AVSA_CAUSAL lim = length[s] - L + i + 1: the L queries are the last L tokens of the
+ * sequence.  Rows with lim <= 0, and all rows of a batch entry with seq[b] < 0, are empty: o = 0, lse = -inf.
+ *
+ *   k_pool, v_pool  [pages,Hkv,page,d]: stride_b is the distance of pages, stride_h of heads, stride_n of tokens
+ *   prefix_pages    the first prefix_pages pages of all sequences of the batch are the same ones (of a shorter
+ *                   sequence: all it has).  Where it costs less they are read once for the whole batch, all its queries stacked on
+ *                   each other; the longest sequence's row of the table then says which pages they are.  0: nothing is shared.
+ *
+ * What pages hold behind a sequence's last token is never used (it may be anything, NaN too).  Values of tokens that a
+ * causal row must not see have to be finite.  A page of the table out of range contributes nothing and sets AVSA_ERR_BAD_TABLE, a
+ * length beyond the table's width is cut there and sets it as well.
+ * d is 64 or 128, H a multiple of Hkv, H/Hkv at most 128.  table has `seqs` rows of `width` entries.  Same bits on every run.
+ */
+#define AVSA_CAUSAL 1u
+AVSA_API int avsa_prefix_attn(int B, int H, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d q,
+                              avsa_bf16_4d k_pool, avsa_bf16_4d v_pool, const int32_t* table, const int32_t* length,
+                              const int32_t* seq, int prefix_pages, unsigned flags, float softmax_scale, void* o_bf16, float* lse,
+                              void* ws, size_t ws_bytes, void* stream);
+AVSA_API size_t avsa_prefix_attn_workspace_bytes(int B, int H, int Hkv, int L, int d, int page, int width, int prefix_pages);
+
+/*
+ * (7) Changes of a paged cache.  Lists are device int32 [n]; a negative entry is left out, a list names no sequence twice
+ * (a second time is left out and sets AVSA_ERR_BAD_TABLE; for avsa_cache_free it is empty by then).  Free pages are taken from the lowest on, in the order of the list, and
+ * what cannot be had leaves its sequence as it was and sets AVSA_ERR_NO_PAGES.  Every call sees the state before it.
+ *
+ * avsa_cache_extend   room for count[k] more tokens (>= 0) in sequence seq[k]: new pages where its last one does not
+ *                     hold them, length += count[k].
+ * avsa_cache_write    the last count[k] tokens of sequence seq[k] (seq NULL: k, count NULL: L) from k_new and v_new
+ *                     [n,Hkv,L,d], of which they are the first count[k] (0..L), into the pages.  Tokens whose page is missing are left out.
+ * avsa_cache_fork     sequence child[k], which has to be empty, becomes a copy of parent[k]: it shares the pages that are full, and the
+ *                     contents of the one that is not are copied to a page of its own, in all planes of `pool`.
+ * avsa_cache_free     sequence seq[k] gives its pages back and is empty (all that its row of the table names; `page` is not looked at).
+ * avsa_cache_compact  the pages in use become the first n_live[0] ones: the k-th of those behind moves to the k-th free place among them.
+ *
+ * All need the workspace but avsa_cache_write, which has none and no status record.
+ */
+AVSA_API int avsa_cache_extend(avsa_cache c, const int32_t* seq, const int32_t* count, int n, void* ws, size_t ws_bytes, void* stream);
+AVSA_API int avsa_cache_write(int n, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d k_new,
+                              avsa_bf16_4d v_new, avsa_bf16_4d k_pool, avsa_bf16_4d v_pool, const int32_t* table,
+                              const int32_t* length, const int32_t* seq, const int32_t* count, void* stream);
+AVSA_API int avsa_cache_fork(avsa_cache c, avsa_pages pool, const int32_t* parent, const int32_t* child, int n, void* ws, size_t ws_bytes,
+                             void* stream);
+AVSA_API int avsa_cache_free(avsa_cache c, const int32_t* seq, int n, void* ws, size_t ws_bytes, void* stream);
+AVSA_API int avsa_cache_compact(avsa_cache c, avsa_pages pool, int32_t* n_live, void* ws, size_t ws_bytes, void* stream);
+AVSA_API size_t avsa_cache_workspace_bytes(int seqs, int pages, int n);
+
 /* Host integer ceil(pct/100 * n): the count forms of rho and kappa (Eq. 8's ceiling). */
 AVSA_API int avsa_count_from_percent(int pct, int n);
 
 /* Synchronises `stream`, copies the status record of `ws` to the host and returns its code
- * (AVSA_OK, AVSA_ERR_TIMEOUT or AVSA_ERR_BAD_MASK).  detail (host, optional) receives 3 ints that
+ * (AVSA_OK, AVSA_ERR_TIMEOUT, AVSA_ERR_BAD_MASK, AVSA_ERR_BAD_TABLE or AVSA_ERR_NO_PAGES).  detail (host, optional) receives 3 ints that
  * say where the check failed.  For tests and debugging; the hot path never calls it. */
 AVSA_API int avsa_read_status(const void* ws, void* stream, int* detail);
 

@@ -27,12 +27,16 @@ AVSA_ERR_WORKSPACE = 3
 AVSA_ERR_CUDA = 4
 AVSA_ERR_TIMEOUT = 5
 AVSA_ERR_BAD_MASK = 6
+AVSA_ERR_BAD_TABLE = 7
+AVSA_ERR_NO_PAGES = 8
 
 AVSA_PROTECT_ROWS = 1
 AVSA_PROTECT_COLS = 2
 AVSA_USE_GIVEN_BLOCK_SCORES = 4
 AVSA_PROTECT_TOKENS = 8
 AVSA_PROTECT_BLOCK_SUM = 16
+
+AVSA_CAUSAL = 1
 
 
 def AVSA_MIN_TOKENS_PER_BLOCK(n: int) -> int:
@@ -46,6 +50,8 @@ EXPORTS = (
     "avsa_sparse_self_attn", "avsa_sparse_self_attn_workspace_bytes",
     "avsa_protected_rows_attn", "avsa_protected_rows_attn_workspace_bytes",
     "avsa_cache_indicators", "avsa_cache_indicators_workspace_bytes",
+    "avsa_prefix_attn", "avsa_prefix_attn_workspace_bytes",
+    "avsa_cache_extend", "avsa_cache_write", "avsa_cache_fork", "avsa_cache_free", "avsa_cache_compact", "avsa_cache_workspace_bytes",
     "avsa_count_from_percent", "avsa_read_status", "avsa_selftest_bounded_wait", "avsa_status_string", "avsa_version",
 )
 
@@ -61,9 +67,20 @@ class _Bf16Tensor4(ctypes.Structure):
                 ("stride_n", ctypes.c_int64)]
 
 
+class _Cache(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("table", "length", "ref", "table_out", "length_out", "ref_out")] + \
+               [(name, ctypes.c_int) for name in ("seqs", "width", "pages", "page")]
+
+
+class _Pages(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("planes", ctypes.c_int), ("page_bytes", ctypes.c_int64), ("stride_plane", ctypes.c_int64),
+                ("stride_page", ctypes.c_int64)]
+
+
 _lib = None
 _host_module = None
 _alloc_module = None
+_cache_module = None
 
 
 def _extension(name: str):
@@ -107,6 +124,20 @@ def _alloc():
     return _alloc_module
 
 
+def _cache():
+    """The extension module that makes the paged cache's calls, bound to the loaded library."""
+    global _cache_module
+    if _cache_module is None:
+        lib = load_library()
+        module = _extension("_avsa_cache")
+        entries = ("avsa_prefix_attn", "avsa_prefix_attn_workspace_bytes", "avsa_cache_extend", "avsa_cache_write", "avsa_cache_fork",
+                   "avsa_cache_free", "avsa_cache_compact", "avsa_cache_workspace_bytes")
+        module.bind(*(ctypes.cast(getattr(lib, e), ctypes.c_void_p).value for e in entries),
+                    getattr(torch._C, "_cuda_getCurrentRawStream", None))
+        _cache_module = module
+    return _cache_module
+
+
 def load_library() -> ctypes.CDLL:
     """Loads libavsa.so (built in-tree by ``build.py``) and declares the prototypes."""
     global _lib
@@ -140,6 +171,22 @@ def load_library() -> ctypes.CDLL:
     lib.avsa_cache_indicators.restype = i
     lib.avsa_cache_indicators_workspace_bytes.argtypes = [i, i, i, i]
     lib.avsa_cache_indicators_workspace_bytes.restype = sz
+    lib.avsa_prefix_attn.argtypes = [i, i, i, i, i, i, i, i, i, T, T, T, vp, vp, vp, i, u, f, vp, vp, vp, sz, vp]
+    lib.avsa_prefix_attn.restype = i
+    lib.avsa_prefix_attn_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
+    lib.avsa_prefix_attn_workspace_bytes.restype = sz
+    lib.avsa_cache_extend.argtypes = [_Cache, vp, vp, i, vp, sz, vp]
+    lib.avsa_cache_extend.restype = i
+    lib.avsa_cache_write.argtypes = [i, i, i, i, i, i, i, i, T, T, T, T, vp, vp, vp, vp, vp]
+    lib.avsa_cache_write.restype = i
+    lib.avsa_cache_fork.argtypes = [_Cache, _Pages, vp, vp, i, vp, sz, vp]
+    lib.avsa_cache_fork.restype = i
+    lib.avsa_cache_free.argtypes = [_Cache, vp, i, vp, sz, vp]
+    lib.avsa_cache_free.restype = i
+    lib.avsa_cache_compact.argtypes = [_Cache, _Pages, vp, vp, sz, vp]
+    lib.avsa_cache_compact.restype = i
+    lib.avsa_cache_workspace_bytes.argtypes = [i, i, i]
+    lib.avsa_cache_workspace_bytes.restype = sz
     lib.avsa_count_from_percent.argtypes = [i, i]
     lib.avsa_count_from_percent.restype = i
     lib.avsa_read_status.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_int)]
@@ -418,3 +465,67 @@ def avsa_cache_indicators(y_v, yhat_v, y_a, yhat_a, prot_tok=None, s_cur=None, s
     if st != AVSA_OK:
         raise AvsaError(st, "avsa_cache_indicators")
     return out, ws
+
+
+# ------------------------------------------------------------------------------------------------
+# paged cache
+# ------------------------------------------------------------------------------------------------
+def avsa_prefix_attn_workspace_bytes(B, H, Hkv, L, d, page, width, prefix_pages) -> int:
+    return int(load_library().avsa_prefix_attn_workspace_bytes(B, H, Hkv, L, d, page, width, prefix_pages))
+
+
+def avsa_prefix_attn(q, k_pool, v_pool, table, length, prefix_pages=0, seq=None, causal=False, softmax_scale=0.0, want_lse=False,
+                     o=None, lse=None, ws=None):
+    """Attention of q [B,H,L,d] to the paged sequences seq (None: 0 .. B-1), whose first prefix_pages pages are the same ones.
+
+    k_pool/v_pool [pages,Hkv,page,d] bf16, table [seqs,width] and length [seqs] int32.  causal: the queries are the last L tokens of
+    their sequence.  Returns (o, lse or None, ws)."""
+    done = (_cache_module or _cache()).attn(q, k_pool, v_pool, table, length, prefix_pages, seq, causal, softmax_scale, want_lse, o, lse, ws)
+    if done[0] != AVSA_OK:
+        raise AvsaError(done[0], "avsa_prefix_attn")
+    return done[1:]
+
+
+def avsa_cache_workspace_bytes(seqs, pages, n) -> int:
+    return int(load_library().avsa_cache_workspace_bytes(seqs, pages, n))
+
+
+def avsa_cache_extend(table, length, ref, seq, count, page, out=None, ws=None):
+    """Room for count[k] more tokens in sequence seq[k].  out: (table, length, ref) that the state behind the call goes to (None: in place).
+    Returns (table, length, ref, ws)."""
+    done = (_cache_module or _cache()).extend(table, length, ref, seq, count, page, *(out or (None, None, None)), ws)
+    if done[0] != AVSA_OK:
+        raise AvsaError(done[0], "avsa_cache_extend")
+    return done[1:]
+
+
+def avsa_cache_write(k_new, v_new, k_pool, v_pool, table, length, seq=None, count=None):
+    """The first count[k] (None: all L) tokens of k_new/v_new [n,Hkv,L,d] become the last ones of sequence seq[k] (None: k)."""
+    st = (_cache_module or _cache()).write(k_new, v_new, k_pool, v_pool, table, length, seq, count)
+    if st != AVSA_OK:
+        raise AvsaError(st, "avsa_cache_write")
+
+
+def avsa_cache_fork(pool, table, length, ref, parent, child, out=None, ws=None):
+    """Sequence child[k], which is empty, becomes a copy of parent[k] that shares its full pages.  pool [planes,pages,Hkv,page,d].
+    Returns (table, length, ref, ws)."""
+    done = (_cache_module or _cache()).fork(pool, table, length, ref, parent, child, *(out or (None, None, None)), ws)
+    if done[0] != AVSA_OK:
+        raise AvsaError(done[0], "avsa_cache_fork")
+    return done[1:]
+
+
+def avsa_cache_free(table, length, ref, seq, out=None, ws=None):
+    """Sequence seq[k] gives its pages back.  Returns (table, length, ref, ws)."""
+    done = (_cache_module or _cache()).free(table, length, ref, seq, *(out or (None, None, None)), ws)
+    if done[0] != AVSA_OK:
+        raise AvsaError(done[0], "avsa_cache_free")
+    return done[1:]
+
+
+def avsa_cache_compact(pool, table, length, ref, out=None, n_live=None, ws=None):
+    """The pages in use become the first ones of the pool.  Returns (n_live int32 [1], ws)."""
+    done = (_cache_module or _cache()).compact(pool, table, length, ref, *(out or (None, None, None)), n_live, ws)
+    if done[0] != AVSA_OK:
+        raise AvsaError(done[0], "avsa_cache_compact")
+    return done[1:]

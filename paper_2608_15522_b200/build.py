@@ -1,4 +1,4 @@
-"""Builds libavsa.so and the two host extensions of its binding in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
+"""Builds libavsa.so and the three host extensions of its binding in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
 from __future__ import annotations
 
 import os
@@ -12,8 +12,9 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libavsa.so")
 HOST = os.path.join(HERE, "_avsa_host" + sysconfig.get_config_var("EXT_SUFFIX"))      # marshalling for this interpreter
 ALLOC = os.path.join(HERE, "_avsa_alloc" + sysconfig.get_config_var("EXT_SUFFIX"))    # tensors for the wrappers
-ALLOC_FOR = os.path.join(HERE, "build", "alloc_built_for.txt")      # the PyTorch that ALLOC was compiled against
-SOURCES = ["api.cu", "mask.cu", "sparse_attn.cu", "cross_attn.cu", "protected_rows.cu", "cache_indicators.cu"]
+CACHE = os.path.join(HERE, "_avsa_cache" + sysconfig.get_config_var("EXT_SUFFIX"))    # the paged cache's calls
+ALLOC_FOR = os.path.join(HERE, "build", "alloc_built_for.txt")      # the PyTorch that ALLOC and CACHE were compiled against
+SOURCES = ["api.cu", "mask.cu", "sparse_attn.cu", "cross_attn.cu", "protected_rows.cu", "cache_indicators.cu", "paged_cache.cu", "prefix_attn.cu"]
 HEADERS = sorted(f for f in os.listdir(CSRC) if f.endswith(".cuh")) + [os.path.join("..", "..", "include", "avsa.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]
@@ -27,36 +28,36 @@ def _nvcc() -> str:
 
 
 def _torch_abi() -> str:
-    """What the allocating extension is bound to besides its source."""
+    """What the extensions that allocate are bound to besides their sources."""
     import torch
     return f"torch {torch.__version__} cxx11 abi {int(torch.compiled_with_cxx11_abi())}"
 
 
 def _stale() -> bool:
-    outputs = (LIB, HOST, ALLOC)
+    outputs = (LIB, HOST, ALLOC, CACHE)
     if not all(os.path.exists(o) for o in outputs + (ALLOC_FOR,)):
         return True
     with open(ALLOC_FOR) as f:
         if f.read() != _torch_abi():
             return True
     t = min(os.path.getmtime(o) for o in outputs)
-    deps = [os.path.join(CSRC, s) for s in SOURCES + HEADERS + ["host_call.cc", "host_alloc.cc"]]
+    deps = [os.path.join(CSRC, s) for s in SOURCES + HEADERS + ["host_call.cc", "host_alloc.cc", "host_cache.cc"]]
     return any(os.path.getmtime(p) > t for p in deps)
 
 
 def _start_host_builds():
-    """g++ on the two host extensions: (source, process) each."""
+    """g++ on the host extensions: (source, process) each."""
     import torch
     base = torch.__path__[0]
     include = [os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include")]
     common = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-I" + sysconfig.get_paths()["include"]]
     host = common + ["-Wall", "-Wno-cast-function-type", os.path.join(CSRC, "host_call.cc"), "-o", HOST]
-    alloc = common + [f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"]
-    alloc += [flag for path in include for flag in ("-isystem", path)]
-    alloc += [os.path.join(CSRC, "host_alloc.cc"), "-o", ALLOC, "-L" + os.path.join(base, "lib"),
-              "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10"]
-    return [(name, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
-            for name, cmd in (("host_call.cc", host), ("host_alloc.cc", alloc))]
+    torch_flags = [f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"] + [f for path in include for f in ("-isystem", path)]
+    torch_libs = ["-L" + os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10"]
+    cmds = [("host_call.cc", host)]
+    for source, out in (("host_alloc.cc", ALLOC), ("host_cache.cc", CACHE)):
+        cmds.append((source, common + torch_flags + [os.path.join(CSRC, source), "-o", out] + torch_libs))
+    return [(name, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)) for name, cmd in cmds]
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:

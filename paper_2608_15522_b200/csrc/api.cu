@@ -144,6 +144,8 @@ const char* avsa_status_string(int status) {
     case AVSA_ERR_CUDA: return "CUDA call failed";
     case AVSA_ERR_TIMEOUT: return "device-side wait timed out";
     case AVSA_ERR_BAD_MASK: return "malformed column list";
+    case AVSA_ERR_BAD_TABLE: return "malformed page table, length or sequence list";
+    case AVSA_ERR_NO_PAGES: return "no free page, or no room in the page table";
     default: return "unknown status";
   }
 }

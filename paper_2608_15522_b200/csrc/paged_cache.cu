@@ -1,0 +1,669 @@
+// Changes of a paged K/V cache: room for more tokens, new tokens into the pages, branches, pages given back, compaction.
+//
+// What a call decides (which page goes where) is a few thousand integers: one kernel, a cluster of CTAs on one GPC, whose steps are
+// separated by cluster barriers instead of launches (about 0.5 us each against 2-3).  What it moves (page contents) is
+// a second kernel over the whole GPU behind it, bound by HBM: every byte read once and written once.
+//
+// Free pages are those with ref == 0; they are taken in ascending order, so that a result is determined by the state alone and what
+// is in use stays low in the pool.
+#include <climits>
+
+#include "avsa_common.cuh"
+#include "sm100_ptx.cuh"
+
+namespace avsa {
+
+constexpr int kMetaThreads = 1024, kMetaWarps = kMetaThreads / 32;
+// CTAs of the cluster: one as long as it has no more than this many integers to look at or copy, else the portable maximum.
+constexpr int kMetaCluster = 8;
+constexpr long long kMetaSingle = 16384;
+
+enum CacheWhere { kCacheSeq = 201, kCacheTwice, kCacheLength, kCachePage, kCacheRef, kCacheFull, kCacheChild };
+
+// One entry of a call's list, decided by the first CTA: sequences, what they hold, and where their free pages begin.
+struct ListEntry {
+  int seq, other;       // other: fork's parent; seq < 0: left out
+  int tokens, new_tokens;
+  int first, need;      // free pages [first, first + need) of the list of free pages
+  int pad[2];
+};
+static_assert(sizeof(ListEntry) == 32, "two 16-byte accesses");
+
+// A workspace: status record | counts of the CTAs | claims [seqs] | list entries [n] | free pages [pages] | moves [max(n, pages)] int4
+struct CacheWs {
+  StatusRecord* status;
+  int* counts;       // [3][kMetaCluster], then [62] free pages / moves in all, [63] needed pages in all
+  int* claims;
+  ListEntry* list;
+  int* free_pages;
+  int4* moves;       // from, to, ref
+  static size_t bytes(int seqs, int pages, int n) {
+    const size_t m = static_cast<size_t>(n > pages ? n : pages);
+    return kStatusBytes + 256 + align_up(static_cast<size_t>(seqs) * 4, 256) + align_up(static_cast<size_t>(n) * sizeof(ListEntry), 256) +
+           align_up(static_cast<size_t>(pages) * 4, 256) + align_up(m * sizeof(int4), 256);
+  }
+  CacheWs(void* ws, int seqs, int pages, int n) {
+    uint8_t* p = static_cast<uint8_t*>(ws);
+    status = reinterpret_cast<StatusRecord*>(p);
+    counts = reinterpret_cast<int*>(p + kStatusBytes);
+    p += kStatusBytes + 256;
+    claims = reinterpret_cast<int*>(p);
+    p += align_up(static_cast<size_t>(seqs) * 4, 256);
+    list = reinterpret_cast<ListEntry*>(p);
+    p += align_up(static_cast<size_t>(n) * sizeof(ListEntry), 256);
+    free_pages = reinterpret_cast<int*>(p);
+    p += align_up(static_cast<size_t>(pages) * 4, 256);
+    moves = reinterpret_cast<int4*>(p);
+  }
+};
+constexpr int kNumMoves = 62, kNumNeeded = 63;
+
+struct MetaArgs {
+  avsa_cache c;
+  CacheWs w;
+  const int32_t* seq;       // extend, free; fork: child
+  const int32_t* other;     // extend: count; fork: parent
+  int n;
+  int32_t* n_live;
+};
+
+__device__ __forceinline__ int cluster_rank() {
+  int r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ int cluster_size() {
+  int r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ unsigned lanes_below() {
+  unsigned m;
+  asm volatile("mov.u32 %0, %%lanemask_lt;" : "=r"(m));
+  return m;
+}
+
+// Sum over the CTA, for every thread.  `sm`: kMetaWarps ints; a barrier has to lie between two uses.
+__device__ __forceinline__ int block_sum(int v, int* sm) {
+  v = __reduce_add_sync(0xffffffffu, v);
+  if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
+  __syncthreads();
+  return __reduce_add_sync(0xffffffffu, sm[threadIdx.x & 31]);
+}
+// Sum of the threads before this one, and of all; the same conditions.
+__device__ __forceinline__ int block_scan(int v, int& all, int* sm) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int inc = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int o = __shfl_up_sync(0xffffffffu, inc, d);
+    if (lane >= d) inc += o;
+  }
+  if (lane == 31) sm[warp] = inc;
+  __syncthreads();
+  const int mine = sm[lane];
+  all = __reduce_add_sync(0xffffffffu, mine);
+  return __reduce_add_sync(0xffffffffu, lane < warp ? mine : 0) + inc - v;
+}
+
+constexpr int kVals = 8;      // values a thread has in flight in the passes over `ref`
+
+// Calls emit(index, value, rank) for the indices of [lo, hi) whose value is taken, in ascending order from rank `base` on.
+template <class Take, class Emit>
+__device__ __forceinline__ void for_taken(const int32_t* v, int lo, int hi, int base, Take take, Emit emit, int* sm) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int t0 = lo; t0 < hi; t0 += kMetaThreads * kVals) {
+    int x[kVals];
+    unsigned m[kVals];
+#pragma unroll
+    for (int i = 0; i < kVals; i++) {
+      const int at = t0 + i * kMetaThreads + threadIdx.x;
+      x[i] = at < hi ? v[at] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < kVals; i++) {
+      const int at = t0 + i * kMetaThreads + threadIdx.x;
+      m[i] = __ballot_sync(0xffffffffu, at < hi && take(at, x[i]));
+      if (lane == 0) sm[i * 32 + warp] = __popc(m[i]);
+    }
+    __syncthreads();
+    // every warp sums what lies before it itself: the counts of 32 warps are one load
+    int before = base;
+#pragma unroll
+    for (int i = 0; i < kVals; i++) {
+      const int c = sm[i * 32 + lane];
+      const int mine = before + __reduce_add_sync(0xffffffffu, lane < warp ? c : 0);
+      const int at = t0 + i * kMetaThreads + threadIdx.x;
+      if ((m[i] >> lane) & 1u) emit(at, x[i], mine + __popc(m[i] & lanes_below()));
+      before += __reduce_add_sync(0xffffffffu, c);
+    }
+    base = before;
+    __syncthreads();
+  }
+}
+template <class Take>
+__device__ __forceinline__ int count_taken(const int32_t* v, int lo, int hi, Take take, int* sm) {
+  int n = 0;
+  for (int t0 = lo + threadIdx.x; t0 < hi; t0 += kMetaThreads * kVals) {
+    int x[kVals];
+#pragma unroll
+    for (int i = 0; i < kVals; i++) x[i] = t0 + i * kMetaThreads < hi ? v[t0 + i * kMetaThreads] : 0;
+#pragma unroll
+    for (int i = 0; i < kVals; i++) n += t0 + i * kMetaThreads < hi && take(t0 + i * kMetaThreads, x[i]);
+  }
+  const int all = block_sum(n, sm);
+  __syncthreads();
+  return all;
+}
+
+// The cluster's share of an array copied to another, if it is another.
+__device__ __forceinline__ void copy_ints(const int32_t* from, int32_t* to, long long n, int rank, int ctas) {
+  if (from == to) return;
+  const long long step = static_cast<long long>(ctas) * kMetaThreads;
+  for (long long i = static_cast<long long>(rank) * kMetaThreads + threadIdx.x; i < n; i += step * 4) {
+    int x[4];
+#pragma unroll
+    for (int u = 0; u < 4; u++)
+      if (i + u * step < n) x[u] = from[i + u * step];
+#pragma unroll
+    for (int u = 0; u < 4; u++)
+      if (i + u * step < n) to[i + u * step] = x[u];
+  }
+}
+__device__ __forceinline__ void copy_state(const avsa_cache& c, int rank, int ctas) {
+  copy_ints(c.table, c.table_out, static_cast<long long>(c.seqs) * c.width, rank, ctas);
+  copy_ints(c.length, c.length_out, c.seqs, rank, ctas);
+  copy_ints(c.ref, c.ref_out, c.pages, rank, ctas);
+}
+__device__ __forceinline__ void clear_status(StatusRecord* st) {
+  st->code = st->where = st->item = st->aux = st->redo_count = st->next_item = 0;
+}
+__device__ __forceinline__ void page_share(const avsa_cache& c, int rank, int ctas, int& lo, int& hi) {
+  const int part = (c.pages + ctas - 1) / ctas;
+  lo = min(c.pages, rank * part);
+  hi = min(c.pages, lo + part);
+}
+
+enum { kExtend = 0, kFork = 1 };
+
+// extend and fork: which free pages go to which sequence.
+template <int OP>
+__global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const MetaArgs a) {
+  __shared__ int sm[kVals * 32];
+  pdl_wait();
+  pdl_launch();
+  const avsa_cache& c = a.c;
+  const CacheWs& w = a.w;
+  const int rank = cluster_rank(), ctas = cluster_size(), tid = threadIdx.x, lane = tid & 31;
+  if (rank == 0 && tid == 0) clear_status(w.status);
+  copy_state(c, rank, ctas);
+  int lo, hi;
+  page_share(c, rank, ctas, lo, hi);
+  {
+    const int mine = count_taken(c.ref, lo, hi, [](int, int r) { return r <= 0; }, sm);
+    if (tid == 0) w.counts[rank] = mine;
+  }
+  if (rank == 0) {
+    // the list: entries that name a sequence again lose to the first one
+    for (int k = tid; k < a.n; k += kMetaThreads) {
+      const int s = a.seq[k];
+      if (s >= 0 && s < c.seqs) w.claims[s] = INT_MAX;
+    }
+    __syncthreads();
+    for (int k = tid; k < a.n; k += kMetaThreads) {
+      const int s = a.seq[k];
+      if (s >= 0 && s < c.seqs) atomicMin(&w.claims[s], k);
+    }
+    __syncthreads();
+    int taken = 0;
+    for (int k0 = 0; k0 < a.n; k0 += kMetaThreads) {
+      const int k = k0 + tid;
+      ListEntry e = {};
+      e.seq = -1;
+      if (k < a.n) {
+        const int s = a.seq[k], o = a.other[k];
+        int bad = 0, code = AVSA_ERR_BAD_TABLE;
+        if (s >= 0 && (OP == kExtend || o >= 0)) {
+          if (s >= c.seqs || (OP == kFork && o >= c.seqs)) bad = kCacheSeq;
+          else if (__ldcg(&w.claims[s]) != k) bad = kCacheTwice;
+          else {
+            const int n = c.length[OP == kFork ? o : s];
+            const long long room = static_cast<long long>(c.width) * c.page;
+            if (n < 0 || n > room || (OP == kExtend && o < 0)) bad = kCacheLength;
+            else if (OP == kFork && c.length[s] != 0) bad = kCacheChild;
+            else if (OP == kExtend && n + static_cast<long long>(o) > room) bad = kCacheFull, code = AVSA_ERR_NO_PAGES;
+            else {
+              e.seq = s;
+              e.other = o;
+              e.tokens = n;
+              if (OP == kExtend) {
+                e.new_tokens = o;
+                e.need = (n + o + c.page - 1) / c.page - (n + c.page - 1) / c.page;
+              } else {
+                e.need = n % c.page != 0;
+              }
+            }
+          }
+        }
+        if (bad) report_status(w.status, code, bad, k, s);
+      }
+      int all;
+      e.first = taken + block_scan(e.need, all, sm);
+      taken += all;
+      if (k < a.n) w.list[k] = e;
+      __syncthreads();
+    }
+    if (tid == 0) w.counts[kNumNeeded] = taken;
+  }
+  cluster_sync_all();
+  const int needed = __ldcg(&w.counts[kNumNeeded]);
+  int base = 0, n_free = 0;
+  for (int r = 0; r < ctas; r++) {
+    const int m = __ldcg(&w.counts[r]);
+    if (r < rank) base += m;
+    n_free += m;
+  }
+  if (base < needed) {      // (uniform over the CTA)
+    // (ref has not been written yet: in place it is still the state before the call)
+    for_taken(c.ref, lo, hi, base, [](int, int r) { return r <= 0; },
+              [&](int page, int, int at) { if (at < needed) w.free_pages[at] = page; }, sm);
+  }
+  cluster_sync_all();
+  const int warps = ctas * kMetaWarps;
+  for (int k = rank * kMetaWarps + (tid >> 5); k < a.n; k += warps) {      // a warp to an entry
+    const int4 e0 = __ldcg(reinterpret_cast<const int4*>(&w.list[k])), e1 = __ldcg(reinterpret_cast<const int4*>(&w.list[k]) + 1);
+    const int s = e0.x, other = e0.y, tokens = e0.z, new_tokens = e0.w, first = e1.x, need = e1.y;
+    const bool refused = s >= 0 && need > 0 && first + need > n_free;
+    if (refused && lane == 0) report_status(w.status, AVSA_ERR_NO_PAGES, kCacheFull, k, s);
+    if (OP == kFork && lane == 0 && (s < 0 || refused || need == 0)) w.moves[k] = make_int4(-1, -1, 0, 0);
+    if (s < 0 || refused) continue;
+    int32_t* row = c.table_out + static_cast<long long>(s) * c.width;
+    if (OP == kExtend) {
+      const int have = (tokens + c.page - 1) / c.page;
+      for (int j = lane; j < need; j += 32) {
+        const int page = __ldcg(&w.free_pages[first + j]);
+        row[have + j] = page;
+        c.ref_out[page] = 1;
+      }
+      if (lane == 0) c.length_out[s] = tokens + new_tokens;
+    } else {
+      const int whole = tokens / c.page;
+      const int32_t* from = c.table + static_cast<long long>(other) * c.width;
+      for (int j = lane; j < c.width; j += 32) {
+        int page = -1;
+        if (j < whole) {
+          page = from[j];
+          if (page >= 0 && page < c.pages) {
+            atomicAdd(&c.ref_out[page], 1);
+          } else {
+            report_status(w.status, AVSA_ERR_BAD_TABLE, kCachePage, other, j);
+          }
+        } else if (j == whole && need) {
+          page = __ldcg(&w.free_pages[first]);
+          c.ref_out[page] = 1;
+          const int src = from[j];
+          const bool good = src >= 0 && src < c.pages;
+          w.moves[k] = good ? make_int4(src, page, 1, 0) : make_int4(-1, -1, 0, 0);
+          if (!good) report_status(w.status, AVSA_ERR_BAD_TABLE, kCachePage, other, j);
+        }
+        row[j] = page;
+      }
+      if (lane == 0) c.length_out[s] = tokens;
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kMetaThreads, 1) free_pages_kernel(const MetaArgs a) {
+  pdl_wait();
+  pdl_launch();
+  const avsa_cache& c = a.c;
+  const int rank = cluster_rank(), ctas = cluster_size(), tid = threadIdx.x, lane = tid & 31;
+  if (rank == 0 && tid == 0) clear_status(a.w.status);
+  copy_state(c, rank, ctas);
+  cluster_sync_all();
+  for (int k = rank * kMetaWarps + (tid >> 5); k < a.n; k += ctas * kMetaWarps) {
+    const int s = a.seq[k];
+    if (s < 0) continue;
+    if (s >= c.seqs) {
+      if (lane == 0) report_status(a.w.status, AVSA_ERR_BAD_TABLE, kCacheSeq, k, s);
+      continue;
+    }
+    // whoever takes an entry of the row gives its page back: a sequence that is listed again has none left by then
+    int32_t* row = c.table_out + static_cast<long long>(s) * c.width;
+    for (int j = lane; j < c.width; j += 32) {
+      const int page = atomicExch(&row[j], -1);
+      if (page == -1) continue;
+      if (page < -1 || page >= c.pages) report_status(a.w.status, AVSA_ERR_BAD_TABLE, kCachePage, s, j);
+      else if (atomicSub(&c.ref_out[page], 1) <= 0) report_status(a.w.status, AVSA_ERR_BAD_TABLE, kCacheRef, s, page);
+    }
+    if (lane == 0) c.length_out[s] = 0;
+  }
+}
+
+// Which pages move, and the references behind the moves.  Both lists are ascending, so the k-th move is known from the k-th
+// free place below n_live and the k-th page in use from n_live on.
+__global__ void __launch_bounds__(kMetaThreads, 1) plan_compaction_kernel(const MetaArgs a) {
+  __shared__ int sm[kVals * 32];
+  pdl_wait();
+  pdl_launch();
+  const avsa_cache& c = a.c;
+  const CacheWs& w = a.w;
+  const int rank = cluster_rank(), ctas = cluster_size(), tid = threadIdx.x;
+  if (rank == 0 && tid == 0) clear_status(w.status);
+  copy_ints(c.length, c.length_out, c.seqs, rank, ctas);
+  int lo, hi;
+  page_share(c, rank, ctas, lo, hi);
+  const int mine = count_taken(c.ref, lo, hi, [](int, int r) { return r > 0; }, sm);
+  if (tid == 0) w.counts[rank] = mine;
+  cluster_sync_all();
+  int n_live = 0;
+  for (int r = 0; r < ctas; r++) n_live += __ldcg(&w.counts[r]);
+  const int holes = count_taken(c.ref, lo, min(hi, n_live), [](int, int r) { return r <= 0; }, sm);
+  // (pages in use from n_live on: all in use but those below n_live)
+  const int below = max(0, min(hi, n_live) - lo) - holes;
+  if (tid == 0) {
+    w.counts[kMetaCluster + rank] = holes;
+    w.counts[2 * kMetaCluster + rank] = mine - below;
+    if (rank == 0) a.n_live[0] = n_live;
+  }
+  cluster_sync_all();
+  int hole0 = 0, move0 = 0, n_moves = 0;
+  for (int r = 0; r < ctas; r++) {
+    const int h = __ldcg(&w.counts[kMetaCluster + r]), m = __ldcg(&w.counts[2 * kMetaCluster + r]);
+    if (r < rank) hole0 += h, move0 += m;
+    n_moves += h;
+  }
+  if (rank == 0 && tid == 0) w.counts[kNumMoves] = n_moves;
+  int* const move_words = reinterpret_cast<int*>(w.moves);
+  for_taken(c.ref, lo, min(hi, n_live), hole0, [](int, int r) { return r <= 0; },
+            [&](int page, int, int at) { move_words[4 * at + 1] = page; }, sm);
+  for_taken(c.ref, max(lo, min(hi, n_live)), hi, move0, [](int, int r) { return r > 0; },
+            [&](int page, int r, int at) {
+              move_words[4 * at] = page;
+              move_words[4 * at + 2] = r;
+            }, sm);
+  __syncthreads();
+  for (int p = lo + tid; p < hi; p += kMetaThreads) {
+    const int r = c.ref[p];
+    if (p >= n_live) {
+      c.ref_out[p] = 0;
+      w.free_pages[p] = -1;
+    } else if (r > 0) {
+      c.ref_out[p] = r;
+    }
+  }
+  cluster_sync_all();
+  // free_pages[p] is where page p >= n_live has gone, -1 for one that was not in use
+  for (int k = rank * kMetaThreads + tid; k < n_moves; k += ctas * kMetaThreads) {
+    const int4 m = __ldcg(&w.moves[k]);
+    c.ref_out[m.y] = m.z;
+    w.free_pages[m.x] = m.y;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ page contents
+constexpr int kCopyThreads = 256, kCopyVecs = 4;
+constexpr int kCopyChunk = kCopyThreads * kCopyVecs * 16;      // bytes a CTA moves at a time
+
+struct CopyArgs {
+  avsa_pages pool;
+  const int4* moves;
+  const int* n_moves;       // or NULL: n
+  int n;
+  // compaction: the table's pages by their new numbers
+  const int32_t* table;
+  int32_t* table_out;
+  const int32_t* place;
+  const int32_t* n_live;
+  int seqs, width, pages, page;
+  StatusRecord* status;
+};
+
+__global__ void __launch_bounds__(kCopyThreads) move_pages_kernel(const CopyArgs a) {
+  pdl_wait();
+  pdl_launch();
+  const int tid = threadIdx.x;
+  if (a.table != nullptr) {
+    const int n_live = a.n_live[0];
+    const long long entries = static_cast<long long>(a.seqs) * a.width;
+    for (long long i = static_cast<long long>(blockIdx.x) * kCopyThreads + tid; i < entries; i += static_cast<long long>(gridDim.x) * kCopyThreads) {
+      const int page = a.table[i];
+      int to = page;
+      bool bad = page >= a.pages || page < -1;
+      if (!bad && page >= n_live) {
+        to = a.place[page];
+        bad = to < 0;
+      }
+      if (bad) report_status(a.status, AVSA_ERR_BAD_TABLE, kCachePage, static_cast<int>(i / a.width), static_cast<int>(i % a.width));
+      if (a.table != a.table_out || to != page) a.table_out[i] = to;
+    }
+  }
+  const int n = a.n_moves != nullptr ? a.n_moves[0] : a.n;
+  const long long chunks = (a.pool.page_bytes + kCopyChunk - 1) / kCopyChunk;
+  const long long total = static_cast<long long>(n) * a.pool.planes * chunks;
+  for (long long u = blockIdx.x; u < total; u += gridDim.x) {
+    const long long r = u / chunks;
+    const int chunk = static_cast<int>(u - r * chunks), plane = static_cast<int>(r % a.pool.planes), k = static_cast<int>(r / a.pool.planes);
+    const int4 m = a.moves[k];
+    if (m.x < 0) continue;
+    uint8_t* const base = static_cast<uint8_t*>(a.pool.ptr) + plane * a.pool.stride_plane;
+    const long long at = static_cast<long long>(chunk) * kCopyChunk + tid * 16;
+    const uint4* const from = reinterpret_cast<const uint4*>(base + m.x * a.pool.stride_page + at);
+    uint4* const to = reinterpret_cast<uint4*>(base + m.y * a.pool.stride_page + at);
+    uint4 x[kCopyVecs];
+#pragma unroll
+    for (int i = 0; i < kCopyVecs; i++)
+      if (at + i * kCopyThreads * 16 < a.pool.page_bytes) x[i] = __ldcs(from + i * kCopyThreads);
+#pragma unroll
+    for (int i = 0; i < kCopyVecs; i++)
+      if (at + i * kCopyThreads * 16 < a.pool.page_bytes) __stcs(to + i * kCopyThreads, x[i]);
+  }
+}
+
+struct WriteArgs {
+  avsa_bf16_4d k_new, v_new, k_pool, v_pool;
+  const int32_t *table, *length, *seq, *count;
+  int Hkv, L, vecs;       // vecs: 16-byte vectors of a token's row of one head
+  int page, pages, seqs, width, tokens;      // tokens: of one CTA
+};
+
+// A CTA takes `tokens` tokens of one list entry; neighbouring threads take neighbouring vectors of a token's heads.
+__global__ void __launch_bounds__(kCopyThreads) write_tokens_kernel(const WriteArgs a) {
+  pdl_wait();
+  pdl_launch();
+  const int k = blockIdx.y;
+  const int s = a.seq != nullptr ? a.seq[k] : k;
+  if (s < 0 || s >= a.seqs) return;
+  const int count = a.count != nullptr ? min(a.count[k], a.L) : a.L;
+  const int t0 = blockIdx.x * a.tokens, t1 = min(count, t0 + a.tokens);
+  if (t0 >= t1) return;
+  const long long start = static_cast<long long>(a.length[s]) - count;
+  const int per_token = a.Hkv * a.vecs;
+  const int total = (t1 - t0) * per_token;
+  const int32_t* const row = a.table + static_cast<long long>(s) * a.width;
+  constexpr int U = 2;
+  for (int i0 = threadIdx.x; i0 < total; i0 += kCopyThreads * U) {
+    uint4 x[U], y[U];
+    long long to_k[U], to_v[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int i = i0 + u * kCopyThreads;
+      to_k[u] = -1;
+      if (i >= total) continue;
+      const int t = t0 + i / per_token, r = i % per_token, h = r / a.vecs, c = (r % a.vecs) * 8;
+      const long long pos = start + t;
+      if (pos < 0 || pos / a.page >= a.width) continue;
+      const int page = row[pos / a.page];
+      if (page < 0 || page >= a.pages) continue;
+      const int in = static_cast<int>(pos % a.page);
+      to_k[u] = page * a.k_pool.stride_b + h * a.k_pool.stride_h + in * a.k_pool.stride_n + c;
+      to_v[u] = page * a.v_pool.stride_b + h * a.v_pool.stride_h + in * a.v_pool.stride_n + c;
+      x[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.k_new.ptr) + k * a.k_new.stride_b + h * a.k_new.stride_h + t * a.k_new.stride_n + c));
+      y[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.v_new.ptr) + k * a.v_new.stride_b + h * a.v_new.stride_h + t * a.v_new.stride_n + c));
+    }
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      if (to_k[u] < 0) continue;
+      *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(const_cast<void*>(a.k_pool.ptr)) + to_k[u]) = x[u];
+      *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(const_cast<void*>(a.v_pool.ptr)) + to_v[u]) = y[u];
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+static bool page_size_ok(int page) { return page == 16 || page == 32 || page == 64 || page == 128; }
+
+// As tensor_ok, but an axis of one element has no stride to speak of.
+static bool tokens_ok(avsa_bf16_4d t, int B, int H, int N) {
+  if (N == 1) t.stride_n = 8;
+  return tensor_ok(t, B, H);
+}
+
+// [p, p + n) and [q, q + m) in ints share nothing
+static bool apart(const int32_t* p, long long n, const int32_t* q, long long m) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return a + 4 * static_cast<uintptr_t>(n) <= b || b + 4 * static_cast<uintptr_t>(m) <= a;
+}
+
+static int check_cache(const avsa_cache& c, bool by_page) {
+  if (c.seqs <= 0 || c.width <= 0 || c.pages <= 0) return AVSA_ERR_INVALID_ARG;
+  if ((by_page && !page_size_ok(c.page)) || static_cast<long long>(c.seqs) * c.width > INT_MAX || c.pages > (1 << 30)) return AVSA_ERR_UNSUPPORTED;
+  const int32_t* in[] = {c.table, c.length, c.ref};
+  const int32_t* out[] = {c.table_out, c.length_out, c.ref_out};
+  const long long size[] = {static_cast<long long>(c.seqs) * c.width, c.seqs, c.pages};
+  for (int i = 0; i < 3; i++) {
+    if (in[i] == nullptr || out[i] == nullptr || (reinterpret_cast<uintptr_t>(in[i]) & 3u) != 0 || (reinterpret_cast<uintptr_t>(out[i]) & 3u) != 0)
+      return AVSA_ERR_INVALID_ARG;
+    for (int j = 0; j < 3; j++) {
+      if (i == j && in[i] == out[i]) continue;
+      if (!apart(out[i], size[i], in[j], size[j]) || (i < j && !apart(out[i], size[i], out[j], size[j]))) return AVSA_ERR_INVALID_ARG;
+    }
+  }
+  return AVSA_OK;
+}
+static int check_list(const avsa_cache& c, const int32_t* a, const int32_t* b, int n, const void* ws, size_t ws_bytes,
+                      bool by_page = true) {
+  const int st = check_cache(c, by_page);
+  if (st != AVSA_OK) return st;
+  if (n < 0 || (n > 0 && (a == nullptr || b == nullptr))) return AVSA_ERR_INVALID_ARG;
+  if (ws == nullptr || ws_bytes < CacheWs::bytes(c.seqs, c.pages, n)) return AVSA_ERR_WORKSPACE;
+  if (!ws_aligned(ws, kWsVectors)) return AVSA_ERR_INVALID_ARG;
+  return AVSA_OK;
+}
+static int check_pool(const avsa_pages& p, int pages) {
+  if (p.ptr == nullptr || !aligned16(p.ptr) || p.planes <= 0 || p.page_bytes <= 0 || p.page_bytes % 16 != 0) return AVSA_ERR_INVALID_ARG;
+  if (pages > 1 && (p.stride_page < p.page_bytes || p.stride_page % 16 != 0)) return AVSA_ERR_INVALID_ARG;
+  if (p.planes > 1 && (p.stride_plane <= 0 || p.stride_plane % 16 != 0)) return AVSA_ERR_INVALID_ARG;
+  return AVSA_OK;
+}
+
+static unsigned meta_cluster(const avsa_cache& c) {
+  long long ints = c.pages;
+  if (c.table != c.table_out) ints += static_cast<long long>(c.seqs) * c.width;
+  return ints <= kMetaSingle ? 1u : static_cast<unsigned>(kMetaCluster);
+}
+static cudaError_t launch_meta(void (*kernel)(MetaArgs), const MetaArgs& a, cudaStream_t st) {
+  const unsigned ctas = meta_cluster(a.c);
+  return launch_pdl_clusters(kernel, ctas, ctas, kMetaThreads, 0, st, a);
+}
+static int launch_moves(const CopyArgs& a, long long most, cudaStream_t st) {
+  const long long chunks = (a.pool.page_bytes + kCopyChunk - 1) / kCopyChunk;
+  long long want = most * a.pool.planes * chunks;
+  if (a.table != nullptr) {
+    const long long rows = (static_cast<long long>(a.seqs) * a.width + kCopyThreads - 1) / kCopyThreads;
+    want = want > rows ? want : rows;
+  }
+  const int grid = persistent_grid(1 << 30) * 8;
+  return launch_pdl(move_pages_kernel, static_cast<unsigned>(want < grid ? want : grid), kCopyThreads, 0, st, a) == cudaSuccess ? AVSA_OK
+                                                                                                                     : AVSA_ERR_CUDA;
+}
+static int done() { return cudaGetLastError() == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA; }
+
+}  // namespace avsa
+
+using namespace avsa;
+
+extern "C" size_t avsa_cache_workspace_bytes(int seqs, int pages, int n) {
+  if (seqs <= 0 || pages <= 0 || n < 0) return 0;
+  return CacheWs::bytes(seqs, pages, n);
+}
+
+extern "C" int avsa_cache_extend(avsa_cache c, const int32_t* seq, const int32_t* count, int n, void* ws, size_t ws_bytes, void* stream) {
+  const int st = check_list(c, seq, count, n, ws, ws_bytes);
+  if (st != AVSA_OK) return st;
+  if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
+  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), seq, count, n, nullptr};
+  if (launch_meta(assign_pages_kernel<kExtend>, a, as_stream(stream)) != cudaSuccess) return AVSA_ERR_CUDA;
+  return done();
+}
+
+extern "C" int avsa_cache_fork(avsa_cache c, avsa_pages pool, const int32_t* parent, const int32_t* child, int n, void* ws, size_t ws_bytes,
+                               void* stream) {
+  int st = check_list(c, parent, child, n, ws, ws_bytes);
+  if (st == AVSA_OK) st = check_pool(pool, c.pages);
+  if (st != AVSA_OK) return st;
+  if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
+  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), child, parent, n, nullptr};
+  if (launch_meta(assign_pages_kernel<kFork>, a, as_stream(stream)) != cudaSuccess) return AVSA_ERR_CUDA;
+  if (n > 0) {
+    CopyArgs m = {};
+    m.pool = pool;
+    m.moves = a.w.moves;
+    m.n = n;
+    m.status = a.w.status;
+    if (launch_moves(m, n, as_stream(stream)) != AVSA_OK) return AVSA_ERR_CUDA;
+  }
+  return done();
+}
+
+extern "C" int avsa_cache_free(avsa_cache c, const int32_t* seq, int n, void* ws, size_t ws_bytes, void* stream) {
+  const int st = check_list(c, seq, seq, n, ws, ws_bytes, false);
+  if (st != AVSA_OK) return st;
+  if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
+  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), seq, nullptr, n, nullptr};
+  if (launch_meta(free_pages_kernel, a, as_stream(stream)) != cudaSuccess) return AVSA_ERR_CUDA;
+  return done();
+}
+
+extern "C" int avsa_cache_compact(avsa_cache c, avsa_pages pool, int32_t* n_live, void* ws, size_t ws_bytes, void* stream) {
+  int st = check_list(c, nullptr, nullptr, 0, ws, ws_bytes);
+  if (st == AVSA_OK) st = check_pool(pool, c.pages);
+  if (st != AVSA_OK) return st;
+  if (n_live == nullptr || (reinterpret_cast<uintptr_t>(n_live) & 3u) != 0) return AVSA_ERR_INVALID_ARG;
+  if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
+  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, 0), nullptr, nullptr, 0, n_live};
+  if (launch_meta(plan_compaction_kernel, a, as_stream(stream)) != cudaSuccess) return AVSA_ERR_CUDA;
+  CopyArgs m = {};
+  m.pool = pool;
+  m.moves = a.w.moves;
+  m.n_moves = a.w.counts + kNumMoves;
+  m.table = c.table;
+  m.table_out = c.table_out;
+  m.place = a.w.free_pages;
+  m.n_live = n_live;
+  m.seqs = c.seqs;
+  m.width = c.width;
+  m.pages = c.pages;
+  m.status = a.w.status;
+  if (launch_moves(m, c.pages, as_stream(stream)) != AVSA_OK) return AVSA_ERR_CUDA;
+  return done();
+}
+
+extern "C" int avsa_cache_write(int n, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d k_new,
+                                avsa_bf16_4d v_new, avsa_bf16_4d k_pool, avsa_bf16_4d v_pool, const int32_t* table,
+                                const int32_t* length, const int32_t* seq, const int32_t* count, void* stream) {
+  if (n < 0 || Hkv <= 0 || L < 0 || pages <= 0 || seqs <= 0 || width <= 0) return AVSA_ERR_INVALID_ARG;
+  if ((d != 64 && d != 128) || !page_size_ok(page) || n > 65535 || Hkv > 65535 || static_cast<long long>(seqs) * width > INT_MAX) return AVSA_ERR_UNSUPPORTED;
+  if (seq == nullptr && n > seqs) return AVSA_ERR_INVALID_ARG;
+  if (table == nullptr || length == nullptr || !tensor_ok(k_pool, pages, Hkv) || !tensor_ok(v_pool, pages, Hkv)) return AVSA_ERR_INVALID_ARG;
+  if (n == 0 || L == 0) return AVSA_OK;
+  if (!tokens_ok(k_new, n, Hkv, L) || !tokens_ok(v_new, n, Hkv, L)) return AVSA_ERR_INVALID_ARG;
+  if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
+  WriteArgs a = {k_new, v_new, k_pool, v_pool, table, length, seq, count, Hkv, L, d / 8, page, pages, seqs, width, 0};
+  // about four vectors of each tensor a thread, and no more than 32 bits count
+  const int per_token = Hkv * a.vecs;
+  a.tokens = per_token >= 4 * kCopyThreads ? 1 : 4 * kCopyThreads / per_token;
+  const dim3 grid(static_cast<unsigned>((L + a.tokens - 1) / a.tokens), static_cast<unsigned>(n));
+  if (launch_pdl(write_tokens_kernel, grid, kCopyThreads, 0, as_stream(stream), a) != cudaSuccess) return AVSA_ERR_CUDA;
+  return done();
+}
