@@ -281,7 +281,7 @@ AVSA_API int avsa_build_block_mask_static(int B, int H, int N, int d, int blk, a
  *                   each other; the longest sequence's row of the table then says which pages they are.  0: nothing is shared.
  *
  * What pages hold behind a sequence's last token is never used (it may be anything, NaN too).  Values of tokens that a
- * causal row must not see have to be finite.  A page of the table out of range contributes nothing and sets AVSA_ERR_BAD_TABLE, a
+ * causal row must not see have to be finite.  A page of the table out of range reads as zeros and sets AVSA_ERR_BAD_TABLE, a
  * length beyond the table's width is cut there and sets it as well.
  * d is 64 or 128, H a multiple of Hkv, H/Hkv at most 128.  table has `seqs` rows of `width` entries.  Same bits on every run.
  */

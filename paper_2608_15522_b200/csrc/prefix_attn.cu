@@ -1,76 +1,96 @@
 // Attention of a batch that shares a long beginning, over a paged cache.
 #include <math.h>
 
-#include "avsa_common.cuh"
-#include "sm100_ptx.cuh"
+#include "prefix_attn_kernel.cuh"
 
 namespace avsa {
 
-enum PrefixWhere { kPrefixPage = 221, kPrefixLength, kPrefixSeq };
-
-struct PrefixParams {
-  avsa_bf16_4d q, k, v;
-  __nv_bfloat16* o;
-  float* lse;
-  const int32_t *table, *length, *seq;
-  StatusRecord* status;
-  int B, H, G, L;           // G: query heads of a key head
-  int page, pages, seqs, width;
-  int causal;
-  float scale_log2;
-};
-
-// A warp per row, key after key: the running maximum and sum, the row of O in registers.
-template <int D>
-__global__ void __launch_bounds__(256) prefix_rows_kernel(const PrefixParams p) {
+static __global__ void clear_counter_kernel(int* counter) {
   pdl_wait();
   pdl_launch();
-  const long long r = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (r >= static_cast<long long>(p.B) * p.H * p.L) return;
-  const int i = static_cast<int>(r % p.L), h = static_cast<int>(r / p.L % p.H), b = static_cast<int>(r / p.L / p.H);
-  constexpr int C = D / 32;
-  float q[C], o[C] = {};
-  const __nv_bfloat16* qr = static_cast<const __nv_bfloat16*>(p.q.ptr) + b * p.q.stride_b + h * p.q.stride_h + i * p.q.stride_n;
-#pragma unroll
-  for (int c = 0; c < C; c++) q[c] = __bfloat162float(qr[lane * C + c]) * p.scale_log2;
-  const int s = p.seq != nullptr ? p.seq[b] : b;
-  long long lim = 0;
-  if (s >= p.seqs) {
-    if (lane == 0) report_status(p.status, AVSA_ERR_BAD_TABLE, kPrefixSeq, b, s);
-  } else if (s >= 0) {
-    long long n = p.length[s];
-    if (n < 0 || n > static_cast<long long>(p.width) * p.page) {
-      if (lane == 0) report_status(p.status, AVSA_ERR_BAD_TABLE, kPrefixLength, s, static_cast<int>(n));
-      n = n < 0 ? 0 : static_cast<long long>(p.width) * p.page;
-    }
-    lim = p.causal ? n - p.L + i + 1 : n;
+  *counter = 0;
+}
+
+constexpr int kChunk = 8;        // row tiles that go through the beginning side by side, at most
+
+struct PrefixLayout {
+  PrefixShape s;
+  int n_cta;
+  size_t rows;                  // partial rows
+  int own_row0, cut_row0;
+  size_t plan, cta_err, own_rec, cut_rec, lse, o, total;       // offsets in the workspace
+};
+
+// False: more units than 32 bits count.
+static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int width, int prefix_pages, int causal, PrefixLayout& y) {
+  PrefixShape& s = y.s;
+  s = {};
+  s.B = B;
+  s.Hkv = Hkv;
+  s.G = H / Hkv;
+  s.L = L;
+  const long long R = static_cast<long long>(L) * s.G, TO = (R + 127) / 128, F = TO * B, RS = R * B, TP = (RS + 127) / 128;
+  const long long most = (static_cast<long long>(width) * page + 127) / 128, PT = static_cast<long long>(prefix_pages) * page / 128;
+  if (RS > 0x3fffffffll || F * Hkv > 0x3fffffffll || F * Hkv * (most > 0 ? most : 1) > 0x7fffffffll) return false;
+  s.R = static_cast<int>(R);
+  s.TO = static_cast<int>(TO);
+  s.F = static_cast<int>(F);
+  s.rows = R < 128 ? s.R : 128;
+  s.causal = causal;
+  s.page = page;
+  s.page_shift = page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7;
+  const int sms = persistent_grid(1 << 30);
+  // Stacked, the beginning's key tiles are walked TP times a head instead of F times, but every row goes through the merge: its parts are
+  // 2 KB written and read, a tile is 64 KB.
+  s.stack = TP * PT + RS / 32 + 2 <= F * PT;
+  const long long units = F * Hkv * most + (s.stack ? TP * Hkv * PT : 0);
+  y.n_cta = static_cast<int>(units < sms ? units : sms);
+  if (y.n_cta < 1) y.n_cta = 1;
+  if (s.stack) {
+    s.k0 = prefix_pages * page;
+    s.TP = static_cast<int>(TP);
+    const int side = kChunk < y.n_cta ? kChunk : y.n_cta;
+    s.nrc = (s.TP + side - 1) / side;
+    s.chunk = (s.TP + s.nrc - 1) / s.nrc;
   }
-  float m = -INFINITY, l = 0.f;
-  for (int t = 0; t < lim; t++) {
-    const int page = p.table[static_cast<long long>(s) * p.width + t / p.page];
-    if (page < 0 || page >= p.pages) {
-      if (lane == 0) report_status(p.status, AVSA_ERR_BAD_TABLE, kPrefixPage, s, t / p.page);
-      continue;
-    }
-    const __nv_bfloat16* kr = static_cast<const __nv_bfloat16*>(p.k.ptr) + page * p.k.stride_b + h / p.G * p.k.stride_h + t % p.page * p.k.stride_n;
-    const __nv_bfloat16* vr = static_cast<const __nv_bfloat16*>(p.v.ptr) + page * p.v.stride_b + h / p.G * p.v.stride_h + t % p.page * p.v.stride_n;
-    float x = 0.f;
-#pragma unroll
-    for (int c = 0; c < C; c++) x += q[c] * __bfloat162float(kr[lane * C + c]);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    const float m2 = fmaxf(m, x);
-    const float a = m2 == -INFINITY ? 1.f : exp2f(m - m2), e = m2 == -INFINITY ? 0.f : exp2f(x - m2);
-    m = m2;
-    l = l * a + e;
-#pragma unroll
-    for (int c = 0; c < C; c++) o[c] = o[c] * a + e * __bfloat162float(vr[lane * C + c]);
-  }
-  __nv_bfloat16* orow = p.o + b * p.q.stride_b + h * p.q.stride_h + i * p.q.stride_n;
-#pragma unroll
-  for (int c = 0; c < C; c++) orow[lane * C + c] = __float2bfloat16(l != 0.f ? o[c] / l : 0.f);
-  if (lane == 0 && p.lse != nullptr) p.lse[r] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+  s.queue = TO > 1 && F * Hkv > y.n_cta;
+  s.nb_max = s.queue ? 8 * y.n_cta : y.n_cta;
+  const size_t pre = s.stack ? (static_cast<size_t>(y.n_cta) + static_cast<size_t>(Hkv) * s.nrc * s.chunk) * 128 : 0;
+  const size_t own = s.stack ? static_cast<size_t>(F) * Hkv * s.rows : 0;
+  y.rows = pre + own + 2 * static_cast<size_t>(s.nb_max) * s.rows;
+  if (y.rows > 0x7fffffffu) return false;
+  y.own_row0 = static_cast<int>(pre);
+  y.cut_row0 = static_cast<int>(pre + own);
+  size_t at = kStatusBytes;
+  y.plan = at;
+  at += 256;
+  y.cta_err = at;
+  at += align_up(static_cast<size_t>(y.n_cta) * 32, 256);
+  y.own_rec = at;
+  at += align_up(s.stack ? static_cast<size_t>(F) * Hkv * 8 : 0, 256);
+  y.cut_rec = at;
+  at += align_up(static_cast<size_t>(s.nb_max) * 8, 256);
+  y.lse = at;
+  at += align_up(y.rows * 4, 256);
+  y.o = at;
+  y.total = at + y.rows * d * 4;
+  return true;
+}
+
+template <int D>
+static int launch_prefix(const PrefixLayout& y, const avsa_bf16_4d& k, const avsa_bf16_4d& v, const PrefixParams& p, cudaStream_t st) {
+  const PrefixShape& s = y.s;
+  CUtensorMap tk, tv;
+  if (!encode_bf16_tile_map(&tk, k.ptr, s.pages, s.Hkv, s.page, D, k.stride_b, k.stride_h, k.stride_n, s.page) ||
+      !encode_bf16_tile_map(&tv, v.ptr, s.pages, s.Hkv, s.page, D, v.stride_b, v.stride_h, v.stride_n, s.page))
+    return AVSA_ERR_CUDA;
+  if (s.queue && launch_pdl(clear_counter_kernel, 1, 1, 0, st, p.counter) != cudaSuccess) return AVSA_ERR_CUDA;
+  if (cudaFuncSetAttribute(prefix_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PrefixSmem<D>::kTotal) != cudaSuccess) return AVSA_ERR_CUDA;
+  if (launch_pdl(prefix_attn_kernel<D>, y.n_cta, kPxThreads, PrefixSmem<D>::kTotal, st, tk, tv, p) != cudaSuccess) return AVSA_ERR_CUDA;
+  dim3 grid(static_cast<unsigned>(s.nb_max), s.rows > 64 ? 2 : 1);
+  if (s.stack) grid = dim3(static_cast<unsigned>((static_cast<long long>(s.B) * s.R * s.Hkv + kPxMergeWarps - 1) / kPxMergeWarps));
+  if (launch_pdl(prefix_merge_kernel<D>, grid, kPxMergeWarps * 32, 0, st, p, y.n_cta) != cudaSuccess) return AVSA_ERR_CUDA;
+  return cudaGetLastError() == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
 }
 
 static bool rows_ok(avsa_bf16_4d t, int B, int H, int N) {
@@ -82,9 +102,15 @@ static bool rows_ok(avsa_bf16_4d t, int B, int H, int N) {
 
 using namespace avsa;
 
+static bool prefix_sizes_ok(int B, int H, int Hkv, int L, int d, int page, int width, int prefix_pages) {
+  return B > 0 && H > 0 && Hkv > 0 && L > 0 && width > 0 && prefix_pages >= 0 && prefix_pages <= width && H % Hkv == 0 && H / Hkv <= 128 &&
+         (d == 64 || d == 128) && (page == 16 || page == 32 || page == 64 || page == 128) && H <= 65535 && B <= 65535;
+}
+
 extern "C" size_t avsa_prefix_attn_workspace_bytes(int B, int H, int Hkv, int L, int d, int page, int width, int prefix_pages) {
-  if (B <= 0 || H <= 0 || Hkv <= 0 || L <= 0 || d <= 0 || page <= 0 || width <= 0 || prefix_pages < 0) return 0;
-  return kStatusBytes;
+  PrefixLayout y;
+  if (!prefix_sizes_ok(B, H, Hkv, L, d, page, width, prefix_pages) || !prefix_layout(B, H, Hkv, L, d, page, width, prefix_pages, 0, y)) return 0;
+  return y.total;
 }
 
 extern "C" int avsa_prefix_attn(int B, int H, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d q,
@@ -102,15 +128,34 @@ extern "C" int avsa_prefix_attn(int B, int H, int Hkv, int L, int d, int page, i
   if (B == 0 || L == 0) return AVSA_OK;
   if (!rows_ok(q, B, H, L) || !tensor_ok(k_pool, pages, Hkv) || !tensor_ok(v_pool, pages, Hkv)) return AVSA_ERR_INVALID_ARG;
   if (table == nullptr || length == nullptr || o_bf16 == nullptr || !aligned16(o_bf16)) return AVSA_ERR_INVALID_ARG;
-  if (ws == nullptr || ws_bytes < avsa_prefix_attn_workspace_bytes(B, H, Hkv, L, d, page, width, prefix_pages)) return AVSA_ERR_WORKSPACE;
+  PrefixLayout y;
+  if (!prefix_layout(B, H, Hkv, L, d, page, width, prefix_pages, flags & AVSA_CAUSAL ? 1 : 0, y)) return AVSA_ERR_UNSUPPORTED;
+  if (ws == nullptr || ws_bytes < y.total) return AVSA_ERR_WORKSPACE;
   if (!ws_aligned(ws, kWsParts)) return AVSA_ERR_INVALID_ARG;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
-  const cudaStream_t st = as_stream(stream);
   const float scale = softmax_scale != 0.f ? softmax_scale : 1.0f / sqrtf(static_cast<float>(d));
-  const PrefixParams p = {q, k_pool, v_pool, static_cast<__nv_bfloat16*>(o_bf16), lse, table, length, seq, static_cast<StatusRecord*>(ws), B, H, H / Hkv, L,
-                          page, pages, seqs, width, flags & AVSA_CAUSAL ? 1 : 0, scale * 1.4426950408889634f};
-  if (launch_pdl(clear_status_kernel, 1, 1, 0, st, p.status) != cudaSuccess) return AVSA_ERR_CUDA;
-  const unsigned grid = static_cast<unsigned>((static_cast<long long>(B) * H * L + 7) / 8);
-  if (launch_pdl(d == 128 ? prefix_rows_kernel<128> : prefix_rows_kernel<64>, grid, 256, 0, st, p) != cudaSuccess) return AVSA_ERR_CUDA;
-  return cudaGetLastError() == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
+  uint8_t* w = static_cast<uint8_t*>(ws);
+  y.s.pages = pages;
+  y.s.seqs = seqs;
+  y.s.width = width;
+  PrefixParams p = {};
+  p.s = y.s;
+  p.q = q;
+  p.o = static_cast<__nv_bfloat16*>(o_bf16);
+  p.lse = lse;
+  p.table = table;
+  p.length = length;
+  p.seq = seq;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.status = static_cast<StatusRecord*>(ws);
+  p.plan = reinterpret_cast<int*>(w + y.plan);
+  p.counter = p.plan + 32;
+  p.cta_err = reinterpret_cast<int4*>(w + y.cta_err);
+  p.own_rec = reinterpret_cast<int2*>(w + y.own_rec);
+  p.cut_rec = reinterpret_cast<int2*>(w + y.cut_rec);
+  p.part_lse2 = reinterpret_cast<float*>(w + y.lse);
+  p.part_o = reinterpret_cast<float*>(w + y.o);
+  p.own_row0 = y.own_row0;
+  p.cut_row0 = y.cut_row0;
+  return d == 128 ? launch_prefix<128>(y, k_pool, v_pool, p, as_stream(stream)) : launch_prefix<64>(y, k_pool, v_pool, p, as_stream(stream));
 }

@@ -1,0 +1,1029 @@
+// Attention over a paged cache: the tile kernel, and the kernel that joins what it has cut.
+//
+// A tile is 128 query rows against 128 keys of one key/value head.  Query rows are all that share keys: the L queries times the G query heads of
+// that key head (row i*G + g of a batch entry), and, over the beginning that the whole batch shares, those of all batch
+// entries one after the other ("stacked").  One token of 64 sequences with 4 query heads to a key head makes 4 rows a sequence, which leave 124 rows of a
+// tile empty, but 256 rows stacked: the beginning is read twice instead of 64 times, and the tensor cores work on full tiles.
+//
+// Work.  An item is a row tile with all its keys; its key tiles are units.  Which units a CTA takes:
+//   - prefix pieces: the key tiles of the beginning, head after head, are one stream of columns; `chunk` row tiles go through it side by side (a CTA each, so that
+//     the second reader of a key tile finds it in L2), and each group of `chunk` CTAs gets the same number of columns;
+//   - B pieces: the own items of all sequences, one after the other, are a stream that is cut into equal pieces: lengths as ragged as they may be,
+//     every CTA gets the same number of units, and all of them stream pages from HBM side by side;
+//   - A pieces: with several row tiles to a sequence (long blocks of queries) whole items come off a queue first, so that CTAs that run at the
+//     same time work on the same keys (as equal shares of the stream they would be heads apart: each tile from HBM), and only the last ones are cut.
+// What a cut or a stacked item leaves are fp32 rows, normalised by their own sum, and their log2 sums; prefix_merge_kernel joins them in a fixed order.
+// Lengths are on the device: every CTA's scheduler warp counts the units itself (a scan over the batch), nothing comes back to the host.
+//
+// Pipeline (one persistent CTA per SM): as in attn_persist_kernel.cuh, whose softmax against one fixed reference per row this is:
+// K and V tiles through two rings of TMA loads, here page by page (a page id beyond the pool reads as zeros: what lies behind the
+// last page), S = Q K^T and O += P V by tcgen05 from two issuing warps, two softmax groups of four warps on alternate key tiles.  Query rows are gathered by
+// two warps with cp.async, since neighbouring rows of a tile lie in different heads or sequences.  An item with a row that outgrew its reference runs again
+// in the same CTA: once for the row maxima alone, once with these as the references.
+#pragma once
+#include <math.h>
+
+#include "attn_persist_kernel.cuh"
+
+namespace avsa {
+
+constexpr int kPxThreads = 512;
+// 512 x 128 registers at launch; then 8 service warps of 64 and 8 softmax warps of 192: 65536 both ways.
+constexpr int kPxServiceRegs = 64, kPxSoftmaxRegs = 192;
+static_assert(8 * 32 * kPxServiceRegs + 8 * 32 * kPxSoftmaxRegs <= kPxThreads * 128, "setmaxnreg budget exceeded");
+constexpr int kPxRing = 4, kPxRedo = 16;
+constexpr int kPxQWarps = 2;             // warps 13 and 14 gather query rows
+constexpr int kPxConsumers = 4 + kPxQWarps + 8;      // warps that read the item ring
+
+enum PrefixWhere {
+  kPrefixPage = 221, kPrefixLength, kPrefixSeq, kPxItem, kPxItemEmpty, kPxQEmpty, kPxQFull, kPxKEmpty, kPxVEmpty, kPxKFull, kPxVFull, kPxSFull, kPxSFree,
+  kPxPFull, kPxPFree, kPxOFull, kPxOFree, kPxMref, kPxLsum, kPxAlign
+};
+
+// What of the work depends on sizes alone.
+struct PrefixShape {
+  int B, Hkv, G, L;
+  int R;               // query rows of a batch entry and key head: L*G
+  int TO, F;           // row tiles of these, and of the whole batch (F = B*TO)
+  int stack;           // the beginning's pages are read for the stacked rows
+  int k0;              // first key of the own items: 0, or behind the beginning
+  int TP, chunk, nrc;  // row tiles of the stacked rows, taken `chunk` at a time (nrc times)
+  int rows;            // rows of an own item's partial result: min(128, R)
+  int queue;           // whole items off a queue
+  int nb_max;          // B pieces at most
+  int page, page_shift, pages, seqs, width;
+  int causal;
+};
+
+struct PrefixParams {
+  PrefixShape s;
+  avsa_bf16_4d q;
+  __nv_bfloat16* o;
+  float* lse;
+  const int32_t *table, *length, *seq;
+  float scale_log2;
+  // workspace
+  StatusRecord* status;
+  int* counter;        // head of the queue
+  int* plan;           // for the merge: PT, columns a group, B pieces
+  int4* cta_err;       // [2 * CTAs]: code, where, item, aux; recomputed items
+  int2* own_rec;       // stack: [Hkv*F] first B piece and number of parts of an own item
+  int2* cut_rec;       // else: [nb_max] the item that a B piece begins and does not end, and its number of parts
+  float* part_o;       // [rows][D]: prefix slots of 128 rows, own items (stack), two cut ends a B piece
+  float* part_lse2;
+  int own_row0, cut_row0;      // first rows of the latter two
+};
+
+struct PrefixItem {
+  int type;            // -1: no more; bit 0: stacked rows, bits 1-2: 0, or 1 maxima only, 2 with given maxima
+  int b, hk, row0, nrows;
+  int pos0, cnt, kv_end;       // first key, key tiles, end of the keys
+  int slot;            // row of the page table
+  int len;             // own items: tokens of the sequence
+  int out;             // first partial row, -1: final rows
+  int pad;
+};
+static_assert(sizeof(PrefixItem) == 48, "three 16-byte accesses");
+
+template <int D>
+struct PrefixSmem {
+  static constexpr int kTile = 128 * D * 2;
+  static constexpr int kKS = D == 128 ? 3 : 6, kVS = D == 128 ? 3 : 6;
+  static constexpr int kQ = 0;
+  static constexpr int kK = kTile;
+  static constexpr int kV = kK + kKS * kTile;
+  static constexpr int kBars = kV + kVS * kTile;
+  static constexpr int kNumBars = 2 + 2 * kKS + 2 * kVS + 13 + 2 * kPxRing + 4;
+  static constexpr int kStats = (kBars + kNumBars * 8 + 15) / 16 * 16;       // float mref[128], lsum[2][128]
+  static constexpr int kItems = kStats + 3 * 128 * 4;
+  static constexpr int kRedo = kItems + 48 * kPxRing;
+  static constexpr int kMisc = kRedo + 48 * kPxRedo;                          // tmem base, stop, redo flags [2], listed, recomputed, error [4]
+  static constexpr int kTotal = kMisc + 48;
+  static_assert(kTotal <= 232448, "shared memory of a CTA exceeded");
+};
+
+// ------------------------------------------------------------------------------------------------ sizes on the device
+// Table row of a batch entry (-1: none) and its tokens.  `bad`: what is out of range.
+__device__ __forceinline__ int prefix_sequence(const PrefixParams& p, int b, int& slot, int& bad) {
+  const int s = p.seq != nullptr ? p.seq[b] : b;
+  slot = s < 0 || s >= p.s.seqs ? -1 : s;
+  bad = s >= p.s.seqs ? kPrefixSeq : 0;
+  if (slot < 0) return 0;
+  const int n = p.length[slot], most = p.s.width << p.s.page_shift;
+  if (n < 0 || n > most) bad = kPrefixLength;
+  return n < 0 ? 0 : n > most ? most : n;
+}
+// Key tiles of an own item: row tile rt of a sequence of n tokens.
+__device__ __forceinline__ int prefix_own_tiles(const PrefixShape& s, int n, int rt) {
+  int end = n;
+  if (s.causal) end = n - s.L + min(s.L - 1, (rt * 128 + 127) / s.G) + 1;
+  const int x = end - s.k0;
+  const int t = x > 0 ? (x + 127) >> 7 : 0;
+  return s.stack ? t : max(t, 1);      // (without a beginning of its own every row tile is written by somebody)
+}
+
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)) : "memory");
+}
+
+constexpr int kPxMinPiece = 4;       // key tiles: a CTA with fewer ends later than one that takes another's as well
+
+// How the units are cut: the same in every CTA.
+struct PrefixPlan {
+  int PT, PE, donor;           // key tiles and tokens of the beginning, the table row that names its pages
+  int cg, groups;              // columns of a group
+  int W, MA, uA;               // units of a key head; items of the queue, their units
+  int TB, sB, NB;              // units of the B pieces, of one, pieces
+};
+
+template <int D>
+__global__ void __launch_bounds__(kPxThreads, 1)
+prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const __grid_constant__ PrefixParams p) {
+  using L_ = PrefixSmem<D>;
+  constexpr int NPANEL = D / 64, PANEL = 128 * 128, KS = L_::kKS, VS = L_::kVS;
+  constexpr unsigned FULLM = 0xffffffffu;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const PrefixShape& S = p.s;
+
+  const uint32_t bar0 = smem_u32(smem + L_::kBars);
+  auto BAR = [&](int i) { return bar0 + static_cast<uint32_t>(i) * 8u; };
+  constexpr int Q_FULL = 0, Q_EMPTY = 1, K_FULL = 2, K_EMPTY = K_FULL + KS, V_FULL = K_EMPTY + KS, V_EMPTY = V_FULL + VS,
+                S_FULL = V_EMPTY + VS, S_FREE = S_FULL + 2, P_FULL = S_FREE + 2 /* + 2*group + half */, P_FREE = P_FULL + 4, O_FULL = P_FREE + 2,
+                O_FREE = O_FULL + 1, MREF = O_FREE + 1, ITEM_FULL = MREF + 1, ITEM_EMPTY = ITEM_FULL + kPxRing, QK_DRAIN = ITEM_EMPTY + kPxRing,
+                PV_DRAIN = QK_DRAIN + 1, LSUM_A = PV_DRAIN + 1, LSUM_B = LSUM_A + 1;
+  static_assert(LSUM_B + 1 <= L_::kNumBars, "barrier table too small");
+  constexpr uint32_t TM_O = 256, TM_P = 256 + D;      // tensor memory: S of group 0 | S of group 1 | O | P of group 0 | P of group 1
+  float* mref_s = reinterpret_cast<float*>(smem + L_::kStats);
+  float* lsum_s = mref_s + 128;
+  PrefixItem* ring = reinterpret_cast<PrefixItem*>(smem + L_::kItems);
+  PrefixItem* redo = reinterpret_cast<PrefixItem*>(smem + L_::kRedo);
+  volatile int* misc = reinterpret_cast<volatile int*>(smem + L_::kMisc);
+  enum { TMEM = 0, STOP, FLAG /* + item parity */, LISTED = FLAG + 2, RECOMPUTED, ERR };
+
+  const bool aligned = (smem_u32(smem) & 1023u) == 0u;
+  if (tid == 0) {
+    mbar_init(BAR(Q_FULL), 32 * kPxQWarps);
+    mbar_init(BAR(Q_EMPTY), 1);
+    for (int s = 0; s < KS; s++) {
+      mbar_init(BAR(K_FULL + s), 1);
+      mbar_init(BAR(K_EMPTY + s), 1);
+    }
+    for (int s = 0; s < VS; s++) {
+      mbar_init(BAR(V_FULL + s), 1);
+      mbar_init(BAR(V_EMPTY + s), 1);
+    }
+    for (int g = 0; g < 2; g++) {
+      mbar_init(BAR(S_FULL + g), 1);
+      mbar_init(BAR(S_FREE + g), 128);
+      mbar_init(BAR(P_FULL + 2 * g), 128);
+      mbar_init(BAR(P_FULL + 2 * g + 1), 128);
+      mbar_init(BAR(P_FREE + g), 1);
+    }
+    for (int r = 0; r < kPxRing; r++) {
+      mbar_init(BAR(ITEM_FULL + r), 1);
+      mbar_init(BAR(ITEM_EMPTY + r), kPxConsumers);
+    }
+    mbar_init(BAR(O_FULL), 1);
+    mbar_init(BAR(O_FREE), 256);
+    mbar_init(BAR(MREF), 128);
+    mbar_init(BAR(QK_DRAIN), 1);
+    mbar_init(BAR(PV_DRAIN), 1);
+    mbar_init(BAR(LSUM_A), 256);
+    mbar_init(BAR(LSUM_B), 256);
+    for (int i = STOP; i < ERR + 4; i++) misc[i] = 0;
+    fence_mbar_init();
+    prefetch_tmap(&tmk);
+    prefetch_tmap(&tmv);
+  }
+  if (warp == 2) {
+    tmem_alloc(smem_u32(smem + L_::kMisc), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = misc[TMEM];
+  pdl_wait();
+  pdl_launch();
+
+  // The CTA's first error, for the merge kernel to report.
+  auto report = [&](int code, int where, int item, int aux) {
+    if (atomicCAS(const_cast<int*>(&misc[ERR]), 0, code) == 0) {
+      misc[ERR + 1] = where;
+      misc[ERR + 2] = item;
+      misc[ERR + 3] = aux;
+    }
+  };
+  auto wait_or_stop = [&](int bar, uint32_t parity, int where, int tag) -> bool {
+    if (mbar_try_wait(BAR(bar), parity)) return true;
+    const long long t0 = clock64();
+    while (true) {
+      if (misc[STOP] != 0) return false;
+      if (mbar_try_wait(BAR(bar), parity)) return true;
+      if (clock64() - t0 > AVSA_WAIT_LIMIT_CYCLES) {
+        report(AVSA_ERR_TIMEOUT, where, blockIdx.x, tag);
+        misc[STOP] = 1;
+        return false;
+      }
+    }
+  };
+  auto wait_all = [&](int bar, uint32_t parity, int where, int tag) -> bool {
+    return __all_sync(FULLM, wait_or_stop(bar, parity, where, tag));
+  };
+  auto get_item = [&](int n, PrefixItem& it) -> bool {     // false: stopped, or no more items
+    const int slot = n % kPxRing;
+    if (!wait_all(ITEM_FULL + slot, (n / kPxRing) & 1, kPxItem, n)) return false;
+    it = ring[slot];
+    return it.type >= 0;
+  };
+  auto item_done = [&](int n) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(BAR(ITEM_EMPTY + n % kPxRing));
+  };
+
+  // (every role changes its registers by itself, as its first step: the compiler goes by that)
+  if (!aligned) {
+    if (tid == 0) report(AVSA_ERR_CUDA, kPxAlign, blockIdx.x, 0);
+    if (tid == 0 && blockIdx.x == 0) p.plan[0] = p.plan[2] = 0;
+  } else if (warp == 0 || warp == 12) {
+    // ------------------------------------------------------------------ TMA producers: warp 0 K, warp 12 V
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    const bool is_k = warp == 0;
+    const CUtensorMap* tm = is_k ? &tmk : &tmv;
+    const int FULL = is_k ? K_FULL : V_FULL, EMPTY = is_k ? K_EMPTY : V_EMPTY, STAGES = is_k ? KS : VS;
+    const uint32_t base = smem_u32(smem + (is_k ? L_::kK : L_::kV));
+    const int ppt_shift = 7 - S.page_shift, ppt = 1 << ppt_shift;      // pages of a tile
+    int stage = 0, round = 0, loads = 0;
+    bool ok = true;
+    for (int n = 0; ok; n++) {
+      PrefixItem it;
+      if (!get_item(n, it)) break;
+      if (is_k || (it.type >> 1) != 1) {
+        const int32_t* row = p.table + static_cast<int64_t>(max(it.slot, 0)) * S.width;
+        const int e0 = it.pos0 >> S.page_shift, e1 = (it.kv_end + S.page - 1) >> S.page_shift;      // its pages
+        const int per = 32 >> ppt_shift;       // tiles whose pages a warp reads at once
+        for (int t0 = 0; t0 < it.cnt && ok; t0 += per) {
+          const int e = e0 + (t0 << ppt_shift) + lane;
+          int mine = S.pages;                  // behind the last page: beyond the pool, where the copy reads zeros
+          if (e < e1 && e < e0 + (it.cnt << ppt_shift)) {
+            mine = row[e];
+            if (mine < 0 || mine >= S.pages) {
+              report(AVSA_ERR_BAD_TABLE, kPrefixPage, it.slot, e);
+              mine = S.pages;
+            }
+          }
+          const int nn = min(per, it.cnt - t0);
+          for (int j = 0; j < nn; j++) {
+            const int id = __shfl_sync(FULLM, mine, (j << ppt_shift) + (lane & (ppt - 1)));
+            int good = 1;
+            if (lane == 0) {
+              if (round > 0) good = wait_or_stop(EMPTY + stage, (round - 1) & 1, is_k ? kPxKEmpty : kPxVEmpty, t0 + j) ? 1 : 0;
+              if (good) mbar_expect_tx(BAR(FULL + stage), L_::kTile);
+            }
+            good = __shfl_sync(FULLM, good, 0);
+            if (!good) {
+              ok = false;
+              break;
+            }
+            if (lane < ppt * NPANEL) {
+              const int panel = lane >> ppt_shift, in = lane & (ppt - 1);
+              tma_load_4d(base + stage * L_::kTile + panel * PANEL + ((in << S.page_shift) << 7), tm, BAR(FULL + stage), panel * 64, 0, it.hk, id);
+            }
+            __syncwarp();
+            loads++;
+            if (++stage == STAGES) {
+              stage = 0;
+              round++;
+            }
+          }
+        }
+      }
+      if (ok) item_done(n);
+    }
+    if (lane == 0 && misc[STOP] != 0)      // loads still in flight must land before this CTA's shared memory is given away
+      for (int c = max(0, loads - STAGES); c < loads; c++) mbar_wait(BAR(FULL + c % STAGES), (c / STAGES) & 1);
+  } else if (warp == 13 || warp == 14) {
+    // ------------------------------------------------------------------ query rows into shared memory, 128-byte swizzled like a TMA tile
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    constexpr int VPR = D / 8, RPI = 32 / VPR;      // 16-byte vectors of a row; rows of an instruction
+    const uint32_t base = smem_u32(smem + L_::kQ);
+    bool ok = true;
+    for (int n = 0; ok; n++) {
+      PrefixItem it;
+      if (!get_item(n, it)) break;
+      if (n > 0) ok = wait_all(Q_EMPTY, (n - 1) & 1, kPxQEmpty, n);
+      if (!ok) break;
+      for (int r0 = (warp - 13) * 32; r0 < it.nrows; r0 += 32 * kPxQWarps) {
+        int64_t off = 0;
+        if (r0 + lane < it.nrows) {
+          int rr = it.row0 + r0 + lane, b = it.b;
+          if (it.type & 1) {
+            b = rr / S.R;
+            rr -= b * S.R;
+          }
+          const int i = rr / S.G, g = rr - i * S.G;
+          off = b * p.q.stride_b + (it.hk * S.G + g) * p.q.stride_h + i * p.q.stride_n;
+        }
+        const int rows = min(32, it.nrows - r0);
+        for (int k = 0; k < rows; k += RPI) {
+          const int rl = k + lane / VPR, c = lane % VPR;
+          const int64_t o = __shfl_sync(FULLM, off, rl & 31);
+          const int r = r0 + rl;
+          if (rl < rows)
+            cp_async_16(base + (c >> 3) * PANEL + r * 128 + (((c & 7) ^ (r & 7)) << 4), static_cast<const __nv_bfloat16*>(p.q.ptr) + o + c * 8);
+        }
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      fence_proxy_async();
+      mbar_arrive(BAR(Q_FULL));
+      item_done(n);
+    }
+  } else if (warp == 3) {
+    // ------------------------------------------------------------------ scheduler
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    const int n_cta = gridDim.x;
+    int published = 0;
+    auto publish = [&](const PrefixItem& it) -> bool {
+      const int m = published, slot = m % kPxRing;
+      if (m >= kPxRing && !wait_all(ITEM_EMPTY + slot, ((m / kPxRing) - 1) & 1, kPxItemEmpty, m)) return false;
+      if (lane == 0) {
+        ring[slot] = it;
+        mbar_arrive(BAR(ITEM_FULL + slot));
+      }
+      __syncwarp();
+      published++;
+      return true;
+    };
+    // All published items are done; those with a row that outgrew its reference run again.
+    auto settle = [&]() -> bool {
+      if (published == 0) return true;
+      const int m = published - 1;
+      if (!wait_all(ITEM_EMPTY + m % kPxRing, (m / kPxRing) & 1, kPxItemEmpty, m)) return false;
+      const int listed = __shfl_sync(FULLM, misc[LISTED], 0);
+      if (lane == 0) misc[LISTED] = 0;
+      for (int i = 0; i < listed; i++) {
+        PrefixItem it = redo[i];
+        const int type = it.type;
+        it.type = type | 2;
+        if (!publish(it)) return false;
+        it.type = type | 4;
+        if (!publish(it)) return false;
+      }
+      return true;
+    };
+    auto give = [&](const PrefixItem& it) -> bool {
+      if (__shfl_sync(FULLM, misc[LISTED], 0) >= kPxRedo - kPxRing - 1 && !settle()) return false;
+      return publish(it);
+    };
+    // Item f of a key head that holds its unit `rest` < W, and the units before it.
+    auto find = [&](int rest, int& f, int& before) {
+      f = before = 0;
+      for (int f0 = 0; f0 < S.F; f0 += 32) {
+        int nt = 0;
+        if (f0 + lane < S.F) {
+          const int b = (f0 + lane) / S.TO;
+          int slot, bad;
+          const int len = prefix_sequence(p, b, slot, bad);
+          nt = prefix_own_tiles(S, len, f0 + lane - b * S.TO);
+        }
+        int inc = nt;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int o = __shfl_up_sync(FULLM, inc, d);
+          if (lane >= d) inc += o;
+        }
+        const unsigned beyond = __ballot_sync(FULLM, before + inc > rest);
+        if (beyond != 0u) {
+          const int l = __ffs(beyond) - 1;
+          f = f0 + l;
+          before += __shfl_sync(FULLM, inc - nt, l);
+          return;
+        }
+        before += __shfl_sync(FULLM, inc, 31);
+      }
+    };
+    // ---- the plan
+    PrefixPlan P = {};
+    {
+      int most = 0, at = 0;
+      int W = 0;
+      for (int f = lane; f < S.F; f += 32) {
+        const int b = f / S.TO;
+        int slot, bad;
+        const int len = prefix_sequence(p, b, slot, bad);
+        if (bad && blockIdx.x == 0) report(AVSA_ERR_BAD_TABLE, bad, b, slot);
+        W += prefix_own_tiles(S, len, f - b * S.TO);
+        if (len > most) most = len, at = slot;
+      }
+      P.W = __reduce_add_sync(FULLM, W);
+      if (S.stack) {
+        const int top = __reduce_max_sync(FULLM, most);
+        const unsigned who = __ballot_sync(FULLM, most == top);
+        P.donor = __shfl_sync(FULLM, at, __ffs(who) - 1);
+        P.PE = min(S.k0, top);
+        P.PT = (P.PE + 127) >> 7;
+      }
+      const int T = P.W * S.Hkv, columns = S.Hkv * S.nrc * P.PT;
+      int n_pre = 0;
+      if (columns > 0) {
+        const float share = static_cast<float>(S.Hkv) * S.TP * P.PT;
+        int groups = max(1, static_cast<int>(n_cta * (share / (share + T)) / S.chunk + 0.5f));
+        groups = min(groups, max(1, (T > 0 ? n_cta - 1 : n_cta) / S.chunk));
+        groups = min(groups, (columns + kPxMinPiece - 1) / kPxMinPiece);
+        P.cg = (columns + groups - 1) / groups;
+        P.groups = (columns + P.cg - 1) / P.cg;
+        n_pre = P.groups * S.chunk;
+      }
+      P.TB = T;
+      int want = max(1, n_cta - n_pre);
+      if (S.queue && T > 0) {
+        // the last item's worth of every CTA, in quarters
+        const int per_item = max(1, T / (S.Hkv * S.F));
+        const int tail = min(T, n_cta * per_item);
+        P.sB = max(kPxMinPiece, (per_item + 3) / 4);
+        // the item that holds unit T - tail
+        const int u = T - tail;
+        const int hk = u / P.W, rest = u - hk * P.W;
+        int f, before;
+        find(rest, f, before);
+        P.MA = hk * S.F + f;
+        P.uA = hk * P.W + before;
+        P.TB = T - P.uA;
+        want = (P.TB + P.sB - 1) / P.sB;
+      } else {
+        want = min(want, (T + kPxMinPiece - 1) / kPxMinPiece);
+      }
+      want = max(1, min(want, S.nb_max));
+      P.sB = max(1, (P.TB + want - 1) / want);
+      P.NB = (P.TB + P.sB - 1) / P.sB;
+      if (blockIdx.x == 0 && lane == 0) {
+        p.plan[0] = P.PT;
+        p.plan[1] = P.cg;
+        p.plan[2] = P.NB;
+      }
+    }
+    const int n_pre = P.groups * S.chunk;
+    const int pieces = n_pre + P.MA + P.NB;
+    auto own_item = [&](int hk, int f, int kt, int take, int nt, int len, int slot, int piece, int unit) -> bool {
+      // (unit: of the item's first tile among the units of the B pieces; piece < 0: of the queue)
+      PrefixItem it = {};
+      const int b = f / S.TO, rt = f - b * S.TO;
+      it.b = b;
+      it.hk = hk;
+      it.row0 = rt * 128;
+      it.nrows = min(128, S.R - it.row0);
+      it.pos0 = S.k0 + kt * 128;
+      it.cnt = take;
+      it.kv_end = len;
+      it.slot = slot;
+      it.len = len;
+      const int m = hk * S.F + f;
+      const bool whole = take == nt;
+      it.out = whole ? (S.stack ? p.own_row0 + m * S.rows : -1) : p.cut_row0 + (2 * piece + (kt == 0 ? 1 : 0)) * S.rows;
+      if (kt == 0 && lane == 0) {
+        const int parts = whole ? 1 : (unit + nt + P.sB - 1) / P.sB - piece;
+        if (S.stack) p.own_rec[m] = make_int2(piece, parts);
+        else if (!whole) p.cut_rec[piece] = make_int2(m, parts);
+      }
+      return give(it);
+    };
+    bool ok = true;
+    for (int id = blockIdx.x; ok && id < pieces;) {
+      if (id < n_pre) {
+        const int g = id / S.chunk, j = id - g * S.chunk;
+        const int c1 = min((g + 1) * P.cg, S.Hkv * S.nrc * P.PT);
+        for (int c = g * P.cg; c < c1 && ok;) {
+          const int U = c / P.PT, kt = c - U * P.PT, take = min(P.PT - kt, c1 - c);
+          const int hk = U / S.nrc, rt = (U - hk * S.nrc) * S.chunk + j;
+          if (rt < S.TP) {
+            PrefixItem it = {};
+            it.type = 1;
+            it.hk = hk;
+            it.row0 = rt * 128;
+            it.nrows = min(128, S.B * S.R - it.row0);
+            it.pos0 = kt * 128;
+            it.cnt = take;
+            it.kv_end = P.PE;
+            it.slot = P.donor;
+            it.out = ((g + U) * S.chunk + j) * 128;
+            ok = give(it);
+          }
+          c += take;
+        }
+      } else if (id < n_pre + P.MA) {
+        const int m = id - n_pre, hk = m / S.F, f = m - hk * S.F;
+        int slot, bad;
+        const int len = prefix_sequence(p, f / S.TO, slot, bad);
+        const int nt = prefix_own_tiles(S, len, f - f / S.TO * S.TO);
+        if (nt > 0) ok = own_item(hk, f, 0, nt, nt, len, slot, 0, 0);
+      } else {
+        const int piece = id - n_pre - P.MA;
+        const int u0 = piece * P.sB, u1 = min(P.TB, u0 + P.sB);
+        if (!S.stack && lane == 0) p.cut_rec[piece] = make_int2(-1, 0);
+        int hk = (P.uA + u0) / P.W;
+        const int rest = P.uA + u0 - hk * P.W;
+        int before, f;
+        find(rest, f, before);
+        int kt = rest - before;
+        for (int u = u0; u < u1 && ok;) {
+          const int b = f / S.TO;
+          int slot, bad;
+          const int len = prefix_sequence(p, b, slot, bad);
+          const int nt = prefix_own_tiles(S, len, f - b * S.TO);
+          if (nt > 0) {
+            const int take = min(nt - kt, u1 - u);
+            ok = own_item(hk, f, kt, take, nt, len, slot, piece, u - kt);
+            u += take;
+          }
+          kt = 0;
+          if (++f == S.F) {
+            f = 0;
+            hk++;
+          }
+        }
+      }
+      if (S.queue) {
+        int next = 0;
+        if (lane == 0) next = n_cta + atomicAdd(p.counter, 1);
+        id = __shfl_sync(FULLM, next, 0);
+      } else {
+        id += n_cta;
+      }
+    }
+    // (a row can outgrow its reference only in the first run, so settling once is enough)
+    if (ok) ok = settle();
+    if (ok) {
+      PrefixItem end = {};
+      end.type = -1;
+      publish(end);
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ Q K^T issuer
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    const bool leader = elect_one_sync();
+    constexpr uint32_t desc_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+    constexpr uint32_t idesc_qk = make_idesc_bf16(128, 128, 0, 0);
+    const uint32_t tmem_u = __shfl_sync(FULLM, tmem, 0);
+    auto desc64 = [](uint32_t lo) { return (static_cast<uint64_t>(desc_hi) << 32) | lo; };
+    const uint32_t q_lo = ((smem_u32(smem + L_::kQ) & 0x3FFFFu) >> 4) | (1u << 16);
+    const uint32_t k_lo0 = ((smem_u32(smem + L_::kK) & 0x3FFFFu) >> 4) | (1u << 16);
+    int stage = 0, round = 0;
+    int used[2] = {0, 0};
+    bool ok = true;
+    for (int n = 0; ok; n++) {
+      PrefixItem it;
+      if (!get_item(n, it)) break;
+      const int cnt = it.cnt;
+      ok = wait_all(Q_FULL, n & 1, kPxQFull, n);
+      for (int t = 0; t < cnt && ok; t++) {
+        const int j = t & 1;
+        ok = wait_all(K_FULL + stage, round & 1, kPxKFull, t);
+        if (!ok) break;
+        if (used[j] > 0) {
+          ok = wait_all(S_FREE + j, (used[j] - 1) & 1, kPxSFree, t);
+          if (!ok) break;
+        }
+        tc_fence_after();
+        const uint32_t k_lo = k_lo0 + stage * (L_::kTile >> 4);
+        const uint32_t tm_s = tmem_u + j * 128;
+        if (leader) {
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ks++) {
+            const uint32_t off = ((ks >> 2) * PANEL + (ks & 3) * 32) >> 4;
+            umma_ss(tm_s, desc64(q_lo + off), desc64(k_lo + off), idesc_qk, ks > 0 ? 1u : 0u);
+          }
+          umma_commit(BAR(S_FULL + j));
+          umma_commit(BAR(K_EMPTY + stage));
+          if (t == cnt - 1) umma_commit(BAR(Q_EMPTY));
+        }
+        __syncwarp();
+        used[j]++;
+        if (++stage == KS) {
+          stage = 0;
+          round++;
+        }
+      }
+      if (ok) item_done(n);
+    }
+    if (leader) umma_commit(BAR(QK_DRAIN));
+    __syncwarp();
+    mbar_wait(BAR(QK_DRAIN), 0);
+  } else if (warp == 2) {
+    // ------------------------------------------------------------------ P V issuer
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    const bool leader = elect_one_sync();
+    constexpr uint32_t desc_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+    constexpr uint32_t idesc_pv = make_idesc_bf16(128, D, 0, 1);
+    const uint32_t tmem_u = __shfl_sync(FULLM, tmem, 0);
+    auto desc64 = [](uint32_t lo) { return (static_cast<uint64_t>(desc_hi) << 32) | lo; };
+    const uint32_t v_lo0 = ((smem_u32(smem + L_::kV) & 0x3FFFFu) >> 4) | (static_cast<uint32_t>(PANEL >> 4) << 16);
+    auto issue_half = [&](uint32_t tm_buf, uint32_t v_lo, int half, uint32_t acc_first) {
+#pragma unroll
+      for (int kk = 0; kk < 4; kk++) {
+        const int ks = half * 4 + kk;
+        umma_ts(tmem_u + TM_O, tm_buf + ks * 8, desc64(v_lo + ks * (2048 >> 4)), idesc_pv, kk > 0 ? 1u : acc_first);
+      }
+    };
+    int stage = 0, round = 0, outputs = 0;
+    int used[2] = {0, 0};
+    bool ok = true;
+    for (int n = 0; ok; n++) {
+      PrefixItem it;
+      if (!get_item(n, it)) break;
+      if ((it.type >> 1) != 1) {
+        const int cnt = it.cnt;
+        for (int t = 0; t < cnt && ok; t++) {
+          const int j = t & 1;
+          ok = wait_all(V_FULL + stage, round & 1, kPxVFull, t);
+          if (!ok) break;
+          const int valid = it.kv_end - it.pos0 - t * 128;
+          if (valid < 128 && (valid & (S.page - 1)) != 0) {
+            // behind the last token its page may hold anything; P is zero there, and 0 * NaN is not
+            const int end = (valid + S.page - 1) & ~(S.page - 1);
+            uint8_t* tile = smem + L_::kV + stage * L_::kTile;
+            for (int c = valid * 8 + lane; c < end * 8; c += 32) {
+#pragma unroll
+              for (int pn = 0; pn < NPANEL; pn++) *reinterpret_cast<uint4*>(tile + pn * PANEL + c * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            fence_proxy_async();
+            __syncwarp();
+          }
+          ok = wait_all(P_FULL + 2 * j, used[j] & 1, kPxPFull, t);
+          if (!ok) break;
+          if (t == 0 && outputs > 0) {
+            ok = wait_all(O_FREE, (outputs - 1) & 1, kPxOFree, n);
+            if (!ok) break;
+          }
+          tc_fence_after();
+          const uint32_t v_lo = v_lo0 + stage * (L_::kTile >> 4);
+          const uint32_t tm_buf = tmem_u + TM_P + j * 64;
+          if (leader) issue_half(tm_buf, v_lo, 0, t > 0 ? 1u : 0u);
+          __syncwarp();
+          ok = wait_all(P_FULL + 2 * j + 1, used[j] & 1, kPxPFull, t);
+          if (!ok) break;
+          tc_fence_after();
+          if (leader) {
+            issue_half(tm_buf, v_lo, 1, 1u);
+            umma_commit(BAR(P_FREE + j));
+            umma_commit(BAR(V_EMPTY + stage));
+            if (t == cnt - 1) umma_commit(BAR(O_FULL));
+          }
+          __syncwarp();
+          used[j]++;
+          if (++stage == VS) {
+            stage = 0;
+            round++;
+          }
+        }
+        outputs++;
+      }
+      if (ok) item_done(n);
+    }
+    if (leader) umma_commit(BAR(PV_DRAIN));
+    __syncwarp();
+    mbar_wait(BAR(PV_DRAIN), 0);
+  } else if (warp == 15) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+  } else {
+    // ------------------------------------------------------------------ softmax groups + epilogue
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+    const int w = (warp - 4) >> 2;
+    const int row = ((warp & 3) << 5) + lane;
+    const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t tm_s = tmem + w * 128 + lane_off;
+    const uint32_t tm_p = tmem + TM_P + w * 64 + lane_off;
+    int tiles = 0;              // S tiles this group has taken, over all items
+    int used = 0;               // P tiles it has written
+    int mrefs = 0, outputs = 0; // items with a first-tile reference, with an output
+    float m_given = 0.f;
+    bool ok = true;
+    for (int n = 0; ok; n++) {
+      PrefixItem it;
+      if (!get_item(n, it)) break;
+      const int cnt = it.cnt, run = it.type >> 1;
+      if ((warp & 3) * 32 >= it.nrows) {
+        // no rows in this warp: its arrivals alone
+        for (int t = w; t < cnt && ok; t += 2) {
+          ok = wait_all(S_FULL + w, tiles & 1, kPxSFull, t);
+          if (!ok) break;
+          mbar_arrive(BAR(S_FREE + w));
+          tiles++;
+          if (run == 1) continue;
+          if (run == 0 && t == 0) mbar_arrive(BAR(MREF));
+          if (used > 0) ok = wait_all(P_FREE + w, (used - 1) & 1, kPxPFree, t);
+          if (!ok) break;
+          mbar_arrive(BAR(P_FULL + 2 * w));
+          mbar_arrive(BAR(P_FULL + 2 * w + 1));
+          used++;
+        }
+        if (!ok) break;
+        if (run == 0) mrefs++;
+        mbar_arrive(BAR(LSUM_A));
+        ok = wait_all(LSUM_A, n & 1, kPxLsum, n);
+        if (!ok) break;
+        mbar_arrive(BAR(LSUM_B));
+        ok = wait_all(LSUM_B, n & 1, kPxLsum, n);
+        if (!ok) break;
+        if (run != 1) {
+          ok = wait_all(O_FULL, outputs & 1, kPxOFull, n);
+          if (!ok) break;
+          outputs++;
+          mbar_arrive(BAR(O_FREE));
+        }
+        item_done(n);
+        continue;
+      }
+      // the thread's row: where it goes, how far it sees
+      int b = it.b, i = 0, g = 0, rel = 0x7fffffff;
+      if (row < it.nrows) {
+        int rr = it.row0 + row, len = it.len;
+        if (it.type & 1) {
+          b = rr / S.R;
+          rr -= b * S.R;
+          int slot, bad;
+          len = prefix_sequence(p, b, slot, bad);
+        }
+        i = rr / S.G;
+        g = rr - i * S.G;
+        rel = min(it.kv_end, S.causal ? len - S.L + i + 1 : len) - it.pos0;
+      }
+      float m_ref = run == 2 ? m_given : 0.f, m_max = -INFINITY;
+      uint64_t sum2[4] = {0ull, 0ull, 0ull, 0ull};
+      for (int t = w; t < cnt && ok; t += 2) {
+        ok = __all_sync(FULLM, wait_or_stop(S_FULL + w, tiles & 1, kPxSFull, t));
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t s[128];
+#pragma unroll
+        for (int c = 0; c < 4; c++) tmem_ld32(tm_s + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
+        tmem_wait_ld();
+        tc_fence_before();
+        mbar_arrive(BAR(S_FREE + w));
+        tiles++;
+        const int see = rel - t * 128;
+        if (__any_sync(FULLM, see < 128)) {
+#pragma unroll
+          for (int j = 0; j < 128; j++)
+            if (j >= see) s[j] = 0xff800000u;
+        }
+        if (run == 1 || (run == 0 && t == 0)) {
+          float mx8[8];
+#pragma unroll
+          for (int u = 0; u < 8; u++) mx8[u] = fmaxf(__uint_as_float(s[2 * u]), __uint_as_float(s[2 * u + 1]));
+#pragma unroll
+          for (int j = 16; j < 128; j += 16) {
+#pragma unroll
+            for (int u = 0; u < 8; u++) mx8[u] = max3f(mx8[u], __uint_as_float(s[j + 2 * u]), __uint_as_float(s[j + 2 * u + 1]));
+          }
+          const float mx = p.scale_log2 * fmaxf(max3f(mx8[0], mx8[1], mx8[2]), fmaxf(max3f(mx8[3], mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7])));
+          if (run == 1) {
+            m_max = fmaxf(m_max, mx);
+            continue;
+          }
+          m_ref = mx == -INFINITY ? 0.f : mx;      // (a row that sees nothing here sees nothing in later tiles either)
+          mref_s[row] = m_ref;
+          mbar_arrive(BAR(MREF));
+        } else if (run == 0 && t == 1) {
+          ok = __all_sync(FULLM, wait_or_stop(MREF, mrefs & 1, kPxMref, t));
+          if (!ok) break;
+          m_ref = mref_s[row];
+        }
+        const uint64_t c2 = pack_f32x2(p.scale_log2, p.scale_log2);
+        const uint64_t nm2 = pack_f32x2(-m_ref, -m_ref);
+#pragma unroll
+        for (int c = 0; c < 4; c++) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int j = 0; j < 16; j++) {
+            float x0, x1;
+            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[c * 32 + 2 * j]), __uint_as_float(s[c * 32 + 2 * j + 1])), c2, nm2), x0, x1);
+            const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+            sum2[j & 3] = add_f32x2(sum2[j & 3], pack_f32x2(p0, p1));
+            pk[j] = pack_bf16x2(p0, p1);
+          }
+          if (c == 0 && used > 0) {
+            ok = __all_sync(FULLM, wait_or_stop(P_FREE + w, (used - 1) & 1, kPxPFree, t));
+            if (!ok) break;
+          }
+          tmem_st16(tm_p + c * 16, pk);
+          if (c == 1 || c == 3) {
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(BAR(P_FULL + 2 * w + (c >> 1)));
+          }
+        }
+        if (ok) used++;
+      }
+      if (!ok) break;
+      if (run == 0) mrefs++;
+      float l_run;
+      {
+        float sa, sb;
+        unpack_f32x2(add_f32x2(add_f32x2(sum2[0], sum2[1]), add_f32x2(sum2[2], sum2[3])), sa, sb);
+        l_run = sa + sb;
+      }
+      // (a group without a tile of its own has no sum; the reference is the other one's)
+      if (run == 0 && row < it.nrows && !(l_run <= kFastRowSumLimit)) misc[FLAG + (n & 1)] = 1;
+      lsum_s[w * 128 + row] = run == 1 ? m_max : l_run;
+      mbar_arrive(BAR(LSUM_A));
+      ok = __all_sync(FULLM, wait_or_stop(LSUM_A, n & 1, kPxLsum, n));
+      if (!ok) break;
+      const float other = lsum_s[(1 - w) * 128 + row];
+      const bool again = misc[FLAG + (n & 1)] != 0;
+      if (run == 0 && cnt == 1 && w == 1) m_ref = mref_s[row];
+      mbar_arrive(BAR(LSUM_B));
+      ok = __all_sync(FULLM, wait_or_stop(LSUM_B, n & 1, kPxLsum, n));
+      if (!ok) break;
+      if (run == 1) {
+        m_given = fmaxf(m_max, other);
+        if (m_given == -INFINITY) m_given = 0.f;
+        item_done(n);
+        continue;
+      }
+      if (tid == 128) {
+        misc[FLAG + (n & 1)] = 0;
+        if (again) {
+          redo[misc[LISTED]] = it;
+          misc[LISTED] = misc[LISTED] + 1;
+          misc[RECOMPUTED] = misc[RECOMPUTED] + 1;
+        }
+      }
+      ok = __all_sync(FULLM, wait_or_stop(O_FULL, outputs & 1, kPxOFull, n));
+      if (!ok) break;
+      outputs++;
+      tc_fence_after();
+      constexpr int HALF = D / 2;
+      uint32_t o0[HALF];
+#pragma unroll
+      for (int c = 0; c < HALF / 32; c++)
+        tmem_ld32(tmem + TM_O + lane_off + w * HALF + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&o0[c * 32]));
+      tmem_wait_ld();
+      tc_fence_before();
+      mbar_arrive(BAR(O_FREE));
+      if (!again && row < it.nrows) {
+        const float sum = l_run + other;
+        const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+        const float lse2 = sum != 0.f ? m_ref + log2f(sum) : -INFINITY;
+        if (it.out >= 0) {
+          const int64_t at = it.out + row;
+          if (w == 0) p.part_lse2[at] = lse2;
+          float* dst = p.part_o + at * D + w * HALF;
+#pragma unroll
+          for (int c = 0; c < HALF / 8; c++) {
+            uint32_t r[8];
+#pragma unroll
+            for (int x = 0; x < 8; x++) r[x] = __float_as_uint(__uint_as_float(o0[c * 8 + x]) * inv);
+            st_global_v8(dst + c * 8, r);
+          }
+        } else {
+          const int head = it.hk * S.G + g;
+          if (w == 0 && p.lse != nullptr) p.lse[(static_cast<int64_t>(b) * S.Hkv * S.G + head) * S.L + i] = lse2 * 0.6931471805599453f;
+          uint4* dst = reinterpret_cast<uint4*>(p.o + b * p.q.stride_b + head * p.q.stride_h + i * p.q.stride_n + w * HALF);
+#pragma unroll
+          for (int c = 0; c < HALF / 8; c++) {
+            uint4 v;
+            v.x = pack_bf16x2(__uint_as_float(o0[c * 8 + 0]) * inv, __uint_as_float(o0[c * 8 + 1]) * inv);
+            v.y = pack_bf16x2(__uint_as_float(o0[c * 8 + 2]) * inv, __uint_as_float(o0[c * 8 + 3]) * inv);
+            v.z = pack_bf16x2(__uint_as_float(o0[c * 8 + 4]) * inv, __uint_as_float(o0[c * 8 + 5]) * inv);
+            v.w = pack_bf16x2(__uint_as_float(o0[c * 8 + 6]) * inv, __uint_as_float(o0[c * 8 + 7]) * inv);
+            dst[c] = v;
+          }
+        }
+      }
+      item_done(n);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 2) tmem_dealloc(tmem, 512);
+  if (tid == 0) {
+    p.cta_err[2 * blockIdx.x] = make_int4(misc[ERR], misc[ERR + 1], misc[ERR + 2], misc[ERR + 3]);
+    p.cta_err[2 * blockIdx.x + 1] = make_int4(misc[RECOMPUTED], 0, 0, 0);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ joining the parts
+// A warp per row; the lanes hold D/32 channels each.  Parts are joined in the order of the key axis.  Stacked rows: the groups of the beginning, whose numbers
+// follow from the plan, and the parts of the row's own item.  Else: the rows of the items that a B piece begins and another ends (a CTA per piece).
+constexpr int kPxMergeWarps = 8;
+
+template <int D>
+__device__ __forceinline__ void prefix_merge_row(const PrefixParams& p, int first, int step, int n_first, int second, int n_second, int second_at1, int second_step,
+                                                 int b, int head, int i) {
+  // parts 0 .. n_first-1 at first + k*step; then one at `second`, and the others at second_at1 + (k-1)*second_step
+  constexpr int C = D / 32;
+  const int lane = threadIdx.x & 31;
+  const int n = n_first + n_second;
+  auto at = [&](int k) {
+    if (k < n_first) return first + k * step;
+    k -= n_first;
+    return k == 0 ? second : second_at1 + (k - 1) * second_step;
+  };
+  float m = -INFINITY;
+  bool nan = false;
+  for (int k = lane; k < n; k += 32) {
+    const float x = p.part_lse2[at(k)];
+    nan = nan || x != x;
+    m = fmaxf(m, x);
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  nan = __any_sync(0xffffffffu, nan);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float o[C] = {}, den = 0.f;
+#pragma unroll 4
+  for (int k = 0; k < n; k++) {
+    const int64_t r = at(k);
+    const float wt = exp2f(p.part_lse2[r] - ref);
+    den += wt;
+    if constexpr (C == 4) {
+      const float4 x = *reinterpret_cast<const float4*>(p.part_o + r * D + lane * 4);
+      o[0] += wt * x.x;
+      o[1] += wt * x.y;
+      o[2] += wt * x.z;
+      o[3] += wt * x.w;
+    } else {
+      const float2 x = *reinterpret_cast<const float2*>(p.part_o + r * D + lane * 2);
+      o[0] += wt * x.x;
+      o[1] += wt * x.y;
+    }
+  }
+  const float inv = nan ? NAN : den > 0.f ? 1.0f / den : 0.f;
+  __nv_bfloat16* dst = p.o + b * p.q.stride_b + head * p.q.stride_h + i * p.q.stride_n + lane * C;
+  if constexpr (C == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+  else *reinterpret_cast<uint32_t*>(dst) = pack_bf16x2(o[0] * inv, o[1] * inv);
+  if (lane == 0 && p.lse != nullptr)
+    p.lse[(static_cast<int64_t>(b) * p.s.Hkv * p.s.G + head) * p.s.L + i] = nan ? NAN : den > 0.f ? (ref + log2f(den)) * 0.6931471805599453f : -INFINITY;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kPxMergeWarps * 32) prefix_merge_kernel(const __grid_constant__ PrefixParams p, int n_cta) {
+  pdl_wait();
+  pdl_launch();
+  const PrefixShape& S = p.s;
+  const int warp = threadIdx.x >> 5;
+  if (blockIdx.x == 0 && warp == 0) {
+    // the status record: the first CTA's error, and how many items were recomputed
+    const int lane = threadIdx.x;
+    int4 err = make_int4(0, 0, 0, 0);
+    int again = 0;
+    for (int c = lane; c < n_cta; c += 32) {
+      const int4 e = p.cta_err[2 * c];
+      if (err.x == 0) err = e;
+      again += p.cta_err[2 * c + 1].x;
+    }
+    again = __reduce_add_sync(0xffffffffu, again);
+    const unsigned who = __ballot_sync(0xffffffffu, err.x != 0);
+    const int from = who ? __ffs(who) - 1 : 0;
+    if (lane == from) {
+      p.status->code = err.x;
+      p.status->where = err.y;
+      p.status->item = err.z;
+      p.status->aux = err.w;
+      p.status->redo_count = again;
+      p.status->next_item = 0;
+    }
+  }
+  if (S.stack) {
+    const int PT = p.plan[0], cg = p.plan[1];
+    const int rows = S.B * S.R;                // of a key head, stacked
+    const int64_t r = static_cast<int64_t>(blockIdx.x) * kPxMergeWarps + warp;
+    if (r >= static_cast<int64_t>(rows) * S.Hkv) return;
+    const int hk = static_cast<int>(r / rows), rho = static_cast<int>(r - static_cast<int64_t>(hk) * rows);
+    const int b = rho / S.R, rr = rho - b * S.R, i = rr / S.G, g = rr - i * S.G;
+    int first = 0, n_first = 0;
+    if (PT > 0) {
+      const int rt = rho >> 7, rc = rt / S.chunk, j = rt - rc * S.chunk, U = hk * S.nrc + rc;
+      const int g0 = U * PT / cg, g1 = ((U + 1) * PT - 1) / cg;
+      first = ((g0 + U) * S.chunk + j) * 128 + (rho & 127);
+      n_first = g1 - g0 + 1;
+    }
+    int slot, bad, second = 0, n_second = 0, next = 0;
+    const int len = prefix_sequence(p, b, slot, bad), rt = rr >> 7;
+    if (prefix_own_tiles(S, len, rt) > 0) {
+      const int m = hk * S.F + b * S.TO + rt, in = rr & 127;
+      int2 rec = p.own_rec[m];
+      // (a kernel that gave up, for a wait that ran out, may have left records unwritten)
+      if (rec.x < 0 || rec.y < 1 || (rec.y > 1 && rec.x > p.plan[2] - rec.y)) rec = make_int2(0, 0);
+      n_second = rec.y;
+      second = rec.y == 1 ? p.own_row0 + m * S.rows + in : p.cut_row0 + (2 * rec.x + 1) * S.rows + in;
+      next = p.cut_row0 + (2 * rec.x + 2) * S.rows + in;
+    }
+    prefix_merge_row<D>(p, first, S.chunk * 128, n_first, second, n_second, next, 2 * S.rows, b, hk * S.G + g, i);
+  } else {
+    const int piece = blockIdx.x;
+    if (piece >= p.plan[2]) return;
+    const int2 rec = p.cut_rec[piece];
+    if (rec.x < 0 || rec.x >= S.Hkv * S.F || rec.y < 1 || rec.y > p.plan[2] - piece) return;      // (also one that a kernel that gave up did not write)
+    const int hk = rec.x / S.F, f = rec.x - hk * S.F, b = f / S.TO, row0 = (f - b * S.TO) * 128;
+    const int rows = min(128, S.R - row0);
+    for (int in = blockIdx.y * kPxMergeWarps + warp; in < rows; in += gridDim.y * kPxMergeWarps) {
+      const int rr = row0 + in, i = rr / S.G, g = rr - i * S.G;
+      prefix_merge_row<D>(p, 0, 0, 0, p.cut_row0 + (2 * piece + 1) * S.rows + in, rec.y, p.cut_row0 + (2 * piece + 2) * S.rows + in, 2 * S.rows, b,
+                          hk * S.G + g, i);
+    }
+  }
+}
+
+}  // namespace avsa
