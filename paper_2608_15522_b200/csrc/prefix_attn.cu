@@ -18,7 +18,7 @@ struct PrefixLayout {
   int n_cta;
   size_t rows;                  // partial rows
   int own_row0, cut_row0;
-  size_t plan, cta_err, own_rec, cut_rec, lse, o, total;       // offsets in the workspace
+  size_t plan, cta_err, own_rec, cut_rec, redo, lse, o, total;       // offsets in the workspace
 };
 
 // False: more units than 32 bits count.
@@ -40,9 +40,9 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   s.page = page;
   s.page_shift = page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7;
   const int sms = persistent_grid(1 << 30);
-  // Stacked, the beginning's key tiles are walked TP times a head instead of F times, but every row goes through the merge: its parts are
-  // 2 KB written and read, a tile is 64 KB.
-  s.stack = TP * PT + RS / 32 + 2 <= F * PT;
+  // Stacked, the beginning's key tiles are walked TP times a head instead of F times, but every row goes through the merge, which costs a key
+  // tile's time for about six rows (149760 rows: 108 us, a tile of every SM 0.8).
+  s.stack = TP * PT + RS / 6 + 2 <= F * PT;
   const long long units = F * Hkv * most + (s.stack ? TP * Hkv * PT : 0);
   y.n_cta = static_cast<int>(units < sms ? units : sms);
   if (y.n_cta < 1) y.n_cta = 1;
@@ -53,6 +53,8 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     s.nrc = (s.TP + side - 1) / side;
     s.chunk = (s.TP + s.nrc - 1) / s.nrc;
   }
+  s.pre_narrow = RS <= kPxNarrow;
+  s.own_narrow = R <= kPxNarrow;
   s.queue = TO > 1 && F * Hkv > y.n_cta;
   s.nb_max = s.queue ? 8 * y.n_cta : y.n_cta;
   const size_t pre = s.stack ? (static_cast<size_t>(y.n_cta) + static_cast<size_t>(Hkv) * s.nrc * s.chunk) * 128 : 0;
@@ -61,6 +63,12 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   if (y.rows > 0x7fffffffu) return false;
   y.own_row0 = static_cast<int>(pre);
   y.cut_row0 = static_cast<int>(pre + own);
+  s.by_R = Divisor(s.R);
+  s.by_G = Divisor(s.G);
+  s.by_TO = Divisor(s.TO);
+  s.by_F = Divisor(s.F);
+  s.by_chunk = Divisor(s.chunk > 0 ? s.chunk : 1);
+  s.by_nrc = Divisor(s.nrc > 0 ? s.nrc : 1);
   size_t at = kStatusBytes;
   y.plan = at;
   at += 256;
@@ -70,6 +78,8 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   at += align_up(s.stack ? static_cast<size_t>(F) * Hkv * 8 : 0, 256);
   y.cut_rec = at;
   at += align_up(static_cast<size_t>(s.nb_max) * 8, 256);
+  y.redo = at;
+  at += align_up(static_cast<size_t>(y.n_cta) * kPxRedo * sizeof(PrefixItem), 256);
   y.lse = at;
   at += align_up(y.rows * 4, 256);
   y.o = at;
@@ -85,9 +95,13 @@ static int launch_prefix(const PrefixLayout& y, const avsa_bf16_4d& k, const avs
       !encode_bf16_tile_map(&tv, v.ptr, s.pages, s.Hkv, s.page, D, v.stride_b, v.stride_h, v.stride_n, s.page))
     return AVSA_ERR_CUDA;
   if (s.queue && launch_pdl(clear_counter_kernel, 1, 1, 0, st, p.counter) != cudaSuccess) return AVSA_ERR_CUDA;
-  if (cudaFuncSetAttribute(prefix_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PrefixSmem<D>::kTotal) != cudaSuccess) return AVSA_ERR_CUDA;
-  if (launch_pdl(prefix_attn_kernel<D>, y.n_cta, kPxThreads, PrefixSmem<D>::kTotal, st, tk, tv, p) != cudaSuccess) return AVSA_ERR_CUDA;
-  dim3 grid(static_cast<unsigned>(s.nb_max), s.rows > 64 ? 2 : 1);
+  const bool slim = s.own_narrow || (s.stack && s.pre_narrow), wide = !s.own_narrow || (s.stack && !s.pre_narrow);
+  auto kernel = slim && wide ? prefix_attn_kernel<D, kPxBoth> : slim ? prefix_attn_kernel<D, kPxSlim> : prefix_attn_kernel<D, kPxWide>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PrefixSmem<D>::kTotal) != cudaSuccess) return AVSA_ERR_CUDA;
+  if (launch_pdl(kernel, y.n_cta, kPxThreads, PrefixSmem<D>::kTotal, st, tk, tv, p) != cudaSuccess) return AVSA_ERR_CUDA;
+  // (cut rows: at most nb_max times 128, a warp each)
+  const long long most = static_cast<long long>(s.nb_max) * 128 / kPxMergeWarps, ctas = 8ll * y.n_cta;
+  dim3 grid(static_cast<unsigned>(most < ctas ? most : ctas));
   if (s.stack) grid = dim3(static_cast<unsigned>((static_cast<long long>(s.B) * s.R * s.Hkv + kPxMergeWarps - 1) / kPxMergeWarps));
   if (launch_pdl(prefix_merge_kernel<D>, grid, kPxMergeWarps * 32, 0, st, p, y.n_cta) != cudaSuccess) return AVSA_ERR_CUDA;
   return cudaGetLastError() == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
@@ -153,6 +167,7 @@ extern "C" int avsa_prefix_attn(int B, int H, int Hkv, int L, int d, int page, i
   p.cta_err = reinterpret_cast<int4*>(w + y.cta_err);
   p.own_rec = reinterpret_cast<int2*>(w + y.own_rec);
   p.cut_rec = reinterpret_cast<int2*>(w + y.cut_rec);
+  p.redo = reinterpret_cast<PrefixItem*>(w + y.redo);
   p.part_lse2 = reinterpret_cast<float*>(w + y.lse);
   p.part_o = reinterpret_cast<float*>(w + y.o);
   p.own_row0 = y.own_row0;

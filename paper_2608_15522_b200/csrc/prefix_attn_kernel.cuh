@@ -23,6 +23,8 @@
 #pragma once
 #include <math.h>
 
+#include <type_traits>
+
 #include "attn_persist_kernel.cuh"
 
 namespace avsa {
@@ -31,7 +33,8 @@ constexpr int kPxThreads = 512;
 // 512 x 128 registers at launch; then 8 service warps of 64 and 8 softmax warps of 192: 65536 both ways.
 constexpr int kPxServiceRegs = 64, kPxSoftmaxRegs = 192;
 static_assert(8 * 32 * kPxServiceRegs + 8 * 32 * kPxSoftmaxRegs <= kPxThreads * 128, "setmaxnreg budget exceeded");
-constexpr int kPxRing = 4, kPxRedo = 16;
+constexpr int kPxNarrow = 32;            // query rows of a narrow item, at most
+constexpr int kPxRing = 4, kPxRedo = 14;
 constexpr int kPxQWarps = 2;             // warps 13 and 14 gather query rows
 constexpr int kPxConsumers = 4 + kPxQWarps + 8;      // warps that read the item ring
 
@@ -39,6 +42,25 @@ enum PrefixWhere {
   kPrefixPage = 221, kPrefixLength, kPrefixSeq, kPxItem, kPxItemEmpty, kPxQEmpty, kPxQFull, kPxKEmpty, kPxVEmpty, kPxKFull, kPxVFull, kPxSFull, kPxSFree,
   kPxPFull, kPxPFree, kPxOFull, kPxOFree, kPxMref, kPxLsum, kPxAlign
 };
+
+// A divisor known on the host: n / d for 0 <= n < 2^31 without a division (which is 30 dependent instructions).
+struct Divisor {
+  uint32_t d, mul, shift;
+  __host__ __device__ Divisor() {}
+  __host__ explicit Divisor(int n) : d(static_cast<uint32_t>(n)), mul(0), shift(31) {
+    while ((1ull << (shift - 31)) < d) shift++;
+    mul = static_cast<uint32_t>(((1ull << shift) + d - 1) / d);
+  }
+  __device__ __forceinline__ int div(int n) const { return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(n)) * mul) >> shift); }
+};
+// One that is not: the quotient of floats, put right.
+__device__ __forceinline__ int float_div(int a, int b) {
+  int q = __float2int_rz(__fdividef(static_cast<float>(a), static_cast<float>(b)));
+  int r = a - q * b;
+  while (r < 0) q--, r += b;
+  while (r >= b) q++, r -= b;
+  return q;
+}
 
 // What of the work depends on sizes alone.
 struct PrefixShape {
@@ -50,9 +72,11 @@ struct PrefixShape {
   int TP, chunk, nrc;  // row tiles of the stacked rows, taken `chunk` at a time (nrc times)
   int rows;            // rows of an own item's partial result: min(128, R)
   int queue;           // whole items off a queue
+  int pre_narrow, own_narrow;  // rows of the stacked items, of the own ones: at most kPxNarrow
   int nb_max;          // B pieces at most
   int page, page_shift, pages, seqs, width;
   int causal;
+  Divisor by_R, by_G, by_TO, by_F, by_chunk, by_nrc;
 };
 
 struct PrefixParams {
@@ -72,16 +96,17 @@ struct PrefixParams {
   float* part_o;       // [rows][D]: prefix slots of 128 rows, own items (stack), two cut ends a B piece
   float* part_lse2;
   int own_row0, cut_row0;      // first rows of the latter two
+  struct PrefixItem* redo;     // [CTAs][kPxRedo] items to run again
 };
 
 struct PrefixItem {
-  int type;            // -1: no more; bit 0: stacked rows, bits 1-2: 0, or 1 maxima only, 2 with given maxima
+  int type;            // -1: no more; bit 0: stacked rows, bits 1-2: 0, or 1 maxima only, 2 with given maxima, bit 3: narrow
   int b, hk, row0, nrows;
   int pos0, cnt, kv_end;       // first key, key tiles, end of the keys
   int slot;            // row of the page table
   int len;             // own items: tokens of the sequence
   int out;             // first partial row, -1: final rows
-  int pad;
+  int group;           // narrow: the softmax group whose item it is
 };
 static_assert(sizeof(PrefixItem) == 48, "three 16-byte accesses");
 
@@ -89,15 +114,17 @@ template <int D>
 struct PrefixSmem {
   static constexpr int kTile = 128 * D * 2;
   static constexpr int kKS = D == 128 ? 3 : 6, kVS = D == 128 ? 3 : 6;
+  // Query rows: wide, 128 of them (64 channels: two buffers); narrow, two buffers of 32 rows, in front of the two groups' P in the second half of each 16 KB
   static constexpr int kQ = 0;
-  static constexpr int kK = kTile;
+  static constexpr int kQSlot = D == 64 ? 16384 : 0, kNarrowSlot = 32 * 128, kNarrowP = 8192;
+  static constexpr int kK = 32768;
   static constexpr int kV = kK + kKS * kTile;
   static constexpr int kBars = kV + kVS * kTile;
-  static constexpr int kNumBars = 2 + 2 * kKS + 2 * kVS + 13 + 2 * kPxRing + 4;
-  static constexpr int kStats = (kBars + kNumBars * 8 + 15) / 16 * 16;       // float mref[128], lsum[2][128]
+  static constexpr int kNumBars = 4 + 2 * kKS + 2 * kVS + 13 + 2 * kPxRing + 4 + 22;
+  static constexpr int kStats = (kBars + kNumBars * 8 + 15) / 16 * 16;       // float mref[128], lsum[2][128]; narrow: mref[2][32], lsum[2][4][32]
   static constexpr int kItems = kStats + 3 * 128 * 4;
-  static constexpr int kRedo = kItems + 48 * kPxRing;
-  static constexpr int kMisc = kRedo + 48 * kPxRedo;                          // tmem base, stop, redo flags [2], listed, recomputed, error [4]
+  static constexpr int kPages = kItems + 48 * kPxRing;                        // int[kPxRing][32]: an item's first pages
+  static constexpr int kMisc = kPages + 128 * kPxRing;                        // tmem base, stop, redo flags [2], listed, recomputed, error [4]
   static constexpr int kTotal = kMisc + 48;
   static_assert(kTotal <= 232448, "shared memory of a CTA exceeded");
 };
@@ -116,7 +143,7 @@ __device__ __forceinline__ int prefix_sequence(const PrefixParams& p, int b, int
 // Key tiles of an own item: row tile rt of a sequence of n tokens.
 __device__ __forceinline__ int prefix_own_tiles(const PrefixShape& s, int n, int rt) {
   int end = n;
-  if (s.causal) end = n - s.L + min(s.L - 1, (rt * 128 + 127) / s.G) + 1;
+  if (s.causal) end = n - s.L + min(s.L - 1, s.by_G.div(rt * 128 + 127)) + 1;
   const int x = end - s.k0;
   const int t = x > 0 ? (x + 127) >> 7 : 0;
   return s.stack ? t : max(t, 1);      // (without a beginning of its own every row tile is written by somebody)
@@ -124,6 +151,23 @@ __device__ __forceinline__ int prefix_own_tiles(const PrefixShape& s, int n, int
 
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)) : "memory");
+}
+
+// Over the lanes of a warp: lane l gets value l mod N of all lanes, combined.  Every step halves the values that a lane holds.
+template <int N, class Op>
+__device__ __forceinline__ float lane_reduce(float (&v)[N], Op op) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int d = N / 2; d > 0; d >>= 1) {
+    const bool upper = (lane & d) != 0;
+#pragma unroll
+    for (int i = 0; i < d; i++) {
+      const float give = upper ? v[i] : v[i + d], keep = upper ? v[i + d] : v[i];
+      v[i] = op(keep, __shfl_xor_sync(0xffffffffu, give, d));
+    }
+  }
+  if constexpr (N == 16) v[0] = op(v[0], __shfl_xor_sync(0xffffffffu, v[0], 16));
+  return v[0];
 }
 
 constexpr int kPxMinPiece = 4;       // key tiles: a CTA with fewer ends later than one that takes another's as well
@@ -136,35 +180,55 @@ struct PrefixPlan {
   int TB, sB, NB;              // units of the B pieces, of one, pieces
 };
 
-template <int D>
+// The CTA's first error, for the merge kernel to report.  (Not inlined: a call's first items run through cold code, and what stands between the lines that
+// they need is fetched with them.)
+__device__ __noinline__ void px_report(int* err, int code, int where, int item, int aux) {
+  if (atomicCAS(err, 0, code) == 0) {
+    err[1] = where;
+    err[2] = item;
+    err[3] = aux;
+  }
+}
+
+// Which items a call has.  A kernel for one kind alone is faster: its loops share the instruction cache with less.
+enum { kPxWide = 1, kPxSlim = 2, kPxBoth = 3 };
+
+template <int D, int KINDS>
 __global__ void __launch_bounds__(kPxThreads, 1)
 prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const __grid_constant__ PrefixParams p) {
   using L_ = PrefixSmem<D>;
   constexpr int NPANEL = D / 64, PANEL = 128 * 128, KS = L_::kKS, VS = L_::kVS;
   constexpr unsigned FULLM = 0xffffffffu;
+  auto is_narrow = [](int type) { return KINDS == kPxBoth ? (type & 8) != 0 : KINDS == kPxSlim; };
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const PrefixShape& S = p.s;
 
   const uint32_t bar0 = smem_u32(smem + L_::kBars);
   auto BAR = [&](int i) { return bar0 + static_cast<uint32_t>(i) * 8u; };
-  constexpr int Q_FULL = 0, Q_EMPTY = 1, K_FULL = 2, K_EMPTY = K_FULL + KS, V_FULL = K_EMPTY + KS, V_EMPTY = V_FULL + VS,
+  constexpr int Q_FULL = 0, Q_EMPTY = 2, K_FULL = 4, K_EMPTY = K_FULL + KS, V_FULL = K_EMPTY + KS, V_EMPTY = V_FULL + VS,
                 S_FULL = V_EMPTY + VS, S_FREE = S_FULL + 2, P_FULL = S_FREE + 2 /* + 2*group + half */, P_FREE = P_FULL + 4, O_FULL = P_FREE + 2,
                 O_FREE = O_FULL + 1, MREF = O_FREE + 1, ITEM_FULL = MREF + 1, ITEM_EMPTY = ITEM_FULL + kPxRing, QK_DRAIN = ITEM_EMPTY + kPxRing,
-                PV_DRAIN = QK_DRAIN + 1, LSUM_A = PV_DRAIN + 1, LSUM_B = LSUM_A + 1;
-  static_assert(LSUM_B + 1 <= L_::kNumBars, "barrier table too small");
-  constexpr uint32_t TM_O = 256, TM_P = 256 + D;      // tensor memory: S of group 0 | S of group 1 | O | P of group 0 | P of group 1
+                PV_DRAIN = QK_DRAIN + 1, LSUM_A = PV_DRAIN + 1, LSUM_B = LSUM_A + 1,
+                NS_FULL = LSUM_B + 1 /* + 2*group + buffer */, NS_FREE = NS_FULL + 4, NP_FULL = NS_FREE + 4 /* + group */, NP_FREE = NP_FULL + 2,
+                NO_FULL = NP_FREE + 2, NO_FREE = NO_FULL + 2, NREF = NO_FREE + 2, NSUM = NREF + 2, NREAD = NSUM + 2;
+  static_assert(NREAD + 2 <= L_::kNumBars, "barrier table too small");
+  // tensor memory: S of group 0 | S of group 1 | O | P of group 0 | P of group 1; narrow: two S buffers of 32 columns of each group | O of each group
+  constexpr uint32_t TM_O = 256, TM_P = 256 + D, TM_NO = 128;
   float* mref_s = reinterpret_cast<float*>(smem + L_::kStats);
   float* lsum_s = mref_s + 128;
   PrefixItem* ring = reinterpret_cast<PrefixItem*>(smem + L_::kItems);
-  PrefixItem* redo = reinterpret_cast<PrefixItem*>(smem + L_::kRedo);
+  int* ring_pages = reinterpret_cast<int*>(smem + L_::kPages);
+  PrefixItem* redo = p.redo + blockIdx.x * kPxRedo;
   volatile int* misc = reinterpret_cast<volatile int*>(smem + L_::kMisc);
   enum { TMEM = 0, STOP, FLAG /* + item parity */, LISTED = FLAG + 2, RECOMPUTED, ERR };
 
   const bool aligned = (smem_u32(smem) & 1023u) == 0u;
   if (tid == 0) {
-    mbar_init(BAR(Q_FULL), 32 * kPxQWarps);
-    mbar_init(BAR(Q_EMPTY), 1);
+    for (int s = 0; s < 2; s++) {
+      mbar_init(BAR(Q_FULL + s), 32 * kPxQWarps);
+      mbar_init(BAR(Q_EMPTY + s), 1);
+    }
     for (int s = 0; s < KS; s++) {
       mbar_init(BAR(K_FULL + s), 1);
       mbar_init(BAR(K_EMPTY + s), 1);
@@ -191,6 +255,19 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     mbar_init(BAR(PV_DRAIN), 1);
     mbar_init(BAR(LSUM_A), 256);
     mbar_init(BAR(LSUM_B), 256);
+    for (int g = 0; g < 2; g++) {
+      for (int k = 0; k < 2; k++) {
+        mbar_init(BAR(NS_FULL + 2 * g + k), 1);
+        mbar_init(BAR(NS_FREE + 2 * g + k), 128);
+      }
+      mbar_init(BAR(NP_FULL + g), 128);
+      mbar_init(BAR(NP_FREE + g), 1);
+      mbar_init(BAR(NO_FULL + g), 1);
+      mbar_init(BAR(NO_FREE + g), 128);
+      mbar_init(BAR(NREF + g), 32);
+      mbar_init(BAR(NSUM + g), 128);
+      mbar_init(BAR(NREAD + g), 128);
+    }
     for (int i = STOP; i < ERR + 4; i++) misc[i] = 0;
     fence_mbar_init();
     prefetch_tmap(&tmk);
@@ -207,14 +284,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
   pdl_wait();
   pdl_launch();
 
-  // The CTA's first error, for the merge kernel to report.
-  auto report = [&](int code, int where, int item, int aux) {
-    if (atomicCAS(const_cast<int*>(&misc[ERR]), 0, code) == 0) {
-      misc[ERR + 1] = where;
-      misc[ERR + 2] = item;
-      misc[ERR + 3] = aux;
-    }
-  };
+  auto report = [&](int code, int where, int item, int aux) { px_report(const_cast<int*>(misc) + ERR, code, where, item, aux); };
   auto wait_or_stop = [&](int bar, uint32_t parity, int where, int tag) -> bool {
     if (mbar_try_wait(BAR(bar), parity)) return true;
     const long long t0 = clock64();
@@ -256,24 +326,23 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     const int ppt_shift = 7 - S.page_shift, ppt = 1 << ppt_shift;      // pages of a tile
     int stage = 0, round = 0, loads = 0;
     bool ok = true;
+#pragma unroll 1
     for (int n = 0; ok; n++) {
       PrefixItem it;
       if (!get_item(n, it)) break;
-      if (is_k || (it.type >> 1) != 1) {
+      if (is_k || ((it.type >> 1) & 3) != 1) {
         const int32_t* row = p.table + static_cast<int64_t>(max(it.slot, 0)) * S.width;
-        const int e0 = it.pos0 >> S.page_shift, e1 = (it.kv_end + S.page - 1) >> S.page_shift;      // its pages
-        const int per = 32 >> ppt_shift;       // tiles whose pages a warp reads at once
+        const int e0 = it.pos0 >> S.page_shift;      // its pages
+        const int e1 = min(e0 + (it.cnt << ppt_shift), (it.kv_end + S.page - 1) >> S.page_shift);
+        const int per = 32 >> ppt_shift;       // tiles whose pages a warp holds at once; the first come with the item
+        int mine = ring_pages[(n % kPxRing) * 32 + lane];
+#pragma unroll 1
         for (int t0 = 0; t0 < it.cnt && ok; t0 += per) {
-          const int e = e0 + (t0 << ppt_shift) + lane;
-          int mine = S.pages;                  // behind the last page: beyond the pool, where the copy reads zeros
-          if (e < e1 && e < e0 + (it.cnt << ppt_shift)) {
-            mine = row[e];
-            if (mine < 0 || mine >= S.pages) {
-              report(AVSA_ERR_BAD_TABLE, kPrefixPage, it.slot, e);
-              mine = S.pages;
-            }
-          }
+          int next = S.pages;                  // behind the last page: beyond the pool, where the copy reads zeros
+          const int e = e0 + ((t0 + per) << ppt_shift) + lane;
+          if (e < e1) next = row[e];
           const int nn = min(per, it.cnt - t0);
+#pragma unroll 1
           for (int j = 0; j < nn; j++) {
             const int id = __shfl_sync(FULLM, mine, (j << ppt_shift) + (lane & (ppt - 1)));
             int good = 1;
@@ -297,6 +366,11 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
               round++;
             }
           }
+          if (next < 0 || next > S.pages) {
+            report(AVSA_ERR_BAD_TABLE, kPrefixPage, it.slot, e);
+            next = S.pages;
+          }
+          mine = next;
         }
       }
       if (ok) item_done(n);
@@ -309,241 +383,272 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     constexpr int VPR = D / 8, RPI = 32 / VPR;      // 16-byte vectors of a row; rows of an instruction
     const uint32_t base = smem_u32(smem + L_::kQ);
     bool ok = true;
+#pragma unroll 1
     for (int n = 0; ok; n++) {
       PrefixItem it;
       if (!get_item(n, it)) break;
-      if (n > 0) ok = wait_all(Q_EMPTY, (n - 1) & 1, kPxQEmpty, n);
+      const bool narrow = is_narrow(it.type);
+      if (n >= 2) ok = wait_all(Q_EMPTY + (n & 1), ((n >> 1) - 1) & 1, kPxQEmpty, n);
+      if (ok && n >= 1 && !narrow && L_::kQSlot == 0) ok = wait_all(Q_EMPTY + ((n - 1) & 1), ((n - 1) >> 1) & 1, kPxQEmpty, n);      // one buffer
       if (!ok) break;
+      const uint32_t dst = base + (n & 1) * (narrow ? L_::kNarrowSlot : L_::kQSlot);
+#pragma unroll 1
       for (int r0 = (warp - 13) * 32; r0 < it.nrows; r0 += 32 * kPxQWarps) {
         int64_t off = 0;
         if (r0 + lane < it.nrows) {
           int rr = it.row0 + r0 + lane, b = it.b;
           if (it.type & 1) {
-            b = rr / S.R;
+            b = S.by_R.div(rr);
             rr -= b * S.R;
           }
-          const int i = rr / S.G, g = rr - i * S.G;
+          const int i = S.by_G.div(rr), g = rr - i * S.G;
           off = b * p.q.stride_b + (it.hk * S.G + g) * p.q.stride_h + i * p.q.stride_n;
         }
         const int rows = min(32, it.nrows - r0);
+#pragma unroll 1
         for (int k = 0; k < rows; k += RPI) {
           const int rl = k + lane / VPR, c = lane % VPR;
           const int64_t o = __shfl_sync(FULLM, off, rl & 31);
           const int r = r0 + rl;
           if (rl < rows)
-            cp_async_16(base + (c >> 3) * PANEL + r * 128 + (((c & 7) ^ (r & 7)) << 4), static_cast<const __nv_bfloat16*>(p.q.ptr) + o + c * 8);
+            cp_async_16(dst + (c >> 3) * PANEL + r * 128 + (((c & 7) ^ (r & 7)) << 4), static_cast<const __nv_bfloat16*>(p.q.ptr) + o + c * 8);
         }
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
       fence_proxy_async();
-      mbar_arrive(BAR(Q_FULL));
+      mbar_arrive(BAR(Q_FULL + (n & 1)));
       item_done(n);
     }
   } else if (warp == 3) {
     // ------------------------------------------------------------------ scheduler
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     const int n_cta = gridDim.x;
-    int published = 0;
+    int published = 0, kind = -1, turn = 0;
+    // The last published item, and all before it, are done.
+    auto all_done = [&]() -> bool {
+      const int m = published - 1;
+      return m < 0 || wait_all(ITEM_EMPTY + m % kPxRing, (m / kPxRing) & 1, kPxItemEmpty, m);
+    };
     auto publish = [&](const PrefixItem& it) -> bool {
       const int m = published, slot = m % kPxRing;
-      if (m >= kPxRing && !wait_all(ITEM_EMPTY + slot, ((m / kPxRing) - 1) & 1, kPxItemEmpty, m)) return false;
-      if (lane == 0) {
-        ring[slot] = it;
-        mbar_arrive(BAR(ITEM_FULL + slot));
+      int page = S.pages;
+      if (it.type >= 0) {
+        const int e0 = it.pos0 >> S.page_shift, e = e0 + lane;
+        if (e < min(e0 + (it.cnt << (7 - S.page_shift)), (it.kv_end + S.page - 1) >> S.page_shift)) {
+          page = p.table[static_cast<int64_t>(it.slot) * S.width + e];
+          if (page < 0 || page >= S.pages) {
+            report(AVSA_ERR_BAD_TABLE, kPrefixPage, it.slot, e);
+            page = S.pages;
+          }
+        }
       }
+      if (m >= kPxRing && !wait_all(ITEM_EMPTY + slot, ((m / kPxRing) - 1) & 1, kPxItemEmpty, m)) return false;
+      ring_pages[slot * 32 + lane] = page;
+      if (lane == 0) ring[slot] = it;
       __syncwarp();
+      if (lane == 0) mbar_arrive(BAR(ITEM_FULL + slot));
       published++;
       return true;
     };
-    // All published items are done; those with a row that outgrew its reference run again.
+    // What has been published is done; items with a row that outgrew its reference run again (narrow: both runs by the group whose item it was).
     auto settle = [&]() -> bool {
-      if (published == 0) return true;
-      const int m = published - 1;
-      if (!wait_all(ITEM_EMPTY + m % kPxRing, (m / kPxRing) & 1, kPxItemEmpty, m)) return false;
+      if (!all_done()) return false;
       const int listed = __shfl_sync(FULLM, misc[LISTED], 0);
       if (lane == 0) misc[LISTED] = 0;
-      for (int i = 0; i < listed; i++) {
-        PrefixItem it = redo[i];
-        const int type = it.type;
-        it.type = type | 2;
-        if (!publish(it)) return false;
-        it.type = type | 4;
+#pragma unroll 1
+      for (int i = 0; i < 2 * listed; i++) {
+        PrefixItem it = redo[i >> 1];
+        it.type |= i & 1 ? 4 : 2;
         if (!publish(it)) return false;
       }
-      return true;
+      return all_done();
     };
-    auto give = [&](const PrefixItem& it) -> bool {
-      if (__shfl_sync(FULLM, misc[LISTED], 0) >= kPxRedo - kPxRing - 1 && !settle()) return false;
-      return publish(it);
+    // Lane l: the own item f0 + l of a key head.
+    auto own_items = [&](int f0, int& nt, int& len, int& slot) {
+      nt = len = 0;
+      slot = -1;
+      const int f = f0 + lane;
+      if (f < S.F) {
+        const int b = S.by_TO.div(f);
+        int bad;
+        len = prefix_sequence(p, b, slot, bad);
+        if (bad && blockIdx.x == 0) report(AVSA_ERR_BAD_TABLE, bad, b, slot);
+        nt = prefix_own_tiles(S, len, f - b * S.TO);
+      }
     };
-    // Item f of a key head that holds its unit `rest` < W, and the units before it.
-    auto find = [&](int rest, int& f, int& before) {
-      f = before = 0;
-      for (int f0 = 0; f0 < S.F; f0 += 32) {
-        int nt = 0;
-        if (f0 + lane < S.F) {
-          const int b = (f0 + lane) / S.TO;
-          int slot, bad;
-          const int len = prefix_sequence(p, b, slot, bad);
-          nt = prefix_own_tiles(S, len, f0 + lane - b * S.TO);
-        }
-        int inc = nt;
+    auto scan = [&](int v) {      // of the lanes up to this one
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const int o = __shfl_up_sync(FULLM, inc, d);
-          if (lane >= d) inc += o;
-        }
-        const unsigned beyond = __ballot_sync(FULLM, before + inc > rest);
-        if (beyond != 0u) {
-          const int l = __ffs(beyond) - 1;
-          f = f0 + l;
-          before += __shfl_sync(FULLM, inc - nt, l);
-          return;
-        }
-        before += __shfl_sync(FULLM, inc, 31);
+      for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(FULLM, v, d);
+        if (lane >= d) v += o;
       }
+      return v;
     };
     // ---- the plan
     PrefixPlan P = {};
+    int n_pre = 0;
     {
-      int most = 0, at = 0;
-      int W = 0;
-      for (int f = lane; f < S.F; f += 32) {
-        const int b = f / S.TO;
-        int slot, bad;
-        const int len = prefix_sequence(p, b, slot, bad);
-        if (bad && blockIdx.x == 0) report(AVSA_ERR_BAD_TABLE, bad, b, slot);
-        W += prefix_own_tiles(S, len, f - b * S.TO);
+      int most = 0, at = 0, W = 0;
+#pragma unroll 1
+      for (int f0 = 0; f0 < S.F; f0 += 32) {
+        int nt, len, slot;
+        own_items(f0, nt, len, slot);
+        W += nt;
         if (len > most) most = len, at = slot;
       }
       P.W = __reduce_add_sync(FULLM, W);
       if (S.stack) {
         const int top = __reduce_max_sync(FULLM, most);
-        const unsigned who = __ballot_sync(FULLM, most == top);
-        P.donor = __shfl_sync(FULLM, at, __ffs(who) - 1);
+        P.donor = __shfl_sync(FULLM, at, __ffs(__ballot_sync(FULLM, most == top)) - 1);
         P.PE = min(S.k0, top);
         P.PT = (P.PE + 127) >> 7;
       }
       const int T = P.W * S.Hkv, columns = S.Hkv * S.nrc * P.PT;
-      int n_pre = 0;
       if (columns > 0) {
         const float share = static_cast<float>(S.Hkv) * S.TP * P.PT;
-        int groups = max(1, static_cast<int>(n_cta * (share / (share + T)) / S.chunk + 0.5f));
-        groups = min(groups, max(1, (T > 0 ? n_cta - 1 : n_cta) / S.chunk));
+        int groups = max(1, __float2int_rz(__fdividef(n_cta * share, (share + T) * S.chunk) + 0.5f));
+        groups = min(groups, max(1, S.by_chunk.div(T > 0 ? n_cta - 1 : n_cta)));
         groups = min(groups, (columns + kPxMinPiece - 1) / kPxMinPiece);
-        P.cg = (columns + groups - 1) / groups;
-        P.groups = (columns + P.cg - 1) / P.cg;
+        P.cg = float_div(columns + groups - 1, groups);
+        P.groups = float_div(columns + P.cg - 1, P.cg);
         n_pre = P.groups * S.chunk;
       }
       P.TB = T;
-      int want = max(1, n_cta - n_pre);
+      int want = min(max(1, n_cta - n_pre), (T + kPxMinPiece - 1) / kPxMinPiece);
       if (S.queue && T > 0) {
-        // the last item's worth of every CTA, in quarters
-        const int per_item = max(1, T / (S.Hkv * S.F));
-        const int tail = min(T, n_cta * per_item);
-        P.sB = max(kPxMinPiece, (per_item + 3) / 4);
-        // the item that holds unit T - tail
-        const int u = T - tail;
-        const int hk = u / P.W, rest = u - hk * P.W;
-        int f, before;
-        find(rest, f, before);
+        // cut are the last items, one's worth of every CTA, in quarters
+        const int per_item = max(1, float_div(T, S.Hkv * S.F));
+        const int u = T - min(T, n_cta * per_item);
+        const int hk = float_div(u, P.W), rest = u - hk * P.W;
+        int before = 0, f = 0;
+#pragma unroll 1
+        for (int f0 = 0; f0 < S.F; f0 += 32) {
+          int nt, len, slot;
+          own_items(f0, nt, len, slot);
+          const int inc = scan(nt);
+          const unsigned beyond = __ballot_sync(FULLM, before + inc > rest);
+          if (beyond != 0u) {
+            const int l = __ffs(beyond) - 1;
+            f = f0 + l;
+            before += __shfl_sync(FULLM, inc - nt, l);
+            break;
+          }
+          before += __shfl_sync(FULLM, inc, 31);
+        }
         P.MA = hk * S.F + f;
         P.uA = hk * P.W + before;
         P.TB = T - P.uA;
-        want = (P.TB + P.sB - 1) / P.sB;
-      } else {
-        want = min(want, (T + kPxMinPiece - 1) / kPxMinPiece);
+        want = float_div(P.TB - 1, max(kPxMinPiece, (per_item + 3) / 4)) + 1;
       }
       want = max(1, min(want, S.nb_max));
-      P.sB = max(1, (P.TB + want - 1) / want);
-      P.NB = (P.TB + P.sB - 1) / P.sB;
+      P.sB = max(1, float_div(P.TB + want - 1, want));
+      P.NB = float_div(P.TB + P.sB - 1, P.sB);
       if (blockIdx.x == 0 && lane == 0) {
         p.plan[0] = P.PT;
         p.plan[1] = P.cg;
         p.plan[2] = P.NB;
       }
     }
-    const int n_pre = P.groups * S.chunk;
-    const int pieces = n_pre + P.MA + P.NB;
-    auto own_item = [&](int hk, int f, int kt, int take, int nt, int len, int slot, int piece, int unit) -> bool {
-      // (unit: of the item's first tile among the units of the B pieces; piece < 0: of the queue)
-      PrefixItem it = {};
-      const int b = f / S.TO, rt = f - b * S.TO;
-      it.b = b;
-      it.hk = hk;
-      it.row0 = rt * 128;
-      it.nrows = min(128, S.R - it.row0);
-      it.pos0 = S.k0 + kt * 128;
-      it.cnt = take;
-      it.kv_end = len;
-      it.slot = slot;
-      it.len = len;
-      const int m = hk * S.F + f;
-      const bool whole = take == nt;
-      it.out = whole ? (S.stack ? p.own_row0 + m * S.rows : -1) : p.cut_row0 + (2 * piece + (kt == 0 ? 1 : 0)) * S.rows;
-      if (kt == 0 && lane == 0) {
-        const int parts = whole ? 1 : (unit + nt + P.sB - 1) / P.sB - piece;
-        if (S.stack) p.own_rec[m] = make_int2(piece, parts);
-        else if (!whole) p.cut_rec[piece] = make_int2(m, parts);
-      }
-      return give(it);
-    };
+    // ---- the pieces: `n_pre` of the beginning, P.MA whole own items, P.NB of the others' stream
     bool ok = true;
+    const int pieces = n_pre + P.MA + P.NB;
+#pragma unroll 1
     for (int id = blockIdx.x; ok && id < pieces;) {
+      // its units [u, u1) of a stream that goes head after head (or chunk of row tiles after chunk), `per` units each; whole items: item `only`
+      int head = 0, only = -1, u, u1, per, j = 0;
+      const int piece = id - n_pre - P.MA;
       if (id < n_pre) {
-        const int g = id / S.chunk, j = id - g * S.chunk;
-        const int c1 = min((g + 1) * P.cg, S.Hkv * S.nrc * P.PT);
-        for (int c = g * P.cg; c < c1 && ok;) {
-          const int U = c / P.PT, kt = c - U * P.PT, take = min(P.PT - kt, c1 - c);
-          const int hk = U / S.nrc, rt = (U - hk * S.nrc) * S.chunk + j;
-          if (rt < S.TP) {
-            PrefixItem it = {};
-            it.type = 1;
-            it.hk = hk;
-            it.row0 = rt * 128;
-            it.nrows = min(128, S.B * S.R - it.row0);
-            it.pos0 = kt * 128;
-            it.cnt = take;
-            it.kv_end = P.PE;
-            it.slot = P.donor;
-            it.out = ((g + U) * S.chunk + j) * 128;
-            ok = give(it);
-          }
-          c += take;
-        }
-      } else if (id < n_pre + P.MA) {
-        const int m = id - n_pre, hk = m / S.F, f = m - hk * S.F;
-        int slot, bad;
-        const int len = prefix_sequence(p, f / S.TO, slot, bad);
-        const int nt = prefix_own_tiles(S, len, f - f / S.TO * S.TO);
-        if (nt > 0) ok = own_item(hk, f, 0, nt, nt, len, slot, 0, 0);
+        const int g = S.by_chunk.div(id);
+        j = id - g * S.chunk;
+        per = P.PT;
+        u = g * P.cg;
+        u1 = min(u + P.cg, S.Hkv * S.nrc * P.PT);
+      } else if (piece < 0) {
+        const int m = id - n_pre;
+        head = S.by_F.div(m);
+        only = m - head * S.F;
+        per = P.W;
+        u = 0;
+        u1 = P.W;
       } else {
-        const int piece = id - n_pre - P.MA;
-        const int u0 = piece * P.sB, u1 = min(P.TB, u0 + P.sB);
+        per = P.W;
+        u = P.uA + piece * P.sB;
+        u1 = min(u + P.sB, P.uA + P.TB);
         if (!S.stack && lane == 0) p.cut_rec[piece] = make_int2(-1, 0);
-        int hk = (P.uA + u0) / P.W;
-        const int rest = P.uA + u0 - hk * P.W;
-        int before, f;
-        find(rest, f, before);
-        int kt = rest - before;
-        for (int u = u0; u < u1 && ok;) {
-          const int b = f / S.TO;
-          int slot, bad;
-          const int len = prefix_sequence(p, b, slot, bad);
-          const int nt = prefix_own_tiles(S, len, f - b * S.TO);
-          if (nt > 0) {
-            const int take = min(nt - kt, u1 - u);
-            ok = own_item(hk, f, kt, take, nt, len, slot, piece, u - kt);
-            u += take;
-          }
-          kt = 0;
-          if (++f == S.F) {
-            f = 0;
-            hk++;
+      }
+      if (only < 0) {
+        head = float_div(u, per);
+        u -= head * per;
+        u1 -= head * per;
+      }
+#pragma unroll 1
+      while (ok && u < u1) {       // one head's
+        int before = 0;
+        const int f_end = id < n_pre ? 1 : S.F;
+#pragma unroll 1
+        for (int f0 = only < 0 ? 0 : only & ~31; ok && f0 < f_end && before < u1; f0 += 32) {
+          int nt = 0, len = 0, slot = -1;
+          if (id >= n_pre) own_items(f0, nt, len, slot);
+          else if (lane == 0) nt = per;
+          const int inc = scan(nt), first = before + inc - nt;
+          const int lo = only < 0 ? max(u, first) : first, hi = only < 0 ? min(u1, before + inc) : only == f0 + lane ? first + nt : first;
+          before += __shfl_sync(FULLM, inc, 31);
+#pragma unroll 1
+          for (unsigned todo = __ballot_sync(FULLM, hi > lo); todo != 0u && ok; todo &= todo - 1) {
+            const int l = __ffs(todo) - 1, f = f0 + l;
+            const int kt = __shfl_sync(FULLM, lo - first, l), take = __shfl_sync(FULLM, hi - lo, l);
+            PrefixItem it = {};
+            it.cnt = take;
+            if (id < n_pre) {
+              const int hk = S.by_nrc.div(head), rt = (head - hk * S.nrc) * S.chunk + j;
+              if (rt >= S.TP) continue;
+              it.type = S.pre_narrow ? 9 : 1;
+              it.hk = hk;
+              it.row0 = rt * 128;
+              it.nrows = min(128, S.B * S.R - it.row0);
+              it.pos0 = kt * 128;
+              it.kv_end = P.PE;
+              it.slot = P.donor;
+              it.out = ((S.by_chunk.div(id) + head) * S.chunk + j) * 128;
+            } else {
+              const int all = __shfl_sync(FULLM, nt, l), b = S.by_TO.div(f), m = head * S.F + f;
+              it.type = S.own_narrow ? 8 : 0;
+              it.b = b;
+              it.hk = head;
+              it.row0 = (f - b * S.TO) * 128;
+              it.nrows = min(128, S.R - it.row0);
+              it.pos0 = S.k0 + kt * 128;
+              it.len = it.kv_end = __shfl_sync(FULLM, len, l);
+              it.slot = __shfl_sync(FULLM, slot, l);
+              const bool whole = take == all;
+              it.out = whole ? (S.stack ? p.own_row0 + m * S.rows : -1) : p.cut_row0 + (2 * piece + (kt == 0 ? 1 : 0)) * S.rows;
+              if (kt == 0) {
+                // the item's parts: this piece's and those of the pieces up to its last unit
+                const int last = head * P.W + __shfl_sync(FULLM, first, l) + all - 1 - P.uA;
+                const int parts = whole ? 1 : float_div(last, P.sB) - piece + 1;
+                if (lane == 0) {
+                  if (S.stack) p.own_rec[m] = make_int2(whole ? 0 : piece, parts);
+                  else if (!whole) p.cut_rec[piece] = make_int2(m, parts);
+                }
+              }
+            }
+            // (narrow and wide items use the same memory in different ways: what has been published is done before the other kind begins)
+            if ((kind >= 0 && kind != (it.type & 8)) || __shfl_sync(FULLM, misc[LISTED], 0) >= kPxRedo - kPxRing - 1) ok = settle();
+            kind = it.type & 8;
+            it.group = turn++ & 1;
+            if (ok) ok = publish(it);
           }
         }
+        // the next head's
+        if (only >= 0) break;
+        head++;
+        u = 0;
+        u1 -= per;
       }
       if (S.queue) {
+        // (one item beyond the one being worked on: whatever else this CTA held, others could not take at the end)
+        const int m = published - 2;
+        if (ok && m >= 0) ok = wait_all(ITEM_EMPTY + m % kPxRing, (m / kPxRing) & 1, kPxItemEmpty, m);
         int next = 0;
         if (lane == 0) next = n_cta + atomicAdd(p.counter, 1);
         id = __shfl_sync(FULLM, next, 0);
@@ -569,13 +674,53 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     const uint32_t q_lo = ((smem_u32(smem + L_::kQ) & 0x3FFFFu) >> 4) | (1u << 16);
     const uint32_t k_lo0 = ((smem_u32(smem + L_::kK) & 0x3FFFFu) >> 4) | (1u << 16);
     int stage = 0, round = 0;
-    int used[2] = {0, 0};
+    int used[2] = {0, 0}, nused[2] = {0, 0};
     bool ok = true;
+#pragma unroll 1
     for (int n = 0; ok; n++) {
       PrefixItem it;
       if (!get_item(n, it)) break;
       const int cnt = it.cnt;
-      ok = wait_all(Q_FULL, n & 1, kPxQFull, n);
+      ok = wait_all(Q_FULL + (n & 1), (n >> 1) & 1, kPxQFull, n);
+      if (is_narrow(it.type)) {
+        // S^T = K Q^T: keys are the lanes, query rows the columns
+        const int g = it.group;
+        const uint32_t idesc = it.nrows > 16 ? make_idesc_bf16(128, 32, 0, 0) : make_idesc_bf16(128, 16, 0, 0);
+        const uint32_t qn_lo = q_lo + (n & 1) * (L_::kNarrowSlot >> 4);
+#pragma unroll 1
+        for (int t = 0; t < cnt && ok; t++) {
+          const int k = nused[g] & 1;
+          ok = wait_all(K_FULL + stage, round & 1, kPxKFull, t);
+          if (!ok) break;
+          if (nused[g] >= 2) {
+            ok = wait_all(NS_FREE + 2 * g + k, ((nused[g] >> 1) - 1) & 1, kPxSFree, t);
+            if (!ok) break;
+          }
+          tc_fence_after();
+          const uint32_t k_lo = k_lo0 + stage * (L_::kTile >> 4);
+          const uint32_t tm_s = tmem_u + g * 64 + k * 32;
+          if (leader) {
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ks++) {
+              const uint32_t off = ((ks >> 2) * PANEL + (ks & 3) * 32) >> 4;
+              umma_ss(tm_s, desc64(k_lo + off), desc64(qn_lo + off), idesc, ks > 0 ? 1u : 0u);
+            }
+            umma_commit(BAR(NS_FULL + 2 * g + k));
+            umma_commit(BAR(K_EMPTY + stage));
+            if (t == cnt - 1) umma_commit(BAR(Q_EMPTY + (n & 1)));
+          }
+          __syncwarp();
+          nused[g]++;
+          if (++stage == KS) {
+            stage = 0;
+            round++;
+          }
+        }
+        if (ok) item_done(n);
+        continue;
+      }
+      const uint32_t qw_lo = q_lo + (n & 1) * (L_::kQSlot >> 4);
+#pragma unroll 1
       for (int t = 0; t < cnt && ok; t++) {
         const int j = t & 1;
         ok = wait_all(K_FULL + stage, round & 1, kPxKFull, t);
@@ -591,11 +736,11 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
 #pragma unroll
           for (int ks = 0; ks < D / 16; ks++) {
             const uint32_t off = ((ks >> 2) * PANEL + (ks & 3) * 32) >> 4;
-            umma_ss(tm_s, desc64(q_lo + off), desc64(k_lo + off), idesc_qk, ks > 0 ? 1u : 0u);
+            umma_ss(tm_s, desc64(qw_lo + off), desc64(k_lo + off), idesc_qk, ks > 0 ? 1u : 0u);
           }
           umma_commit(BAR(S_FULL + j));
           umma_commit(BAR(K_EMPTY + stage));
-          if (t == cnt - 1) umma_commit(BAR(Q_EMPTY));
+          if (t == cnt - 1) umma_commit(BAR(Q_EMPTY + (n & 1)));
         }
         __syncwarp();
         used[j]++;
@@ -625,14 +770,23 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
         umma_ts(tmem_u + TM_O, tm_buf + ks * 8, desc64(v_lo + ks * (2048 >> 4)), idesc_pv, kk > 0 ? 1u : acc_first);
       }
     };
+    // O^T += V^T P^T: channels are the lanes (with 64 of them the upper 64 lanes read the tile 8 keys on, for nothing), query rows the columns
+    constexpr uint32_t ndesc_hi = desc_hi;
+    const uint32_t nv_lo0 = ((smem_u32(smem + L_::kV) & 0x3FFFFu) >> 4) | (static_cast<uint32_t>((D == 128 ? PANEL : 1024) >> 4) << 16);
+    const uint32_t np_lo0 = ((smem_u32(smem + L_::kQ + L_::kNarrowP) & 0x3FFFFu) >> 4) | (1u << 16);
+    auto ndesc64 = [](uint32_t lo) { return (static_cast<uint64_t>(ndesc_hi) << 32) | lo; };
     int stage = 0, round = 0, outputs = 0;
-    int used[2] = {0, 0};
+    int used[2] = {0, 0}, nused[2] = {0, 0}, nouts[2] = {0, 0};
     bool ok = true;
+#pragma unroll 1
     for (int n = 0; ok; n++) {
       PrefixItem it;
       if (!get_item(n, it)) break;
-      if ((it.type >> 1) != 1) {
+      if (((it.type >> 1) & 3) != 1) {
         const int cnt = it.cnt;
+        const bool narrow = is_narrow(it.type);
+        const int ng = it.group;
+#pragma unroll 1
         for (int t = 0; t < cnt && ok; t++) {
           const int j = t & 1;
           ok = wait_all(V_FULL + stage, round & 1, kPxVFull, t);
@@ -642,12 +796,42 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
             // behind the last token its page may hold anything; P is zero there, and 0 * NaN is not
             const int end = (valid + S.page - 1) & ~(S.page - 1);
             uint8_t* tile = smem + L_::kV + stage * L_::kTile;
+#pragma unroll 1
             for (int c = valid * 8 + lane; c < end * 8; c += 32) {
 #pragma unroll
               for (int pn = 0; pn < NPANEL; pn++) *reinterpret_cast<uint4*>(tile + pn * PANEL + c * 16) = make_uint4(0u, 0u, 0u, 0u);
             }
             fence_proxy_async();
             __syncwarp();
+          }
+          if (narrow) {
+            ok = wait_all(NP_FULL + ng, nused[ng] & 1, kPxPFull, t);
+            if (!ok) break;
+            if (t == 0 && nouts[ng] > 0) {
+              ok = wait_all(NO_FREE + ng, (nouts[ng] - 1) & 1, kPxOFree, n);
+              if (!ok) break;
+            }
+            tc_fence_after();
+            if (leader) {
+              const bool n32 = it.nrows > 16;
+              const uint32_t idesc = n32 ? make_idesc_bf16(128, 32, 1, 0) : make_idesc_bf16(128, 16, 1, 0);
+              const uint32_t v_lo = nv_lo0 + stage * (L_::kTile >> 4);
+              const uint32_t p_lo = np_lo0 + ng * (16384 >> 4), panel = n32 ? 4096 >> 4 : 2048 >> 4;
+#pragma unroll
+              for (int ks = 0; ks < 8; ks++)
+                umma_ss(tmem_u + TM_NO + ng * 32, ndesc64(v_lo + ks * (2048 >> 4)), ndesc64(p_lo + (ks >> 2) * panel + (ks & 3) * 2), idesc,
+                        t > 0 || ks > 0 ? 1u : 0u);
+              umma_commit(BAR(NP_FREE + ng));
+              umma_commit(BAR(V_EMPTY + stage));
+              if (t == cnt - 1) umma_commit(BAR(NO_FULL + ng));
+            }
+            __syncwarp();
+            nused[ng]++;
+            if (++stage == VS) {
+              stage = 0;
+              round++;
+            }
+            continue;
           }
           ok = wait_all(P_FULL + 2 * j, used[j] & 1, kPxPFull, t);
           if (!ok) break;
@@ -676,7 +860,8 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
             round++;
           }
         }
-        outputs++;
+        if (narrow) nouts[ng]++;
+        else outputs++;
       }
       if (ok) item_done(n);
     }
@@ -697,13 +882,185 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     int used = 0;               // P tiles it has written
     int mrefs = 0, outputs = 0; // items with a first-tile reference, with an output
     float m_given = 0.f;
+    int n_tiles = 0, n_p = 0, n_refs = 0, n_outs = 0, n_sums = 0;      // narrow items: of this group
+    float n_given = 0.f;
+    // A narrow item: the thread's lane is a key (S^T) and then a channel (O^T), the columns are the query rows.
+    auto narrow_item = [&](auto columns, const PrefixItem& it, int n) -> bool {
+      constexpr int N = decltype(columns)::value;
+      const int wq = warp & 3, run = (it.type >> 1) & 3;
+      // lane r: how far row r sees, from the item's first key on
+      int rel = 0x7fffffff;
+      if (lane < it.nrows) {
+        int rr = it.row0 + lane, len = it.len;
+        if (it.type & 1) {
+          const int b = S.by_R.div(rr);
+          rr -= b * S.R;
+          int slot, bad;
+          len = prefix_sequence(p, b, slot, bad);
+        }
+        rel = min(it.kv_end, S.causal ? len - S.L + S.by_G.div(rr) + 1 : len) - it.pos0;
+      }
+      const int rel_min = __reduce_min_sync(FULLM, rel);
+      float nm[N], m_max[N];
+      uint64_t l2[N / 2];
+#pragma unroll
+      for (int r = 0; r < N; r++) m_max[r] = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < N / 2; r++) l2[r] = 0ull;
+      if (run == 2) {
+#pragma unroll
+        for (int r = 0; r < N; r++) nm[r] = -__shfl_sync(FULLM, n_given, r);
+      }
+      float* ref = mref_s + w * 32;
+      const uint32_t p_even = static_cast<uint32_t>(((row & 63) & ~1) * 2) ^ (static_cast<uint32_t>(lane & 1) << 4);
+      const uint32_t p_base = smem_u32(smem + L_::kQ + L_::kNarrowP) + w * 16384 + (row >> 6) * (N * 128) + (lane & 1) * 128;
+#pragma unroll 1
+      for (int t = 0; t < it.cnt; t++) {
+        const int k = n_tiles & 1;
+        if (!wait_all(NS_FULL + 2 * w + k, (n_tiles >> 1) & 1, kPxSFull, t)) return false;
+        tc_fence_after();
+        uint32_t s[N];
+        if constexpr (N == 32) tmem_ld32(tmem + lane_off + w * 64 + k * 32, s);
+        else tmem_ld16(tmem + lane_off + w * 64 + k * 32, s);
+        tmem_wait_ld_regs(s);
+        tc_fence_before();
+        mbar_arrive(BAR(NS_FREE + 2 * w + k));
+        n_tiles++;
+        if (t * 128 + 128 > rel_min) {
+#pragma unroll
+          for (int r = 0; r < N; r++)
+            if (row >= __shfl_sync(FULLM, rel, r) - t * 128) s[r] = 0xff800000u;
+        }
+        if (run == 1) {
+#pragma unroll
+          for (int r = 0; r < N; r++) m_max[r] = fmaxf(m_max[r], __uint_as_float(s[r]));
+          continue;
+        }
+        if (run == 0 && t == 0) {
+          // the reference: a row's maximum over the first 32 keys, which one warp holds (a row that sees any sees the first)
+          if (wq == 0) {
+            if (n_sums > 0 && !wait_all(NREAD + w, (n_sums - 1) & 1, kPxLsum, n)) return false;      // (who reads the item's before)
+            float x[N];
+#pragma unroll
+            for (int r = 0; r < N; r++) x[r] = __uint_as_float(s[r]);
+            const float top = p.scale_log2 * lane_reduce<N>(x, [](float a, float b) { return fmaxf(a, b); });
+            if (lane < N) ref[lane] = top == -INFINITY ? 0.f : top;
+            mbar_arrive(BAR(NREF + w));
+          }
+          if (!wait_all(NREF + w, n_refs & 1, kPxMref, n)) return false;
+#pragma unroll
+          for (int r = 0; r < N; r += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(ref + r);
+            nm[r] = -v.x;
+            nm[r + 1] = -v.y;
+            nm[r + 2] = -v.z;
+            nm[r + 3] = -v.w;
+          }
+        }
+        const uint64_t c2 = pack_f32x2(p.scale_log2, p.scale_log2);
+        uint32_t pk[N / 2];
+#pragma unroll
+        for (int r = 0; r < N; r += 2) {
+          float x0, x1;
+          unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[r]), __uint_as_float(s[r + 1])), c2, pack_f32x2(nm[r], nm[r + 1])), x0, x1);
+          const float e0 = fast_exp2(x0), e1 = fast_exp2(x1);
+          l2[r / 2] = add_f32x2(l2[r / 2], pack_f32x2(e0, e1));
+          // neighbouring lanes hold neighbouring keys: the even one stores both of row r, the odd one both of row r + 1
+          const float got = __shfl_xor_sync(FULLM, (lane & 1) ? e0 : e1, 1);
+          pk[r / 2] = (lane & 1) ? pack_bf16x2(got, e1) : pack_bf16x2(e0, got);
+        }
+        if (n_p > 0 && !wait_all(NP_FREE + w, (n_p - 1) & 1, kPxPFree, t)) return false;      // the product that read this group's last P has run
+#pragma unroll
+        for (int r = 0; r < N; r += 2)
+          asm volatile("st.shared.b32 [%0], %1;" ::"r"(p_base + r * 128 + (p_even ^ ((r & 7) << 4))), "r"(pk[r / 2]) : "memory");
+        fence_proxy_async();
+        mbar_arrive(BAR(NP_FULL + w));
+        n_p++;
+      }
+      if (run == 0) n_refs++;
+      // sums (or maxima) over the lanes, then over the warps: lane r holds row r's
+      float x[N];
+#pragma unroll
+      for (int r = 0; r < N; r += 2) {
+        unpack_f32x2(l2[r / 2], x[r], x[r + 1]);
+        if (run == 1) x[r] = m_max[r], x[r + 1] = m_max[r + 1];
+      }
+      const float part = run == 1 ? lane_reduce<N>(x, [](float a, float b) { return fmaxf(a, b); }) : lane_reduce<N>(x, [](float a, float b) { return a + b; });
+      float* sums = mref_s + 64 + w * 128;
+      if (n_sums > 0 && !wait_all(NREAD + w, (n_sums - 1) & 1, kPxLsum, n)) return false;      // the item before has been read
+      if (lane < N) sums[wq * 32 + lane] = part;
+      mbar_arrive(BAR(NSUM + w));
+      if (!wait_all(NSUM + w, n_sums & 1, kPxLsum, n)) return false;
+      n_sums++;
+      const int rl = lane & (N - 1);
+      const float a0 = sums[rl], a1 = sums[32 + rl], a2 = sums[64 + rl], a3 = sums[96 + rl];
+      const float m_ref = run == 2 ? n_given : ref[rl];
+      mbar_arrive(BAR(NREAD + w));
+      if (run == 1) {
+        const float top = p.scale_log2 * fmaxf(fmaxf(a0, a1), fmaxf(a2, a3));
+        n_given = top == -INFINITY ? 0.f : top;
+        return true;
+      }
+      const float sum = (a0 + a1) + (a2 + a3);
+      const bool again = run == 0 && __any_sync(FULLM, lane < it.nrows && !(sum <= kFastRowSumLimit));
+      if (again && wq == 0 && lane == 0) {
+        redo[atomicAdd(const_cast<int*>(&misc[LISTED]), 1)] = it;
+        atomicAdd(const_cast<int*>(&misc[RECOMPUTED]), 1);
+      }
+      if (!wait_all(NO_FULL + w, n_outs & 1, kPxOFull, n)) return false;
+      n_outs++;
+      tc_fence_after();
+      const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+      const float lse2 = sum != 0.f ? m_ref + log2f(sum) : -INFINITY;
+      // lane r: where row r goes (partial rows: as fp32 rows of D, one behind the other)
+      int64_t to = 0;
+      if (lane < it.nrows && !again) {
+        if (it.out >= 0) {
+          to = static_cast<int64_t>(it.out + lane) * D;
+          if (wq == 0) p.part_lse2[it.out + lane] = lse2;
+        } else {
+          const int rr = it.row0 + lane, i = S.by_G.div(rr), head = it.hk * S.G + rr - i * S.G;
+          to = it.b * p.q.stride_b + head * p.q.stride_h + i * p.q.stride_n;
+          if (wq == 0 && p.lse != nullptr) p.lse[(static_cast<int64_t>(it.b) * S.Hkv * S.G + head) * S.L + i] = lse2 * 0.6931471805599453f;
+        }
+      }
+      const int rows = again ? 0 : it.nrows;
+#pragma unroll 1
+      for (int c = 0; c < rows; c += 8) {
+        uint32_t o[8];
+        tmem_ld8(tmem + TM_NO + w * 32 + lane_off + c, o);
+        tmem_wait_ld_regs(o);
+#pragma unroll
+        for (int r = 0; r < 8; r++) {
+          const float x = __uint_as_float(o[r]) * __shfl_sync(FULLM, inv, c + r);
+          const int64_t at = __shfl_sync(FULLM, to, c + r) + row;
+          if (c + r < rows && row < D) {
+            if (it.out >= 0) p.part_o[at] = x;
+            else p.o[at] = __float2bfloat16(x);
+          }
+        }
+      }
+      tc_fence_before();
+      mbar_arrive(BAR(NO_FREE + w));
+      return true;
+    };
     bool ok = true;
+#pragma unroll 1
     for (int n = 0; ok; n++) {
       PrefixItem it;
       if (!get_item(n, it)) break;
+      if (is_narrow(it.type)) {
+        if (it.group == w) {
+          ok = it.nrows > 16 ? narrow_item(std::integral_constant<int, 32>(), it, n) : narrow_item(std::integral_constant<int, 16>(), it, n);
+          if (!ok) break;
+        }
+        item_done(n);
+        continue;
+      }
       const int cnt = it.cnt, run = it.type >> 1;
       if ((warp & 3) * 32 >= it.nrows) {
         // no rows in this warp: its arrivals alone
+#pragma unroll 1
         for (int t = w; t < cnt && ok; t += 2) {
           ok = wait_all(S_FULL + w, tiles & 1, kPxSFull, t);
           if (!ok) break;
@@ -739,17 +1096,18 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       if (row < it.nrows) {
         int rr = it.row0 + row, len = it.len;
         if (it.type & 1) {
-          b = rr / S.R;
+          b = S.by_R.div(rr);
           rr -= b * S.R;
           int slot, bad;
           len = prefix_sequence(p, b, slot, bad);
         }
-        i = rr / S.G;
+        i = S.by_G.div(rr);
         g = rr - i * S.G;
         rel = min(it.kv_end, S.causal ? len - S.L + i + 1 : len) - it.pos0;
       }
       float m_ref = run == 2 ? m_given : 0.f, m_max = -INFINITY;
       uint64_t sum2[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll 1
       for (int t = w; t < cnt && ok; t += 2) {
         ok = __all_sync(FULLM, wait_or_stop(S_FULL + w, tiles & 1, kPxSFull, t));
         if (!ok) break;
@@ -905,7 +1263,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
 
 // ------------------------------------------------------------------------------------------------ joining the parts
 // A warp per row; the lanes hold D/32 channels each.  Parts are joined in the order of the key axis.  Stacked rows: the groups of the beginning, whose numbers
-// follow from the plan, and the parts of the row's own item.  Else: the rows of the items that a B piece begins and another ends (a CTA per piece).
+// follow from the plan, and the parts of the row's own item.  Else: the rows of the items that a B piece begins and another ends.
 constexpr int kPxMergeWarps = 8;
 
 template <int D>
@@ -991,7 +1349,7 @@ __global__ void __launch_bounds__(kPxMergeWarps * 32) prefix_merge_kernel(const 
     const int64_t r = static_cast<int64_t>(blockIdx.x) * kPxMergeWarps + warp;
     if (r >= static_cast<int64_t>(rows) * S.Hkv) return;
     const int hk = static_cast<int>(r / rows), rho = static_cast<int>(r - static_cast<int64_t>(hk) * rows);
-    const int b = rho / S.R, rr = rho - b * S.R, i = rr / S.G, g = rr - i * S.G;
+    const int b = S.by_R.div(rho), rr = rho - b * S.R, i = S.by_G.div(rr), g = rr - i * S.G;
     int first = 0, n_first = 0;
     if (PT > 0) {
       const int rt = rho >> 7, rc = rt / S.chunk, j = rt - rc * S.chunk, U = hk * S.nrc + rc;
@@ -1012,14 +1370,15 @@ __global__ void __launch_bounds__(kPxMergeWarps * 32) prefix_merge_kernel(const 
     }
     prefix_merge_row<D>(p, first, S.chunk * 128, n_first, second, n_second, next, 2 * S.rows, b, hk * S.G + g, i);
   } else {
-    const int piece = blockIdx.x;
-    if (piece >= p.plan[2]) return;
-    const int2 rec = p.cut_rec[piece];
-    if (rec.x < 0 || rec.x >= S.Hkv * S.F || rec.y < 1 || rec.y > p.plan[2] - piece) return;      // (also one that a kernel that gave up did not write)
-    const int hk = rec.x / S.F, f = rec.x - hk * S.F, b = f / S.TO, row0 = (f - b * S.TO) * 128;
-    const int rows = min(128, S.R - row0);
-    for (int in = blockIdx.y * kPxMergeWarps + warp; in < rows; in += gridDim.y * kPxMergeWarps) {
-      const int rr = row0 + in, i = rr / S.G, g = rr - i * S.G;
+    const int NB = p.plan[2];
+    for (int at = blockIdx.x * kPxMergeWarps + warp; at < NB * 128; at += gridDim.x * kPxMergeWarps) {
+      const int piece = at >> 7, in = at & 127;
+      const int2 rec = p.cut_rec[piece];
+      // (one that a kernel that gave up did not write either)
+      if (rec.x < 0 || rec.x >= S.Hkv * S.F || rec.y < 1 || rec.y > NB - piece) continue;
+      const int hk = S.by_F.div(rec.x), f = rec.x - hk * S.F, b = S.by_TO.div(f), rr = (f - b * S.TO) * 128 + in;
+      if (in >= S.rows || rr >= S.R) continue;
+      const int i = S.by_G.div(rr), g = rr - i * S.G;
       prefix_merge_row<D>(p, 0, 0, 0, p.cut_row0 + (2 * piece + 1) * S.rows + in, rec.y, p.cut_row0 + (2 * piece + 2) * S.rows + in, 2 * S.rows, b,
                           hk * S.G + g, i);
     }
