@@ -46,23 +46,18 @@ static const DriverFns& driver_fns() {
   return fns;
 }
 
-bool encode_bf16_tile_map(CUtensorMap* map, const void* ptr, int B, int H, int N, int d, int64_t stride_b,
-                          int64_t stride_h, int64_t stride_n, int box_rows) {
+bool encode_bf16_map(CUtensorMap* map, const void* ptr, const int64_t (&size)[4], const int64_t (&stride)[3], const int (&box)[4]) {
   const DriverFns& fns = driver_fns();
   if (fns.encode == nullptr || fns.current == nullptr) return false;
-  // A dimension of extent 1 never has its stride used for addressing, but the encoder still wants a
-  // multiple of 16 bytes; give it a harmless one.
-  const int64_t sn = stride_n;
-  const int64_t sh = (H > 1) ? stride_h : sn * N;
-  const int64_t sb = (B > 1) ? stride_b : sh * (H > 1 ? H : 1);
-  cuuint64_t dims[4] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(N), static_cast<cuuint64_t>(H),
-                        static_cast<cuuint64_t>(B)};
-  cuuint64_t strides[3] = {static_cast<cuuint64_t>(sn) * 2u, static_cast<cuuint64_t>(sh) * 2u,
-                           static_cast<cuuint64_t>(sb) * 2u};
-  cuuint32_t box[4] = {64u, static_cast<cuuint32_t>(box_rows), 1u, 1u};
-  cuuint32_t elem[4] = {1u, 1u, 1u, 1u};
+  cuuint64_t dims[4], strides[3];
+  cuuint32_t boxes[4], elem[4] = {1u, 1u, 1u, 1u};
+  for (int i = 0; i < 4; i++) {
+    dims[i] = static_cast<cuuint64_t>(size[i]);
+    boxes[i] = static_cast<cuuint32_t>(box[i]);
+  }
+  for (int i = 0; i < 3; i++) strides[i] = static_cast<cuuint64_t>(stride[i]) * 2u;
   auto encode = [&] {
-    return fns.encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, elem,
+    return fns.encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, boxes, elem,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
   };
@@ -73,6 +68,16 @@ bool encode_bf16_tile_map(CUtensorMap* map, const void* ptr, int B, int H, int N
   if (fns.current(&ctx) == CUDA_SUCCESS && ctx != nullptr) return false;
   int dev = 0;
   return cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess && encode();
+}
+
+bool encode_bf16_tile_map(CUtensorMap* map, const void* ptr, int B, int H, int N, int d, int64_t stride_b,
+                          int64_t stride_h, int64_t stride_n, int box_rows) {
+  // A dimension of extent 1 never has its stride used for addressing, but the encoder still wants a
+  // multiple of 16 bytes; give it a harmless one.
+  const int64_t sn = stride_n;
+  const int64_t sh = (H > 1) ? stride_h : sn * N;
+  const int64_t sb = (B > 1) ? stride_b : sh * (H > 1 ? H : 1);
+  return encode_bf16_map(map, ptr, {d, N, H, B}, {sn, sh, sb}, {64, box_rows, 1, 1});
 }
 
 uint64_t current_context_id() {

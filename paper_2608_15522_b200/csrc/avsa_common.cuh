@@ -122,6 +122,9 @@ inline bool tensor_ok(const avsa_bf16_4d& t, int B, int H) {
 bool encode_bf16_tile_map(CUtensorMap* map, const void* ptr, int B, int H, int N, int d, int64_t stride_b,
                           int64_t stride_h, int64_t stride_n, int box_rows);
 
+// The same for any four dimensions (in elements, the first one contiguous, strides of the others) and any box.
+bool encode_bf16_map(CUtensorMap* map, const void* ptr, const int64_t (&size)[4], const int64_t (&stride)[3], const int (&box)[4]);
+
 // True when the current device is compute capability 10.x.
 bool device_is_sm100();
 

@@ -55,6 +55,11 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   }
   s.pre_narrow = RS <= kPxNarrow;
   s.own_narrow = R <= kPxNarrow;
+  // Query rows as a box of a tensor map: (G heads, tokens, batch entries) that are the item's rows in their order.
+  if (s.own_narrow) s.own_box = s.R;
+  else if (128 % s.G == 0) s.own_box = 128;
+  if (s.stack && s.pre_narrow) s.pre_box = static_cast<int>(RS);
+  else if (s.stack && 128 % s.R == 0) s.pre_box = 128;
   s.queue = TO > 1 && F * Hkv > y.n_cta;
   s.nb_max = s.queue ? 8 * y.n_cta : y.n_cta;
   const size_t pre = s.stack ? (static_cast<size_t>(y.n_cta) + static_cast<size_t>(Hkv) * s.nrc * s.chunk) * 128 : 0;
@@ -90,15 +95,27 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
 template <int D>
 static int launch_prefix(const PrefixLayout& y, const avsa_bf16_4d& k, const avsa_bf16_4d& v, const PrefixParams& p, cudaStream_t st) {
   const PrefixShape& s = y.s;
-  CUtensorMap tk, tv;
+  CUtensorMap tk, tv, tq_own, tq_pre;
   if (!encode_bf16_tile_map(&tk, k.ptr, s.pages, s.Hkv, s.page, D, k.stride_b, k.stride_h, k.stride_n, s.page) ||
       !encode_bf16_tile_map(&tv, v.ptr, s.pages, s.Hkv, s.page, D, v.stride_b, v.stride_h, v.stride_n, s.page))
     return AVSA_ERR_CUDA;
+  {
+    // (an axis of one element has no stride to speak of: any multiple of 16 bytes)
+    const int H = s.Hkv * s.G;
+    const int64_t sh = H > 1 ? p.q.stride_h : D, sn = s.L > 1 ? p.q.stride_n : D, sb = s.B > 1 ? p.q.stride_b : D;
+    auto box = [&](CUtensorMap* map, int tokens, int entries) {
+      return encode_bf16_map(map, p.q.ptr, {D, H, s.L, s.B}, {sh, sn, sb}, {64, s.G, tokens, entries});
+    };
+    if (s.own_box > 0 && !box(&tq_own, s.own_box / s.G, 1)) return AVSA_ERR_CUDA;
+    if (s.pre_box > 0 && !box(&tq_pre, s.L, s.pre_box / s.R)) return AVSA_ERR_CUDA;
+    if (s.own_box == 0) tq_own = tk;      // (not used)
+    if (s.pre_box == 0) tq_pre = tk;
+  }
   if (s.queue && launch_pdl(clear_counter_kernel, 1, 1, 0, st, p.counter) != cudaSuccess) return AVSA_ERR_CUDA;
   const bool slim = s.own_narrow || (s.stack && s.pre_narrow), wide = !s.own_narrow || (s.stack && !s.pre_narrow);
   auto kernel = slim && wide ? prefix_attn_kernel<D, kPxBoth> : slim ? prefix_attn_kernel<D, kPxSlim> : prefix_attn_kernel<D, kPxWide>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PrefixSmem<D>::kTotal) != cudaSuccess) return AVSA_ERR_CUDA;
-  if (launch_pdl(kernel, y.n_cta, kPxThreads, PrefixSmem<D>::kTotal, st, tk, tv, p) != cudaSuccess) return AVSA_ERR_CUDA;
+  if (launch_pdl(kernel, y.n_cta, kPxThreads, PrefixSmem<D>::kTotal, st, tk, tv, tq_own, tq_pre, p) != cudaSuccess) return AVSA_ERR_CUDA;
   // (cut rows: at most nb_max times 128, a warp each)
   const long long most = static_cast<long long>(s.nb_max) * 128 / kPxMergeWarps, ctas = 8ll * y.n_cta;
   dim3 grid(static_cast<unsigned>(most < ctas ? most : ctas));

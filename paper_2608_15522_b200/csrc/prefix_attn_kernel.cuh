@@ -17,8 +17,8 @@
 //
 // Pipeline (one persistent CTA per SM): as in attn_persist_kernel.cuh, whose softmax against one fixed reference per row this is:
 // K and V tiles through two rings of TMA loads, here page by page (a page id beyond the pool reads as zeros: what lies behind the
-// last page), S = Q K^T and O += P V by tcgen05 from two issuing warps, two softmax groups of four warps on alternate key tiles.  Query rows are gathered by
-// two warps with cp.async, since neighbouring rows of a tile lie in different heads or sequences.  An item with a row that outgrew its reference runs again
+// last page), S = Q K^T and O += P V by tcgen05 from two issuing warps, two softmax groups of four warps on alternate key tiles.  The query rows of an item are a
+// box of (heads, tokens, batch entries) where the sizes allow it, else two warps gather them with cp.async (1500 cycles more).  An item with a row that outgrew its reference runs again
 // in the same CTA: once for the row maxima alone, once with these as the references.
 #pragma once
 #include <math.h>
@@ -72,6 +72,7 @@ struct PrefixShape {
   int TP, chunk, nrc;  // row tiles of the stacked rows, taken `chunk` at a time (nrc times)
   int rows;            // rows of an own item's partial result: min(128, R)
   int queue;           // whole items off a queue
+  int pre_box, own_box;        // rows of the TMA box that holds the query rows of an item; 0: they are gathered
   int pre_narrow, own_narrow;  // rows of the stacked items, of the own ones: at most kPxNarrow
   int nb_max;          // B pieces at most
   int page, page_shift, pages, seqs, width;
@@ -166,7 +167,8 @@ __device__ __forceinline__ float lane_reduce(float (&v)[N], Op op) {
       v[i] = op(keep, __shfl_xor_sync(0xffffffffu, give, d));
     }
   }
-  if constexpr (N == 16) v[0] = op(v[0], __shfl_xor_sync(0xffffffffu, v[0], 16));
+#pragma unroll
+  for (int d = N; d < 32; d <<= 1) v[0] = op(v[0], __shfl_xor_sync(0xffffffffu, v[0], d));
   return v[0];
 }
 
@@ -195,7 +197,8 @@ enum { kPxWide = 1, kPxSlim = 2, kPxBoth = 3 };
 
 template <int D, int KINDS>
 __global__ void __launch_bounds__(kPxThreads, 1)
-prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const __grid_constant__ PrefixParams p) {
+prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const __grid_constant__ CUtensorMap tmq_own,
+                   const __grid_constant__ CUtensorMap tmq_pre, const __grid_constant__ PrefixParams p) {
   using L_ = PrefixSmem<D>;
   constexpr int NPANEL = D / 64, PANEL = 128 * 128, KS = L_::kKS, VS = L_::kVS;
   constexpr unsigned FULLM = 0xffffffffu;
@@ -272,6 +275,8 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     fence_mbar_init();
     prefetch_tmap(&tmk);
     prefetch_tmap(&tmv);
+    prefetch_tmap(&tmq_own);
+    if (S.stack) prefetch_tmap(&tmq_pre);
   }
   if (warp == 2) {
     tmem_alloc(smem_u32(smem + L_::kMisc), 512);
@@ -382,6 +387,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     constexpr int VPR = D / 8, RPI = 32 / VPR;      // 16-byte vectors of a row; rows of an instruction
     const uint32_t base = smem_u32(smem + L_::kQ);
+    int q_loads = 0;          // items up to the last one whose rows came by TMA
     bool ok = true;
 #pragma unroll 1
     for (int n = 0; ok; n++) {
@@ -392,6 +398,21 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       if (ok && n >= 1 && !narrow && L_::kQSlot == 0) ok = wait_all(Q_EMPTY + ((n - 1) & 1), ((n - 1) >> 1) & 1, kPxQEmpty, n);      // one buffer
       if (!ok) break;
       const uint32_t dst = base + (n & 1) * (narrow ? L_::kNarrowSlot : L_::kQSlot);
+      const bool stacked = (it.type & 1) != 0;
+      const int box = stacked ? S.pre_box : S.own_box;
+      if (box > 0) {
+        if (warp == 13 && lane == 0) {
+          mbar_expect_tx(BAR(Q_FULL + (n & 1)), box * 128 * NPANEL);
+          const int token = stacked ? 0 : S.by_G.div(it.row0), entry = stacked ? S.by_R.div(it.row0) : it.b;
+          for (int pn = 0; pn < NPANEL; pn++)
+            tma_load_4d(dst + pn * PANEL, stacked ? &tmq_pre : &tmq_own, BAR(Q_FULL + (n & 1)), pn * 64, it.hk * S.G, token, entry);
+        } else {
+          mbar_arrive(BAR(Q_FULL + (n & 1)));
+        }
+        q_loads = n + 1;
+        item_done(n);
+        continue;
+      }
 #pragma unroll 1
       for (int r0 = (warp - 13) * 32; r0 < it.nrows; r0 += 32 * kPxQWarps) {
         int64_t off = 0;
@@ -419,6 +440,8 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       mbar_arrive(BAR(Q_FULL + (n & 1)));
       item_done(n);
     }
+    if (misc[STOP] != 0)
+      for (int c = max(0, q_loads - 2); c < q_loads; c++) mbar_wait(BAR(Q_FULL + (c & 1)), (c >> 1) & 1);
   } else if (warp == 3) {
     // ------------------------------------------------------------------ scheduler
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
@@ -432,14 +455,12 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     auto publish = [&](const PrefixItem& it) -> bool {
       const int m = published, slot = m % kPxRing;
       int page = S.pages;
-      if (it.type >= 0) {
-        const int e0 = it.pos0 >> S.page_shift, e = e0 + lane;
-        if (e < min(e0 + (it.cnt << (7 - S.page_shift)), (it.kv_end + S.page - 1) >> S.page_shift)) {
-          page = p.table[static_cast<int64_t>(it.slot) * S.width + e];
-          if (page < 0 || page >= S.pages) {
-            report(AVSA_ERR_BAD_TABLE, kPrefixPage, it.slot, e);
-            page = S.pages;
-          }
+      const int e0 = it.pos0 >> S.page_shift, e = e0 + lane;
+      if (e < min(e0 + (it.cnt << (7 - S.page_shift)), (it.kv_end + S.page - 1) >> S.page_shift)) {
+        page = p.table[static_cast<int64_t>(it.slot) * S.width + e];
+        if (page < 0 || page >= S.pages) {
+          report(AVSA_ERR_BAD_TABLE, kPrefixPage, it.slot, e);
+          page = S.pages;
         }
       }
       if (m >= kPxRing && !wait_all(ITEM_EMPTY + slot, ((m / kPxRing) - 1) & 1, kPxItemEmpty, m)) return false;
@@ -461,7 +482,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
         it.type |= i & 1 ? 4 : 2;
         if (!publish(it)) return false;
       }
-      return all_done();
+      return listed == 0 || all_done();
     };
     // Lane l: the own item f0 + l of a key head.
     auto own_items = [&](int f0, int& nt, int& len, int& slot) {
@@ -484,6 +505,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       }
       return v;
     };
+    int nt0 = 0, len0 = 0, slot0 = -1;      // own_items(0)
     // ---- the plan
     PrefixPlan P = {};
     int n_pre = 0;
@@ -493,6 +515,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       for (int f0 = 0; f0 < S.F; f0 += 32) {
         int nt, len, slot;
         own_items(f0, nt, len, slot);
+        if (f0 == 0) nt0 = nt, len0 = len, slot0 = slot;
         W += nt;
         if (len > most) most = len, at = slot;
       }
@@ -588,8 +611,13 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
 #pragma unroll 1
         for (int f0 = only < 0 ? 0 : only & ~31; ok && f0 < f_end && before < u1; f0 += 32) {
           int nt = 0, len = 0, slot = -1;
-          if (id >= n_pre) own_items(f0, nt, len, slot);
-          else if (lane == 0) nt = per;
+          if (id < n_pre) {
+            if (lane == 0) nt = per;
+          } else if (f0 == 0) {
+            nt = nt0, len = len0, slot = slot0;
+          } else {
+            own_items(f0, nt, len, slot);
+          }
           const int inc = scan(nt), first = before + inc - nt;
           const int lo = only < 0 ? max(u, first) : first, hi = only < 0 ? min(u1, before + inc) : only == f0 + lane ? first + nt : first;
           before += __shfl_sync(FULLM, inc, 31);
@@ -658,10 +686,9 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     }
     // (a row can outgrow its reference only in the first run, so settling once is enough)
     if (ok) ok = settle();
-    if (ok) {
-      PrefixItem end = {};
-      end.type = -1;
-      publish(end);
+    if (ok && lane == 0) {      // (all items are done: the slot is free)
+      ring[published % kPxRing].type = -1;
+      mbar_arrive(BAR(ITEM_FULL + published % kPxRing));
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ Q K^T issuer
@@ -751,9 +778,12 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       }
       if (ok) item_done(n);
     }
-    if (leader) umma_commit(BAR(QK_DRAIN));
-    __syncwarp();
-    mbar_wait(BAR(QK_DRAIN), 0);
+    // tensor memory must not be freed under a running product (of items that have been read out none is)
+    if (misc[STOP] != 0) {
+      if (leader) umma_commit(BAR(QK_DRAIN));
+      __syncwarp();
+      mbar_wait(BAR(QK_DRAIN), 0);
+    }
   } else if (warp == 2) {
     // ------------------------------------------------------------------ P V issuer
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
@@ -865,9 +895,11 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       }
       if (ok) item_done(n);
     }
-    if (leader) umma_commit(BAR(PV_DRAIN));
-    __syncwarp();
-    mbar_wait(BAR(PV_DRAIN), 0);
+    if (misc[STOP] != 0) {
+      if (leader) umma_commit(BAR(PV_DRAIN));
+      __syncwarp();
+      mbar_wait(BAR(PV_DRAIN), 0);
+    }
   } else if (warp == 15) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
   } else {
@@ -886,7 +918,8 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     float n_given = 0.f;
     // A narrow item: the thread's lane is a key (S^T) and then a channel (O^T), the columns are the query rows.
     auto narrow_item = [&](auto columns, const PrefixItem& it, int n) -> bool {
-      constexpr int N = decltype(columns)::value;
+      constexpr int N = decltype(columns)::value;      // columns that are looked at (the product's are 16 or 32)
+      constexpr int NP = N < 16 ? 16 : N;
       const int wq = warp & 3, run = (it.type >> 1) & 3;
       // lane r: how far row r sees, from the item's first key on
       int rel = 0x7fffffff;
@@ -913,7 +946,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       }
       float* ref = mref_s + w * 32;
       const uint32_t p_even = static_cast<uint32_t>(((row & 63) & ~1) * 2) ^ (static_cast<uint32_t>(lane & 1) << 4);
-      const uint32_t p_base = smem_u32(smem + L_::kQ + L_::kNarrowP) + w * 16384 + (row >> 6) * (N * 128) + (lane & 1) * 128;
+      const uint32_t p_base = smem_u32(smem + L_::kQ + L_::kNarrowP) + w * 16384 + (row >> 6) * (NP * 128) + (lane & 1) * 128;
 #pragma unroll 1
       for (int t = 0; t < it.cnt; t++) {
         const int k = n_tiles & 1;
@@ -921,7 +954,9 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
         tc_fence_after();
         uint32_t s[N];
         if constexpr (N == 32) tmem_ld32(tmem + lane_off + w * 64 + k * 32, s);
-        else tmem_ld16(tmem + lane_off + w * 64 + k * 32, s);
+        else if constexpr (N == 16) tmem_ld16(tmem + lane_off + w * 64 + k * 32, s);
+        else if constexpr (N == 8) tmem_ld8(tmem + lane_off + w * 64 + k * 32, s);
+        else tmem_ld2(tmem + lane_off + w * 64 + k * 32, s);
         tmem_wait_ld_regs(s);
         tc_fence_before();
         mbar_arrive(BAR(NS_FREE + 2 * w + k));
@@ -949,12 +984,10 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
           }
           if (!wait_all(NREF + w, n_refs & 1, kPxMref, n)) return false;
 #pragma unroll
-          for (int r = 0; r < N; r += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(ref + r);
+          for (int r = 0; r < N; r += 2) {
+            const float2 v = *reinterpret_cast<const float2*>(ref + r);
             nm[r] = -v.x;
             nm[r + 1] = -v.y;
-            nm[r + 2] = -v.z;
-            nm[r + 3] = -v.w;
           }
         }
         const uint64_t c2 = pack_f32x2(p.scale_log2, p.scale_log2);
@@ -1051,7 +1084,10 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       if (!get_item(n, it)) break;
       if (is_narrow(it.type)) {
         if (it.group == w) {
-          ok = it.nrows > 16 ? narrow_item(std::integral_constant<int, 32>(), it, n) : narrow_item(std::integral_constant<int, 16>(), it, n);
+          if (it.nrows <= 2) ok = narrow_item(std::integral_constant<int, 2>(), it, n);
+          else if (it.nrows <= 8) ok = narrow_item(std::integral_constant<int, 8>(), it, n);
+          else if (it.nrows <= 16) ok = narrow_item(std::integral_constant<int, 16>(), it, n);
+          else ok = narrow_item(std::integral_constant<int, 32>(), it, n);
           if (!ok) break;
         }
         item_done(n);
