@@ -1,7 +1,7 @@
 // Attention of a batch that shares a long beginning, over a paged cache.
 #include <math.h>
 
-#include "prefix_attn_kernel.cuh"
+#include "prefix_stream.cuh"
 
 namespace avsa {
 
@@ -13,9 +13,15 @@ static __global__ void clear_counter_kernel(int* counter) {
 
 constexpr int kChunk = 8;        // row tiles that go through the beginning side by side, at most
 
+constexpr int kStreamRows = 32;      // query rows of a batch entry and key head that the stream kernel takes, at most; of the stacked rows as well
+
 struct PrefixLayout {
   PrefixShape s;
-  int n_cta;
+  int n_cta;                    // of the tile kernel
+  int tile;                     // there is one
+  int pre_stream, own_stream;   // the stream kernel takes the beginning, the own items
+  StreamParams pre, own;
+  int own_cluster;
   size_t rows;                  // partial rows
   int own_row0, cut_row0;
   size_t plan, cta_err, own_rec, cut_rec, redo, lse, o, total;       // offsets in the workspace
@@ -31,7 +37,7 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   s.L = L;
   const long long R = static_cast<long long>(L) * s.G, TO = (R + 127) / 128, F = TO * B, RS = R * B, TP = (RS + 127) / 128;
   const long long most = (static_cast<long long>(width) * page + 127) / 128, PT = static_cast<long long>(prefix_pages) * page / 128;
-  if (RS > 0x3fffffffll || F * Hkv > 0x3fffffffll || F * Hkv * (most > 0 ? most : 1) > 0x7fffffffll) return false;
+  if (RS > 0x3fffffffll || F * Hkv > 0x3fffffffll || RS * Hkv > 0x3fffffffll || F * Hkv * (most > 0 ? most : 1) > 0x7fffffffll) return false;
   s.R = static_cast<int>(R);
   s.TO = static_cast<int>(TO);
   s.F = static_cast<int>(F);
@@ -41,33 +47,75 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   s.page_shift = page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7;
   const int sms = persistent_grid(1 << 30);
   // Stacked, the beginning's key tiles are walked TP times a head instead of F times, but every row goes through the merge, which costs a key
-  // tile's time for about six rows (149760 rows: 108 us, a tile of every SM 0.8).
-  s.stack = TP * PT + RS / 6 + 2 <= F * PT;
-  const long long units = F * Hkv * most + (s.stack ? TP * Hkv * PT : 0);
+  // tile's time for about six rows (149760 rows: 108 us, a tile of every SM 0.8), and the call has a kernel more (about eight tiles' time of every SM).
+  s.stack = TP * PT + RS / 6 < F * PT && (F * PT - TP * PT - RS / 6) * Hkv > 8 * sms;
+  if (s.stack) s.k0 = prefix_pages * page;
+  y.own_stream = R <= kStreamRows;
+  y.pre_stream = s.stack && RS <= kStreamRows;
+  y.tile = !y.own_stream || (s.stack && !y.pre_stream);
+  s.own_off = y.own_stream;
+  const long long units = (y.own_stream ? 0 : F * Hkv * most) + (s.stack ? TP * Hkv * PT : 0);
   y.n_cta = static_cast<int>(units < sms ? units : sms);
   if (y.n_cta < 1) y.n_cta = 1;
   if (s.stack) {
-    s.k0 = prefix_pages * page;
     s.TP = static_cast<int>(TP);
     const int side = kChunk < y.n_cta ? kChunk : y.n_cta;
     s.nrc = (s.TP + side - 1) / side;
     s.chunk = (s.TP + s.nrc - 1) / s.nrc;
   }
-  s.pre_narrow = RS <= kPxNarrow;
-  s.own_narrow = R <= kPxNarrow;
   // Query rows as a box of a tensor map: (G heads, tokens, batch entries) that are the item's rows in their order.
-  if (s.own_narrow) s.own_box = s.R;
-  else if (128 % s.G == 0) s.own_box = 128;
-  if (s.stack && s.pre_narrow) s.pre_box = static_cast<int>(RS);
-  else if (s.stack && 128 % s.R == 0) s.pre_box = 128;
-  s.queue = TO > 1 && F * Hkv > y.n_cta;
+  if (128 % s.G == 0) s.own_box = 128;
+  if (s.stack && 128 % s.R == 0) s.pre_box = 128;
+  s.queue = !y.own_stream && TO > 1 && F * Hkv > y.n_cta;
   s.nb_max = s.queue ? 8 * y.n_cta : y.n_cta;
-  const size_t pre = s.stack ? (static_cast<size_t>(y.n_cta) + static_cast<size_t>(Hkv) * s.nrc * s.chunk) * 128 : 0;
-  const size_t own = s.stack ? static_cast<size_t>(F) * Hkv * s.rows : 0;
-  y.rows = pre + own + 2 * static_cast<size_t>(s.nb_max) * s.rows;
+  // the stream kernel: CTAs that an SM holds, times SMs, are to be busy
+  const int slots = sms * 2;
+  size_t rows = 0;
+  y.pre = {};
+  y.own = {};
+  if (y.pre_stream) {
+    y.pre.stacked = 1;
+    y.pre.first = 1;
+    y.pre.begin = 1;
+    y.pre.tiles = static_cast<int>((RS + kStRows - 1) / kStRows);
+    y.pre.items = y.pre.tiles * Hkv;
+    const long long by_keys = PT / 2;      // 256 keys a CTA at least: four blocks a warp
+    y.pre.splits = static_cast<int>(slots / y.pre.items < by_keys ? slots / y.pre.items : by_keys);
+    if (y.pre.splits < 1) y.pre.splits = 1;
+    rows += static_cast<size_t>(y.pre.items) * y.pre.splits * kStRows;
+  } else if (s.stack) {
+    rows += (static_cast<size_t>(y.n_cta) + static_cast<size_t>(Hkv) * s.nrc * s.chunk) * 128;
+  }
+  const size_t own0 = rows;
+  if (y.own_stream) {
+    y.own.first = !s.stack;
+    y.own.join = !s.stack ? 0 : y.pre_stream ? kStJoinStream : kStJoinTile;
+    y.own.join_tiles = y.pre.tiles;
+    y.own.join_splits = y.pre.splits;
+    y.own.tiles = static_cast<int>((R + kStRows - 1) / kStRows);
+    y.own.items = y.own.tiles * Hkv * B;
+    y.own.out0 = static_cast<int>(own0);
+    const long long keys = static_cast<long long>(width) * page - s.k0;      // at most
+    // An item's keys over a cluster: all slots busy, and no CTA with more than 1024 keys while others have none.  What eight CTAs an item do not fill
+    // is cut into parts that a kernel behind joins.
+    y.own_cluster = 1;
+    while (y.own_cluster < 8 && keys > 128ll * y.own_cluster && (static_cast<long long>(y.own.items) * y.own_cluster < slots || keys > 1024ll * y.own_cluster)) y.own_cluster *= 2;
+    y.own.splits = 1;
+    if (static_cast<long long>(y.own.items) * 8 < sms && keys >= 4096) {
+      y.own_cluster = 1;
+      y.own.splits = slots / y.own.items;
+      rows += static_cast<size_t>(y.own.items) * y.own.splits * kStRows;
+    }
+    y.own.check = 1;
+    y.own.begin = !y.pre_stream;
+  } else {
+    const size_t own = s.stack ? static_cast<size_t>(F) * Hkv * s.rows : 0;
+    y.cut_row0 = static_cast<int>(own0 + own);
+    rows = own0 + own + 2 * static_cast<size_t>(s.nb_max) * s.rows;
+  }
+  y.own_row0 = static_cast<int>(own0);
+  y.rows = rows;
   if (y.rows > 0x7fffffffu) return false;
-  y.own_row0 = static_cast<int>(pre);
-  y.cut_row0 = static_cast<int>(pre + own);
   s.by_R = Divisor(s.R);
   s.by_G = Divisor(s.G);
   s.by_TO = Divisor(s.TO);
@@ -80,7 +128,7 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   y.cta_err = at;
   at += align_up(static_cast<size_t>(y.n_cta) * 32, 256);
   y.own_rec = at;
-  at += align_up(s.stack ? static_cast<size_t>(F) * Hkv * 8 : 0, 256);
+  at += align_up(s.stack && !y.own_stream ? static_cast<size_t>(F) * Hkv * 8 : 0, 256);
   y.cut_rec = at;
   at += align_up(static_cast<size_t>(s.nb_max) * 8, 256);
   y.redo = at;
@@ -93,34 +141,61 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
 }
 
 template <int D>
-static int launch_prefix(const PrefixLayout& y, const avsa_bf16_4d& k, const avsa_bf16_4d& v, const PrefixParams& p, cudaStream_t st) {
+static int launch_stream(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixParams& p, const StreamParams& t, int cluster, cudaStream_t st) {
+  // (8 rows or less: the second product's columns would be empty)
+  auto kernel = (t.stacked ? p.s.B * p.s.R : p.s.R) <= 8 ? prefix_stream_kernel<D, 1> : prefix_stream_kernel<D, 2>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(StreamSmem<D>)) != cudaSuccess) return AVSA_ERR_CUDA;
+  const unsigned grid = static_cast<unsigned>((static_cast<long long>(t.items) * t.splits + t.check) * cluster);
+  return launch_pdl_clusters(kernel, cluster, grid, kStThreads, sizeof(StreamSmem<D>), st, tk, tv, p, t) == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
+}
+
+template <int D>
+static int launch_tile(const PrefixLayout& y, const avsa_bf16_4d& k, const avsa_bf16_4d& v, const PrefixParams& p, cudaStream_t st) {
   const PrefixShape& s = y.s;
   CUtensorMap tk, tv, tq_own, tq_pre;
   if (!encode_bf16_tile_map(&tk, k.ptr, s.pages, s.Hkv, s.page, D, k.stride_b, k.stride_h, k.stride_n, s.page) ||
       !encode_bf16_tile_map(&tv, v.ptr, s.pages, s.Hkv, s.page, D, v.stride_b, v.stride_h, v.stride_n, s.page))
     return AVSA_ERR_CUDA;
-  {
-    // (an axis of one element has no stride to speak of: any multiple of 16 bytes)
-    const int H = s.Hkv * s.G;
-    const int64_t sh = H > 1 ? p.q.stride_h : D, sn = s.L > 1 ? p.q.stride_n : D, sb = s.B > 1 ? p.q.stride_b : D;
-    auto box = [&](CUtensorMap* map, int tokens, int entries) {
-      return encode_bf16_map(map, p.q.ptr, {D, H, s.L, s.B}, {sh, sn, sb}, {64, s.G, tokens, entries});
-    };
-    if (s.own_box > 0 && !box(&tq_own, s.own_box / s.G, 1)) return AVSA_ERR_CUDA;
-    if (s.pre_box > 0 && !box(&tq_pre, s.L, s.pre_box / s.R)) return AVSA_ERR_CUDA;
-    if (s.own_box == 0) tq_own = tk;      // (not used)
-    if (s.pre_box == 0) tq_pre = tk;
-  }
+  // (an axis of one element has no stride to speak of: any multiple of 16 bytes)
+  const int H = s.Hkv * s.G;
+  const int64_t sh = H > 1 ? p.q.stride_h : D, sn = s.L > 1 ? p.q.stride_n : D, sb = s.B > 1 ? p.q.stride_b : D;
+  auto box = [&](CUtensorMap* map, int tokens, int entries) {
+    return encode_bf16_map(map, p.q.ptr, {D, H, s.L, s.B}, {sh, sn, sb}, {64, s.G, tokens, entries});
+  };
+  tq_own = tq_pre = tk;      // (where there is no box)
+  if (!s.own_off && s.own_box > 0 && !box(&tq_own, s.own_box / s.G, 1)) return AVSA_ERR_CUDA;
+  if (s.pre_box > 0 && !box(&tq_pre, s.L, s.pre_box / s.R)) return AVSA_ERR_CUDA;
   if (s.queue && launch_pdl(clear_counter_kernel, 1, 1, 0, st, p.counter) != cudaSuccess) return AVSA_ERR_CUDA;
-  const bool slim = s.own_narrow || (s.stack && s.pre_narrow), wide = !s.own_narrow || (s.stack && !s.pre_narrow);
-  auto kernel = slim && wide ? prefix_attn_kernel<D, kPxBoth> : slim ? prefix_attn_kernel<D, kPxSlim> : prefix_attn_kernel<D, kPxWide>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PrefixSmem<D>::kTotal) != cudaSuccess) return AVSA_ERR_CUDA;
-  if (launch_pdl(kernel, y.n_cta, kPxThreads, PrefixSmem<D>::kTotal, st, tk, tv, tq_own, tq_pre, p) != cudaSuccess) return AVSA_ERR_CUDA;
-  // (cut rows: at most nb_max times 128, a warp each)
-  const long long most = static_cast<long long>(s.nb_max) * 128 / kPxMergeWarps, ctas = 8ll * y.n_cta;
-  dim3 grid(static_cast<unsigned>(most < ctas ? most : ctas));
-  if (s.stack) grid = dim3(static_cast<unsigned>((static_cast<long long>(s.B) * s.R * s.Hkv + kPxMergeWarps - 1) / kPxMergeWarps));
-  if (launch_pdl(prefix_merge_kernel<D>, grid, kPxMergeWarps * 32, 0, st, p, y.n_cta) != cudaSuccess) return AVSA_ERR_CUDA;
+  if (cudaFuncSetAttribute(prefix_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PrefixSmem<D>::kTotal) != cudaSuccess) return AVSA_ERR_CUDA;
+  return launch_pdl(prefix_attn_kernel<D>, y.n_cta, kPxThreads, PrefixSmem<D>::kTotal, st, tk, tv, tq_own, tq_pre, p) == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
+}
+
+template <int D>
+static int launch_prefix(const PrefixLayout& y, const avsa_bf16_4d& k, const avsa_bf16_4d& v, const PrefixParams& p, cudaStream_t st) {
+  const PrefixShape& s = y.s;
+  int r = AVSA_OK;
+  CUtensorMap tk, tv;      // of 16 keys
+  if (y.own_stream && (!encode_bf16_tile_map(&tk, k.ptr, s.pages, s.Hkv, s.page, D, k.stride_b, k.stride_h, k.stride_n, 16) ||
+                       !encode_bf16_tile_map(&tv, v.ptr, s.pages, s.Hkv, s.page, D, v.stride_b, v.stride_h, v.stride_n, 16)))
+    return AVSA_ERR_CUDA;
+  if (y.pre_stream) r = launch_stream<D>(tk, tv, p, y.pre, 1, st);
+  if (y.tile) r = launch_tile<D>(y, k, v, p, st);
+  if (r != AVSA_OK) return r;
+  if (y.own_stream) {
+    r = launch_stream<D>(tk, tv, p, y.own, y.own_cluster, st);
+    if (r != AVSA_OK) return r;
+    if (y.own.splits > 1) {
+      const long long rows = static_cast<long long>(s.B) * s.Hkv * s.R;
+      if (launch_pdl(prefix_join_kernel<D>, static_cast<unsigned>((rows + kPxMergeWarps - 1) / kPxMergeWarps), kPxMergeWarps * 32, 0, st, p, y.own) != cudaSuccess)
+        return AVSA_ERR_CUDA;
+    }
+  } else {
+    // (cut rows: at most nb_max times 128, a warp each)
+    const long long most = static_cast<long long>(s.nb_max) * 128 / kPxMergeWarps, ctas = 8ll * y.n_cta;
+    dim3 grid(static_cast<unsigned>(most < ctas ? most : ctas));
+    if (s.stack) grid = dim3(static_cast<unsigned>((static_cast<long long>(s.B) * s.R * s.Hkv + kPxMergeWarps - 1) / kPxMergeWarps));
+    if (launch_pdl(prefix_merge_kernel<D>, grid, kPxMergeWarps * 32, 0, st, p, y.n_cta) != cudaSuccess) return AVSA_ERR_CUDA;
+  }
   return cudaGetLastError() == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
 }
 
@@ -172,6 +247,8 @@ extern "C" int avsa_prefix_attn(int B, int H, int Hkv, int L, int d, int page, i
   PrefixParams p = {};
   p.s = y.s;
   p.q = q;
+  p.k = k_pool;
+  p.v = v_pool;
   p.o = static_cast<__nv_bfloat16*>(o_bf16);
   p.lse = lse;
   p.table = table;
@@ -187,6 +264,7 @@ extern "C" int avsa_prefix_attn(int B, int H, int Hkv, int L, int d, int page, i
   p.redo = reinterpret_cast<PrefixItem*>(w + y.redo);
   p.part_lse2 = reinterpret_cast<float*>(w + y.lse);
   p.part_o = reinterpret_cast<float*>(w + y.o);
+  p.tile_ctas = y.tile ? y.n_cta : 0;
   p.own_row0 = y.own_row0;
   p.cut_row0 = y.cut_row0;
   return d == 128 ? launch_prefix<128>(y, k_pool, v_pool, p, as_stream(stream)) : launch_prefix<64>(y, k_pool, v_pool, p, as_stream(stream));

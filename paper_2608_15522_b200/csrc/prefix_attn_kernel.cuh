@@ -23,8 +23,6 @@
 #pragma once
 #include <math.h>
 
-#include <type_traits>
-
 #include "attn_persist_kernel.cuh"
 
 namespace avsa {
@@ -33,7 +31,6 @@ constexpr int kPxThreads = 512;
 // 512 x 128 registers at launch; then 8 service warps of 64 and 8 softmax warps of 192: 65536 both ways.
 constexpr int kPxServiceRegs = 64, kPxSoftmaxRegs = 192;
 static_assert(8 * 32 * kPxServiceRegs + 8 * 32 * kPxSoftmaxRegs <= kPxThreads * 128, "setmaxnreg budget exceeded");
-constexpr int kPxNarrow = 32;            // query rows of a narrow item, at most
 constexpr int kPxRing = 4, kPxRedo = 14;
 constexpr int kPxQWarps = 2;             // warps 13 and 14 gather query rows
 constexpr int kPxConsumers = 4 + kPxQWarps + 8;      // warps that read the item ring
@@ -72,8 +69,8 @@ struct PrefixShape {
   int TP, chunk, nrc;  // row tiles of the stacked rows, taken `chunk` at a time (nrc times)
   int rows;            // rows of an own item's partial result: min(128, R)
   int queue;           // whole items off a queue
+  int own_off;         // the beginning alone: the own items are another kernel's
   int pre_box, own_box;        // rows of the TMA box that holds the query rows of an item; 0: they are gathered
-  int pre_narrow, own_narrow;  // rows of the stacked items, of the own ones: at most kPxNarrow
   int nb_max;          // B pieces at most
   int page, page_shift, pages, seqs, width;
   int causal;
@@ -82,7 +79,7 @@ struct PrefixShape {
 
 struct PrefixParams {
   PrefixShape s;
-  avsa_bf16_4d q;
+  avsa_bf16_4d q, k, v;
   __nv_bfloat16* o;
   float* lse;
   const int32_t *table, *length, *seq;
@@ -97,17 +94,18 @@ struct PrefixParams {
   float* part_o;       // [rows][D]: prefix slots of 128 rows, own items (stack), two cut ends a B piece
   float* part_lse2;
   int own_row0, cut_row0;      // first rows of the latter two
+  int tile_ctas;       // CTAs of the tile kernel
   struct PrefixItem* redo;     // [CTAs][kPxRedo] items to run again
 };
 
 struct PrefixItem {
-  int type;            // -1: no more; bit 0: stacked rows, bits 1-2: 0, or 1 maxima only, 2 with given maxima, bit 3: narrow
+  int type;            // -1: no more; bit 0: stacked rows, bits 1-2: 0, or 1 maxima only, 2 with given maxima
   int b, hk, row0, nrows;
   int pos0, cnt, kv_end;       // first key, key tiles, end of the keys
   int slot;            // row of the page table
   int len;             // own items: tokens of the sequence
   int out;             // first partial row, -1: final rows
-  int group;           // narrow: the softmax group whose item it is
+  int pad;
 };
 static_assert(sizeof(PrefixItem) == 48, "three 16-byte accesses");
 
@@ -115,14 +113,13 @@ template <int D>
 struct PrefixSmem {
   static constexpr int kTile = 128 * D * 2;
   static constexpr int kKS = D == 128 ? 3 : 6, kVS = D == 128 ? 3 : 6;
-  // Query rows: wide, 128 of them (64 channels: two buffers); narrow, two buffers of 32 rows, in front of the two groups' P in the second half of each 16 KB
-  static constexpr int kQ = 0;
-  static constexpr int kQSlot = D == 64 ? 16384 : 0, kNarrowSlot = 32 * 128, kNarrowP = 8192;
+  // (64 channels: two buffers of query rows)
+  static constexpr int kQ = 0, kQSlot = D == 64 ? 16384 : 0;
   static constexpr int kK = 32768;
   static constexpr int kV = kK + kKS * kTile;
   static constexpr int kBars = kV + kVS * kTile;
-  static constexpr int kNumBars = 4 + 2 * kKS + 2 * kVS + 13 + 2 * kPxRing + 4 + 22;
-  static constexpr int kStats = (kBars + kNumBars * 8 + 15) / 16 * 16;       // float mref[128], lsum[2][128]; narrow: mref[2][32], lsum[2][4][32]
+  static constexpr int kNumBars = 4 + 2 * kKS + 2 * kVS + 13 + 2 * kPxRing + 4;
+  static constexpr int kStats = (kBars + kNumBars * 8 + 15) / 16 * 16;       // float mref[128], lsum[2][128]
   static constexpr int kItems = kStats + 3 * 128 * 4;
   static constexpr int kPages = kItems + 48 * kPxRing;                        // int[kPxRing][32]: an item's first pages
   static constexpr int kMisc = kPages + 128 * kPxRing;                        // tmem base, stop, redo flags [2], listed, recomputed, error [4]
@@ -143,6 +140,7 @@ __device__ __forceinline__ int prefix_sequence(const PrefixParams& p, int b, int
 }
 // Key tiles of an own item: row tile rt of a sequence of n tokens.
 __device__ __forceinline__ int prefix_own_tiles(const PrefixShape& s, int n, int rt) {
+  if (s.own_off) return 0;
   int end = n;
   if (s.causal) end = n - s.L + min(s.L - 1, s.by_G.div(rt * 128 + 127)) + 1;
   const int x = end - s.k0;
@@ -152,24 +150,6 @@ __device__ __forceinline__ int prefix_own_tiles(const PrefixShape& s, int n, int
 
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)) : "memory");
-}
-
-// Over the lanes of a warp: lane l gets value l mod N of all lanes, combined.  Every step halves the values that a lane holds.
-template <int N, class Op>
-__device__ __forceinline__ float lane_reduce(float (&v)[N], Op op) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int d = N / 2; d > 0; d >>= 1) {
-    const bool upper = (lane & d) != 0;
-#pragma unroll
-    for (int i = 0; i < d; i++) {
-      const float give = upper ? v[i] : v[i + d], keep = upper ? v[i + d] : v[i];
-      v[i] = op(keep, __shfl_xor_sync(0xffffffffu, give, d));
-    }
-  }
-#pragma unroll
-  for (int d = N; d < 32; d <<= 1) v[0] = op(v[0], __shfl_xor_sync(0xffffffffu, v[0], d));
-  return v[0];
 }
 
 constexpr int kPxMinPiece = 4;       // key tiles: a CTA with fewer ends later than one that takes another's as well
@@ -192,17 +172,13 @@ __device__ __noinline__ void px_report(int* err, int code, int where, int item, 
   }
 }
 
-// Which items a call has.  A kernel for one kind alone is faster: its loops share the instruction cache with less.
-enum { kPxWide = 1, kPxSlim = 2, kPxBoth = 3 };
-
-template <int D, int KINDS>
+template <int D>
 __global__ void __launch_bounds__(kPxThreads, 1)
 prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const __grid_constant__ CUtensorMap tmq_own,
                    const __grid_constant__ CUtensorMap tmq_pre, const __grid_constant__ PrefixParams p) {
   using L_ = PrefixSmem<D>;
   constexpr int NPANEL = D / 64, PANEL = 128 * 128, KS = L_::kKS, VS = L_::kVS;
   constexpr unsigned FULLM = 0xffffffffu;
-  auto is_narrow = [](int type) { return KINDS == kPxBoth ? (type & 8) != 0 : KINDS == kPxSlim; };
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const PrefixShape& S = p.s;
@@ -212,12 +188,9 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
   constexpr int Q_FULL = 0, Q_EMPTY = 2, K_FULL = 4, K_EMPTY = K_FULL + KS, V_FULL = K_EMPTY + KS, V_EMPTY = V_FULL + VS,
                 S_FULL = V_EMPTY + VS, S_FREE = S_FULL + 2, P_FULL = S_FREE + 2 /* + 2*group + half */, P_FREE = P_FULL + 4, O_FULL = P_FREE + 2,
                 O_FREE = O_FULL + 1, MREF = O_FREE + 1, ITEM_FULL = MREF + 1, ITEM_EMPTY = ITEM_FULL + kPxRing, QK_DRAIN = ITEM_EMPTY + kPxRing,
-                PV_DRAIN = QK_DRAIN + 1, LSUM_A = PV_DRAIN + 1, LSUM_B = LSUM_A + 1,
-                NS_FULL = LSUM_B + 1 /* + 2*group + buffer */, NS_FREE = NS_FULL + 4, NP_FULL = NS_FREE + 4 /* + group */, NP_FREE = NP_FULL + 2,
-                NO_FULL = NP_FREE + 2, NO_FREE = NO_FULL + 2, NREF = NO_FREE + 2, NSUM = NREF + 2, NREAD = NSUM + 2;
-  static_assert(NREAD + 2 <= L_::kNumBars, "barrier table too small");
-  // tensor memory: S of group 0 | S of group 1 | O | P of group 0 | P of group 1; narrow: two S buffers of 32 columns of each group | O of each group
-  constexpr uint32_t TM_O = 256, TM_P = 256 + D, TM_NO = 128;
+                PV_DRAIN = QK_DRAIN + 1, LSUM_A = PV_DRAIN + 1, LSUM_B = LSUM_A + 1;
+  static_assert(LSUM_B + 1 <= L_::kNumBars, "barrier table too small");
+  constexpr uint32_t TM_O = 256, TM_P = 256 + D;      // tensor memory: S of group 0 | S of group 1 | O | P of group 0 | P of group 1
   float* mref_s = reinterpret_cast<float*>(smem + L_::kStats);
   float* lsum_s = mref_s + 128;
   PrefixItem* ring = reinterpret_cast<PrefixItem*>(smem + L_::kItems);
@@ -258,19 +231,6 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     mbar_init(BAR(PV_DRAIN), 1);
     mbar_init(BAR(LSUM_A), 256);
     mbar_init(BAR(LSUM_B), 256);
-    for (int g = 0; g < 2; g++) {
-      for (int k = 0; k < 2; k++) {
-        mbar_init(BAR(NS_FULL + 2 * g + k), 1);
-        mbar_init(BAR(NS_FREE + 2 * g + k), 128);
-      }
-      mbar_init(BAR(NP_FULL + g), 128);
-      mbar_init(BAR(NP_FREE + g), 1);
-      mbar_init(BAR(NO_FULL + g), 1);
-      mbar_init(BAR(NO_FREE + g), 128);
-      mbar_init(BAR(NREF + g), 32);
-      mbar_init(BAR(NSUM + g), 128);
-      mbar_init(BAR(NREAD + g), 128);
-    }
     for (int i = STOP; i < ERR + 4; i++) misc[i] = 0;
     fence_mbar_init();
     prefetch_tmap(&tmk);
@@ -335,7 +295,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     for (int n = 0; ok; n++) {
       PrefixItem it;
       if (!get_item(n, it)) break;
-      if (is_k || ((it.type >> 1) & 3) != 1) {
+      if (is_k || (it.type >> 1) != 1) {
         const int32_t* row = p.table + static_cast<int64_t>(max(it.slot, 0)) * S.width;
         const int e0 = it.pos0 >> S.page_shift;      // its pages
         const int e1 = min(e0 + (it.cnt << ppt_shift), (it.kv_end + S.page - 1) >> S.page_shift);
@@ -393,11 +353,10 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     for (int n = 0; ok; n++) {
       PrefixItem it;
       if (!get_item(n, it)) break;
-      const bool narrow = is_narrow(it.type);
       if (n >= 2) ok = wait_all(Q_EMPTY + (n & 1), ((n >> 1) - 1) & 1, kPxQEmpty, n);
-      if (ok && n >= 1 && !narrow && L_::kQSlot == 0) ok = wait_all(Q_EMPTY + ((n - 1) & 1), ((n - 1) >> 1) & 1, kPxQEmpty, n);      // one buffer
+      if (ok && n >= 1 && L_::kQSlot == 0) ok = wait_all(Q_EMPTY + ((n - 1) & 1), ((n - 1) >> 1) & 1, kPxQEmpty, n);      // one buffer
       if (!ok) break;
-      const uint32_t dst = base + (n & 1) * (narrow ? L_::kNarrowSlot : L_::kQSlot);
+      const uint32_t dst = base + (n & 1) * L_::kQSlot;
       const bool stacked = (it.type & 1) != 0;
       const int box = stacked ? S.pre_box : S.own_box;
       if (box > 0) {
@@ -446,7 +405,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     // ------------------------------------------------------------------ scheduler
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     const int n_cta = gridDim.x;
-    int published = 0, kind = -1, turn = 0;
+    int published = 0;
     // The last published item, and all before it, are done.
     auto all_done = [&]() -> bool {
       const int m = published - 1;
@@ -471,7 +430,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       published++;
       return true;
     };
-    // What has been published is done; items with a row that outgrew its reference run again (narrow: both runs by the group whose item it was).
+    // What has been published is done; items with a row that outgrew its reference run again.
     auto settle = [&]() -> bool {
       if (!all_done()) return false;
       const int listed = __shfl_sync(FULLM, misc[LISTED], 0);
@@ -630,7 +589,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
             if (id < n_pre) {
               const int hk = S.by_nrc.div(head), rt = (head - hk * S.nrc) * S.chunk + j;
               if (rt >= S.TP) continue;
-              it.type = S.pre_narrow ? 9 : 1;
+              it.type = 1;
               it.hk = hk;
               it.row0 = rt * 128;
               it.nrows = min(128, S.B * S.R - it.row0);
@@ -640,7 +599,6 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
               it.out = ((S.by_chunk.div(id) + head) * S.chunk + j) * 128;
             } else {
               const int all = __shfl_sync(FULLM, nt, l), b = S.by_TO.div(f), m = head * S.F + f;
-              it.type = S.own_narrow ? 8 : 0;
               it.b = b;
               it.hk = head;
               it.row0 = (f - b * S.TO) * 128;
@@ -660,10 +618,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
                 }
               }
             }
-            // (narrow and wide items use the same memory in different ways: what has been published is done before the other kind begins)
-            if ((kind >= 0 && kind != (it.type & 8)) || __shfl_sync(FULLM, misc[LISTED], 0) >= kPxRedo - kPxRing - 1) ok = settle();
-            kind = it.type & 8;
-            it.group = turn++ & 1;
+            if (__shfl_sync(FULLM, misc[LISTED], 0) >= kPxRedo - kPxRing - 1) ok = settle();
             if (ok) ok = publish(it);
           }
         }
@@ -701,7 +656,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     const uint32_t q_lo = ((smem_u32(smem + L_::kQ) & 0x3FFFFu) >> 4) | (1u << 16);
     const uint32_t k_lo0 = ((smem_u32(smem + L_::kK) & 0x3FFFFu) >> 4) | (1u << 16);
     int stage = 0, round = 0;
-    int used[2] = {0, 0}, nused[2] = {0, 0};
+    int used[2] = {0, 0};
     bool ok = true;
 #pragma unroll 1
     for (int n = 0; ok; n++) {
@@ -709,43 +664,6 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       if (!get_item(n, it)) break;
       const int cnt = it.cnt;
       ok = wait_all(Q_FULL + (n & 1), (n >> 1) & 1, kPxQFull, n);
-      if (is_narrow(it.type)) {
-        // S^T = K Q^T: keys are the lanes, query rows the columns
-        const int g = it.group;
-        const uint32_t idesc = it.nrows > 16 ? make_idesc_bf16(128, 32, 0, 0) : make_idesc_bf16(128, 16, 0, 0);
-        const uint32_t qn_lo = q_lo + (n & 1) * (L_::kNarrowSlot >> 4);
-#pragma unroll 1
-        for (int t = 0; t < cnt && ok; t++) {
-          const int k = nused[g] & 1;
-          ok = wait_all(K_FULL + stage, round & 1, kPxKFull, t);
-          if (!ok) break;
-          if (nused[g] >= 2) {
-            ok = wait_all(NS_FREE + 2 * g + k, ((nused[g] >> 1) - 1) & 1, kPxSFree, t);
-            if (!ok) break;
-          }
-          tc_fence_after();
-          const uint32_t k_lo = k_lo0 + stage * (L_::kTile >> 4);
-          const uint32_t tm_s = tmem_u + g * 64 + k * 32;
-          if (leader) {
-#pragma unroll
-            for (int ks = 0; ks < D / 16; ks++) {
-              const uint32_t off = ((ks >> 2) * PANEL + (ks & 3) * 32) >> 4;
-              umma_ss(tm_s, desc64(k_lo + off), desc64(qn_lo + off), idesc, ks > 0 ? 1u : 0u);
-            }
-            umma_commit(BAR(NS_FULL + 2 * g + k));
-            umma_commit(BAR(K_EMPTY + stage));
-            if (t == cnt - 1) umma_commit(BAR(Q_EMPTY + (n & 1)));
-          }
-          __syncwarp();
-          nused[g]++;
-          if (++stage == KS) {
-            stage = 0;
-            round++;
-          }
-        }
-        if (ok) item_done(n);
-        continue;
-      }
       const uint32_t qw_lo = q_lo + (n & 1) * (L_::kQSlot >> 4);
 #pragma unroll 1
       for (int t = 0; t < cnt && ok; t++) {
@@ -800,22 +718,15 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
         umma_ts(tmem_u + TM_O, tm_buf + ks * 8, desc64(v_lo + ks * (2048 >> 4)), idesc_pv, kk > 0 ? 1u : acc_first);
       }
     };
-    // O^T += V^T P^T: channels are the lanes (with 64 of them the upper 64 lanes read the tile 8 keys on, for nothing), query rows the columns
-    constexpr uint32_t ndesc_hi = desc_hi;
-    const uint32_t nv_lo0 = ((smem_u32(smem + L_::kV) & 0x3FFFFu) >> 4) | (static_cast<uint32_t>((D == 128 ? PANEL : 1024) >> 4) << 16);
-    const uint32_t np_lo0 = ((smem_u32(smem + L_::kQ + L_::kNarrowP) & 0x3FFFFu) >> 4) | (1u << 16);
-    auto ndesc64 = [](uint32_t lo) { return (static_cast<uint64_t>(ndesc_hi) << 32) | lo; };
     int stage = 0, round = 0, outputs = 0;
-    int used[2] = {0, 0}, nused[2] = {0, 0}, nouts[2] = {0, 0};
+    int used[2] = {0, 0};
     bool ok = true;
 #pragma unroll 1
     for (int n = 0; ok; n++) {
       PrefixItem it;
       if (!get_item(n, it)) break;
-      if (((it.type >> 1) & 3) != 1) {
+      if ((it.type >> 1) != 1) {
         const int cnt = it.cnt;
-        const bool narrow = is_narrow(it.type);
-        const int ng = it.group;
 #pragma unroll 1
         for (int t = 0; t < cnt && ok; t++) {
           const int j = t & 1;
@@ -833,35 +744,6 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
             }
             fence_proxy_async();
             __syncwarp();
-          }
-          if (narrow) {
-            ok = wait_all(NP_FULL + ng, nused[ng] & 1, kPxPFull, t);
-            if (!ok) break;
-            if (t == 0 && nouts[ng] > 0) {
-              ok = wait_all(NO_FREE + ng, (nouts[ng] - 1) & 1, kPxOFree, n);
-              if (!ok) break;
-            }
-            tc_fence_after();
-            if (leader) {
-              const bool n32 = it.nrows > 16;
-              const uint32_t idesc = n32 ? make_idesc_bf16(128, 32, 1, 0) : make_idesc_bf16(128, 16, 1, 0);
-              const uint32_t v_lo = nv_lo0 + stage * (L_::kTile >> 4);
-              const uint32_t p_lo = np_lo0 + ng * (16384 >> 4), panel = n32 ? 4096 >> 4 : 2048 >> 4;
-#pragma unroll
-              for (int ks = 0; ks < 8; ks++)
-                umma_ss(tmem_u + TM_NO + ng * 32, ndesc64(v_lo + ks * (2048 >> 4)), ndesc64(p_lo + (ks >> 2) * panel + (ks & 3) * 2), idesc,
-                        t > 0 || ks > 0 ? 1u : 0u);
-              umma_commit(BAR(NP_FREE + ng));
-              umma_commit(BAR(V_EMPTY + stage));
-              if (t == cnt - 1) umma_commit(BAR(NO_FULL + ng));
-            }
-            __syncwarp();
-            nused[ng]++;
-            if (++stage == VS) {
-              stage = 0;
-              round++;
-            }
-            continue;
           }
           ok = wait_all(P_FULL + 2 * j, used[j] & 1, kPxPFull, t);
           if (!ok) break;
@@ -890,8 +772,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
             round++;
           }
         }
-        if (narrow) nouts[ng]++;
-        else outputs++;
+        outputs++;
       }
       if (ok) item_done(n);
     }
@@ -914,185 +795,11 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     int used = 0;               // P tiles it has written
     int mrefs = 0, outputs = 0; // items with a first-tile reference, with an output
     float m_given = 0.f;
-    int n_tiles = 0, n_p = 0, n_refs = 0, n_outs = 0, n_sums = 0;      // narrow items: of this group
-    float n_given = 0.f;
-    // A narrow item: the thread's lane is a key (S^T) and then a channel (O^T), the columns are the query rows.
-    auto narrow_item = [&](auto columns, const PrefixItem& it, int n) -> bool {
-      constexpr int N = decltype(columns)::value;      // columns that are looked at (the product's are 16 or 32)
-      constexpr int NP = N < 16 ? 16 : N;
-      const int wq = warp & 3, run = (it.type >> 1) & 3;
-      // lane r: how far row r sees, from the item's first key on
-      int rel = 0x7fffffff;
-      if (lane < it.nrows) {
-        int rr = it.row0 + lane, len = it.len;
-        if (it.type & 1) {
-          const int b = S.by_R.div(rr);
-          rr -= b * S.R;
-          int slot, bad;
-          len = prefix_sequence(p, b, slot, bad);
-        }
-        rel = min(it.kv_end, S.causal ? len - S.L + S.by_G.div(rr) + 1 : len) - it.pos0;
-      }
-      const int rel_min = __reduce_min_sync(FULLM, rel);
-      float nm[N], m_max[N];
-      uint64_t l2[N / 2];
-#pragma unroll
-      for (int r = 0; r < N; r++) m_max[r] = -INFINITY;
-#pragma unroll
-      for (int r = 0; r < N / 2; r++) l2[r] = 0ull;
-      if (run == 2) {
-#pragma unroll
-        for (int r = 0; r < N; r++) nm[r] = -__shfl_sync(FULLM, n_given, r);
-      }
-      float* ref = mref_s + w * 32;
-      const uint32_t p_even = static_cast<uint32_t>(((row & 63) & ~1) * 2) ^ (static_cast<uint32_t>(lane & 1) << 4);
-      const uint32_t p_base = smem_u32(smem + L_::kQ + L_::kNarrowP) + w * 16384 + (row >> 6) * (NP * 128) + (lane & 1) * 128;
-#pragma unroll 1
-      for (int t = 0; t < it.cnt; t++) {
-        const int k = n_tiles & 1;
-        if (!wait_all(NS_FULL + 2 * w + k, (n_tiles >> 1) & 1, kPxSFull, t)) return false;
-        tc_fence_after();
-        uint32_t s[N];
-        if constexpr (N == 32) tmem_ld32(tmem + lane_off + w * 64 + k * 32, s);
-        else if constexpr (N == 16) tmem_ld16(tmem + lane_off + w * 64 + k * 32, s);
-        else if constexpr (N == 8) tmem_ld8(tmem + lane_off + w * 64 + k * 32, s);
-        else tmem_ld2(tmem + lane_off + w * 64 + k * 32, s);
-        tmem_wait_ld_regs(s);
-        tc_fence_before();
-        mbar_arrive(BAR(NS_FREE + 2 * w + k));
-        n_tiles++;
-        if (t * 128 + 128 > rel_min) {
-#pragma unroll
-          for (int r = 0; r < N; r++)
-            if (row >= __shfl_sync(FULLM, rel, r) - t * 128) s[r] = 0xff800000u;
-        }
-        if (run == 1) {
-#pragma unroll
-          for (int r = 0; r < N; r++) m_max[r] = fmaxf(m_max[r], __uint_as_float(s[r]));
-          continue;
-        }
-        if (run == 0 && t == 0) {
-          // the reference: a row's maximum over the first 32 keys, which one warp holds (a row that sees any sees the first)
-          if (wq == 0) {
-            if (n_sums > 0 && !wait_all(NREAD + w, (n_sums - 1) & 1, kPxLsum, n)) return false;      // (who reads the item's before)
-            float x[N];
-#pragma unroll
-            for (int r = 0; r < N; r++) x[r] = __uint_as_float(s[r]);
-            const float top = p.scale_log2 * lane_reduce<N>(x, [](float a, float b) { return fmaxf(a, b); });
-            if (lane < N) ref[lane] = top == -INFINITY ? 0.f : top;
-            mbar_arrive(BAR(NREF + w));
-          }
-          if (!wait_all(NREF + w, n_refs & 1, kPxMref, n)) return false;
-#pragma unroll
-          for (int r = 0; r < N; r += 2) {
-            const float2 v = *reinterpret_cast<const float2*>(ref + r);
-            nm[r] = -v.x;
-            nm[r + 1] = -v.y;
-          }
-        }
-        const uint64_t c2 = pack_f32x2(p.scale_log2, p.scale_log2);
-        uint32_t pk[N / 2];
-#pragma unroll
-        for (int r = 0; r < N; r += 2) {
-          float x0, x1;
-          unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[r]), __uint_as_float(s[r + 1])), c2, pack_f32x2(nm[r], nm[r + 1])), x0, x1);
-          const float e0 = fast_exp2(x0), e1 = fast_exp2(x1);
-          l2[r / 2] = add_f32x2(l2[r / 2], pack_f32x2(e0, e1));
-          // neighbouring lanes hold neighbouring keys: the even one stores both of row r, the odd one both of row r + 1
-          const float got = __shfl_xor_sync(FULLM, (lane & 1) ? e0 : e1, 1);
-          pk[r / 2] = (lane & 1) ? pack_bf16x2(got, e1) : pack_bf16x2(e0, got);
-        }
-        if (n_p > 0 && !wait_all(NP_FREE + w, (n_p - 1) & 1, kPxPFree, t)) return false;      // the product that read this group's last P has run
-#pragma unroll
-        for (int r = 0; r < N; r += 2)
-          asm volatile("st.shared.b32 [%0], %1;" ::"r"(p_base + r * 128 + (p_even ^ ((r & 7) << 4))), "r"(pk[r / 2]) : "memory");
-        fence_proxy_async();
-        mbar_arrive(BAR(NP_FULL + w));
-        n_p++;
-      }
-      if (run == 0) n_refs++;
-      // sums (or maxima) over the lanes, then over the warps: lane r holds row r's
-      float x[N];
-#pragma unroll
-      for (int r = 0; r < N; r += 2) {
-        unpack_f32x2(l2[r / 2], x[r], x[r + 1]);
-        if (run == 1) x[r] = m_max[r], x[r + 1] = m_max[r + 1];
-      }
-      const float part = run == 1 ? lane_reduce<N>(x, [](float a, float b) { return fmaxf(a, b); }) : lane_reduce<N>(x, [](float a, float b) { return a + b; });
-      float* sums = mref_s + 64 + w * 128;
-      if (n_sums > 0 && !wait_all(NREAD + w, (n_sums - 1) & 1, kPxLsum, n)) return false;      // the item before has been read
-      if (lane < N) sums[wq * 32 + lane] = part;
-      mbar_arrive(BAR(NSUM + w));
-      if (!wait_all(NSUM + w, n_sums & 1, kPxLsum, n)) return false;
-      n_sums++;
-      const int rl = lane & (N - 1);
-      const float a0 = sums[rl], a1 = sums[32 + rl], a2 = sums[64 + rl], a3 = sums[96 + rl];
-      const float m_ref = run == 2 ? n_given : ref[rl];
-      mbar_arrive(BAR(NREAD + w));
-      if (run == 1) {
-        const float top = p.scale_log2 * fmaxf(fmaxf(a0, a1), fmaxf(a2, a3));
-        n_given = top == -INFINITY ? 0.f : top;
-        return true;
-      }
-      const float sum = (a0 + a1) + (a2 + a3);
-      const bool again = run == 0 && __any_sync(FULLM, lane < it.nrows && !(sum <= kFastRowSumLimit));
-      if (again && wq == 0 && lane == 0) {
-        redo[atomicAdd(const_cast<int*>(&misc[LISTED]), 1)] = it;
-        atomicAdd(const_cast<int*>(&misc[RECOMPUTED]), 1);
-      }
-      if (!wait_all(NO_FULL + w, n_outs & 1, kPxOFull, n)) return false;
-      n_outs++;
-      tc_fence_after();
-      const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
-      const float lse2 = sum != 0.f ? m_ref + log2f(sum) : -INFINITY;
-      // lane r: where row r goes (partial rows: as fp32 rows of D, one behind the other)
-      int64_t to = 0;
-      if (lane < it.nrows && !again) {
-        if (it.out >= 0) {
-          to = static_cast<int64_t>(it.out + lane) * D;
-          if (wq == 0) p.part_lse2[it.out + lane] = lse2;
-        } else {
-          const int rr = it.row0 + lane, i = S.by_G.div(rr), head = it.hk * S.G + rr - i * S.G;
-          to = it.b * p.q.stride_b + head * p.q.stride_h + i * p.q.stride_n;
-          if (wq == 0 && p.lse != nullptr) p.lse[(static_cast<int64_t>(it.b) * S.Hkv * S.G + head) * S.L + i] = lse2 * 0.6931471805599453f;
-        }
-      }
-      const int rows = again ? 0 : it.nrows;
-#pragma unroll 1
-      for (int c = 0; c < rows; c += 8) {
-        uint32_t o[8];
-        tmem_ld8(tmem + TM_NO + w * 32 + lane_off + c, o);
-        tmem_wait_ld_regs(o);
-#pragma unroll
-        for (int r = 0; r < 8; r++) {
-          const float x = __uint_as_float(o[r]) * __shfl_sync(FULLM, inv, c + r);
-          const int64_t at = __shfl_sync(FULLM, to, c + r) + row;
-          if (c + r < rows && row < D) {
-            if (it.out >= 0) p.part_o[at] = x;
-            else p.o[at] = __float2bfloat16(x);
-          }
-        }
-      }
-      tc_fence_before();
-      mbar_arrive(BAR(NO_FREE + w));
-      return true;
-    };
     bool ok = true;
 #pragma unroll 1
     for (int n = 0; ok; n++) {
       PrefixItem it;
       if (!get_item(n, it)) break;
-      if (is_narrow(it.type)) {
-        if (it.group == w) {
-          if (it.nrows <= 2) ok = narrow_item(std::integral_constant<int, 2>(), it, n);
-          else if (it.nrows <= 8) ok = narrow_item(std::integral_constant<int, 8>(), it, n);
-          else if (it.nrows <= 16) ok = narrow_item(std::integral_constant<int, 16>(), it, n);
-          else ok = narrow_item(std::integral_constant<int, 32>(), it, n);
-          if (!ok) break;
-        }
-        item_done(n);
-        continue;
-      }
       const int cnt = it.cnt, run = it.type >> 1;
       if ((warp & 3) * 32 >= it.nrows) {
         // no rows in this warp: its arrivals alone
