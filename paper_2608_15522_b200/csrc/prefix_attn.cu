@@ -15,6 +15,9 @@ constexpr int kChunk = 8;        // row tiles that go through the beginning side
 
 constexpr int kStreamRows = 32;      // query rows of a batch entry and key head that the stream kernel takes, at most; of the stacked rows as well
 
+// Products of 8 columns for so many query rows: with 8 or less the second one's would be empty.
+static int stream_products(long long rows) { return rows <= 8 ? 1 : 2; }
+
 struct PrefixLayout {
   PrefixShape s;
   int n_cta;                    // of the tile kernel
@@ -68,8 +71,6 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   if (s.stack && 128 % s.R == 0) s.pre_box = 128;
   s.queue = !y.own_stream && TO > 1 && F * Hkv > y.n_cta;
   s.nb_max = s.queue ? 8 * y.n_cta : y.n_cta;
-  // the stream kernel: CTAs that an SM holds, times SMs, are to be busy
-  const int slots = sms * 2;
   size_t rows = 0;
   y.pre = {};
   y.own = {};
@@ -79,6 +80,7 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     y.pre.begin = 1;
     y.pre.tiles = static_cast<int>((RS + kStRows - 1) / kStRows);
     y.pre.items = y.pre.tiles * Hkv;
+    const int slots = sms * stream_ctas(stream_products(RS));      // CTAs of the stream kernel that the SMs hold
     const long long by_keys = PT / 2;      // 256 keys a CTA at least: four blocks a warp
     y.pre.splits = static_cast<int>(slots / y.pre.items < by_keys ? slots / y.pre.items : by_keys);
     if (y.pre.splits < 1) y.pre.splits = 1;
@@ -96,6 +98,7 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     y.own.items = y.own.tiles * Hkv * B;
     y.own.out0 = static_cast<int>(own0);
     const long long keys = static_cast<long long>(width) * page - s.k0;      // at most
+    const int slots = sms * stream_ctas(stream_products(R));
     // An item's keys over a cluster: all slots busy, and no CTA with more than 1024 keys while others have none.  What eight CTAs an item do not fill
     // is cut into parts that a kernel behind joins.
     y.own_cluster = 1;
@@ -140,13 +143,18 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   return true;
 }
 
+template <int D, int NT>
+static int launch_stream_of(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixParams& p, const StreamParams& t, int cluster, cudaStream_t st) {
+  auto kernel = prefix_stream_kernel<D, NT>;
+  constexpr size_t kSmem = sizeof(StreamSmem<D, NT>);
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return AVSA_ERR_CUDA;
+  const unsigned grid = static_cast<unsigned>((static_cast<long long>(t.items) * t.splits + t.check) * cluster);
+  return launch_pdl_clusters(kernel, cluster, grid, kStThreads, kSmem, st, tk, tv, p, t) == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
+}
 template <int D>
 static int launch_stream(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixParams& p, const StreamParams& t, int cluster, cudaStream_t st) {
-  // (8 rows or less: the second product's columns would be empty)
-  auto kernel = (t.stacked ? p.s.B * p.s.R : p.s.R) <= 8 ? prefix_stream_kernel<D, 1> : prefix_stream_kernel<D, 2>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(StreamSmem<D>)) != cudaSuccess) return AVSA_ERR_CUDA;
-  const unsigned grid = static_cast<unsigned>((static_cast<long long>(t.items) * t.splits + t.check) * cluster);
-  return launch_pdl_clusters(kernel, cluster, grid, kStThreads, sizeof(StreamSmem<D>), st, tk, tv, p, t) == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
+  return stream_products(t.stacked ? static_cast<long long>(p.s.B) * p.s.R : p.s.R) == 1 ? launch_stream_of<D, 1>(tk, tv, p, t, cluster, st)
+                                                                                          : launch_stream_of<D, 2>(tk, tv, p, t, cluster, st);
 }
 
 template <int D>

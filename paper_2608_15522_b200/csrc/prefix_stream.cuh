@@ -74,31 +74,53 @@ __device__ __forceinline__ uint32_t stream_cluster_size() {
 // The call's status: what is out of range in the sequences of the batch, else the first error of a CTA of the tile kernel.  One CTA, the call's first one to write
 // the record (a wait of the stream kernel that runs out does so a second later).
 __device__ __noinline__ void prefix_check(const PrefixParams& p, int n_cta) {
-  __shared__ int worst;
-  if (threadIdx.x == 0) worst = 0x7fffffff;
+  __shared__ int worst, tile_error, again;
+  const PrefixShape& S = p.s;
+  if (threadIdx.x == 0) worst = 0x7fffffff, tile_error = 0x7fffffff, again = 0;
   __syncthreads();
-  for (int b = threadIdx.x >> 5; b < p.s.B; b += blockDim.x >> 5) {
+  constexpr int U = 8;      // loads in flight
+  // the pages that are read: of every sequence those behind the shared ones, and these of the longest
+  for (int b = threadIdx.x >> 5; b < S.B; b += blockDim.x >> 5) {
     int slot, bad;
     const int len = prefix_sequence(p, b, slot, bad);
-    const int used = (len + p.s.page - 1) >> p.s.page_shift;
-    for (int e = threadIdx.x & 31; e < used; e += 32) {
-      const int page = p.table[static_cast<int64_t>(slot) * p.s.width + e];
-      if (page < 0 || page >= p.s.pages) bad = kPrefixPage;
+    const int used = (len + S.page - 1) >> S.page_shift;
+    for (int e0 = (S.k0 >> S.page_shift) + (threadIdx.x & 31); e0 < used; e0 += 32 * U) {
+      int page[U];
+#pragma unroll
+      for (int u = 0; u < U; u++) page[u] = e0 + 32 * u < used ? p.table[static_cast<int64_t>(slot) * S.width + e0 + 32 * u] : 0;
+#pragma unroll
+      for (int u = 0; u < U; u++)
+        if (page[u] < 0 || page[u] >= S.pages) bad = kPrefixPage;
     }
     if (bad) atomicMin(&worst, (b << 9) | bad);
   }
+  if (S.stack) {
+    int top = 0, slot = 0, who = 0;
+    for (int b = 0; b < S.B; b++) {
+      int s, bad;
+      const int len = prefix_sequence(p, b, s, bad);
+      if (len > top) top = len, slot = s, who = b;
+    }
+    const int used = (min(top, S.k0) + S.page - 1) >> S.page_shift;
+    for (int e = threadIdx.x; e < used; e += blockDim.x) {
+      const int page = p.table[static_cast<int64_t>(slot) * S.width + e];
+      if (page < 0 || page >= S.pages) atomicMin(&worst, (who << 9) | kPrefixPage);
+    }
+  }
+  for (int c = threadIdx.x; c < n_cta; c += blockDim.x) {
+    const int code = p.cta_err[2 * c].x, more = p.cta_err[2 * c + 1].x;
+    if (code != 0 && code != AVSA_ERR_BAD_TABLE) atomicMin(&tile_error, c);
+    if (more != 0) atomicAdd(&again, more);
+  }
   __syncthreads();
   if (threadIdx.x == 0) {
-    int4 err = make_int4(0, 0, 0, 0);
-    int again = 0;
-    if (worst != 0x7fffffff) err = make_int4(AVSA_ERR_BAD_TABLE, worst & 511, worst >> 9, 0);
-    for (int c = 0; c < n_cta; c++) {
-      const int4 e = p.cta_err[2 * c];
-      if (err.x == 0 || (err.x == AVSA_ERR_BAD_TABLE && e.x != 0 && e.x != AVSA_ERR_BAD_TABLE)) err = e;
-      again += p.cta_err[2 * c + 1].x;
-    }
     p.status->redo_count = again;
-    if (err.x != 0) report_status(p.status, err.x, err.y, err.z, err.w);
+    if (tile_error != 0x7fffffff) {
+      const int4 e = p.cta_err[2 * tile_error];
+      report_status(p.status, e.x, e.y, e.z, e.w);
+    } else if (worst != 0x7fffffff) {
+      report_status(p.status, AVSA_ERR_BAD_TABLE, worst & 511, worst >> 9, 0);
+    }
   }
 }
 __device__ __forceinline__ void prefix_check_begin(const PrefixParams& p) {
@@ -108,9 +130,13 @@ __device__ __forceinline__ void prefix_check_begin(const PrefixParams& p) {
   }
 }
 
-template <int D>
+// CTAs that an SM holds, by shared memory: with one product's columns three of two stages (of 8 KB; 64 sequences of 100 to 2048 keys, us: 55.4, two of three stages 58.7),
+// with two products' the warps take longer and want more ahead (32 sequences x 8 x 2048 keys, 16 rows: 71.5 and 58.0).
+constexpr int stream_ctas(int NT) { return NT == 1 ? 3 : 2; }
+
+template <int D, int NT>
 struct StreamSmem {
-  static constexpr int kStages = D == 128 ? 3 : 6, kPanel = 16 * 128, kStage = 2 * (D / 64) * kPanel;      // a stage: panels of K, panels of V
+  static constexpr int kStages = (NT == 1 ? 2 : 3) * (128 / D), kPanel = 16 * 128, kStage = 2 * (D / 64) * kPanel;      // a stage: panels of K, panels of V
   union {
     uint8_t ring[kStWarps][kStages][kStage];      // 128-byte swizzled
     float4 o[kStWarps][kStRows][D / 4];           // behind the keys; [0] becomes the CTA's
@@ -158,6 +184,7 @@ __device__ __forceinline__ void stream_finish(const PrefixParams& p, const Strea
     prefix_parts(p, t, hk, entry * S.R + rr, first, step, n);
     float top = L != 0.f ? M : -INFINITY;
     bool nan = lse2 != lse2;
+#pragma unroll 8
     for (int k = 0; k < n; k++) {
       const float y = p.part_lse2[first + k * step];
       nan = nan || y != y;
@@ -170,7 +197,7 @@ __device__ __forceinline__ void stream_finish(const PrefixParams& p, const Strea
     acc.z *= f;
     acc.w *= f;
     const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll 4
+#pragma unroll 8
     for (int k = 0; k < n; k++) {
       const int64_t at = first + k * step;
       const float w = fast_exp2(p.part_lse2[at] - ref);
@@ -191,16 +218,17 @@ __device__ __forceinline__ void stream_finish(const PrefixParams& p, const Strea
 
 // NT: products of 8 query rows, 1 or 2.
 template <int D, int NT>
-__global__ void __launch_bounds__(kStThreads, 2)
+__global__ void __launch_bounds__(kStThreads, stream_ctas(NT))
 prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const __grid_constant__ PrefixParams p, const StreamParams t) {
   extern __shared__ __align__(1024) uint8_t smem[];
-  StreamSmem<D>& sm = *reinterpret_cast<StreamSmem<D>*>(smem);
+  using L_ = StreamSmem<D, NT>;
+  L_& sm = *reinterpret_cast<L_*>(smem);
   constexpr unsigned FULLM = 0xffffffffu;
   const PrefixShape& S = p.s;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, c = lane & 3;
   const int rank = static_cast<int>(stream_cluster_rank()), ctas = static_cast<int>(stream_cluster_size());
   if (lane == 0) {
-    for (int k = 0; k < StreamSmem<D>::kStages; k++) mbar_init(smem_u32(&sm.full[warp][k]), 1);
+    for (int k = 0; k < L_::kStages; k++) mbar_init(smem_u32(&sm.full[warp][k]), 1);
     fence_mbar_init();
     prefetch_tmap(&tmk);
     prefetch_tmap(&tmv);
@@ -294,14 +322,14 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
   const int step = ctas * kStWarps;
   const int block_shift = S.page_shift - 4;
   const int32_t* const pages = p.table + static_cast<int64_t>(max(slot, 0)) * S.width;
-  constexpr int STAGES = StreamSmem<D>::kStages, PANEL = StreamSmem<D>::kPanel, NPANEL = D / 64;
+  constexpr int STAGES = L_::kStages, PANEL = L_::kPanel, NPANEL = D / 64;
   const uint32_t ring = smem_u32(&sm.ring[warp][0][0]), full = smem_u32(&sm.full[warp][0]);
   // (a page that does not exist reads as zeros)
   auto load = [&](int blk, int page, int stage) {
     if (lane == 0 && blk < b1) {
-      const uint32_t bar = full + stage * 8, dst = ring + stage * StreamSmem<D>::kStage;
+      const uint32_t bar = full + stage * 8, dst = ring + stage * L_::kStage;
       const int in = (blk & ((1 << block_shift) - 1)) * 16, pg = page < 0 ? S.pages : page;
-      mbar_expect_tx(bar, StreamSmem<D>::kStage);
+      mbar_expect_tx(bar, L_::kStage);
       for (int pn = 0; pn < NPANEL; pn++) tma_load_4d(dst + pn * PANEL, &tmk, bar, pn * 64, in, hk, pg);
       for (int pn = 0; pn < NPANEL; pn++) tma_load_4d(dst + (NPANEL + pn) * PANEL, &tmv, bar, pn * 64, in, hk, pg);
     }
