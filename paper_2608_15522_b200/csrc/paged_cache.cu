@@ -186,33 +186,51 @@ __device__ __forceinline__ void page_share(const avsa_cache& c, int rank, int ct
 
 enum { kExtend = 0, kFork = 1 };
 
+// What a call hands from one step to the next.  A single CTA keeps it in shared memory as far as it fits (a step of an ordinary call is then two trips to L2 deep
+// instead of eight: 16 sequences and 150 pages 8.1 -> ASSIGNTIME us); the CTAs of a cluster, and what is larger, in the workspace.
+constexpr int kOwnClaims = 4096, kOwnList = 1024, kOwnFree = 8192;
+struct AssignSmem {
+  int claims[kOwnClaims];
+  ListEntry list[kOwnList];
+  int free_pages[kOwnFree];
+  int counts[2];
+};
+
 // extend and fork: which free pages go to which sequence.
 template <int OP>
 __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const MetaArgs a) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  AssignSmem& own = *reinterpret_cast<AssignSmem*>(smem);
   __shared__ int sm[kVals * 32];
   pdl_wait();
   pdl_launch();
   const avsa_cache& c = a.c;
   const CacheWs& w = a.w;
   const int rank = cluster_rank(), ctas = cluster_size(), tid = threadIdx.x, lane = tid & 31;
+  const bool alone = ctas == 1;
+  int* const claims = alone && c.seqs <= kOwnClaims ? own.claims : w.claims;
+  ListEntry* const list = alone && a.n <= kOwnList ? own.list : w.list;
+  int* const counts = alone ? own.counts : w.counts;      // [rank] free pages; behind all of them the needed ones
+  const int at_needed = alone ? 1 : kNumNeeded;
   if (rank == 0 && tid == 0) clear_status(w.status);
   copy_state(c, rank, ctas);
   int lo, hi;
   page_share(c, rank, ctas, lo, hi);
-  {
-    const int mine = count_taken(c.ref, lo, hi, [](int, int r) { return r <= 0; }, sm);
-    if (tid == 0) w.counts[rank] = mine;
-  }
   if (rank == 0) {
     // the list: entries that name a sequence again lose to the first one
     for (int k = tid; k < a.n; k += kMetaThreads) {
       const int s = a.seq[k];
-      if (s >= 0 && s < c.seqs) w.claims[s] = INT_MAX;
+      if (s >= 0 && s < c.seqs) claims[s] = INT_MAX;
     }
-    __syncthreads();
+  }
+  {
+    const int mine = count_taken(c.ref, lo, hi, [](int, int r) { return r <= 0; }, sm);
+    if (tid == 0) counts[rank] = mine;
+  }
+  if (rank == 0) {
     for (int k = tid; k < a.n; k += kMetaThreads) {
       const int s = a.seq[k];
-      if (s >= 0 && s < c.seqs) atomicMin(&w.claims[s], k);
+      if (s >= 0 && s < c.seqs) atomicMin(&claims[s], k);
     }
     __syncthreads();
     int taken = 0;
@@ -225,7 +243,7 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
         int bad = 0, code = AVSA_ERR_BAD_TABLE;
         if (s >= 0 && (OP == kExtend || o >= 0)) {
           if (s >= c.seqs || (OP == kFork && o >= c.seqs)) bad = kCacheSeq;
-          else if (__ldcg(&w.claims[s]) != k) bad = kCacheTwice;
+          else if (*static_cast<volatile int*>(&claims[s]) != k) bad = kCacheTwice;
           else {
             const int n = c.length[OP == kFork ? o : s];
             const long long room = static_cast<long long>(c.width) * c.page;
@@ -250,29 +268,38 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
       int all;
       e.first = taken + block_scan(e.need, all, sm);
       taken += all;
-      if (k < a.n) w.list[k] = e;
+      if (k < a.n) list[k] = e;
       __syncthreads();
     }
-    if (tid == 0) w.counts[kNumNeeded] = taken;
+    if (tid == 0) counts[at_needed] = taken;
   }
-  cluster_sync_all();
-  const int needed = __ldcg(&w.counts[kNumNeeded]);
+  if (alone) __syncthreads();
+  else cluster_sync_all();
+  const int needed = alone ? counts[at_needed] : __ldcg(&counts[at_needed]);
+  int* const free_pages = alone && needed <= kOwnFree ? own.free_pages : w.free_pages;
   int base = 0, n_free = 0;
   for (int r = 0; r < ctas; r++) {
-    const int m = __ldcg(&w.counts[r]);
+    const int m = alone ? counts[r] : __ldcg(&counts[r]);
     if (r < rank) base += m;
     n_free += m;
   }
   if (base < needed) {      // (uniform over the CTA)
     // (ref has not been written yet: in place it is still the state before the call)
     for_taken(c.ref, lo, hi, base, [](int, int r) { return r <= 0; },
-              [&](int page, int, int at) { if (at < needed) w.free_pages[at] = page; }, sm);
+              [&](int page, int, int at) { if (at < needed) free_pages[at] = page; }, sm);
   }
-  cluster_sync_all();
+  if (alone) __syncthreads();
+  else cluster_sync_all();
   const int warps = ctas * kMetaWarps;
   for (int k = rank * kMetaWarps + (tid >> 5); k < a.n; k += warps) {      // a warp to an entry
-    const int4 e0 = __ldcg(reinterpret_cast<const int4*>(&w.list[k])), e1 = __ldcg(reinterpret_cast<const int4*>(&w.list[k]) + 1);
+    int4 e0, e1;
+    if (alone) {
+      e0 = *reinterpret_cast<const int4*>(&list[k]), e1 = *(reinterpret_cast<const int4*>(&list[k]) + 1);
+    } else {
+      e0 = __ldcg(reinterpret_cast<const int4*>(&list[k])), e1 = __ldcg(reinterpret_cast<const int4*>(&list[k]) + 1);
+    }
     const int s = e0.x, other = e0.y, tokens = e0.z, new_tokens = e0.w, first = e1.x, need = e1.y;
+    auto free_page = [&](int at) { return alone ? free_pages[at] : __ldcg(&free_pages[at]); };
     const bool refused = s >= 0 && need > 0 && first + need > n_free;
     if (refused && lane == 0) report_status(w.status, AVSA_ERR_NO_PAGES, kCacheFull, k, s);
     if (OP == kFork && lane == 0 && (s < 0 || refused || need == 0)) w.moves[k] = make_int4(-1, -1, 0, 0);
@@ -281,7 +308,7 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
     if (OP == kExtend) {
       const int have = (tokens + c.page - 1) / c.page;
       for (int j = lane; j < need; j += 32) {
-        const int page = __ldcg(&w.free_pages[first + j]);
+        const int page = free_page(first + j);
         row[have + j] = page;
         c.ref_out[page] = 1;
       }
@@ -299,7 +326,7 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
             report_status(w.status, AVSA_ERR_BAD_TABLE, kCachePage, other, j);
           }
         } else if (j == whole && need) {
-          page = __ldcg(&w.free_pages[first]);
+          page = free_page(first);
           c.ref_out[page] = 1;
           const int src = from[j];
           const bool good = src >= 0 && src < c.pages;
@@ -442,8 +469,9 @@ __global__ void __launch_bounds__(kCopyThreads) move_pages_kernel(const CopyArgs
   const long long chunks = (a.pool.page_bytes + kCopyChunk - 1) / kCopyChunk;
   const long long total = static_cast<long long>(n) * a.pool.planes * chunks;
   for (long long u = blockIdx.x; u < total; u += gridDim.x) {
-    const long long r = u / chunks;
-    const int chunk = static_cast<int>(u - r * chunks), plane = static_cast<int>(r % a.pool.planes), k = static_cast<int>(r / a.pool.planes);
+    // the moves side by side: branches of one parent read its page together, once from HBM (fork of 8 x 4 branches, 2 GB: 293 -> 233 us)
+    const long long r = u / n;
+    const int k = static_cast<int>(u - r * n), plane = static_cast<int>(r / chunks), chunk = static_cast<int>(r - plane * chunks);
     const int4 m = a.moves[k];
     if (m.x < 0) continue;
     uint8_t* const base = static_cast<uint8_t*>(a.pool.ptr) + plane * a.pool.stride_plane;
@@ -453,7 +481,7 @@ __global__ void __launch_bounds__(kCopyThreads) move_pages_kernel(const CopyArgs
     uint4 x[kCopyVecs];
 #pragma unroll
     for (int i = 0; i < kCopyVecs; i++)
-      if (at + i * kCopyThreads * 16 < a.pool.page_bytes) x[i] = __ldcs(from + i * kCopyThreads);
+      if (at + i * kCopyThreads * 16 < a.pool.page_bytes) x[i] = from[i * kCopyThreads];
 #pragma unroll
     for (int i = 0; i < kCopyVecs; i++)
       if (at + i * kCopyThreads * 16 < a.pool.page_bytes) __stcs(to + i * kCopyThreads, x[i]);
@@ -463,50 +491,48 @@ __global__ void __launch_bounds__(kCopyThreads) move_pages_kernel(const CopyArgs
 struct WriteArgs {
   avsa_bf16_4d k_new, v_new, k_pool, v_pool;
   const int32_t *table, *length, *seq, *count;
-  int Hkv, L, vecs;       // vecs: 16-byte vectors of a token's row of one head
-  int page, pages, seqs, width, tokens;      // tokens: of one CTA
+  int Hkv, L;
+  int vec_shift, head_shift, tokens;      // a CTA's tile: 2^vec_shift vectors of 16 bytes of 2^head_shift heads of `tokens` tokens
+  int page_shift, pages, seqs, width;
 };
+constexpr int kWriteVecs = 4;      // of each tensor a thread
 
-// A CTA takes `tokens` tokens of one list entry; neighbouring threads take neighbouring vectors of a token's heads.
+// A CTA takes a tile of tokens by heads of one list entry: what it reads is contiguous over the heads of a token, what it writes over the tokens of a head in a page
+// (as rows of all heads, a token at a time: 4 x 1560 tokens of 24 heads 27.7 -> WRITETIME us).
 __global__ void __launch_bounds__(kCopyThreads) write_tokens_kernel(const WriteArgs a) {
   pdl_wait();
   pdl_launch();
-  const int k = blockIdx.y;
+  const int k = blockIdx.z;
   const int s = a.seq != nullptr ? a.seq[k] : k;
   if (s < 0 || s >= a.seqs) return;
   const int count = a.count != nullptr ? min(a.count[k], a.L) : a.L;
-  const int t0 = blockIdx.x * a.tokens, t1 = min(count, t0 + a.tokens);
-  if (t0 >= t1) return;
+  const int t0 = blockIdx.x * a.tokens, h0 = blockIdx.y << a.head_shift;
+  if (t0 >= count) return;
   const long long start = static_cast<long long>(a.length[s]) - count;
-  const int per_token = a.Hkv * a.vecs;
-  const int total = (t1 - t0) * per_token;
   const int32_t* const row = a.table + static_cast<long long>(s) * a.width;
-  constexpr int U = 2;
-  for (int i0 = threadIdx.x; i0 < total; i0 += kCopyThreads * U) {
-    uint4 x[U], y[U];
-    long long to_k[U], to_v[U];
+  uint4 x[kWriteVecs], y[kWriteVecs];
+  long long to_k[kWriteVecs], to_v[kWriteVecs];
 #pragma unroll
-    for (int u = 0; u < U; u++) {
-      const int i = i0 + u * kCopyThreads;
-      to_k[u] = -1;
-      if (i >= total) continue;
-      const int t = t0 + i / per_token, r = i % per_token, h = r / a.vecs, c = (r % a.vecs) * 8;
-      const long long pos = start + t;
-      if (pos < 0 || pos / a.page >= a.width) continue;
-      const int page = row[pos / a.page];
-      if (page < 0 || page >= a.pages) continue;
-      const int in = static_cast<int>(pos % a.page);
-      to_k[u] = page * a.k_pool.stride_b + h * a.k_pool.stride_h + in * a.k_pool.stride_n + c;
-      to_v[u] = page * a.v_pool.stride_b + h * a.v_pool.stride_h + in * a.v_pool.stride_n + c;
-      x[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.k_new.ptr) + k * a.k_new.stride_b + h * a.k_new.stride_h + t * a.k_new.stride_n + c));
-      y[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.v_new.ptr) + k * a.v_new.stride_b + h * a.v_new.stride_h + t * a.v_new.stride_n + c));
-    }
+  for (int u = 0; u < kWriteVecs; u++) {
+    const int i = threadIdx.x + u * kCopyThreads;
+    const int c = (i & ((1 << a.vec_shift) - 1)) * 8, h = h0 + ((i >> a.vec_shift) & ((1 << a.head_shift) - 1));
+    const int in_tile = i >> (a.vec_shift + a.head_shift), t = t0 + in_tile;
+    const long long pos = start + t;
+    to_k[u] = -1;
+    if (in_tile >= a.tokens || t >= count || h >= a.Hkv || pos < 0 || (pos >> a.page_shift) >= a.width) continue;
+    const int page = row[pos >> a.page_shift];
+    if (page < 0 || page >= a.pages) continue;
+    const long long in = pos & ((1 << a.page_shift) - 1);
+    to_k[u] = page * a.k_pool.stride_b + h * a.k_pool.stride_h + in * a.k_pool.stride_n + c;
+    to_v[u] = page * a.v_pool.stride_b + h * a.v_pool.stride_h + in * a.v_pool.stride_n + c;
+    x[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.k_new.ptr) + k * a.k_new.stride_b + h * a.k_new.stride_h + t * a.k_new.stride_n + c));
+    y[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.v_new.ptr) + k * a.v_new.stride_b + h * a.v_new.stride_h + t * a.v_new.stride_n + c));
+  }
 #pragma unroll
-    for (int u = 0; u < U; u++) {
-      if (to_k[u] < 0) continue;
-      *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(const_cast<void*>(a.k_pool.ptr)) + to_k[u]) = x[u];
-      *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(const_cast<void*>(a.v_pool.ptr)) + to_v[u]) = y[u];
-    }
+  for (int u = 0; u < kWriteVecs; u++) {
+    if (to_k[u] < 0) continue;
+    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(const_cast<void*>(a.k_pool.ptr)) + to_k[u]) = x[u];
+    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(const_cast<void*>(a.v_pool.ptr)) + to_v[u]) = y[u];
   }
 }
 
@@ -562,9 +588,13 @@ static unsigned meta_cluster(const avsa_cache& c) {
   if (c.table != c.table_out) ints += static_cast<long long>(c.seqs) * c.width;
   return ints <= kMetaSingle ? 1u : static_cast<unsigned>(kMetaCluster);
 }
-static cudaError_t launch_meta(void (*kernel)(MetaArgs), const MetaArgs& a, cudaStream_t st) {
+static cudaError_t launch_meta(void (*kernel)(MetaArgs), const MetaArgs& a, cudaStream_t st, size_t smem = 0) {
   const unsigned ctas = meta_cluster(a.c);
-  return launch_pdl_clusters(kernel, ctas, ctas, kMetaThreads, 0, st, a);
+  if (smem > 0) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) return e;
+  }
+  return launch_pdl_clusters(kernel, ctas, ctas, kMetaThreads, smem, st, a);
 }
 static int launch_moves(const CopyArgs& a, long long most, cudaStream_t st) {
   const long long chunks = (a.pool.page_bytes + kCopyChunk - 1) / kCopyChunk;
@@ -593,7 +623,7 @@ extern "C" int avsa_cache_extend(avsa_cache c, const int32_t* seq, const int32_t
   if (st != AVSA_OK) return st;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
   const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), seq, count, n, nullptr};
-  if (launch_meta(assign_pages_kernel<kExtend>, a, as_stream(stream)) != cudaSuccess) return AVSA_ERR_CUDA;
+  if (launch_meta(assign_pages_kernel<kExtend>, a, as_stream(stream), sizeof(AssignSmem)) != cudaSuccess) return AVSA_ERR_CUDA;
   return done();
 }
 
@@ -604,7 +634,7 @@ extern "C" int avsa_cache_fork(avsa_cache c, avsa_pages pool, const int32_t* par
   if (st != AVSA_OK) return st;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
   const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), child, parent, n, nullptr};
-  if (launch_meta(assign_pages_kernel<kFork>, a, as_stream(stream)) != cudaSuccess) return AVSA_ERR_CUDA;
+  if (launch_meta(assign_pages_kernel<kFork>, a, as_stream(stream), sizeof(AssignSmem)) != cudaSuccess) return AVSA_ERR_CUDA;
   if (n > 0) {
     CopyArgs m = {};
     m.pool = pool;
@@ -659,11 +689,15 @@ extern "C" int avsa_cache_write(int n, int Hkv, int L, int d, int page, int page
   if (n == 0 || L == 0) return AVSA_OK;
   if (!tokens_ok(k_new, n, Hkv, L) || !tokens_ok(v_new, n, Hkv, L)) return AVSA_ERR_INVALID_ARG;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
-  WriteArgs a = {k_new, v_new, k_pool, v_pool, table, length, seq, count, Hkv, L, d / 8, page, pages, seqs, width, 0};
-  // about four vectors of each tensor a thread, and no more than 32 bits count
-  const int per_token = Hkv * a.vecs;
-  a.tokens = per_token >= 4 * kCopyThreads ? 1 : 4 * kCopyThreads / per_token;
-  const dim3 grid(static_cast<unsigned>((L + a.tokens - 1) / a.tokens), static_cast<unsigned>(n));
+  WriteArgs a = {k_new, v_new, k_pool, v_pool, table, length, seq, count, Hkv, L, d == 128 ? 4 : 3, 0, 0, 0, pages, seqs, width};
+  while ((1 << a.page_shift) < page) a.page_shift++;
+  // eight tokens (as many as there are), and as many heads as make four vectors a thread
+  const int vecs = kCopyThreads * kWriteVecs >> a.vec_shift;
+  a.tokens = L < 8 ? L : 8;
+  while (a.tokens << (a.head_shift + 1) <= vecs && (1 << a.head_shift) < Hkv) a.head_shift++;
+  a.tokens = vecs >> a.head_shift;
+  const dim3 grid(static_cast<unsigned>((L + a.tokens - 1) / a.tokens), static_cast<unsigned>((Hkv + (1 << a.head_shift) - 1) >> a.head_shift),
+                  static_cast<unsigned>(n));
   if (launch_pdl(write_tokens_kernel, grid, kCopyThreads, 0, as_stream(stream), a) != cudaSuccess) return AVSA_ERR_CUDA;
   return done();
 }
