@@ -160,22 +160,22 @@ static int launch_stream(const CUtensorMap& tk, const CUtensorMap& tv, const Pre
 template <int D>
 static int launch_tile(const PrefixLayout& y, const avsa_bf16_4d& k, const avsa_bf16_4d& v, const PrefixParams& p, cudaStream_t st) {
   const PrefixShape& s = y.s;
-  CUtensorMap tk, tv, tq_own, tq_pre;
+  CUtensorMap tk, tv, tq_own, tq_pre, to;
   if (!encode_bf16_tile_map(&tk, k.ptr, s.pages, s.Hkv, s.page, D, k.stride_b, k.stride_h, k.stride_n, s.page) ||
       !encode_bf16_tile_map(&tv, v.ptr, s.pages, s.Hkv, s.page, D, v.stride_b, v.stride_h, v.stride_n, s.page))
     return AVSA_ERR_CUDA;
   // (an axis of one element has no stride to speak of: any multiple of 16 bytes)
   const int H = s.Hkv * s.G;
   const int64_t sh = H > 1 ? p.q.stride_h : D, sn = s.L > 1 ? p.q.stride_n : D, sb = s.B > 1 ? p.q.stride_b : D;
-  auto box = [&](CUtensorMap* map, int tokens, int entries) {
-    return encode_bf16_map(map, p.q.ptr, {D, H, s.L, s.B}, {sh, sn, sb}, {64, s.G, tokens, entries});
+  auto box = [&](CUtensorMap* map, const void* ptr, int tokens, int entries) {
+    return encode_bf16_map(map, ptr, {D, H, s.L, s.B}, {sh, sn, sb}, {64, s.G, tokens, entries});
   };
-  tq_own = tq_pre = tk;      // (where there is no box)
-  if (!s.own_off && s.own_box > 0 && !box(&tq_own, s.own_box / s.G, 1)) return AVSA_ERR_CUDA;
-  if (s.pre_box > 0 && !box(&tq_pre, s.L, s.pre_box / s.R)) return AVSA_ERR_CUDA;
+  tq_own = tq_pre = to = tk;      // (where there is no box)
+  if (!s.own_off && s.own_box > 0 && !(box(&tq_own, p.q.ptr, s.own_box / s.G, 1) && box(&to, p.o, s.own_box / s.G, 1))) return AVSA_ERR_CUDA;
+  if (s.pre_box > 0 && !box(&tq_pre, p.q.ptr, s.L, s.pre_box / s.R)) return AVSA_ERR_CUDA;
   if (s.queue && launch_pdl(clear_counter_kernel, 1, 1, 0, st, p.counter) != cudaSuccess) return AVSA_ERR_CUDA;
   if (cudaFuncSetAttribute(prefix_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PrefixSmem<D>::kTotal) != cudaSuccess) return AVSA_ERR_CUDA;
-  return launch_pdl(prefix_attn_kernel<D>, y.n_cta, kPxThreads, PrefixSmem<D>::kTotal, st, tk, tv, tq_own, tq_pre, p) == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
+  return launch_pdl(prefix_attn_kernel<D>, y.n_cta, kPxThreads, PrefixSmem<D>::kTotal, st, tk, tv, tq_own, tq_pre, to, p) == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
 }
 
 template <int D>

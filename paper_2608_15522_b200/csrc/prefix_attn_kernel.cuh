@@ -118,7 +118,7 @@ struct PrefixSmem {
   static constexpr int kK = 32768;
   static constexpr int kV = kK + kKS * kTile;
   static constexpr int kBars = kV + kVS * kTile;
-  static constexpr int kNumBars = 4 + 2 * kKS + 2 * kVS + 13 + 2 * kPxRing + 4;
+  static constexpr int kNumBars = 4 + 2 * kKS + 2 * kVS + 13 + 2 * kPxRing + 5;
   static constexpr int kStats = (kBars + kNumBars * 8 + 15) / 16 * 16;       // float mref[128], lsum[2][128]
   static constexpr int kItems = kStats + 3 * 128 * 4;
   static constexpr int kPages = kItems + 48 * kPxRing;                        // int[kPxRing][32]: an item's first pages
@@ -175,7 +175,7 @@ __device__ __noinline__ void px_report(int* err, int code, int where, int item, 
 template <int D>
 __global__ void __launch_bounds__(kPxThreads, 1)
 prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const __grid_constant__ CUtensorMap tmq_own,
-                   const __grid_constant__ CUtensorMap tmq_pre, const __grid_constant__ PrefixParams p) {
+                   const __grid_constant__ CUtensorMap tmq_pre, const __grid_constant__ CUtensorMap tmo, const __grid_constant__ PrefixParams p) {
   using L_ = PrefixSmem<D>;
   constexpr int NPANEL = D / 64, PANEL = 128 * 128, KS = L_::kKS, VS = L_::kVS;
   constexpr unsigned FULLM = 0xffffffffu;
@@ -188,8 +188,8 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
   constexpr int Q_FULL = 0, Q_EMPTY = 2, K_FULL = 4, K_EMPTY = K_FULL + KS, V_FULL = K_EMPTY + KS, V_EMPTY = V_FULL + VS,
                 S_FULL = V_EMPTY + VS, S_FREE = S_FULL + 2, P_FULL = S_FREE + 2 /* + 2*group + half */, P_FREE = P_FULL + 4, O_FULL = P_FREE + 2,
                 O_FREE = O_FULL + 1, MREF = O_FREE + 1, ITEM_FULL = MREF + 1, ITEM_EMPTY = ITEM_FULL + kPxRing, QK_DRAIN = ITEM_EMPTY + kPxRing,
-                PV_DRAIN = QK_DRAIN + 1, LSUM_A = PV_DRAIN + 1, LSUM_B = LSUM_A + 1;
-  static_assert(LSUM_B + 1 <= L_::kNumBars, "barrier table too small");
+                PV_DRAIN = QK_DRAIN + 1, LSUM_A = PV_DRAIN + 1, LSUM_B = LSUM_A + 1, STAGED = LSUM_B + 1;
+  static_assert(STAGED + 1 <= L_::kNumBars, "barrier table too small");
   constexpr uint32_t TM_O = 256, TM_P = 256 + D;      // tensor memory: S of group 0 | S of group 1 | O | P of group 0 | P of group 1
   float* mref_s = reinterpret_cast<float*>(smem + L_::kStats);
   float* lsum_s = mref_s + 128;
@@ -231,6 +231,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     mbar_init(BAR(PV_DRAIN), 1);
     mbar_init(BAR(LSUM_A), 256);
     mbar_init(BAR(LSUM_B), 256);
+    mbar_init(BAR(STAGED), 256);
     for (int i = STOP; i < ERR + 4; i++) misc[i] = 0;
     fence_mbar_init();
     prefetch_tmap(&tmk);
@@ -249,6 +250,11 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
   pdl_wait();
   pdl_launch();
 
+  // Final rows go out through shared memory, 128-byte swizzled, and a TMA store where they are a box (64 channels, 4096 rows x 2048 keys: 16-byte stores by row
+  // took 2000 cycles an item, the box STORECYCLES); its place is the last V stage, which such a call does without.
+  const bool staging = S.own_box > 0 && !S.own_off && !S.stack;
+  const int n_vs = staging ? VS - 1 : VS;
+  uint8_t* const stage_out = smem + L_::kV + (VS - 1) * L_::kTile;
   auto report = [&](int code, int where, int item, int aux) { px_report(const_cast<int*>(misc) + ERR, code, where, item, aux); };
   auto wait_or_stop = [&](int bar, uint32_t parity, int where, int tag) -> bool {
     if (mbar_try_wait(BAR(bar), parity)) return true;
@@ -286,7 +292,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     const bool is_k = warp == 0;
     const CUtensorMap* tm = is_k ? &tmk : &tmv;
-    const int FULL = is_k ? K_FULL : V_FULL, EMPTY = is_k ? K_EMPTY : V_EMPTY, STAGES = is_k ? KS : VS;
+    const int FULL = is_k ? K_FULL : V_FULL, EMPTY = is_k ? K_EMPTY : V_EMPTY, STAGES = is_k ? KS : n_vs;
     const uint32_t base = smem_u32(smem + (is_k ? L_::kK : L_::kV));
     const int ppt_shift = 7 - S.page_shift, ppt = 1 << ppt_shift;      // pages of a tile
     int stage = 0, round = 0, loads = 0;
@@ -767,7 +773,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
           }
           __syncwarp();
           used[j]++;
-          if (++stage == VS) {
+          if (++stage == n_vs) {
             stage = 0;
             round++;
           }
@@ -794,6 +800,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     int tiles = 0;              // S tiles this group has taken, over all items
     int used = 0;               // P tiles it has written
     int mrefs = 0, outputs = 0; // items with a first-tile reference, with an output
+    int n_staged = 0;           // with final rows by TMA
     float m_given = 0.f;
     bool ok = true;
 #pragma unroll 1
@@ -830,6 +837,10 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
           if (!ok) break;
           outputs++;
           mbar_arrive(BAR(O_FREE));
+          if (staging && it.out < 0) {
+            mbar_arrive(BAR(STAGED));
+            n_staged++;
+          }
         }
         item_done(n);
         continue;
@@ -927,6 +938,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       // (a group without a tile of its own has no sum; the reference is the other one's)
       if (run == 0 && row < it.nrows && !(l_run <= kFastRowSumLimit)) misc[FLAG + (n & 1)] = 1;
       lsum_s[w * 128 + row] = run == 1 ? m_max : l_run;
+      if (tid == 128) tma_store_wait_read();      // the rows staged before have been read when the groups have met
       mbar_arrive(BAR(LSUM_A));
       ok = __all_sync(FULLM, wait_or_stop(LSUM_A, n & 1, kPxLsum, n));
       if (!ok) break;
@@ -962,7 +974,29 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       tmem_wait_ld();
       tc_fence_before();
       mbar_arrive(BAR(O_FREE));
-      if (!again && row < it.nrows) {
+      if (staging && it.out < 0) {
+        const float sum = l_run + other;
+        const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+        if (!again && w == 0 && row < it.nrows && p.lse != nullptr)
+          p.lse[(static_cast<int64_t>(b) * S.Hkv * S.G + it.hk * S.G + g) * S.L + i] = sum != 0.f ? (m_ref + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+#pragma unroll
+        for (int c = 0; c < HALF / 8; c++) {
+          const int col = w * HALF + c * 8;
+          uint4 v;
+          v.x = pack_bf16x2(__uint_as_float(o0[c * 8 + 0]) * inv, __uint_as_float(o0[c * 8 + 1]) * inv);
+          v.y = pack_bf16x2(__uint_as_float(o0[c * 8 + 2]) * inv, __uint_as_float(o0[c * 8 + 3]) * inv);
+          v.z = pack_bf16x2(__uint_as_float(o0[c * 8 + 4]) * inv, __uint_as_float(o0[c * 8 + 5]) * inv);
+          v.w = pack_bf16x2(__uint_as_float(o0[c * 8 + 6]) * inv, __uint_as_float(o0[c * 8 + 7]) * inv);
+          *reinterpret_cast<uint4*>(stage_out + (col >> 6) * PANEL + row * 128 + ((((col & 63) >> 3) ^ (row & 7)) << 4)) = v;
+        }
+        fence_proxy_async();
+        mbar_arrive(BAR(STAGED));
+        if (tid == 128 && wait_or_stop(STAGED, n_staged & 1, kPxLsum, n) && !again) {
+          for (int pn = 0; pn < NPANEL; pn++) tma_store_4d(&tmo, smem_u32(stage_out) + pn * PANEL, pn * 64, it.hk * S.G, S.by_G.div(it.row0), it.b);
+          tma_store_commit();
+        }
+        n_staged++;
+      } else if (!again && row < it.nrows) {
         const float sum = l_run + other;
         const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
         const float lse2 = sum != 0.f ? m_ref + log2f(sum) : -INFINITY;
@@ -994,6 +1028,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       }
       item_done(n);
     }
+    if (tid == 128) tma_store_wait_read();      // (the last rows)
   }
   tc_fence_before();
   __syncthreads();
