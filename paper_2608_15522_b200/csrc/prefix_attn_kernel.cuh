@@ -10,8 +10,8 @@
 //     the second reader of a key tile finds it in L2), and each group of `chunk` CTAs gets the same number of columns;
 //   - B pieces: the own items of all sequences, one after the other, are a stream that is cut into equal pieces: lengths as ragged as they may be,
 //     every CTA gets the same number of units, and all of them stream pages from HBM side by side;
-//   - A pieces: with several row tiles to a sequence (long blocks of queries) whole items come off a queue first, so that CTAs that run at the
-//     same time work on the same keys (as equal shares of the stream they would be heads apart: each tile from HBM), and only the last ones are cut.
+//   - A pieces: with several row tiles to a sequence (long blocks of queries) whole items come off a queue, so that CTAs that run at the
+//     same time work on the same keys (as equal shares of the stream they would be heads apart: each tile from HBM), and only last ones that are few are cut.
 // What a cut or a stacked item leaves are fp32 rows, normalised by their own sum, and their log2 sums; prefix_merge_kernel joins them in a fixed order.
 // Lengths are on the device: every CTA's scheduler warp counts the units itself (a scan over the batch), nothing comes back to the host.
 //
@@ -504,29 +504,25 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       P.TB = T;
       int want = min(max(1, n_cta - n_pre), (T + kPxMinPiece - 1) / kPxMinPiece);
       if (S.queue && T > 0) {
-        // cut are the last items, one's worth of every CTA, in quarters
-        const int per_item = max(1, float_div(T, S.Hkv * S.F));
-        const int u = T - min(T, n_cta * per_item);
-        const int hk = float_div(u, P.W), rest = u - hk * P.W;
-        int before = 0, f = 0;
+        // Whole items, but those that would leave half of the CTAs or more without one at the end: they are cut into as many parts as there are CTAs for each
+        // (a part costs four tiles' time and its rows' merge: 1024 items of 16 tiles, 6.9 a CTA, us: the last one of every CTA in quarters 152, none cut 123).
+        const int items = S.Hkv * S.F, over = items - float_div(items, n_cta) * n_cta, parts = over > 0 ? min(8, float_div(n_cta, over)) : 1;
+        P.MA = items;
+        P.uA = T;
+        if (parts > 1) {
+          P.MA = items - over;
+          const int hk = S.by_F.div(P.MA), f = P.MA - hk * S.F;
+          int before = 0;
 #pragma unroll 1
-        for (int f0 = 0; f0 < S.F; f0 += 32) {
-          int nt, len, slot;
-          own_items(f0, nt, len, slot);
-          const int inc = scan(nt);
-          const unsigned beyond = __ballot_sync(FULLM, before + inc > rest);
-          if (beyond != 0u) {
-            const int l = __ffs(beyond) - 1;
-            f = f0 + l;
-            before += __shfl_sync(FULLM, inc - nt, l);
-            break;
+          for (int f0 = 0; f0 < f; f0 += 32) {
+            int nt, len, slot;
+            own_items(f0, nt, len, slot);
+            before += __reduce_add_sync(FULLM, f0 + lane < f ? nt : 0);
           }
-          before += __shfl_sync(FULLM, inc, 31);
+          P.uA = hk * P.W + before;
         }
-        P.MA = hk * S.F + f;
-        P.uA = hk * P.W + before;
         P.TB = T - P.uA;
-        want = float_div(P.TB - 1, max(kPxMinPiece, (per_item + 3) / 4)) + 1;
+        want = min(over * parts, (P.TB + kPxMinPiece - 1) / kPxMinPiece);
       }
       want = max(1, min(want, S.nb_max));
       P.sB = max(1, float_div(P.TB + want - 1, want));
