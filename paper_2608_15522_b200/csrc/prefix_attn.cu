@@ -65,6 +65,9 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     const int side = kChunk < y.n_cta ? kChunk : y.n_cta;
     s.nrc = (s.TP + side - 1) / side;
     s.chunk = (s.TP + s.nrc - 1) / s.nrc;
+    const int columns = Hkv * s.nrc * ((s.k0 + 127) / 128), most_groups = y.n_cta / s.chunk, by_piece = (columns + kPxMinPiece - 1) / kPxMinPiece;
+    const int groups = most_groups < by_piece ? most_groups : by_piece;
+    s.cg = (columns + groups - 1) / groups;
   }
   // Query rows as a box of a tensor map: (G heads, tokens, batch entries) that are the item's rows in their order.
   if (128 % s.G == 0) s.own_box = 128;
@@ -125,6 +128,7 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   s.by_F = Divisor(s.F);
   s.by_chunk = Divisor(s.chunk > 0 ? s.chunk : 1);
   s.by_nrc = Divisor(s.nrc > 0 ? s.nrc : 1);
+  s.by_cg = Divisor(s.cg > 0 ? s.cg : 1);
   size_t at = kStatusBytes;
   y.plan = at;
   at += 256;

@@ -70,11 +70,12 @@ struct PrefixShape {
   int rows;            // rows of an own item's partial result: min(128, R)
   int queue;           // whole items off a queue
   int own_off;         // the beginning alone: the own items are another kernel's
+  int cg;              // columns of a group then (as if all sequences had the whole beginning)
   int pre_box, own_box;        // rows of the TMA box that holds the query rows of an item; 0: they are gathered
   int nb_max;          // B pieces at most
   int page, page_shift, pages, seqs, width;
   int causal;
-  Divisor by_R, by_G, by_TO, by_F, by_chunk, by_nrc;
+  Divisor by_R, by_G, by_TO, by_F, by_chunk, by_nrc, by_cg;
 };
 
 struct PrefixParams {
@@ -490,9 +491,14 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
         P.donor = __shfl_sync(FULLM, at, __ffs(__ballot_sync(FULLM, most == top)) - 1);
         P.PE = min(S.k0, top);
         P.PT = (P.PE + 127) >> 7;
+        if (S.own_off) P.PT = (S.k0 + 127) >> 7;      // (a shorter one's last tiles read as zeros, and nobody sees them)
       }
       const int T = P.W * S.Hkv, columns = S.Hkv * S.nrc * P.PT;
-      if (columns > 0) {
+      if (S.own_off) {
+        P.cg = S.cg;
+        P.groups = float_div(columns + P.cg - 1, P.cg);
+        n_pre = P.groups * S.chunk;
+      } else if (columns > 0) {
         const float share = static_cast<float>(S.Hkv) * S.TP * P.PT;
         int groups = max(1, __float2int_rz(__fdividef(n_cta * share, (share + T) * S.chunk) + 0.5f));
         groups = min(groups, max(1, S.by_chunk.div(T > 0 ? n_cta - 1 : n_cta)));
@@ -1040,53 +1046,59 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
 // follow from the plan, and the parts of the row's own item.  Else: the rows of the items that a B piece begins and another ends.
 constexpr int kPxMergeWarps = 8;
 
+// Adds n parts, `step` rows apart, to C channels of a row that stand at `col`: acc is the sum of weights times values and L that of the weights, against the reference M
+// (L == 0: nothing yet).  Eight parts' sums and values are on their way together: one trip to L2.
+template <int D, int C>
+__device__ __forceinline__ void join_parts(const PrefixParams& p, int64_t first, int64_t step, int n, int col, float (&acc)[C], float& M, float& L, bool& nan) {
+  constexpr int U = 8;
+  for (int k0 = 0; k0 < n; k0 += U) {
+    float y[U], v[U][C];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int64_t at = first + min(k0 + u, n - 1) * step;
+      y[u] = p.part_lse2[at];
+      if constexpr (C == 4) *reinterpret_cast<float4*>(v[u]) = *reinterpret_cast<const float4*>(p.part_o + at * D + col);
+      else *reinterpret_cast<float2*>(v[u]) = *reinterpret_cast<const float2*>(p.part_o + at * D + col);
+    }
+    float top = L != 0.f ? M : -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      if (k0 + u >= n) y[u] = -INFINITY;
+      nan = nan || y[u] != y[u];
+      top = fmaxf(top, y[u]);
+    }
+    const float ref = top == -INFINITY ? 0.f : top, f = L != 0.f ? fast_exp2(M - ref) : 0.f;
+    M = ref;
+    L *= f;
+#pragma unroll
+    for (int x = 0; x < C; x++) acc[x] *= f;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const float w = fast_exp2(y[u] - ref);
+      L += w;
+#pragma unroll
+      for (int x = 0; x < C; x++) acc[x] += w != 0.f ? w * v[u][x] : 0.f;
+    }
+  }
+}
+
 template <int D>
 __device__ __forceinline__ void prefix_merge_row(const PrefixParams& p, int first, int step, int n_first, int second, int n_second, int second_at1, int second_step,
                                                  int b, int head, int i) {
   // parts 0 .. n_first-1 at first + k*step; then one at `second`, and the others at second_at1 + (k-1)*second_step
   constexpr int C = D / 32;
   const int lane = threadIdx.x & 31;
-  const int n = n_first + n_second;
-  auto at = [&](int k) {
-    if (k < n_first) return first + k * step;
-    k -= n_first;
-    return k == 0 ? second : second_at1 + (k - 1) * second_step;
-  };
-  float m = -INFINITY;
+  float o[C] = {}, M = 0.f, L = 0.f;
   bool nan = false;
-  for (int k = lane; k < n; k += 32) {
-    const float x = p.part_lse2[at(k)];
-    nan = nan || x != x;
-    m = fmaxf(m, x);
-  }
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-  nan = __any_sync(0xffffffffu, nan);
-  const float ref = m == -INFINITY ? 0.f : m;
-  float o[C] = {}, den = 0.f;
-#pragma unroll 4
-  for (int k = 0; k < n; k++) {
-    const int64_t r = at(k);
-    const float wt = exp2f(p.part_lse2[r] - ref);
-    den += wt;
-    if constexpr (C == 4) {
-      const float4 x = *reinterpret_cast<const float4*>(p.part_o + r * D + lane * 4);
-      o[0] += wt * x.x;
-      o[1] += wt * x.y;
-      o[2] += wt * x.z;
-      o[3] += wt * x.w;
-    } else {
-      const float2 x = *reinterpret_cast<const float2*>(p.part_o + r * D + lane * 2);
-      o[0] += wt * x.x;
-      o[1] += wt * x.y;
-    }
-  }
-  const float inv = nan ? NAN : den > 0.f ? 1.0f / den : 0.f;
+  join_parts<D, C>(p, first, step, n_first, lane * C, o, M, L, nan);
+  join_parts<D, C>(p, second, 0, n_second > 0 ? 1 : 0, lane * C, o, M, L, nan);
+  join_parts<D, C>(p, second_at1, second_step, n_second - 1, lane * C, o, M, L, nan);
+  const float inv = nan ? NAN : L > 0.f ? 1.0f / L : 0.f;
   __nv_bfloat16* dst = p.o + b * p.q.stride_b + head * p.q.stride_h + i * p.q.stride_n + lane * C;
   if constexpr (C == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
   else *reinterpret_cast<uint32_t*>(dst) = pack_bf16x2(o[0] * inv, o[1] * inv);
   if (lane == 0 && p.lse != nullptr)
-    p.lse[(static_cast<int64_t>(b) * p.s.Hkv * p.s.G + head) * p.s.L + i] = nan ? NAN : den > 0.f ? (ref + log2f(den)) * 0.6931471805599453f : -INFINITY;
+    p.lse[(static_cast<int64_t>(b) * p.s.Hkv * p.s.G + head) * p.s.L + i] = nan ? NAN : L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
 
 template <int D>

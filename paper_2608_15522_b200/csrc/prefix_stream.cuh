@@ -155,15 +155,12 @@ __device__ __forceinline__ void prefix_parts(const PrefixParams& p, const Stream
     first = (hk * t.join_tiles + (rho >> 4)) * n * kStRows + (rho & 15);
     return;
   }
-  const int PT = p.plan[0], cg = p.plan[1];
+  const int PT = (S.k0 + 127) >> 7;
+  const int rt = rho >> 7, rc = S.by_chunk.div(rt), j = rt - rc * S.chunk, U = hk * S.nrc + rc;
+  const int g0 = S.by_cg.div(U * PT), g1 = S.by_cg.div((U + 1) * PT - 1);
   step = S.chunk * 128;
-  n = first = 0;
-  if (PT > 0) {
-    const int rt = rho >> 7, rc = S.by_chunk.div(rt), j = rt - rc * S.chunk, U = hk * S.nrc + rc;
-    const int g0 = float_div(U * PT, cg), g1 = float_div((U + 1) * PT - 1, cg);
-    first = ((g0 + U) * S.chunk + j) * 128 + (rho & 127);
-    n = g1 - g0 + 1;
-  }
+  first = ((g0 + U) * S.chunk + j) * 128 + (rho & 127);
+  n = g1 - g0 + 1;
 }
 
 // Four channels of a row: acc is the sum of its weights times values against the reference M, L the sum of its weights.
@@ -182,33 +179,11 @@ __device__ __forceinline__ void stream_finish(const PrefixParams& p, const Strea
   if (t.join != 0) {
     int first, step, n;
     prefix_parts(p, t, hk, entry * S.R + rr, first, step, n);
-    float top = L != 0.f ? M : -INFINITY;
     bool nan = lse2 != lse2;
-#pragma unroll 8
-    for (int k = 0; k < n; k++) {
-      const float y = p.part_lse2[first + k * step];
-      nan = nan || y != y;
-      top = fmaxf(top, y);
-    }
-    const float f = top == -INFINITY || L == 0.f ? 0.f : fast_exp2(M - top);
-    L *= f;
-    acc.x *= f;
-    acc.y *= f;
-    acc.z *= f;
-    acc.w *= f;
-    const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll 8
-    for (int k = 0; k < n; k++) {
-      const int64_t at = first + k * step;
-      const float w = fast_exp2(p.part_lse2[at] - ref);
-      const float4 v = *reinterpret_cast<const float4*>(p.part_o + at * D + 4 * x);
-      L += w;
-      acc.x += w * v.x;
-      acc.y += w * v.y;
-      acc.z += w * v.z;
-      acc.w += w * v.w;
-    }
-    lse2 = nan ? NAN : L > 0.f ? ref + log2f(L) : -INFINITY;
+    float sum[4] = {acc.x, acc.y, acc.z, acc.w};
+    join_parts<D, 4>(p, first, step, n, 4 * x, sum, M, L, nan);
+    acc = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    lse2 = nan ? NAN : L > 0.f ? M + log2f(L) : -INFINITY;
     inv = nan ? NAN : L > 0.f ? 1.0f / L : 0.f;
   }
   __nv_bfloat16* dst = p.o + entry * p.q.stride_b + head * p.q.stride_h + i * p.q.stride_n + 4 * x;
