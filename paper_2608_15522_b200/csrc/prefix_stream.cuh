@@ -71,9 +71,24 @@ __device__ __forceinline__ uint32_t stream_cluster_size() {
   return r;
 }
 
-// The call's status: what is out of range in the sequences of the batch, else the first error of a CTA of the tile kernel.  One CTA, the call's first one to write
-// the record (a wait of the stream kernel that runs out does so a second later).
-__device__ __noinline__ void prefix_check(const PrefixParams& p, int n_cta) {
+// The longest sequence of the batch: its row of the page table names the shared pages.  A warp.
+__device__ __forceinline__ void longest_sequence(const PrefixParams& p, int& slot, int& tokens, int& entry) {
+  const int lane = threadIdx.x & 31;
+  int top = 0, at = 0, who = 0;
+  for (int b = lane; b < p.s.B; b += 32) {
+    int s, bad;
+    const int len = prefix_sequence(p, b, s, bad);
+    if (len > top) top = len, at = s, who = b;
+  }
+  tokens = __reduce_max_sync(0xffffffffu, top);
+  const int from = __ffs(__ballot_sync(0xffffffffu, top == tokens)) - 1;
+  slot = __shfl_sync(0xffffffffu, at, from);
+  entry = __shfl_sync(0xffffffffu, who, from);
+}
+
+// The call's status: what is out of range in the sequences of the batch, else the first error of a CTA of the tile kernel in front (`wait`: nothing has waited for it
+// yet).  One CTA, the call's first one to write the record (a wait of the stream kernel that runs out does so a second later).
+__device__ __noinline__ void prefix_check(const PrefixParams& p, int n_cta, int wait) {
   __shared__ int worst, tile_error, again;
   const PrefixShape& S = p.s;
   if (threadIdx.x == 0) worst = 0x7fffffff, tile_error = 0x7fffffff, again = 0;
@@ -95,17 +110,17 @@ __device__ __noinline__ void prefix_check(const PrefixParams& p, int n_cta) {
     if (bad) atomicMin(&worst, (b << 9) | bad);
   }
   if (S.stack) {
-    int top = 0, slot = 0, who = 0;
-    for (int b = 0; b < S.B; b++) {
-      int s, bad;
-      const int len = prefix_sequence(p, b, s, bad);
-      if (len > top) top = len, slot = s, who = b;
-    }
+    int slot, top, who;
+    longest_sequence(p, slot, top, who);
     const int used = (min(top, S.k0) + S.page - 1) >> S.page_shift;
     for (int e = threadIdx.x; e < used; e += blockDim.x) {
       const int page = p.table[static_cast<int64_t>(slot) * S.width + e];
       if (page < 0 || page >= S.pages) atomicMin(&worst, (who << 9) | kPrefixPage);
     }
+  }
+  if (wait) {
+    pdl_wait();
+    pdl_launch();
   }
   for (int c = threadIdx.x; c < n_cta; c += blockDim.x) {
     const int code = p.cta_err[2 * c].x, more = p.cta_err[2 * c + 1].x;
@@ -217,11 +232,12 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
   int id = static_cast<int>(blockIdx.x) / ctas;
   if (t.check) {
     if (id == 0) {
-      if (!t.first) {
+      if (rank == 0) {
+        prefix_check(p, t.join == kStJoinTile ? p.tile_ctas : 0, !t.first);
+      } else if (!t.first) {
         pdl_wait();
         pdl_launch();
       }
-      if (rank == 0) prefix_check(p, t.join == kStJoinTile ? p.tile_ctas : 0);
       return;
     }
     id--;
@@ -235,15 +251,8 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
   const int row0 = tile * kStRows, n_rows = t.stacked ? S.B * S.R : S.R, rows = min(kStRows, n_rows - row0);
   int slot, bad, k0, k1;
   if (t.stacked) {
-    // the longest sequence's row names the pages
-    int top = 0, at = 0;
-    for (int b = lane; b < S.B; b += 32) {
-      int s;
-      const int len = prefix_sequence(p, b, s, bad);
-      if (len > top) top = len, at = s;
-    }
-    const int most = __reduce_max_sync(FULLM, top);
-    slot = __shfl_sync(FULLM, at, __ffs(__ballot_sync(FULLM, top == most)) - 1);
+    int most, who;
+    longest_sequence(p, slot, most, who);
     k0 = 0;
     k1 = min(S.k0, most);
   } else {
