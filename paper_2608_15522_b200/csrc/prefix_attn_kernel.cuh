@@ -741,7 +741,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
           ok = wait_all(V_FULL + stage, round & 1, kPxVFull, t);
           if (!ok) break;
           const int valid = it.kv_end - it.pos0 - t * 128;
-          if (valid < 128 && (valid & (S.page - 1)) != 0) {
+          if (valid > 0 && valid < 128 && (valid & (S.page - 1)) != 0) {
             // behind the last token its page may hold anything; P is zero there, and 0 * NaN is not
             const int end = (valid + S.page - 1) & ~(S.page - 1);
             uint8_t* tile = smem + L_::kV + stage * L_::kTile;

@@ -614,3 +614,157 @@ def test_attention_offsets_beyond_32_bits():
     new = torch.randn((2, 1, 3, d), device="cuda").bfloat16()
     av.avsa_cache_write(new, new, pool, vpool, cu(table), cu(length))
     assert torch.equal(pool[4, 0, 39:42], new[0, 0]) and torch.equal(vpool[1, 0, 61:64], new[1, 0])
+
+
+# ------------------------------------------------------------------------------------------------ every way the work is cut
+def exact_on_gpu(q, k, v, table, length, seq=None, causal=False):
+    """orc.prefix_attention for sizes that numpy takes too long for: the same statement in 64 bits on the GPU."""
+    B, H, L, d = q.shape
+    page, group = k.shape[2], H // k.shape[1]
+    o = torch.zeros((B, H, L, d), dtype=torch.float64, device="cuda")
+    lse = torch.full((B, H, L), float("-inf"), dtype=torch.float64, device="cuda")
+    for b in range(B):
+        s = b if seq is None else seq[b]
+        n = int(length[s]) if s >= 0 else 0
+        if n == 0:
+            continue
+        at = torch.arange(n, device="cuda")
+        pages = cu(table)[s].long()[at // page]
+        kk, vv = k[pages, :, at % page].double().transpose(0, 1), v[pages, :, at % page].double().transpose(0, 1)      # [Hkv,n,d]
+        x = q[b].double().reshape(-1, group * L, d) @ kk.transpose(1, 2) / math.sqrt(d)
+        if causal:
+            lim = torch.arange(L, device="cuda").repeat(group) + n - L + 1
+            x.masked_fill_(at[None, :] >= lim[:, None], float("-inf"))
+        z = torch.logsumexp(x, 2)
+        w = torch.exp(x - torch.where(torch.isinf(z), 0.0, z)[..., None])
+        o[b], lse[b] = (w @ vv).reshape(H, L, d), z.reshape(H, L)
+    return o, lse
+
+
+def check_on_gpu(q, k, v, table, length, what, **kw):
+    seq = kw.pop("seq", None)
+    o, lse, ws = av.avsa_prefix_attn(q, k, v, cu(table), cu(length), seq=None if seq is None else ints(seq), want_lse=True, **kw)
+    assert status(ws) == av.AVSA_OK
+    want, want_lse = exact_on_gpu(q, k, v, table, length, seq, kw.get("causal", False))
+    empty = torch.isinf(want_lse)
+    assert torch.equal(torch.isinf(lse), empty) and (o[empty] == 0).all(), what
+    close_o(o.double()[~empty].cpu().numpy(), want[~empty].cpu().numpy(), what)
+    close_lse(lse.double()[~empty].cpu().numpy(), want_lse[~empty].cpu().numpy(), what)
+    return o, lse, ws
+
+
+def lengths_behind(rng, B, shared, page, most):
+    """Ragged lengths behind a shared beginning; with a few of them one sequence holds nothing and one a part of the beginning."""
+    v = [shared * page + rng.choice((0, 1, page - 1, rng.randint(0, most))) for _ in range(B)]
+    if B > 3:
+        v[1], v[2] = 0, shared * page // 2 + 3
+    v[-1] = shared * page + most
+    return v
+
+
+@gpu
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,L,H,Hkv,page,tokens,most", [
+    (8, 1, 32, 32, 16, 2048, 300),        # 8 stacked rows: parts by warps' products of one column block
+    (16, 1, 24, 24, 64, 2048, 700),       # 16: two
+    (30, 1, 16, 16, 32, 2048, 100),       # 30: two row tiles
+    (4, 7, 24, 24, 64, 4096, 90),         # 28 rows, several tokens
+    (40, 1, 32, 8, 128, 2048, 500),       # 160: the tile kernel, own keys by warps
+    (64, 1, 32, 4, 64, 2048, 260),        # 512: four row tiles side by side
+    (200, 1, 16, 2, 16, 2048, 40),        # 1600: thirteen, in two turns
+    (12, 10, 24, 8, 32, 4096, 200),       # 30 rows a sequence, gathered (three query heads to a key head)
+    (12, 20, 8, 2, 32, 16384, 400),       # 80 rows: the tile kernel for both
+    (9, 50, 24, 8, 64, 16384, 333)])      # 150: two row tiles of own rows, gathered
+def test_attention_stacked(B, L, H, Hkv, page, tokens, most, d, causal):
+    """The beginning is read for the rows of all sequences at once; the same call without saying that it is shared gives the same."""
+    rng = random.Random(B + d)
+    shared = tokens // page
+    case = attention_case(B, H, Hkv, L, d, page, lengths_behind(rng, B, shared, page, most), shared=shared, seed=B, q_layout="blhd")
+    a = check_on_gpu(*case, "stacked", prefix_pages=shared, causal=causal)
+    b = check_on_gpu(*case, "each by itself", causal=causal)
+    assert torch.allclose(a[0].float(), b[0].float(), atol=2e-2, rtol=2e-2)
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,L,H,Hkv,width,lengths", [
+    (1, 1, 8, 8, 400, (6000,)),           # few items, long rows: parts that another kernel joins
+    (1, 3, 8, 2, 400, (6400,)),
+    (2, 1, 4, 1, 500, (1, 7900)),
+    (1, 31, 4, 4, 300, (4700,)),
+    (3, 1, 24, 24, 60, (900, 0, 17)),     # a cluster of CTAs an item
+    (20, 2, 16, 16, 80, tuple(range(5, 1285, 64))),
+    (70, 1, 32, 8, 300, tuple(range(1, 4700, 67))[:70])])
+def test_attention_of_few_rows(B, L, H, Hkv, width, lengths, d):
+    rng = random.Random(d)
+    case = attention_case(B, H, Hkv, L, d, 16, list(lengths), seed=B, width=width)
+    for causal in (False, True):
+        check_on_gpu(*case, "few rows", causal=causal)
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,L,H,Hkv,page,lengths,causal", [
+    (1, 700, 32, 32, 64, (3000,), False),          # whole items off a queue, the last ones cut
+    (1, 2500, 8, 8, 128, (2500,), True),
+    (3, 509, 32, 8, 64, (509, 3000, 1754), True),
+    (5, 200, 24, 8, 32, (1000, 77, 0, 500, 640), True),
+    (2, 129, 6, 6, 16, (2000, 129), False),        # fewer items than SMs
+    (1, 33, 2, 2, 16, (5000,), False)])
+def test_attention_of_many_rows(B, L, H, Hkv, page, lengths, causal, d):
+    check_on_gpu(*attention_case(B, H, Hkv, L, d, page, list(lengths), seed=L, q_layout="blhd"), "many rows", causal=causal)
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,L,H,Hkv,tokens", [(16, 1, 24, 24, 2048), (40, 1, 32, 8, 2048), (12, 20, 8, 2, 16384), (1, 300, 4, 4, 0)])
+def test_attention_rows_that_outgrow_their_reference(B, L, H, Hkv, tokens, d):
+    """Logits that rise by 300 (as powers of e) along the keys: every way of cutting, the tile kernel's second run among them."""
+    page, shared = 64, tokens // 64
+    q, k, v, table, length = attention_case(B, H, Hkv, L, d, page, [tokens + 700 + b for b in range(B)], shared=shared, seed=4, poison=False)
+    one = torch.zeros(d, device="cuda")
+    one[0] = 1.0
+    q = (q.float() * (1 - one) + one * 4.0).bfloat16()
+    k = k.clone()
+    for s in range(B):
+        at = torch.arange(int(length[s]), device="cuda")
+        k[cu(table)[s].long()[at // page], :, at % page, 0] = (300.0 * math.sqrt(d) / 4.0 * at / (tokens + 800)).bfloat16()[:, None].expand(-1, Hkv)
+    _, _, ws = check_on_gpu(q, k, v, table, length, "growing", prefix_pages=shared)
+    if L >= 300:
+        assert av.avsa_redo_count(ws) > 0
+
+
+@gpu
+@pytest.mark.parametrize("B,L,H,Hkv", [(8, 1, 32, 32), (40, 1, 32, 8), (12, 20, 8, 2)])
+def test_attention_stacked_reports_and_reproduces(B, L, H, Hkv):
+    """A page out of range in the beginning and behind it, a length that is cut; the same bits twice, on memory full of ones."""
+    page, shared = 64, 256 if L > 1 else 32
+    q, k, v, table, length = attention_case(B, H, Hkv, L, 64, page, [shared * page + 100] * B, shared=shared, seed=2)
+    first = av.avsa_prefix_attn(q, k, v, cu(table), cu(length), prefix_pages=shared, want_lse=True)
+    again = av.avsa_prefix_attn(q, k, v, cu(table), cu(length), prefix_pages=shared, want_lse=True, ws=torch.full_like(first[2], 255))
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1]) and status(again[2]) == av.AVSA_OK
+    for where in ((0, 5), (3, shared), (B - 1, shared + 1)):
+        bad = table.copy()
+        bad[where] = 10 ** 6
+        assert status(av.avsa_prefix_attn(q, k, v, cu(bad), cu(length), prefix_pages=shared)[2]) == av.AVSA_ERR_BAD_TABLE, where
+    bad = length.copy()
+    bad[3] = -5
+    assert status(av.avsa_prefix_attn(q, k, v, cu(table), cu(bad), prefix_pages=shared)[2]) == av.AVSA_ERR_BAD_TABLE
+
+
+@gpu
+def test_attention_workspaces_depend_on_the_shape_alone():
+    """What the query says is enough for every call of the shape, whatever the lengths."""
+    for B, L, H, Hkv, page, width, prefix in ((1, 1, 8, 8, 16, 400, 0), (16, 1, 24, 24, 64, 60, 32), (40, 1, 32, 8, 128, 40, 16), (3, 509, 32, 8, 64, 50, 0)):
+        need = av.avsa_prefix_attn_workspace_bytes(B, H, Hkv, L, 64, page, width, prefix)
+        assert need > 256
+        q = torch.randn((B, H, L, 64), device="cuda").bfloat16()
+        pool = torch.randn((width, Hkv, page, 64), device="cuda").bfloat16()
+        table = torch.arange(width, dtype=torch.int32, device="cuda").repeat(B, 1)
+        guard = torch.full((need + 4096,), 77, dtype=torch.uint8, device="cuda")
+        for n in (width * page, prefix * page, 1, 0):
+            av.avsa_prefix_attn(q, pool, pool, table, ints([n] * B), prefix_pages=prefix, ws=guard[:need])
+            assert (guard[need:] == 77).all()
+        with pytest.raises(av.AvsaError):
+            av.avsa_prefix_attn(q, pool, pool, table, ints([1] * B), prefix_pages=prefix, ws=guard[:need - 32])
