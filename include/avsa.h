@@ -28,8 +28,8 @@
  *     when a device-side check fails (a wait that ran out of time, or a malformed column list) -- then at
  *     byte 16 a count of work items or query tiles (see below) and at byte 20 the head of the persistent
  *     kernels' work queue.  Calls on the same workspace must not overlap on the GPU.
- *   - Alignment of `ws`: 32 bytes are enough for every call, 4 bytes for sparse self-attention, for cross-attention
- *     against at most 256 keys and for a mask under given block scores.  With less than a call's kernels need
+ *   - Alignment of `ws`: 32 bytes are enough for every call, 16 for the changes of a paged cache, 4 for sparse self-attention, for
+ *     cross-attention against at most 256 keys and for a mask under given block scores.  With less than a call's kernels need
  *     (16 or 32 bytes, by shape) it returns AVSA_ERR_INVALID_ARG and enqueues nothing.
  *   - The attention calls (cross-attention against more than 256 keys that is not short, sparse self-attention, protected rows) run
  *     a kernel that normalises each row by the maximum of its first key tile instead of a running maximum
@@ -46,7 +46,7 @@
  *     avsa_status codes.
  *   - Supported shapes: (blk, d) in {(128,128), (64,64)}; B and H up to 65535, B*H below 2^31 (mask: up to
  *     65535); any N >= 1 (the last block may be partial: pooled means divide by the valid count, invalid
- *     keys are masked, rows >= N are not written).
+ *     keys are masked, rows >= N are not written).  Those of the paged cache stand at its calls, (6) and (7).
  */
 #ifndef AVSA_H_
 #define AVSA_H_
@@ -283,7 +283,8 @@ AVSA_API int avsa_build_block_mask_static(int B, int H, int N, int d, int blk, a
  * What pages hold behind a sequence's last token is never used (it may be anything, NaN too).  Values of tokens that a
  * causal row must not see have to be finite.  A page of the table out of range reads as zeros and sets AVSA_ERR_BAD_TABLE, a
  * length beyond the table's width is cut there and sets it as well.
- * d is 64 or 128, H a multiple of Hkv, H/Hkv at most 128.  table has `seqs` rows of `width` entries.  Same bits on every run.
+ * d is 64 or 128, H a multiple of Hkv, H/Hkv at most 128.  table has `seqs` rows of `width` entries.  o overlaps no input.  Rows that outgrow the maximum of
+ * their first key tile are run again as in the other attention calls (up to 32 query rows a key head take a running maximum instead).  Same bits on every run.
  */
 #define AVSA_CAUSAL 1u
 AVSA_API int avsa_prefix_attn(int B, int H, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d q,

@@ -98,6 +98,7 @@ constexpr long long kL2KeepBytes = 64ll << 20;
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // The widest access of a call to its workspace (whose parts begin at multiples of 256 bytes) needs this alignment of it.

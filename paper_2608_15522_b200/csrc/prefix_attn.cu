@@ -105,7 +105,8 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     // An item's keys over a cluster: all slots busy, and no CTA with more than 1024 keys while others have none.  What eight CTAs an item do not fill
     // is cut into parts that a kernel behind joins.
     y.own_cluster = 1;
-    while (y.own_cluster < 8 && keys > 128ll * y.own_cluster && (static_cast<long long>(y.own.items) * y.own_cluster < slots || keys > 1024ll * y.own_cluster)) y.own_cluster *= 2;
+    while (y.own_cluster < 8 && y.own.items < (1 << 27) && keys > 128ll * y.own_cluster &&
+           (static_cast<long long>(y.own.items) * y.own_cluster < slots || keys > 1024ll * y.own_cluster)) y.own_cluster *= 2;
     y.own.splits = 1;
     if (static_cast<long long>(y.own.items) * 8 < sms && keys >= 4096) {
       y.own_cluster = 1;
@@ -246,6 +247,7 @@ extern "C" int avsa_prefix_attn(int B, int H, int Hkv, int L, int d, int page, i
   if (B == 0 || L == 0) return AVSA_OK;
   if (!rows_ok(q, B, H, L) || !tensor_ok(k_pool, pages, Hkv) || !tensor_ok(v_pool, pages, Hkv)) return AVSA_ERR_INVALID_ARG;
   if (table == nullptr || length == nullptr || o_bf16 == nullptr || !aligned16(o_bf16)) return AVSA_ERR_INVALID_ARG;
+  if (!aligned4(table) || !aligned4(length) || !aligned4(seq) || !aligned4(lse)) return AVSA_ERR_INVALID_ARG;
   PrefixLayout y;
   if (!prefix_layout(B, H, Hkv, L, d, page, width, prefix_pages, flags & AVSA_CAUSAL ? 1 : 0, y)) return AVSA_ERR_UNSUPPORTED;
   if (ws == nullptr || ws_bytes < y.total) return AVSA_ERR_WORKSPACE;
@@ -259,8 +261,6 @@ extern "C" int avsa_prefix_attn(int B, int H, int Hkv, int L, int d, int page, i
   PrefixParams p = {};
   p.s = y.s;
   p.q = q;
-  p.k = k_pool;
-  p.v = v_pool;
   p.o = static_cast<__nv_bfloat16*>(o_bf16);
   p.lse = lse;
   p.table = table;

@@ -11,7 +11,7 @@
 //                  word y of which are rows n and n + 8 of product (j, y); two keys of a channel meet in a register by byte permutes.
 // With the query rows as columns a product is half as wide as with them as rows (8 against 16 that one token hardly ever has); more than 8 rows are two columns' products
 // on the same operands.  What counts then is how much is in flight (64 sequences x 8 key heads x 2048 keys, 537 MB, us: vectors to registers, 60 KB of an SM ahead, 117; by
-// cp.async to shared memory, 96 KB ahead, 132, and the loop without its products 125: 16-byte copies reach no more; by TMA, 128 KB ahead, TMATIME).
+// cp.async to shared memory, 96 KB ahead, 132, and the loop without its products 125: 16-byte copies reach no more; by TMA, 128 KB ahead, 93).
 // Each warp has its own running maximum and sum (rescaled when a maximum grew by more than 2^8) and takes every (warps of the item)-th 16 keys; warps are joined
 // through shared memory, the CTAs of an item (a cluster) through each other's.  Then a row is final, or meets the parts of the beginning, or is a part itself.
 #pragma once

@@ -194,6 +194,22 @@ def test_write_refuses():
         assert lib.avsa_cache_write(*{**good, **change}.values(), 0) == want, change
 
 
+def test_integers_off_their_grid_are_refused():
+    """int32 arrays begin at multiples of four bytes, the optional ones too."""
+    lib = av.load_library()
+    attn = dict(B=4, H=4, Hkv=2, L=3, d=64, page=64, pages=10, seqs=4, width=8, q=_T, k=_T, v=_T, table=8192, length=8192, seq=None, prefix=2, flags=0, scale=0.0,
+                o=1 << 25, lse=None, ws=1 << 16, ws_bytes=1 << 40)
+    write = dict(n=2, Hkv=2, L=3, d=64, page=64, pages=10, seqs=4, width=8, kn=_T, vn=_T, k=_T, v=_T, table=8192, length=8192, seq=None, count=None)
+    for name in ("table", "length", "seq", "lse"):
+        assert lib.avsa_prefix_attn(*{**attn, name: 8194}.values(), 0) == av.AVSA_ERR_INVALID_ARG, name
+    for name in ("table", "length", "seq", "count"):
+        assert lib.avsa_cache_write(*{**write, name: 8193}.values(), 0) == av.AVSA_ERR_INVALID_ARG, name
+    for a, b in ((8194, 8192), (8192, 8193)):
+        assert lib.avsa_cache_extend(_cache(), a, b, 2, 1 << 16, 1 << 30, 0) == av.AVSA_ERR_INVALID_ARG
+        assert lib.avsa_cache_fork(_cache(), _pages(), a, b, 2, 1 << 16, 1 << 30, 0) == av.AVSA_ERR_INVALID_ARG
+    assert lib.avsa_cache_free(_cache(), 8194, 2, 1 << 16, 1 << 30, 0) == av.AVSA_ERR_INVALID_ARG
+
+
 def test_wrappers_refuse_what_is_no_cuda_tensor():
     i = torch.zeros(4, dtype=torch.int32)
     t = torch.zeros((4, 2), dtype=torch.int32)
