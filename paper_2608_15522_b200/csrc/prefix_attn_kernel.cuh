@@ -110,6 +110,9 @@ struct PrefixItem {
 };
 static_assert(sizeof(PrefixItem) == 48, "three 16-byte accesses");
 
+// Words of the CTA's `misc`.
+enum { kPxTmem = 0, kPxStop, kPxWhere, kPxProgress, kPxFlag /* + item parity */, kPxListed = kPxFlag + 2, kPxRecomputed, kPxErr, kPxWords = kPxErr + 4 };
+
 template <int D>
 struct PrefixSmem {
   static constexpr int kTile = 128 * D * 2;
@@ -119,12 +122,13 @@ struct PrefixSmem {
   static constexpr int kK = 32768;
   static constexpr int kV = kK + kKS * kTile;
   static constexpr int kBars = kV + kVS * kTile;
-  static constexpr int kNumBars = 4 + 2 * kKS + 2 * kVS + 13 + 2 * kPxRing + 5;
+  static constexpr int kNumBars = 4 + 2 * kKS + 2 * kVS + 13 + 2 * kPxRing + 6;
   static constexpr int kStats = (kBars + kNumBars * 8 + 15) / 16 * 16;       // float mref[128], lsum[2][128]
   static constexpr int kItems = kStats + 3 * 128 * 4;
   static constexpr int kPages = kItems + 48 * kPxRing;                        // int[kPxRing][32]: an item's first pages
-  static constexpr int kMisc = kPages + 128 * kPxRing;                        // tmem base, stop, redo flags [2], listed, recomputed, error [4]
+  static constexpr int kMisc = kPages + 128 * kPxRing;
   static constexpr int kTotal = kMisc + 48;
+  static_assert(kPxWords * 4 <= 48, "words of the CTA");
   static_assert(kTotal <= 232448, "shared memory of a CTA exceeded");
 };
 
@@ -189,8 +193,9 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
   constexpr int Q_FULL = 0, Q_EMPTY = 2, K_FULL = 4, K_EMPTY = K_FULL + KS, V_FULL = K_EMPTY + KS, V_EMPTY = V_FULL + VS,
                 S_FULL = V_EMPTY + VS, S_FREE = S_FULL + 2, P_FULL = S_FREE + 2 /* + 2*group + half */, P_FREE = P_FULL + 4, O_FULL = P_FREE + 2,
                 O_FREE = O_FULL + 1, MREF = O_FREE + 1, ITEM_FULL = MREF + 1, ITEM_EMPTY = ITEM_FULL + kPxRing, QK_DRAIN = ITEM_EMPTY + kPxRing,
-                PV_DRAIN = QK_DRAIN + 1, LSUM_A = PV_DRAIN + 1, LSUM_B = LSUM_A + 1, STAGED = LSUM_B + 1;
-  static_assert(STAGED + 1 <= L_::kNumBars, "barrier table too small");
+                PV_DRAIN = QK_DRAIN + 1, LSUM_A = PV_DRAIN + 1, LSUM_B = LSUM_A + 1, STAGED = LSUM_B + 1,
+                DONE = STAGED + 1;
+  static_assert(DONE + 1 <= L_::kNumBars, "barrier table too small");
   constexpr uint32_t TM_O = 256, TM_P = 256 + D;      // tensor memory: S of group 0 | S of group 1 | O | P of group 0 | P of group 1
   float* mref_s = reinterpret_cast<float*>(smem + L_::kStats);
   float* lsum_s = mref_s + 128;
@@ -198,7 +203,6 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
   int* ring_pages = reinterpret_cast<int*>(smem + L_::kPages);
   PrefixItem* redo = p.redo + blockIdx.x * kPxRedo;
   volatile int* misc = reinterpret_cast<volatile int*>(smem + L_::kMisc);
-  enum { TMEM = 0, STOP, FLAG /* + item parity */, LISTED = FLAG + 2, RECOMPUTED, ERR };
 
   const bool aligned = (smem_u32(smem) & 1023u) == 0u;
   if (tid == 0) {
@@ -233,7 +237,8 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     mbar_init(BAR(LSUM_A), 256);
     mbar_init(BAR(LSUM_B), 256);
     mbar_init(BAR(STAGED), 256);
-    for (int i = STOP; i < ERR + 4; i++) misc[i] = 0;
+    mbar_init(BAR(DONE), 1);
+    for (int i = kPxStop; i < kPxWords; i++) misc[i] = 0;
     fence_mbar_init();
     prefetch_tmap(&tmk);
     prefetch_tmap(&tmv);
@@ -247,7 +252,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = misc[TMEM];
+  const uint32_t tmem = misc[kPxTmem];
   pdl_wait();
   pdl_launch();
 
@@ -256,26 +261,33 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
   const bool staging = S.own_box > 0 && !S.own_off && !S.stack;
   const int n_vs = staging ? VS - 1 : VS;
   uint8_t* const stage_out = smem + L_::kV + (VS - 1) * L_::kTile;
-  auto report = [&](int code, int where, int item, int aux) { px_report(const_cast<int*>(misc) + ERR, code, where, item, aux); };
-  auto wait_or_stop = [&](int bar, uint32_t parity, int where, int tag) -> bool {
-    if (mbar_try_wait(BAR(bar), parity)) return true;
-    const long long t0 = clock64();
-    while (true) {
-      if (misc[STOP] != 0) return false;
-      if (mbar_try_wait(BAR(bar), parity)) return true;
-      if (clock64() - t0 > AVSA_WAIT_LIMIT_CYCLES) {
-        report(AVSA_ERR_TIMEOUT, where, blockIdx.x, tag);
-        misc[STOP] = 1;
+  auto report = [&](int code, int where, int item, int aux) { px_report(const_cast<int*>(misc) + kPxErr, code, where, item, aux); };
+  // A wait is as few instructions as it can be: an item runs through a dozen of them, and items of few tiles are short of instructions (the SM's cache holds less than the
+  // roles' code: a third of its lookups missed with 3 tiles to an item).  So no wait looks at the clock; the watch of warp 15 sets the word that ends them all.
+  auto wait_or_stop = [&](int bar, uint32_t parity, int where) -> bool {
+    while (!mbar_try_wait(BAR(bar), parity))
+      if (misc[kPxStop] != 0) {
+        misc[kPxWhere] = where;
         return false;
       }
+    return true;
+  };
+  // The warps that load ahead wait most of the time, for a place: with sleeps between their looks the others have the issue slots (frames of 4 candidates, us: 952, with
+  // sleeps 880).
+  auto wait_idly = [&](int bar, uint32_t parity, int where) -> bool {
+    while (!mbar_try_wait(BAR(bar), parity)) {
+      if (misc[kPxStop] != 0) {
+        misc[kPxWhere] = where;
+        return false;
+      }
+      __nanosleep(64);
     }
+    return true;
   };
-  auto wait_all = [&](int bar, uint32_t parity, int where, int tag) -> bool {
-    return __all_sync(FULLM, wait_or_stop(bar, parity, where, tag));
-  };
+  auto wait_all = [&](int bar, uint32_t parity, int where) -> bool { return __all_sync(FULLM, wait_or_stop(bar, parity, where)); };
   auto get_item = [&](int n, PrefixItem& it) -> bool {     // false: stopped, or no more items
     const int slot = n % kPxRing;
-    if (!wait_all(ITEM_FULL + slot, (n / kPxRing) & 1, kPxItem, n)) return false;
+    if (!wait_all(ITEM_FULL + slot, (n / kPxRing) & 1, kPxItem)) return false;
     it = ring[slot];
     return it.type >= 0;
   };
@@ -319,7 +331,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
             const int id = __shfl_sync(FULLM, mine, (j << ppt_shift) + (lane & (ppt - 1)));
             int good = 1;
             if (lane == 0) {
-              if (round > 0) good = wait_or_stop(EMPTY + stage, (round - 1) & 1, is_k ? kPxKEmpty : kPxVEmpty, t0 + j) ? 1 : 0;
+              if (round > 0) good = wait_idly(EMPTY + stage, (round - 1) & 1, is_k ? kPxKEmpty : kPxVEmpty) ? 1 : 0;
               if (good) mbar_expect_tx(BAR(FULL + stage), L_::kTile);
             }
             good = __shfl_sync(FULLM, good, 0);
@@ -333,6 +345,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
             }
             __syncwarp();
             loads++;
+            if (is_k && lane == 0) misc[kPxProgress] = loads;
             if (++stage == STAGES) {
               stage = 0;
               round++;
@@ -347,7 +360,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       }
       if (ok) item_done(n);
     }
-    if (lane == 0 && misc[STOP] != 0)      // loads still in flight must land before this CTA's shared memory is given away
+    if (lane == 0 && misc[kPxStop] != 0)      // loads still in flight must land before this CTA's shared memory is given away
       for (int c = max(0, loads - STAGES); c < loads; c++) mbar_wait(BAR(FULL + c % STAGES), (c / STAGES) & 1);
   } else if (warp == 13 || warp == 14) {
     // ------------------------------------------------------------------ query rows into shared memory, 128-byte swizzled like a TMA tile
@@ -360,8 +373,8 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     for (int n = 0; ok; n++) {
       PrefixItem it;
       if (!get_item(n, it)) break;
-      if (n >= 2) ok = wait_all(Q_EMPTY + (n & 1), ((n >> 1) - 1) & 1, kPxQEmpty, n);
-      if (ok && n >= 1 && L_::kQSlot == 0) ok = wait_all(Q_EMPTY + ((n - 1) & 1), ((n - 1) >> 1) & 1, kPxQEmpty, n);      // one buffer
+      if (n >= 2) ok = __all_sync(FULLM, wait_idly(Q_EMPTY + (n & 1), ((n >> 1) - 1) & 1, kPxQEmpty));
+      if (ok && n >= 1 && L_::kQSlot == 0) ok = __all_sync(FULLM, wait_idly(Q_EMPTY + ((n - 1) & 1), ((n - 1) >> 1) & 1, kPxQEmpty));      // one buffer
       if (!ok) break;
       const uint32_t dst = base + (n & 1) * L_::kQSlot;
       const bool stacked = (it.type & 1) != 0;
@@ -406,7 +419,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       mbar_arrive(BAR(Q_FULL + (n & 1)));
       item_done(n);
     }
-    if (misc[STOP] != 0)
+    if (misc[kPxStop] != 0)
       for (int c = max(0, q_loads - 2); c < q_loads; c++) mbar_wait(BAR(Q_FULL + (c & 1)), (c >> 1) & 1);
   } else if (warp == 3) {
     // ------------------------------------------------------------------ scheduler
@@ -416,7 +429,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     // The last published item, and all before it, are done.
     auto all_done = [&]() -> bool {
       const int m = published - 1;
-      return m < 0 || wait_all(ITEM_EMPTY + m % kPxRing, (m / kPxRing) & 1, kPxItemEmpty, m);
+      return m < 0 || wait_all(ITEM_EMPTY + m % kPxRing, (m / kPxRing) & 1, kPxItemEmpty);
     };
     auto publish = [&](const PrefixItem& it) -> bool {
       const int m = published, slot = m % kPxRing;
@@ -429,7 +442,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
           page = S.pages;
         }
       }
-      if (m >= kPxRing && !wait_all(ITEM_EMPTY + slot, ((m / kPxRing) - 1) & 1, kPxItemEmpty, m)) return false;
+      if (m >= kPxRing && !wait_all(ITEM_EMPTY + slot, ((m / kPxRing) - 1) & 1, kPxItemEmpty)) return false;
       ring_pages[slot * 32 + lane] = page;
       if (lane == 0) ring[slot] = it;
       __syncwarp();
@@ -437,18 +450,25 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       published++;
       return true;
     };
-    // What has been published is done; items with a row that outgrew its reference run again.
-    auto settle = [&]() -> bool {
-      if (!all_done()) return false;
-      const int listed = __shfl_sync(FULLM, misc[LISTED], 0);
-      if (lane == 0) misc[LISTED] = 0;
-#pragma unroll 1
-      for (int i = 0; i < 2 * listed; i++) {
-        PrefixItem it = redo[i >> 1];
-        it.type |= i & 1 ? 4 : 2;
-        if (!publish(it)) return false;
+    // Publishes `it` (`last`: nothing), and in front of it, when the list is nearly full or this is the end, the items with a row that outgrew its reference again.
+    auto emit = [&](const PrefixItem& it, bool last) -> bool {
+      int again = 0;
+      if (last || __shfl_sync(FULLM, misc[kPxListed], 0) >= kPxRedo - kPxRing - 1) {
+        if (!all_done()) return false;
+        again = __shfl_sync(FULLM, misc[kPxListed], 0);
+        if (lane == 0) misc[kPxListed] = 0;
       }
-      return listed == 0 || all_done();
+      const int n = 2 * again + (last ? 0 : 1);
+#pragma unroll 1
+      for (int i = 0; i < n; i++) {
+        PrefixItem x = it;
+        if (i < 2 * again) {
+          x = redo[i >> 1];
+          x.type |= i & 1 ? 4 : 2;
+        }
+        if (!publish(x)) return false;
+      }
+      return again == 0 || !last || all_done();
     };
     // Lane l: the own item f0 + l of a key head.
     auto own_items = [&](int f0, int& nt, int& len, int& slot) {
@@ -626,8 +646,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
                 }
               }
             }
-            if (__shfl_sync(FULLM, misc[LISTED], 0) >= kPxRedo - kPxRing - 1) ok = settle();
-            if (ok) ok = publish(it);
+            ok = emit(it, false);
           }
         }
         // the next head's
@@ -639,7 +658,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       if (S.queue) {
         // (one item beyond the one being worked on: whatever else this CTA held, others could not take at the end)
         const int m = published - 2;
-        if (ok && m >= 0) ok = wait_all(ITEM_EMPTY + m % kPxRing, (m / kPxRing) & 1, kPxItemEmpty, m);
+        if (ok && m >= 0) ok = wait_all(ITEM_EMPTY + m % kPxRing, (m / kPxRing) & 1, kPxItemEmpty);
         int next = 0;
         if (lane == 0) next = n_cta + atomicAdd(p.counter, 1);
         id = __shfl_sync(FULLM, next, 0);
@@ -647,8 +666,8 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
         id += n_cta;
       }
     }
-    // (a row can outgrow its reference only in the first run, so settling once is enough)
-    if (ok) ok = settle();
+    // (a row can outgrow its reference only in the first run, so once is enough)
+    if (ok) ok = emit(PrefixItem{}, true);
     if (ok && lane == 0) {      // (all items are done: the slot is free)
       ring[published % kPxRing].type = -1;
       mbar_arrive(BAR(ITEM_FULL + published % kPxRing));
@@ -671,15 +690,15 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       PrefixItem it;
       if (!get_item(n, it)) break;
       const int cnt = it.cnt;
-      ok = wait_all(Q_FULL + (n & 1), (n >> 1) & 1, kPxQFull, n);
+      ok = wait_all(Q_FULL + (n & 1), (n >> 1) & 1, kPxQFull);
       const uint32_t qw_lo = q_lo + (n & 1) * (L_::kQSlot >> 4);
 #pragma unroll 1
       for (int t = 0; t < cnt && ok; t++) {
         const int j = t & 1;
-        ok = wait_all(K_FULL + stage, round & 1, kPxKFull, t);
+        ok = wait_all(K_FULL + stage, round & 1, kPxKFull);
         if (!ok) break;
         if (used[j] > 0) {
-          ok = wait_all(S_FREE + j, (used[j] - 1) & 1, kPxSFree, t);
+          ok = wait_all(S_FREE + j, (used[j] - 1) & 1, kPxSFree);
           if (!ok) break;
         }
         tc_fence_after();
@@ -705,7 +724,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       if (ok) item_done(n);
     }
     // tensor memory must not be freed under a running product (of items that have been read out none is)
-    if (misc[STOP] != 0) {
+    if (misc[kPxStop] != 0) {
       if (leader) umma_commit(BAR(QK_DRAIN));
       __syncwarp();
       mbar_wait(BAR(QK_DRAIN), 0);
@@ -738,7 +757,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
 #pragma unroll 1
         for (int t = 0; t < cnt && ok; t++) {
           const int j = t & 1;
-          ok = wait_all(V_FULL + stage, round & 1, kPxVFull, t);
+          ok = wait_all(V_FULL + stage, round & 1, kPxVFull);
           if (!ok) break;
           const int valid = it.kv_end - it.pos0 - t * 128;
           if (valid > 0 && valid < 128 && (valid & (S.page - 1)) != 0) {
@@ -753,10 +772,10 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
             fence_proxy_async();
             __syncwarp();
           }
-          ok = wait_all(P_FULL + 2 * j, used[j] & 1, kPxPFull, t);
+          ok = wait_all(P_FULL + 2 * j, used[j] & 1, kPxPFull);
           if (!ok) break;
           if (t == 0 && outputs > 0) {
-            ok = wait_all(O_FREE, (outputs - 1) & 1, kPxOFree, n);
+            ok = wait_all(O_FREE, (outputs - 1) & 1, kPxOFree);
             if (!ok) break;
           }
           tc_fence_after();
@@ -764,7 +783,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
           const uint32_t tm_buf = tmem_u + TM_P + j * 64;
           if (leader) issue_half(tm_buf, v_lo, 0, t > 0 ? 1u : 0u);
           __syncwarp();
-          ok = wait_all(P_FULL + 2 * j + 1, used[j] & 1, kPxPFull, t);
+          ok = wait_all(P_FULL + 2 * j + 1, used[j] & 1, kPxPFull);
           if (!ok) break;
           tc_fence_after();
           if (leader) {
@@ -784,13 +803,27 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       }
       if (ok) item_done(n);
     }
-    if (misc[STOP] != 0) {
+    if (misc[kPxStop] != 0) {
       if (leader) umma_commit(BAR(PV_DRAIN));
       __syncwarp();
       mbar_wait(BAR(PV_DRAIN), 0);
     }
   } else if (warp == 15) {
+    // ------------------------------------------------------------------ the watch: no key tile for a second, and every wait ends
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (lane == 0) {
+      long long since = clock64();
+      int seen = 0;
+      while (!mbar_try_wait(BAR(DONE), 0) && misc[kPxStop] == 0) {
+        const int now = misc[kPxProgress];
+        if (now != seen) {
+          seen = now;
+          since = clock64();
+        } else if (clock64() - since > AVSA_WAIT_LIMIT_CYCLES) {
+          misc[kPxStop] = 1;
+        }
+      }
+    }
   } else {
     // ------------------------------------------------------------------ softmax groups + epilogue
     asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
@@ -814,13 +847,13 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
         // no rows in this warp: its arrivals alone
 #pragma unroll 1
         for (int t = w; t < cnt && ok; t += 2) {
-          ok = wait_all(S_FULL + w, tiles & 1, kPxSFull, t);
+          ok = wait_all(S_FULL + w, tiles & 1, kPxSFull);
           if (!ok) break;
           mbar_arrive(BAR(S_FREE + w));
           tiles++;
           if (run == 1) continue;
           if (run == 0 && t == 0) mbar_arrive(BAR(MREF));
-          if (used > 0) ok = wait_all(P_FREE + w, (used - 1) & 1, kPxPFree, t);
+          if (used > 0) ok = wait_all(P_FREE + w, (used - 1) & 1, kPxPFree);
           if (!ok) break;
           mbar_arrive(BAR(P_FULL + 2 * w));
           mbar_arrive(BAR(P_FULL + 2 * w + 1));
@@ -829,13 +862,13 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
         if (!ok) break;
         if (run == 0) mrefs++;
         mbar_arrive(BAR(LSUM_A));
-        ok = wait_all(LSUM_A, n & 1, kPxLsum, n);
+        ok = wait_all(LSUM_A, n & 1, kPxLsum);
         if (!ok) break;
         mbar_arrive(BAR(LSUM_B));
-        ok = wait_all(LSUM_B, n & 1, kPxLsum, n);
+        ok = wait_all(LSUM_B, n & 1, kPxLsum);
         if (!ok) break;
         if (run != 1) {
-          ok = wait_all(O_FULL, outputs & 1, kPxOFull, n);
+          ok = wait_all(O_FULL, outputs & 1, kPxOFull);
           if (!ok) break;
           outputs++;
           mbar_arrive(BAR(O_FREE));
@@ -865,7 +898,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       uint64_t sum2[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll 1
       for (int t = w; t < cnt && ok; t += 2) {
-        ok = __all_sync(FULLM, wait_or_stop(S_FULL + w, tiles & 1, kPxSFull, t));
+        ok = __all_sync(FULLM, wait_or_stop(S_FULL + w, tiles & 1, kPxSFull));
         if (!ok) break;
         tc_fence_after();
         uint32_t s[128];
@@ -878,8 +911,11 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
         const int see = rel - t * 128;
         if (__any_sync(FULLM, see < 128)) {
 #pragma unroll
-          for (int j = 0; j < 128; j++)
-            if (j >= see) s[j] = 0xff800000u;
+          for (int c = 0; c < 4; c++) {      // (bits of a register: eight of them become predicates at once)
+            const uint32_t seen = see >= 32 * c + 32 ? 0xffffffffu : see <= 32 * c ? 0u : (1u << (see - 32 * c)) - 1u;
+#pragma unroll
+            for (int j = 0; j < 32; j++) s[c * 32 + j] = seen & (1u << j) ? s[c * 32 + j] : 0xff800000u;
+          }
         }
         if (run == 1 || (run == 0 && t == 0)) {
           float mx8[8];
@@ -899,7 +935,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
           mref_s[row] = m_ref;
           mbar_arrive(BAR(MREF));
         } else if (run == 0 && t == 1) {
-          ok = __all_sync(FULLM, wait_or_stop(MREF, mrefs & 1, kPxMref, t));
+          ok = __all_sync(FULLM, wait_or_stop(MREF, mrefs & 1, kPxMref));
           if (!ok) break;
           m_ref = mref_s[row];
         }
@@ -917,7 +953,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
             pk[j] = pack_bf16x2(p0, p1);
           }
           if (c == 0 && used > 0) {
-            ok = __all_sync(FULLM, wait_or_stop(P_FREE + w, (used - 1) & 1, kPxPFree, t));
+            ok = __all_sync(FULLM, wait_or_stop(P_FREE + w, (used - 1) & 1, kPxPFree));
             if (!ok) break;
           }
           tmem_st16(tm_p + c * 16, pk);
@@ -938,17 +974,17 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
         l_run = sa + sb;
       }
       // (a group without a tile of its own has no sum; the reference is the other one's)
-      if (run == 0 && row < it.nrows && !(l_run <= kFastRowSumLimit)) misc[FLAG + (n & 1)] = 1;
+      if (run == 0 && row < it.nrows && !(l_run <= kFastRowSumLimit)) misc[kPxFlag + (n & 1)] = 1;
       lsum_s[w * 128 + row] = run == 1 ? m_max : l_run;
       if (tid == 128) tma_store_wait_read();      // the rows staged before have been read when the groups have met
       mbar_arrive(BAR(LSUM_A));
-      ok = __all_sync(FULLM, wait_or_stop(LSUM_A, n & 1, kPxLsum, n));
+      ok = __all_sync(FULLM, wait_or_stop(LSUM_A, n & 1, kPxLsum));
       if (!ok) break;
       const float other = lsum_s[(1 - w) * 128 + row];
-      const bool again = misc[FLAG + (n & 1)] != 0;
+      const bool again = misc[kPxFlag + (n & 1)] != 0;
       if (run == 0 && cnt == 1 && w == 1) m_ref = mref_s[row];
       mbar_arrive(BAR(LSUM_B));
-      ok = __all_sync(FULLM, wait_or_stop(LSUM_B, n & 1, kPxLsum, n));
+      ok = __all_sync(FULLM, wait_or_stop(LSUM_B, n & 1, kPxLsum));
       if (!ok) break;
       if (run == 1) {
         m_given = fmaxf(m_max, other);
@@ -957,14 +993,14 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
         continue;
       }
       if (tid == 128) {
-        misc[FLAG + (n & 1)] = 0;
+        misc[kPxFlag + (n & 1)] = 0;
         if (again) {
-          redo[misc[LISTED]] = it;
-          misc[LISTED] = misc[LISTED] + 1;
-          misc[RECOMPUTED] = misc[RECOMPUTED] + 1;
+          redo[misc[kPxListed]] = it;
+          misc[kPxListed] = misc[kPxListed] + 1;
+          misc[kPxRecomputed] = misc[kPxRecomputed] + 1;
         }
       }
-      ok = __all_sync(FULLM, wait_or_stop(O_FULL, outputs & 1, kPxOFull, n));
+      ok = __all_sync(FULLM, wait_or_stop(O_FULL, outputs & 1, kPxOFull));
       if (!ok) break;
       outputs++;
       tc_fence_after();
@@ -976,11 +1012,13 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       tmem_wait_ld();
       tc_fence_before();
       mbar_arrive(BAR(O_FREE));
+      // (the short forms of quotient and logarithm: 1 to 2^64 as sums go, two units in the last place of fp32 and 1e-7; the long ones are 60 instructions)
+      const float sum = l_run + other;
+      const float inv = sum > 0.f || sum != sum ? __fdividef(1.0f, sum) : 0.f;
+      const float lse2 = sum != 0.f ? m_ref + __log2f(sum) : -INFINITY;
+      if (it.out < 0 && !again && w == 0 && row < it.nrows && p.lse != nullptr)
+        p.lse[(static_cast<int64_t>(b) * S.Hkv * S.G + it.hk * S.G + g) * S.L + i] = lse2 * 0.6931471805599453f;
       if (staging && it.out < 0) {
-        const float sum = l_run + other;
-        const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
-        if (!again && w == 0 && row < it.nrows && p.lse != nullptr)
-          p.lse[(static_cast<int64_t>(b) * S.Hkv * S.G + it.hk * S.G + g) * S.L + i] = sum != 0.f ? (m_ref + log2f(sum)) * 0.6931471805599453f : -INFINITY;
 #pragma unroll
         for (int c = 0; c < HALF / 8; c++) {
           const int col = w * HALF + c * 8;
@@ -993,15 +1031,12 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
         }
         fence_proxy_async();
         mbar_arrive(BAR(STAGED));
-        if (tid == 128 && wait_or_stop(STAGED, n_staged & 1, kPxLsum, n) && !again) {
+        if (tid == 128 && wait_or_stop(STAGED, n_staged & 1, kPxLsum) && !again) {
           for (int pn = 0; pn < NPANEL; pn++) tma_store_4d(&tmo, smem_u32(stage_out) + pn * PANEL, pn * 64, it.hk * S.G, S.by_G.div(it.row0), it.b);
           tma_store_commit();
         }
         n_staged++;
       } else if (!again && row < it.nrows) {
-        const float sum = l_run + other;
-        const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
-        const float lse2 = sum != 0.f ? m_ref + log2f(sum) : -INFINITY;
         if (it.out >= 0) {
           const int64_t at = it.out + row;
           if (w == 0) p.part_lse2[at] = lse2;
@@ -1014,9 +1049,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
             st_global_v8(dst + c * 8, r);
           }
         } else {
-          const int head = it.hk * S.G + g;
-          if (w == 0 && p.lse != nullptr) p.lse[(static_cast<int64_t>(b) * S.Hkv * S.G + head) * S.L + i] = lse2 * 0.6931471805599453f;
-          uint4* dst = reinterpret_cast<uint4*>(p.o + b * p.q.stride_b + head * p.q.stride_h + i * p.q.stride_n + w * HALF);
+          uint4* dst = reinterpret_cast<uint4*>(p.o + b * p.q.stride_b + (it.hk * S.G + g) * p.q.stride_h + i * p.q.stride_n + w * HALF);
 #pragma unroll
           for (int c = 0; c < HALF / 8; c++) {
             uint4 v;
@@ -1030,14 +1063,18 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       }
       item_done(n);
     }
-    if (tid == 128) tma_store_wait_read();      // (the last rows)
+    if (tid == 128) {
+      tma_store_wait_read();      // (the last rows)
+      mbar_arrive(BAR(DONE));
+    }
   }
   tc_fence_before();
   __syncthreads();
   if (warp == 2) tmem_dealloc(tmem, 512);
   if (tid == 0) {
-    p.cta_err[2 * blockIdx.x] = make_int4(misc[ERR], misc[ERR + 1], misc[ERR + 2], misc[ERR + 3]);
-    p.cta_err[2 * blockIdx.x + 1] = make_int4(misc[RECOMPUTED], 0, 0, 0);
+    p.cta_err[2 * blockIdx.x] = misc[kPxStop] != 0 ? make_int4(AVSA_ERR_TIMEOUT, misc[kPxWhere], blockIdx.x, misc[kPxProgress])
+                                          : make_int4(misc[kPxErr], misc[kPxErr + 1], misc[kPxErr + 2], misc[kPxErr + 3]);
+    p.cta_err[2 * blockIdx.x + 1] = make_int4(misc[kPxRecomputed], 0, 0, 0);
   }
 }
 
