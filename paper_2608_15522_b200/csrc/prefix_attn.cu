@@ -40,7 +40,7 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   s.L = L;
   const long long R = static_cast<long long>(L) * s.G, TO = (R + 127) / 128, F = TO * B, RS = R * B, TP = (RS + 127) / 128;
   const long long most = (static_cast<long long>(width) * page + 127) / 128, PT = static_cast<long long>(prefix_pages) * page / 128;
-  if (RS > 0x3fffffffll || F * Hkv > 0x3fffffffll || RS * Hkv > 0x3fffffffll || F * Hkv * (most > 0 ? most : 1) > 0x7fffffffll) return false;
+  if (RS > 0x3fffffffll || F * Hkv > 0x3fffffffll || RS * Hkv > 0x3fffffffll || F * Hkv * (most + kPxItemUnits) > 0x7fffffffll) return false;
   s.R = static_cast<int>(R);
   s.TO = static_cast<int>(TO);
   s.F = static_cast<int>(F);

@@ -5,12 +5,12 @@
 // entries one after the other ("stacked").  One token of 64 sequences with 4 query heads to a key head makes 4 rows a sequence, which leave 124 rows of a
 // tile empty, but 256 rows stacked: the beginning is read twice instead of 64 times, and the tensor cores work on full tiles.
 //
-// Work.  An item is a row tile with all its keys; its key tiles are units.  Which units a CTA takes:
+// Work.  An item is a row tile with all its keys; its key tiles, and a few more for what an item costs by itself, are units.  Which units a CTA takes:
 //   - prefix pieces: the key tiles of the beginning, head after head, are one stream of columns; `chunk` row tiles go through it side by side (a CTA each, so that
 //     the second reader of a key tile finds it in L2), and each group of `chunk` CTAs gets the same number of columns;
 //   - B pieces: the own items of all sequences, one after the other, are a stream that is cut into equal pieces: lengths as ragged as they may be,
 //     every CTA gets the same number of units, and all of them stream pages from HBM side by side;
-//   - A pieces: with several row tiles to a sequence (long blocks of queries) whole items come off a queue, so that CTAs that run at the
+//   - A pieces: with several row tiles to a sequence (long blocks of queries) and more keys than L2 keeps, whole items come off a queue, so that CTAs that run at the
 //     same time work on the same keys (as equal shares of the stream they would be heads apart: each tile from HBM), and only last ones that are few are cut.
 // What a cut or a stacked item leaves are fp32 rows, normalised by their own sum, and their log2 sums; prefix_merge_kernel joins them in a fixed order.
 // Lengths are on the device: every CTA's scheduler warp counts the units itself (a scan over the batch), nothing comes back to the host.
@@ -157,7 +157,10 @@ __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)) : "memory");
 }
 
-constexpr int kPxMinPiece = 4;       // key tiles: a CTA with fewer ends later than one that takes another's as well
+constexpr int kPxMinPiece = 4;       // units: a CTA with fewer ends later than one that takes another's as well
+// Units that an own item counts for beyond its key tiles, in front of them: what it costs apart from these (3 sequences of 500 to 9000 tokens under 300
+// queries each, us: 102 without, 82 with them; two or four instead of three are within 3 %).
+constexpr int kPxItemUnits = 3;
 
 // How the units are cut: the same in every CTA.
 struct PrefixPlan {
@@ -491,21 +494,28 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       }
       return v;
     };
+    auto units = [](int nt) { return nt > 0 ? nt + kPxItemUnits : 0; };
     int nt0 = 0, len0 = 0, slot0 = -1;      // own_items(0)
     // ---- the plan
     PrefixPlan P = {};
     int n_pre = 0;
+    bool queue = S.queue != 0;
     {
-      int most = 0, at = 0, W = 0;
+      int most = 0, at = 0, W = 0, tiles = 0;
 #pragma unroll 1
       for (int f0 = 0; f0 < S.F; f0 += 32) {
         int nt, len, slot;
         own_items(f0, nt, len, slot);
         if (f0 == 0) nt0 = nt, len0 = len, slot0 = slot;
-        W += nt;
+        W += units(nt);
+        tiles += nt;
         if (len > most) most = len, at = slot;
       }
       P.W = __reduce_add_sync(FULLM, W);
+      // keys and values that stay in L2 need no CTAs that work on the same ones (us, with them and without: the sequences of kPxItemUnits, 64 MB at most, 126 and 82;
+      // 30000 tokens under 4096 queries, 123 MB, 1420 and 1566)
+      const float bytes = static_cast<float>(__reduce_add_sync(FULLM, tiles)) * S.Hkv * (128.f * D * 4.f);
+      queue = queue && bytes > static_cast<float>(kL2KeepBytes) * S.TO;
       if (S.stack) {
         const int top = __reduce_max_sync(FULLM, most);
         P.donor = __shfl_sync(FULLM, at, __ffs(__ballot_sync(FULLM, most == top)) - 1);
@@ -529,7 +539,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       }
       P.TB = T;
       int want = min(max(1, n_cta - n_pre), (T + kPxMinPiece - 1) / kPxMinPiece);
-      if (S.queue && T > 0) {
+      if (queue && T > 0) {
         // Whole items, but those that would leave half of the CTAs or more without one at the end: they are cut into as many parts as there are CTAs for each
         // (a part costs four tiles' time and its rows' merge: 1024 items of 16 tiles, 6.9 a CTA, us: the last one of every CTA in quarters 152, none cut 123).
         const int items = S.Hkv * S.F, over = items - float_div(items, n_cta) * n_cta, parts = over > 0 ? min(8, float_div(n_cta, over)) : 1;
@@ -543,7 +553,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
           for (int f0 = 0; f0 < f; f0 += 32) {
             int nt, len, slot;
             own_items(f0, nt, len, slot);
-            before += __reduce_add_sync(FULLM, f0 + lane < f ? nt : 0);
+            before += __reduce_add_sync(FULLM, f0 + lane < f ? units(nt) : 0);
           }
           P.uA = hk * P.W + before;
         }
@@ -605,7 +615,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
           } else {
             own_items(f0, nt, len, slot);
           }
-          const int inc = scan(nt), first = before + inc - nt;
+          const int inc = scan(id < n_pre ? nt : units(nt)), first = before + inc - nt;
           const int lo = only < 0 ? max(u, first) : first, hi = only < 0 ? min(u1, before + inc) : only == f0 + lane ? first + nt : first;
           before += __shfl_sync(FULLM, inc, 31);
 #pragma unroll 1
@@ -655,7 +665,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
         u = 0;
         u1 -= per;
       }
-      if (S.queue) {
+      if (queue) {
         // (one item beyond the one being worked on: whatever else this CTA held, others could not take at the end)
         const int m = published - 2;
         if (ok && m >= 0) ok = wait_all(ITEM_EMPTY + m % kPxRing, (m / kPxRing) & 1, kPxItemEmpty);
