@@ -186,6 +186,7 @@ static int launch_tile(const PrefixLayout& y, const avsa_bf16_4d& k, const avsa_
 template <int D>
 static int launch_prefix(const PrefixLayout& y, const avsa_bf16_4d& k, const avsa_bf16_4d& v, const PrefixParams& p, cudaStream_t st) {
   const PrefixShape& s = y.s;
+  constexpr int kRows = prefix_merge_rows(D);
   int r = AVSA_OK;
   CUtensorMap tk, tv;      // of 16 keys
   if (y.own_stream && (!encode_bf16_tile_map(&tk, k.ptr, s.pages, s.Hkv, s.page, D, k.stride_b, k.stride_h, k.stride_n, 16) ||
@@ -199,15 +200,15 @@ static int launch_prefix(const PrefixLayout& y, const avsa_bf16_4d& k, const avs
     if (r != AVSA_OK) return r;
     if (y.own.splits > 1) {
       const long long rows = static_cast<long long>(s.B) * s.Hkv * s.R;
-      if (launch_pdl(prefix_join_kernel<D>, static_cast<unsigned>((rows + kPxMergeWarps - 1) / kPxMergeWarps), kPxMergeWarps * 32, 0, st, p, y.own) != cudaSuccess)
+      if (launch_pdl(prefix_join_kernel<D>, static_cast<unsigned>((rows + kRows - 1) / kRows), kPxMergeThreads, 0, st, p, y.own) != cudaSuccess)
         return AVSA_ERR_CUDA;
     }
   } else {
-    // (cut rows: at most nb_max times 128, a warp each)
-    const long long most = static_cast<long long>(s.nb_max) * 128 / kPxMergeWarps, ctas = 8ll * y.n_cta;
+    // (cut rows: at most nb_max times 128)
+    const long long most = static_cast<long long>(s.nb_max) * 128 / kRows, ctas = 8ll * y.n_cta;
     dim3 grid(static_cast<unsigned>(most < ctas ? most : ctas));
-    if (s.stack) grid = dim3(static_cast<unsigned>((static_cast<long long>(s.B) * s.R * s.Hkv + kPxMergeWarps - 1) / kPxMergeWarps));
-    if (launch_pdl(prefix_merge_kernel<D>, grid, kPxMergeWarps * 32, 0, st, p, y.n_cta) != cudaSuccess) return AVSA_ERR_CUDA;
+    if (s.stack) grid = dim3(static_cast<unsigned>((static_cast<long long>(s.B) * s.R * s.Hkv + kRows - 1) / kRows));
+    if (launch_pdl(prefix_merge_kernel<D>, grid, kPxMergeThreads, 0, st, p, y.n_cta) != cudaSuccess) return AVSA_ERR_CUDA;
   }
   return cudaGetLastError() == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
 }

@@ -195,9 +195,7 @@ __device__ __forceinline__ void stream_finish(const PrefixParams& p, const Strea
     int first, step, n;
     prefix_parts(p, t, hk, entry * S.R + rr, first, step, n);
     bool nan = lse2 != lse2;
-    float sum[4] = {acc.x, acc.y, acc.z, acc.w};
-    join_parts<D, 4>(p, first, step, n, 4 * x, sum, M, L, nan);
-    acc = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    join_parts<D>(p, [=](int k) { return first + static_cast<int64_t>(k) * step; }, n, 4 * x, acc, M, L, nan);
     lse2 = nan ? NAN : L > 0.f ? M + log2f(L) : -INFINITY;
     inv = nan ? NAN : L > 0.f ? 1.0f / L : 0.f;
   }
@@ -527,20 +525,23 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
   }
 }
 
-// The rows of own items whose keys were cut into parts: a warp each.
+// The rows of own items whose keys were cut into parts.
 template <int D>
-__global__ void __launch_bounds__(kPxMergeWarps * 32) prefix_join_kernel(const __grid_constant__ PrefixParams p, const StreamParams t) {
+__global__ void __launch_bounds__(kPxMergeThreads) prefix_join_kernel(const __grid_constant__ PrefixParams p, const StreamParams t) {
   pdl_wait();
   pdl_launch();
   const PrefixShape& S = p.s;
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * kPxMergeWarps + (threadIdx.x >> 5);      // ((entry, key head), row)
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * prefix_merge_rows(D) + threadIdx.x / (D / 4);      // ((entry, key head), row)
   if (at >= static_cast<int64_t>(S.B) * S.Hkv * S.R) return;
   const int pair = S.by_R.div(static_cast<int>(at)), rr = static_cast<int>(at) - pair * S.R, entry = pair / S.Hkv, hk = pair - entry * S.Hkv;
   const int i = S.by_G.div(rr), g = rr - i * S.G;
-  int first = 0, step = 0, n = 0;
-  if (t.join != 0) prefix_parts(p, t, hk, entry * S.R + rr, first, step, n);
-  const int own = t.out0 + (pair * t.tiles + (rr >> 4)) * t.splits * kStRows + (rr & 15);
-  prefix_merge_row<D>(p, first, step, n, own, t.splits, own + kStRows, kStRows, entry, hk * S.G + g, i);
+  PrefixRow row = {};
+  if (t.join != 0) prefix_parts(p, t, hk, entry * S.R + rr, row.first, row.step, row.n_first);
+  row.second = t.out0 + (pair * t.tiles + (rr >> 4)) * t.splits * kStRows + (rr & 15);
+  row.n_second = t.splits;
+  row.next = row.second + kStRows;
+  row.second_step = kStRows;
+  prefix_merge_row<D>(p, row, entry, hk * S.G + g, i, threadIdx.x % (D / 4));
 }
 
 }  // namespace avsa
