@@ -2,7 +2,8 @@
 //
 // What a call decides (which page goes where) is a few thousand integers: one kernel, a cluster of CTAs on one GPC, whose steps are
 // separated by cluster barriers instead of launches (about 0.5 us each against 2-3).  What it moves (page contents) is
-// a second kernel over the whole GPU behind it, bound by HBM: every byte read once and written once.
+// a second kernel over the whole GPU behind it, bound by HBM: every byte read once and written once (compaction of 1.5 GB: 499 us, 5.9 TB/s; 8 parents with four
+// branches each, 1.3 GB read and written: 228 us, 5.5 TB/s).
 //
 // Free pages are those with ref == 0; they are taken in ascending order, so that a result is determined by the state alone and what
 // is in use stays low in the pool.
