@@ -33,7 +33,7 @@ static_assert(sizeof(ListEntry) == 32, "two 16-byte accesses");
 // A workspace: status record | counts of the CTAs | claims [seqs] | list entries [n] | free pages [pages] | moves [max(n, pages)] int4
 struct CacheWs {
   StatusRecord* status;
-  int* counts;       // [3][kMetaCluster], then [62] free pages / moves in all, [63] needed pages in all
+  int* counts;       // [3][kMetaCluster], then [62] moves in all, [63] needed pages in all
   int* claims;
   ListEntry* list;
   int* free_pages;
@@ -109,9 +109,9 @@ __device__ __forceinline__ int block_scan(int v, int& all, int* sm) {
 
 constexpr int kVals = 8;      // values a thread has in flight in the passes over `ref`
 
-// Calls emit(index, value, rank) for the indices of [lo, hi) whose value is taken, in ascending order from rank `base` on.
+// Calls emit(index, value, rank) for the indices of [lo, hi) whose value is taken, in ascending order from rank `base` on; the rank behind the last one.
 template <class Take, class Emit>
-__device__ __forceinline__ void for_taken(const int32_t* v, int lo, int hi, int base, Take take, Emit emit, int* sm) {
+__device__ __forceinline__ int for_taken(const int32_t* v, int lo, int hi, int base, Take take, Emit emit, int* sm) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int t0 = lo; t0 < hi; t0 += kMetaThreads * kVals) {
     int x[kVals];
@@ -141,6 +141,7 @@ __device__ __forceinline__ void for_taken(const int32_t* v, int lo, int hi, int 
     base = before;
     __syncthreads();
   }
+  return base;
 }
 template <class Take>
 __device__ __forceinline__ int count_taken(const int32_t* v, int lo, int hi, Take take, int* sm) {
@@ -188,20 +189,21 @@ __device__ __forceinline__ void page_share(const avsa_cache& c, int rank, int ct
 enum { kExtend = 0, kFork = 1 };
 
 // What a call hands from one step to the next.  A single CTA keeps it in shared memory as far as it fits (a step of an ordinary call is then two trips to L2 deep
-// instead of eight: 16 sequences and 150 pages 8.3 -> 7.4 us); the CTAs of a cluster, and what is larger, in the workspace.
-constexpr int kOwnClaims = 4096, kOwnList = 1024, kOwnFree = 8192;
+// instead of eight: 16 sequences and 150 pages 8.3 -> 7.4 us); the CTAs of a cluster, and longer lists, in the workspace.  Its free pages it lists in one pass,
+// all of them, while the list is on its way (in a loop of calls 6.1 -> 5.3 us).
+// (As large as the call needs it: up to 48 KB need no kernel attribute, which costs the host as much as an argument check.)
+constexpr int kOwnClaims = 4096, kOwnList = 1024;
 struct AssignSmem {
-  int claims[kOwnClaims];
-  ListEntry list[kOwnList];
-  int free_pages[kOwnFree];
-  int counts[2];
+  size_t claims, free_pages, bytes;      // offsets behind the list entries
+  __host__ __device__ AssignSmem(const avsa_cache& c, int n)
+      : claims(n <= kOwnList ? static_cast<size_t>(n) * sizeof(ListEntry) : 0), free_pages(claims + (c.seqs <= kOwnClaims ? static_cast<size_t>(c.seqs) * 4 : 0)),
+        bytes(free_pages + static_cast<size_t>(c.pages) * 4) {}
 };
 
 // extend and fork: which free pages go to which sequence.
 template <int OP>
 __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const MetaArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];
-  AssignSmem& own = *reinterpret_cast<AssignSmem*>(smem);
   __shared__ int sm[kVals * 32];
   pdl_wait();
   pdl_launch();
@@ -209,28 +211,44 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
   const CacheWs& w = a.w;
   const int rank = cluster_rank(), ctas = cluster_size(), tid = threadIdx.x, lane = tid & 31;
   const bool alone = ctas == 1;
-  int* const claims = alone && c.seqs <= kOwnClaims ? own.claims : w.claims;
-  ListEntry* const list = alone && a.n <= kOwnList ? own.list : w.list;
-  int* const counts = alone ? own.counts : w.counts;      // [rank] free pages; behind all of them the needed ones
-  const int at_needed = alone ? 1 : kNumNeeded;
+  const AssignSmem own(c, a.n);
+  int* const claims = alone && c.seqs <= kOwnClaims ? reinterpret_cast<int*>(smem + own.claims) : w.claims;
+  ListEntry* const list = alone && a.n <= kOwnList ? reinterpret_cast<ListEntry*>(smem) : w.list;
+  int* const free_pages = alone ? reinterpret_cast<int*>(smem + own.free_pages) : w.free_pages;
+  // the thread's first entry: sequence, count or parent, tokens
+  int s0 = -1, o0 = -1, n0 = 0;
+  if (rank == 0 && tid < a.n) {
+    s0 = a.seq[tid];
+    o0 = a.other[tid];
+  }
   if (rank == 0 && tid == 0) clear_status(w.status);
   copy_state(c, rank, ctas);
-  int lo, hi;
-  page_share(c, rank, ctas, lo, hi);
+  {
+    const int of = OP == kFork ? o0 : s0;
+    if (of >= 0 && of < c.seqs) n0 = c.length[of];
+  }
+  // the list: entries that name a sequence again lose to the first one
+  auto seq_of = [&](int k) { return k == tid ? s0 : a.seq[k]; };
   if (rank == 0) {
-    // the list: entries that name a sequence again lose to the first one
     for (int k = tid; k < a.n; k += kMetaThreads) {
-      const int s = a.seq[k];
+      const int s = seq_of(k);
       if (s >= 0 && s < c.seqs) claims[s] = INT_MAX;
     }
   }
-  {
-    const int mine = count_taken(c.ref, lo, hi, [](int, int r) { return r <= 0; }, sm);
-    if (tid == 0) counts[rank] = mine;
+  int lo, hi;
+  page_share(c, rank, ctas, lo, hi);
+  auto is_free = [](int, int r) { return r <= 0; };
+  int n_free = 0;
+  if (alone) {
+    n_free = for_taken(c.ref, lo, hi, 0, is_free, [&](int page, int, int at) { free_pages[at] = page; }, sm);
+    // (its last step is a barrier)
+  } else {
+    const int mine = count_taken(c.ref, lo, hi, is_free, sm);
+    if (tid == 0) w.counts[rank] = mine;
   }
   if (rank == 0) {
     for (int k = tid; k < a.n; k += kMetaThreads) {
-      const int s = a.seq[k];
+      const int s = seq_of(k);
       if (s >= 0 && s < c.seqs) atomicMin(&claims[s], k);
     }
     __syncthreads();
@@ -240,13 +258,13 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
       ListEntry e = {};
       e.seq = -1;
       if (k < a.n) {
-        const int s = a.seq[k], o = a.other[k];
+        const int s = seq_of(k), o = k0 == 0 ? o0 : a.other[k];
         int bad = 0, code = AVSA_ERR_BAD_TABLE;
         if (s >= 0 && (OP == kExtend || o >= 0)) {
           if (s >= c.seqs || (OP == kFork && o >= c.seqs)) bad = kCacheSeq;
           else if (*static_cast<volatile int*>(&claims[s]) != k) bad = kCacheTwice;
           else {
-            const int n = c.length[OP == kFork ? o : s];
+            const int n = k0 == 0 ? n0 : c.length[OP == kFork ? o : s];
             const long long room = static_cast<long long>(c.width) * c.page;
             if (n < 0 || n > room || (OP == kExtend && o < 0)) bad = kCacheLength;
             else if (OP == kFork && c.length[s] != 0) bad = kCacheChild;
@@ -272,25 +290,23 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
       if (k < a.n) list[k] = e;
       __syncthreads();
     }
-    if (tid == 0) counts[at_needed] = taken;
+    if (tid == 0 && !alone) w.counts[kNumNeeded] = taken;
   }
-  if (alone) __syncthreads();
-  else cluster_sync_all();
-  const int needed = alone ? counts[at_needed] : __ldcg(&counts[at_needed]);
-  int* const free_pages = alone && needed <= kOwnFree ? own.free_pages : w.free_pages;
-  int base = 0, n_free = 0;
-  for (int r = 0; r < ctas; r++) {
-    const int m = alone ? counts[r] : __ldcg(&counts[r]);
-    if (r < rank) base += m;
-    n_free += m;
+  if (!alone) {
+    cluster_sync_all();
+    const int needed = __ldcg(&w.counts[kNumNeeded]);
+    int base = 0;
+    for (int r = 0; r < ctas; r++) {
+      const int m = __ldcg(&w.counts[r]);
+      if (r < rank) base += m;
+      n_free += m;
+    }
+    if (base < needed) {      // (uniform over the CTA)
+      // (ref has not been written yet: in place it is still the state before the call)
+      for_taken(c.ref, lo, hi, base, is_free, [&](int page, int, int at) { if (at < needed) free_pages[at] = page; }, sm);
+    }
+    cluster_sync_all();
   }
-  if (base < needed) {      // (uniform over the CTA)
-    // (ref has not been written yet: in place it is still the state before the call)
-    for_taken(c.ref, lo, hi, base, [](int, int r) { return r <= 0; },
-              [&](int page, int, int at) { if (at < needed) free_pages[at] = page; }, sm);
-  }
-  if (alone) __syncthreads();
-  else cluster_sync_all();
   const int warps = ctas * kMetaWarps;
   for (int k = rank * kMetaWarps + (tid >> 5); k < a.n; k += warps) {      // a warp to an entry
     int4 e0, e1;
@@ -347,10 +363,11 @@ __global__ void __launch_bounds__(kMetaThreads, 1) free_pages_kernel(const MetaA
   const avsa_cache& c = a.c;
   const int rank = cluster_rank(), ctas = cluster_size(), tid = threadIdx.x, lane = tid & 31;
   if (rank == 0 && tid == 0) clear_status(a.w.status);
+  const int k0 = rank * kMetaWarps + (tid >> 5), s0 = k0 < a.n ? a.seq[k0] : -1;
   copy_state(c, rank, ctas);
   cluster_sync_all();
-  for (int k = rank * kMetaWarps + (tid >> 5); k < a.n; k += ctas * kMetaWarps) {
-    const int s = a.seq[k];
+  for (int k = k0; k < a.n; k += ctas * kMetaWarps) {
+    const int s = k == k0 ? s0 : a.seq[k];
     if (s < 0) continue;
     if (s >= c.seqs) {
       if (lane == 0) report_status(a.w.status, AVSA_ERR_BAD_TABLE, kCacheSeq, k, s);
@@ -369,47 +386,67 @@ __global__ void __launch_bounds__(kMetaThreads, 1) free_pages_kernel(const MetaA
 }
 
 // Which pages move, and the references behind the moves.  Both lists are ascending, so the k-th move is known from the k-th
-// free place below n_live and the k-th page in use from n_live on.
+// free place below n_live and the k-th page in use from n_live on.  A single CTA keeps them in shared memory (freed and compacted, 3 kernels, 4.9 MB moved: 14.5 -> 12.6 us).
+__host__ __device__ inline int most_moves(const avsa_cache& c) { return c.pages / 2; }      // (as many places below n_live as pages behind)
+
 __global__ void __launch_bounds__(kMetaThreads, 1) plan_compaction_kernel(const MetaArgs a) {
+  extern __shared__ __align__(16) uint8_t smem[];
   __shared__ int sm[kVals * 32];
   pdl_wait();
   pdl_launch();
   const avsa_cache& c = a.c;
   const CacheWs& w = a.w;
   const int rank = cluster_rank(), ctas = cluster_size(), tid = threadIdx.x;
+  const bool alone = ctas == 1;
   if (rank == 0 && tid == 0) clear_status(w.status);
   copy_ints(c.length, c.length_out, c.seqs, rank, ctas);
   int lo, hi;
   page_share(c, rank, ctas, lo, hi);
-  const int mine = count_taken(c.ref, lo, hi, [](int, int r) { return r > 0; }, sm);
-  if (tid == 0) w.counts[rank] = mine;
-  cluster_sync_all();
-  int n_live = 0;
-  for (int r = 0; r < ctas; r++) n_live += __ldcg(&w.counts[r]);
-  const int holes = count_taken(c.ref, lo, min(hi, n_live), [](int, int r) { return r <= 0; }, sm);
-  // (pages in use from n_live on: all in use but those below n_live)
-  const int below = max(0, min(hi, n_live) - lo) - holes;
-  if (tid == 0) {
-    w.counts[kMetaCluster + rank] = holes;
-    w.counts[2 * kMetaCluster + rank] = mine - below;
-    if (rank == 0) a.n_live[0] = n_live;
+  auto is_free = [](int, int r) { return r <= 0; };
+  auto in_use = [](int, int r) { return r > 0; };
+  int* const own_from = reinterpret_cast<int*>(smem);
+  int* const own_to = own_from + most_moves(c);
+  int* const own_ref = own_to + most_moves(c);
+  const int mine = count_taken(c.ref, lo, hi, in_use, sm);
+  int n_live = mine, hole0 = 0, move0 = 0, n_moves = 0;
+  if (!alone) {
+    if (tid == 0) w.counts[rank] = mine;
+    cluster_sync_all();
+    n_live = 0;
+    for (int r = 0; r < ctas; r++) n_live += __ldcg(&w.counts[r]);
+    const int holes = count_taken(c.ref, lo, min(hi, n_live), is_free, sm);
+    // (pages in use from n_live on: all in use but those below n_live)
+    const int below = max(0, min(hi, n_live) - lo) - holes;
+    if (tid == 0) {
+      w.counts[kMetaCluster + rank] = holes;
+      w.counts[2 * kMetaCluster + rank] = mine - below;
+    }
+    cluster_sync_all();
+    for (int r = 0; r < ctas; r++) {
+      const int h = __ldcg(&w.counts[kMetaCluster + r]), m = __ldcg(&w.counts[2 * kMetaCluster + r]);
+      if (r < rank) hole0 += h, move0 += m;
+      n_moves += h;
+    }
   }
-  cluster_sync_all();
-  int hole0 = 0, move0 = 0, n_moves = 0;
-  for (int r = 0; r < ctas; r++) {
-    const int h = __ldcg(&w.counts[kMetaCluster + r]), m = __ldcg(&w.counts[2 * kMetaCluster + r]);
-    if (r < rank) hole0 += h, move0 += m;
-    n_moves += h;
-  }
-  if (rank == 0 && tid == 0) w.counts[kNumMoves] = n_moves;
   int* const move_words = reinterpret_cast<int*>(w.moves);
-  for_taken(c.ref, lo, min(hi, n_live), hole0, [](int, int r) { return r <= 0; },
-            [&](int page, int, int at) { move_words[4 * at + 1] = page; }, sm);
-  for_taken(c.ref, max(lo, min(hi, n_live)), hi, move0, [](int, int r) { return r > 0; },
-            [&](int page, int r, int at) {
-              move_words[4 * at] = page;
-              move_words[4 * at + 2] = r;
-            }, sm);
+  const int holes_end = for_taken(c.ref, lo, min(hi, n_live), hole0, is_free, [&](int page, int, int at) {
+    if (alone) own_to[at] = page;
+    else move_words[4 * at + 1] = page;
+  }, sm);
+  if (alone) n_moves = holes_end;
+  for_taken(c.ref, max(lo, min(hi, n_live)), hi, move0, in_use, [&](int page, int r, int at) {
+    if (alone) {
+      own_from[at] = page;
+      own_ref[at] = r;
+    } else {
+      move_words[4 * at] = page;
+      move_words[4 * at + 2] = r;
+    }
+  }, sm);
+  if (rank == 0 && tid == 0) {
+    a.n_live[0] = n_live;
+    w.counts[kNumMoves] = n_moves;
+  }
   __syncthreads();
   for (int p = lo + tid; p < hi; p += kMetaThreads) {
     const int r = c.ref[p];
@@ -420,10 +457,12 @@ __global__ void __launch_bounds__(kMetaThreads, 1) plan_compaction_kernel(const 
       c.ref_out[p] = r;
     }
   }
-  cluster_sync_all();
+  if (alone) __syncthreads();
+  else cluster_sync_all();
   // free_pages[p] is where page p >= n_live has gone, -1 for one that was not in use
   for (int k = rank * kMetaThreads + tid; k < n_moves; k += ctas * kMetaThreads) {
-    const int4 m = __ldcg(&w.moves[k]);
+    const int4 m = alone ? make_int4(own_from[k], own_to[k], own_ref[k], 0) : __ldcg(&w.moves[k]);
+    if (alone) w.moves[k] = m;
     c.ref_out[m.y] = m.z;
     w.free_pages[m.x] = m.y;
   }
@@ -591,7 +630,8 @@ static unsigned meta_cluster(const avsa_cache& c) {
 }
 static cudaError_t launch_meta(void (*kernel)(MetaArgs), const MetaArgs& a, cudaStream_t st, size_t smem = 0) {
   const unsigned ctas = meta_cluster(a.c);
-  if (smem > 0) {
+  if (ctas > 1) smem = 0;
+  if (smem > 48 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
   }
@@ -624,7 +664,7 @@ extern "C" int avsa_cache_extend(avsa_cache c, const int32_t* seq, const int32_t
   if (st != AVSA_OK) return st;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
   const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), seq, count, n, nullptr};
-  if (launch_meta(assign_pages_kernel<kExtend>, a, as_stream(stream), sizeof(AssignSmem)) != cudaSuccess) return AVSA_ERR_CUDA;
+  if (launch_meta(assign_pages_kernel<kExtend>, a, as_stream(stream), AssignSmem(c, n).bytes) != cudaSuccess) return AVSA_ERR_CUDA;
   return done();
 }
 
@@ -635,7 +675,7 @@ extern "C" int avsa_cache_fork(avsa_cache c, avsa_pages pool, const int32_t* par
   if (st != AVSA_OK) return st;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
   const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), child, parent, n, nullptr};
-  if (launch_meta(assign_pages_kernel<kFork>, a, as_stream(stream), sizeof(AssignSmem)) != cudaSuccess) return AVSA_ERR_CUDA;
+  if (launch_meta(assign_pages_kernel<kFork>, a, as_stream(stream), AssignSmem(c, n).bytes) != cudaSuccess) return AVSA_ERR_CUDA;
   if (n > 0) {
     CopyArgs m = {};
     m.pool = pool;
@@ -663,7 +703,7 @@ extern "C" int avsa_cache_compact(avsa_cache c, avsa_pages pool, int32_t* n_live
   if (n_live == nullptr || !aligned4(n_live)) return AVSA_ERR_INVALID_ARG;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
   const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, 0), nullptr, nullptr, 0, n_live};
-  if (launch_meta(plan_compaction_kernel, a, as_stream(stream)) != cudaSuccess) return AVSA_ERR_CUDA;
+  if (launch_meta(plan_compaction_kernel, a, as_stream(stream), static_cast<size_t>(most_moves(c)) * 12) != cudaSuccess) return AVSA_ERR_CUDA;
   CopyArgs m = {};
   m.pool = pool;
   m.moves = a.w.moves;
