@@ -227,12 +227,16 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
     const int of = OP == kFork ? o0 : s0;
     if (of >= 0 && of < c.seqs) n0 = c.length[of];
   }
-  // the list: entries that name a sequence again lose to the first one
+  // the list: entries that name a sequence again lose to the first one (of those that are not left out)
   auto seq_of = [&](int k) { return k == tid ? s0 : a.seq[k]; };
+  auto claims_of = [&](int k) {
+    const int s = seq_of(k), o = k == tid ? o0 : a.other[k];
+    return s < c.seqs && (OP == kExtend || o >= 0) ? s : -1;
+  };
   if (rank == 0) {
     for (int k = tid; k < a.n; k += kMetaThreads) {
-      const int s = seq_of(k);
-      if (s >= 0 && s < c.seqs) claims[s] = INT_MAX;
+      const int s = claims_of(k);
+      if (s >= 0) claims[s] = INT_MAX;
     }
   }
   int lo, hi;
@@ -248,8 +252,8 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
   }
   if (rank == 0) {
     for (int k = tid; k < a.n; k += kMetaThreads) {
-      const int s = seq_of(k);
-      if (s >= 0 && s < c.seqs) atomicMin(&claims[s], k);
+      const int s = claims_of(k);
+      if (s >= 0) atomicMin(&claims[s], k);
     }
     __syncthreads();
     int taken = 0;

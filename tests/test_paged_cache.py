@@ -410,6 +410,21 @@ def test_fork_refuses_what_cannot_be_had():
 
 
 @gpu
+def test_fork_entries_that_are_left_out_take_no_place():
+    """A negative parent leaves its entry out; a later one may name the same child."""
+    table, length, ref = np.array([[0, 1], [-1, -1]], np.int32), np.array([20, 0], np.int32), np.array([1, 1, 0], np.int32)
+    pool = torch.randn((1, 3, 1, 16, 64), device="cuda").bfloat16()
+    want = orc.fork(table, length, ref, [-1, 0], [1, 1], 16)
+    assert not want[4] and want[3] == [(1, 2)]
+    state = [cu(x) for x in (table, length, ref)]
+    ws = av.avsa_cache_fork(pool, *state, ints([-1, 0]), ints([1, 1]))[3]
+    assert status(ws) == av.AVSA_OK
+    for g, w in zip(state, want):
+        assert np.array_equal(nump(g), w)
+    assert torch.equal(pool[:, 2], pool[:, 1])
+
+
+@gpu
 def test_malformed_rows_are_reported():
     """Pages out of range and pages that nobody holds: reported, nothing outside the arrays touched."""
     table, length, ref = ints([[0, 9, -3]]), ints([40]), ints([0, 0, 1])
