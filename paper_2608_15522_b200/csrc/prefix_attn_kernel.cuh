@@ -21,7 +21,7 @@
 // box of (heads, tokens, batch entries) where the sizes allow it, else two warps gather them with cp.async (1500 cycles more).  An item with a row that outgrew its reference runs again
 // in the same CTA: once for the row maxima alone, once with these as the references.
 //
-// Bound by the exponentials (1024 cycles of a tile) and the products (1024 with 128 channels) in turn, 1650 cycles a tile, and by 4000 cycles an item for its query rows, first
+// Bound by the exponentials (1024 cycles of a tile) and the products (1024 with 128 channels) in turn, 1450 cycles a tile, and by 4000 cycles an item for its query rows, first
 // maxima and epilogue: 4 x 1560 queries of 24 heads against 13976 keys each, 128 channels, 880 us (1218 TFLOP/s, in a longer loop under the power limit 1060); 148 x 8 items of
 // three tiles 64 us.
 #pragma once
