@@ -149,3 +149,42 @@ def test_command(capsys):
     assert int(cache.table.max()) == live - 1
     main("--layers 1 --heads 2 --heads-kv 1 --d 64 --beginning 64 --chunk 16 --audio 1 --candidates 2 --rounds 1 --page 32".split())
     assert "compacted: pages 0..2" in capsys.readouterr().out
+
+
+@gpu
+@pytest.mark.parametrize("L, H, Hkv", [(1, 8, 2), (40, 4, 4)])
+def test_step_as_a_graph(L, H, Hkv):
+    """Lengths and pages are read on the device only: a step captured once goes on where the last replay ended."""
+    d, page, seqs, shared, steps = 64, 16, 3, 4, 9
+
+    def begin():
+        cache = ClipCache(2, Hkv, d, page, 120, seqs, 40)
+        gen = torch.Generator().manual_seed(5)
+        draw = lambda n, h, m: torch.randn((n, h, m, d), generator=gen).bfloat16().cuda()
+        cache.begin_step([0], [shared * page + 3])
+        for layer in range(2):
+            cache.attend(layer, *(draw(1, h, shared * page + 3) for h in (H, Hkv, Hkv)), causal=True)
+        cache.branch([0, 0], [1, 2])
+        return cache, [[draw(seqs, h, L) for h in (H, Hkv, Hkv)] for _ in range(2)]
+
+    seq, count = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([2, 0, 1], [L, L - 1, L]))
+
+    def step(cache, inputs):
+        cache.begin_step(seq, count)
+        return [cache.attend(i, *x, shared, causal=True) for i, x in enumerate(inputs)]
+
+    plain, inputs = begin()
+    want = [[o.clone() for o in step(plain, inputs)] for _ in range(steps)]
+    plain.check()
+    cache, inputs = begin()
+    graph = torch.cuda.CUDAGraph()
+    state = [t.clone() for t in cache._state()]
+    with torch.cuda.graph(graph):
+        got = step(cache, inputs)
+    assert all(torch.equal(a, b) for a, b in zip(state, cache._state()))          # captured, not run
+    for n in range(steps):
+        graph.replay()
+        for a, b in zip(got, want[n]):
+            assert torch.equal(a, b), n
+    cache.check()
+    assert all(torch.equal(a, b) for a, b in zip(plain._state(), cache._state()))
