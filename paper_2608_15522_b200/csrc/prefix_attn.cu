@@ -102,15 +102,19 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     y.own.out0 = static_cast<int>(own0);
     const long long keys = static_cast<long long>(width) * page - s.k0;      // at most
     const int slots = sms * stream_ctas(stream_products(R));
-    // An item's keys over a cluster: all slots busy, and no CTA with more than 1024 keys while others have none.  What eight CTAs an item do not fill
-    // is cut into parts that a kernel behind joins.
-    y.own_cluster = 1;
-    while (y.own_cluster < 8 && y.own.items < (1 << 27) && keys > 128ll * y.own_cluster &&
-           (static_cast<long long>(y.own.items) * y.own_cluster < slots || keys > 1024ll * y.own_cluster)) y.own_cluster *= 2;
+    // An item's keys over a cluster, 64 keys a CTA at least (a block a warp), as many CTAs as the SMs hold side by side: nine tenths of the slots, since a cluster takes its
+    // own from one GPC and what does not fit waits for a whole item (us, filled to the last slot and like this: 96 items of 500 keys of 64 channels 14.4 and 9.7, 72
+    // of 900 keys of 128 channels 16.4 and 10.3, 144 of 800 17.5 and 13.0).  No CTA has more than 1024 keys while others may have none (30 x 8 items of 1 to 1500
+    // keys 15.7, of up to 1500 keys a CTA 17.0, but all of 1500 keys 24.5 and 19.7).  What eight CTAs an item do not fill is cut into parts that a kernel behind joins.
+    const long long fit = slots * 9ll / 10 / (y.own.items + 1ll), by_keys = keys / 64;
+    long long ctas = fit < by_keys ? fit : by_keys;
+    ctas = ctas < 1 ? 1 : ctas > 8 ? 8 : ctas;
+    while (ctas < 8 && y.own.items < (1 << 27) && keys > 1024 * ctas) ctas = 2 * ctas < 8 ? 2 * ctas : 8;
+    y.own_cluster = static_cast<int>(ctas);
     y.own.splits = 1;
     if (static_cast<long long>(y.own.items) * 8 < sms && keys >= 4096) {
       y.own_cluster = 1;
-      y.own.splits = slots / y.own.items;
+      y.own.splits = (slots - 1) / y.own.items;      // (one slot for the check of the tables)
       rows += static_cast<size_t>(y.own.items) * y.own.splits * kStRows;
     }
     y.own.check = 1;
