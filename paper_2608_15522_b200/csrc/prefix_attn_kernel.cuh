@@ -1143,18 +1143,22 @@ struct PrefixRow {
     return k == 0 ? second : next + static_cast<int64_t>(k - 1) * second_step;
   }
 };
-// Thread x of the row's D/4.
+// Thread x of the row's D/4: the final row.
+template <int D>
+__device__ __forceinline__ void prefix_final_row(const PrefixParams& p, float4 o, float M, float L, bool nan, int b, int head, int i, int x) {
+  const float inv = nan ? NAN : L > 0.f ? 1.0f / L : 0.f;
+  __nv_bfloat16* dst = p.o + b * p.q.stride_b + head * p.q.stride_h + i * p.q.stride_n + 4 * x;
+  *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+  if (x == 0 && p.lse != nullptr)
+    p.lse[(static_cast<int64_t>(b) * p.s.Hkv * p.s.G + head) * p.s.L + i] = nan ? NAN : L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+}
 template <int D>
 __device__ __forceinline__ void prefix_merge_row(const PrefixParams& p, const PrefixRow& row, int b, int head, int i, int x) {
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   float M = 0.f, L = 0.f;
   bool nan = false;
   join_parts<D>(p, row, row.n_first + row.n_second, 4 * x, o, M, L, nan);
-  const float inv = nan ? NAN : L > 0.f ? 1.0f / L : 0.f;
-  __nv_bfloat16* dst = p.o + b * p.q.stride_b + head * p.q.stride_h + i * p.q.stride_n + 4 * x;
-  *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-  if (x == 0 && p.lse != nullptr)
-    p.lse[(static_cast<int64_t>(b) * p.s.Hkv * p.s.G + head) * p.s.L + i] = nan ? NAN : L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+  prefix_final_row<D>(p, o, M, L, nan, b, head, i, x);
 }
 
 template <int D>
