@@ -108,6 +108,7 @@ __device__ __forceinline__ int block_scan(int v, int& all, int* sm) {
 }
 
 constexpr int kVals = 8;      // values a thread has in flight in the passes over `ref`
+constexpr size_t kScanBytes = kVals * 32 * sizeof(int);      // of the kernels' own shared memory, for their counts
 
 // Calls emit(index, value, rank) for the indices of [lo, hi) whose value is taken, in ascending order from rank `base` on; the rank behind the last one.
 template <class Take, class Emit>
@@ -191,7 +192,7 @@ enum { kExtend = 0, kFork = 1 };
 // What a call hands from one step to the next.  A single CTA keeps it in shared memory as far as it fits (a step of an ordinary call is then two trips to L2 deep
 // instead of eight: 16 sequences and 150 pages 8.3 -> 7.4 us); the CTAs of a cluster, and longer lists, in the workspace.  Its free pages it lists in one pass,
 // all of them, while the list is on its way (in a loop of calls 6.1 -> 5.3 us).
-// (As large as the call needs it: up to 48 KB need no kernel attribute, which costs the host as much as an argument check.)
+// (As large as the call needs it: up to 48 KB, the kernels' own arrays among them, need no kernel attribute, which costs the host as much as an argument check.)
 constexpr int kOwnClaims = 4096, kOwnList = 1024;
 struct AssignSmem {
   size_t claims, free_pages, bytes;      // offsets behind the list entries
@@ -635,7 +636,7 @@ static unsigned meta_cluster(const avsa_cache& c) {
 static cudaError_t launch_meta(void (*kernel)(MetaArgs), const MetaArgs& a, cudaStream_t st, size_t smem = 0) {
   const unsigned ctas = meta_cluster(a.c);
   if (ctas > 1) smem = 0;
-  if (smem > 48 * 1024) {
+  if (smem + kScanBytes > 48 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
   }
