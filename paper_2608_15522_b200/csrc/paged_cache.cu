@@ -200,6 +200,7 @@ struct AssignSmem {
       : claims(n <= kOwnList ? static_cast<size_t>(n) * sizeof(ListEntry) : 0), free_pages(claims + (c.seqs <= kOwnClaims ? static_cast<size_t>(c.seqs) * 4 : 0)),
         bytes(free_pages + static_cast<size_t>(c.pages) * 4) {}
 };
+constexpr size_t kAssignMost = kOwnList * sizeof(ListEntry) + kOwnClaims * 4 + kMetaSingle * 4;      // (a single CTA has kMetaSingle pages at most)
 
 // extend and fork: which free pages go to which sequence.
 template <int OP>
@@ -393,6 +394,7 @@ __global__ void __launch_bounds__(kMetaThreads, 1) free_pages_kernel(const MetaA
 // Which pages move, and the references behind the moves.  Both lists are ascending, so the k-th move is known from the k-th
 // free place below n_live and the k-th page in use from n_live on.  A single CTA keeps them in shared memory (freed and compacted, 3 kernels, 4.9 MB moved: 14.5 -> 12.6 us).
 __host__ __device__ inline int most_moves(const avsa_cache& c) { return c.pages / 2; }      // (as many places below n_live as pages behind)
+constexpr size_t kMoveBytes = 12, kPlanMost = kMetaSingle / 2 * kMoveBytes;
 
 __global__ void __launch_bounds__(kMetaThreads, 1) plan_compaction_kernel(const MetaArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];
@@ -633,11 +635,13 @@ static unsigned meta_cluster(const avsa_cache& c) {
   if (c.table != c.table_out) ints += static_cast<long long>(c.seqs) * c.width;
   return ints <= kMetaSingle ? 1u : static_cast<unsigned>(kMetaCluster);
 }
-static cudaError_t launch_meta(void (*kernel)(MetaArgs), const MetaArgs& a, cudaStream_t st, size_t smem = 0) {
+// `most`: the largest `smem` of any call of the kernel.  The limit belongs to the kernel, not to the call: host threads with pools of different sizes would lower it
+// for one another between setting it and the launch, so all of them set the same.
+static cudaError_t launch_meta(void (*kernel)(MetaArgs), const MetaArgs& a, cudaStream_t st, size_t smem = 0, size_t most = 0) {
   const unsigned ctas = meta_cluster(a.c);
   if (ctas > 1) smem = 0;
   if (smem + kScanBytes > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most));
     if (e != cudaSuccess) return e;
   }
   return launch_pdl_clusters(kernel, ctas, ctas, kMetaThreads, smem, st, a);
@@ -669,7 +673,7 @@ extern "C" int avsa_cache_extend(avsa_cache c, const int32_t* seq, const int32_t
   if (st != AVSA_OK) return st;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
   const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), seq, count, n, nullptr};
-  if (launch_meta(assign_pages_kernel<kExtend>, a, as_stream(stream), AssignSmem(c, n).bytes) != cudaSuccess) return AVSA_ERR_CUDA;
+  if (launch_meta(assign_pages_kernel<kExtend>, a, as_stream(stream), AssignSmem(c, n).bytes, kAssignMost) != cudaSuccess) return AVSA_ERR_CUDA;
   return done();
 }
 
@@ -680,7 +684,7 @@ extern "C" int avsa_cache_fork(avsa_cache c, avsa_pages pool, const int32_t* par
   if (st != AVSA_OK) return st;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
   const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), child, parent, n, nullptr};
-  if (launch_meta(assign_pages_kernel<kFork>, a, as_stream(stream), AssignSmem(c, n).bytes) != cudaSuccess) return AVSA_ERR_CUDA;
+  if (launch_meta(assign_pages_kernel<kFork>, a, as_stream(stream), AssignSmem(c, n).bytes, kAssignMost) != cudaSuccess) return AVSA_ERR_CUDA;
   if (n > 0) {
     CopyArgs m = {};
     m.pool = pool;
@@ -708,7 +712,7 @@ extern "C" int avsa_cache_compact(avsa_cache c, avsa_pages pool, int32_t* n_live
   if (n_live == nullptr || !aligned4(n_live)) return AVSA_ERR_INVALID_ARG;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
   const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, 0), nullptr, nullptr, 0, n_live};
-  if (launch_meta(plan_compaction_kernel, a, as_stream(stream), static_cast<size_t>(most_moves(c)) * 12) != cudaSuccess) return AVSA_ERR_CUDA;
+  if (launch_meta(plan_compaction_kernel, a, as_stream(stream), most_moves(c) * kMoveBytes, kPlanMost) != cudaSuccess) return AVSA_ERR_CUDA;
   CopyArgs m = {};
   m.pool = pool;
   m.moves = a.w.moves;

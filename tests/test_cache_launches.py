@@ -2,8 +2,12 @@
 import os
 import subprocess
 import sys
+import threading
 
 import pytest
+import torch
+
+from paper_2608_15522_b200 import binding as av
 
 gpu = pytest.mark.gpu
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -57,3 +61,31 @@ def test_pools_around_the_shared_memory_that_needs_no_asking():
     """In a process of its own, smallest first: a larger call before would leave the limit raised."""
     r = subprocess.run([sys.executable, "-c", POOLS], cwd=ROOT, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     assert r.returncode == 0, r.stdout
+
+
+@gpu
+def test_threads_with_pools_of_different_sizes():
+    """Two threads, streams and workspaces; what the kernels of both need lies above what they get without asking."""
+    refused = []
+
+    def work(pages):
+        ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+        with torch.cuda.stream(torch.cuda.Stream()):
+            table, length, ref = torch.full((2, 4), -1, dtype=torch.int32, device="cuda"), ints([0, 0]), torch.zeros(pages, dtype=torch.int32, device="cuda")
+            pool = torch.zeros((1, pages, 1, 16, 64), dtype=torch.bfloat16, device="cuda")
+            seq, count = ints([0]), ints([0])
+            try:
+                for _ in range(4000):
+                    av.avsa_cache_extend(table, length, ref, seq, count, 16)
+                    av.avsa_cache_fork(pool, table, length, ref, seq, seq)
+                    av.avsa_cache_compact(pool, table, length, ref)
+            except av.AvsaError as e:
+                refused.append((pages, str(e)))
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=work, args=(pages,)) for pages in (12500, 16000)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not refused
