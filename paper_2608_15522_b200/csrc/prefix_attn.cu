@@ -30,7 +30,7 @@ struct PrefixLayout {
   size_t plan, cta_err, own_rec, cut_rec, redo, lse, o, total;       // offsets in the workspace
 };
 
-// False: more units than 32 bits count.
+// False: more units, or key positions rounded up to a tile, than 32 bits count.
 static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int width, int prefix_pages, int causal, PrefixLayout& y) {
   PrefixShape& s = y.s;
   s = {};
@@ -40,7 +40,7 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   s.L = L;
   const long long R = static_cast<long long>(L) * s.G, TO = (R + 127) / 128, F = TO * B, RS = R * B, TP = (RS + 127) / 128;
   const long long most = (static_cast<long long>(width) * page + 127) / 128, PT = static_cast<long long>(prefix_pages) * page / 128;
-  if (RS > 0x3fffffffll || F * Hkv > 0x3fffffffll || RS * Hkv > 0x3fffffffll || F * Hkv * (most + kPxItemUnits) > 0x7fffffffll) return false;
+  if (static_cast<long long>(width) * page > 0x7fffff80ll || RS > 0x3fffffffll || F * Hkv > 0x3fffffffll || RS * Hkv > 0x3fffffffll || F * Hkv * (most + kPxItemUnits) > 0x7fffffffll) return false;
   s.R = static_cast<int>(R);
   s.TO = static_cast<int>(TO);
   s.F = static_cast<int>(F);
