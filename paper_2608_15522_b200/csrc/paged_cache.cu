@@ -187,6 +187,9 @@ __device__ __forceinline__ void page_share(const avsa_cache& c, int rank, int ct
   hi = min(c.pages, lo + part);
 }
 
+// Pages of so many tokens.
+__device__ __forceinline__ int pages_of(int tokens, int page) { return tokens / page + (tokens % page != 0); }
+
 enum { kExtend = 0, kFork = 1 };
 
 // What a call hands from one step to the next.  A single CTA keeps it in shared memory as far as it fits (a step of an ordinary call is then two trips to L2 deep
@@ -271,7 +274,7 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
           else if (*static_cast<volatile int*>(&claims[s]) != k) bad = kCacheTwice;
           else {
             const int n = k0 == 0 ? n0 : c.length[OP == kFork ? o : s];
-            const long long room = static_cast<long long>(c.width) * c.page;
+            const long long room = min(static_cast<long long>(c.width) * c.page, static_cast<long long>(INT_MAX));      // (a length has 31 bits)
             if (n < 0 || n > room || (OP == kExtend && o < 0)) bad = kCacheLength;
             else if (OP == kFork && c.length[s] != 0) bad = kCacheChild;
             else if (OP == kExtend && n + static_cast<long long>(o) > room) bad = kCacheFull, code = AVSA_ERR_NO_PAGES;
@@ -281,7 +284,7 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
               e.tokens = n;
               if (OP == kExtend) {
                 e.new_tokens = o;
-                e.need = (n + o + c.page - 1) / c.page - (n + c.page - 1) / c.page;
+                e.need = pages_of(n + o, c.page) - pages_of(n, c.page);
               } else {
                 e.need = n % c.page != 0;
               }
@@ -329,7 +332,7 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
     if (s < 0 || refused) continue;
     int32_t* row = c.table_out + static_cast<long long>(s) * c.width;
     if (OP == kExtend) {
-      const int have = (tokens + c.page - 1) / c.page;
+      const int have = pages_of(tokens, c.page);
       for (int j = lane; j < need; j += 32) {
         const int page = free_page(first + j);
         row[have + j] = page;

@@ -1,4 +1,4 @@
-"""Launches of the paged cache's calls that one CTA takes alone, by the shared memory that they ask for."""
+"""Launches of the paged cache's calls that one CTA takes alone, by the shared memory that they ask for; lengths of 31 bits."""
 import os
 import subprocess
 import sys
@@ -89,3 +89,23 @@ def test_threads_with_pools_of_different_sizes():
     for t in threads:
         t.join()
     assert not refused
+
+
+@gpu
+def test_extend_lengths_up_to_31_bits():
+    """A row that could hold 2^31 tokens: pages are counted without wrapping, what a length cannot say is refused."""
+    page, width, top = 128, 1 << 24, (1 << 31) - 1
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    table = torch.full((2, width), -1, dtype=torch.int32, device="cuda")
+    for length, count, want, code in (([top - 5, 0], [3, 1], [top - 2, 1], av.AVSA_OK),
+                                      ([top - 128, 0], [2, 1], [top - 126, 1], av.AVSA_OK),          # one page more
+                                      ([top - 5, 0], [6, 1], [top - 5, 1], av.AVSA_ERR_NO_PAGES),
+                                      ([0, 0], [top, 1], [0, 0], av.AVSA_ERR_NO_PAGES)):             # 2^24 pages: there are four, and who is behind gets none
+        table.fill_(-1)
+        n, ref = ints(length), ints([0, 1, 0, 0])
+        ws = av.avsa_cache_extend(table, n, ref, ints([0, 1]), ints(count), page)[3]
+        assert av.avsa_read_status(ws)[0] == code and n.tolist() == want
+        crossing = length[0] == top - 128
+        assert int(table[0, -1]) == (0 if crossing else -1)
+        assert int(table[1, 0]) == (-1 if want[1] == 0 else 2 if crossing else 0)
+        assert int((ref > 0).sum()) == 1 + int(crossing) + int(want[1] == 1)
