@@ -300,8 +300,12 @@ AVSA_API size_t avsa_prefix_attn_workspace_bytes(int B, int H, int Hkv, int L, i
  *
  * avsa_cache_extend   room for count[k] more tokens (>= 0) in sequence seq[k]: new pages where its last one does not
  *                     hold them, length += count[k].
+ * avsa_cache_extend_step  the same, and granted[k] (int32 [n], apart from all other arrays; NULL: not wanted) becomes what entry k got: count[k], or 0
+                     where it was refused or left out.
  * avsa_cache_write    the last count[k] tokens of sequence seq[k] (seq NULL: k, count NULL: L) from k_new and v_new
  *                     [n,Hkv,L,d], of which they are the first count[k] (0..L), into the pages.  Tokens whose page is missing are left out.
+ *                   `count` is what avsa_cache_extend_step granted, wherever it may have refused something: a sequence that was refused has its old
+ *                   length, and the count that was asked for would replace its last tokens, which it may share with others.
  * avsa_cache_fork     sequence child[k], which has to be empty, becomes a copy of parent[k]: it shares the pages that are full, and the
  *                     contents of the one that is not are copied to a page of its own, in all planes of `pool`.
  * avsa_cache_free     sequence seq[k] gives its pages back and is empty (all that its row of the table names; `page` is not looked at).
@@ -310,6 +314,8 @@ AVSA_API size_t avsa_prefix_attn_workspace_bytes(int B, int H, int Hkv, int L, i
  * All need the workspace but avsa_cache_write, which has none and no status record.
  */
 AVSA_API int avsa_cache_extend(avsa_cache c, const int32_t* seq, const int32_t* count, int n, void* ws, size_t ws_bytes, void* stream);
+AVSA_API int avsa_cache_extend_step(avsa_cache c, const int32_t* seq, const int32_t* count, int n, int32_t* granted, void* ws, size_t ws_bytes,
+                                    void* stream);
 AVSA_API int avsa_cache_write(int n, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d k_new,
                               avsa_bf16_4d v_new, avsa_bf16_4d k_pool, avsa_bf16_4d v_pool, const int32_t* table,
                               const int32_t* length, const int32_t* seq, const int32_t* count, void* stream);

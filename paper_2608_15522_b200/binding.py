@@ -51,7 +51,8 @@ EXPORTS = (
     "avsa_protected_rows_attn", "avsa_protected_rows_attn_workspace_bytes",
     "avsa_cache_indicators", "avsa_cache_indicators_workspace_bytes",
     "avsa_prefix_attn", "avsa_prefix_attn_workspace_bytes",
-    "avsa_cache_extend", "avsa_cache_write", "avsa_cache_fork", "avsa_cache_free", "avsa_cache_compact", "avsa_cache_workspace_bytes",
+    "avsa_cache_extend", "avsa_cache_extend_step", "avsa_cache_write", "avsa_cache_fork", "avsa_cache_free", "avsa_cache_compact",
+    "avsa_cache_workspace_bytes",
     "avsa_count_from_percent", "avsa_read_status", "avsa_selftest_bounded_wait", "avsa_status_string", "avsa_version",
 )
 
@@ -130,7 +131,7 @@ def _cache():
     if _cache_module is None:
         lib = load_library()
         module = _extension("_avsa_cache")
-        entries = ("avsa_prefix_attn", "avsa_prefix_attn_workspace_bytes", "avsa_cache_extend", "avsa_cache_write", "avsa_cache_fork",
+        entries = ("avsa_prefix_attn", "avsa_prefix_attn_workspace_bytes", "avsa_cache_extend_step", "avsa_cache_write", "avsa_cache_fork",
                    "avsa_cache_free", "avsa_cache_compact", "avsa_cache_workspace_bytes")
         module.bind(*(ctypes.cast(getattr(lib, e), ctypes.c_void_p).value for e in entries),
                     getattr(torch._C, "_cuda_getCurrentRawStream", None))
@@ -177,6 +178,8 @@ def load_library() -> ctypes.CDLL:
     lib.avsa_prefix_attn_workspace_bytes.restype = sz
     lib.avsa_cache_extend.argtypes = [_Cache, vp, vp, i, vp, sz, vp]
     lib.avsa_cache_extend.restype = i
+    lib.avsa_cache_extend_step.argtypes = [_Cache, vp, vp, i, vp, vp, sz, vp]
+    lib.avsa_cache_extend_step.restype = i
     lib.avsa_cache_write.argtypes = [i, i, i, i, i, i, i, i, T, T, T, T, vp, vp, vp, vp, vp]
     lib.avsa_cache_write.restype = i
     lib.avsa_cache_fork.argtypes = [_Cache, _Pages, vp, vp, i, vp, sz, vp]
@@ -490,17 +493,20 @@ def avsa_cache_workspace_bytes(seqs, pages, n) -> int:
     return int(load_library().avsa_cache_workspace_bytes(seqs, pages, n))
 
 
-def avsa_cache_extend(table, length, ref, seq, count, page, out=None, ws=None):
+def avsa_cache_extend(table, length, ref, seq, count, page, out=None, ws=None, granted=None):
     """Room for count[k] more tokens in sequence seq[k].  out: (table, length, ref) that the state behind the call goes to (None: in place).
+    granted: int32 [n] that receives what each entry got, count[k] or 0; the count to write with wherever a pool may run out.
     Returns (table, length, ref, ws)."""
-    done = (_cache_module or _cache()).extend(table, length, ref, seq, count, page, *(out or (None, None, None)), ws)
+    done = (_cache_module or _cache()).extend(table, length, ref, seq, count, page, *(out or (None, None, None)), ws, granted)
     if done[0] != AVSA_OK:
         raise AvsaError(done[0], "avsa_cache_extend")
     return done[1:]
 
 
 def avsa_cache_write(k_new, v_new, k_pool, v_pool, table, length, seq=None, count=None):
-    """The first count[k] (None: all L) tokens of k_new/v_new [n,Hkv,L,d] become the last ones of sequence seq[k] (None: k)."""
+    """The first count[k] (None: all L) tokens of k_new/v_new [n,Hkv,L,d] become the last ones of sequence seq[k] (None: k).
+
+    Behind an extend that may have refused something, count is what it granted: what was asked for would replace old tokens."""
     st = (_cache_module or _cache()).write(k_new, v_new, k_pool, v_pool, table, length, seq, count)
     if st != AVSA_OK:
         raise AvsaError(st, "avsa_cache_write")

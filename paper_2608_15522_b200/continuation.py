@@ -11,6 +11,7 @@ can be handed on.  Of ``ClipCache`` only ``check`` waits for the GPU.
 from __future__ import annotations
 
 import argparse
+import inspect
 from typing import Optional, Sequence
 
 import torch
@@ -19,20 +20,23 @@ import torch
 class ClipCache:
     """Keys and values of up to ``seqs`` candidates of up to ``width`` pages each, for ``layers`` layers.
 
-    ``calls`` has the cache calls of ``binding`` (injectable, so that the sequencing can be exercised without a GPU).  Sequence numbers are
-    given as int32 tensors on the device, or as lists, which are copied there.
+    ``calls`` has the cache calls of ``binding`` (injectable, so that the sequencing can be exercised without a GPU; a stand-in whose extend takes no
+    ``granted`` is taken to grant everything).  Sequence numbers are given as int32 tensors on the device, or as lists, which are copied there.
+
+    A sequence that cannot have its pages is left as it was: a step writes nothing to it, and ``check`` says so.
     """
 
     def __init__(self, layers: int, heads: int, d: int, page: int, pages: int, seqs: int, width: int, device="cuda", calls=None):
         if calls is None:
             from . import binding as calls
         self.calls, self.layers, self.page = calls, layers, page
+        self._grants = "granted" in inspect.signature(calls.avsa_cache_extend).parameters
         # plane 2i: keys of layer i, plane 2i + 1: its values (what no token has been written to is never used)
         self.pool = torch.empty((2 * layers, pages, heads, page, d), dtype=torch.bfloat16, device=device)
         self.table = torch.full((seqs, width), -1, dtype=torch.int32, device=device)
         self.length = torch.zeros(seqs, dtype=torch.int32, device=device)
         self.ref = torch.zeros(pages, dtype=torch.int32, device=device)
-        self._step = None          # sequences and counts of the step under way
+        self._step = None          # sequences of the step under way, and the tokens that each of them was granted
         self._ws = {}              # the last call's workspace, by kind: its status record is read by check()
 
     def ints(self, x) -> torch.Tensor:
@@ -44,8 +48,9 @@ class ClipCache:
     def begin_step(self, seq: Sequence[int], count: Sequence[int]) -> None:
         """Room for count[k] more tokens in sequence seq[k]; ``attend`` then writes and attends, layer by layer."""
         seq, count = self.ints(seq), self.ints(count)
-        self._ws["extend"] = self.calls.avsa_cache_extend(*self._state(), seq, count, self.page)[3]
-        self._step = (seq, count)
+        granted = {"granted": torch.empty_like(count)} if self._grants else {}
+        self._ws["extend"] = self.calls.avsa_cache_extend(*self._state(), seq, count, self.page, **granted)[3]
+        self._step = (seq, granted.get("granted", count))
 
     def attend(self, layer: int, q, k_new, v_new, prefix_pages: int = 0, causal: bool = False, softmax_scale: float = 0.0):
         """One layer of the step: k_new/v_new [n,Hkv,L,d] go into the pages, q [n,H,L,d] attends to all tokens of its sequence (causal: up to its

@@ -14,7 +14,7 @@ namespace {
 
 decltype(&avsa_prefix_attn) f_attn;
 decltype(&avsa_prefix_attn_workspace_bytes) f_attn_ws;
-decltype(&avsa_cache_extend) f_extend;
+decltype(&avsa_cache_extend_step) f_extend;
 decltype(&avsa_cache_write) f_write;
 decltype(&avsa_cache_fork) f_fork;
 decltype(&avsa_cache_free) f_free;
@@ -239,21 +239,23 @@ int list_size(const Arg& x, const Arg& y, const char* text) {
   return static_cast<int>(x.numel);
 }
 
-// extend(table, length, ref, seq, count, page, table_out, length_out, ref_out, ws) -> (status, table, length, ref, ws)
+// extend(table, length, ref, seq, count, page, table_out, length_out, ref_out, ws, granted) -> (status, table, length, ref, ws)
 PyObject* py_extend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  arity(n, 10);
+  arity(n, 11);
   Call c{a};
   const State s(c, 0, 6);
   const Arg seq = c.ints(3, "seq", 1), count = c.ints(4, "count", 1);
   const int entries = list_size(seq, count, "seq and count have different lengths");
   const avsa_cache cache = s.cache(c.integer(5, "page"));
   Arg ws = c.plain(9, "ws", at::kByte, 1, true);
+  const Arg granted = c.ints(10, "granted", 1, true);
+  TORCH_CHECK_VALUE(!granted.there() || granted.numel == entries, "granted: one entry for each of seq");
   c.find_stream();
   int st;
   without_lock([&] {
     if (!ws.there()) c.make_ws(ws, f_ws(cache.seqs, cache.pages, entries));
-    st = f_extend(cache, seq.as<int32_t>(), count.as<int32_t>(), entries, ws.ptr, static_cast<size_t>(ws.numel), c.stream);
+    st = f_extend(cache, seq.as<int32_t>(), count.as<int32_t>(), entries, granted.as<int32_t>(), ws.ptr, static_cast<size_t>(ws.numel), c.stream);
   });
   return result(st, {wrap(s.table_out), wrap(s.length_out), wrap(s.ref_out), c.give(9, ws)});
   END_HANDLE_TH_ERRORS

@@ -66,6 +66,7 @@ struct MetaArgs {
   const int32_t* other;     // extend: count; fork: parent
   int n;
   int32_t* n_live;
+  int32_t* granted;         // extend: [n], or NULL
 };
 
 __device__ __forceinline__ int cluster_rank() {
@@ -328,6 +329,7 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
     auto free_page = [&](int at) { return alone ? free_pages[at] : __ldcg(&free_pages[at]); };
     const bool refused = s >= 0 && need > 0 && first + need > n_free;
     if (refused && lane == 0) report_status(w.status, AVSA_ERR_NO_PAGES, kCacheFull, k, s);
+    if (OP == kExtend && lane == 0 && a.granted != nullptr) a.granted[k] = s < 0 || refused ? 0 : new_tokens;
     if (OP == kFork && lane == 0 && (s < 0 || refused || need == 0)) w.moves[k] = make_int4(-1, -1, 0, 0);
     if (s < 0 || refused) continue;
     int32_t* row = c.table_out + static_cast<long long>(s) * c.width;
@@ -617,6 +619,12 @@ static int check_cache(const avsa_cache& c, bool by_page) {
   }
   return AVSA_OK;
 }
+// An output of n ints shares nothing with the state that the call reads or writes.
+static bool apart_from_state(const avsa_cache& c, const int32_t* p, long long n) {
+  const long long entries = static_cast<long long>(c.seqs) * c.width;
+  return apart(p, n, c.table, entries) && apart(p, n, c.table_out, entries) && apart(p, n, c.length, c.seqs) && apart(p, n, c.length_out, c.seqs) &&
+         apart(p, n, c.ref, c.pages) && apart(p, n, c.ref_out, c.pages);
+}
 static int check_list(const avsa_cache& c, const int32_t* a, const int32_t* b, int n, const void* ws, size_t ws_bytes,
                       bool by_page = true) {
   const int st = check_cache(c, by_page);
@@ -671,13 +679,21 @@ extern "C" size_t avsa_cache_workspace_bytes(int seqs, int pages, int n) {
   return CacheWs::bytes(seqs, pages, n);
 }
 
-extern "C" int avsa_cache_extend(avsa_cache c, const int32_t* seq, const int32_t* count, int n, void* ws, size_t ws_bytes, void* stream) {
+extern "C" int avsa_cache_extend_step(avsa_cache c, const int32_t* seq, const int32_t* count, int n, int32_t* granted, void* ws, size_t ws_bytes,
+                                      void* stream) {
   const int st = check_list(c, seq, count, n, ws, ws_bytes);
   if (st != AVSA_OK) return st;
+  if (granted != nullptr) {
+    if (!aligned4(granted) || !apart_from_state(c, granted, n) || !apart(granted, n, seq, n) || !apart(granted, n, count, n)) return AVSA_ERR_INVALID_ARG;
+  }
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
-  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), seq, count, n, nullptr};
+  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), seq, count, n, nullptr, granted};
   if (launch_meta(assign_pages_kernel<kExtend>, a, as_stream(stream), AssignSmem(c, n).bytes, kAssignMost) != cudaSuccess) return AVSA_ERR_CUDA;
   return done();
+}
+
+extern "C" int avsa_cache_extend(avsa_cache c, const int32_t* seq, const int32_t* count, int n, void* ws, size_t ws_bytes, void* stream) {
+  return avsa_cache_extend_step(c, seq, count, n, nullptr, ws, ws_bytes, stream);
 }
 
 extern "C" int avsa_cache_fork(avsa_cache c, avsa_pages pool, const int32_t* parent, const int32_t* child, int n, void* ws, size_t ws_bytes,
@@ -686,7 +702,7 @@ extern "C" int avsa_cache_fork(avsa_cache c, avsa_pages pool, const int32_t* par
   if (st == AVSA_OK) st = check_pool(pool, c.pages);
   if (st != AVSA_OK) return st;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
-  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), child, parent, n, nullptr};
+  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), child, parent, n, nullptr, nullptr};
   if (launch_meta(assign_pages_kernel<kFork>, a, as_stream(stream), AssignSmem(c, n).bytes, kAssignMost) != cudaSuccess) return AVSA_ERR_CUDA;
   if (n > 0) {
     CopyArgs m = {};
@@ -703,7 +719,7 @@ extern "C" int avsa_cache_free(avsa_cache c, const int32_t* seq, int n, void* ws
   const int st = check_list(c, seq, seq, n, ws, ws_bytes, false);
   if (st != AVSA_OK) return st;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
-  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), seq, nullptr, n, nullptr};
+  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), seq, nullptr, n, nullptr, nullptr};
   if (launch_meta(free_pages_kernel, a, as_stream(stream)) != cudaSuccess) return AVSA_ERR_CUDA;
   return done();
 }
@@ -714,7 +730,7 @@ extern "C" int avsa_cache_compact(avsa_cache c, avsa_pages pool, int32_t* n_live
   if (st != AVSA_OK) return st;
   if (n_live == nullptr || !aligned4(n_live)) return AVSA_ERR_INVALID_ARG;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
-  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, 0), nullptr, nullptr, 0, n_live};
+  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, 0), nullptr, nullptr, 0, n_live, nullptr};
   if (launch_meta(plan_compaction_kernel, a, as_stream(stream), most_moves(c) * kMoveBytes, kPlanMost) != cudaSuccess) return AVSA_ERR_CUDA;
   CopyArgs m = {};
   m.pool = pool;
