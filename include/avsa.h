@@ -275,6 +275,11 @@ AVSA_API int avsa_build_block_mask_static(int B, int H, int N, int d, int blk, a
  * lim = length[s], or with AVSA_CAUSAL lim = length[s] - L + i + 1: the L queries are the last L tokens of the
  * sequence.  Rows with lim <= 0, and all rows of a batch entry with seq[b] < 0, are empty: o = 0, lse = -inf.
  *
+ * avsa_prefix_attn_step  the same for a step in which the sequences got different numbers of tokens: with AVSA_CAUSAL the first count[b] (int32 [B],
+ *                   0..L; NULL: L) of the L queries are the last count[b] tokens of their sequence, lim = length[s] - count[b] + i + 1, and the rows
+ *                   behind them are empty.  Without AVSA_CAUSAL all L queries see all tokens.  A count out of range sets AVSA_ERR_BAD_TABLE
+ *                   and is cut; it says that not all tokens of the step were written.
+ *
  *   k_pool, v_pool  [pages,Hkv,page,d]: stride_b is the distance of pages, stride_h of heads, stride_n of tokens
  *   prefix_pages    the first prefix_pages pages of all sequences of the batch are the same ones (of a shorter
  *                   sequence: all it has).  Where it costs less they are read once for the whole batch, all its queries stacked on
@@ -291,6 +296,10 @@ AVSA_API int avsa_prefix_attn(int B, int H, int Hkv, int L, int d, int page, int
                               avsa_bf16_4d k_pool, avsa_bf16_4d v_pool, const int32_t* table, const int32_t* length,
                               const int32_t* seq, int prefix_pages, unsigned flags, float softmax_scale, void* o_bf16, float* lse,
                               void* ws, size_t ws_bytes, void* stream);
+AVSA_API int avsa_prefix_attn_step(int B, int H, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d q,
+                                   avsa_bf16_4d k_pool, avsa_bf16_4d v_pool, const int32_t* table, const int32_t* length,
+                                   const int32_t* seq, const int32_t* count, int prefix_pages, unsigned flags, float softmax_scale,
+                                   void* o_bf16, float* lse, void* ws, size_t ws_bytes, void* stream);
 AVSA_API size_t avsa_prefix_attn_workspace_bytes(int B, int H, int Hkv, int L, int d, int page, int width, int prefix_pages);
 
 /*

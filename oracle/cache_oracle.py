@@ -107,23 +107,24 @@ def compact(table, ref):
     return np.where(table >= 0, place[np.maximum(table, 0)], -1).astype(table.dtype), new.astype(ref.dtype), n, list(zip(used, holes))
 
 
-def limits(length, seq, B, L, causal):
-    """[B,L]: how many of its sequence's tokens a row sees."""
+def limits(length, seq, B, L, causal, count=None):
+    """[B,L]: how many of its sequence's tokens a row sees.  count [B]: the first count[b] rows are the sequence's last tokens (None: all L)."""
     out = np.zeros((B, L), np.int64)
     for b in range(B):
         s = int(seq[b])
         if s >= 0:
-            out[b] = np.maximum(0, length[s] - L + 1 + np.arange(L)) if causal else length[s]
+            n, i = L if count is None else int(count[b]), np.arange(L)
+            out[b] = np.where(i < n, np.maximum(0, length[s] - n + 1 + i), 0) if causal else length[s]
     return out
 
 
-def prefix_attention(q, k_pool, v_pool, table, length, seq=None, causal=False, scale=None):
+def prefix_attention(q, k_pool, v_pool, table, length, seq=None, causal=False, scale=None, count=None):
     """q [B,H,L,d], pools [pages,Hkv,page,d] in fp64 -> (o, lse); an empty row is 0 and -inf."""
     B, H, L, d = q.shape
     Hkv, page = k_pool.shape[1:3]
     seq = np.arange(B) if seq is None else seq
     scale = scale or 1.0 / np.sqrt(d)
-    lim = limits(length, seq, B, L, causal)
+    lim = limits(length, seq, B, L, causal, count)
     o, lse = np.zeros((B, H, L, d)), np.full((B, H, L), -np.inf)
     for b in range(B):
         n = int(length[seq[b]]) if seq[b] >= 0 else 0

@@ -50,7 +50,7 @@ EXPORTS = (
     "avsa_sparse_self_attn", "avsa_sparse_self_attn_workspace_bytes",
     "avsa_protected_rows_attn", "avsa_protected_rows_attn_workspace_bytes",
     "avsa_cache_indicators", "avsa_cache_indicators_workspace_bytes",
-    "avsa_prefix_attn", "avsa_prefix_attn_workspace_bytes",
+    "avsa_prefix_attn", "avsa_prefix_attn_step", "avsa_prefix_attn_workspace_bytes",
     "avsa_cache_extend", "avsa_cache_extend_step", "avsa_cache_write", "avsa_cache_fork", "avsa_cache_free", "avsa_cache_compact",
     "avsa_cache_workspace_bytes",
     "avsa_count_from_percent", "avsa_read_status", "avsa_selftest_bounded_wait", "avsa_status_string", "avsa_version",
@@ -131,7 +131,7 @@ def _cache():
     if _cache_module is None:
         lib = load_library()
         module = _extension("_avsa_cache")
-        entries = ("avsa_prefix_attn", "avsa_prefix_attn_workspace_bytes", "avsa_cache_extend_step", "avsa_cache_write", "avsa_cache_fork",
+        entries = ("avsa_prefix_attn_step", "avsa_prefix_attn_workspace_bytes", "avsa_cache_extend_step", "avsa_cache_write", "avsa_cache_fork",
                    "avsa_cache_free", "avsa_cache_compact", "avsa_cache_workspace_bytes")
         module.bind(*(ctypes.cast(getattr(lib, e), ctypes.c_void_p).value for e in entries),
                     getattr(torch._C, "_cuda_getCurrentRawStream", None))
@@ -174,6 +174,8 @@ def load_library() -> ctypes.CDLL:
     lib.avsa_cache_indicators_workspace_bytes.restype = sz
     lib.avsa_prefix_attn.argtypes = [i, i, i, i, i, i, i, i, i, T, T, T, vp, vp, vp, i, u, f, vp, vp, vp, sz, vp]
     lib.avsa_prefix_attn.restype = i
+    lib.avsa_prefix_attn_step.argtypes = [i, i, i, i, i, i, i, i, i, T, T, T, vp, vp, vp, vp, i, u, f, vp, vp, vp, sz, vp]
+    lib.avsa_prefix_attn_step.restype = i
     lib.avsa_prefix_attn_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
     lib.avsa_prefix_attn_workspace_bytes.restype = sz
     lib.avsa_cache_extend.argtypes = [_Cache, vp, vp, i, vp, sz, vp]
@@ -478,12 +480,12 @@ def avsa_prefix_attn_workspace_bytes(B, H, Hkv, L, d, page, width, prefix_pages)
 
 
 def avsa_prefix_attn(q, k_pool, v_pool, table, length, prefix_pages=0, seq=None, causal=False, softmax_scale=0.0, want_lse=False,
-                     o=None, lse=None, ws=None):
+                     o=None, lse=None, ws=None, count=None):
     """Attention of q [B,H,L,d] to the paged sequences seq (None: 0 .. B-1), whose first prefix_pages pages are the same ones.
 
     k_pool/v_pool [pages,Hkv,page,d] bf16, table [seqs,width] and length [seqs] int32.  causal: the queries are the last L tokens of
-    their sequence.  Returns (o, lse or None, ws)."""
-    done = (_cache_module or _cache()).attn(q, k_pool, v_pool, table, length, prefix_pages, seq, causal, softmax_scale, want_lse, o, lse, ws)
+    their sequence, or with count int32 [B] the first count[b] of them its last count[b] tokens, and the rows behind are empty.  Returns (o, lse or None, ws)."""
+    done = (_cache_module or _cache()).attn(q, k_pool, v_pool, table, length, prefix_pages, seq, causal, softmax_scale, want_lse, o, lse, ws, count)
     if done[0] != AVSA_OK:
         raise AvsaError(done[0], "avsa_prefix_attn")
     return done[1:]

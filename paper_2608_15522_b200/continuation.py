@@ -21,7 +21,7 @@ class ClipCache:
     """Keys and values of up to ``seqs`` candidates of up to ``width`` pages each, for ``layers`` layers.
 
     ``calls`` has the cache calls of ``binding`` (injectable, so that the sequencing can be exercised without a GPU; a stand-in whose extend takes no
-    ``granted`` is taken to grant everything).  Sequence numbers are given as int32 tensors on the device, or as lists, which are copied there.
+    ``granted`` is taken to grant everything, one whose attention takes no ``count`` gets full steps only).  Sequence numbers are given as int32 tensors on the device, or as lists, which are copied there.
 
     A sequence that cannot have its pages is left as it was: a step writes nothing to it, and ``check`` says so.
     """
@@ -30,7 +30,8 @@ class ClipCache:
         if calls is None:
             from . import binding as calls
         self.calls, self.layers, self.page = calls, layers, page
-        self._grants = "granted" in inspect.signature(calls.avsa_cache_extend).parameters
+        takes = lambda call, name: name in inspect.signature(call).parameters
+        self._grants, self._counts = takes(calls.avsa_cache_extend, "granted"), takes(calls.avsa_prefix_attn, "count")
         # plane 2i: keys of layer i, plane 2i + 1: its values (what no token has been written to is never used)
         self.pool = torch.empty((2 * layers, pages, heads, page, d), dtype=torch.bfloat16, device=device)
         self.table = torch.full((seqs, width), -1, dtype=torch.int32, device=device)
@@ -53,15 +54,17 @@ class ClipCache:
         self._step = (seq, granted.get("granted", count))
 
     def attend(self, layer: int, q, k_new, v_new, prefix_pages: int = 0, causal: bool = False, softmax_scale: float = 0.0):
-        """One layer of the step: k_new/v_new [n,Hkv,L,d] go into the pages, q [n,H,L,d] attends to all tokens of its sequence (causal: up to its
-        own).  The first prefix_pages pages of the step's sequences are the same ones.  Returns o."""
+        """One layer of the step: the first count[k] of the L tokens of k_new/v_new [n,Hkv,L,d] go into the pages, q [n,H,L,d] attends to all tokens of its
+        sequence (causal: up to its own, and rows behind the first count[k] are zero).  The first prefix_pages pages of the step's sequences are the same
+        ones.  Returns o."""
         if self._step is None:
             raise ValueError("begin_step first")
         seq, count = self._step
         k, v = self.pool[2 * layer], self.pool[2 * layer + 1]
         self.calls.avsa_cache_write(k_new, v_new, k, v, self.table, self.length, seq, count)
+        more = {"count": count} if self._counts else {}
         o, _, self._ws["attention"] = self.calls.avsa_prefix_attn(q, k, v, self.table, self.length, prefix_pages=prefix_pages, seq=seq, causal=causal,
-                                                                 softmax_scale=softmax_scale)
+                                                                 softmax_scale=softmax_scale, **more)
         return o
 
     def branch(self, parent: Sequence[int], child: Sequence[int]) -> None:

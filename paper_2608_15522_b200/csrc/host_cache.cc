@@ -12,7 +12,7 @@
 
 namespace {
 
-decltype(&avsa_prefix_attn) f_attn;
+decltype(&avsa_prefix_attn_step) f_attn;
 decltype(&avsa_prefix_attn_workspace_bytes) f_attn_ws;
 decltype(&avsa_cache_extend_step) f_extend;
 decltype(&avsa_cache_write) f_write;
@@ -153,10 +153,10 @@ void arity(Py_ssize_t got, Py_ssize_t want) {
   TORCH_CHECK_TYPE(got == want && f_attn != nullptr, "wrong number of arguments, or bind() has not been called");
 }
 
-// attn(q, k_pool, v_pool, table, length, prefix_pages, seq, causal, softmax_scale, want_lse, o, lse, ws) -> (status, o, lse, ws)
+// attn(q, k_pool, v_pool, table, length, prefix_pages, seq, causal, softmax_scale, want_lse, o, lse, ws, count) -> (status, o, lse, ws)
 PyObject* py_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  arity(n, 13);
+  arity(n, 14);
   Call c{a};
   const View q = take_view(c, 0, "q"), k = take_view(c, 1, "k_pool"), v = take_view(c, 2, "v_pool");
   const Arg table = c.ints(3, "table", 2), length = c.ints(4, "length", 1);
@@ -183,6 +183,8 @@ PyObject* py_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     TORCH_CHECK_VALUE(!lse.there() || lse.numel == static_cast<int64_t>(B) * H * L, "lse: expected [B,H,L]");
   }
   Arg ws = c.plain(12, "ws", at::kByte, 1, true);
+  const Arg count = c.ints(13, "count", 1, true);
+  TORCH_CHECK_VALUE(!count.there() || count.numel == B, "count: one entry for each batch entry of q");
   c.find_stream();
   int st;
   without_lock([&] {
@@ -192,8 +194,8 @@ PyObject* py_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     if (want_lse) c.make(lse, at::kFloat, {B, H, L});
     if (!ws.there()) c.make_ws(ws, f_attn_ws(B, H, Hkv, L, d, page, width, prefix_pages));
-    st = f_attn(B, H, Hkv, L, d, page, pages, seqs, width, q, k, v, table.as<int32_t>(), length.as<int32_t>(), seq.as<int32_t>(), prefix_pages,
-                causal ? AVSA_CAUSAL : 0u, scale, o.ptr, lse.as<float>(), ws.ptr, static_cast<size_t>(ws.numel), c.stream);
+    st = f_attn(B, H, Hkv, L, d, page, pages, seqs, width, q, k, v, table.as<int32_t>(), length.as<int32_t>(), seq.as<int32_t>(),
+                count.as<int32_t>(), prefix_pages, causal ? AVSA_CAUSAL : 0u, scale, o.ptr, lse.as<float>(), ws.ptr, static_cast<size_t>(ws.numel), c.stream);
   });
   return result(st, {c.give(10, o), c.give(11, lse), c.give(12, ws)});
   END_HANDLE_TH_ERRORS

@@ -41,7 +41,7 @@ constexpr int kPxConsumers = 4 + kPxQWarps + 8;      // warps that read the item
 
 enum PrefixWhere {
   kPrefixPage = 221, kPrefixLength, kPrefixSeq, kPxItem, kPxItemEmpty, kPxQEmpty, kPxQFull, kPxKEmpty, kPxVEmpty, kPxKFull, kPxVFull, kPxSFull, kPxSFree,
-  kPxPFull, kPxPFree, kPxOFull, kPxOFree, kPxMref, kPxLsum, kPxAlign
+  kPxPFull, kPxPFree, kPxOFull, kPxOFree, kPxMref, kPxLsum, kPxAlign, kPrefixCount
 };
 
 // A divisor known on the host: n / d for 0 <= n < 2^31 without a division (which is 30 dependent instructions).
@@ -88,6 +88,7 @@ struct PrefixParams {
   __nv_bfloat16* o;
   float* lse;
   const int32_t *table, *length, *seq;
+  const int32_t* count;        // queries of a batch entry, or NULL: L
   float scale_log2;
   // workspace
   StatusRecord* status;
@@ -145,13 +146,28 @@ __device__ __forceinline__ int prefix_sequence(const PrefixParams& p, int b, int
   if (slot < 0) return 0;
   const int n = p.length[slot], most = p.s.width << p.s.page_shift;
   if (n < 0 || n > most) bad = kPrefixLength;
+  if (p.count != nullptr && (p.count[b] < 0 || p.count[b] > p.s.L)) bad = kPrefixCount;
   return n < 0 ? 0 : n > most ? most : n;
 }
-// Key tiles of an own item: row tile rt of a sequence of n tokens.
-__device__ __forceinline__ int prefix_own_tiles(const PrefixShape& s, int n, int rt) {
+// Queries of a batch entry that are tokens of its sequence, its last ones.
+__device__ __forceinline__ int prefix_queries(const PrefixParams& p, int b) {
+  return p.count != nullptr ? min(max(p.count[b], 0), p.s.L) : p.s.L;
+}
+// How many of the n tokens of its sequence query i of batch entry b sees (less than one: none).
+__device__ __forceinline__ int prefix_limit(const PrefixParams& p, int b, int n, int i) {
+  if (!p.s.causal) return n;
+  const int q = prefix_queries(p, b);
+  return i < q ? n - q + i + 1 : 0;
+}
+// Key tiles of an own item: row tile rt of batch entry b, whose sequence has n tokens.
+__device__ __forceinline__ int prefix_own_tiles(const PrefixParams& p, int b, int n, int rt) {
+  const PrefixShape& s = p.s;
   if (s.own_off) return 0;
   int end = n;
-  if (s.causal) end = n - s.L + min(s.L - 1, s.by_G.div(rt * 128 + 127)) + 1;
+  if (s.causal) {
+    const int q = prefix_queries(p, b);
+    end = s.by_G.div(rt * 128) < q ? n - q + min(q, s.by_G.div(rt * 128 + 127) + 1) : 0;
+  }
   const int x = end - s.k0;
   const int t = x > 0 ? (x + 127) >> 7 : 0;
   return s.stack ? t : max(t, 1);      // (without a beginning of its own every row tile is written by somebody)
@@ -487,7 +503,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
         int bad;
         len = prefix_sequence(p, b, slot, bad);
         if (bad && blockIdx.x == 0) report(AVSA_ERR_BAD_TABLE, bad, b, slot);
-        nt = prefix_own_tiles(S, len, f - b * S.TO);
+        nt = prefix_own_tiles(p, b, len, f - b * S.TO);
       }
     };
     auto scan = [&](int v) {      // of the lanes up to this one
@@ -908,7 +924,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
         }
         i = S.by_G.div(rr);
         g = rr - i * S.G;
-        rel = min(it.kv_end, S.causal ? len - S.L + i + 1 : len) - it.pos0;
+        rel = min(it.kv_end, prefix_limit(p, b, len, i)) - it.pos0;
       }
       float m_ref = run == 2 ? m_given : 0.f, m_max = -INFINITY;
       uint64_t sum2[4] = {0ull, 0ull, 0ull, 0ull};
@@ -1209,7 +1225,7 @@ __global__ void __launch_bounds__(kPxMergeThreads) prefix_merge_kernel(const __g
       row.step = S.chunk * 128;
       row.n_first = g1 - g0 + 1;
     }
-    if (prefix_own_tiles(S, len, own) > 0) {
+    if (prefix_own_tiles(p, b, len, own) > 0) {
       // (a kernel that gave up, for a wait that ran out, may have left records unwritten)
       if (rec.x < 0 || rec.y < 1 || (rec.y > 1 && rec.x > p.plan[2] - rec.y)) rec = make_int2(0, 0);
       row.n_second = rec.y;

@@ -275,7 +275,7 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
   if (lane < rows) {
     int b, i, head, len;
     row_of(lane, b, i, head, len);
-    rel = S.causal ? len - S.L + i + 1 : len;
+    rel = prefix_limit(p, b, len, i);
   }
   const int rel_min = __reduce_min_sync(FULLM, rel);
   k1 = min(k1, __reduce_max_sync(FULLM, lane < rows ? rel : 0));

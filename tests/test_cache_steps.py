@@ -8,9 +8,9 @@ import torch
 from oracle import cache_oracle as orc
 from paper_2608_15522_b200 import binding as av
 from paper_2608_15522_b200.continuation import ClipCache
-from parity_bars import close_o
+from parity_bars import close_lse, close_o
 from test_continuation import OracleCalls
-from test_paged_cache import SIZES, cu, ints, nump, random_state, status
+from test_paged_cache import SIZES, attention_case, cu, ints, lengths_behind, nump, random_state, status
 
 gpu = pytest.mark.gpu
 
@@ -22,6 +22,11 @@ class StepCalls(OracleCalls):
         refused = orc.extend(table.numpy(), length.numpy(), ref.numpy(), seq.tolist(), count.tolist(), page)[3]
         granted.copy_(torch.tensor(granted_of(seq.tolist(), count.tolist(), refused)))
         return super().avsa_cache_extend(table, length, ref, seq, count, page)
+
+    def avsa_prefix_attn(self, q, k, v, table, length, prefix_pages=0, seq=None, causal=False, softmax_scale=0.0, count=None):
+        f64 = lambda t: t.double().numpy()
+        o, lse = orc.prefix_attention(f64(q), f64(k), f64(v), table.numpy(), length.numpy(), seq.tolist(), causal, softmax_scale or None, count.tolist())
+        return torch.from_numpy(o).bfloat16(), None, av.AVSA_OK
 
 
 def granted_of(seq, count, refused):
@@ -113,3 +118,134 @@ def test_wrapper_refuses_another_number_of_granted_entries():
         av.avsa_cache_extend(ints([[0, 0]] * 4), i, ints([0] * 5), ints([0, 1]), ints([1, 1]), 16, granted=ints([0]))
     with pytest.raises(ValueError, match="granted"):
         av.avsa_cache_extend(ints([[0, 0]] * 4), i, ints([0] * 5), ints([0, 1]), ints([1, 1]), 16, granted=torch.zeros(2, device="cuda"))
+
+
+# ------------------------------------------------------------------------------------------------ different numbers of tokens
+def test_oracle_counts_closed_forms():
+    """Two sequences, three queries each, of which the second one has two."""
+    assert orc.limits(np.array([3, 2, 9]), [0, 1, 2], 3, 3, True, [3, 2, 0]).tolist() == [[1, 2, 3], [1, 2, 0], [0, 0, 0]]
+    assert orc.limits(np.array([5, 2]), [0, 1], 2, 3, True, [2, 3]).tolist() == [[4, 5, 0], [0, 1, 2]]
+    assert orc.limits(np.array([5, 2]), [0, 1], 2, 3, False, [2, 3]).tolist() == [[5] * 3, [2] * 3]
+
+
+@pytest.mark.parametrize("where", WHERE)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("H,Hkv,L,shared", [(1, 1, 3, 0), (4, 2, 5, 2), (2, 2, 40, 2), (6, 2, 23, 0)])
+def test_a_ragged_step(where, H, Hkv, L, shared, causal):
+    """Sequences of a step get none, one, some and all of its tokens: what each of them adds sees the tokens up to itself."""
+    page, d, n = 16, 64, 5
+    cache = clip_cache(where, 1, Hkv, d, page, 80, n, 12)
+    gen = torch.Generator().manual_seed(L)
+    draw = lambda h, n, L: torch.randn((n, h, L, d), generator=gen).bfloat16()
+    kept = [torch.zeros((2, Hkv, 0, d), dtype=torch.bfloat16)] * n
+
+    def step(seq, count, L, shared):
+        q, k, v = draw(H, len(seq), L), draw(Hkv, len(seq), L), draw(Hkv, len(seq), L)
+        cache.begin_step(seq, count)
+        o = cache.attend(0, *(x.to(where) for x in (q, k, v)), shared, causal).cpu()
+        for b, (s, c) in enumerate(zip(seq, count)):
+            kept[s] = torch.cat([kept[s], torch.stack([k[b, :, :c], v[b, :, :c]])], 2)
+            all_ = kept[s].shape[2]
+            lim = [all_ - c + i + 1 if i < c else 0 for i in range(L)] if causal else [all_] * L
+            want = plain_rows(q[b], *kept[s], lim)
+            empty = torch.tensor(lim) == 0
+            assert (o[b][:, empty] == 0).all()
+            if not empty.all():
+                close_o(o[b][:, ~empty].double().numpy(), want[:, ~empty].numpy(), f"sequence {s}")
+
+    if shared:
+        step([0], [shared * page], shared * page, 0)
+        cache.branch([0] * (n - 1), list(range(1, n)))
+        kept[1:] = [kept[0]] * (n - 1)
+    step([2, 0, 4, 1, 3], [L, L - 1, 0, 1, (L + 1) // 2], L, shared)
+    step([4, 1, 0], [L // 2, L, 1], L, shared)
+    step([3, 2, 1, 0, 4], [1] * 5, 1, shared)
+    cache.check()
+
+
+def exact_counts(q, k, v, table, length, count, causal):
+    """orc.prefix_attention in 64 bits on the GPU."""
+    B, H, L, d = q.shape
+    page, group = k.shape[2], H // k.shape[1]
+    lim = orc.limits(length, range(B), B, L, causal, count)
+    o, lse = torch.zeros((B, H, L, d), dtype=torch.float64, device="cuda"), torch.full((B, H, L), -float("inf"), dtype=torch.float64, device="cuda")
+    for b in range(B):
+        n = int(length[b])
+        if n == 0:
+            continue
+        at = torch.arange(n, device="cuda")
+        pages = cu(table)[b].long()[at // page]
+        kk, vv = (x[pages, :, at % page].double().transpose(0, 1) for x in (k, v))
+        x = q[b].double().reshape(-1, group * L, d) @ kk.transpose(1, 2) * d ** -0.5
+        x.masked_fill_(at >= cu(lim[b]).repeat(group)[:, None], -float("inf"))
+        z = torch.logsumexp(x, 2)
+        o[b], lse[b] = (torch.exp(x - torch.where(torch.isinf(z), 0.0, z)[..., None]) @ vv).reshape(H, L, d), z.reshape(H, L)
+    return o, lse
+
+
+WAYS = [(1, 3, 8, 2, 16, 0, (6400,)),                        # parts that another kernel joins
+        (3, 5, 24, 24, 16, 0, (900, 0, 17)),                 # a cluster of CTAs an item
+        (8, 2, 16, 16, 32, 2048, 300),                       # the beginning by the stream kernel: 16 stacked rows
+        (4, 7, 24, 24, 64, 4096, 90),                        # 28
+        (12, 10, 24, 8, 32, 4096, 200),                      # the beginning by the tile kernel, own keys by warps
+        (12, 20, 8, 2, 32, 16384, 400),                      # the tile kernel for both
+        (9, 50, 24, 8, 64, 16384, 333),                      # two row tiles of own rows, gathered
+        (1, 700, 32, 32, 64, 0, (3000,)),                    # whole items off a queue, the last ones cut
+        (3, 509, 32, 8, 64, 0, (509, 3000, 1754)),
+        (2, 300, 6, 6, 16, 0, (2000, 299))]                  # fewer items than SMs
+
+
+@gpu
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,L,H,Hkv,page,tokens,most", WAYS)
+def test_attention_of_counts(B, L, H, Hkv, page, tokens, most, d, causal):
+    """Every way that the work is cut; with the full count the bits of the call without one."""
+    rng = random.Random(B + d)
+    shared = tokens // page
+    lengths = list(most) if isinstance(most, tuple) else lengths_behind(rng, B, shared, page, most)
+    q, k, v, table, length = attention_case(B, H, Hkv, L, d, page, lengths, shared=shared, seed=B, q_layout="blhd")
+    call = lambda count: av.avsa_prefix_attn(q, k, v, cu(table), cu(length), prefix_pages=shared, causal=causal, want_lse=True, count=count)
+    plain, full = call(None), call(ints([L] * B))
+    assert torch.equal(plain[0], full[0]) and torch.equal(plain[1], full[1])
+    for counts in ([rng.randint(0, L) for _ in range(B)], [(0, 1, L - 1)[(b + 1) % 3] for b in range(B)], [min(L, L // 3 + 1)] * B):
+        o, lse, ws = call(ints(counts))
+        assert status(ws) == av.AVSA_OK
+        if not causal:
+            assert torch.equal(o, plain[0]) and torch.equal(lse, plain[1])
+            continue
+        want, want_lse = exact_counts(q, k, v, table, length, counts, causal)
+        empty = torch.isinf(want_lse)
+        assert torch.equal(torch.isinf(lse), empty) and (o[empty] == 0).all(), counts
+        if not empty.all():
+            close_o(o.double()[~empty].cpu().numpy(), want[~empty].cpu().numpy(), counts)
+            close_lse(lse.double()[~empty].cpu().numpy(), want_lse[~empty].cpu().numpy(), counts)
+
+
+@gpu
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("B,L,H,Hkv,page,tokens,most", WAYS)
+def test_counts_out_of_range_are_reported(B, L, H, Hkv, page, tokens, most, causal):
+    """More queries than there are, or less than none: reported, and cut."""
+    shared = tokens // page
+    lengths = list(most) if isinstance(most, tuple) else [tokens + most] * B
+    q, k, v, table, length = attention_case(B, H, Hkv, L, 64, page, lengths, shared=shared, seed=B)
+    call = lambda count: av.avsa_prefix_attn(q, k, v, cu(table), cu(length), prefix_pages=shared, causal=causal, want_lse=True, count=ints(count))
+    for bad, cut in ((L + 1, L), (2 ** 31 - 1, L), (-1, 0), (-2 ** 31, 0)):
+        got, want = call([L] * (B - 1) + [bad]), call([L] * (B - 1) + [cut])
+        assert status(got[2]) == av.AVSA_ERR_BAD_TABLE and status(want[2]) == av.AVSA_OK
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@gpu
+def test_wrapper_refuses_other_counts():
+    q, k, v, table, length = attention_case(3, 2, 2, 4, 64, 16, [100, 100, 100], seed=1)
+    for count in (ints([1, 2]), torch.ones(3, device="cuda"), ints([[1, 2, 3]]), ints([1, 0, 2, 0, 3, 0])[::2]):
+        with pytest.raises(ValueError, match="count"):
+            av.avsa_prefix_attn(q, k, v, cu(table), cu(length), count=count)
+
+
+def test_counts_off_their_grid_are_refused():
+    t = av._Bf16Tensor4(1 << 24, 2 * 64 * 64, 64 * 64, 64)
+    assert av.load_library().avsa_prefix_attn_step(4, 4, 2, 3, 64, 64, 10, 4, 8, t, t, t, 8192, 8192, None, 8194, 2, 0, 0.0, 1 << 25, None, 1 << 16, 1 << 40,
+                                                   0) == av.AVSA_ERR_INVALID_ARG
