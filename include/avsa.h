@@ -278,7 +278,7 @@ AVSA_API int avsa_build_block_mask_static(int B, int H, int N, int d, int blk, a
  * avsa_prefix_attn_step  the same for a step in which the sequences got different numbers of tokens: with AVSA_CAUSAL the first count[b] (int32 [B],
  *                   0..L; NULL: L) of the L queries are the last count[b] tokens of their sequence, lim = length[s] - count[b] + i + 1, and the rows
  *                   behind them are empty.  Without AVSA_CAUSAL all L queries see all tokens.  A count out of range sets AVSA_ERR_BAD_TABLE
- *                   and is cut; it says that not all tokens of the step were written.
+ *                   and is cut; it says that not all tokens of the step were written.  `log` as in (7).
  *
  *   k_pool, v_pool  [pages,Hkv,page,d]: stride_b is the distance of pages, stride_h of heads, stride_n of tokens
  *   prefix_pages    the first prefix_pages pages of all sequences of the batch are the same ones (of a shorter
@@ -299,7 +299,7 @@ AVSA_API int avsa_prefix_attn(int B, int H, int Hkv, int L, int d, int page, int
 AVSA_API int avsa_prefix_attn_step(int B, int H, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d q,
                                    avsa_bf16_4d k_pool, avsa_bf16_4d v_pool, const int32_t* table, const int32_t* length,
                                    const int32_t* seq, const int32_t* count, int prefix_pages, unsigned flags, float softmax_scale,
-                                   void* o_bf16, float* lse, void* ws, size_t ws_bytes, void* stream);
+                                   void* o_bf16, float* lse, int32_t* log, void* ws, size_t ws_bytes, void* stream);
 AVSA_API size_t avsa_prefix_attn_workspace_bytes(int B, int H, int Hkv, int L, int d, int page, int width, int prefix_pages);
 
 /*
@@ -320,11 +320,16 @@ AVSA_API size_t avsa_prefix_attn_workspace_bytes(int B, int H, int Hkv, int L, i
  * avsa_cache_free     sequence seq[k] gives its pages back and is empty (all that its row of the table names; `page` is not looked at).
  * avsa_cache_compact  the pages in use become the first n_live[0] ones: the k-th of those behind moves to the k-th free place among them.
  *
+ * avsa_cache_fork_step, avsa_cache_free_step, avsa_cache_compact_step  the same with a log.
+ *
  * All need the workspace but avsa_cache_write, which has none and no status record.
+ *
+ * `log` of the *_step calls (int32 [4], apart from all other arrays; NULL: none) is a record that no call clears: code, where, item and aux of the first error since
+ * the caller set its code to 0.  A status record holds the last call's alone; a log may be one for many calls, replays of a graph among them.
  */
 AVSA_API int avsa_cache_extend(avsa_cache c, const int32_t* seq, const int32_t* count, int n, void* ws, size_t ws_bytes, void* stream);
-AVSA_API int avsa_cache_extend_step(avsa_cache c, const int32_t* seq, const int32_t* count, int n, int32_t* granted, void* ws, size_t ws_bytes,
-                                    void* stream);
+AVSA_API int avsa_cache_extend_step(avsa_cache c, const int32_t* seq, const int32_t* count, int n, int32_t* granted, int32_t* log, void* ws,
+                                    size_t ws_bytes, void* stream);
 AVSA_API int avsa_cache_write(int n, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d k_new,
                               avsa_bf16_4d v_new, avsa_bf16_4d k_pool, avsa_bf16_4d v_pool, const int32_t* table,
                               const int32_t* length, const int32_t* seq, const int32_t* count, void* stream);
@@ -332,6 +337,10 @@ AVSA_API int avsa_cache_fork(avsa_cache c, avsa_pages pool, const int32_t* paren
                              void* stream);
 AVSA_API int avsa_cache_free(avsa_cache c, const int32_t* seq, int n, void* ws, size_t ws_bytes, void* stream);
 AVSA_API int avsa_cache_compact(avsa_cache c, avsa_pages pool, int32_t* n_live, void* ws, size_t ws_bytes, void* stream);
+AVSA_API int avsa_cache_fork_step(avsa_cache c, avsa_pages pool, const int32_t* parent, const int32_t* child, int n, int32_t* log, void* ws,
+                                  size_t ws_bytes, void* stream);
+AVSA_API int avsa_cache_free_step(avsa_cache c, const int32_t* seq, int n, int32_t* log, void* ws, size_t ws_bytes, void* stream);
+AVSA_API int avsa_cache_compact_step(avsa_cache c, avsa_pages pool, int32_t* n_live, int32_t* log, void* ws, size_t ws_bytes, void* stream);
 AVSA_API size_t avsa_cache_workspace_bytes(int seqs, int pages, int n);
 
 /* Host integer ceil(pct/100 * n): the count forms of rho and kappa (Eq. 8's ceiling). */

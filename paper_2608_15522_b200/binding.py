@@ -51,8 +51,8 @@ EXPORTS = (
     "avsa_protected_rows_attn", "avsa_protected_rows_attn_workspace_bytes",
     "avsa_cache_indicators", "avsa_cache_indicators_workspace_bytes",
     "avsa_prefix_attn", "avsa_prefix_attn_step", "avsa_prefix_attn_workspace_bytes",
-    "avsa_cache_extend", "avsa_cache_extend_step", "avsa_cache_write", "avsa_cache_fork", "avsa_cache_free", "avsa_cache_compact",
-    "avsa_cache_workspace_bytes",
+    "avsa_cache_extend", "avsa_cache_extend_step", "avsa_cache_write", "avsa_cache_fork", "avsa_cache_fork_step", "avsa_cache_free",
+    "avsa_cache_free_step", "avsa_cache_compact", "avsa_cache_compact_step", "avsa_cache_workspace_bytes",
     "avsa_count_from_percent", "avsa_read_status", "avsa_selftest_bounded_wait", "avsa_status_string", "avsa_version",
 )
 
@@ -131,8 +131,8 @@ def _cache():
     if _cache_module is None:
         lib = load_library()
         module = _extension("_avsa_cache")
-        entries = ("avsa_prefix_attn_step", "avsa_prefix_attn_workspace_bytes", "avsa_cache_extend_step", "avsa_cache_write", "avsa_cache_fork",
-                   "avsa_cache_free", "avsa_cache_compact", "avsa_cache_workspace_bytes")
+        entries = ("avsa_prefix_attn_step", "avsa_prefix_attn_workspace_bytes", "avsa_cache_extend_step", "avsa_cache_write",
+                   "avsa_cache_fork_step", "avsa_cache_free_step", "avsa_cache_compact_step", "avsa_cache_workspace_bytes")
         module.bind(*(ctypes.cast(getattr(lib, e), ctypes.c_void_p).value for e in entries),
                     getattr(torch._C, "_cuda_getCurrentRawStream", None))
         _cache_module = module
@@ -174,22 +174,28 @@ def load_library() -> ctypes.CDLL:
     lib.avsa_cache_indicators_workspace_bytes.restype = sz
     lib.avsa_prefix_attn.argtypes = [i, i, i, i, i, i, i, i, i, T, T, T, vp, vp, vp, i, u, f, vp, vp, vp, sz, vp]
     lib.avsa_prefix_attn.restype = i
-    lib.avsa_prefix_attn_step.argtypes = [i, i, i, i, i, i, i, i, i, T, T, T, vp, vp, vp, vp, i, u, f, vp, vp, vp, sz, vp]
+    lib.avsa_prefix_attn_step.argtypes = [i, i, i, i, i, i, i, i, i, T, T, T, vp, vp, vp, vp, i, u, f, vp, vp, vp, vp, sz, vp]
     lib.avsa_prefix_attn_step.restype = i
     lib.avsa_prefix_attn_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
     lib.avsa_prefix_attn_workspace_bytes.restype = sz
     lib.avsa_cache_extend.argtypes = [_Cache, vp, vp, i, vp, sz, vp]
     lib.avsa_cache_extend.restype = i
-    lib.avsa_cache_extend_step.argtypes = [_Cache, vp, vp, i, vp, vp, sz, vp]
+    lib.avsa_cache_extend_step.argtypes = [_Cache, vp, vp, i, vp, vp, vp, sz, vp]
     lib.avsa_cache_extend_step.restype = i
     lib.avsa_cache_write.argtypes = [i, i, i, i, i, i, i, i, T, T, T, T, vp, vp, vp, vp, vp]
     lib.avsa_cache_write.restype = i
     lib.avsa_cache_fork.argtypes = [_Cache, _Pages, vp, vp, i, vp, sz, vp]
     lib.avsa_cache_fork.restype = i
+    lib.avsa_cache_fork_step.argtypes = [_Cache, _Pages, vp, vp, i, vp, vp, sz, vp]
+    lib.avsa_cache_fork_step.restype = i
     lib.avsa_cache_free.argtypes = [_Cache, vp, i, vp, sz, vp]
     lib.avsa_cache_free.restype = i
+    lib.avsa_cache_free_step.argtypes = [_Cache, vp, i, vp, vp, sz, vp]
+    lib.avsa_cache_free_step.restype = i
     lib.avsa_cache_compact.argtypes = [_Cache, _Pages, vp, vp, sz, vp]
     lib.avsa_cache_compact.restype = i
+    lib.avsa_cache_compact_step.argtypes = [_Cache, _Pages, vp, vp, vp, sz, vp]
+    lib.avsa_cache_compact_step.restype = i
     lib.avsa_cache_workspace_bytes.argtypes = [i, i, i]
     lib.avsa_cache_workspace_bytes.restype = sz
     lib.avsa_count_from_percent.argtypes = [i, i]
@@ -474,18 +480,21 @@ def avsa_cache_indicators(y_v, yhat_v, y_a, yhat_a, prot_tok=None, s_cur=None, s
 
 # ------------------------------------------------------------------------------------------------
 # paged cache
+#
+# ``log`` of these calls: int32 [4] on the device, all zero, that keeps code, where, item and aux of the first error of all calls that are given it.  No call
+# clears it, unlike the status record of a workspace, which is the last call's.
 # ------------------------------------------------------------------------------------------------
 def avsa_prefix_attn_workspace_bytes(B, H, Hkv, L, d, page, width, prefix_pages) -> int:
     return int(load_library().avsa_prefix_attn_workspace_bytes(B, H, Hkv, L, d, page, width, prefix_pages))
 
 
 def avsa_prefix_attn(q, k_pool, v_pool, table, length, prefix_pages=0, seq=None, causal=False, softmax_scale=0.0, want_lse=False,
-                     o=None, lse=None, ws=None, count=None):
+                     o=None, lse=None, ws=None, count=None, log=None):
     """Attention of q [B,H,L,d] to the paged sequences seq (None: 0 .. B-1), whose first prefix_pages pages are the same ones.
 
     k_pool/v_pool [pages,Hkv,page,d] bf16, table [seqs,width] and length [seqs] int32.  causal: the queries are the last L tokens of
     their sequence, or with count int32 [B] the first count[b] of them its last count[b] tokens, and the rows behind are empty.  Returns (o, lse or None, ws)."""
-    done = (_cache_module or _cache()).attn(q, k_pool, v_pool, table, length, prefix_pages, seq, causal, softmax_scale, want_lse, o, lse, ws, count)
+    done = (_cache_module or _cache()).attn(q, k_pool, v_pool, table, length, prefix_pages, seq, causal, softmax_scale, want_lse, o, lse, ws, count, log)
     if done[0] != AVSA_OK:
         raise AvsaError(done[0], "avsa_prefix_attn")
     return done[1:]
@@ -495,11 +504,11 @@ def avsa_cache_workspace_bytes(seqs, pages, n) -> int:
     return int(load_library().avsa_cache_workspace_bytes(seqs, pages, n))
 
 
-def avsa_cache_extend(table, length, ref, seq, count, page, out=None, ws=None, granted=None):
+def avsa_cache_extend(table, length, ref, seq, count, page, out=None, ws=None, granted=None, log=None):
     """Room for count[k] more tokens in sequence seq[k].  out: (table, length, ref) that the state behind the call goes to (None: in place).
     granted: int32 [n] that receives what each entry got, count[k] or 0; the count to write with wherever a pool may run out.
     Returns (table, length, ref, ws)."""
-    done = (_cache_module or _cache()).extend(table, length, ref, seq, count, page, *(out or (None, None, None)), ws, granted)
+    done = (_cache_module or _cache()).extend(table, length, ref, seq, count, page, *(out or (None, None, None)), ws, granted, log)
     if done[0] != AVSA_OK:
         raise AvsaError(done[0], "avsa_cache_extend")
     return done[1:]
@@ -514,26 +523,26 @@ def avsa_cache_write(k_new, v_new, k_pool, v_pool, table, length, seq=None, coun
         raise AvsaError(st, "avsa_cache_write")
 
 
-def avsa_cache_fork(pool, table, length, ref, parent, child, out=None, ws=None):
+def avsa_cache_fork(pool, table, length, ref, parent, child, out=None, ws=None, log=None):
     """Sequence child[k], which is empty, becomes a copy of parent[k] that shares its full pages.  pool [planes,pages,Hkv,page,d].
     Returns (table, length, ref, ws)."""
-    done = (_cache_module or _cache()).fork(pool, table, length, ref, parent, child, *(out or (None, None, None)), ws)
+    done = (_cache_module or _cache()).fork(pool, table, length, ref, parent, child, *(out or (None, None, None)), ws, log)
     if done[0] != AVSA_OK:
         raise AvsaError(done[0], "avsa_cache_fork")
     return done[1:]
 
 
-def avsa_cache_free(table, length, ref, seq, out=None, ws=None):
+def avsa_cache_free(table, length, ref, seq, out=None, ws=None, log=None):
     """Sequence seq[k] gives its pages back.  Returns (table, length, ref, ws)."""
-    done = (_cache_module or _cache()).free(table, length, ref, seq, *(out or (None, None, None)), ws)
+    done = (_cache_module or _cache()).free(table, length, ref, seq, *(out or (None, None, None)), ws, log)
     if done[0] != AVSA_OK:
         raise AvsaError(done[0], "avsa_cache_free")
     return done[1:]
 
 
-def avsa_cache_compact(pool, table, length, ref, out=None, n_live=None, ws=None):
+def avsa_cache_compact(pool, table, length, ref, out=None, n_live=None, ws=None, log=None):
     """The pages in use become the first ones of the pool.  Returns (n_live int32 [1], ws)."""
-    done = (_cache_module or _cache()).compact(pool, table, length, ref, *(out or (None, None, None)), n_live, ws)
+    done = (_cache_module or _cache()).compact(pool, table, length, ref, *(out or (None, None, None)), n_live, ws, log)
     if done[0] != AVSA_OK:
         raise AvsaError(done[0], "avsa_cache_compact")
     return done[1:]

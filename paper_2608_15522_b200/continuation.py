@@ -21,7 +21,8 @@ class ClipCache:
     """Keys and values of up to ``seqs`` candidates of up to ``width`` pages each, for ``layers`` layers.
 
     ``calls`` has the cache calls of ``binding`` (injectable, so that the sequencing can be exercised without a GPU; a stand-in whose extend takes no
-    ``granted`` is taken to grant everything, one whose attention takes no ``count`` gets full steps only).  Sequence numbers are given as int32 tensors on the device, or as lists, which are copied there.
+    ``granted`` is taken to grant everything, one whose attention takes no ``count`` gets full steps only, and of calls that take no ``log`` the
+    last one's workspace is read).  Sequence numbers are given as int32 tensors on the device, or as lists, which are copied there.
 
     A sequence that cannot have its pages is left as it was: a step writes nothing to it, and ``check`` says so.
     """
@@ -32,13 +33,18 @@ class ClipCache:
         self.calls, self.layers, self.page = calls, layers, page
         takes = lambda call, name: name in inspect.signature(call).parameters
         self._grants, self._counts = takes(calls.avsa_cache_extend, "granted"), takes(calls.avsa_prefix_attn, "count")
+        kinds = {"extend": calls.avsa_cache_extend, "attention": calls.avsa_prefix_attn, "fork": calls.avsa_cache_fork, "free": calls.avsa_cache_free,
+                 "compact": calls.avsa_cache_compact}
+        # the first error of each kind of call since the last check(), which replays of a captured step report as well
+        self._errors = torch.zeros((len(kinds), 4), dtype=torch.int32, device=device)
+        self._log = {kind: {"log": log} if takes(call, "log") else {} for (kind, call), log in zip(kinds.items(), self._errors)}
         # plane 2i: keys of layer i, plane 2i + 1: its values (what no token has been written to is never used)
         self.pool = torch.empty((2 * layers, pages, heads, page, d), dtype=torch.bfloat16, device=device)
         self.table = torch.full((seqs, width), -1, dtype=torch.int32, device=device)
         self.length = torch.zeros(seqs, dtype=torch.int32, device=device)
         self.ref = torch.zeros(pages, dtype=torch.int32, device=device)
         self._step = None          # sequences of the step under way, and the tokens that each of them was granted
-        self._ws = {}              # the last call's workspace, by kind: its status record is read by check()
+        self._ws = {}              # without a log: the last call's workspace, by kind
 
     def ints(self, x) -> torch.Tensor:
         return x if isinstance(x, torch.Tensor) else torch.tensor(x, dtype=torch.int32, device=self.table.device)
@@ -46,11 +52,15 @@ class ClipCache:
     def _state(self):
         return self.table, self.length, self.ref
 
+    def _keep(self, kind, ws):
+        if not self._log[kind]:
+            self._ws[kind] = ws
+
     def begin_step(self, seq: Sequence[int], count: Sequence[int]) -> None:
         """Room for count[k] more tokens in sequence seq[k]; ``attend`` then writes and attends, layer by layer."""
         seq, count = self.ints(seq), self.ints(count)
         granted = {"granted": torch.empty_like(count)} if self._grants else {}
-        self._ws["extend"] = self.calls.avsa_cache_extend(*self._state(), seq, count, self.page, **granted)[3]
+        self._keep("extend", self.calls.avsa_cache_extend(*self._state(), seq, count, self.page, **granted, **self._log["extend"])[3])
         self._step = (seq, granted.get("granted", count))
 
     def attend(self, layer: int, q, k_new, v_new, prefix_pages: int = 0, causal: bool = False, softmax_scale: float = 0.0):
@@ -63,31 +73,37 @@ class ClipCache:
         k, v = self.pool[2 * layer], self.pool[2 * layer + 1]
         self.calls.avsa_cache_write(k_new, v_new, k, v, self.table, self.length, seq, count)
         more = {"count": count} if self._counts else {}
-        o, _, self._ws["attention"] = self.calls.avsa_prefix_attn(q, k, v, self.table, self.length, prefix_pages=prefix_pages, seq=seq, causal=causal,
-                                                                 softmax_scale=softmax_scale, **more)
+        o, _, ws = self.calls.avsa_prefix_attn(q, k, v, self.table, self.length, prefix_pages=prefix_pages, seq=seq, causal=causal,
+                                               softmax_scale=softmax_scale, **more, **self._log["attention"])
+        self._keep("attention", ws)
         return o
 
     def branch(self, parent: Sequence[int], child: Sequence[int]) -> None:
         """Sequence child[k], which is empty, becomes a copy of parent[k] that shares its full pages."""
         parent, child = self.ints(parent), self.ints(child)
-        self._ws["fork"] = self.calls.avsa_cache_fork(self.pool, *self._state(), parent, child)[3]
+        self._keep("fork", self.calls.avsa_cache_fork(self.pool, *self._state(), parent, child, **self._log["fork"])[3])
 
     def drop(self, seq: Sequence[int]) -> None:
         """Sequences seq give their pages back."""
-        self._ws["free"] = self.calls.avsa_cache_free(*self._state(), self.ints(seq))[3]
+        self._keep("free", self.calls.avsa_cache_free(*self._state(), self.ints(seq), **self._log["free"])[3])
 
     def compact(self) -> torch.Tensor:
         """The pages in use become the first ones of the pool; their number, int32 [1] on the device."""
-        n_live, self._ws["compact"] = self.calls.avsa_cache_compact(self.pool, *self._state())
+        n_live, ws = self.calls.avsa_cache_compact(self.pool, *self._state(), **self._log["compact"])
+        self._keep("compact", ws)
         return n_live
 
     def check(self) -> None:
-        """Waits for the stream and raises for the last call of each kind that met an error on the device."""
-        from .binding import AVSA_OK, AvsaError
-        for kind, ws in self._ws.items():
-            code, detail = self.calls.avsa_read_status(ws)
-            if code != AVSA_OK:
-                raise AvsaError(code, f"ClipCache: {kind}, detail {detail}")
+        """Waits for the stream and raises for the first error of each kind of call that the device has met since the last check."""
+        from .binding import AVSA_OK, AvsaError, status_string
+        found = [(kind, code, tuple(detail)) for kind, (code, *detail) in zip(self._log, self._errors.tolist())]
+        found += [(kind, *self.calls.avsa_read_status(ws)) for kind, ws in self._ws.items()]
+        found = [(kind, code, detail) for kind, code, detail in found if code != AVSA_OK]
+        if found:
+            self._errors.zero_()
+            (kind, code, detail), more = found[0], found[1:]
+            also = "".join(f"; {kind}: {status_string(c)}, detail {d}" for kind, c, d in more)
+            raise AvsaError(code, f"ClipCache: {kind}, detail {detail}{also}")
 
 
 class ToyGenerator:

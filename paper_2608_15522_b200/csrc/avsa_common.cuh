@@ -33,6 +33,16 @@ __device__ __forceinline__ void report_status(StatusRecord* st, int code, int wh
   }
 }
 
+// The same, and the first error since the caller last cleared it into a record of the caller's own (int32 [4]: code, where, item, aux; NULL: none).
+__device__ __forceinline__ void report_logged(StatusRecord* st, int32_t* log, int code, int where, int item, int aux) {
+  report_status(st, code, where, item, aux);
+  if (log != nullptr && atomicCAS(log, 0, code) == 0) {
+    log[1] = where;
+    log[2] = item;
+    log[3] = aux;
+  }
+}
+
 // ------------------------------------------------------------------------------------ programmatic dependent launch
 // Every kernel of the library's calls is launched as a programmatic dependent of the kernel before it on the stream:
 // it is set up while that one drains, waits (pdl_wait) for that kernel's end, and lets its own successor be set up

@@ -16,9 +16,9 @@ decltype(&avsa_prefix_attn_step) f_attn;
 decltype(&avsa_prefix_attn_workspace_bytes) f_attn_ws;
 decltype(&avsa_cache_extend_step) f_extend;
 decltype(&avsa_cache_write) f_write;
-decltype(&avsa_cache_fork) f_fork;
-decltype(&avsa_cache_free) f_free;
-decltype(&avsa_cache_compact) f_compact;
+decltype(&avsa_cache_fork_step) f_fork;
+decltype(&avsa_cache_free_step) f_free;
+decltype(&avsa_cache_compact_step) f_compact;
 decltype(&avsa_cache_workspace_bytes) f_ws;
 PyObject* o_raw_stream;
 
@@ -69,6 +69,12 @@ struct Call {
     return r;
   }
   Arg ints(int i, const char* name, int64_t dims, bool optional = false) { return plain(i, name, at::kInt, dims, optional); }
+  // the record of the first error of many calls
+  Arg log(int i) {
+    const Arg r = ints(i, "log", 1, true);
+    TORCH_CHECK_VALUE(!r.there() || r.numel == 4, "log: expected four entries");
+    return r;
+  }
   bool flag(int i, const char* name) {
     TORCH_CHECK_TYPE(PyBool_Check(a[i]), name, ": expected a bool");
     return a[i] == Py_True;
@@ -153,10 +159,10 @@ void arity(Py_ssize_t got, Py_ssize_t want) {
   TORCH_CHECK_TYPE(got == want && f_attn != nullptr, "wrong number of arguments, or bind() has not been called");
 }
 
-// attn(q, k_pool, v_pool, table, length, prefix_pages, seq, causal, softmax_scale, want_lse, o, lse, ws, count) -> (status, o, lse, ws)
+// attn(q, k_pool, v_pool, table, length, prefix_pages, seq, causal, softmax_scale, want_lse, o, lse, ws, count, log) -> (status, o, lse, ws)
 PyObject* py_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  arity(n, 14);
+  arity(n, 15);
   Call c{a};
   const View q = take_view(c, 0, "q"), k = take_view(c, 1, "k_pool"), v = take_view(c, 2, "v_pool");
   const Arg table = c.ints(3, "table", 2), length = c.ints(4, "length", 1);
@@ -185,6 +191,7 @@ PyObject* py_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Arg ws = c.plain(12, "ws", at::kByte, 1, true);
   const Arg count = c.ints(13, "count", 1, true);
   TORCH_CHECK_VALUE(!count.there() || count.numel == B, "count: one entry for each batch entry of q");
+  const Arg log = c.log(14);
   c.find_stream();
   int st;
   without_lock([&] {
@@ -195,7 +202,8 @@ PyObject* py_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (want_lse) c.make(lse, at::kFloat, {B, H, L});
     if (!ws.there()) c.make_ws(ws, f_attn_ws(B, H, Hkv, L, d, page, width, prefix_pages));
     st = f_attn(B, H, Hkv, L, d, page, pages, seqs, width, q, k, v, table.as<int32_t>(), length.as<int32_t>(), seq.as<int32_t>(),
-                count.as<int32_t>(), prefix_pages, causal ? AVSA_CAUSAL : 0u, scale, o.ptr, lse.as<float>(), ws.ptr, static_cast<size_t>(ws.numel), c.stream);
+                count.as<int32_t>(), prefix_pages, causal ? AVSA_CAUSAL : 0u, scale, o.ptr, lse.as<float>(), log.as<int32_t>(), ws.ptr,
+                static_cast<size_t>(ws.numel), c.stream);
   });
   return result(st, {c.give(10, o), c.give(11, lse), c.give(12, ws)});
   END_HANDLE_TH_ERRORS
@@ -241,10 +249,10 @@ int list_size(const Arg& x, const Arg& y, const char* text) {
   return static_cast<int>(x.numel);
 }
 
-// extend(table, length, ref, seq, count, page, table_out, length_out, ref_out, ws, granted) -> (status, table, length, ref, ws)
+// extend(table, length, ref, seq, count, page, table_out, length_out, ref_out, ws, granted, log) -> (status, table, length, ref, ws)
 PyObject* py_extend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  arity(n, 11);
+  arity(n, 12);
   Call c{a};
   const State s(c, 0, 6);
   const Arg seq = c.ints(3, "seq", 1), count = c.ints(4, "count", 1);
@@ -253,11 +261,13 @@ PyObject* py_extend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Arg ws = c.plain(9, "ws", at::kByte, 1, true);
   const Arg granted = c.ints(10, "granted", 1, true);
   TORCH_CHECK_VALUE(!granted.there() || granted.numel == entries, "granted: one entry for each of seq");
+  const Arg log = c.log(11);
   c.find_stream();
   int st;
   without_lock([&] {
     if (!ws.there()) c.make_ws(ws, f_ws(cache.seqs, cache.pages, entries));
-    st = f_extend(cache, seq.as<int32_t>(), count.as<int32_t>(), entries, granted.as<int32_t>(), ws.ptr, static_cast<size_t>(ws.numel), c.stream);
+    st = f_extend(cache, seq.as<int32_t>(), count.as<int32_t>(), entries, granted.as<int32_t>(), log.as<int32_t>(), ws.ptr,
+                  static_cast<size_t>(ws.numel), c.stream);
   });
   return result(st, {wrap(s.table_out), wrap(s.length_out), wrap(s.ref_out), c.give(9, ws)});
   END_HANDLE_TH_ERRORS
@@ -287,10 +297,10 @@ PyObject* py_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// fork(pool, table, length, ref, parent, child, table_out, length_out, ref_out, ws) -> (status, table, length, ref, ws)
+// fork(pool, table, length, ref, parent, child, table_out, length_out, ref_out, ws, log) -> (status, table, length, ref, ws)
 PyObject* py_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  arity(n, 10);
+  arity(n, 11);
   Call c{a};
   const State s(c, 1, 6);
   Arg hold;
@@ -300,40 +310,42 @@ PyObject* py_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int entries = list_size(parent, child, "parent and child have different lengths");
   const avsa_cache cache = s.cache(page);
   Arg ws = c.plain(9, "ws", at::kByte, 1, true);
+  const Arg log = c.log(10);
   c.find_stream();
   int st;
   without_lock([&] {
     if (!ws.there()) c.make_ws(ws, f_ws(cache.seqs, cache.pages, entries));
-    st = f_fork(cache, pool, parent.as<int32_t>(), child.as<int32_t>(), entries, ws.ptr, static_cast<size_t>(ws.numel), c.stream);
+    st = f_fork(cache, pool, parent.as<int32_t>(), child.as<int32_t>(), entries, log.as<int32_t>(), ws.ptr, static_cast<size_t>(ws.numel), c.stream);
   });
   return result(st, {wrap(s.table_out), wrap(s.length_out), wrap(s.ref_out), c.give(9, ws)});
   END_HANDLE_TH_ERRORS
 }
 
-// free(table, length, ref, seq, table_out, length_out, ref_out, ws) -> (status, table, length, ref, ws)
+// free(table, length, ref, seq, table_out, length_out, ref_out, ws, log) -> (status, table, length, ref, ws)
 PyObject* py_free(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  arity(n, 8);
+  arity(n, 9);
   Call c{a};
   const State s(c, 0, 4);
   const Arg seq = c.ints(3, "seq", 1);
   const int entries = list_size(seq, seq, "seq");
   const avsa_cache cache = s.cache(0);
   Arg ws = c.plain(7, "ws", at::kByte, 1, true);
+  const Arg log = c.log(8);
   c.find_stream();
   int st;
   without_lock([&] {
     if (!ws.there()) c.make_ws(ws, f_ws(cache.seqs, cache.pages, entries));
-    st = f_free(cache, seq.as<int32_t>(), entries, ws.ptr, static_cast<size_t>(ws.numel), c.stream);
+    st = f_free(cache, seq.as<int32_t>(), entries, log.as<int32_t>(), ws.ptr, static_cast<size_t>(ws.numel), c.stream);
   });
   return result(st, {wrap(s.table_out), wrap(s.length_out), wrap(s.ref_out), c.give(7, ws)});
   END_HANDLE_TH_ERRORS
 }
 
-// compact(pool, table, length, ref, table_out, length_out, ref_out, n_live, ws) -> (status, n_live, ws)
+// compact(pool, table, length, ref, table_out, length_out, ref_out, n_live, ws, log) -> (status, n_live, ws)
 PyObject* py_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  arity(n, 9);
+  arity(n, 10);
   Call c{a};
   const State s(c, 1, 4);
   Arg hold;
@@ -341,13 +353,14 @@ PyObject* py_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const avsa_pages pool = take_pool(c, 0, s.ref.numel, &page, hold);
   const avsa_cache cache = s.cache(page);
   Arg n_live = c.ints(7, "n_live", 1, true), ws = c.plain(8, "ws", at::kByte, 1, true);
+  const Arg log = c.log(9);
   TORCH_CHECK_VALUE(!n_live.there() || n_live.numel >= 1, "n_live: expected one entry");
   c.find_stream();
   int st;
   without_lock([&] {
     c.make(n_live, at::kInt, {1});
     if (!ws.there()) c.make_ws(ws, f_ws(cache.seqs, cache.pages, 0));
-    st = f_compact(cache, pool, n_live.as<int32_t>(), ws.ptr, static_cast<size_t>(ws.numel), c.stream);
+    st = f_compact(cache, pool, n_live.as<int32_t>(), log.as<int32_t>(), ws.ptr, static_cast<size_t>(ws.numel), c.stream);
   });
   return result(st, {c.give(7, n_live), c.give(8, ws)});
   END_HANDLE_TH_ERRORS

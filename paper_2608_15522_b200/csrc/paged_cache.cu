@@ -67,6 +67,7 @@ struct MetaArgs {
   int n;
   int32_t* n_live;
   int32_t* granted;         // extend: [n], or NULL
+  int32_t* log;
 };
 
 __device__ __forceinline__ int cluster_rank() {
@@ -292,7 +293,7 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
             }
           }
         }
-        if (bad) report_status(w.status, code, bad, k, s);
+        if (bad) report_logged(w.status, a.log, code, bad, k, s);
       }
       int all;
       e.first = taken + block_scan(e.need, all, sm);
@@ -328,7 +329,7 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
     const int s = e0.x, other = e0.y, tokens = e0.z, new_tokens = e0.w, first = e1.x, need = e1.y;
     auto free_page = [&](int at) { return alone ? free_pages[at] : __ldcg(&free_pages[at]); };
     const bool refused = s >= 0 && need > 0 && first + need > n_free;
-    if (refused && lane == 0) report_status(w.status, AVSA_ERR_NO_PAGES, kCacheFull, k, s);
+    if (refused && lane == 0) report_logged(w.status, a.log, AVSA_ERR_NO_PAGES, kCacheFull, k, s);
     if (OP == kExtend && lane == 0 && a.granted != nullptr) a.granted[k] = s < 0 || refused ? 0 : new_tokens;
     if (OP == kFork && lane == 0 && (s < 0 || refused || need == 0)) w.moves[k] = make_int4(-1, -1, 0, 0);
     if (s < 0 || refused) continue;
@@ -351,7 +352,7 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
           if (page >= 0 && page < c.pages) {
             atomicAdd(&c.ref_out[page], 1);
           } else {
-            report_status(w.status, AVSA_ERR_BAD_TABLE, kCachePage, other, j);
+            report_logged(w.status, a.log, AVSA_ERR_BAD_TABLE, kCachePage, other, j);
           }
         } else if (j == whole && need) {
           page = free_page(first);
@@ -359,7 +360,7 @@ __global__ void __launch_bounds__(kMetaThreads, 1) assign_pages_kernel(const Met
           const int src = from[j];
           const bool good = src >= 0 && src < c.pages;
           w.moves[k] = good ? make_int4(src, page, 1, 0) : make_int4(-1, -1, 0, 0);
-          if (!good) report_status(w.status, AVSA_ERR_BAD_TABLE, kCachePage, other, j);
+          if (!good) report_logged(w.status, a.log, AVSA_ERR_BAD_TABLE, kCachePage, other, j);
         }
         row[j] = page;
       }
@@ -381,7 +382,7 @@ __global__ void __launch_bounds__(kMetaThreads, 1) free_pages_kernel(const MetaA
     const int s = k == k0 ? s0 : a.seq[k];
     if (s < 0) continue;
     if (s >= c.seqs) {
-      if (lane == 0) report_status(a.w.status, AVSA_ERR_BAD_TABLE, kCacheSeq, k, s);
+      if (lane == 0) report_logged(a.w.status, a.log, AVSA_ERR_BAD_TABLE, kCacheSeq, k, s);
       continue;
     }
     // whoever takes an entry of the row gives its page back: a sequence that is listed again has none left by then
@@ -389,8 +390,8 @@ __global__ void __launch_bounds__(kMetaThreads, 1) free_pages_kernel(const MetaA
     for (int j = lane; j < c.width; j += 32) {
       const int page = atomicExch(&row[j], -1);
       if (page == -1) continue;
-      if (page < -1 || page >= c.pages) report_status(a.w.status, AVSA_ERR_BAD_TABLE, kCachePage, s, j);
-      else if (atomicSub(&c.ref_out[page], 1) <= 0) report_status(a.w.status, AVSA_ERR_BAD_TABLE, kCacheRef, s, page);
+      if (page < -1 || page >= c.pages) report_logged(a.w.status, a.log, AVSA_ERR_BAD_TABLE, kCachePage, s, j);
+      else if (atomicSub(&c.ref_out[page], 1) <= 0) report_logged(a.w.status, a.log, AVSA_ERR_BAD_TABLE, kCacheRef, s, page);
     }
     if (lane == 0) c.length_out[s] = 0;
   }
@@ -496,6 +497,7 @@ struct CopyArgs {
   const int32_t* n_live;
   int seqs, width, pages, page;
   StatusRecord* status;
+  int32_t* log;
 };
 
 __global__ void __launch_bounds__(kCopyThreads) move_pages_kernel(const CopyArgs a) {
@@ -513,7 +515,7 @@ __global__ void __launch_bounds__(kCopyThreads) move_pages_kernel(const CopyArgs
         to = a.place[page];
         bad = to < 0;
       }
-      if (bad) report_status(a.status, AVSA_ERR_BAD_TABLE, kCachePage, static_cast<int>(i / a.width), static_cast<int>(i % a.width));
+      if (bad) report_logged(a.status, a.log, AVSA_ERR_BAD_TABLE, kCachePage, static_cast<int>(i / a.width), static_cast<int>(i % a.width));
       if (a.table != a.table_out || to != page) a.table_out[i] = to;
     }
   }
@@ -634,6 +636,9 @@ static int check_list(const avsa_cache& c, const int32_t* a, const int32_t* b, i
   if (!ws_aligned(ws, kWsVectors)) return AVSA_ERR_INVALID_ARG;
   return AVSA_OK;
 }
+static int check_log(const avsa_cache& c, const int32_t* log) {
+  return log == nullptr || (aligned4(log) && apart_from_state(c, log, 4)) ? AVSA_OK : AVSA_ERR_INVALID_ARG;
+}
 static int check_pool(const avsa_pages& p, int pages) {
   if (p.ptr == nullptr || !aligned16(p.ptr) || p.planes <= 0 || p.page_bytes <= 0 || p.page_bytes % 16 != 0) return AVSA_ERR_INVALID_ARG;
   if (pages > 1 && (p.stride_page < p.page_bytes || p.stride_page % 16 != 0)) return AVSA_ERR_INVALID_ARG;
@@ -679,30 +684,32 @@ extern "C" size_t avsa_cache_workspace_bytes(int seqs, int pages, int n) {
   return CacheWs::bytes(seqs, pages, n);
 }
 
-extern "C" int avsa_cache_extend_step(avsa_cache c, const int32_t* seq, const int32_t* count, int n, int32_t* granted, void* ws, size_t ws_bytes,
-                                      void* stream) {
-  const int st = check_list(c, seq, count, n, ws, ws_bytes);
+extern "C" int avsa_cache_extend_step(avsa_cache c, const int32_t* seq, const int32_t* count, int n, int32_t* granted, int32_t* log, void* ws,
+                                      size_t ws_bytes, void* stream) {
+  int st = check_list(c, seq, count, n, ws, ws_bytes);
+  if (st == AVSA_OK) st = check_log(c, log);
   if (st != AVSA_OK) return st;
   if (granted != nullptr) {
     if (!aligned4(granted) || !apart_from_state(c, granted, n) || !apart(granted, n, seq, n) || !apart(granted, n, count, n)) return AVSA_ERR_INVALID_ARG;
   }
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
-  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), seq, count, n, nullptr, granted};
+  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), seq, count, n, nullptr, granted, log};
   if (launch_meta(assign_pages_kernel<kExtend>, a, as_stream(stream), AssignSmem(c, n).bytes, kAssignMost) != cudaSuccess) return AVSA_ERR_CUDA;
   return done();
 }
 
 extern "C" int avsa_cache_extend(avsa_cache c, const int32_t* seq, const int32_t* count, int n, void* ws, size_t ws_bytes, void* stream) {
-  return avsa_cache_extend_step(c, seq, count, n, nullptr, ws, ws_bytes, stream);
+  return avsa_cache_extend_step(c, seq, count, n, nullptr, nullptr, ws, ws_bytes, stream);
 }
 
-extern "C" int avsa_cache_fork(avsa_cache c, avsa_pages pool, const int32_t* parent, const int32_t* child, int n, void* ws, size_t ws_bytes,
-                               void* stream) {
+extern "C" int avsa_cache_fork_step(avsa_cache c, avsa_pages pool, const int32_t* parent, const int32_t* child, int n, int32_t* log, void* ws,
+                                    size_t ws_bytes, void* stream) {
   int st = check_list(c, parent, child, n, ws, ws_bytes);
   if (st == AVSA_OK) st = check_pool(pool, c.pages);
+  if (st == AVSA_OK) st = check_log(c, log);
   if (st != AVSA_OK) return st;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
-  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), child, parent, n, nullptr, nullptr};
+  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), child, parent, n, nullptr, nullptr, log};
   if (launch_meta(assign_pages_kernel<kFork>, a, as_stream(stream), AssignSmem(c, n).bytes, kAssignMost) != cudaSuccess) return AVSA_ERR_CUDA;
   if (n > 0) {
     CopyArgs m = {};
@@ -710,27 +717,39 @@ extern "C" int avsa_cache_fork(avsa_cache c, avsa_pages pool, const int32_t* par
     m.moves = a.w.moves;
     m.n = n;
     m.status = a.w.status;
+    m.log = log;
     if (launch_moves(m, n, as_stream(stream)) != AVSA_OK) return AVSA_ERR_CUDA;
   }
   return done();
 }
 
-extern "C" int avsa_cache_free(avsa_cache c, const int32_t* seq, int n, void* ws, size_t ws_bytes, void* stream) {
-  const int st = check_list(c, seq, seq, n, ws, ws_bytes, false);
+extern "C" int avsa_cache_fork(avsa_cache c, avsa_pages pool, const int32_t* parent, const int32_t* child, int n, void* ws, size_t ws_bytes,
+                               void* stream) {
+  return avsa_cache_fork_step(c, pool, parent, child, n, nullptr, ws, ws_bytes, stream);
+}
+
+extern "C" int avsa_cache_free_step(avsa_cache c, const int32_t* seq, int n, int32_t* log, void* ws, size_t ws_bytes, void* stream) {
+  int st = check_list(c, seq, seq, n, ws, ws_bytes, false);
+  if (st == AVSA_OK) st = check_log(c, log);
   if (st != AVSA_OK) return st;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
-  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), seq, nullptr, n, nullptr, nullptr};
+  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, n), seq, nullptr, n, nullptr, nullptr, log};
   if (launch_meta(free_pages_kernel, a, as_stream(stream)) != cudaSuccess) return AVSA_ERR_CUDA;
   return done();
 }
 
-extern "C" int avsa_cache_compact(avsa_cache c, avsa_pages pool, int32_t* n_live, void* ws, size_t ws_bytes, void* stream) {
+extern "C" int avsa_cache_free(avsa_cache c, const int32_t* seq, int n, void* ws, size_t ws_bytes, void* stream) {
+  return avsa_cache_free_step(c, seq, n, nullptr, ws, ws_bytes, stream);
+}
+
+extern "C" int avsa_cache_compact_step(avsa_cache c, avsa_pages pool, int32_t* n_live, int32_t* log, void* ws, size_t ws_bytes, void* stream) {
   int st = check_list(c, nullptr, nullptr, 0, ws, ws_bytes);
   if (st == AVSA_OK) st = check_pool(pool, c.pages);
+  if (st == AVSA_OK) st = check_log(c, log);
   if (st != AVSA_OK) return st;
   if (n_live == nullptr || !aligned4(n_live)) return AVSA_ERR_INVALID_ARG;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
-  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, 0), nullptr, nullptr, 0, n_live, nullptr};
+  const MetaArgs a = {c, CacheWs(ws, c.seqs, c.pages, 0), nullptr, nullptr, 0, n_live, nullptr, log};
   if (launch_meta(plan_compaction_kernel, a, as_stream(stream), most_moves(c) * kMoveBytes, kPlanMost) != cudaSuccess) return AVSA_ERR_CUDA;
   CopyArgs m = {};
   m.pool = pool;
@@ -744,8 +763,13 @@ extern "C" int avsa_cache_compact(avsa_cache c, avsa_pages pool, int32_t* n_live
   m.width = c.width;
   m.pages = c.pages;
   m.status = a.w.status;
+  m.log = log;
   if (launch_moves(m, c.pages, as_stream(stream)) != AVSA_OK) return AVSA_ERR_CUDA;
   return done();
+}
+
+extern "C" int avsa_cache_compact(avsa_cache c, avsa_pages pool, int32_t* n_live, void* ws, size_t ws_bytes, void* stream) {
+  return avsa_cache_compact_step(c, pool, n_live, nullptr, ws, ws_bytes, stream);
 }
 
 extern "C" int avsa_cache_write(int n, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d k_new,

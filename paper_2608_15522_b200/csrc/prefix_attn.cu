@@ -242,7 +242,7 @@ extern "C" size_t avsa_prefix_attn_workspace_bytes(int B, int H, int Hkv, int L,
 extern "C" int avsa_prefix_attn_step(int B, int H, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d q,
                                      avsa_bf16_4d k_pool, avsa_bf16_4d v_pool, const int32_t* table, const int32_t* length,
                                      const int32_t* seq, const int32_t* count, int prefix_pages, unsigned flags, float softmax_scale,
-                                     void* o_bf16, float* lse, void* ws, size_t ws_bytes, void* stream) {
+                                     void* o_bf16, float* lse, int32_t* log, void* ws, size_t ws_bytes, void* stream) {
   if (B < 0 || H <= 0 || Hkv <= 0 || L < 0 || pages <= 0 || seqs <= 0 || width <= 0 || prefix_pages < 0 || prefix_pages > width) return AVSA_ERR_INVALID_ARG;
   if (H % Hkv != 0 || (flags & ~AVSA_CAUSAL) != 0 || (seq == nullptr && B > seqs)) return AVSA_ERR_INVALID_ARG;
   if ((d != 64 && d != 128) || (page != 16 && page != 32 && page != 64 && page != 128)) return AVSA_ERR_UNSUPPORTED;
@@ -254,7 +254,7 @@ extern "C" int avsa_prefix_attn_step(int B, int H, int Hkv, int L, int d, int pa
   if (B == 0 || L == 0) return AVSA_OK;
   if (!rows_ok(q, B, H, L) || !tensor_ok(k_pool, pages, Hkv) || !tensor_ok(v_pool, pages, Hkv)) return AVSA_ERR_INVALID_ARG;
   if (table == nullptr || length == nullptr || o_bf16 == nullptr || !aligned16(o_bf16)) return AVSA_ERR_INVALID_ARG;
-  if (!aligned4(table) || !aligned4(length) || !aligned4(seq) || !aligned4(count) || !aligned4(lse)) return AVSA_ERR_INVALID_ARG;
+  if (!aligned4(table) || !aligned4(length) || !aligned4(seq) || !aligned4(count) || !aligned4(lse) || !aligned4(log)) return AVSA_ERR_INVALID_ARG;
   PrefixLayout y;
   if (!prefix_layout(B, H, Hkv, L, d, page, width, prefix_pages, flags & AVSA_CAUSAL ? 1 : 0, y)) return AVSA_ERR_UNSUPPORTED;
   if (ws == nullptr || ws_bytes < y.total) return AVSA_ERR_WORKSPACE;
@@ -276,6 +276,7 @@ extern "C" int avsa_prefix_attn_step(int B, int H, int Hkv, int L, int d, int pa
   p.count = count;
   p.scale_log2 = scale * 1.4426950408889634f;
   p.status = static_cast<StatusRecord*>(ws);
+  p.log = log;
   p.plan = reinterpret_cast<int*>(w + y.plan);
   p.counter = p.plan + 32;
   p.cta_err = reinterpret_cast<int4*>(w + y.cta_err);
@@ -295,5 +296,5 @@ extern "C" int avsa_prefix_attn(int B, int H, int Hkv, int L, int d, int page, i
                                 const int32_t* seq, int prefix_pages, unsigned flags, float softmax_scale, void* o_bf16, float* lse,
                                 void* ws, size_t ws_bytes, void* stream) {
   return avsa_prefix_attn_step(B, H, Hkv, L, d, page, pages, seqs, width, q, k_pool, v_pool, table, length, seq, nullptr, prefix_pages, flags,
-                               softmax_scale, o_bf16, lse, ws, ws_bytes, stream);
+                               softmax_scale, o_bf16, lse, nullptr, ws, ws_bytes, stream);
 }

@@ -92,6 +92,7 @@ struct PrefixParams {
   float scale_log2;
   // workspace
   StatusRecord* status;
+  int32_t* log;        // the caller's record of the first error, or NULL
   int* counter;        // head of the queue
   int* plan;           // for the merge: PT, columns a group, B pieces
   int4* cta_err;       // [2 * CTAs]: code, where, item, aux; recomputed items
@@ -1204,6 +1205,7 @@ __global__ void __launch_bounds__(kPxMergeThreads) prefix_merge_kernel(const __g
       p.status->aux = err.w;
       p.status->redo_count = again;
       p.status->next_item = 0;
+      if (err.x != 0) report_logged(p.status, p.log, err.x, err.y, err.z, err.w);
     }
   }
   if (S.stack) {

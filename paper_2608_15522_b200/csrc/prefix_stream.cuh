@@ -132,9 +132,9 @@ __device__ __noinline__ void prefix_check(const PrefixParams& p, int n_cta, int 
     p.status->redo_count = again;
     if (tile_error != 0x7fffffff) {
       const int4 e = p.cta_err[2 * tile_error];
-      report_status(p.status, e.x, e.y, e.z, e.w);
+      report_logged(p.status, p.log, e.x, e.y, e.z, e.w);
     } else if (worst != 0x7fffffff) {
-      report_status(p.status, AVSA_ERR_BAD_TABLE, worst & 511, worst >> 9, 0);
+      report_logged(p.status, p.log, AVSA_ERR_BAD_TABLE, worst & 511, worst >> 9, 0);
     }
   }
 }
@@ -440,7 +440,7 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
   }
   if (!ok) {
     // a load never came: the rows are left as they are, and what is under way lands before this memory is given away
-    report_status(p.status, AVSA_ERR_TIMEOUT, kPxKFull, item, blk);
+    report_logged(p.status, p.log, AVSA_ERR_TIMEOUT, kPxKFull, item, blk);
     for (int k = 0; k < STAGES; k++) mbar_wait(full + k * 8, (round + (k < stage ? 1 : 0)) & 1);
   }
   __syncthreads();      // the ring is the warps' rows from here on

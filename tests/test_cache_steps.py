@@ -104,7 +104,7 @@ def test_extend_says_what_it_granted(seqs, page, pages, most, out):
 def test_what_is_granted_overlaps_nothing():
     lib = av.load_library()
     state = dict(table=1 << 20, length=2 << 20, ref=3 << 20, table_out=4 << 20, length_out=5 << 20, ref_out=6 << 20, seqs=4, width=8, pages=100, page=16)
-    call = lambda granted: lib.avsa_cache_extend_step(av._Cache(**state), 8192, 16384, 2, granted, 1 << 16, 1 << 30, 0)
+    call = lambda granted: lib.avsa_cache_extend_step(av._Cache(**state), 8192, 16384, 2, granted, None, 1 << 16, 1 << 30, 0)
     for name in ("table", "length", "ref", "table_out", "length_out", "ref_out"):
         assert call(state[name]) == av.AVSA_ERR_INVALID_ARG, name
     for granted in (8196, 16380, 32770):
@@ -247,5 +247,147 @@ def test_wrapper_refuses_other_counts():
 
 def test_counts_off_their_grid_are_refused():
     t = av._Bf16Tensor4(1 << 24, 2 * 64 * 64, 64 * 64, 64)
-    assert av.load_library().avsa_prefix_attn_step(4, 4, 2, 3, 64, 64, 10, 4, 8, t, t, t, 8192, 8192, None, 8194, 2, 0, 0.0, 1 << 25, None, 1 << 16, 1 << 40,
+    assert av.load_library().avsa_prefix_attn_step(4, 4, 2, 3, 64, 64, 10, 4, 8, t, t, t, 8192, 8192, None, 8194, 2, 0, 0.0, 1 << 25, None, None, 1 << 16, 1 << 40,
                                                    0) == av.AVSA_ERR_INVALID_ARG
+
+
+# ------------------------------------------------------------------------------------------------ errors that nobody reads at once
+class LogCalls(StepCalls):
+    """``StepCalls`` with the log of extend and attention."""
+
+    def avsa_cache_extend(self, table, length, ref, seq, count, page, out=None, ws=None, granted=None, log=None):
+        done = super().avsa_cache_extend(table, length, ref, seq, count, page, granted=granted)
+        if done[3] != av.AVSA_OK and log[0] == 0:
+            log[0] = done[3]
+        return done
+
+    def avsa_prefix_attn(self, *args, count=None, log=None, **kw):
+        return super().avsa_prefix_attn(*args, count=count, **kw)
+
+
+@pytest.mark.parametrize("where", WHERE)
+def test_errors_stay_until_they_are_read(where):
+    """A step that is refused, steps and drops that are not: check says so, once."""
+    cache = ClipCache(1, 1, 64, 16, 4, 2, 8, device=where, calls=LogCalls() if where == "cpu" else None)
+    x = torch.ones((1, 1, 1, 64), dtype=torch.bfloat16, device=where)
+    cache.begin_step([0], [16])
+    cache.check()
+    cache.begin_step([1], [100])
+    for _ in range(3):
+        cache.begin_step([0], [1])
+        cache.attend(0, x, x, x)
+    cache.drop([0])
+    with pytest.raises(av.AvsaError, match="extend") as e:
+        cache.check()
+    assert e.value.status == av.AVSA_ERR_NO_PAGES
+    cache.check()
+    cache.begin_step([0], [64])
+    cache.check()
+
+
+@gpu
+def test_errors_of_replays_and_of_every_layer_are_read():
+    """A captured step runs out of pages in one of its replays; in another cache only the first of two layers leaves tokens out, the fork and the drop are refused."""
+    cache = ClipCache(1, 1, 64, 16, 4, 2, 8)
+    seq, count, x = ints([0, 1]), ints([9, 3]), torch.ones((2, 1, 9, 64), dtype=torch.bfloat16, device="cuda")
+
+    def step():
+        cache.begin_step(seq, count)
+        return cache.attend(0, x, x, x, causal=True)
+
+    step()
+    cache.drop([0, 1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(4):
+        graph.replay()
+    cache.check()
+    assert cache.length.tolist() == [36, 12]
+    for _ in range(2):
+        graph.replay()          # 45 and 15 tokens fill four pages up to 3 and 1: of the step behind that neither sequence gets anything
+    assert cache.length.tolist() == [45, 15]
+    with pytest.raises(av.AvsaError, match="extend"):
+        cache.check()
+    cache.drop([0, 1])
+    graph.replay()
+    cache.check()
+
+    cache = ClipCache(2, 1, 64, 16, 4, 3, 8)
+    cache.begin_step(ints([0]), ints([9]))
+    cache.attend(0, x[:1, :, :8], x[:1, :, :8], x[:1, :, :8])
+    cache.attend(1, x[:1], x[:1], x[:1])
+    cache.branch([0, 0], [0, 1])          # 0 is not empty
+    cache.drop([2, 3])
+    cache.compact()
+    with pytest.raises(av.AvsaError, match="attention.*fork.*free") as e:
+        cache.check()
+    assert e.value.status == av.AVSA_ERR_BAD_TABLE and "extend" not in str(e.value) and "compact" not in str(e.value)
+    cache.check()
+
+
+@gpu
+@pytest.mark.parametrize("B,L,H,Hkv,page,tokens,most", WAYS)
+def test_log_of_the_attention(B, L, H, Hkv, page, tokens, most):
+    """Whatever kernel finds it: the first error stays, with the status record's words."""
+    shared = tokens // page
+    lengths = list(most) if isinstance(most, tuple) else [tokens + most] * B
+    q, k, v, table, length = attention_case(B, H, Hkv, L, 64, page, lengths, shared=shared, seed=B)
+    log, n = torch.zeros(4, dtype=torch.int32, device="cuda"), length.copy()
+    call = lambda length, log: av.avsa_prefix_attn(q, k, v, cu(table), cu(length), prefix_pages=shared, log=log)[2]
+    assert status(call(length, log)) == av.AVSA_OK and log.tolist() == [0] * 4
+    n[-1] = -7
+    code, detail = av.avsa_read_status(call(n, log))
+    assert log.tolist() == [code, *detail] and code == av.AVSA_ERR_BAD_TABLE
+    call(length, log)
+    assert log.tolist() == [code, *detail]
+    mine = ints([av.AVSA_ERR_NO_PAGES, 1, 2, 3])
+    call(n, mine)
+    assert mine.tolist() == [av.AVSA_ERR_NO_PAGES, 1, 2, 3]
+
+
+@gpu
+@pytest.mark.parametrize("pages", [6, 20000])
+def test_log_of_the_cache_calls(pages):
+    """A CTA's own work and a cluster's; free, fork, extend and compact one after the other."""
+    pool = torch.zeros((1, pages, 1, 16, 64), dtype=torch.bfloat16, device="cuda")
+    ref = np.zeros(pages, np.int32)
+    ref[[2, 5]] = 1
+    state = lambda bad=False: (ints([[2, pages if bad else 5], [-1, -1]]), ints([20, 0]), cu(ref))
+    calls = {"free": lambda bad, **kw: av.avsa_cache_free(*state(bad), ints([0]), **kw)[3],
+             "fork": lambda bad, **kw: av.avsa_cache_fork(pool, *state(bad), ints([0]), ints([1]), **kw)[3],
+             "extend": lambda bad, **kw: av.avsa_cache_extend(*state(), ints([1]), ints([100 if bad else 3]), 16, **kw)[3],
+             "compact": lambda bad, **kw: av.avsa_cache_compact(pool, *state(bad), **kw)[1]}
+    for name, call in calls.items():
+        log = torch.zeros(4, dtype=torch.int32, device="cuda")
+        assert status(call(False, log=log)) == av.AVSA_OK and log.tolist() == [0] * 4, name
+        code, detail = av.avsa_read_status(call(True, log=log))
+        assert code != av.AVSA_OK and log.tolist() == [code, *detail], name
+        for again in calls.values():
+            again(False, log=log)
+            again(True, log=log)
+        assert log.tolist() == [code, *detail], name
+
+
+def test_logs_that_are_refused():
+    """Off their grid, or a part of what a call reads or writes."""
+    lib, t = av.load_library(), av._Bf16Tensor4(1 << 24, 2 * 64 * 64, 64 * 64, 64)
+    state = dict(table=1 << 20, length=2 << 20, ref=3 << 20, table_out=4 << 20, length_out=5 << 20, ref_out=6 << 20, seqs=4, width=8, pages=100, page=16)
+    c, p, big = av._Cache(**state), av._Pages(ptr=1 << 24, planes=2, page_bytes=4096, stride_plane=409600, stride_page=4096), (1 << 16, 1 << 30, 0)
+    for log in (8194, (1 << 20) + 4, (2 << 20) - 12, (6 << 20) + 396):
+        assert lib.avsa_cache_extend_step(c, 8192, 16384, 2, None, log, *big) == av.AVSA_ERR_INVALID_ARG, log
+        assert lib.avsa_cache_fork_step(c, p, 8192, 16384, 2, log, *big) == av.AVSA_ERR_INVALID_ARG, log
+        assert lib.avsa_cache_free_step(c, 8192, 2, log, *big) == av.AVSA_ERR_INVALID_ARG, log
+        assert lib.avsa_cache_compact_step(c, p, 8192, log, *big) == av.AVSA_ERR_INVALID_ARG, log
+    assert lib.avsa_prefix_attn_step(4, 4, 2, 3, 64, 64, 10, 4, 8, t, t, t, 8192, 8192, None, None, 2, 0, 0.0, 1 << 25, None, 8194, 1 << 16, 1 << 40,
+                                     0) == av.AVSA_ERR_INVALID_ARG
+
+
+@gpu
+def test_wrappers_refuse_other_logs():
+    i, t, ref = ints([0] * 4), ints([[0, 0]] * 4), ints([0] * 5)
+    for log in (ints([0] * 3), torch.zeros(4, device="cuda"), ints([[0] * 4])):
+        with pytest.raises(ValueError, match="log"):
+            av.avsa_cache_free(t, i, ref, i, log=log)
+        with pytest.raises(ValueError, match="log"):
+            av.avsa_cache_extend(t, i, ref, i, i, 16, log=log)
