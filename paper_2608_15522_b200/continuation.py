@@ -44,6 +44,7 @@ class ClipCache:
         self.length = torch.zeros(seqs, dtype=torch.int32, device=device)
         self.ref = torch.zeros(pages, dtype=torch.int32, device=device)
         self._step = None          # sequences of the step under way, and the tokens that each of them was granted
+        self._tokens = 0           # the most of them, where they came in lists
         self._ws = {}              # without a log: the last call's workspace, by kind
 
     def ints(self, x) -> torch.Tensor:
@@ -57,7 +58,10 @@ class ClipCache:
             self._ws[kind] = ws
 
     def begin_step(self, seq: Sequence[int], count: Sequence[int]) -> None:
-        """Room for count[k] more tokens in sequence seq[k]; ``attend`` then writes and attends, layer by layer."""
+        """Room for count[k] more tokens in sequence seq[k]; ``attend`` then writes and attends, layer by layer, with at least so many tokens (where they were
+        fewer, and seq or count is a tensor, ``check`` says it)."""
+        lists = not (isinstance(seq, torch.Tensor) or isinstance(count, torch.Tensor))
+        self._tokens = max((c for s, c in zip(seq, count) if s >= 0), default=0) if lists else 0
         seq, count = self.ints(seq), self.ints(count)
         granted = {"granted": torch.empty_like(count)} if self._grants else {}
         self._keep("extend", self.calls.avsa_cache_extend(*self._state(), seq, count, self.page, **granted, **self._log["extend"])[3])
@@ -69,6 +73,8 @@ class ClipCache:
         ones.  Returns o."""
         if self._step is None:
             raise ValueError("begin_step first")
+        if k_new.shape[2] < self._tokens:
+            raise ValueError(f"{k_new.shape[2]} tokens, where begin_step made room for {self._tokens}")
         seq, count = self._step
         k, v = self.pool[2 * layer], self.pool[2 * layer + 1]
         self.calls.avsa_cache_write(k_new, v_new, k, v, self.table, self.length, seq, count)

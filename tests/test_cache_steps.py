@@ -391,3 +391,36 @@ def test_wrappers_refuse_other_logs():
             av.avsa_cache_free(t, i, ref, i, log=log)
         with pytest.raises(ValueError, match="log"):
             av.avsa_cache_extend(t, i, ref, i, i, 16, log=log)
+
+
+# ------------------------------------------------------------------------------------------------ fewer tokens than there is room for
+@pytest.mark.parametrize("where", WHERE)
+def test_a_step_of_fewer_tokens_than_it_made_room_for(where):
+    """Counts in a list are looked at before anything is written."""
+    cache = ClipCache(1, 1, 64, 16, 8, 2, 8, device=where, calls=LogCalls() if where == "cpu" else None)
+    x = torch.ones((2, 1, 5, 64), dtype=torch.bfloat16, device=where)
+    cache.begin_step([0, 1], [6, 2])
+    before = cache.pool.view(torch.int16).clone()
+    with pytest.raises(ValueError, match="5 tokens.*room for 6"):
+        cache.attend(0, x, x, x)
+    assert torch.equal(cache.pool.view(torch.int16), before)
+    x = torch.ones((2, 1, 6, 64), dtype=torch.bfloat16, device=where)
+    assert (cache.attend(0, x, x, x) == 1).all()
+    cache.begin_step([0, -1], [1, 99])          # an entry that is left out needs none
+    cache.attend(0, x, x, x)
+    cache.begin_step([], [])
+    cache.check()
+
+
+@gpu
+def test_a_tensor_of_more_counts_than_tokens_is_reported():
+    cache = ClipCache(1, 1, 64, 16, 8, 2, 8)
+    x = torch.ones((2, 1, 5, 64), dtype=torch.bfloat16, device="cuda")
+    for count, good in (([5, 2], True), ([6, 2], False)):
+        cache.begin_step(ints([0, 1]), ints(count))
+        cache.attend(0, x, x, x, causal=True)
+        if good:
+            cache.check()
+        else:
+            with pytest.raises(av.AvsaError, match="attention"):
+                cache.check()
