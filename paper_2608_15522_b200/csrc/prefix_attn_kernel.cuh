@@ -964,7 +964,9 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
             m_max = fmaxf(m_max, mx);
             continue;
           }
-          m_ref = mx == -INFINITY ? 0.f : mx;      // (a row that sees nothing here sees nothing in later tiles either)
+          // a row that sees nothing here sees nothing in later tiles either; one that does, but nothing with a weight, has no reference for them
+          m_ref = mx == -INFINITY ? 0.f : mx;
+          if (mx == -INFINITY && rel > 0 && row < it.nrows) misc[kPxFlag + (n & 1)] = 1;
           mref_s[row] = m_ref;
           mbar_arrive(BAR(MREF));
         } else if (run == 0 && t == 1) {
