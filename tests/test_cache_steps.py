@@ -424,3 +424,31 @@ def test_a_tensor_of_more_counts_than_tokens_is_reported():
         else:
             with pytest.raises(av.AvsaError, match="attention"):
                 cache.check()
+
+
+# ------------------------------------------------------------------------------------------------ several passes over the tokens of a step
+@pytest.mark.parametrize("where", WHERE)
+@pytest.mark.parametrize("causal", [False, True])
+def test_passes_of_a_step_replace_its_tokens(where, causal):
+    """One begin_step, attend once for every denoising pass: each pass sees the beginning and its own tokens, the last one's stay."""
+    page, d, H, Hkv, L = 16, 64, 4, 2, 21
+    cache = ClipCache(2, Hkv, d, page, 20, 3, 8, device=where, calls=LogCalls() if where == "cpu" else None)
+    gen = torch.Generator().manual_seed(3)
+    draw = lambda h, n, L: torch.randn((n, h, L, d), generator=gen).bfloat16()
+    attend = lambda layer, x, shared=0: cache.attend(layer, *(t.to(where) for t in x), shared, causal).cpu()
+    old = [[draw(h, 1, 40) for h in (H, Hkv, Hkv)] for _ in range(2)]
+    cache.begin_step([0], [40])
+    for layer in range(2):
+        attend(layer, old[layer])
+    cache.branch([0, 0], [1, 2])
+    cache.begin_step([0, 1, 2], [L, L, 4])
+    for _ in range(3):
+        for layer in range(2):
+            x = [draw(h, 3, L) for h in (H, Hkv, Hkv)]
+            o = attend(layer, x, 2)
+            for b, c in enumerate((L, L, 4)):
+                k, v = (torch.cat([a[0], y[b, :, :c]], 1) for a, y in zip(old[layer][1:], x[1:]))
+                lim = [40 + i + 1 if causal else 40 + c for i in range(c)]
+                close_o(o[b][:, :c].double().numpy(), plain_rows(x[0][b][:, :c], k, v, lim).numpy(), f"sequence {b}, layer {layer}")
+    cache.check()
+    assert cache.length.tolist() == [40 + L, 40 + L, 44]
