@@ -285,11 +285,14 @@ AVSA_API int avsa_build_block_mask_static(int B, int H, int N, int d, int blk, a
  *                   sequence: all it has).  Where it costs less they are read once for the whole batch, all its queries stacked on
  *                   each other; the longest sequence's row of the table then says which pages they are.  0: nothing is shared.
  *
- * What pages hold behind a sequence's last token is never used (it may be anything, NaN too).  Values of tokens that a
- * causal row must not see have to be finite.  A page of the table out of range reads as zeros and sets AVSA_ERR_BAD_TABLE, a
+ * What pages hold behind the last token of the longest sequence that has them is never used (it may be anything, NaN too).  Values of tokens that some rows
+ * of a call see and others must not have to be finite (their weight is 0, and 0 times an infinity is no number): those behind a causal row's limit, and those in
+ * the shared pages that a sequence of the batch ends in front of.  A page of the table out of range reads as zeros and sets AVSA_ERR_BAD_TABLE, a
  * length beyond the table's width is cut there and sets it as well.
  * d is 64 or 128, H a multiple of Hkv, H/Hkv at most 128.  table has `seqs` rows of `width` entries.  o overlaps no input.  Rows that outgrow the maximum of
- * their first key tile are run again as in the other attention calls (up to 32 query rows a key head take a running maximum instead).  Same bits on every run.
+ * their first key tile, or that see keys there but none with a logit above -inf, are run again as in the other attention calls (up to 32 query rows a key head
+ * take a running maximum instead).  Same bits on every run.
+ * There is no backward pass: a cache is read by generation alone.
  */
 #define AVSA_CAUSAL 1u
 AVSA_API int avsa_prefix_attn(int B, int H, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d q,

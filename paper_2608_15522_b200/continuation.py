@@ -4,7 +4,9 @@ A generation that continues a clip chunk by chunk attends to everything it has p
 all layers (one pool of pages, a table of pages for each candidate) and sequences the library's calls: candidates begin as branches that
 share the pages of the beginning, every step writes the new tokens of each and attends to the beginning (read once for all of them)
 and to the candidate's own continuation, rejected candidates give their pages back, and the pool is compacted so that its end
-can be handed on.  Of ``ClipCache`` only ``check`` waits for the GPU.
+can be handed on.  A chunk that takes several passes (the denoising steps of a diffusion model) begins its step once and attends in every pass: each one's
+tokens replace those of the pass before.  Of ``ClipCache`` only ``check`` waits for the GPU, and whatever is given sequence numbers or counts in a list, for the
+copy of it; int32 tensors on the device are taken as they are.
 
     python -m paper_2608_15522_b200.continuation        # a toy generator on random weights: branch, grow, prune, compact
 """

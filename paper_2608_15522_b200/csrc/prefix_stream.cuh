@@ -439,7 +439,7 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
     }
   }
   if (!ok) {
-    // a load never came: the rows are left as they are, and what is under way lands before this memory is given away
+    // a load never came: the status says so, the rows lack this warp's keys from there on, and what is under way lands before this memory is given away
     report_logged(p.status, p.log, AVSA_ERR_TIMEOUT, kPxKFull, item, blk);
     for (int k = 0; k < STAGES; k++) mbar_wait(full + k * 8, (round + (k < stage ? 1 : 0)) & 1);
   }
