@@ -40,6 +40,7 @@ class ClipCache:
         # the first error of each kind of call since the last check(), which replays of a captured step report as well
         self._errors = torch.zeros((len(kinds), 4), dtype=torch.int32, device=device)
         self._log = {kind: {"log": log} if takes(call, "log") else {} for (kind, call), log in zip(kinds.items(), self._errors)}
+        self._attention = self._log["attention"]          # what the step under way gives the attention besides
         # plane 2i: keys of layer i, plane 2i + 1: its values (what no token has been written to is never used)
         self.pool = torch.empty((2 * layers, pages, heads, page, d), dtype=torch.bfloat16, device=device)
         self.table = torch.full((seqs, width), -1, dtype=torch.int32, device=device)
@@ -67,7 +68,9 @@ class ClipCache:
         seq, count = self.ints(seq), self.ints(count)
         granted = {"granted": torch.empty_like(count)} if self._grants else {}
         self._keep("extend", self.calls.avsa_cache_extend(*self._state(), seq, count, self.page, **granted, **self._log["extend"])[3])
-        self._step = (seq, granted.get("granted", count))
+        self._step = seq, count = seq, granted.get("granted", count)
+        if self._counts:
+            self._attention = {"count": count, **self._log["attention"]}
 
     def attend(self, layer: int, q, k_new, v_new, prefix_pages: int = 0, causal: bool = False, softmax_scale: float = 0.0):
         """One layer of the step: the first count[k] of the L tokens of k_new/v_new [n,Hkv,L,d] go into the pages, q [n,H,L,d] attends to all tokens of its
@@ -75,15 +78,15 @@ class ClipCache:
         ones.  Returns o."""
         if self._step is None:
             raise ValueError("begin_step first")
-        if k_new.shape[2] < self._tokens:
+        if self._tokens and k_new.shape[2] < self._tokens:
             raise ValueError(f"{k_new.shape[2]} tokens, where begin_step made room for {self._tokens}")
         seq, count = self._step
         k, v = self.pool[2 * layer], self.pool[2 * layer + 1]
         self.calls.avsa_cache_write(k_new, v_new, k, v, self.table, self.length, seq, count)
-        more = {"count": count} if self._counts else {}
         o, _, ws = self.calls.avsa_prefix_attn(q, k, v, self.table, self.length, prefix_pages=prefix_pages, seq=seq, causal=causal,
-                                               softmax_scale=softmax_scale, **more, **self._log["attention"])
-        self._keep("attention", ws)
+                                               softmax_scale=softmax_scale, **self._attention)
+        if "log" not in self._attention:
+            self._ws["attention"] = ws
         return o
 
     def branch(self, parent: Sequence[int], child: Sequence[int]) -> None:
