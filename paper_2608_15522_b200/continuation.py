@@ -19,6 +19,14 @@ from typing import Optional, Sequence
 import torch
 
 
+def _takes(call, name: str) -> bool:
+    """Whether a call has a parameter of this name."""
+    try:
+        return name in inspect.signature(call).parameters
+    except (TypeError, ValueError):          # there is no such call, or it does not say
+        return False
+
+
 class ClipCache:
     """Keys and values of up to ``seqs`` candidates of up to ``width`` pages each, for ``layers`` layers.
 
@@ -33,13 +41,13 @@ class ClipCache:
         if calls is None:
             from . import binding as calls
         self.calls, self.layers, self.page = calls, layers, page
-        takes = lambda call, name: name in inspect.signature(call).parameters
-        self._grants, self._counts = takes(calls.avsa_cache_extend, "granted"), takes(calls.avsa_prefix_attn, "count")
-        kinds = {"extend": calls.avsa_cache_extend, "attention": calls.avsa_prefix_attn, "fork": calls.avsa_cache_fork, "free": calls.avsa_cache_free,
-                 "compact": calls.avsa_cache_compact}
+        kinds = {"extend": "avsa_cache_extend", "attention": "avsa_prefix_attn", "fork": "avsa_cache_fork", "free": "avsa_cache_free",
+                 "compact": "avsa_cache_compact"}
+        kinds = {kind: getattr(calls, name, None) for kind, name in kinds.items()}
+        self._grants, self._counts = _takes(kinds["extend"], "granted"), _takes(kinds["attention"], "count")
         # the first error of each kind of call since the last check(), which replays of a captured step report as well
         self._errors = torch.zeros((len(kinds), 4), dtype=torch.int32, device=device)
-        self._log = {kind: {"log": log} if takes(call, "log") else {} for (kind, call), log in zip(kinds.items(), self._errors)}
+        self._log = {kind: {"log": log} if _takes(call, "log") else {} for (kind, call), log in zip(kinds.items(), self._errors)}
         self._attention = self._log["attention"]          # what the step under way gives the attention besides
         # plane 2i: keys of layer i, plane 2i + 1: its values (what no token has been written to is never used)
         self.pool = torch.empty((2 * layers, pages, heads, page, d), dtype=torch.bfloat16, device=device)

@@ -452,3 +452,17 @@ def test_passes_of_a_step_replace_its_tokens(where, causal):
                 close_o(o[b][:, :c].double().numpy(), plain_rows(x[0][b][:, :c], k, v, lim).numpy(), f"sequence {b}, layer {layer}")
     cache.check()
     assert cache.length.tolist() == [40 + L, 40 + L, 44]
+
+
+def test_stand_ins_of_some_calls_alone():
+    """Calls that are not there, or that do not say what they take, are missed when they are made."""
+    class Some:
+        avsa_cache_extend = staticmethod(lambda *a: (*a[:3], av.AVSA_OK))
+        avsa_cache_free = print          # (a builtin)
+        avsa_read_status = staticmethod(lambda ws: (ws, (0, 0, 0)))
+
+    cache = ClipCache(1, 1, 64, 16, 4, 2, 4, device="cpu", calls=Some())
+    cache.begin_step([0], [3])
+    cache.check()
+    with pytest.raises(AttributeError):
+        cache.branch([0], [1])
