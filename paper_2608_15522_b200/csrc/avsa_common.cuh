@@ -25,18 +25,19 @@ struct StatusRecord {
 };
 constexpr size_t kStatusBytes = 256;   // the record, padded so that what follows stays 256-byte aligned
 
-__device__ __forceinline__ void report_status(StatusRecord* st, int code, int where, int item, int aux) {
-  if (atomicCAS(&st->code, 0, code) == 0) {
-    st->where = where;
-    st->item = item;
-    st->aux = aux;
-  }
+// The record keeps a call's first error; whether it was this one.
+__device__ __forceinline__ bool report_status(StatusRecord* st, int code, int where, int item, int aux) {
+  if (atomicCAS(&st->code, 0, code) != 0) return false;
+  st->where = where;
+  st->item = item;
+  st->aux = aux;
+  return true;
 }
 
-// The same, and the first error since the caller last cleared it into a record of the caller's own (int32 [4]: code, where, item, aux; NULL: none).
+// The same, and into a record of the caller's own (int32 [4]: code, where, item, aux; NULL: none) the first error that the status records of all its calls have had
+// since the caller cleared it.
 __device__ __forceinline__ void report_logged(StatusRecord* st, int32_t* log, int code, int where, int item, int aux) {
-  report_status(st, code, where, item, aux);
-  if (log != nullptr && atomicCAS(log, 0, code) == 0) {
+  if (report_status(st, code, where, item, aux) && log != nullptr && atomicCAS(log, 0, code) == 0) {
     log[1] = where;
     log[2] = item;
     log[3] = aux;

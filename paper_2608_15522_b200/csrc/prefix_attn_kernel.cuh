@@ -1201,12 +1201,8 @@ __global__ void __launch_bounds__(kPxMergeThreads) prefix_merge_kernel(const __g
     const unsigned who = __ballot_sync(0xffffffffu, err.x != 0);
     const int from = who ? __ffs(who) - 1 : 0;
     if (lane == from) {
-      p.status->code = err.x;
-      p.status->where = err.y;
-      p.status->item = err.z;
-      p.status->aux = err.w;
+      p.status->code = p.status->where = p.status->item = p.status->aux = p.status->next_item = 0;
       p.status->redo_count = again;
-      p.status->next_item = 0;
       if (err.x != 0) report_logged(p.status, p.log, err.x, err.y, err.z, err.w);
     }
   }

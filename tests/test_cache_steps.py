@@ -369,6 +369,19 @@ def test_log_of_the_cache_calls(pages):
         assert log.tolist() == [code, *detail], name
 
 
+@gpu
+@pytest.mark.parametrize("seqs,pages", [(900, 50), (900, 20000)])
+def test_log_of_many_errors_at_once(seqs, pages):
+    """Of errors that hundreds of threads report at the same time the log has the one that the status record has."""
+    table, length, ref = (torch.full((seqs, 4), -1, dtype=torch.int32, device="cuda"), ints([0] * seqs), ints([0] * pages))
+    for k in range(40):
+        log = torch.zeros(4, dtype=torch.int32, device="cuda")
+        count = ints([(-1, 70, 64, 30)[(s * 7 + k) % 4] for s in range(seqs)])          # below 0, beyond the row, beyond the pool or not
+        ws = av.avsa_cache_extend(table.clone(), length.clone(), ref.clone(), ints(list(range(seqs))), count, 16, log=log)[3]
+        code, detail = av.avsa_read_status(ws)
+        assert code != av.AVSA_OK and log.tolist() == [code, *detail]
+
+
 def test_logs_that_are_refused():
     """Off their grid, or a part of what a call reads or writes."""
     lib, t = av.load_library(), av._Bf16Tensor4(1 << 24, 2 * 64 * 64, 64 * 64, 64)
