@@ -113,6 +113,24 @@ typedef struct {
   int64_t page_bytes, stride_plane, stride_page;
 } avsa_pages;
 
+/*
+ * Pages of keys, or of values, held in 4 bits.  A page of a key/value head is one piece of page * (d/2 + d/16) bytes; pages are stride_page bytes apart and
+ * heads stride_head, multiples of 16, as is ptr.  For each 16 tokens there are 16 x d/2 bytes of codes, then 16 x d/32 scales (bf16).  32 channels
+ * of a token share a scale, the nearest number of five significant bits to their largest magnitude over 7 (halfway: the larger one), and each has a code,
+ * the nearest whole number of scales (halfway: the even one), -7 .. 7, so that every value that a page stands for is a bf16 number.  A token's codes are little-endian words
+ * of eight channels, code + 8 of channel 2i at bits 4i, of channel 2i + 1 at bits 16 + 4i.
+ * A group of channels whose largest magnitude is below 2^-100 is held as zeros; one with an infinity, a NaN or a magnitude of 2^125 and more reads as NaN.
+ */
+typedef struct {
+  void* ptr;
+  int64_t stride_page, stride_head;
+} avsa_q4_pool;
+
+/* flags of avsa_rope */
+#define AVSA_ROPE_HALVES 1u    /* the pairs are channels (i, i + d/2), not (2i, 2i + 1) */
+#define AVSA_ROPE_INVERSE 2u   /* turns back: the inverse, and the gradient */
+#define AVSA_ROPE_AXES 4       /* at most */
+
 /* flags of avsa_build_block_mask */
 #define AVSA_PROTECT_ROWS 1u            /* Eq. 9: a protected query block keeps every key block */
 #define AVSA_PROTECT_COLS 2u            /* opt-in superset: protected key blocks visible to all rows */
@@ -345,6 +363,45 @@ AVSA_API int avsa_cache_fork_step(avsa_cache c, avsa_pages pool, const int32_t* 
 AVSA_API int avsa_cache_free_step(avsa_cache c, const int32_t* seq, int n, int32_t* log, void* ws, size_t ws_bytes, void* stream);
 AVSA_API int avsa_cache_compact_step(avsa_cache c, avsa_pages pool, int32_t* n_live, int32_t* log, void* ws, size_t ws_bytes, void* stream);
 AVSA_API size_t avsa_cache_workspace_bytes(int seqs, int pages, int n);
+
+/*
+ * (8) A paged cache held in 4 bits: the same table, length, ref and list calls (avsa_cache_extend, _fork, _free, _compact with page_bytes of such pages), and these
+ * in the places of avsa_cache_write and avsa_prefix_attn_step.  Arguments that have their names mean what they mean there.
+ *
+ * avsa_cache_write_q4 quantises the new tokens into the pages.  A list names no sequence twice.
+ * avsa_cache_read_q4  the last count[k] tokens of sequence seq[k] (count NULL: T of them) become the first count[k] (0..T) tokens of k and v [n,Hkv,T,d], exactly.
+ *                     Tokens that there are not (behind count[k], in front of the sequence's first, without a page) are zeros.
+ * avsa_prefix_attn_q4 attention on the values that the pages stand for.  Where a sequence and key head has more than 32 query rows, or a shared beginning read for
+ *                     the batch at once more than 32 stacked ones, the pages that the batch reads are first made bf16 in the workspace, which has room
+ *                     for one layer's (2 * pages * Hkv * page * d of bf16); it may be the same one for all layers.
+ *
+ * Neither a write nor a read needs a workspace or leaves a status.
+ */
+AVSA_API int avsa_cache_write_q4(int n, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d k_new, avsa_bf16_4d v_new,
+                                 avsa_q4_pool k_pool, avsa_q4_pool v_pool, const int32_t* table, const int32_t* length, const int32_t* seq,
+                                 const int32_t* count, void* stream);
+AVSA_API int avsa_cache_read_q4(int n, int Hkv, int T, int d, int page, int pages, int seqs, int width, avsa_q4_pool k_pool, avsa_q4_pool v_pool,
+                                const int32_t* table, const int32_t* length, const int32_t* seq, const int32_t* count, avsa_bf16_4d k, avsa_bf16_4d v,
+                                void* stream);
+AVSA_API int avsa_prefix_attn_q4(int B, int H, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d q, avsa_q4_pool k_pool,
+                                 avsa_q4_pool v_pool, const int32_t* table, const int32_t* length, const int32_t* seq, const int32_t* count,
+                                 int prefix_pages, unsigned flags, float softmax_scale, void* o_bf16, float* lse, int32_t* log, void* ws,
+                                 size_t ws_bytes, void* stream);
+AVSA_API size_t avsa_prefix_attn_q4_workspace_bytes(int B, int H, int Hkv, int L, int d, int page, int pages, int width, int prefix_pages);
+
+/*
+ * (9) Rotary positions with several axes (time, height, width): pair i of a head's channels turns by the angle 2 pi * pos[b,n,axis] * freq[i],
+ *
+ *   (y_a, y_b) = (x_a cos - x_b sin, x_a sin + x_b cos)
+ *
+ * for the queries q [B,H,N,d] and keys k [B,Hk,N,d] of the same tokens in one call (H or Hk 0: not there, its pointers are not looked at).
+ *   pos       int32 [B,N,axes], contiguous but for the distance pos_stride_b of batch entries (in elements; 0: all have the same)
+ *   sections  host int [axes]: channel pairs of each axis, d/2 in all; pair i belongs to the axis whose section it falls in
+ *   freq      fp64 [d/2], 8-byte aligned: turns of each pair for a step along its axis (base^(-2i/n) / (2 pi) for the i-th of an axis of n channels; 0: never turned)
+ * An output is its input (in place, same strides) or overlaps none.  d is 64 or 128, and neither needs a workspace or leaves a status.
+ */
+AVSA_API int avsa_rope(int B, int H, int Hk, int N, int d, avsa_bf16_4d q, avsa_bf16_4d k, avsa_bf16_4d q_out, avsa_bf16_4d k_out, const int32_t* pos,
+                       int64_t pos_stride_b, int axes, const int* sections, const double* freq, unsigned flags, void* stream);
 
 /* Host integer ceil(pct/100 * n): the count forms of rho and kappa (Eq. 8's ceiling). */
 AVSA_API int avsa_count_from_percent(int pct, int n);

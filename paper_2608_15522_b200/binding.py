@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 import importlib.machinery
 import importlib.util
+import math
 import os
 from typing import Optional, Tuple
 
@@ -53,6 +54,7 @@ EXPORTS = (
     "avsa_prefix_attn", "avsa_prefix_attn_step", "avsa_prefix_attn_workspace_bytes",
     "avsa_cache_extend", "avsa_cache_extend_step", "avsa_cache_write", "avsa_cache_fork", "avsa_cache_fork_step", "avsa_cache_free",
     "avsa_cache_free_step", "avsa_cache_compact", "avsa_cache_compact_step", "avsa_cache_workspace_bytes",
+    "avsa_prefix_attn_q4", "avsa_prefix_attn_q4_workspace_bytes", "avsa_cache_write_q4", "avsa_cache_read_q4", "avsa_rope",
     "avsa_count_from_percent", "avsa_read_status", "avsa_selftest_bounded_wait", "avsa_status_string", "avsa_version",
 )
 
@@ -76,6 +78,10 @@ class _Cache(ctypes.Structure):
 class _Pages(ctypes.Structure):
     _fields_ = [("ptr", ctypes.c_void_p), ("planes", ctypes.c_int), ("page_bytes", ctypes.c_int64), ("stride_plane", ctypes.c_int64),
                 ("stride_page", ctypes.c_int64)]
+
+
+class _Q4Pool(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("stride_page", ctypes.c_int64), ("stride_head", ctypes.c_int64)]
 
 
 _lib = None
@@ -132,7 +138,8 @@ def _cache():
         lib = load_library()
         module = _extension("_avsa_cache")
         entries = ("avsa_prefix_attn_step", "avsa_prefix_attn_workspace_bytes", "avsa_cache_extend_step", "avsa_cache_write",
-                   "avsa_cache_fork_step", "avsa_cache_free_step", "avsa_cache_compact_step", "avsa_cache_workspace_bytes")
+                   "avsa_cache_fork_step", "avsa_cache_free_step", "avsa_cache_compact_step", "avsa_cache_workspace_bytes",
+                   "avsa_prefix_attn_q4", "avsa_prefix_attn_q4_workspace_bytes", "avsa_cache_write_q4", "avsa_cache_read_q4", "avsa_rope")
         module.bind(*(ctypes.cast(getattr(lib, e), ctypes.c_void_p).value for e in entries),
                     getattr(torch._C, "_cuda_getCurrentRawStream", None))
         _cache_module = module
@@ -198,6 +205,16 @@ def load_library() -> ctypes.CDLL:
     lib.avsa_cache_compact_step.restype = i
     lib.avsa_cache_workspace_bytes.argtypes = [i, i, i]
     lib.avsa_cache_workspace_bytes.restype = sz
+    lib.avsa_prefix_attn_q4.argtypes = [i, i, i, i, i, i, i, i, i, T, _Q4Pool, _Q4Pool, vp, vp, vp, vp, i, u, f, vp, vp, vp, vp, sz, vp]
+    lib.avsa_prefix_attn_q4.restype = i
+    lib.avsa_prefix_attn_q4_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i, i]
+    lib.avsa_prefix_attn_q4_workspace_bytes.restype = sz
+    lib.avsa_cache_write_q4.argtypes = [i, i, i, i, i, i, i, i, T, T, _Q4Pool, _Q4Pool, vp, vp, vp, vp, vp]
+    lib.avsa_cache_write_q4.restype = i
+    lib.avsa_cache_read_q4.argtypes = [i, i, i, i, i, i, i, i, _Q4Pool, _Q4Pool, vp, vp, vp, vp, T, T, vp]
+    lib.avsa_cache_read_q4.restype = i
+    lib.avsa_rope.argtypes = [i, i, i, i, i, T, T, T, T, vp, ctypes.c_int64, i, ctypes.POINTER(i), vp, u, vp]
+    lib.avsa_rope.restype = i
     lib.avsa_count_from_percent.argtypes = [i, i]
     lib.avsa_count_from_percent.restype = i
     lib.avsa_read_status.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_int)]
@@ -545,4 +562,68 @@ def avsa_cache_compact(pool, table, length, ref, out=None, n_live=None, ws=None,
     done = (_cache_module or _cache()).compact(pool, table, length, ref, *(out or (None, None, None)), n_live, ws, log)
     if done[0] != AVSA_OK:
         raise AvsaError(done[0], "avsa_cache_compact")
+    return done[1:]
+
+
+# ------------------------------------------------------------------------------------------------
+# paged cache held in 4 bits
+#
+# Pools are uint8 [pages,Hkv,page,q4_token_bytes(d)], a page of a head in one piece; extend, free, and fork and compact (with such a pool of several planes) are
+# those of the bf16 cache.
+# ------------------------------------------------------------------------------------------------
+def q4_token_bytes(d: int) -> int:
+    """Bytes that a token has in a page of a head: codes of 4 bits, and a bf16 scale for each 32 channels."""
+    if d not in (64, 128):
+        raise ValueError("d is 64 or 128")
+    return d // 2 + d // 16
+
+
+def avsa_cache_write_q4(k_new, v_new, k_pool, v_pool, table, length, seq=None, count=None):
+    """avsa_cache_write into pages held in 4 bits: 32 channels of a token share a scale, max|x| / 7 to five significant bits, and each becomes the nearest
+    whole number of scales."""
+    st = (_cache_module or _cache()).write_q4(k_new, v_new, k_pool, v_pool, table, length, seq, count)
+    if st != AVSA_OK:
+        raise AvsaError(st, "avsa_cache_write_q4")
+
+
+def avsa_cache_read_q4(k_pool, v_pool, table, length, tokens, seq=None, count=None, k=None, v=None):
+    """The last count[k] (None: ``tokens``) tokens of sequence seq[k] (None: of every sequence) as the pages have them, exactly.
+
+    Returns (k, v) bf16 [n,Hkv,tokens,d]; tokens that there are not are zeros."""
+    done = (_cache_module or _cache()).read_q4(k_pool, v_pool, table, length, tokens, seq, count, k, v)
+    if done[0] != AVSA_OK:
+        raise AvsaError(done[0], "avsa_cache_read_q4")
+    return done[1:]
+
+
+def avsa_prefix_attn_q4_workspace_bytes(B, H, Hkv, L, d, page, pages, width, prefix_pages) -> int:
+    return int(load_library().avsa_prefix_attn_q4_workspace_bytes(B, H, Hkv, L, d, page, pages, width, prefix_pages))
+
+
+def avsa_prefix_attn_q4(q, k_pool, v_pool, table, length, prefix_pages=0, seq=None, causal=False, softmax_scale=0.0, want_lse=False,
+                        o=None, lse=None, ws=None, count=None, log=None):
+    """avsa_prefix_attn over pages held in 4 bits.  Returns (o, lse or None, ws)."""
+    done = (_cache_module or _cache()).attn_q4(q, k_pool, v_pool, table, length, prefix_pages, seq, causal, softmax_scale, want_lse, o, lse, ws, count, log)
+    if done[0] != AVSA_OK:
+        raise AvsaError(done[0], "avsa_prefix_attn_q4")
+    return done[1:]
+
+
+# ------------------------------------------------------------------------------------------------
+# rotary positions
+# ------------------------------------------------------------------------------------------------
+def avsa_rope_frequencies(sections, base=10000.0, device="cuda") -> torch.Tensor:
+    """``freq`` of avsa_rope: of the n pairs of an axis, pair i makes base^(-i/n) / (2 pi) turns a step.  fp64 [sum(sections)]."""
+    turn = 1.0 / (2.0 * math.pi)
+    return torch.tensor([turn * base ** (-i / n) for n in sections for i in range(n)], dtype=torch.float64, device=device)
+
+
+def avsa_rope(q, k, pos, freq, sections, halves=False, inverse=False, q_out=None, k_out=None):
+    """Rotary positions with several axes: pair i of the channels of q [B,H,N,d] and k [B,Hk,N,d] (or None) turns by 2 pi * pos[b,n,axis] * freq[i].
+
+    pos int32 [B,N,axes] or [N,axes], freq fp64 [d/2] (avsa_rope_frequencies), sections the pairs of each axis.  Pairs are channels (2i, 2i + 1), with halves
+    (i, i + d/2).  inverse turns back; as a rotation's transpose that is its gradient too.  q_out and k_out may be q and k.  Returns (q_out, k_out or None)."""
+    done = (_cache_module or _cache()).rope(q, k, pos, freq, tuple(sections), halves, inverse, q_out, k_out)
+    if done[0] != AVSA_OK:
+        raise AvsaError(done[0], "avsa_rope")
     return done[1:]

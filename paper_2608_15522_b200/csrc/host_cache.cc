@@ -6,6 +6,7 @@
 #include <ATen/ATen.h>
 #include <torch/csrc/utils/object_ptr.h>
 
+#include <algorithm>
 #include <climits>
 
 #include "../../include/avsa.h"
@@ -20,6 +21,11 @@ decltype(&avsa_cache_fork_step) f_fork;
 decltype(&avsa_cache_free_step) f_free;
 decltype(&avsa_cache_compact_step) f_compact;
 decltype(&avsa_cache_workspace_bytes) f_ws;
+decltype(&avsa_prefix_attn_q4) f_attn_q4;
+decltype(&avsa_prefix_attn_q4_workspace_bytes) f_attn_q4_ws;
+decltype(&avsa_cache_write_q4) f_write_q4;
+decltype(&avsa_cache_read_q4) f_read_q4;
+decltype(&avsa_rope) f_rope;
 PyObject* o_raw_stream;
 
 template <typename F>
@@ -138,6 +144,33 @@ View take_view(Call& c, int i, const char* name) {
   return r;
 }
 
+// uint8 [pages,Hkv,page,d/2 + d/16], a page of a head in one piece
+struct PoolQ4 : Arg {
+  int pages, Hkv, page, d;
+  int64_t stride_page, stride_head;
+  operator avsa_q4_pool() const { return avsa_q4_pool{ptr, stride_page, stride_head}; }
+};
+PoolQ4 take_pool_q4(Call& c, int i, const char* name) {
+  const at::Tensor& t = c.tensor(i, name);
+  TORCH_CHECK_VALUE(t.scalar_type() == at::kByte && t.dim() == 4, name, ": expected a uint8 tensor [pages,Hkv,page,d/2 + d/16]");
+  TORCH_CHECK_VALUE(t.size(3) == 36 || t.size(3) == 72, name, ": a token has 36 bytes (64 channels) or 72 (128)");
+  TORCH_CHECK_VALUE(t.stride(3) == 1 && (t.size(2) <= 1 || t.stride(2) == t.size(3)), name, ": a page of a head has to be in one piece");
+  PoolQ4 r;
+  r.pages = size32(t, 0);
+  r.Hkv = size32(t, 1);
+  r.page = size32(t, 2);
+  r.d = t.size(3) == 72 ? 128 : 64;
+  r.stride_page = t.stride(0);
+  r.stride_head = t.stride(1);
+  r.t = t;
+  r.ptr = t.data_ptr();
+  r.numel = t.numel();
+  return r;
+}
+void same_pools(const PoolQ4& k, const PoolQ4& v) {
+  TORCH_CHECK_VALUE(k.pages == v.pages && k.Hkv == v.Hkv && k.page == v.page && k.d == v.d, "k_pool and v_pool have different shapes");
+}
+
 PyObject* result(int status, std::initializer_list<PyObject*> items) {
   PyObject* r = PyTuple_New(static_cast<Py_ssize_t>(items.size()) + 1);
   PyObject* st = PyLong_FromLong(status);
@@ -160,21 +193,38 @@ void arity(Py_ssize_t got, Py_ssize_t want) {
 }
 
 // attn(q, k_pool, v_pool, table, length, prefix_pages, seq, causal, softmax_scale, want_lse, o, lse, ws, count, log) -> (status, o, lse, ws)
-PyObject* py_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+template <bool Q4>
+PyObject* attn(PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   arity(n, 15);
   Call c{a};
-  const View q = take_view(c, 0, "q"), k = take_view(c, 1, "k_pool"), v = take_view(c, 2, "v_pool");
+  const View q = take_view(c, 0, "q");
+  View k, v;
+  PoolQ4 k4, v4;
+  int pages, Hkv, page, pool_d;
+  if constexpr (Q4) {
+    k4 = take_pool_q4(c, 1, "k_pool");
+    v4 = take_pool_q4(c, 2, "v_pool");
+    pages = k4.pages, Hkv = k4.Hkv, page = k4.page, pool_d = k4.d;
+  } else {
+    k = take_view(c, 1, "k_pool");
+    v = take_view(c, 2, "v_pool");
+    pages = k.dim(0), Hkv = k.dim(1), page = k.dim(2), pool_d = k.dim(3);
+  }
   const Arg table = c.ints(3, "table", 2), length = c.ints(4, "length", 1);
   const int prefix_pages = c.integer(5, "prefix_pages");
   const Arg seq = c.ints(6, "seq", 1, true);
   const bool causal = c.flag(7, "causal");
   const float scale = c.number(8, "softmax_scale");
   const bool want_lse = c.flag(9, "want_lse");
-  const int B = q.dim(0), H = q.dim(1), L = q.dim(2), d = q.dim(3), pages = k.dim(0), Hkv = k.dim(1), page = k.dim(2);
+  const int B = q.dim(0), H = q.dim(1), L = q.dim(2), d = q.dim(3);
   const int seqs = size32(table.t, 0), width = size32(table.t, 1);
-  for (int i = 0; i < 4; i++) TORCH_CHECK_VALUE(k.size[i] == v.size[i], "k_pool and v_pool have different shapes");
-  TORCH_CHECK_VALUE(k.dim(3) == d, "q and the pools have different head dimensions");
+  if constexpr (Q4) {
+    same_pools(k4, v4);
+  } else {
+    for (int i = 0; i < 4; i++) TORCH_CHECK_VALUE(k.size[i] == v.size[i], "k_pool and v_pool have different shapes");
+  }
+  TORCH_CHECK_VALUE(pool_d == d, "q and the pools have different head dimensions");
   TORCH_CHECK_VALUE(length.numel == seqs, "length: one entry for each row of the table");
   TORCH_CHECK_VALUE(seq.there() ? seq.numel == B : B <= seqs, "q has more batch entries than there are sequences");
   Arg o, lse;
@@ -200,14 +250,22 @@ PyObject* py_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
       o.ptr = o.t.data_ptr();
     }
     if (want_lse) c.make(lse, at::kFloat, {B, H, L});
-    if (!ws.there()) c.make_ws(ws, f_attn_ws(B, H, Hkv, L, d, page, width, prefix_pages));
-    st = f_attn(B, H, Hkv, L, d, page, pages, seqs, width, q, k, v, table.as<int32_t>(), length.as<int32_t>(), seq.as<int32_t>(),
-                count.as<int32_t>(), prefix_pages, causal ? AVSA_CAUSAL : 0u, scale, o.ptr, lse.as<float>(), log.as<int32_t>(), ws.ptr,
-                static_cast<size_t>(ws.numel), c.stream);
+    if (!ws.there())
+      c.make_ws(ws, Q4 ? f_attn_q4_ws(B, H, Hkv, L, d, page, pages, width, prefix_pages) : f_attn_ws(B, H, Hkv, L, d, page, width, prefix_pages));
+    if constexpr (Q4)
+      st = f_attn_q4(B, H, Hkv, L, d, page, pages, seqs, width, q, k4, v4, table.as<int32_t>(), length.as<int32_t>(), seq.as<int32_t>(),
+                     count.as<int32_t>(), prefix_pages, causal ? AVSA_CAUSAL : 0u, scale, o.ptr, lse.as<float>(), log.as<int32_t>(), ws.ptr,
+                     static_cast<size_t>(ws.numel), c.stream);
+    else
+      st = f_attn(B, H, Hkv, L, d, page, pages, seqs, width, q, k, v, table.as<int32_t>(), length.as<int32_t>(), seq.as<int32_t>(),
+                  count.as<int32_t>(), prefix_pages, causal ? AVSA_CAUSAL : 0u, scale, o.ptr, lse.as<float>(), log.as<int32_t>(), ws.ptr,
+                  static_cast<size_t>(ws.numel), c.stream);
   });
   return result(st, {c.give(10, o), c.give(11, lse), c.give(12, ws)});
   END_HANDLE_TH_ERRORS
 }
+PyObject* py_attn(PyObject*, PyObject* const* a, Py_ssize_t n) { return attn<false>(a, n); }
+PyObject* py_attn_q4(PyObject*, PyObject* const* a, Py_ssize_t n) { return attn<true>(a, n); }
 
 // The state of a cache at arguments [at, at + 3), and the arrays that the state behind the call goes to at [to, to + 3) (None: the same).
 struct State {
@@ -230,18 +288,20 @@ struct State {
 };
 PyObject* wrap(const Arg& r) { return THPVariable_Wrap(r.t); }
 
-// bf16 [planes,pages,Hkv,page,d], a page of a plane in one piece, its heads or its tokens outermost
+// bf16 [planes,pages,Hkv,page,d], or uint8 with the bytes of a token held in 4 bits, a page of a plane in one piece, its heads or (bf16) its tokens outermost
 avsa_pages take_pool(Call& c, int i, int64_t pages, int* page, Arg& hold) {
   const at::Tensor& t = c.tensor(i, "pool");
-  TORCH_CHECK_VALUE(t.scalar_type() == at::kBFloat16 && t.dim() == 5, "pool: expected a bf16 tensor [planes,pages,Hkv,page,d]");
+  const bool codes = t.scalar_type() == at::kByte;
+  TORCH_CHECK_VALUE((codes || t.scalar_type() == at::kBFloat16) && t.dim() == 5, "pool: expected a bf16 tensor [planes,pages,Hkv,page,d], or one of uint8");
   TORCH_CHECK_VALUE(t.size(1) == pages, "pool: as many pages as ref has entries");
   const int64_t h = t.size(2), p = t.size(3), d = t.size(4), sh = t.stride(2), sp = t.stride(3);
   const bool heads_out = (h <= 1 || sh == p * d) && (p <= 1 || sp == d), tokens_out = (p <= 1 || sp == h * d) && (h <= 1 || sh == d);
-  TORCH_CHECK_VALUE((d <= 1 || t.stride(4) == 1) && (heads_out || tokens_out), "pool: a page has to be in one piece");
+  TORCH_CHECK_VALUE((d <= 1 || t.stride(4) == 1) && (heads_out || (tokens_out && !codes)), "pool: a page has to be in one piece");
   *page = size32(t, 3);
   hold.t = t;
   hold.ptr = t.data_ptr();
-  return avsa_pages{hold.ptr, size32(t, 0), h * p * d * 2, t.stride(0) * 2, t.stride(1) * 2};
+  const int64_t bytes = codes ? 1 : 2;
+  return avsa_pages{hold.ptr, size32(t, 0), h * p * d * bytes, t.stride(0) * bytes, t.stride(1) * bytes};
 }
 
 int list_size(const Arg& x, const Arg& y, const char* text) {
@@ -294,6 +354,143 @@ PyObject* py_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
                  seq.as<int32_t>(), count.as<int32_t>(), c.stream);
   });
   return PyLong_FromLong(st);
+  END_HANDLE_TH_ERRORS
+}
+
+// write_q4(k_new, v_new, k_pool, v_pool, table, length, seq, count) -> status
+PyObject* py_write_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  arity(n, 8);
+  Call c{a};
+  const View kn = take_view(c, 0, "k_new"), vn = take_view(c, 1, "v_new");
+  const PoolQ4 k = take_pool_q4(c, 2, "k_pool"), v = take_pool_q4(c, 3, "v_pool");
+  const Arg table = c.ints(4, "table", 2), length = c.ints(5, "length", 1), seq = c.ints(6, "seq", 1, true), count = c.ints(7, "count", 1, true);
+  const int seqs = size32(table.t, 0), width = size32(table.t, 1), entries = kn.dim(0);
+  same_pools(k, v);
+  for (int i = 0; i < 4; i++) TORCH_CHECK_VALUE(kn.size[i] == vn.size[i], "keys and values have different shapes");
+  TORCH_CHECK_VALUE(kn.dim(1) == k.Hkv && kn.dim(3) == k.d, "the new tokens and the pools have different heads");
+  TORCH_CHECK_VALUE(length.numel == seqs, "length: one entry for each row of the table");
+  TORCH_CHECK_VALUE((seq.there() ? seq.numel == entries : entries <= seqs) && (!count.there() || count.numel == entries),
+                    "seq and count: one entry for each of the new tokens' batch entries");
+  c.find_stream();
+  int st;
+  without_lock([&] {
+    st = f_write_q4(entries, k.Hkv, kn.dim(2), k.d, k.page, k.pages, seqs, width, kn, vn, k, v, table.as<int32_t>(), length.as<int32_t>(),
+                    seq.as<int32_t>(), count.as<int32_t>(), c.stream);
+  });
+  return PyLong_FromLong(st);
+  END_HANDLE_TH_ERRORS
+}
+
+// A bf16 output of four dimensions: the caller's, or contiguous and to be allocated.
+View output_view(Call& c, int i, const char* name, std::initializer_list<int64_t> size) {
+  if (c.a[i] == Py_None) {
+    View r;
+    int k = 0;
+    for (int64_t x : size) r.size[k++] = x;
+    r.stride[3] = 1;
+    for (k = 3; k > 0; k--) r.stride[k - 1] = r.stride[k] * r.size[k];
+    return r;
+  }
+  const View r = take_view(c, i, name);
+  int k = 0;
+  for (int64_t x : size) TORCH_CHECK_VALUE(r.size[k++] == x, name, ": expected the shape of the result");
+  return r;
+}
+void make_view(const Call& c, View& r) {
+  if (r.there()) return;
+  r.t = at::empty_strided(r.size, r.stride, at::TensorOptions().dtype(at::kBFloat16).device(c.device));
+  r.ptr = r.t.data_ptr();
+}
+
+// read_q4(k_pool, v_pool, table, length, tokens, seq, count, k, v) -> (status, k, v)
+PyObject* py_read_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  arity(n, 9);
+  Call c{a};
+  const PoolQ4 kp = take_pool_q4(c, 0, "k_pool"), vp = take_pool_q4(c, 1, "v_pool");
+  const Arg table = c.ints(2, "table", 2), length = c.ints(3, "length", 1);
+  const int tokens = c.integer(4, "tokens");
+  const Arg seq = c.ints(5, "seq", 1, true), count = c.ints(6, "count", 1, true);
+  const int seqs = size32(table.t, 0), width = size32(table.t, 1);
+  same_pools(kp, vp);
+  TORCH_CHECK_VALUE(tokens >= 0, "tokens: out of range");
+  TORCH_CHECK_VALUE(length.numel == seqs, "length: one entry for each row of the table");
+  TORCH_CHECK_VALUE(!seq.there() || seq.numel <= INT_MAX, "seq: too many entries");
+  const int entries = seq.there() ? static_cast<int>(seq.numel) : seqs;
+  TORCH_CHECK_VALUE(!count.there() || count.numel == entries, "count: one entry for each sequence that is read");
+  View k = output_view(c, 7, "k", {entries, kp.Hkv, tokens, kp.d}), v = output_view(c, 8, "v", {entries, kp.Hkv, tokens, kp.d});
+  c.find_stream();
+  int st;
+  without_lock([&] {
+    make_view(c, k);
+    make_view(c, v);
+    st = f_read_q4(entries, kp.Hkv, tokens, kp.d, kp.page, kp.pages, seqs, width, kp, vp, table.as<int32_t>(), length.as<int32_t>(), seq.as<int32_t>(),
+                   count.as<int32_t>(), k, v, c.stream);
+  });
+  return result(st, {c.give(7, k), c.give(8, v)});
+  END_HANDLE_TH_ERRORS
+}
+
+// rope(q, k, pos, freq, sections, halves, inverse, q_out, k_out) -> (status, q, k)
+PyObject* py_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  arity(n, 9);
+  Call c{a};
+  const View q = take_view(c, 0, "q");
+  View k = {};
+  if (a[1] != Py_None) k = take_view(c, 1, "k");
+  TORCH_CHECK_VALUE(a[1] != Py_None || a[8] == Py_None, "k_out without k");
+  const int B = q.dim(0), H = q.dim(1), N = q.dim(2), d = q.dim(3), Hk = k.there() ? k.dim(1) : 0;
+  TORCH_CHECK_VALUE(!k.there() || (k.dim(0) == B && k.dim(2) == N && k.dim(3) == d), "q and k have different tokens or channels");
+  const at::Tensor& pt = c.tensor(2, "pos");
+  TORCH_CHECK_VALUE(pt.scalar_type() == at::kInt && (pt.dim() == 2 || pt.dim() == 3), "pos: expected an int32 tensor [B,N,axes] or [N,axes]");
+  const int64_t at = pt.dim() - 2, axes = pt.size(at + 1);
+  TORCH_CHECK_VALUE((at == 0 || pt.size(0) == B) && pt.size(at) == N, "pos: one entry for each token");
+  TORCH_CHECK_VALUE((axes <= 1 || pt.stride(at + 1) == 1) && (N <= 1 || pt.stride(at) == axes), "pos: the tokens of a batch entry have to be in one piece");
+  const int64_t pos_stride = at == 1 && B > 1 ? pt.stride(0) : 0;
+  Arg pos;
+  pos.t = pt;
+  pos.ptr = pt.data_ptr();
+  const Arg freq = c.plain(3, "freq", at::kDouble, 1);
+  TORCH_CHECK_VALUE(freq.numel == d / 2, "freq: one entry for each pair of channels");
+  TORCH_CHECK_TYPE(PyTuple_Check(a[4]), "sections: expected a tuple");
+  TORCH_CHECK_VALUE(PyTuple_GET_SIZE(a[4]) == axes && axes <= AVSA_ROPE_AXES, "sections: one entry for each axis of pos, four at most");
+  int sections[AVSA_ROPE_AXES] = {};
+  for (int64_t i = 0; i < axes; i++) {
+    const long x = PyLong_AsLong(PyTuple_GET_ITEM(a[4], i));
+    if (x == -1 && PyErr_Occurred()) throw python_error();
+    TORCH_CHECK_VALUE(x >= 0 && x <= d / 2, "sections: out of range");
+    sections[i] = static_cast<int>(x);
+  }
+  const unsigned flags = (c.flag(5, "halves") ? AVSA_ROPE_HALVES : 0u) | (c.flag(6, "inverse") ? AVSA_ROPE_INVERSE : 0u);
+  auto output = [&](int i, const char* name, const View& x) {
+    if (a[i] != Py_None) return output_view(c, i, name, {x.size[0], x.size[1], x.size[2], x.size[3]});
+    // its shape, with the dimensions in its order and without its gaps (q may be a slice of a projection of q, k and v)
+    View r = x;
+    r.t = at::Tensor();
+    r.ptr = nullptr;
+    int order[3] = {0, 1, 2};
+    std::stable_sort(order, order + 3, [&](int i, int j) { return x.stride[i] < x.stride[j]; });
+    int64_t next = x.size[3];
+    for (int i : order) {
+      if (x.size[i] == 1) continue;
+      r.stride[i] = next;
+      next *= std::max<int64_t>(x.size[i], 1);
+    }
+    r.stride[3] = 1;
+    return r;
+  };
+  View q_out = output(7, "q_out", q), k_out = {};
+  if (k.there()) k_out = output(8, "k_out", k);
+  c.find_stream();
+  int st;
+  without_lock([&] {
+    make_view(c, q_out);
+    if (k.there()) make_view(c, k_out);
+    st = f_rope(B, H, Hk, N, d, q, k, q_out, k_out, pos.as<int32_t>(), pos_stride, static_cast<int>(axes), sections, freq.as<double>(), flags, c.stream);
+  });
+  return result(st, {c.give(7, q_out), c.give(8, k_out)});
   END_HANDLE_TH_ERRORS
 }
 
@@ -366,19 +563,21 @@ PyObject* py_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// bind(addresses of prefix_attn, its workspace query, extend, write, fork, free, compact, the cache's workspace query; reader of the raw current stream)
+// bind(addresses of prefix_attn, its workspace query, extend, write, fork, free, compact, the cache's workspace query, of the 4-bit cache's attention, its workspace query,
+// write and read, of rope; reader of the raw current stream)
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  TORCH_CHECK_TYPE(n == 9, "wrong number of arguments");
-  void* p[8];
-  for (int i = 0; i < 8; i++) {
+  constexpr int kEntries = 13;
+  TORCH_CHECK_TYPE(n == kEntries + 1, "wrong number of arguments");
+  void* p[kEntries];
+  for (int i = 0; i < kEntries; i++) {
     p[i] = PyLong_AsVoidPtr(a[i]);
     if (p[i] == nullptr) {
       TORCH_CHECK_VALUE(PyErr_Occurred(), "a null address");
       return nullptr;
     }
   }
-  o_raw_stream = Py_NewRef(a[8]);
+  o_raw_stream = Py_NewRef(a[kEntries]);
   f_attn = reinterpret_cast<decltype(f_attn)>(p[0]);
   f_attn_ws = reinterpret_cast<decltype(f_attn_ws)>(p[1]);
   f_extend = reinterpret_cast<decltype(f_extend)>(p[2]);
@@ -387,6 +586,11 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   f_free = reinterpret_cast<decltype(f_free)>(p[5]);
   f_compact = reinterpret_cast<decltype(f_compact)>(p[6]);
   f_ws = reinterpret_cast<decltype(f_ws)>(p[7]);
+  f_attn_q4 = reinterpret_cast<decltype(f_attn_q4)>(p[8]);
+  f_attn_q4_ws = reinterpret_cast<decltype(f_attn_q4_ws)>(p[9]);
+  f_write_q4 = reinterpret_cast<decltype(f_write_q4)>(p[10]);
+  f_read_q4 = reinterpret_cast<decltype(f_read_q4)>(p[11]);
+  f_rope = reinterpret_cast<decltype(f_rope)>(p[12]);
   Py_RETURN_NONE;
   END_HANDLE_TH_ERRORS
 }
@@ -399,6 +603,10 @@ PyMethodDef methods[] = {
     {"fork", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_fork)), METH_FASTCALL, nullptr},
     {"free", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_free)), METH_FASTCALL, nullptr},
     {"compact", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_compact)), METH_FASTCALL, nullptr},
+    {"attn_q4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_attn_q4)), METH_FASTCALL, nullptr},
+    {"write_q4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_write_q4)), METH_FASTCALL, nullptr},
+    {"read_q4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_read_q4)), METH_FASTCALL, nullptr},
+    {"rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_rope)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_avsa_cache", "whole calls of the paged cache", -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -27,11 +27,12 @@ struct PrefixLayout {
   int own_cluster;
   size_t rows;                  // partial rows
   int own_row0, cut_row0;
-  size_t plan, cta_err, own_rec, cut_rec, redo, lse, o, total;       // offsets in the workspace
+  size_t plan, cta_err, own_rec, cut_rec, redo, lse, o, wide, total;       // offsets in the workspace
+  size_t wide_pool;             // bytes of the keys as bf16, and of the values, where the tile kernel reads pages of codes
 };
 
-// False: more units, or key positions rounded up to a tile, than 32 bits count.
-static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int width, int prefix_pages, int causal, PrefixLayout& y) {
+// False: more units, or key positions rounded up to a tile, than 32 bits count.  `codes`: pages of a pool held in 4 bits, or 0.
+static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int width, int prefix_pages, int causal, int codes, PrefixLayout& y) {
   PrefixShape& s = y.s;
   s = {};
   s.B = B;
@@ -83,7 +84,7 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     y.pre.begin = 1;
     y.pre.tiles = static_cast<int>((RS + kStRows - 1) / kStRows);
     y.pre.items = y.pre.tiles * Hkv;
-    const int slots = sms * stream_ctas(stream_products(RS));      // CTAs of the stream kernel that the SMs hold
+    const int slots = sms * stream_ctas(stream_products(RS), codes > 0);      // CTAs of the stream kernel that the SMs hold
     const long long by_keys = PT / 2;      // 256 keys a CTA at least: four blocks a warp
     y.pre.splits = static_cast<int>(slots / y.pre.items < by_keys ? slots / y.pre.items : by_keys);
     // The kernel behind joins a row's parts eight at a time, 0.7 us each, so with few heads fewer and longer parts end earlier (4 heads x 60000 keys, us: 111 parts 35.8, 70 31.7).
@@ -103,7 +104,7 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     y.own.items = y.own.tiles * Hkv * B;
     y.own.out0 = static_cast<int>(own0);
     const long long keys = static_cast<long long>(width) * page - s.k0;      // at most
-    const int slots = sms * stream_ctas(stream_products(R));
+    const int slots = sms * stream_ctas(stream_products(R), codes > 0);
     // An item's keys over a cluster, 64 keys a CTA at least (a block a warp), as many CTAs as the SMs hold side by side: nine tenths of the slots, since a cluster takes its
     // own from one GPC and what does not fit waits for a whole item (us, filled to the last slot and like this: 96 items of 500 keys of 64 channels 14.4 and 9.7, 72
     // of 900 keys of 128 channels 16.4 and 10.3, 144 of 800 17.5 and 13.0).  No CTA has more than 1024 keys while others may have none (30 x 8 items of 1 to 1500
@@ -151,21 +152,27 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   at += align_up(y.rows * 4, 256);
   y.o = at;
   y.total = at + y.rows * d * 4;
+  y.wide = y.wide_pool = 0;
+  if (codes > 0 && y.tile) {
+    y.wide = align_up(y.total, 256);
+    y.wide_pool = static_cast<size_t>(codes) * Hkv * page * d * 2;      // (below 2^62)
+    y.total = y.wide + 2 * y.wide_pool;
+  }
   return true;
 }
 
-template <int D, int NT>
-static int launch_stream_of(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixParams& p, const StreamParams& t, int cluster, cudaStream_t st) {
-  auto kernel = prefix_stream_kernel<D, NT>;
-  constexpr size_t kSmem = sizeof(StreamSmem<D, NT>);
+template <int D, int NT, class Source>
+static int launch_stream_of(const Source& src, const PrefixParams& p, const StreamParams& t, int cluster, cudaStream_t st) {
+  auto kernel = prefix_stream_kernel<D, NT, Source>;
+  constexpr size_t kSmem = sizeof(StreamSmem<D, NT, Source::kQ4>);
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return AVSA_ERR_CUDA;
   const unsigned grid = static_cast<unsigned>((static_cast<long long>(t.items) * t.splits + t.check) * cluster);
-  return launch_pdl_clusters(kernel, cluster, grid, kStThreads, kSmem, st, tk, tv, p, t) == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
+  return launch_pdl_clusters(kernel, cluster, grid, kStThreads, kSmem, st, src, p, t) == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
 }
-template <int D>
-static int launch_stream(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixParams& p, const StreamParams& t, int cluster, cudaStream_t st) {
-  return stream_products(t.stacked ? static_cast<long long>(p.s.B) * p.s.R : p.s.R) == 1 ? launch_stream_of<D, 1>(tk, tv, p, t, cluster, st)
-                                                                                          : launch_stream_of<D, 2>(tk, tv, p, t, cluster, st);
+template <int D, class Source>
+static int launch_stream(const Source& src, const PrefixParams& p, const StreamParams& t, int cluster, cudaStream_t st) {
+  return stream_products(t.stacked ? static_cast<long long>(p.s.B) * p.s.R : p.s.R) == 1 ? launch_stream_of<D, 1>(src, p, t, cluster, st)
+                                                                                          : launch_stream_of<D, 2>(src, p, t, cluster, st);
 }
 
 template <int D>
@@ -189,20 +196,23 @@ static int launch_tile(const PrefixLayout& y, const avsa_bf16_4d& k, const avsa_
   return launch_pdl(prefix_attn_kernel<D>, y.n_cta, kPxThreads, PrefixSmem<D>::kTotal, st, tk, tv, tq_own, tq_pre, to, p) == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
 }
 
-template <int D>
-static int launch_prefix(const PrefixLayout& y, const avsa_bf16_4d& k, const avsa_bf16_4d& v, const PrefixParams& p, cudaStream_t st) {
+// The pools of a call: bf16, or codes, whose pages that the tile kernel reads are made bf16 in the workspace first.
+struct PrefixPools {
+  bool codes;
+  avsa_bf16_4d k, v;
+  avsa_q4_pool k4, v4;
+};
+
+template <int D, class Source>
+static int launch_kernels(const PrefixLayout& y, const Source& src, const avsa_bf16_4d& k, const avsa_bf16_4d& v, const PrefixParams& p, cudaStream_t st) {
   const PrefixShape& s = y.s;
   constexpr int kRows = prefix_merge_rows(D);
   int r = AVSA_OK;
-  CUtensorMap tk, tv;      // of 16 keys
-  if (y.own_stream && (!encode_bf16_tile_map(&tk, k.ptr, s.pages, s.Hkv, s.page, D, k.stride_b, k.stride_h, k.stride_n, 16) ||
-                       !encode_bf16_tile_map(&tv, v.ptr, s.pages, s.Hkv, s.page, D, v.stride_b, v.stride_h, v.stride_n, 16)))
-    return AVSA_ERR_CUDA;
-  if (y.pre_stream) r = launch_stream<D>(tk, tv, p, y.pre, 1, st);
+  if (y.pre_stream) r = launch_stream<D>(src, p, y.pre, 1, st);
   if (y.tile) r = launch_tile<D>(y, k, v, p, st);
   if (r != AVSA_OK) return r;
   if (y.own_stream) {
-    r = launch_stream<D>(tk, tv, p, y.own, y.own_cluster, st);
+    r = launch_stream<D>(src, p, y.own, y.own_cluster, st);
     if (r != AVSA_OK) return r;
     if (y.own.splits > 1) {
       const long long rows = static_cast<long long>(s.B) * s.Hkv * s.R;
@@ -217,6 +227,28 @@ static int launch_prefix(const PrefixLayout& y, const avsa_bf16_4d& k, const avs
     if (launch_pdl(prefix_merge_kernel<D>, grid, kPxMergeThreads, 0, st, p, y.n_cta) != cudaSuccess) return AVSA_ERR_CUDA;
   }
   return cudaGetLastError() == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
+}
+
+template <int D>
+static int launch_prefix(const PrefixLayout& y, const PrefixPools& pools, const PrefixParams& p, uint8_t* ws, cudaStream_t st) {
+  const PrefixShape& s = y.s;
+  if (pools.codes) {
+    const StreamCodes src = {q4_pool(pools.k4), q4_pool(pools.v4)};
+    avsa_bf16_4d k = {}, v = {};
+    if (y.tile) {
+      k = {ws + y.wide, static_cast<int64_t>(s.Hkv) * s.page * D, static_cast<int64_t>(s.page) * D, D};
+      v = k;
+      v.ptr = ws + y.wide + y.wide_pool;
+      const int r = launch_widen(p, src.k, src.v, ws + y.wide, ws + y.wide + y.wide_pool, !y.own_stream, D, st);
+      if (r != AVSA_OK) return r;
+    }
+    return launch_kernels<D>(y, src, k, v, p, st);
+  }
+  StreamTiles src;      // of 16 keys
+  if (y.own_stream && (!encode_bf16_tile_map(&src.k, pools.k.ptr, s.pages, s.Hkv, s.page, D, pools.k.stride_b, pools.k.stride_h, pools.k.stride_n, 16) ||
+                       !encode_bf16_tile_map(&src.v, pools.v.ptr, s.pages, s.Hkv, s.page, D, pools.v.stride_b, pools.v.stride_h, pools.v.stride_n, 16)))
+    return AVSA_ERR_CUDA;
+  return launch_kernels<D>(y, src, pools.k, pools.v, p, st);
 }
 
 static bool rows_ok(avsa_bf16_4d t, int B, int H, int N) {
@@ -235,14 +267,19 @@ static bool prefix_sizes_ok(int B, int H, int Hkv, int L, int d, int page, int w
 
 extern "C" size_t avsa_prefix_attn_workspace_bytes(int B, int H, int Hkv, int L, int d, int page, int width, int prefix_pages) {
   PrefixLayout y;
-  if (!prefix_sizes_ok(B, H, Hkv, L, d, page, width, prefix_pages) || !prefix_layout(B, H, Hkv, L, d, page, width, prefix_pages, 0, y)) return 0;
+  if (!prefix_sizes_ok(B, H, Hkv, L, d, page, width, prefix_pages) || !prefix_layout(B, H, Hkv, L, d, page, width, prefix_pages, 0, 0, y)) return 0;
   return y.total;
 }
 
-extern "C" int avsa_prefix_attn_step(int B, int H, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d q,
-                                     avsa_bf16_4d k_pool, avsa_bf16_4d v_pool, const int32_t* table, const int32_t* length,
-                                     const int32_t* seq, const int32_t* count, int prefix_pages, unsigned flags, float softmax_scale,
-                                     void* o_bf16, float* lse, int32_t* log, void* ws, size_t ws_bytes, void* stream) {
+extern "C" size_t avsa_prefix_attn_q4_workspace_bytes(int B, int H, int Hkv, int L, int d, int page, int pages, int width, int prefix_pages) {
+  PrefixLayout y;
+  if (pages <= 0 || !prefix_sizes_ok(B, H, Hkv, L, d, page, width, prefix_pages) || !prefix_layout(B, H, Hkv, L, d, page, width, prefix_pages, 0, pages, y)) return 0;
+  return y.total;
+}
+
+static int prefix_attn(int B, int H, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d q, const PrefixPools& pools, const int32_t* table,
+                       const int32_t* length, const int32_t* seq, const int32_t* count, int prefix_pages, unsigned flags, float softmax_scale, void* o_bf16,
+                       float* lse, int32_t* log, void* ws, size_t ws_bytes, void* stream) {
   if (B < 0 || H <= 0 || Hkv <= 0 || L < 0 || pages <= 0 || seqs <= 0 || width <= 0 || prefix_pages < 0 || prefix_pages > width) return AVSA_ERR_INVALID_ARG;
   if (H % Hkv != 0 || (flags & ~AVSA_CAUSAL) != 0 || (seq == nullptr && B > seqs)) return AVSA_ERR_INVALID_ARG;
   if ((d != 64 && d != 128) || (page != 16 && page != 32 && page != 64 && page != 128)) return AVSA_ERR_UNSUPPORTED;
@@ -252,11 +289,14 @@ extern "C" int avsa_prefix_attn_step(int B, int H, int Hkv, int L, int d, int pa
     return AVSA_ERR_UNSUPPORTED;
   if (!(softmax_scale >= 0.f) || isinf(softmax_scale)) return AVSA_ERR_INVALID_ARG;
   if (B == 0 || L == 0) return AVSA_OK;
-  if (!rows_ok(q, B, H, L) || !tensor_ok(k_pool, pages, Hkv) || !tensor_ok(v_pool, pages, Hkv)) return AVSA_ERR_INVALID_ARG;
+  if (!rows_ok(q, B, H, L)) return AVSA_ERR_INVALID_ARG;
+  if (pools.codes ? !q4_pool_ok(pools.k4, pages, Hkv, page, d) || !q4_pool_ok(pools.v4, pages, Hkv, page, d)
+                  : !tensor_ok(pools.k, pages, Hkv) || !tensor_ok(pools.v, pages, Hkv))
+    return AVSA_ERR_INVALID_ARG;
   if (table == nullptr || length == nullptr || o_bf16 == nullptr || !aligned16(o_bf16)) return AVSA_ERR_INVALID_ARG;
   if (!aligned4(table) || !aligned4(length) || !aligned4(seq) || !aligned4(count) || !aligned4(lse) || !aligned4(log)) return AVSA_ERR_INVALID_ARG;
   PrefixLayout y;
-  if (!prefix_layout(B, H, Hkv, L, d, page, width, prefix_pages, flags & AVSA_CAUSAL ? 1 : 0, y)) return AVSA_ERR_UNSUPPORTED;
+  if (!prefix_layout(B, H, Hkv, L, d, page, width, prefix_pages, flags & AVSA_CAUSAL ? 1 : 0, pools.codes ? pages : 0, y)) return AVSA_ERR_UNSUPPORTED;
   if (ws == nullptr || ws_bytes < y.total) return AVSA_ERR_WORKSPACE;
   if (!ws_aligned(ws, kWsParts)) return AVSA_ERR_INVALID_ARG;
   if (!device_is_sm100()) return AVSA_ERR_UNSUPPORTED;
@@ -288,7 +328,24 @@ extern "C" int avsa_prefix_attn_step(int B, int H, int Hkv, int L, int d, int pa
   p.tile_ctas = y.tile ? y.n_cta : 0;
   p.own_row0 = y.own_row0;
   p.cut_row0 = y.cut_row0;
-  return d == 128 ? launch_prefix<128>(y, k_pool, v_pool, p, as_stream(stream)) : launch_prefix<64>(y, k_pool, v_pool, p, as_stream(stream));
+  return d == 128 ? launch_prefix<128>(y, pools, p, w, as_stream(stream)) : launch_prefix<64>(y, pools, p, w, as_stream(stream));
+}
+
+extern "C" int avsa_prefix_attn_step(int B, int H, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d q,
+                                     avsa_bf16_4d k_pool, avsa_bf16_4d v_pool, const int32_t* table, const int32_t* length,
+                                     const int32_t* seq, const int32_t* count, int prefix_pages, unsigned flags, float softmax_scale,
+                                     void* o_bf16, float* lse, int32_t* log, void* ws, size_t ws_bytes, void* stream) {
+  const PrefixPools pools = {false, k_pool, v_pool, {}, {}};
+  return prefix_attn(B, H, Hkv, L, d, page, pages, seqs, width, q, pools, table, length, seq, count, prefix_pages, flags, softmax_scale, o_bf16, lse, log, ws,
+                     ws_bytes, stream);
+}
+
+extern "C" int avsa_prefix_attn_q4(int B, int H, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d q, avsa_q4_pool k_pool,
+                                   avsa_q4_pool v_pool, const int32_t* table, const int32_t* length, const int32_t* seq, const int32_t* count, int prefix_pages,
+                                   unsigned flags, float softmax_scale, void* o_bf16, float* lse, int32_t* log, void* ws, size_t ws_bytes, void* stream) {
+  const PrefixPools pools = {true, {}, {}, k_pool, v_pool};
+  return prefix_attn(B, H, Hkv, L, d, page, pages, seqs, width, q, pools, table, length, seq, count, prefix_pages, flags, softmax_scale, o_bf16, lse, log, ws,
+                     ws_bytes, stream);
 }
 
 extern "C" int avsa_prefix_attn(int B, int H, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d q,

@@ -193,7 +193,7 @@ struct PrefixPlan {
 
 // The CTA's first error, for the merge kernel to report.  (Not inlined: a call's first items run through cold code, and what stands between the lines that
 // they need is fetched with them.)
-__device__ __noinline__ void px_report(int* err, int code, int where, int item, int aux) {
+static __device__ __noinline__ void px_report(int* err, int code, int where, int item, int aux) {
   if (atomicCAS(err, 0, code) == 0) {
     err[1] = where;
     err[2] = item;

@@ -18,6 +18,7 @@
 #include <math.h>
 
 #include "prefix_attn_kernel.cuh"
+#include "q4.cuh"
 
 namespace avsa {
 
@@ -88,7 +89,7 @@ __device__ __forceinline__ void longest_sequence(const PrefixParams& p, int& slo
 
 // The call's status: what is out of range in the sequences of the batch, else the first error of a CTA of the tile kernel in front (`wait`: nothing has waited for it
 // yet).  One CTA, the call's first one to write the record (a wait of the stream kernel that runs out does so a second later).
-__device__ __noinline__ void prefix_check(const PrefixParams& p, int n_cta, int wait) {
+static __device__ __noinline__ void prefix_check(const PrefixParams& p, int n_cta, int wait) {
   __shared__ int worst, tile_error, again;
   const PrefixShape& S = p.s;
   if (threadIdx.x == 0) worst = 0x7fffffff, tile_error = 0x7fffffff, again = 0;
@@ -147,11 +148,23 @@ __device__ __forceinline__ void prefix_check_begin(const PrefixParams& p) {
 
 // CTAs that an SM holds, by shared memory: with one product's columns three of two stages (of 8 KB; 64 sequences of 100 to 2048 keys, us: 55.4, two of three stages 58.7),
 // with two products' the warps take longer and want more ahead (32 sequences x 8 x 2048 keys, 16 rows: 71.5 and 58.0).
-constexpr int stream_ctas(int NT) { return NT == 1 ? 3 : 2; }
+constexpr int stream_ctas(int NT, bool q4) { return q4 ? (NT == 1 ? 4 : 3) : NT == 1 ? 3 : 2; }
 
-template <int D, int NT>
+// Where the keys and values come from.
+struct StreamTiles {      // bf16, tensor maps of 16 keys
+  static constexpr bool kQ4 = false;
+  CUtensorMap k, v;
+};
+struct StreamCodes {      // 4 bits, blocks of 16 keys
+  static constexpr bool kQ4 = true;
+  Q4Pool k, v;
+};
+
+template <int D, int NT, bool Q4>
 struct StreamSmem {
-  static constexpr int kStages = (NT == 1 ? 2 : 3) * (128 / D), kPanel = 16 * 128, kStage = 2 * (D / 64) * kPanel;      // a stage: panels of K, panels of V
+  static constexpr int kPanel = 16 * 128, kBlock = q4_block_bytes(D);
+  static constexpr int kStages = Q4 ? 4 * (128 / D) : (NT == 1 ? 2 : 3) * (128 / D);
+  static constexpr int kStage = Q4 ? 2 * kBlock : 2 * (D / 64) * kPanel;      // a stage: panels of K, panels of V, or a block of each
   union {
     uint8_t ring[kStWarps][kStages][kStage];      // 128-byte swizzled
     float4 o[kStWarps][kStRows][D / 4];           // behind the keys; [0] becomes the CTA's
@@ -160,6 +173,10 @@ struct StreamSmem {
   float m[kStWarps][kStRows], l[kStWarps][kStRows];
   float cm[kStRows], cl[kStRows];
 };
+
+// The key of a block of codes that is row r (of 8) of S^T.  Keys' codes are 64 bytes apart (128 channels), so that a product's operands come from shared memory without
+// two lanes of a phase at one bank where neighbouring rows, and rows two apart, alternate between even and odd keys.
+__device__ __forceinline__ int stream_key(int r) { return r ^ ((r >> 1) & 1); }
 
 // Where the parts of the beginning of stacked row rho are: `n` of them, `step` rows apart.
 __device__ __forceinline__ void prefix_parts(const PrefixParams& p, const StreamParams& t, int hk, int rho, int& first, int& step, int& n) {
@@ -205,11 +222,12 @@ __device__ __forceinline__ void stream_finish(const PrefixParams& p, const Strea
 }
 
 // NT: products of 8 query rows, 1 or 2.
-template <int D, int NT>
-__global__ void __launch_bounds__(kStThreads, stream_ctas(NT))
-prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const __grid_constant__ PrefixParams p, const StreamParams t) {
+template <int D, int NT, class Source>
+__global__ void __launch_bounds__(kStThreads, stream_ctas(NT, Source::kQ4))
+prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__ PrefixParams p, const StreamParams t) {
   extern __shared__ __align__(1024) uint8_t smem[];
-  using L_ = StreamSmem<D, NT>;
+  constexpr bool Q4 = Source::kQ4;
+  using L_ = StreamSmem<D, NT, Q4>;
   L_& sm = *reinterpret_cast<L_*>(smem);
   constexpr unsigned FULLM = 0xffffffffu;
   const PrefixShape& S = p.s;
@@ -218,8 +236,10 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
   if (lane == 0) {
     for (int k = 0; k < L_::kStages; k++) mbar_init(smem_u32(&sm.full[warp][k]), 1);
     fence_mbar_init();
-    prefetch_tmap(&tmk);
-    prefetch_tmap(&tmv);
+    if constexpr (!Q4) {
+      prefetch_tmap(&src.k);
+      prefetch_tmap(&src.v);
+    }
   }
   __syncwarp();
   if (t.first) {
@@ -290,9 +310,9 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
     const bool have = 8 * x + n < rows;
     int b = 0, i = 0, head = 0, len;
     if (have) row_of(8 * x + n, b, i, head, len);
-    const __nv_bfloat16* at = static_cast<const __nv_bfloat16*>(p.q.ptr) + b * p.q.stride_b + head * p.q.stride_h + i * p.q.stride_n + 8 * c;
+    const __nv_bfloat16* at = static_cast<const __nv_bfloat16*>(p.q.ptr) + b * p.q.stride_b + head * p.q.stride_h + i * p.q.stride_n + (Q4 ? D / 4 : 8) * c;
 #pragma unroll
-    for (int j = 0; j < D / 32; j++) q[x][j] = have ? *reinterpret_cast<const uint4*>(at + 32 * j) : make_uint4(0u, 0u, 0u, 0u);
+    for (int j = 0; j < D / 32; j++) q[x][j] = have ? *reinterpret_cast<const uint4*>(at + (Q4 ? 8 : 32) * j) : make_uint4(0u, 0u, 0u, 0u);
   }
   // 16-key blocks [b0, b1) of the part, every `step`-th from the warp's own on
   int b0 = k0 >> 4, b1 = (k1 + 15) >> 4;
@@ -308,12 +328,32 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
   const uint32_t ring = smem_u32(&sm.ring[warp][0][0]), full = smem_u32(&sm.full[warp][0]);
   // (a page that does not exist reads as zeros)
   auto load = [&](int blk, int page, int stage) {
-    if (lane == 0 && blk < b1) {
+    if constexpr (Q4) {
+      if (blk >= b1) return;
+      const uint32_t bar = full + stage * 8, dst = ring + stage * L_::kStage;
+      if (static_cast<unsigned>(page) < static_cast<unsigned>(S.pages)) {
+        if (lane == 0) {
+          const int64_t in = static_cast<int64_t>(blk & ((1 << block_shift) - 1)) * L_::kBlock;
+          mbar_expect_tx(bar, L_::kStage);
+          bulk_load_1d(dst, src.k.ptr + page * src.k.stride_page + hk * src.k.stride_head + in, L_::kBlock, bar);
+          bulk_load_1d(dst + L_::kBlock, src.v.ptr + page * src.v.stride_page + hk * src.v.stride_head + in, L_::kBlock, bar);
+        }
+      } else {
+        // scales of zero; the codes may be anything
+        for (int at = lane; at < D / 16 * 16 / 4; at += 32) {
+          *reinterpret_cast<uint32_t*>(&sm.ring[warp][stage][q4_scales_at(D) + 4 * at]) = 0u;
+          *reinterpret_cast<uint32_t*>(&sm.ring[warp][stage][L_::kBlock + q4_scales_at(D) + 4 * at]) = 0u;
+        }
+        fence_proxy_async();      // (a copy lands there later)
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+      }
+    } else if (lane == 0 && blk < b1) {
       const uint32_t bar = full + stage * 8, dst = ring + stage * L_::kStage;
       const int in = (blk & ((1 << block_shift) - 1)) * 16, pg = page < 0 ? S.pages : page;
       mbar_expect_tx(bar, L_::kStage);
-      for (int pn = 0; pn < NPANEL; pn++) tma_load_4d(dst + pn * PANEL, &tmk, bar, pn * 64, in, hk, pg);
-      for (int pn = 0; pn < NPANEL; pn++) tma_load_4d(dst + (NPANEL + pn) * PANEL, &tmv, bar, pn * 64, in, hk, pg);
+      for (int pn = 0; pn < NPANEL; pn++) tma_load_4d(dst + pn * PANEL, &src.k, bar, pn * 64, in, hk, pg);
+      for (int pn = 0; pn < NPANEL; pn++) tma_load_4d(dst + (NPANEL + pn) * PANEL, &src.v, bar, pn * 64, in, hk, pg);
     }
   };
   // vectors of a stage: `chunk` of 16 bytes of row `key` in a panel
@@ -331,7 +371,7 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
     load(ahead, page, k);
     ahead += step;
   }
-  float o[NT][D / 16][4];       // product 4j + y: {channel 64j + 8n + 2y, the next} x {row 2c, the next}, as [2 * channel + row]
+  float o[NT][D / 16][4];       // product 4j + y: {channel 64j + 8n + 2y (of codes (D/8)n + 8j + 2y), the next} x {row 2c, the next}, as [2 * channel + row]
 #pragma unroll
   for (int x = 0; x < NT; x++)
 #pragma unroll
@@ -339,6 +379,7 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
   float m[NT][2], l[NT][2];
 #pragma unroll
   for (int x = 0; x < NT; x++) m[x][0] = m[x][1] = -INFINITY, l[x][0] = l[x][1] = 0.f;
+  const int key = Q4 ? stream_key(n) : n;
   int stage = 0, round = 0;
   bool ok = true;
 #pragma unroll 1
@@ -348,6 +389,36 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
       break;
     }
     float s[NT][2][4] = {};      // two chains of products each
+    if constexpr (Q4) {
+      // lane (n, c): a quarter of the channels of keys `key` and `key` + 8, in whole words
+      constexpr int W = D / 32;
+      const uint8_t* const k = &sm.ring[warp][stage][0];
+      uint32_t ka[W], kb[W];
+      if constexpr (W == 4) {
+        *reinterpret_cast<uint4*>(ka) = *reinterpret_cast<const uint4*>(k + key * (D / 2) + 16 * c);
+        *reinterpret_cast<uint4*>(kb) = *reinterpret_cast<const uint4*>(k + (key + 8) * (D / 2) + 16 * c);
+      } else {
+        *reinterpret_cast<uint2*>(ka) = *reinterpret_cast<const uint2*>(k + key * (D / 2) + 8 * c);
+        *reinterpret_cast<uint2*>(kb) = *reinterpret_cast<const uint2*>(k + (key + 8) * (D / 2) + 8 * c);
+      }
+      const int group = c * (D / 4) / kQ4Group;
+      const uint16_t* const scales = reinterpret_cast<const uint16_t*>(k + q4_scales_at(D));
+      uint32_t sa = scales[key * (D / kQ4Group) + group], sb = scales[(key + 8) * (D / kQ4Group) + group];
+      sa |= sa << 16;
+      sb |= sb << 16;
+      const uint32_t oa = q4_offset(sa), ob = q4_offset(sb);
+#pragma unroll
+      for (int j = 0; j < W; j++) {
+        uint32_t a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) a[i] = q4_pair(ka[j], i, sa, oa), b[i] = q4_pair(kb[j], i, sb, ob);
+#pragma unroll
+        for (int x = 0; x < NT; x++) {
+          mma_16816(s[x][0], a[0], b[0], a[1], b[1], q[x][j].x, q[x][j].y);
+          mma_16816(s[x][1], a[2], b[2], a[3], b[3], q[x][j].z, q[x][j].w);
+        }
+      }
+    } else {
 #pragma unroll
     for (int j = 0; j < D / 32; j++) {
       const uint4 ka = vec(stage, j >> 1, n, (j & 1) * 4 + c), kb = vec(stage, j >> 1, n + 8, (j & 1) * 4 + c);
@@ -356,6 +427,7 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
         mma_16816(s[x][0], ka.x, kb.x, ka.y, kb.y, q[x][j].x, q[x][j].y);
         mma_16816(s[x][1], ka.z, kb.z, ka.w, kb.w, q[x][j].z, q[x][j].w);
       }
+    }
     }
     uint32_t pt[NT][2];
 #pragma unroll
@@ -366,7 +438,7 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
       if (blk * 16 + 16 > rel_min || blk * 16 + 16 > k1) {
 #pragma unroll
         for (int e = 0; e < 4; e++)
-          if (blk * 16 + n + 8 * (e >> 1) >= min(see[x][e & 1], k1)) v[e] = -INFINITY;
+          if (blk * 16 + key + 8 * (e >> 1) >= min(see[x][e & 1], k1)) v[e] = -INFINITY;
       }
       float top[2];
 #pragma unroll
@@ -400,6 +472,49 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
       pt[x][0] = transpose_8x8(pack_bf16x2(e4[0], e4[1]));
       pt[x][1] = transpose_8x8(pack_bf16x2(e4[2], e4[3]));
     }
+    if constexpr (Q4) {
+      // lane (n, c): an eighth of the channels, of the keys that are rows 2c, 2c + 1, 2c + 8 and 2c + 9 of S^T
+      constexpr int W = D / 64;
+      const uint8_t* const v = &sm.ring[warp][stage][L_::kBlock];
+      const int key0 = stream_key(2 * c), key1 = stream_key(2 * c + 1), group = n * (D / 8) / kQ4Group;
+      uint32_t w0[W], w1[W], w2[W], w3[W];
+      auto codes = [&](int key, uint32_t (&w)[W]) {
+        if constexpr (W == 2) {
+          *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(v + key * (D / 2) + 8 * n);
+        } else {
+          w[0] = *reinterpret_cast<const uint32_t*>(v + key * (D / 2) + 4 * n);
+        }
+      };
+      codes(key0, w0);
+      codes(key1, w1);
+      codes(key0 + 8, w2);
+      codes(key1 + 8, w3);
+      const uint16_t* const scales = reinterpret_cast<const uint16_t*>(v + q4_scales_at(D)) + group;
+      uint32_t s0 = scales[key0 * (D / kQ4Group)], s1 = scales[key1 * (D / kQ4Group)], s2 = scales[(key0 + 8) * (D / kQ4Group)],
+               s3 = scales[(key1 + 8) * (D / kQ4Group)];
+      if (blk * 16 + 16 > k1) {
+        // behind the last token its page may hold anything; P is zero there, and 0 * NaN is not
+        const int left = k1 - blk * 16;
+        if (key0 >= left) s0 = 0u;
+        if (key1 >= left) s1 = 0u;
+        if (key0 + 8 >= left) s2 = 0u;
+        if (key1 + 8 >= left) s3 = 0u;
+      }
+      s0 |= s1 << 16;
+      s2 |= s3 << 16;
+      const uint32_t o0 = q4_offset(s0), o2 = q4_offset(s2);
+#pragma unroll
+      for (int j = 0; j < W; j++) {
+        const uint32_t e0 = __byte_perm(w0[j], w1[j], 0x5410), d0 = __byte_perm(w0[j], w1[j], 0x7632);      // even channels of both keys, odd ones
+        const uint32_t e2 = __byte_perm(w2[j], w3[j], 0x5410), d2 = __byte_perm(w2[j], w3[j], 0x7632);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          const uint32_t a0 = q4_pair(e0, i, s0, o0), a1 = q4_pair(d0, i, s0, o0), a2 = q4_pair(e2, i, s2, o2), a3 = q4_pair(d2, i, s2, o2);
+#pragma unroll
+          for (int x = 0; x < NT; x++) mma_16816(o[x][4 * j + i], a0, a1, a2, a3, pt[x][0], pt[x][1]);
+        }
+      }
+    } else {
 #pragma unroll
     for (int j = 0; j < D / 64; j++) {
       uint32_t v0[4], v1[4], v2[4], v3[4];
@@ -425,6 +540,7 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
 #pragma unroll
         for (int x = 0; x < NT; x++) mma_16816(o[x][4 * j + y], a0, a1, a2, a3, pt[x][0], pt[x][1]);
       }
+    }
     }
     __syncwarp();      // all lanes have read the stage
     {
@@ -460,7 +576,7 @@ prefix_stream_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_const
         }
 #pragma unroll
         for (int y = 0; y < D / 16; y += 2)
-          sm.o[warp][r][((y >> 2) * 64 + 8 * n + 2 * (y & 3)) / 4] = make_float4(o[x][y][e], o[x][y][2 + e], o[x][y + 1][e], o[x][y + 1][2 + e]);
+          sm.o[warp][r][((y >> 2) * (Q4 ? 8 : 64) + (Q4 ? D / 8 : 8) * n + 2 * (y & 3)) / 4] = make_float4(o[x][y][e], o[x][y][2 + e], o[x][y + 1][e], o[x][y + 1][2 + e]);
       }
     }
   __syncthreads();
