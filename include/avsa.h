@@ -371,9 +371,9 @@ AVSA_API size_t avsa_cache_workspace_bytes(int seqs, int pages, int n);
  * avsa_cache_write_q4 quantises the new tokens into the pages.  A list names no sequence twice.
  * avsa_cache_read_q4  the last count[k] tokens of sequence seq[k] (count NULL: T of them) become the first count[k] (0..T) tokens of k and v [n,Hkv,T,d], exactly.
  *                     Tokens that there are not (behind count[k], in front of the sequence's first, without a page) are zeros.
- * avsa_prefix_attn_q4 attention on the values that the pages stand for.  Where a sequence and key head has more than 32 query rows, or a shared beginning read for
- *                     the batch at once more than 32 stacked ones, the pages that the batch reads are first made bf16 in the workspace, which has room
- *                     for one layer's (2 * pages * Hkv * page * d of bf16); it may be the same one for all layers.
+ * avsa_prefix_attn_q4 attention on the values that the pages stand for.  Where many query rows read the same keys (more than 6 x 128 of a sequence and key head, or
+ *                     stacked ones) the pages that the batch reads are first made bf16 in the workspace, which then has room for a layer's
+ *                     (2 * pages * Hkv * page * d of bf16); it may be the same one for all layers.
  *
  * Neither a write nor a read needs a workspace or leaves a status.
  */

@@ -8,7 +8,7 @@
 
 namespace avsa {
 
-constexpr int kQ4Threads = 256;
+constexpr int kQ4Threads = 128;
 
 // 64 bytes of a thread's own, in vectors of 32 bytes where they are aligned to these.
 template <bool WIDE>
@@ -85,7 +85,7 @@ struct TokensQ4Args {
 
 // The last count[k] of the length[s] tokens of sequence s = seq[k].  READ: out of the pages, and zeros where there is none; else into them.
 template <int D, bool READ, bool WIDE>
-__global__ void __launch_bounds__(kQ4Threads) tokens_q4_kernel(const __grid_constant__ TokensQ4Args a) {
+__global__ void __launch_bounds__(kQ4Threads, 8) tokens_q4_kernel(const __grid_constant__ TokensQ4Args a) {
   pdl_wait();
   pdl_launch();
   constexpr int G = D / kQ4Group;

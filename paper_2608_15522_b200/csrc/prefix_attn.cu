@@ -15,6 +15,8 @@ constexpr int kChunk = 8;        // row tiles that go through the beginning side
 
 constexpr int kStreamRows = 32;      // query rows of a batch entry and key head that the stream kernel takes, at most; of the stacked rows as well
 
+constexpr int kWidenTiles = 6;       // row tiles that read a tile of codes, beyond which it is made bf16 once for all of them
+
 // Products of 8 columns for so many query rows: with 8 or less the second one's would be empty.
 static int stream_products(long long rows) { return rows <= 8 ? 1 : 2; }
 
@@ -28,7 +30,7 @@ struct PrefixLayout {
   size_t rows;                  // partial rows
   int own_row0, cut_row0;
   size_t plan, cta_err, own_rec, cut_rec, redo, lse, o, wide, total;       // offsets in the workspace
-  size_t wide_pool;             // bytes of the keys as bf16, and of the values, where the tile kernel reads pages of codes
+  size_t wide_pool;             // bytes of the keys as bf16, and of the values, where pages of codes become that before the tile kernel; else 0
 };
 
 // False: more units, or key positions rounded up to a tile, than 32 bits count.  `codes`: pages of a pool held in 4 bits, or 0.
@@ -153,7 +155,11 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   y.o = at;
   y.total = at + y.rows * d * 4;
   y.wide = y.wide_pool = 0;
-  if (codes > 0 && y.tile) {
+  // Pages of codes become tiles in the tile kernel, or, where a key tile meets many row tiles (each of which would do it again), bf16 pages in the workspace first.
+  // 2 x 16 heads x 12000 keys of 128 channels, us, in the kernel and before it, by row tiles: two 76 and 130, four 134 and 188, five 157 and 162, six 182 and 181, eight 250
+  // and 217, twelve 365 and 292 (of 64 channels: six 140 and 147, eight 194 and 191); 12800 shared ones: two 54 and 72, six 125 and 124, twelve 240 and 207.
+  const long long own = y.own_stream ? 0 : s.stack ? most - PT : most, shared = s.stack ? PT : 0;
+  if (codes > 0 && y.tile && TP * shared + F * own > kWidenTiles * (shared + B * own)) {
     y.wide = align_up(y.total, 256);
     y.wide_pool = static_cast<size_t>(codes) * Hkv * page * d * 2;      // (below 2^62)
     y.total = y.wide + 2 * y.wide_pool;
@@ -175,25 +181,23 @@ static int launch_stream(const Source& src, const PrefixParams& p, const StreamP
                                                                                           : launch_stream_of<D, 2>(src, p, t, cluster, st);
 }
 
-template <int D>
-static int launch_tile(const PrefixLayout& y, const avsa_bf16_4d& k, const avsa_bf16_4d& v, const PrefixParams& p, cudaStream_t st) {
+// `src`: of pages, where it is bf16.
+template <int D, class Source>
+static int launch_tile(const PrefixLayout& y, const Source& src, const PrefixParams& p, cudaStream_t st) {
   const PrefixShape& s = y.s;
-  CUtensorMap tk, tv, tq_own, tq_pre, to;
-  if (!encode_bf16_tile_map(&tk, k.ptr, s.pages, s.Hkv, s.page, D, k.stride_b, k.stride_h, k.stride_n, s.page) ||
-      !encode_bf16_tile_map(&tv, v.ptr, s.pages, s.Hkv, s.page, D, v.stride_b, v.stride_h, v.stride_n, s.page))
-    return AVSA_ERR_CUDA;
+  CUtensorMap tq_own = {}, tq_pre = {}, to = {};      // (not looked at where there is no box)
   // (an axis of one element has no stride to speak of: any multiple of 16 bytes)
   const int H = s.Hkv * s.G;
   const int64_t sh = H > 1 ? p.q.stride_h : D, sn = s.L > 1 ? p.q.stride_n : D, sb = s.B > 1 ? p.q.stride_b : D;
   auto box = [&](CUtensorMap* map, const void* ptr, int tokens, int entries) {
     return encode_bf16_map(map, ptr, {D, H, s.L, s.B}, {sh, sn, sb}, {64, s.G, tokens, entries});
   };
-  tq_own = tq_pre = to = tk;      // (where there is no box)
   if (!s.own_off && s.own_box > 0 && !(box(&tq_own, p.q.ptr, s.own_box / s.G, 1) && box(&to, p.o, s.own_box / s.G, 1))) return AVSA_ERR_CUDA;
   if (s.pre_box > 0 && !box(&tq_pre, p.q.ptr, s.L, s.pre_box / s.R)) return AVSA_ERR_CUDA;
   if (s.queue && launch_pdl(clear_counter_kernel, 1, 1, 0, st, p.counter) != cudaSuccess) return AVSA_ERR_CUDA;
-  if (cudaFuncSetAttribute(prefix_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PrefixSmem<D>::kTotal) != cudaSuccess) return AVSA_ERR_CUDA;
-  return launch_pdl(prefix_attn_kernel<D>, y.n_cta, kPxThreads, PrefixSmem<D>::kTotal, st, tk, tv, tq_own, tq_pre, to, p) == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
+  auto kernel = prefix_attn_kernel<D, Source>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PrefixSmem<D, Source::kQ4>::kTotal) != cudaSuccess) return AVSA_ERR_CUDA;
+  return launch_pdl(kernel, y.n_cta, px_threads(Source::kQ4), PrefixSmem<D, Source::kQ4>::kTotal, st, src, tq_own, tq_pre, to, p) == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
 }
 
 // The pools of a call: bf16, or codes, whose pages that the tile kernel reads are made bf16 in the workspace first.
@@ -203,13 +207,14 @@ struct PrefixPools {
   avsa_q4_pool k4, v4;
 };
 
-template <int D, class Source>
-static int launch_kernels(const PrefixLayout& y, const Source& src, const avsa_bf16_4d& k, const avsa_bf16_4d& v, const PrefixParams& p, cudaStream_t st) {
+// `src` is what the stream kernel reads, `tiles` what the tile kernel does.
+template <int D, class Source, class TileSource>
+static int launch_kernels(const PrefixLayout& y, const Source& src, const TileSource& tiles, const PrefixParams& p, cudaStream_t st) {
   const PrefixShape& s = y.s;
   constexpr int kRows = prefix_merge_rows(D);
   int r = AVSA_OK;
   if (y.pre_stream) r = launch_stream<D>(src, p, y.pre, 1, st);
-  if (y.tile) r = launch_tile<D>(y, k, v, p, st);
+  if (y.tile) r = launch_tile<D>(y, tiles, p, st);
   if (r != AVSA_OK) return r;
   if (y.own_stream) {
     r = launch_stream<D>(src, p, y.own, y.own_cluster, st);
@@ -229,26 +234,29 @@ static int launch_kernels(const PrefixLayout& y, const Source& src, const avsa_b
   return cudaGetLastError() == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
 }
 
+// Tensor maps of a bf16 pool, `rows` keys each.
+template <int D>
+static bool encode_tiles(PrefixTiles& t, const PrefixShape& s, const avsa_bf16_4d& k, const avsa_bf16_4d& v, int rows) {
+  return encode_bf16_tile_map(&t.k, k.ptr, s.pages, s.Hkv, s.page, D, k.stride_b, k.stride_h, k.stride_n, rows) &&
+         encode_bf16_tile_map(&t.v, v.ptr, s.pages, s.Hkv, s.page, D, v.stride_b, v.stride_h, v.stride_n, rows);
+}
+
 template <int D>
 static int launch_prefix(const PrefixLayout& y, const PrefixPools& pools, const PrefixParams& p, uint8_t* ws, cudaStream_t st) {
   const PrefixShape& s = y.s;
   if (pools.codes) {
-    const StreamCodes src = {q4_pool(pools.k4), q4_pool(pools.v4)};
-    avsa_bf16_4d k = {}, v = {};
-    if (y.tile) {
-      k = {ws + y.wide, static_cast<int64_t>(s.Hkv) * s.page * D, static_cast<int64_t>(s.page) * D, D};
-      v = k;
-      v.ptr = ws + y.wide + y.wide_pool;
-      const int r = launch_widen(p, src.k, src.v, ws + y.wide, ws + y.wide + y.wide_pool, !y.own_stream, D, st);
-      if (r != AVSA_OK) return r;
-    }
-    return launch_kernels<D>(y, src, k, v, p, st);
+    const PrefixCodes src = {q4_pool(pools.k4), q4_pool(pools.v4)};
+    if (y.wide_pool == 0) return launch_kernels<D>(y, src, src, p, st);
+    avsa_bf16_4d k = {ws + y.wide, static_cast<int64_t>(s.Hkv) * s.page * D, static_cast<int64_t>(s.page) * D, D}, v = k;
+    v.ptr = ws + y.wide + y.wide_pool;
+    PrefixTiles wide;
+    if (!encode_tiles<D>(wide, s, k, v, s.page)) return AVSA_ERR_CUDA;
+    const int r = launch_widen(p, src.k, src.v, ws + y.wide, ws + y.wide + y.wide_pool, !y.own_stream, D, st);
+    return r != AVSA_OK ? r : launch_kernels<D>(y, src, wide, p, st);
   }
-  StreamTiles src;      // of 16 keys
-  if (y.own_stream && (!encode_bf16_tile_map(&src.k, pools.k.ptr, s.pages, s.Hkv, s.page, D, pools.k.stride_b, pools.k.stride_h, pools.k.stride_n, 16) ||
-                       !encode_bf16_tile_map(&src.v, pools.v.ptr, s.pages, s.Hkv, s.page, D, pools.v.stride_b, pools.v.stride_h, pools.v.stride_n, 16)))
-    return AVSA_ERR_CUDA;
-  return launch_kernels<D>(y, src, pools.k, pools.v, p, st);
+  PrefixTiles few = {}, tiles = {};
+  if ((y.own_stream && !encode_tiles<D>(few, s, pools.k, pools.v, 16)) || (y.tile && !encode_tiles<D>(tiles, s, pools.k, pools.v, s.page))) return AVSA_ERR_CUDA;
+  return launch_kernels<D>(y, few, tiles, p, st);
 }
 
 static bool rows_ok(avsa_bf16_4d t, int B, int H, int N) {

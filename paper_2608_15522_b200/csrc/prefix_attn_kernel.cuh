@@ -28,16 +28,32 @@
 #include <math.h>
 
 #include "attn_persist_kernel.cuh"
+#include "q4.cuh"
 
 namespace avsa {
 
-constexpr int kPxThreads = 512;
-// 512 x 128 registers at launch; then 8 service warps of 64 and 8 softmax warps of 192: 65536 both ways.
-constexpr int kPxServiceRegs = 64, kPxSoftmaxRegs = 192;
-static_assert(8 * 32 * kPxServiceRegs + 8 * 32 * kPxSoftmaxRegs <= kPxThreads * 128, "setmaxnreg budget exceeded");
+// Registers: 512 x 128 at launch; then 8 service warps of 64 and 8 softmax warps of 192: 65536 both ways.  With pages of codes, where four warps make tiles of
+// keys of them and four more tiles of values, 640 x 96; then 12 service warps of 48 and 8 softmax warps of 168: 61440 both ways.
+constexpr __host__ __device__ int px_threads(bool q4) { return q4 ? 640 : 512; }
+constexpr __host__ __device__ int px_service_regs(bool q4) { return q4 ? 48 : 64; }
+constexpr __host__ __device__ int px_softmax_regs(bool q4) { return q4 ? 168 : 192; }
+constexpr bool px_regs_fit(bool q4) {
+  return (px_threads(q4) - 256) * px_service_regs(q4) + 256 * px_softmax_regs(q4) <= px_threads(q4) * (q4 ? 96 : 128);
+}
+static_assert(px_regs_fit(false) && px_regs_fit(true), "setmaxnreg budget exceeded");
+template <int N>
+__device__ __forceinline__ void fewer_regs() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void more_regs() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
 constexpr int kPxRing = 4, kPxRedo = 14;
-constexpr int kPxQWarps = 2;             // warps 13 and 14 gather query rows
-constexpr int kPxConsumers = 4 + kPxQWarps + 8;      // warps that read the item ring
+// Warps that gather query rows: 13 and 14, or with pages of codes 16 to 19, which make the tiles of values.
+constexpr int kPxCodeWarps = 4;
+constexpr __host__ __device__ int px_q_warps(bool q4) { return q4 ? kPxCodeWarps : 2; }
+constexpr __host__ __device__ int px_consumers(bool q4) { return q4 ? 3 + 2 * kPxCodeWarps + 8 : 4 + px_q_warps(q4) + 8; }      // warps that read the item ring
 
 enum PrefixWhere {
   kPrefixPage = 221, kPrefixLength, kPrefixSeq, kPxItem, kPxItemEmpty, kPxQEmpty, kPxQFull, kPxKEmpty, kPxVEmpty, kPxKFull, kPxVFull, kPxSFull, kPxSFree,
@@ -119,21 +135,25 @@ static_assert(sizeof(PrefixItem) == 48, "three 16-byte accesses");
 // Words of the CTA's `misc`.
 enum { kPxTmem = 0, kPxStop, kPxWhere, kPxProgress, kPxFlag /* + item parity */, kPxListed = kPxFlag + 2, kPxRecomputed, kPxErr, kPxWords = kPxErr + 4 };
 
-template <int D>
+template <int D, bool Q4>
 struct PrefixSmem {
   static constexpr int kTile = 128 * D * 2;
-  static constexpr int kKS = D == 128 ? 3 : 6, kVS = D == 128 ? 3 : 6;
+  // (codes: a stage or two less of each, and a ring of tiles of keys or values as they come)
+  static constexpr int kKS = Q4 ? (D == 128 ? 2 : 4) : D == 128 ? 3 : 6, kVS = Q4 ? (D == 128 ? 3 : 5) : D == 128 ? 3 : 6;
+  static constexpr int kRS = Q4 ? (D == 128 ? 3 : 6) : 0, kRaw = 8 * q4_block_bytes(D);
   // (64 channels: two buffers of query rows)
   static constexpr int kQ = 0, kQSlot = D == 64 ? 16384 : 0;
   static constexpr int kK = 32768;
   static constexpr int kV = kK + kKS * kTile;
-  static constexpr int kBars = kV + kVS * kTile;
-  static constexpr int kNumBars = 4 + 2 * kKS + 2 * kVS + 13 + 2 * kPxRing + 6;
+  static constexpr int kRaws = kV + kVS * kTile;
+  static constexpr int kBars = kRaws + kRS * kRaw;
+  static constexpr int kNumBars = 4 + 2 * kKS + 2 * kVS + 13 + 2 * kPxRing + 6 + 2 * kRS;
   static constexpr int kStats = (kBars + kNumBars * 8 + 15) / 16 * 16;       // float mref[128], lsum[2][128]
   static constexpr int kItems = kStats + 3 * 128 * 4;
   static constexpr int kPages = kItems + 48 * kPxRing;                        // int[kPxRing][32]: an item's first pages
   static constexpr int kMisc = kPages + 128 * kPxRing;
-  static constexpr int kTotal = kMisc + 48;
+  static constexpr int kThere = kMisc + 48;                                   // int[kRS]: pages of a tile of codes that exist, a bit each
+  static constexpr int kTotal = kThere + (4 * kRS + 15) / 16 * 16;
   static_assert(kPxWords * 4 <= 48, "words of the CTA");
   static_assert(kTotal <= 232448, "shared memory of a CTA exceeded");
 };
@@ -201,11 +221,50 @@ static __device__ __noinline__ void px_report(int* err, int code, int where, int
   }
 }
 
+// Where the keys and values come from.
+struct PrefixTiles {      // bf16: tensor maps of a page, or of 16 keys
+  static constexpr bool kQ4 = false;
+  CUtensorMap k, v;
+};
+struct PrefixCodes {      // 4 bits: blocks of 16 keys
+  static constexpr bool kQ4 = true;
+  Q4Pool k, v;
+};
+
+// A lane's row of a tile: of codes (blocks of 16 tokens) and of panels of 64 channels, 128-byte swizzled.  A group of channels at a time,
+// which one is another's turn from lane to lane so that (with 128 channels) the eight lanes of a phase read from eight different places of 128 bytes and write to eight as
+// well.  A loop and not its turns in a row: those are 5 KB, and what the softmax groups run through fills the instruction cache (tiles took twice as long).
 template <int D>
-__global__ void __launch_bounds__(kPxThreads, 1)
-prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const __grid_constant__ CUtensorMap tmq_own,
-                   const __grid_constant__ CUtensorMap tmq_pre, const __grid_constant__ CUtensorMap tmo, const __grid_constant__ PrefixParams p) {
-  using L_ = PrefixSmem<D>;
+struct WidenRow {
+  uint32_t codes, scales, row, first;
+  __device__ __forceinline__ explicit WidenRow(int r)
+      : codes((r / kQ4Tokens) * q4_block_bytes(D) + (r % kQ4Tokens) * (D / 2)),
+        scales((r / kQ4Tokens) * q4_block_bytes(D) + q4_scales_at(D) + (r % kQ4Tokens) * (D / 16)), row(r * 128 + ((r & 7) << 4)),
+        first(D == 128 ? (r >> 1) & 3 : 0) {}
+  __device__ __forceinline__ void operator()(uint32_t raw, uint32_t tile, bool there) const {
+#pragma unroll 1
+    for (int turn = 0; turn < D / kQ4Group; turn++) {
+      const uint32_t g = first ^ turn;
+      uint32_t w[4], s2;
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(raw + codes + g * (kQ4Group / 2)));
+      asm volatile("{.reg .b16 x; ld.shared.b16 x, [%1]; mov.b32 %0, {x, x};}" : "=r"(s2) : "r"(raw + scales + 2 * g));
+      if (!there) s2 = 0u;
+      const uint32_t c2 = q4_offset(s2), to = ((tile + row) ^ ((g & 1) << 6)) + (g >> 1) * (128 * 128);
+#pragma unroll
+      for (int i = 0; i < 4; i++)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to ^ (i << 4)), "r"(q4_pair(w[i], 0, s2, c2)), "r"(q4_pair(w[i], 1, s2, c2)),
+                     "r"(q4_pair(w[i], 2, s2, c2)), "r"(q4_pair(w[i], 3, s2, c2))
+                     : "memory");
+    }
+  }
+};
+
+template <int D, class Source>
+__global__ void __launch_bounds__(px_threads(Source::kQ4), 1)
+prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ CUtensorMap tmq_own, const __grid_constant__ CUtensorMap tmq_pre,
+                   const __grid_constant__ CUtensorMap tmo, const __grid_constant__ PrefixParams p) {
+  constexpr bool Q4 = Source::kQ4;
+  using L_ = PrefixSmem<D, Q4>;
   constexpr int NPANEL = D / 64, PANEL = 128 * 128, KS = L_::kKS, VS = L_::kVS;
   constexpr unsigned FULLM = 0xffffffffu;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -218,8 +277,8 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
                 S_FULL = V_EMPTY + VS, S_FREE = S_FULL + 2, P_FULL = S_FREE + 2 /* + 2*group + half */, P_FREE = P_FULL + 4, O_FULL = P_FREE + 2,
                 O_FREE = O_FULL + 1, MREF = O_FREE + 1, ITEM_FULL = MREF + 1, ITEM_EMPTY = ITEM_FULL + kPxRing, QK_DRAIN = ITEM_EMPTY + kPxRing,
                 PV_DRAIN = QK_DRAIN + 1, LSUM_A = PV_DRAIN + 1, LSUM_B = LSUM_A + 1, STAGED = LSUM_B + 1,
-                DONE = STAGED + 1;
-  static_assert(DONE + 1 <= L_::kNumBars, "barrier table too small");
+                DONE = STAGED + 1, RAW_FULL = DONE + 1, RAW_EMPTY = RAW_FULL + L_::kRS;
+  static_assert(RAW_EMPTY + L_::kRS <= L_::kNumBars, "barrier table too small");
   constexpr uint32_t TM_O = 256, TM_P = 256 + D;      // tensor memory: S of group 0 | S of group 1 | O | P of group 0 | P of group 1
   float* mref_s = reinterpret_cast<float*>(smem + L_::kStats);
   float* lsum_s = mref_s + 128;
@@ -231,15 +290,15 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
   const bool aligned = (smem_u32(smem) & 1023u) == 0u;
   if (tid == 0) {
     for (int s = 0; s < 2; s++) {
-      mbar_init(BAR(Q_FULL + s), 32 * kPxQWarps);
+      mbar_init(BAR(Q_FULL + s), 32 * px_q_warps(Q4));
       mbar_init(BAR(Q_EMPTY + s), 1);
     }
     for (int s = 0; s < KS; s++) {
-      mbar_init(BAR(K_FULL + s), 1);
+      mbar_init(BAR(K_FULL + s), Q4 ? kPxCodeWarps : 1);
       mbar_init(BAR(K_EMPTY + s), 1);
     }
     for (int s = 0; s < VS; s++) {
-      mbar_init(BAR(V_FULL + s), 1);
+      mbar_init(BAR(V_FULL + s), Q4 ? kPxCodeWarps : 1);
       mbar_init(BAR(V_EMPTY + s), 1);
     }
     for (int g = 0; g < 2; g++) {
@@ -251,7 +310,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     }
     for (int r = 0; r < kPxRing; r++) {
       mbar_init(BAR(ITEM_FULL + r), 1);
-      mbar_init(BAR(ITEM_EMPTY + r), kPxConsumers);
+      mbar_init(BAR(ITEM_EMPTY + r), px_consumers(Q4));
     }
     mbar_init(BAR(O_FULL), 1);
     mbar_init(BAR(O_FREE), 256);
@@ -262,12 +321,18 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     mbar_init(BAR(LSUM_B), 256);
     mbar_init(BAR(STAGED), 256);
     mbar_init(BAR(DONE), 1);
+    for (int r = 0; r < L_::kRS; r++) {
+      mbar_init(BAR(RAW_FULL + r), 1);
+      mbar_init(BAR(RAW_EMPTY + r), kPxCodeWarps);
+    }
     for (int i = kPxStop; i < kPxWords; i++) misc[i] = 0;
     fence_mbar_init();
-    prefetch_tmap(&tmk);
-    prefetch_tmap(&tmv);
-    prefetch_tmap(&tmq_own);
-    if (S.stack) prefetch_tmap(&tmq_pre);
+    if constexpr (!Q4) {
+      prefetch_tmap(&src.k);
+      prefetch_tmap(&src.v);
+    }
+    if (S.own_box > 0 && !S.own_off) prefetch_tmap(&tmq_own);
+    if (S.pre_box > 0) prefetch_tmap(&tmq_pre);
   }
   if (warp == 2) {
     tmem_alloc(smem_u32(smem + L_::kMisc), 512);
@@ -324,11 +389,104 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
   if (!aligned) {
     if (tid == 0) report(AVSA_ERR_CUDA, kPxAlign, blockIdx.x, 0);
     if (tid == 0 && blockIdx.x == 0) p.plan[0] = p.plan[2] = 0;
-  } else if (warp == 0 || warp == 12) {
+  } else if (Q4 && warp == 0) {
+    // ------------------------------------------------------------------ tiles of codes, K and V in turn; and the watch, in each wait and behind the last item
+    fewer_regs<px_service_regs(Q4)>();
+    if constexpr (Q4) {
+      int* const there = reinterpret_cast<int*>(smem + L_::kThere);
+      const int ppt_shift = 7 - S.page_shift, ppt = 1 << ppt_shift, page_bytes = S.page * q4_token_bytes(D);
+      int stage = 0, round = 0, loads = 0;
+      bool ok = true;
+      long long since = clock64();
+      int seen = 0;
+      auto watch = [&]() {
+        if (lane == 0) {
+          const int now = misc[kPxProgress];
+          if (now != seen) {
+            seen = now;
+            since = clock64();
+          } else if (clock64() - since > AVSA_WAIT_LIMIT_CYCLES) {
+            misc[kPxStop] = 1;
+          }
+        }
+      };
+      auto wait_watching = [&](int bar, uint32_t parity, int where) -> bool {
+        while (!mbar_try_wait(BAR(bar), parity)) {
+          if (misc[kPxStop] != 0) {
+            misc[kPxWhere] = where;
+            return false;
+          }
+          watch();
+          __nanosleep(64);
+        }
+        return true;
+      };
+#pragma unroll 1
+      for (int n = 0; ok; n++) {
+        PrefixItem it;
+        if (!__all_sync(FULLM, wait_watching(ITEM_FULL + n % kPxRing, (n / kPxRing) & 1, kPxItem)) || !get_item(n, it)) break;
+        const int32_t* row = p.table + static_cast<int64_t>(max(it.slot, 0)) * S.width;
+        const int e0 = it.pos0 >> S.page_shift;
+        const int e1 = min(e0 + (it.cnt << ppt_shift), (it.kv_end + S.page - 1) >> S.page_shift);
+        const int per = 32 >> ppt_shift, kinds = (it.type >> 1) != 1 ? 2 : 1;
+        int mine = ring_pages[(n % kPxRing) * 32 + lane];
+#pragma unroll 1
+        for (int t0 = 0; t0 < it.cnt && ok; t0 += per) {
+          int next = S.pages;
+          const int e = e0 + ((t0 + per) << ppt_shift) + lane;
+          if (e < e1) next = row[e];
+          const int nn = min(per, it.cnt - t0);
+#pragma unroll 1
+          for (int j = 0; j < nn && ok; j++) {
+            const int id = __shfl_sync(FULLM, mine, (j << ppt_shift) + (lane & (ppt - 1)));
+            const bool mine_is = lane < ppt && id >= 0 && id < S.pages;
+            const unsigned bits = __ballot_sync(FULLM, mine_is);
+#pragma unroll 1
+            for (int kind = 0; kind < kinds; kind++) {
+              if (round > 0) ok = __all_sync(FULLM, wait_watching(RAW_EMPTY + stage, (round - 1) & 1, kind == 0 ? kPxKEmpty : kPxVEmpty));
+              if (!ok) break;
+              if (lane == 0) {
+                there[stage] = static_cast<int>(bits);
+                if (bits != 0u) {
+                  mbar_expect_tx(BAR(RAW_FULL + stage), __popc(bits) * page_bytes);
+                } else {
+                  mbar_arrive(BAR(RAW_FULL + stage));
+                }
+              }
+              __syncwarp();
+              if (mine_is) {
+                const Q4Pool& pool = kind == 0 ? src.k : src.v;
+                bulk_load_1d(smem_u32(smem + L_::kRaws) + stage * L_::kRaw + lane * page_bytes, pool.ptr + id * pool.stride_page + it.hk * pool.stride_head, page_bytes,
+                             BAR(RAW_FULL + stage));
+              }
+              loads++;
+              if (lane == 0) misc[kPxProgress] = loads;
+              if (++stage == L_::kRS) {
+                stage = 0;
+                round++;
+              }
+            }
+          }
+          if (next < 0 || next > S.pages) {
+            report(AVSA_ERR_BAD_TABLE, kPrefixPage, it.slot, e);
+            next = S.pages;
+          }
+          mine = next;
+        }
+        if (ok) item_done(n);
+      }
+      if (lane == 0) {
+        while (!mbar_try_wait(BAR(DONE), 0) && misc[kPxStop] == 0) watch();
+        if (misc[kPxStop] != 0)      // loads still in flight must land before this CTA's shared memory is given away
+          for (int c = max(0, loads - L_::kRS); c < loads; c++) mbar_wait(BAR(RAW_FULL + c % L_::kRS), (c / L_::kRS) & 1);
+      }
+    }
+  } else if (!Q4 && (warp == 0 || warp == 12)) {
     // ------------------------------------------------------------------ TMA producers: warp 0 K, warp 12 V
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    fewer_regs<px_service_regs(Q4)>();
+    if constexpr (!Q4) {
     const bool is_k = warp == 0;
-    const CUtensorMap* tm = is_k ? &tmk : &tmv;
+    const CUtensorMap* tm = is_k ? &src.k : &src.v;
     const int FULL = is_k ? K_FULL : V_FULL, EMPTY = is_k ? K_EMPTY : V_EMPTY, STAGES = is_k ? KS : n_vs;
     const uint32_t base = smem_u32(smem + (is_k ? L_::kK : L_::kV));
     const int ppt_shift = 7 - S.page_shift, ppt = 1 << ppt_shift;      // pages of a tile
@@ -386,25 +544,26 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     }
     if (lane == 0 && misc[kPxStop] != 0)      // loads still in flight must land before this CTA's shared memory is given away
       for (int c = max(0, loads - STAGES); c < loads; c++) mbar_wait(BAR(FULL + c % STAGES), (c / STAGES) & 1);
-  } else if (warp == 13 || warp == 14) {
-    // ------------------------------------------------------------------ query rows into shared memory, 128-byte swizzled like a TMA tile
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    }
+  } else if (Q4 ? warp >= 12 : warp == 13 || warp == 14) {
+    // ------------------------------------------------------------------ query rows into shared memory, 128-byte swizzled like a TMA tile; and tiles of codes
+    fewer_regs<px_service_regs(Q4)>();
     constexpr int VPR = D / 8, RPI = 32 / VPR;      // 16-byte vectors of a row; rows of an instruction
     const uint32_t base = smem_u32(smem + L_::kQ);
+    const int q_warp = Q4 ? warp & 3 : warp - 13;
     int q_loads = 0;          // items up to the last one whose rows came by TMA
     bool ok = true;
-#pragma unroll 1
-    for (int n = 0; ok; n++) {
-      PrefixItem it;
-      if (!get_item(n, it)) break;
+    // One item's rows: in front of its first product, behind the last one of the item before it (with one buffer).
+    auto gather = [&](int n, const PrefixItem& it) -> bool {
+      bool ok = true;
       if (n >= 2) ok = __all_sync(FULLM, wait_idly(Q_EMPTY + (n & 1), ((n >> 1) - 1) & 1, kPxQEmpty));
       if (ok && n >= 1 && L_::kQSlot == 0) ok = __all_sync(FULLM, wait_idly(Q_EMPTY + ((n - 1) & 1), ((n - 1) >> 1) & 1, kPxQEmpty));      // one buffer
-      if (!ok) break;
+      if (!ok) return false;
       const uint32_t dst = base + (n & 1) * L_::kQSlot;
       const bool stacked = (it.type & 1) != 0;
       const int box = stacked ? S.pre_box : S.own_box;
       if (box > 0) {
-        if (warp == 13 && lane == 0) {
+        if (q_warp == 0 && lane == 0) {
           mbar_expect_tx(BAR(Q_FULL + (n & 1)), box * 128 * NPANEL);
           const int token = stacked ? 0 : S.by_G.div(it.row0), entry = stacked ? S.by_R.div(it.row0) : it.b;
           for (int pn = 0; pn < NPANEL; pn++)
@@ -413,11 +572,10 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
           mbar_arrive(BAR(Q_FULL + (n & 1)));
         }
         q_loads = n + 1;
-        item_done(n);
-        continue;
+        return true;
       }
 #pragma unroll 1
-      for (int r0 = (warp - 13) * 32; r0 < it.nrows; r0 += 32 * kPxQWarps) {
+      for (int r0 = q_warp * 32; r0 < it.nrows; r0 += 32 * px_q_warps(Q4)) {
         int64_t off = 0;
         if (r0 + lane < it.nrows) {
           int rr = it.row0 + r0 + lane, b = it.b;
@@ -441,13 +599,62 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       asm volatile("cp.async.wait_all;" ::: "memory");
       fence_proxy_async();
       mbar_arrive(BAR(Q_FULL + (n & 1)));
-      item_done(n);
+      return true;
+    };
+    if constexpr (Q4) {
+      // Warps 12 to 15 make the tiles of keys, a row a lane, 16 to 19 those of values and gather the query rows.
+      const bool is_k = warp < 16;
+      const int FULL = is_k ? K_FULL : V_FULL, EMPTY = is_k ? K_EMPTY : V_EMPTY, STAGES = is_k ? KS : n_vs, r = q_warp * 32 + lane;
+      const int where_full = is_k ? kPxKFull : kPxVFull, where_empty = is_k ? kPxKEmpty : kPxVEmpty;
+      const WidenRow<D> widen(r);
+      const uint32_t raws = smem_u32(smem + L_::kRaws), tiles = smem_u32(smem + (is_k ? L_::kK : L_::kV));
+      const int* const there = reinterpret_cast<const int*>(smem + L_::kThere);
+      int raw = 0, raw_round = 0, stage = 0, round = 0;
+      auto pass_raw = [&](int n) {      // at most kRS of them
+        raw += n;
+        if (raw >= L_::kRS) raw -= L_::kRS, raw_round ^= 1;
+      };
+#pragma unroll 1
+      for (int n = 0; ok; n++) {
+        PrefixItem it;
+        if (!get_item(n, it)) break;
+        if (!is_k) ok = gather(n, it);
+        const int kinds = (it.type >> 1) != 1 ? 2 : 1;      // tiles of keys alone, or of both in turn
+        int left = it.kv_end - it.pos0 - r;                 // the lane has a key of the tile where it is above 0
+#pragma unroll 1
+        for (int t = 0; t < it.cnt && ok; t++, left -= 128) {
+          if (!is_k) pass_raw(1);
+          if (is_k || kinds == 2) {
+            if (round > 0) ok = __all_sync(FULLM, wait_idly(EMPTY + stage, (round - 1) & 1, where_empty));
+            if (ok) ok = wait_all(RAW_FULL + raw, raw_round, where_full);
+            if (!ok) break;
+            widen(raws + raw * L_::kRaw, tiles + stage * L_::kTile, left > 0 && (there[raw] >> (r >> S.page_shift) & 1) != 0);
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+              mbar_arrive(BAR(RAW_EMPTY + raw));
+              mbar_arrive(BAR(FULL + stage));
+            }
+            if (++stage == STAGES) stage = 0, round++;
+            pass_raw(is_k ? kinds : 1);
+          }
+        }
+        if (ok) item_done(n);
+      }
+    } else {
+#pragma unroll 1
+      for (int n = 0; ok; n++) {
+        PrefixItem it;
+        if (!get_item(n, it)) break;
+        ok = gather(n, it);
+        if (ok) item_done(n);
+      }
     }
     if (misc[kPxStop] != 0)
       for (int c = max(0, q_loads - 2); c < q_loads; c++) mbar_wait(BAR(Q_FULL + (c & 1)), (c >> 1) & 1);
   } else if (warp == 3) {
     // ------------------------------------------------------------------ scheduler
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    fewer_regs<px_service_regs(Q4)>();
     const int n_cta = gridDim.x;
     int published = 0;
     // The last published item, and all before it, are done.
@@ -707,7 +914,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ Q K^T issuer
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    fewer_regs<px_service_regs(Q4)>();
     const bool leader = elect_one_sync();
     constexpr uint32_t desc_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
     constexpr uint32_t idesc_qk = make_idesc_bf16(128, 128, 0, 0);
@@ -764,7 +971,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     }
   } else if (warp == 2) {
     // ------------------------------------------------------------------ P V issuer
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    fewer_regs<px_service_regs(Q4)>();
     const bool leader = elect_one_sync();
     constexpr uint32_t desc_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
     constexpr uint32_t idesc_pv = make_idesc_bf16(128, D, 0, 1);
@@ -793,7 +1000,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
           ok = wait_all(V_FULL + stage, round & 1, kPxVFull);
           if (!ok) break;
           const int valid = it.kv_end - it.pos0 - t * 128;
-          if (valid > 0 && valid < 128 && (valid & (S.page - 1)) != 0) {
+          if (!Q4 && valid > 0 && valid < 128 && (valid & (S.page - 1)) != 0) {
             // behind the last token its page may hold anything; P is zero there, and 0 * NaN is not
             const int end = (valid + S.page - 1) & ~(S.page - 1);
             uint8_t* tile = smem + L_::kV + stage * L_::kTile;
@@ -841,9 +1048,9 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
       __syncwarp();
       mbar_wait(BAR(PV_DRAIN), 0);
     }
-  } else if (warp == 15) {
+  } else if (!Q4 && warp == 15) {
     // ------------------------------------------------------------------ the watch: no key tile for a second, and every wait ends
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    fewer_regs<px_service_regs(Q4)>();
     if (lane == 0) {
       long long since = clock64();
       int seen = 0;
@@ -859,7 +1066,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constan
     }
   } else {
     // ------------------------------------------------------------------ softmax groups + epilogue
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+    more_regs<px_softmax_regs(Q4)>();
     const int w = (warp - 4) >> 2;
     const int row = ((warp & 3) << 5) + lane;
     const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;

@@ -41,7 +41,7 @@ struct StreamParams {
 enum { kStJoinStream = 1, kStJoinTile = 2 };
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -150,21 +150,11 @@ __device__ __forceinline__ void prefix_check_begin(const PrefixParams& p) {
 // with two products' the warps take longer and want more ahead (32 sequences x 8 x 2048 keys, 16 rows: 71.5 and 58.0).
 constexpr int stream_ctas(int NT, bool q4) { return q4 ? (NT == 1 ? 4 : 3) : NT == 1 ? 3 : 2; }
 
-// Where the keys and values come from.
-struct StreamTiles {      // bf16, tensor maps of 16 keys
-  static constexpr bool kQ4 = false;
-  CUtensorMap k, v;
-};
-struct StreamCodes {      // 4 bits, blocks of 16 keys
-  static constexpr bool kQ4 = true;
-  Q4Pool k, v;
-};
-
 template <int D, int NT, bool Q4>
 struct StreamSmem {
   static constexpr int kPanel = 16 * 128, kBlock = q4_block_bytes(D);
-  static constexpr int kStages = Q4 ? 4 * (128 / D) : (NT == 1 ? 2 : 3) * (128 / D);
-  static constexpr int kStage = Q4 ? 2 * kBlock : 2 * (D / 64) * kPanel;      // a stage: panels of K, panels of V, or a block of each
+  static constexpr int kStages = Q4 ? 3 * (128 / D) : (NT == 1 ? 2 : 3) * (128 / D);
+  static constexpr int kStage = Q4 ? 4 * kBlock : 2 * (D / 64) * kPanel;      // a stage: panels of K, panels of V, or two blocks of each
   union {
     uint8_t ring[kStWarps][kStages][kStage];      // 128-byte swizzled
     float4 o[kStWarps][kStRows][D / 4];           // behind the keys; [0] becomes the CTA's
@@ -177,6 +167,227 @@ struct StreamSmem {
 // The key of a block of codes that is row r (of 8) of S^T.  Keys' codes are 64 bytes apart (128 channels), so that a product's operands come from shared memory without
 // two lanes of a phase at one bank where neighbouring rows, and rows two apart, alternate between even and odd keys.
 __device__ __forceinline__ int stream_key(int r) { return r ^ ((r >> 1) & 1); }
+
+// The keys of a warp, where they are codes: pairs of blocks of 16 (one piece of memory of 4.6 KB each of K and V, with pages of 32 and more), from block `blk` on, every
+// `step`-th.  Rows as in the kernel below.  A block takes some 300 instructions, 3 for each pair of values, where its bytes take 100 cycles of the SM's share of HBM, so that
+// what counts is how many of them are issued: two blocks side by side, for each of which the other's latencies are filled; the rows' maxima looked at
+// by every lane for itself, and brought together only where one has outgrown its reference.
+template <int D, int NT, class Smem>
+__device__ __forceinline__ void stream_codes(const PrefixCodes& src, const PrefixParams& p, Smem& sm, const int32_t* pages, int hk, int blk, int step, int b1, int k1,
+                                             int rel_min, const int (&see)[NT][2], const uint4 (&q)[NT][D / 32], float (&o)[NT][D / 16][4], float (&m)[NT][2],
+                                             float (&l)[NT][2], int item) {
+  constexpr unsigned FULLM = 0xffffffffu;
+  constexpr int STAGES = Smem::kStages, BLOCK = Smem::kBlock, G = D / kQ4Group;
+  const PrefixShape& S = p.s;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, c = lane & 3, block_shift = S.page_shift - 4;
+  const uint32_t ring = smem_u32(&sm.ring[warp][0][0]), full = smem_u32(&sm.full[warp][0]);
+  const bool single = block_shift == 0;      // a page is one block: pairs are two pages
+  const uint8_t* const k_head = src.k.ptr + hk * src.k.stride_head;
+  const uint8_t* const v_head = src.v.ptr + hk * src.v.stride_head;
+  auto page_of = [&](int at) { return at < b1 ? pages[at >> block_shift] : -1; };
+  auto exists = [&](int page) { return static_cast<unsigned>(page) < static_cast<unsigned>(S.pages); };
+  auto load = [&](int at, int page0, int page1, int stage) {
+    if (at >= b1) return;
+    const uint32_t bar = full + stage * 8, dst = ring + stage * Smem::kStage;
+    const bool has0 = exists(page0), has1 = exists(page1);
+    if (!(has0 && (has1 || at + 1 >= b1))) {
+      // a page that does not exist reads as zeros: scales of zero, the codes may be anything
+      for (int h = 0; h < 2; h++)
+        if (!(h == 0 ? has0 : has1))
+          for (int w = lane; w < D / 4; w += 32) {
+            *reinterpret_cast<uint32_t*>(&sm.ring[warp][stage][h * BLOCK + q4_scales_at(D) + 4 * w]) = 0u;
+            *reinterpret_cast<uint32_t*>(&sm.ring[warp][stage][(2 + h) * BLOCK + q4_scales_at(D) + 4 * w]) = 0u;
+          }
+      fence_proxy_async();      // (a copy lands there later)
+      __syncwarp();
+    }
+    if (lane == 0) {
+      if (!single && has0) {
+        const int64_t in = page0 * src.k.stride_page + static_cast<int64_t>(at & ((1 << block_shift) - 1)) * BLOCK;
+        const int64_t in_v = page0 * src.v.stride_page + static_cast<int64_t>(at & ((1 << block_shift) - 1)) * BLOCK;
+        mbar_expect_tx(bar, 4 * BLOCK);
+        bulk_load_1d(dst, k_head + in, 2 * BLOCK, bar);
+        bulk_load_1d(dst + 2 * BLOCK, v_head + in_v, 2 * BLOCK, bar);
+      } else if (single && (has0 || has1)) {
+        mbar_expect_tx(bar, ((has0 ? 2 : 0) + (has1 ? 2 : 0)) * BLOCK);
+        if (has0) {
+          bulk_load_1d(dst, k_head + page0 * src.k.stride_page, BLOCK, bar);
+          bulk_load_1d(dst + 2 * BLOCK, v_head + page0 * src.v.stride_page, BLOCK, bar);
+        }
+        if (has1) {
+          bulk_load_1d(dst + BLOCK, k_head + page1 * src.k.stride_page, BLOCK, bar);
+          bulk_load_1d(dst + 3 * BLOCK, v_head + page1 * src.v.stride_page, BLOCK, bar);
+        }
+      } else {
+        mbar_arrive(bar);
+      }
+    }
+  };
+  int ahead = blk, next0 = page_of(ahead), next1 = single ? page_of(ahead + 1) : next0;
+  auto load_next = [&](int stage) {
+    const int page0 = next0, page1 = next1;
+    next0 = page_of(ahead + step);
+    next1 = single ? page_of(ahead + step + 1) : next0;
+    load(ahead, page0, page1, stage);
+    ahead += step;
+  };
+#pragma unroll 1
+  for (int k = 0; k < STAGES; k++) load_next(k);
+  const int key = stream_key(n), key0 = stream_key(2 * c), key1 = stream_key(2 * c + 1);      // as an operand's rows; as its columns
+  const float inv_scale = 1.0f / p.scale_log2;
+  float limit[NT][2], ref[NT][2];      // logits above it outgrow the reference; the reference, 0 where there is none
+#pragma unroll
+  for (int x = 0; x < NT; x++) limit[x][0] = limit[x][1] = -INFINITY, ref[x][0] = ref[x][1] = 0.f;
+  int stage = 0, round = 0;
+  bool ok = true;
+#pragma unroll 1
+  for (; blk < b1; blk += step) {
+    if (!__all_sync(FULLM, mbar_wait(full + stage * 8, round & 1))) {
+      ok = false;
+      break;
+    }
+    const uint8_t* const tile = &sm.ring[warp][stage][0];
+    // ---- S^T: lane (n, c) has a quarter of the channels of keys `key` and `key` + 8, in whole words
+    float s[2][NT][4] = {};
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      constexpr int W = D / 32;
+      const uint8_t* const k = tile + h * BLOCK;
+      uint32_t ka[W], kb[W];
+      if constexpr (W == 4) {
+        *reinterpret_cast<uint4*>(ka) = *reinterpret_cast<const uint4*>(k + key * (D / 2) + 16 * c);
+        *reinterpret_cast<uint4*>(kb) = *reinterpret_cast<const uint4*>(k + (key + 8) * (D / 2) + 16 * c);
+      } else {
+        *reinterpret_cast<uint2*>(ka) = *reinterpret_cast<const uint2*>(k + key * (D / 2) + 8 * c);
+        *reinterpret_cast<uint2*>(kb) = *reinterpret_cast<const uint2*>(k + (key + 8) * (D / 2) + 8 * c);
+      }
+      const uint16_t* const scales = reinterpret_cast<const uint16_t*>(k + q4_scales_at(D)) + c * (D / 4) / kQ4Group;
+      uint32_t sa = scales[key * G], sb = scales[(key + 8) * G];
+      sa |= sa << 16;
+      sb |= sb << 16;
+      const uint32_t oa = q4_offset(sa), ob = q4_offset(sb);
+#pragma unroll
+      for (int j = 0; j < W; j++) {
+        uint32_t a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) a[i] = q4_pair(ka[j], i, sa, oa), b[i] = q4_pair(kb[j], i, sb, ob);
+#pragma unroll
+        for (int x = 0; x < NT; x++) {
+          mma_16816(s[h][x], a[0], b[0], a[1], b[1], q[x][j].x, q[x][j].y);
+          mma_16816(s[h][x], a[2], b[2], a[3], b[3], q[x][j].z, q[x][j].w);
+        }
+      }
+    }
+    if (blk * 16 + 32 > rel_min || blk * 16 + 32 > k1) {
+#pragma unroll
+      for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int x = 0; x < NT; x++)
+#pragma unroll
+          for (int e = 0; e < 4; e++)
+            if ((blk + h) * 16 + key + 8 * (e >> 1) >= min(see[x][e & 1], k1)) s[h][x][e] = -INFINITY;
+    }
+    // ---- maxima
+    float top[NT][2];
+    bool grown = false;
+#pragma unroll
+    for (int x = 0; x < NT; x++)
+#pragma unroll
+      for (int e = 0; e < 2; e++) {
+        top[x][e] = fmaxf(max3f(s[0][x][e], s[0][x][2 + e], s[1][x][e]), s[1][x][2 + e]);
+        grown = grown || top[x][e] > limit[x][e];
+      }
+    if (__any_sync(FULLM, grown)) {
+#pragma unroll
+      for (int x = 0; x < NT; x++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          float up = top[x][e];
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) up = fmaxf(up, __shfl_xor_sync(FULLM, up, d));
+          up = fmaxf(m[x][e], up * p.scale_log2);
+          const float f = m[x][e] == -INFINITY ? 0.f : fast_exp2(m[x][e] - up);
+          m[x][e] = up;
+          limit[x][e] = (up + 8.f) * inv_scale;
+          ref[x][e] = up == -INFINITY ? 0.f : up;
+          l[x][e] *= f;
+#pragma unroll
+          for (int y = 0; y < D / 16; y++) {
+            o[x][y][e] *= f;
+            o[x][y][2 + e] *= f;
+          }
+        }
+    }
+    // ---- P^T
+    uint32_t pt[2][NT][2];
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+#pragma unroll
+      for (int x = 0; x < NT; x++) {
+        float w[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          w[e] = fast_exp2(fmaf(s[h][x][e], p.scale_log2, -ref[x][e & 1]));
+          l[x][e & 1] += w[e];
+        }
+        pt[h][x][0] = transpose_8x8(pack_bf16x2(w[0], w[1]));
+        pt[h][x][1] = transpose_8x8(pack_bf16x2(w[2], w[3]));
+      }
+    // ---- O^T: lane (n, c) has an eighth of the channels of the keys that are rows 2c, 2c + 1, 2c + 8 and 2c + 9 of S^T
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      constexpr int W = D / 64;
+      const uint8_t* const v = tile + (2 + h) * BLOCK;
+      uint32_t w0[W], w1[W], w2[W], w3[W];
+      auto codes = [&](int at, uint32_t (&w)[W]) {
+        if constexpr (W == 2) {
+          *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(v + at * (D / 2) + 8 * n);
+        } else {
+          w[0] = *reinterpret_cast<const uint32_t*>(v + at * (D / 2) + 4 * n);
+        }
+      };
+      codes(key0, w0);
+      codes(key1, w1);
+      codes(key0 + 8, w2);
+      codes(key1 + 8, w3);
+      const uint16_t* const scales = reinterpret_cast<const uint16_t*>(v + q4_scales_at(D)) + n * (D / 8) / kQ4Group;
+      uint32_t s0 = scales[key0 * G], s1 = scales[key1 * G], s2 = scales[(key0 + 8) * G], s3 = scales[(key1 + 8) * G];
+      if (blk * 16 + 32 > k1) {
+        // behind the last token its page may hold anything; P is zero there, and 0 * NaN is not
+        const int left = k1 - (blk + h) * 16;
+        if (key0 >= left) s0 = 0u;
+        if (key1 >= left) s1 = 0u;
+        if (key0 + 8 >= left) s2 = 0u;
+        if (key1 + 8 >= left) s3 = 0u;
+      }
+      s0 |= s1 << 16;
+      s2 |= s3 << 16;
+      const uint32_t o0 = q4_offset(s0), o2 = q4_offset(s2);
+#pragma unroll
+      for (int j = 0; j < W; j++) {
+        const uint32_t e0 = __byte_perm(w0[j], w1[j], 0x5410), d0 = __byte_perm(w0[j], w1[j], 0x7632);      // even channels of both keys, odd ones
+        const uint32_t e2 = __byte_perm(w2[j], w3[j], 0x5410), d2 = __byte_perm(w2[j], w3[j], 0x7632);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          const uint32_t a0 = q4_pair(e0, i, s0, o0), a1 = q4_pair(d0, i, s0, o0), a2 = q4_pair(e2, i, s2, o2), a3 = q4_pair(d2, i, s2, o2);
+#pragma unroll
+          for (int x = 0; x < NT; x++) mma_16816(o[x][4 * j + i], a0, a1, a2, a3, pt[h][x][0], pt[h][x][1]);
+        }
+      }
+    }
+    __syncwarp();      // all lanes have read the stage
+    load_next(stage);
+    if (++stage == STAGES) {
+      stage = 0;
+      round++;
+    }
+  }
+  if (!ok) {
+    // a load never came: the status says so, the rows lack this warp's keys from there on, and what is under way lands before this memory is given away
+    report_logged(p.status, p.log, AVSA_ERR_TIMEOUT, kPxKFull, item, blk);
+    for (int k = 0; k < STAGES; k++) mbar_wait(full + k * 8, (round + (k < stage ? 1 : 0)) & 1);
+  }
+}
 
 // Where the parts of the beginning of stacked row rho are: `n` of them, `step` rows apart.
 __device__ __forceinline__ void prefix_parts(const PrefixParams& p, const StreamParams& t, int hk, int rho, int& first, int& step, int& n) {
@@ -317,59 +528,10 @@ prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__
   // 16-key blocks [b0, b1) of the part, every `step`-th from the warp's own on
   int b0 = k0 >> 4, b1 = (k1 + 15) >> 4;
   if (t.splits > 1) {
-    const int per = (b1 - b0 + t.splits - 1) / t.splits;
+    int per = (b1 - b0 + t.splits - 1) / t.splits;
+    if (Q4) per = (per + 1) & ~1;      // (pairs of blocks)
     b0 = min(b1, b0 + split * per);
     b1 = min(b1, b0 + per);
-  }
-  const int step = ctas * kStWarps;
-  const int block_shift = S.page_shift - 4;
-  const int32_t* const pages = p.table + static_cast<int64_t>(max(slot, 0)) * S.width;
-  constexpr int STAGES = L_::kStages, PANEL = L_::kPanel, NPANEL = D / 64;
-  const uint32_t ring = smem_u32(&sm.ring[warp][0][0]), full = smem_u32(&sm.full[warp][0]);
-  // (a page that does not exist reads as zeros)
-  auto load = [&](int blk, int page, int stage) {
-    if constexpr (Q4) {
-      if (blk >= b1) return;
-      const uint32_t bar = full + stage * 8, dst = ring + stage * L_::kStage;
-      if (static_cast<unsigned>(page) < static_cast<unsigned>(S.pages)) {
-        if (lane == 0) {
-          const int64_t in = static_cast<int64_t>(blk & ((1 << block_shift) - 1)) * L_::kBlock;
-          mbar_expect_tx(bar, L_::kStage);
-          bulk_load_1d(dst, src.k.ptr + page * src.k.stride_page + hk * src.k.stride_head + in, L_::kBlock, bar);
-          bulk_load_1d(dst + L_::kBlock, src.v.ptr + page * src.v.stride_page + hk * src.v.stride_head + in, L_::kBlock, bar);
-        }
-      } else {
-        // scales of zero; the codes may be anything
-        for (int at = lane; at < D / 16 * 16 / 4; at += 32) {
-          *reinterpret_cast<uint32_t*>(&sm.ring[warp][stage][q4_scales_at(D) + 4 * at]) = 0u;
-          *reinterpret_cast<uint32_t*>(&sm.ring[warp][stage][L_::kBlock + q4_scales_at(D) + 4 * at]) = 0u;
-        }
-        fence_proxy_async();      // (a copy lands there later)
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar);
-      }
-    } else if (lane == 0 && blk < b1) {
-      const uint32_t bar = full + stage * 8, dst = ring + stage * L_::kStage;
-      const int in = (blk & ((1 << block_shift) - 1)) * 16, pg = page < 0 ? S.pages : page;
-      mbar_expect_tx(bar, L_::kStage);
-      for (int pn = 0; pn < NPANEL; pn++) tma_load_4d(dst + pn * PANEL, &src.k, bar, pn * 64, in, hk, pg);
-      for (int pn = 0; pn < NPANEL; pn++) tma_load_4d(dst + (NPANEL + pn) * PANEL, &src.v, bar, pn * 64, in, hk, pg);
-    }
-  };
-  // vectors of a stage: `chunk` of 16 bytes of row `key` in a panel
-  auto vec = [&](int stage, int panel, int key, int chunk) {
-    return *reinterpret_cast<const uint4*>(&sm.ring[warp][stage][panel * PANEL + key * 128 + ((chunk ^ (key & 7)) << 4)]);
-  };
-  auto page_of = [&](int blk) { return blk < b1 ? pages[blk >> block_shift] : -1; };
-
-  int blk = b0 + rank * kStWarps + warp, ahead = blk;
-  int next = page_of(ahead);
-#pragma unroll
-  for (int k = 0; k < STAGES; k++) {
-    const int page = next;
-    next = page_of(ahead + step);
-    load(ahead, page, k);
-    ahead += step;
   }
   float o[NT][D / 16][4];       // product 4j + y: {channel 64j + 8n + 2y (of codes (D/8)n + 8j + 2y), the next} x {row 2c, the next}, as [2 * channel + row]
 #pragma unroll
@@ -379,185 +541,143 @@ prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__
   float m[NT][2], l[NT][2];
 #pragma unroll
   for (int x = 0; x < NT; x++) m[x][0] = m[x][1] = -INFINITY, l[x][0] = l[x][1] = 0.f;
-  const int key = Q4 ? stream_key(n) : n;
-  int stage = 0, round = 0;
-  bool ok = true;
-#pragma unroll 1
-  for (; blk < b1; blk += step) {
-    if (!__all_sync(FULLM, mbar_wait(full + stage * 8, round & 1))) {
-      ok = false;
-      break;
-    }
-    float s[NT][2][4] = {};      // two chains of products each
-    if constexpr (Q4) {
-      // lane (n, c): a quarter of the channels of keys `key` and `key` + 8, in whole words
-      constexpr int W = D / 32;
-      const uint8_t* const k = &sm.ring[warp][stage][0];
-      uint32_t ka[W], kb[W];
-      if constexpr (W == 4) {
-        *reinterpret_cast<uint4*>(ka) = *reinterpret_cast<const uint4*>(k + key * (D / 2) + 16 * c);
-        *reinterpret_cast<uint4*>(kb) = *reinterpret_cast<const uint4*>(k + (key + 8) * (D / 2) + 16 * c);
-      } else {
-        *reinterpret_cast<uint2*>(ka) = *reinterpret_cast<const uint2*>(k + key * (D / 2) + 8 * c);
-        *reinterpret_cast<uint2*>(kb) = *reinterpret_cast<const uint2*>(k + (key + 8) * (D / 2) + 8 * c);
+  const int32_t* const pages = p.table + static_cast<int64_t>(max(slot, 0)) * S.width;
+  if constexpr (Q4) {
+    stream_codes<D, NT>(src, p, sm, pages, hk, b0 + 2 * (rank * kStWarps + warp), 2 * ctas * kStWarps, b1, k1, rel_min, see, q, o, m, l, item);
+  } else {
+    const int step = ctas * kStWarps;
+    const int block_shift = S.page_shift - 4;
+    constexpr int STAGES = L_::kStages, PANEL = L_::kPanel, NPANEL = D / 64;
+    const uint32_t ring = smem_u32(&sm.ring[warp][0][0]), full = smem_u32(&sm.full[warp][0]);
+    // (a page that does not exist reads as zeros)
+    auto load = [&](int blk, int page, int stage) {
+      if (lane == 0 && blk < b1) {
+        const uint32_t bar = full + stage * 8, dst = ring + stage * L_::kStage;
+        const int in = (blk & ((1 << block_shift) - 1)) * 16, pg = page < 0 ? S.pages : page;
+        mbar_expect_tx(bar, L_::kStage);
+        for (int pn = 0; pn < NPANEL; pn++) tma_load_4d(dst + pn * PANEL, &src.k, bar, pn * 64, in, hk, pg);
+        for (int pn = 0; pn < NPANEL; pn++) tma_load_4d(dst + (NPANEL + pn) * PANEL, &src.v, bar, pn * 64, in, hk, pg);
       }
-      const int group = c * (D / 4) / kQ4Group;
-      const uint16_t* const scales = reinterpret_cast<const uint16_t*>(k + q4_scales_at(D));
-      uint32_t sa = scales[key * (D / kQ4Group) + group], sb = scales[(key + 8) * (D / kQ4Group) + group];
-      sa |= sa << 16;
-      sb |= sb << 16;
-      const uint32_t oa = q4_offset(sa), ob = q4_offset(sb);
+    };
+    // vectors of a stage: `chunk` of 16 bytes of row `key` in a panel
+    auto vec = [&](int stage, int panel, int key, int chunk) {
+      return *reinterpret_cast<const uint4*>(&sm.ring[warp][stage][panel * PANEL + key * 128 + ((chunk ^ (key & 7)) << 4)]);
+    };
+    auto page_of = [&](int blk) { return blk < b1 ? pages[blk >> block_shift] : -1; };
+
+    int blk = b0 + rank * kStWarps + warp, ahead = blk;
+    int next = page_of(ahead);
 #pragma unroll
-      for (int j = 0; j < W; j++) {
-        uint32_t a[4], b[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++) a[i] = q4_pair(ka[j], i, sa, oa), b[i] = q4_pair(kb[j], i, sb, ob);
-#pragma unroll
-        for (int x = 0; x < NT; x++) {
-          mma_16816(s[x][0], a[0], b[0], a[1], b[1], q[x][j].x, q[x][j].y);
-          mma_16816(s[x][1], a[2], b[2], a[3], b[3], q[x][j].z, q[x][j].w);
-        }
-      }
-    } else {
-#pragma unroll
-    for (int j = 0; j < D / 32; j++) {
-      const uint4 ka = vec(stage, j >> 1, n, (j & 1) * 4 + c), kb = vec(stage, j >> 1, n + 8, (j & 1) * 4 + c);
-#pragma unroll
-      for (int x = 0; x < NT; x++) {
-        mma_16816(s[x][0], ka.x, kb.x, ka.y, kb.y, q[x][j].x, q[x][j].y);
-        mma_16816(s[x][1], ka.z, kb.z, ka.w, kb.w, q[x][j].z, q[x][j].w);
-      }
-    }
-    }
-    uint32_t pt[NT][2];
-#pragma unroll
-    for (int x = 0; x < NT; x++) {
-      float v[4];      // key n: rows 2c, 2c + 1; key n + 8: the same
-#pragma unroll
-      for (int e = 0; e < 4; e++) v[e] = s[x][0][e] + s[x][1][e];
-      if (blk * 16 + 16 > rel_min || blk * 16 + 16 > k1) {
-#pragma unroll
-        for (int e = 0; e < 4; e++)
-          if (blk * 16 + key + 8 * (e >> 1) >= min(see[x][e & 1], k1)) v[e] = -INFINITY;
-      }
-      float top[2];
-#pragma unroll
-      for (int e = 0; e < 2; e++) top[e] = fmaxf(v[e], v[2 + e]) * p.scale_log2;
-#pragma unroll
-      for (int d = 4; d < 32; d <<= 1) {
-        top[0] = fmaxf(top[0], __shfl_xor_sync(FULLM, top[0], d));
-        top[1] = fmaxf(top[1], __shfl_xor_sync(FULLM, top[1], d));
-      }
-      if (__any_sync(FULLM, top[0] > m[x][0] + 8.f || top[1] > m[x][1] + 8.f)) {
-#pragma unroll
-        for (int e = 0; e < 2; e++) {
-          const float up = fmaxf(m[x][e], top[e]);
-          const float f = m[x][e] == -INFINITY ? 0.f : fast_exp2(m[x][e] - up);
-          m[x][e] = up;
-          l[x][e] *= f;
-#pragma unroll
-          for (int y = 0; y < D / 16; y++) {
-            o[x][y][e] *= f;
-            o[x][y][2 + e] *= f;
-          }
-        }
-      }
-      float e4[4];
-#pragma unroll
-      for (int e = 0; e < 4; e++) {
-        const float ref = m[x][e & 1] == -INFINITY ? 0.f : m[x][e & 1];
-        e4[e] = fast_exp2(fmaf(v[e], p.scale_log2, -ref));
-        l[x][e & 1] += e4[e];
-      }
-      pt[x][0] = transpose_8x8(pack_bf16x2(e4[0], e4[1]));
-      pt[x][1] = transpose_8x8(pack_bf16x2(e4[2], e4[3]));
-    }
-    if constexpr (Q4) {
-      // lane (n, c): an eighth of the channels, of the keys that are rows 2c, 2c + 1, 2c + 8 and 2c + 9 of S^T
-      constexpr int W = D / 64;
-      const uint8_t* const v = &sm.ring[warp][stage][L_::kBlock];
-      const int key0 = stream_key(2 * c), key1 = stream_key(2 * c + 1), group = n * (D / 8) / kQ4Group;
-      uint32_t w0[W], w1[W], w2[W], w3[W];
-      auto codes = [&](int key, uint32_t (&w)[W]) {
-        if constexpr (W == 2) {
-          *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(v + key * (D / 2) + 8 * n);
-        } else {
-          w[0] = *reinterpret_cast<const uint32_t*>(v + key * (D / 2) + 4 * n);
-        }
-      };
-      codes(key0, w0);
-      codes(key1, w1);
-      codes(key0 + 8, w2);
-      codes(key1 + 8, w3);
-      const uint16_t* const scales = reinterpret_cast<const uint16_t*>(v + q4_scales_at(D)) + group;
-      uint32_t s0 = scales[key0 * (D / kQ4Group)], s1 = scales[key1 * (D / kQ4Group)], s2 = scales[(key0 + 8) * (D / kQ4Group)],
-               s3 = scales[(key1 + 8) * (D / kQ4Group)];
-      if (blk * 16 + 16 > k1) {
-        // behind the last token its page may hold anything; P is zero there, and 0 * NaN is not
-        const int left = k1 - blk * 16;
-        if (key0 >= left) s0 = 0u;
-        if (key1 >= left) s1 = 0u;
-        if (key0 + 8 >= left) s2 = 0u;
-        if (key1 + 8 >= left) s3 = 0u;
-      }
-      s0 |= s1 << 16;
-      s2 |= s3 << 16;
-      const uint32_t o0 = q4_offset(s0), o2 = q4_offset(s2);
-#pragma unroll
-      for (int j = 0; j < W; j++) {
-        const uint32_t e0 = __byte_perm(w0[j], w1[j], 0x5410), d0 = __byte_perm(w0[j], w1[j], 0x7632);      // even channels of both keys, odd ones
-        const uint32_t e2 = __byte_perm(w2[j], w3[j], 0x5410), d2 = __byte_perm(w2[j], w3[j], 0x7632);
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const uint32_t a0 = q4_pair(e0, i, s0, o0), a1 = q4_pair(d0, i, s0, o0), a2 = q4_pair(e2, i, s2, o2), a3 = q4_pair(d2, i, s2, o2);
-#pragma unroll
-          for (int x = 0; x < NT; x++) mma_16816(o[x][4 * j + i], a0, a1, a2, a3, pt[x][0], pt[x][1]);
-        }
-      }
-    } else {
-#pragma unroll
-    for (int j = 0; j < D / 64; j++) {
-      uint32_t v0[4], v1[4], v2[4], v3[4];
-      *reinterpret_cast<uint4*>(v0) = vec(stage, NPANEL + j, 2 * c, n);
-      *reinterpret_cast<uint4*>(v1) = vec(stage, NPANEL + j, 2 * c + 1, n);
-      *reinterpret_cast<uint4*>(v2) = vec(stage, NPANEL + j, 2 * c + 8, n);
-      *reinterpret_cast<uint4*>(v3) = vec(stage, NPANEL + j, 2 * c + 9, n);
-      if (blk * 16 + 16 > k1) {
-        // behind the last token its page may hold anything; P is zero there, and 0 * NaN is not
-        const int left = k1 - blk * 16 - 2 * c;
-#pragma unroll
-        for (int y = 0; y < 4; y++) {
-          if (left < 1) v0[y] = 0u;
-          if (left < 2) v1[y] = 0u;
-          if (left < 9) v2[y] = 0u;
-          if (left < 10) v3[y] = 0u;
-        }
-      }
-#pragma unroll
-      for (int y = 0; y < 4; y++) {
-        const uint32_t a0 = __byte_perm(v0[y], v1[y], 0x5410), a1 = __byte_perm(v0[y], v1[y], 0x7632);
-        const uint32_t a2 = __byte_perm(v2[y], v3[y], 0x5410), a3 = __byte_perm(v2[y], v3[y], 0x7632);
-#pragma unroll
-        for (int x = 0; x < NT; x++) mma_16816(o[x][4 * j + y], a0, a1, a2, a3, pt[x][0], pt[x][1]);
-      }
-    }
-    }
-    __syncwarp();      // all lanes have read the stage
-    {
+    for (int k = 0; k < STAGES; k++) {
       const int page = next;
       next = page_of(ahead + step);
-      load(ahead, page, stage);
+      load(ahead, page, k);
       ahead += step;
     }
-    if (++stage == STAGES) {
-      stage = 0;
-      round++;
+    int stage = 0, round = 0;
+    bool ok = true;
+#pragma unroll 1
+    for (; blk < b1; blk += step) {
+      if (!__all_sync(FULLM, mbar_wait(full + stage * 8, round & 1))) {
+        ok = false;
+        break;
+      }
+      float s[NT][2][4] = {};      // two chains of products each
+#pragma unroll
+      for (int j = 0; j < D / 32; j++) {
+        const uint4 ka = vec(stage, j >> 1, n, (j & 1) * 4 + c), kb = vec(stage, j >> 1, n + 8, (j & 1) * 4 + c);
+#pragma unroll
+        for (int x = 0; x < NT; x++) {
+          mma_16816(s[x][0], ka.x, kb.x, ka.y, kb.y, q[x][j].x, q[x][j].y);
+          mma_16816(s[x][1], ka.z, kb.z, ka.w, kb.w, q[x][j].z, q[x][j].w);
+        }
+      }
+      uint32_t pt[NT][2];
+#pragma unroll
+      for (int x = 0; x < NT; x++) {
+        float v[4];      // key n: rows 2c, 2c + 1; key n + 8: the same
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[e] = s[x][0][e] + s[x][1][e];
+        if (blk * 16 + 16 > rel_min || blk * 16 + 16 > k1) {
+#pragma unroll
+          for (int e = 0; e < 4; e++)
+            if (blk * 16 + n + 8 * (e >> 1) >= min(see[x][e & 1], k1)) v[e] = -INFINITY;
+        }
+        float top[2];
+#pragma unroll
+        for (int e = 0; e < 2; e++) top[e] = fmaxf(v[e], v[2 + e]) * p.scale_log2;
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) {
+          top[0] = fmaxf(top[0], __shfl_xor_sync(FULLM, top[0], d));
+          top[1] = fmaxf(top[1], __shfl_xor_sync(FULLM, top[1], d));
+        }
+        if (__any_sync(FULLM, top[0] > m[x][0] + 8.f || top[1] > m[x][1] + 8.f)) {
+#pragma unroll
+          for (int e = 0; e < 2; e++) {
+            const float up = fmaxf(m[x][e], top[e]);
+            const float f = m[x][e] == -INFINITY ? 0.f : fast_exp2(m[x][e] - up);
+            m[x][e] = up;
+            l[x][e] *= f;
+#pragma unroll
+            for (int y = 0; y < D / 16; y++) {
+              o[x][y][e] *= f;
+              o[x][y][2 + e] *= f;
+            }
+          }
+        }
+        float e4[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const float ref = m[x][e & 1] == -INFINITY ? 0.f : m[x][e & 1];
+          e4[e] = fast_exp2(fmaf(v[e], p.scale_log2, -ref));
+          l[x][e & 1] += e4[e];
+        }
+        pt[x][0] = transpose_8x8(pack_bf16x2(e4[0], e4[1]));
+        pt[x][1] = transpose_8x8(pack_bf16x2(e4[2], e4[3]));
+      }
+#pragma unroll
+      for (int j = 0; j < D / 64; j++) {
+        uint32_t v0[4], v1[4], v2[4], v3[4];
+        *reinterpret_cast<uint4*>(v0) = vec(stage, NPANEL + j, 2 * c, n);
+        *reinterpret_cast<uint4*>(v1) = vec(stage, NPANEL + j, 2 * c + 1, n);
+        *reinterpret_cast<uint4*>(v2) = vec(stage, NPANEL + j, 2 * c + 8, n);
+        *reinterpret_cast<uint4*>(v3) = vec(stage, NPANEL + j, 2 * c + 9, n);
+        if (blk * 16 + 16 > k1) {
+          // behind the last token its page may hold anything; P is zero there, and 0 * NaN is not
+          const int left = k1 - blk * 16 - 2 * c;
+#pragma unroll
+          for (int y = 0; y < 4; y++) {
+            if (left < 1) v0[y] = 0u;
+            if (left < 2) v1[y] = 0u;
+            if (left < 9) v2[y] = 0u;
+            if (left < 10) v3[y] = 0u;
+          }
+        }
+#pragma unroll
+        for (int y = 0; y < 4; y++) {
+          const uint32_t a0 = __byte_perm(v0[y], v1[y], 0x5410), a1 = __byte_perm(v0[y], v1[y], 0x7632);
+          const uint32_t a2 = __byte_perm(v2[y], v3[y], 0x5410), a3 = __byte_perm(v2[y], v3[y], 0x7632);
+#pragma unroll
+          for (int x = 0; x < NT; x++) mma_16816(o[x][4 * j + y], a0, a1, a2, a3, pt[x][0], pt[x][1]);
+        }
+      }
+      __syncwarp();      // all lanes have read the stage
+      {
+        const int page = next;
+        next = page_of(ahead + step);
+        load(ahead, page, stage);
+        ahead += step;
+      }
+      if (++stage == STAGES) {
+        stage = 0;
+        round++;
+      }
     }
-  }
-  if (!ok) {
-    // a load never came: the status says so, the rows lack this warp's keys from there on, and what is under way lands before this memory is given away
-    report_logged(p.status, p.log, AVSA_ERR_TIMEOUT, kPxKFull, item, blk);
-    for (int k = 0; k < STAGES; k++) mbar_wait(full + k * 8, (round + (k < stage ? 1 : 0)) & 1);
+    if (!ok) {
+      // a load never came: the status says so, the rows lack this warp's keys from there on, and what is under way lands before this memory is given away
+      report_logged(p.status, p.log, AVSA_ERR_TIMEOUT, kPxKFull, item, blk);
+      for (int k = 0; k < STAGES; k++) mbar_wait(full + k * 8, (round + (k < stage ? 1 : 0)) & 1);
+    }
   }
   __syncthreads();      // the ring is the warps' rows from here on
 

@@ -12,7 +12,7 @@
 
 namespace avsa {
 
-constexpr int kRopeThreads = 256;
+constexpr int kRopeThreads = 128;
 constexpr int kRopeHeads = 8;       // heads of a thread, at most
 
 struct RopeArgs {
@@ -38,7 +38,7 @@ __device__ __forceinline__ void turn_halves(uint32_t& x, uint32_t& y, const floa
 }
 
 template <int D, bool HALVES>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(kRopeThreads, 8) rope_kernel(const __grid_constant__ RopeArgs a) {
   pdl_wait();
   pdl_launch();
   constexpr int V = HALVES ? D / 16 : D / 8, P = HALVES ? 8 : 4, U = HALVES ? kRopeHeads / 2 : kRopeHeads;      // threads of a head, their pairs; loads under way
@@ -68,8 +68,8 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
       if (h + u >= h1) continue;
       const avsa_bf16_4d& t = h + u < a.H ? a.q : a.k;
       const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(t.ptr) + b * t.stride_b + (h + u - (h + u < a.H ? 0 : a.H)) * t.stride_h + n * t.stride_n + 8 * v;
-      x[u] = *reinterpret_cast<const uint4*>(from);
-      if (HALVES) y[u] = *reinterpret_cast<const uint4*>(from + D / 2);
+      x[u] = __ldcs(reinterpret_cast<const uint4*>(from));
+      if (HALVES) y[u] = __ldcs(reinterpret_cast<const uint4*>(from + D / 2));
     }
 #pragma unroll
     for (int u = 0; u < U; u++) {
@@ -81,14 +81,14 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
         turn_halves(x[u].y, y[u].y, c + 2, s + 2);
         turn_halves(x[u].z, y[u].z, c + 4, s + 4);
         turn_halves(x[u].w, y[u].w, c + 6, s + 6);
-        *reinterpret_cast<uint4*>(to + D / 2) = y[u];
+        __stcs(reinterpret_cast<uint4*>(to + D / 2), y[u]);
       } else {
         turn(x[u].x, c[0], s[0]);
         turn(x[u].y, c[1], s[1]);
         turn(x[u].z, c[2], s[2]);
         turn(x[u].w, c[3], s[3]);
       }
-      *reinterpret_cast<uint4*>(to) = x[u];
+      __stcs(reinterpret_cast<uint4*>(to), x[u]);
     }
   }
 }
