@@ -60,10 +60,10 @@ __device__ __forceinline__ uint4 quantise(const uint32_t (&x)[16], uint32_t& sca
 }
 
 // The other way: pairs of neighbours.
-__device__ __forceinline__ void widen(uint4 codes, uint32_t scale, uint32_t (&x)[16]) {
+__device__ __forceinline__ void widen(uint4 codes, uint32_t scale, uint32_t sixteen, uint32_t (&x)[16]) {
   const uint32_t s2 = scale | scale << 16, c2 = q4_offset(s2), w[4] = {codes.x, codes.y, codes.z, codes.w};
 #pragma unroll
-  for (int i = 0; i < 16; i++) x[i] = q4_pair(w[i >> 2], i & 3, s2, c2);
+  for (int i = 0; i < 16; i++) x[i] = q4_pair(w[i >> 2], i & 3, s2, c2, sixteen);
 }
 
 // Where token `in` of a page has the codes and the scale of a group.
@@ -120,8 +120,8 @@ __global__ void __launch_bounds__(kQ4Threads, 8) tokens_q4_kernel(const __grid_c
         ks = *k_scale;
         vs = *v_scale;
       }
-      widen(kc, ks, x);
-      widen(vc, vs, y);
+      widen(kc, ks, a.k_pool.sixteen, x);
+      widen(vc, vs, a.k_pool.sixteen, y);
       if (!there) {      // (-8 times a scale of zero is -0)
 #pragma unroll
         for (int j = 0; j < 16; j++) x[j] = y[j] = 0u;
@@ -177,9 +177,9 @@ __global__ void __launch_bounds__(kQ4Threads) widen_pages_kernel(const __grid_co
     const uint32_t ks = *k_scale, vs = *v_scale;
     const int64_t to = ((static_cast<int64_t>(page) * S.Hkv + h) * S.page + in) * D + group * kQ4Group;
     uint32_t x[16];
-    widen(kc, ks, x);
+    widen(kc, ks, k4.sixteen, x);
     store_group<true>(k + to, x);
-    widen(vc, vs, x);
+    widen(vc, vs, k4.sixteen, x);
     store_group<true>(v + to, x);
   }
 }

@@ -403,6 +403,31 @@ void make_view(const Call& c, View& r) {
   r.ptr = r.t.data_ptr();
 }
 
+// Two outputs without gaps that the caller did not bring: one allocation, the second one's begin at a multiple of 512 bytes.  (An allocation is 0.8 us of a call's 6.)
+void make_views(const Call& c, View& a, View& b) {
+  if (a.there() || b.there()) {
+    make_view(c, a);
+    make_view(c, b);
+    return;
+  }
+  auto elements = [](const View& v) {
+    int64_t n = 1;
+    for (int64_t x : v.size) n *= x;
+    return (n + 255) / 256 * 256;
+  };
+  const int64_t first = elements(a);
+  const at::Tensor both = at::empty({first + elements(b)}, at::TensorOptions().dtype(at::kBFloat16).device(c.device));
+  auto part = [&](View& v, int64_t at) {
+    auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(both.storage()), both.key_set(), both.dtype());
+    impl->set_storage_offset(at);
+    impl->set_sizes_and_strides(v.size, v.stride);
+    v.t = at::Tensor(std::move(impl));
+    v.ptr = static_cast<char*>(both.data_ptr()) + 2 * at;
+  };
+  part(a, 0);
+  part(b, first);
+}
+
 // read_q4(k_pool, v_pool, table, length, tokens, seq, count, k, v) -> (status, k, v)
 PyObject* py_read_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -423,8 +448,7 @@ PyObject* py_read_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
   c.find_stream();
   int st;
   without_lock([&] {
-    make_view(c, k);
-    make_view(c, v);
+    make_views(c, k, v);
     st = f_read_q4(entries, kp.Hkv, tokens, kp.d, kp.page, kp.pages, seqs, width, kp, vp, table.as<int32_t>(), length.as<int32_t>(), seq.as<int32_t>(),
                    count.as<int32_t>(), k, v, c.stream);
   });
@@ -486,8 +510,10 @@ PyObject* py_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   c.find_stream();
   int st;
   without_lock([&] {
-    make_view(c, q_out);
-    if (k.there()) make_view(c, k_out);
+    if (k.there())
+      make_views(c, q_out, k_out);
+    else
+      make_view(c, q_out);
     st = f_rope(B, H, Hk, N, d, q, k, q_out, k_out, pos.as<int32_t>(), pos_stride, static_cast<int>(axes), sections, freq.as<double>(), flags, c.stream);
   });
   return result(st, {c.give(7, q_out), c.give(8, k_out)});

@@ -114,12 +114,17 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     const long long fit = slots * 9ll / 10 / (y.own.items + 1ll), by_keys = keys / 64;
     long long ctas = fit < by_keys ? fit : by_keys;
     ctas = ctas < 1 ? 1 : ctas > 8 ? 8 : ctas;
-    while (ctas < 8 && y.own.items < (1 << 27) && keys > 1024 * ctas) ctas = 2 * ctas < 8 ? 2 * ctas : 8;
+    // (codes, whose CTAs are longer at their start and end than at 128 keys: no second CTA for items that fill three quarters of the slots by themselves; 64 x 8 items of 2048
+    // keys of 128 channels 47 and 44, of 64 34 and 28, of 100 to 2048 keys 37 both ways)
+    const long long most_keys = codes > 0 && 4ll * y.own.items >= 3ll * slots ? 2048 : 1024;
+    while (ctas < 8 && y.own.items < (1 << 27) && keys > most_keys * ctas) ctas = 2 * ctas < 8 ? 2 * ctas : 8;
     y.own_cluster = static_cast<int>(ctas);
     y.own.splits = 1;
-    if (static_cast<long long>(y.own.items) * 8 < sms && keys >= 4096) {
+    // (codes: where eight CTAs an item leave half of the slots empty, and at least 256 keys a part; 24 items of 40000 keys, us, as clusters 59, in 24 parts 40)
+    if (static_cast<long long>(y.own.items) * 8 < (codes > 0 ? slots / 2 : sms) && keys >= (codes > 0 ? 8192 : 4096)) {
       y.own_cluster = 1;
       y.own.splits = (slots - 1) / y.own.items;      // (one slot for the check of the tables)
+      if (codes > 0 && keys / 256 < y.own.splits) y.own.splits = static_cast<int>(keys / 256);
       rows += static_cast<size_t>(y.own.items) * y.own.splits * kStRows;
     }
     y.own.check = 1;
@@ -167,13 +172,23 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   return true;
 }
 
+constexpr size_t kSmOnly = 116 * 1024;      // two CTAs with so much shared memory do not fit an SM (228 KB)
+
 template <int D, int NT, class Source>
 static int launch_stream_of(const Source& src, const PrefixParams& p, const StreamParams& t, int cluster, cudaStream_t st) {
   auto kernel = prefix_stream_kernel<D, NT, Source>;
   constexpr size_t kSmem = sizeof(StreamSmem<D, NT, Source::kQ4>);
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return AVSA_ERR_CUDA;
+  // Codes: no more CTAs to an SM than the call needs, by asking for more shared memory than there is for another one; else some SMs get four of 385 CTAs and others two (16 x 24
+  // items of 1 to 1000 keys, us: 18.6, 17.1).  The limit belongs to the kernel, so every call sets the same.
+  constexpr size_t kMost = Source::kQ4 ? kSmOnly : kSmem;
   const unsigned grid = static_cast<unsigned>((static_cast<long long>(t.items) * t.splits + t.check) * cluster);
-  return launch_pdl_clusters(kernel, cluster, grid, kStThreads, kSmem, st, src, p, t) == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
+  size_t smem = kSmem;
+  if (Source::kQ4) {
+    const unsigned sms = static_cast<unsigned>(persistent_grid(1 << 30)), ctas = (grid + sms - 1) / sms;
+    if (ctas < static_cast<unsigned>(stream_ctas(NT, true)) && kSmOnly * 2 / (ctas + 1) > smem) smem = kSmOnly * 2 / (ctas + 1);
+  }
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost) != cudaSuccess) return AVSA_ERR_CUDA;
+  return launch_pdl_clusters(kernel, cluster, grid, kStThreads, smem, st, src, p, t) == cudaSuccess ? AVSA_OK : AVSA_ERR_CUDA;
 }
 template <int D, class Source>
 static int launch_stream(const Source& src, const PrefixParams& p, const StreamParams& t, int cluster, cudaStream_t st) {

@@ -236,11 +236,11 @@ struct PrefixCodes {      // 4 bits: blocks of 16 keys
 // well.  A loop and not its turns in a row: those are 5 KB, and what the softmax groups run through fills the instruction cache (tiles took twice as long).
 template <int D>
 struct WidenRow {
-  uint32_t codes, scales, row, first;
-  __device__ __forceinline__ explicit WidenRow(int r)
+  uint32_t codes, scales, row, first, sixteen;
+  __device__ __forceinline__ WidenRow(int r, uint32_t sixteen)
       : codes((r / kQ4Tokens) * q4_block_bytes(D) + (r % kQ4Tokens) * (D / 2)),
         scales((r / kQ4Tokens) * q4_block_bytes(D) + q4_scales_at(D) + (r % kQ4Tokens) * (D / 16)), row(r * 128 + ((r & 7) << 4)),
-        first(D == 128 ? (r >> 1) & 3 : 0) {}
+        first(D == 128 ? (r >> 1) & 3 : 0), sixteen(sixteen) {}
   __device__ __forceinline__ void operator()(uint32_t raw, uint32_t tile, bool there) const {
 #pragma unroll 1
     for (int turn = 0; turn < D / kQ4Group; turn++) {
@@ -252,8 +252,8 @@ struct WidenRow {
       const uint32_t c2 = q4_offset(s2), to = ((tile + row) ^ ((g & 1) << 6)) + (g >> 1) * (128 * 128);
 #pragma unroll
       for (int i = 0; i < 4; i++)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to ^ (i << 4)), "r"(q4_pair(w[i], 0, s2, c2)), "r"(q4_pair(w[i], 1, s2, c2)),
-                     "r"(q4_pair(w[i], 2, s2, c2)), "r"(q4_pair(w[i], 3, s2, c2))
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to ^ (i << 4)), "r"(q4_pair(w[i], 0, s2, c2, sixteen)), "r"(q4_pair(w[i], 1, s2, c2, sixteen)),
+                     "r"(q4_pair(w[i], 2, s2, c2, sixteen)), "r"(q4_pair(w[i], 3, s2, c2, sixteen))
                      : "memory");
     }
   }
@@ -606,7 +606,7 @@ prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ C
       const bool is_k = warp < 16;
       const int FULL = is_k ? K_FULL : V_FULL, EMPTY = is_k ? K_EMPTY : V_EMPTY, STAGES = is_k ? KS : n_vs, r = q_warp * 32 + lane;
       const int where_full = is_k ? kPxKFull : kPxVFull, where_empty = is_k ? kPxKEmpty : kPxVEmpty;
-      const WidenRow<D> widen(r);
+      const WidenRow<D> widen(r, src.k.sixteen);
       const uint32_t raws = smem_u32(smem + L_::kRaws), tiles = smem_u32(smem + (is_k ? L_::kK : L_::kV));
       const int* const there = reinterpret_cast<const int*>(smem + L_::kThere);
       int raw = 0, raw_round = 0, stage = 0, round = 0;

@@ -147,13 +147,14 @@ __device__ __forceinline__ void prefix_check_begin(const PrefixParams& p) {
 }
 
 // CTAs that an SM holds, by shared memory: with one product's columns three of two stages (of 8 KB; 64 sequences of 100 to 2048 keys, us: 55.4, two of three stages 58.7),
-// with two products' the warps take longer and want more ahead (32 sequences x 8 x 2048 keys, 16 rows: 71.5 and 58.0).
-constexpr int stream_ctas(int NT, bool q4) { return q4 ? (NT == 1 ? 4 : 3) : NT == 1 ? 3 : 2; }
+// with two products' the warps take longer and want more ahead (32 sequences x 8 x 2048 keys, 16 rows: 71.5 and 58.0).  Codes: by registers, 126 and 206 a thread (32 x 8 items of
+// 2048 keys, 16 rows, us, with two, three and four CTAs of them: 33, 46, 39); two stages (of 4.6 KB) are as good as three.
+constexpr int stream_ctas(int NT, bool q4) { return q4 ? (NT == 1 ? 4 : 2) : NT == 1 ? 3 : 2; }
 
 template <int D, int NT, bool Q4>
 struct StreamSmem {
   static constexpr int kPanel = 16 * 128, kBlock = q4_block_bytes(D);
-  static constexpr int kStages = Q4 ? 3 * (128 / D) : (NT == 1 ? 2 : 3) * (128 / D);
+  static constexpr int kStages = Q4 ? (NT == 1 ? 2 : 3) * (128 / D) : (NT == 1 ? 2 : 3) * (128 / D);
   static constexpr int kStage = Q4 ? 4 * kBlock : 2 * (D / 64) * kPanel;      // a stage: panels of K, panels of V, or two blocks of each
   union {
     uint8_t ring[kStWarps][kStages][kStage];      // 128-byte swizzled
@@ -181,6 +182,7 @@ __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const Prefi
   const PrefixShape& S = p.s;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, c = lane & 3, block_shift = S.page_shift - 4;
   const uint32_t ring = smem_u32(&sm.ring[warp][0][0]), full = smem_u32(&sm.full[warp][0]);
+  const uint32_t sixteen = src.k.sixteen;
   const bool single = block_shift == 0;      // a page is one block: pairs are two pages
   const uint8_t* const k_head = src.k.ptr + hk * src.k.stride_head;
   const uint8_t* const v_head = src.v.ptr + hk * src.v.stride_head;
@@ -270,7 +272,7 @@ __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const Prefi
       for (int j = 0; j < W; j++) {
         uint32_t a[4], b[4];
 #pragma unroll
-        for (int i = 0; i < 4; i++) a[i] = q4_pair(ka[j], i, sa, oa), b[i] = q4_pair(kb[j], i, sb, ob);
+        for (int i = 0; i < 4; i++) a[i] = q4_pair(ka[j], i, sa, oa, sixteen), b[i] = q4_pair(kb[j], i, sb, ob, sixteen);
 #pragma unroll
         for (int x = 0; x < NT; x++) {
           mma_16816(s[h][x], a[0], b[0], a[1], b[1], q[x][j].x, q[x][j].y);
@@ -369,7 +371,7 @@ __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const Prefi
         const uint32_t e2 = __byte_perm(w2[j], w3[j], 0x5410), d2 = __byte_perm(w2[j], w3[j], 0x7632);
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-          const uint32_t a0 = q4_pair(e0, i, s0, o0), a1 = q4_pair(d0, i, s0, o0), a2 = q4_pair(e2, i, s2, o2), a3 = q4_pair(d2, i, s2, o2);
+          const uint32_t a0 = q4_pair(e0, i, s0, o0, sixteen), a1 = q4_pair(d0, i, s0, o0, sixteen), a2 = q4_pair(e2, i, s2, o2, sixteen), a3 = q4_pair(d2, i, s2, o2, sixteen);
 #pragma unroll
           for (int x = 0; x < NT; x++) mma_16816(o[x][4 * j + i], a0, a1, a2, a3, pt[h][x][0], pt[h][x][1]);
         }

@@ -35,18 +35,23 @@ __device__ __forceinline__ uint32_t hmul2_bf16(uint32_t a, uint32_t b) {
 }
 // -24 times a pair of scales.
 __device__ __forceinline__ uint32_t q4_offset(uint32_t s2) { return hmul2_bf16(s2, 0xc1c0c1c0u); }
-// Pair i of a word: s2 the scales of its two values, c2 = q4_offset(s2).
-__device__ __forceinline__ uint32_t q4_pair(uint32_t word, int i, uint32_t s2, uint32_t c2) {
+// Pair i of a word: s2 the scales of its two values, c2 = q4_offset(s2).  `sixteen` is kQ4Sixteen, from a register that the compiler cannot see through: an instruction
+// takes one constant, and mask and exponent are two (the stream kernel had 64 instructions more a block).
+constexpr uint32_t kQ4Sixteen = 0x41804180u;
+__device__ __forceinline__ uint32_t q4_pair(uint32_t word, int i, uint32_t s2, uint32_t c2, uint32_t sixteen) {
   const uint32_t at = i == 0 ? word << 3 : word >> (4 * i - 3);
-  return hfma2_bf16((at & 0x00780078u) | 0x41804180u, s2, c2);
+  uint32_t x;
+  asm("lop3.b32 %0, %1, 0x00780078, %2, 0xea;" : "=r"(x) : "r"(at), "r"(sixteen));
+  return hfma2_bf16(x, s2, c2);
 }
 
 // A pool as the kernels see it.
 struct Q4Pool {
   uint8_t* ptr;
   int64_t stride_page, stride_head;      // bytes
+  uint32_t sixteen;
 };
-inline Q4Pool q4_pool(const avsa_q4_pool& p) { return Q4Pool{static_cast<uint8_t*>(p.ptr), p.stride_page, p.stride_head}; }
+inline Q4Pool q4_pool(const avsa_q4_pool& p) { return Q4Pool{static_cast<uint8_t*>(p.ptr), p.stride_page, p.stride_head, kQ4Sixteen}; }
 
 inline bool q4_pool_ok(const avsa_q4_pool& p, int pages, int Hkv, int page, int d) {
   const int64_t head = static_cast<int64_t>(page) * q4_token_bytes(d);

@@ -322,6 +322,8 @@ def test_attention_stacked(B, L, H, Hkv, page, tokens, most, d, causal):
 @pytest.mark.parametrize("B,L,H,Hkv,width,lengths", [
     (1, 1, 8, 8, 400, (6000,)),           # few items, long rows: parts that another kernel joins
     (1, 31, 4, 4, 300, (4700,)),
+    (1, 1, 24, 24, 1100, (17000,)),       # parts of 24 items
+    (1, 4, 32, 8, 700, (11001,)),
     (3, 1, 24, 24, 60, (900, 0, 17)),     # a cluster of CTAs an item
     (20, 2, 16, 16, 80, tuple(range(5, 1285, 64))),
     (70, 1, 32, 8, 300, tuple(range(1, 4700, 67))[:70]),

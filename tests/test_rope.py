@@ -122,7 +122,7 @@ def test_in_place_slices_and_shared_positions(halves):
     q, k = (qkv[:, :, i].transpose(1, 2) for i in range(2))
     pos, freq = positions(1, N, 2, 500)[0].cuda(), av.avsa_rope_frequencies((16, 16))
     fresh = av.avsa_rope(q, k, pos, freq, (16, 16), halves=halves)
-    assert fresh[0].is_contiguous() == q.is_contiguous() and fresh[0].untyped_storage().nbytes() == q.numel() * 2      # no gaps
+    assert fresh[0].stride() == fresh[1].stride() == (N * H * d, d, H * d, 1)          # in the order of q's dimensions, without the gaps
     own = av.avsa_rope(q, k, pos.repeat(B, 1, 1), freq, (16, 16), halves=halves)
     got = av.avsa_rope(q, k, pos, freq, (16, 16), halves=halves, q_out=q, k_out=k)
     assert got[0] is q and got[1] is k
