@@ -181,6 +181,7 @@ static int launch_stream_of(const Source& src, const PrefixParams& p, const Stre
   // Codes: no more CTAs to an SM than the call needs, by asking for more shared memory than there is for another one; else some SMs get four of 385 CTAs and others two (16 x 24
   // items of 1 to 1000 keys, us: 18.6, 17.1).  The limit belongs to the kernel, so every call sets the same.
   constexpr size_t kMost = Source::kQ4 ? kSmOnly : kSmem;
+  static_assert(kSmem <= kMost, "shared memory of a CTA");
   const unsigned grid = static_cast<unsigned>((static_cast<long long>(t.items) * t.splits + t.check) * cluster);
   size_t smem = kSmem;
   if (Source::kQ4) {

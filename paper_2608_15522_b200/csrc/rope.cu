@@ -14,16 +14,17 @@ namespace avsa {
 
 constexpr int kRopeThreads = 128;
 constexpr int kRopeHeads = 8;       // heads of a thread, at most
+constexpr int kRopePlaces = 8;      // CTAs of an SM
 
 struct RopeArgs {
   avsa_bf16_4d q, k, q_out, k_out;
   const int32_t* pos;
   int64_t pos_stride;      // of batch entries
   const double* freq;
-  int H, heads, N, axes;   // heads: of q and k
+  int H, Hk, N, axes;
   int end[AVSA_ROPE_AXES];      // first pair behind each axis
-  int per, slices;         // heads of a thread, threads that share a token's heads
-  long long items;         // (batch entry, token, slice)
+  int per, q_slices, slices;    // heads of a thread, of q or of k; threads that share a token's heads of q, of both
+  long long items;              // (batch entry, token, slice)
   float sign;
 };
 
@@ -38,7 +39,7 @@ __device__ __forceinline__ void turn_halves(uint32_t& x, uint32_t& y, const floa
 }
 
 template <int D, bool HALVES>
-__global__ void __launch_bounds__(kRopeThreads, 8) rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(kRopeThreads, kRopePlaces) rope_kernel(const __grid_constant__ RopeArgs a) {
   pdl_wait();
   pdl_launch();
   constexpr int V = HALVES ? D / 16 : D / 8, P = HALVES ? 8 : 4, U = HALVES ? kRopeHeads / 2 : kRopeHeads;      // threads of a head, their pairs; loads under way
@@ -60,35 +61,40 @@ __global__ void __launch_bounds__(kRopeThreads, 8) rope_kernel(const __grid_cons
     sincospif(2.f * static_cast<float>(turns), &s[i], &c[i]);
     s[i] *= a.sign;
   }
-  const int h0 = slice * a.per, h1 = min(a.heads, h0 + a.per);
+  const bool of_q = slice < a.q_slices;
+  const avsa_bf16_4d &in = of_q ? a.q : a.k, &out = of_q ? a.q_out : a.k_out;
+  const int h0 = (of_q ? slice : slice - a.q_slices) * a.per, h1 = min(of_q ? a.H : a.Hk, h0 + a.per);
+  const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(in.ptr) + b * in.stride_b + h0 * in.stride_h + n * in.stride_n + 8 * v;
+  __nv_bfloat16* to = static_cast<__nv_bfloat16*>(const_cast<void*>(out.ptr)) + b * out.stride_b + h0 * out.stride_h + n * out.stride_n + 8 * v;
+  const int64_t in_step = in.stride_h, out_step = out.stride_h;
   for (int h = h0; h < h1; h += U) {
     uint4 x[U], y[U];
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      if (h + u >= h1) continue;
-      const avsa_bf16_4d& t = h + u < a.H ? a.q : a.k;
-      const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(t.ptr) + b * t.stride_b + (h + u - (h + u < a.H ? 0 : a.H)) * t.stride_h + n * t.stride_n + 8 * v;
-      x[u] = __ldcs(reinterpret_cast<const uint4*>(from));
-      if (HALVES) y[u] = __ldcs(reinterpret_cast<const uint4*>(from + D / 2));
+      if (h + u < h1) {
+        x[u] = __ldcs(reinterpret_cast<const uint4*>(from));
+        if (HALVES) y[u] = __ldcs(reinterpret_cast<const uint4*>(from + D / 2));
+      }
+      from += in_step;
     }
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      if (h + u >= h1) continue;
-      const avsa_bf16_4d& t = h + u < a.H ? a.q_out : a.k_out;
-      __nv_bfloat16* to = static_cast<__nv_bfloat16*>(const_cast<void*>(t.ptr)) + b * t.stride_b + (h + u - (h + u < a.H ? 0 : a.H)) * t.stride_h + n * t.stride_n + 8 * v;
-      if constexpr (HALVES) {
-        turn_halves(x[u].x, y[u].x, c, s);
-        turn_halves(x[u].y, y[u].y, c + 2, s + 2);
-        turn_halves(x[u].z, y[u].z, c + 4, s + 4);
-        turn_halves(x[u].w, y[u].w, c + 6, s + 6);
-        __stcs(reinterpret_cast<uint4*>(to + D / 2), y[u]);
-      } else {
-        turn(x[u].x, c[0], s[0]);
-        turn(x[u].y, c[1], s[1]);
-        turn(x[u].z, c[2], s[2]);
-        turn(x[u].w, c[3], s[3]);
+      if (h + u < h1) {
+        if constexpr (HALVES) {
+          turn_halves(x[u].x, y[u].x, c, s);
+          turn_halves(x[u].y, y[u].y, c + 2, s + 2);
+          turn_halves(x[u].z, y[u].z, c + 4, s + 4);
+          turn_halves(x[u].w, y[u].w, c + 6, s + 6);
+          __stcs(reinterpret_cast<uint4*>(to + D / 2), y[u]);
+        } else {
+          turn(x[u].x, c[0], s[0]);
+          turn(x[u].y, c[1], s[1]);
+          turn(x[u].z, c[2], s[2]);
+          turn(x[u].w, c[3], s[3]);
+        }
+        __stcs(reinterpret_cast<uint4*>(to), x[u]);
       }
-      __stcs(reinterpret_cast<uint4*>(to), x[u]);
+      to += out_step;
     }
   }
 }
@@ -136,7 +142,7 @@ extern "C" int avsa_rope(int B, int H, int Hk, int N, int d, avsa_bf16_4d q, avs
   a.pos_stride = pos_stride_b;
   a.freq = freq;
   a.H = H;
-  a.heads = H + Hk;
+  a.Hk = Hk;
   a.N = N;
   a.axes = axes;
   a.sign = flags & AVSA_ROPE_INVERSE ? -1.f : 1.f;
@@ -145,9 +151,11 @@ extern "C" int avsa_rope(int B, int H, int Hk, int N, int d, avsa_bf16_4d q, avs
   // Few tokens: fewer heads to a thread, until every SM has a CTA.
   const long long tokens = static_cast<long long>(B) * N;
   const int sms = persistent_grid(1 << 30);
+  auto slices = [&](int heads) { return (heads + a.per - 1) / a.per; };
   a.per = kRopeHeads;
-  while (a.per > 1 && tokens * ((a.heads + a.per - 1) / a.per) < static_cast<long long>(sms) * per_cta) a.per /= 2;
-  a.slices = (a.heads + a.per - 1) / a.per;
+  while (a.per > 1 && tokens * (slices(H) + slices(Hk)) < static_cast<long long>(sms) * per_cta) a.per /= 2;
+  a.q_slices = slices(H);
+  a.slices = a.q_slices + slices(Hk);
   a.items = tokens * a.slices;
   const long long ctas = (a.items + per_cta - 1) / per_cta;
   if (ctas > 0x7fffffffll) return AVSA_ERR_UNSUPPORTED;
