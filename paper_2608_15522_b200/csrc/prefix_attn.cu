@@ -15,6 +15,11 @@ constexpr int kChunk = 8;        // row tiles that go through the beginning side
 
 constexpr int kStreamRows = 32;      // query rows of a batch entry and key head that the stream kernel takes, at most; of the stacked rows as well
 
+// The same for so many keys (of all heads and sequences).  Codes: the stream kernel widens each of them again for every 16 rows, the tile kernel once for 128, but starts later:
+// 17 to 32 rows against 16 x 8 x 6000 keys of 128 channels, us, by either 78 to 83 and 60 to 62, 64 x 8 x 700 45 to 50 and 47 to 48, 8 x 8 x 2000 20 and 25.
+constexpr long long kManyCodes = 512 * 1024;
+static int stream_rows(bool codes, long long keys) { return codes && keys > kManyCodes ? kStRows : kStreamRows; }
+
 constexpr int kWidenTiles = 6;       // row tiles that read a tile of codes, beyond which it is made bf16 once for all of them
 
 // Products of 8 columns for so many query rows: with 8 or less the second one's would be empty.
@@ -56,8 +61,8 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   // tile's time for about six rows (149760 rows: 108 us, a tile of every SM 0.8), and the call has a kernel more (about eight tiles' time of every SM).
   s.stack = TP * PT + RS / 6 < F * PT && (F * PT - TP * PT - RS / 6) * Hkv > 8 * sms;
   if (s.stack) s.k0 = prefix_pages * page;
-  y.own_stream = R <= kStreamRows;
-  y.pre_stream = s.stack && RS <= kStreamRows;
+  y.own_stream = R <= stream_rows(codes > 0, (static_cast<long long>(width) * page - s.k0) * B * Hkv);
+  y.pre_stream = s.stack && RS <= stream_rows(codes > 0, static_cast<long long>(s.k0) * Hkv);
   y.tile = !y.own_stream || (s.stack && !y.pre_stream);
   s.own_off = y.own_stream;
   const long long units = (y.own_stream ? 0 : F * Hkv * most) + (s.stack ? TP * Hkv * PT : 0);

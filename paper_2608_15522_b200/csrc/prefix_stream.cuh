@@ -45,6 +45,12 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// The first of a chain: no accumulator.
+__device__ __forceinline__ void mma_16816_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 // Transposes 8 x 8 16-bit elements: the lane's two of row lane/4 become its two of column lane/4.
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   uint32_t y;
@@ -237,6 +243,7 @@ __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const Prefi
   for (int k = 0; k < STAGES; k++) load_next(k);
   const int key = stream_key(n), key0 = stream_key(2 * c), key1 = stream_key(2 * c + 1);      // as an operand's rows; as its columns
   const float inv_scale = 1.0f / p.scale_log2;
+  const uint64_t scale2 = pack_f32x2(p.scale_log2, p.scale_log2);
   float limit[NT][2], ref[NT][2];      // logits above it outgrow the reference; the reference, 0 where there is none
 #pragma unroll
   for (int x = 0; x < NT; x++) limit[x][0] = limit[x][1] = -INFINITY, ref[x][0] = ref[x][1] = 0.f;
@@ -250,7 +257,7 @@ __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const Prefi
     }
     const uint8_t* const tile = &sm.ring[warp][stage][0];
     // ---- S^T: lane (n, c) has a quarter of the channels of keys `key` and `key` + 8, in whole words
-    float s[2][NT][4] = {};
+    float s[2][NT][4];
 #pragma unroll
     for (int h = 0; h < 2; h++) {
       constexpr int W = D / 32;
@@ -275,7 +282,10 @@ __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const Prefi
         for (int i = 0; i < 4; i++) a[i] = q4_pair(ka[j], i, sa, oa, sixteen), b[i] = q4_pair(kb[j], i, sb, ob, sixteen);
 #pragma unroll
         for (int x = 0; x < NT; x++) {
-          mma_16816(s[h][x], a[0], b[0], a[1], b[1], q[x][j].x, q[x][j].y);
+          if (j == 0)
+            mma_16816_first(s[h][x], a[0], b[0], a[1], b[1], q[x][j].x, q[x][j].y);
+          else
+            mma_16816(s[h][x], a[0], b[0], a[1], b[1], q[x][j].x, q[x][j].y);
           mma_16816(s[h][x], a[2], b[2], a[3], b[3], q[x][j].z, q[x][j].w);
         }
       }
@@ -327,11 +337,16 @@ __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const Prefi
 #pragma unroll
       for (int x = 0; x < NT; x++) {
         float w[4];
+        const uint64_t no_ref = pack_f32x2(-ref[x][0], -ref[x][1]);
+        uint64_t sum = pack_f32x2(l[x][0], l[x][1]);
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-          w[e] = fast_exp2(fmaf(s[h][x][e], p.scale_log2, -ref[x][e & 1]));
-          l[x][e & 1] += w[e];
+        for (int e = 0; e < 4; e += 2) {
+          unpack_f32x2(fma_f32x2(pack_f32x2(s[h][x][e], s[h][x][e + 1]), scale2, no_ref), w[e], w[e + 1]);
+          w[e] = fast_exp2(w[e]);
+          w[e + 1] = fast_exp2(w[e + 1]);
+          sum = add_f32x2(sum, pack_f32x2(w[e], w[e + 1]));
         }
+        unpack_f32x2(sum, l[x][0], l[x][1]);
         pt[h][x][0] = transpose_8x8(pack_bf16x2(w[0], w[1]));
         pt[h][x][1] = transpose_8x8(pack_bf16x2(w[2], w[3]));
       }

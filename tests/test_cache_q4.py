@@ -306,7 +306,8 @@ def test_attention_heads_and_queries(H, Hkv, L, d, causal):
     (12, 20, 8, 2, 32, 16384, 400),       # 80 rows: the tile kernel for both, pages made bf16 before it
     (4, 40, 8, 4, 64, 16384, 300),        # 80 rows, 320 stacked: tiles made in the kernel
     (4, 40, 8, 4, 16, 16384, 300),
-    (5, 24, 16, 8, 128, 16384, 200)])
+    (5, 24, 16, 8, 128, 16384, 200),
+    (24, 1, 32, 32, 64, 20480, 100)])      # 24 rows, so many keys that the tile kernel takes them
 def test_attention_stacked(B, L, H, Hkv, page, tokens, most, d, causal):
     """The beginning is read for the rows of all sequences at once; the same call without saying that it is shared gives the same."""
     rng = random.Random(B + d)
@@ -329,6 +330,7 @@ def test_attention_stacked(B, L, H, Hkv, page, tokens, most, d, causal):
     (70, 1, 32, 8, 300, tuple(range(1, 4700, 67))[:70]),
     (1, 700, 8, 8, 200, (3000,)),         # six row tiles: tiles made in the kernel
     (3, 200, 24, 8, 100, (1000, 0, 640)),
+    (9, 20, 8, 8, 470, (7500,) + (300,) * 8),      # 20 rows of a table with room for so many keys
     (2, 900, 4, 4, 200, (3000, 1111)),    # more: pages made bf16 before it
     (3, 333, 24, 8, 80, (1000, 1, 640))])
 def test_attention_ways_of_cutting(B, L, H, Hkv, width, lengths, d):
