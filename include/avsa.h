@@ -10,7 +10,8 @@
  *   avsa_sparse_self_attn    video self-attention under that mask (Eq. 10 / Eq. 11)
  *
  * A generation that continues a clip keeps keys and values in a paged cache (avsa_cache_*), which the candidates of a
- * continuation share as far as they begin alike, and attends to it with avsa_prefix_attn.
+ * continuation share as far as they begin alike, and attends to it with avsa_prefix_attn.  The cache may be held in 4 bits
+ * (avsa_cache_write_q4, avsa_cache_read_q4, avsa_prefix_attn_q4).  avsa_rope turns queries and keys by their places.
  *
  * Conventions for every call
  *   - All data pointers are DEVICE pointers unless a parameter says "host".  The caller owns every
@@ -46,7 +47,7 @@
  *     avsa_status codes.
  *   - Supported shapes: (blk, d) in {(128,128), (64,64)}; B and H up to 65535, B*H below 2^31 (mask: up to
  *     65535); any N >= 1 (the last block may be partial: pooled means divide by the valid count, invalid
- *     keys are masked, rows >= N are not written).  Those of the paged cache stand at its calls, (6) and (7).
+ *     keys are masked, rows >= N are not written).  Those of the paged cache and of rope stand at their calls, (6) to (9).
  */
 #ifndef AVSA_H_
 #define AVSA_H_

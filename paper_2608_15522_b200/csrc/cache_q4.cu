@@ -1,13 +1,14 @@
 // A paged cache held in 4 bits: new tokens into the pages, tokens out of them again, and the pages of an attention call as bf16.
 //
-// All three are bound by HBM (2.56 bytes a value, 2 outside and 4.5 bits inside).  A thread has the 32 channels of a scale, so a group's maximum needs no other thread, and
+// All three are bound by HBM (2.56 bytes a value, 2 outside and 4.5 bits inside; 49152 tokens of 8 heads of 128 channels read, 258 MB, 41.7 us, 6.2 TB/s; 6018 tokens of 24 heads
+// written, 95 MB, 18.4 us, of which three are the length, the page and the launch before the first token is asked for).  A thread has the 32 channels of a scale, so a group's maximum needs no other thread, and
 // its codes are one 16-byte access.  Neighbouring threads have a token's groups, then the tokens of a head: the codes of a warp's eight tokens (128 channels) are
 // 512 contiguous bytes.
 #include "prefix_stream.cuh"
 
 namespace avsa {
 
-constexpr int kQ4Threads = 128;
+constexpr int kQ4Threads = 128;      // eight CTAs of 64 registers (us, the write and the read above: 19.0 and 41.8; CTAs of 256 threads 21.6 and 46.1, four of them forced 19.7 and 42.3)
 
 // 64 bytes of a thread's own, in vectors of 32 bytes where they are aligned to these.
 template <bool WIDE>

@@ -24,6 +24,10 @@
 // Bound by the exponentials (1024 cycles of a tile) and the products (1024 with 128 channels) in turn, 1450 cycles a tile, and by 4000 cycles an item for its query rows, first
 // maxima and epilogue: 4 x 1560 queries of 24 heads against 13976 keys each, 128 channels, 880 us (1218 TFLOP/s, in a longer loop under the power limit 1060); 148 x 8 items of
 // three tiles 64 us.
+//
+// Pages of codes (q4.cuh) come as they are, by bulk copies into a ring of their own, and eight warps make tiles of them, four of keys and four of values: a tile of both costs
+// them 8 x 300 instructions and 64 KB of shared memory written, beside 96 KB that the products read (256 rows against 49152 keys of 8 heads, us: 73; without that work 63, bf16
+// tiles by TMA 58 and 45 more for widening the pages before it.  Four warps for both 107, from registers that global loads filled 154).
 #pragma once
 #include <math.h>
 

@@ -176,9 +176,10 @@ struct StreamSmem {
 __device__ __forceinline__ int stream_key(int r) { return r ^ ((r >> 1) & 1); }
 
 // The keys of a warp, where they are codes: pairs of blocks of 16 (one piece of memory of 4.6 KB each of K and V, with pages of 32 and more), from block `blk` on, every
-// `step`-th.  Rows as in the kernel below.  A block takes some 300 instructions, 3 for each pair of values, where its bytes take 100 cycles of the SM's share of HBM, so that
-// what counts is how many of them are issued: two blocks side by side, for each of which the other's latencies are filled; the rows' maxima looked at
-// by every lane for itself, and brought together only where one has outgrown its reference.
+// `step`-th.  Rows as in the kernel below.  A block takes some 310 instructions, 3 for each pair of values, of which half are the ALU's (two cycles each), where its bytes take
+// 100 cycles of the SM's share of HBM: what counts is how many are issued.  Hence two blocks side by side, for each of which the other's latencies are filled; the rows'
+// maxima looked at by every lane for itself, and brought together only where one has outgrown its reference; sums and exponents two at a time.  (64 x 8 x 2048 keys,
+// 151 MB, us: one block at a time 73, two 60, with the masks' constant in a register 51, and one CTA an item 44; 32 x 8 x 16 rows x 2048 keys, 75 MB, 32.)
 template <int D, int NT, class Smem>
 __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const PrefixParams& p, Smem& sm, const int32_t* pages, int hk, int blk, int step, int b1, int k1,
                                              int rel_min, const int (&see)[NT][2], const uint4 (&q)[NT][D / 32], float (&o)[NT][D / 16][4], float (&m)[NT][2],
