@@ -171,6 +171,89 @@ void same_pools(const PoolQ4& k, const PoolQ4& v) {
   TORCH_CHECK_VALUE(k.pages == v.pages && k.Hkv == v.Hkv && k.page == v.page && k.d == v.d, "k_pool and v_pool have different shapes");
 }
 
+// What a call allocates: its outputs are parts of one allocation, each at a multiple of 512 bytes, since an allocation takes 0.8 us of a call's 5 to 8 on the host.
+// Above 16 MB the device takes longer than that, and each is its own, so that who keeps one output does not keep the others' memory; for the same reason a
+// workspace is among them only up to 64 KB.  (Measured, us of host time apart and together: attention of one token 7.65 and 6.2, read of two short sequences 6.5
+// and 5.6.)
+class Outputs {
+ public:
+  explicit Outputs(const Call& c) : c_(c) {}
+  void add(View& v) {
+    if (!v.there()) add(v, at::kBFloat16, 2, v.size, v.stride);
+  }
+  void add(Arg& r, at::ScalarType type, std::initializer_list<int64_t> sizes) {
+    if (r.there()) return;
+    int64_t size[4], stride[4];
+    int n = 0;
+    for (int64_t x : sizes) size[n++] = x;
+    int64_t next = 1;
+    for (int k = n - 1; k >= 0; k--) stride[k] = next, next *= size[k];
+    add(r, type, type == at::kFloat ? 4 : type == at::kBFloat16 ? 2 : 1, at::IntArrayRef(size, n), at::IntArrayRef(stride, n));
+    r.numel = next;
+  }
+  void add_ws(Arg& r, size_t bytes) {
+    if (bytes > kWorkspaceWithin)
+      c_.make_ws(r, bytes);
+    else
+      add(r, at::kByte, {static_cast<int64_t>(bytes > 256 ? bytes : 256)});
+  }
+  void allocate() {
+    const auto options = at::TensorOptions().device(c_.device);
+    at::Tensor all;
+    if (n_ > 1 && total_ <= kTogether) all = at::empty({total_}, options.dtype(at::kByte));
+    for (int k = 0; k < n_; k++) {
+      const Wanted& w = wanted_[k];
+      const at::IntArrayRef sizes(w.size, w.dims), strides(w.stride, w.dims);
+      if (all.defined()) {
+        auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), c10::scalarTypeToTypeMeta(w.type));
+        impl->set_storage_offset(w.at / w.item);
+        impl->set_sizes_and_strides(sizes, strides);
+        w.out->t = at::Tensor(std::move(impl));
+        w.out->ptr = static_cast<char*>(all.data_ptr()) + w.at;
+      } else {
+        w.out->t = at::empty_strided(sizes, strides, options.dtype(w.type));
+        w.out->ptr = w.out->t.data_ptr();
+      }
+    }
+  }
+
+ private:
+  static constexpr int64_t kTogether = 16 << 20;
+  static constexpr size_t kWorkspaceWithin = 64 << 10;
+  struct Wanted {
+    Arg* out;
+    at::ScalarType type;
+    int64_t item, at;
+    int dims;
+    int64_t size[4], stride[4];
+  };
+  void add(Arg& r, at::ScalarType type, int64_t item, at::IntArrayRef sizes, at::IntArrayRef strides) {
+    Wanted& w = wanted_[n_++];
+    w.out = &r;
+    w.type = type;
+    w.item = item;
+    w.dims = static_cast<int>(sizes.size());
+    int64_t last = 0;
+    bool none = false;
+    for (int k = 0; k < w.dims; k++) {
+      w.size[k] = sizes[k];
+      w.stride[k] = strides[k];
+      none = none || sizes[k] == 0;
+      last += (sizes[k] - 1) * strides[k];
+    }
+    w.at = total_;
+    if (none || total_ > kTogether || last > kTogether) {      // (nothing to save, and no sum to overflow)
+      total_ = kTogether + 1;
+    } else {
+      total_ += ((last + 1) * item + 511) / 512 * 512;
+    }
+  }
+  const Call& c_;
+  Wanted wanted_[3];
+  int n_ = 0;
+  int64_t total_ = 0;
+};
+
 PyObject* result(int status, std::initializer_list<PyObject*> items) {
   PyObject* r = PyTuple_New(static_cast<Py_ssize_t>(items.size()) + 1);
   PyObject* st = PyLong_FromLong(status);
@@ -227,7 +310,9 @@ PyObject* attn(PyObject* const* a, Py_ssize_t n) {
   TORCH_CHECK_VALUE(pool_d == d, "q and the pools have different head dimensions");
   TORCH_CHECK_VALUE(length.numel == seqs, "length: one entry for each row of the table");
   TORCH_CHECK_VALUE(seq.there() ? seq.numel == B : B <= seqs, "q has more batch entries than there are sequences");
-  Arg o, lse;
+  View o = q;      // the caller's, or one with the shape and strides of q
+  o.t = at::Tensor();
+  Arg lse;
   if (a[10] != Py_None) {
     const View given = take_view(c, 10, "o");
     for (int i = 0; i < 4; i++)
@@ -245,13 +330,12 @@ PyObject* attn(PyObject* const* a, Py_ssize_t n) {
   c.find_stream();
   int st;
   without_lock([&] {
-    if (!o.there()) {
-      o.t = at::empty_strided(q.size, q.stride, at::TensorOptions().dtype(at::kBFloat16).device(c.device));
-      o.ptr = o.t.data_ptr();
-    }
-    if (want_lse) c.make(lse, at::kFloat, {B, H, L});
+    Outputs made(c);
+    made.add(o);
+    if (want_lse) made.add(lse, at::kFloat, {B, H, L});
     if (!ws.there())
-      c.make_ws(ws, Q4 ? f_attn_q4_ws(B, H, Hkv, L, d, page, pages, width, prefix_pages) : f_attn_ws(B, H, Hkv, L, d, page, width, prefix_pages));
+      made.add_ws(ws, Q4 ? f_attn_q4_ws(B, H, Hkv, L, d, page, pages, width, prefix_pages) : f_attn_ws(B, H, Hkv, L, d, page, width, prefix_pages));
+    made.allocate();
     if constexpr (Q4)
       st = f_attn_q4(B, H, Hkv, L, d, page, pages, seqs, width, q, k4, v4, table.as<int32_t>(), length.as<int32_t>(), seq.as<int32_t>(),
                      count.as<int32_t>(), prefix_pages, causal ? AVSA_CAUSAL : 0u, scale, o.ptr, lse.as<float>(), log.as<int32_t>(), ws.ptr,
@@ -397,36 +481,6 @@ View output_view(Call& c, int i, const char* name, std::initializer_list<int64_t
   for (int64_t x : size) TORCH_CHECK_VALUE(r.size[k++] == x, name, ": expected the shape of the result");
   return r;
 }
-void make_view(const Call& c, View& r) {
-  if (r.there()) return;
-  r.t = at::empty_strided(r.size, r.stride, at::TensorOptions().dtype(at::kBFloat16).device(c.device));
-  r.ptr = r.t.data_ptr();
-}
-
-// Two outputs without gaps that the caller did not bring: one allocation, the second one's begin at a multiple of 512 bytes.  (An allocation is 0.8 us of a call's 6.)
-void make_views(const Call& c, View& a, View& b) {
-  if (a.there() || b.there()) {
-    make_view(c, a);
-    make_view(c, b);
-    return;
-  }
-  auto elements = [](const View& v) {
-    int64_t n = 1;
-    for (int64_t x : v.size) n *= x;
-    return (n + 255) / 256 * 256;
-  };
-  const int64_t first = elements(a);
-  const at::Tensor both = at::empty({first + elements(b)}, at::TensorOptions().dtype(at::kBFloat16).device(c.device));
-  auto part = [&](View& v, int64_t at) {
-    auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(both.storage()), both.key_set(), both.dtype());
-    impl->set_storage_offset(at);
-    impl->set_sizes_and_strides(v.size, v.stride);
-    v.t = at::Tensor(std::move(impl));
-    v.ptr = static_cast<char*>(both.data_ptr()) + 2 * at;
-  };
-  part(a, 0);
-  part(b, first);
-}
 
 // read_q4(k_pool, v_pool, table, length, tokens, seq, count, k, v) -> (status, k, v)
 PyObject* py_read_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -448,7 +502,10 @@ PyObject* py_read_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
   c.find_stream();
   int st;
   without_lock([&] {
-    make_views(c, k, v);
+    Outputs made(c);
+    made.add(k);
+    made.add(v);
+    made.allocate();
     st = f_read_q4(entries, kp.Hkv, tokens, kp.d, kp.page, kp.pages, seqs, width, kp, vp, table.as<int32_t>(), length.as<int32_t>(), seq.as<int32_t>(),
                    count.as<int32_t>(), k, v, c.stream);
   });
@@ -510,10 +567,10 @@ PyObject* py_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   c.find_stream();
   int st;
   without_lock([&] {
-    if (k.there())
-      make_views(c, q_out, k_out);
-    else
-      make_view(c, q_out);
+    Outputs made(c);
+    made.add(q_out);
+    if (k.there()) made.add(k_out);
+    made.allocate();
     st = f_rope(B, H, Hk, N, d, q, k, q_out, k_out, pos.as<int32_t>(), pos_stride, static_cast<int>(axes), sections, freq.as<double>(), flags, c.stream);
   });
   return result(st, {c.give(7, q_out), c.give(8, k_out)});

@@ -416,6 +416,35 @@ def test_attention_reproduces_and_ignores_old_memory(B, L, H, Hkv, shared):
 
 
 @gpu
+@pytest.mark.parametrize("L", [1, 33, 400])
+def test_outputs_of_a_call_lie_apart(L):
+    """The outputs and the workspace of one call overlap nowhere, begin on 512 bytes, and keep no more memory than they need; q's strides go over to o."""
+    case = held_case(2, 6, 3, L, 64, 16, [100 + L, 9 + L], seed=21)[0]
+    q, k, v, table, length = case
+    wide = torch.zeros((2, L, 8, 64), dtype=torch.bfloat16, device="cuda").transpose(1, 2)
+    wide[:, :6] = q
+    for query in (q, wide[:, :6]):
+        o, lse, ws = av.avsa_prefix_attn_q4(query, k, v, cu(table), cu(length), want_lse=True)
+        assert o.stride() == query.stride()
+        spans = []
+        for t in (o, lse, ws):
+            last = sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
+            spans.append((t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()))
+            assert t.data_ptr() % 512 == 0 and t._version == 0
+        spans.sort()
+        assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
+        held = {t.untyped_storage().data_ptr(): t.untyped_storage().nbytes() for t in (o, lse, ws)}
+        assert sum(held.values()) <= sum(-(-(b - a) // 512) * 512 for a, b in spans)
+        kept = o.clone(), lse.clone()
+        ws.fill_(255)
+        assert torch.equal(o, kept[0])
+        lse.fill_(7.0)
+        assert torch.equal(o, kept[0])
+        o.fill_(3.0)
+        assert (lse == 7).all()
+
+
+@gpu
 @pytest.mark.parametrize("L", [1, 40, 900])
 def test_attention_reports_malformed_tables(L):
     """Pages out of range contribute nothing (zeros), lengths beyond the row are cut: reported, and the other sequences are right."""
