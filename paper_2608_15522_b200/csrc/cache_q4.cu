@@ -124,12 +124,8 @@ __global__ void __launch_bounds__(kQ4Threads, 8) tokens_q4_kernel(const __grid_c
         ks = *k_scale;
         vs = *v_scale;
       }
-      widen(kc, ks, a.k_pool.sixteen, x);
+      widen(kc, ks, a.k_pool.sixteen, x);      // (a scale of zero: 16 * 0 - 24 * 0 = 0)
       widen(vc, vs, a.k_pool.sixteen, y);
-      if (!there) {      // (-8 times a scale of zero is -0)
-#pragma unroll
-        for (int j = 0; j < 16; j++) x[j] = y[j] = 0u;
-      }
       store_group<WIDE>(k, x);
       store_group<WIDE>(v, y);
     } else if (there) {

@@ -57,16 +57,12 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ float4 load_cluster_f4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-  return v;
+__device__ __forceinline__ void cluster_store_f32x4(uint32_t addr, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
-__device__ __forceinline__ float load_cluster_f(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-  return v;
-}
+// A CTA's shared memory is there once the CTA has begun: each says so at once, and waits for the others only before it writes to them.
+__device__ __forceinline__ void cluster_begun() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_all_begun() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t stream_cluster_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -153,7 +149,7 @@ __device__ __forceinline__ void prefix_check_begin(const PrefixParams& p) {
 }
 
 // CTAs that an SM holds, by shared memory: with one product's columns three of two stages (of 8 KB; 64 sequences of 100 to 2048 keys, us: 55.4, two of three stages 58.7),
-// with two products' the warps take longer and want more ahead (32 sequences x 8 x 2048 keys, 16 rows: 71.5 and 58.0).  Codes: by registers, 127 and 227 a thread (32 x 8 items of
+// with two products' the warps take longer and want more ahead (32 sequences x 8 x 2048 keys, 16 rows: 71.5 and 58.0).  Codes: by registers, 128 and 233 a thread (32 x 8 items of
 // 2048 keys, 16 rows, us, with two, three and four CTAs of them: 33, 46, 39); two stages (of 4.6 KB) are as good as three.
 constexpr int stream_ctas(int NT, bool q4) { return q4 ? (NT == 1 ? 4 : 2) : NT == 1 ? 3 : 2; }
 
@@ -164,42 +160,75 @@ struct StreamSmem {
   static constexpr int kStage = Q4 ? 4 * kBlock : 2 * (D / 64) * kPanel;      // a stage: panels of K, panels of V, or two blocks of each
   union {
     uint8_t ring[kStWarps][kStages][kStage];      // 128-byte swizzled
-    float4 o[kStWarps][kStRows][D / 4];           // behind the keys; [0] becomes the CTA's
+    float4 o[kStWarps][kStRows][D / 4];           // behind the keys
   };
   uint64_t full[kStWarps][kStages];
   float m[kStWarps][kStRows], l[kStWarps][kStRows];
-  float cm[kStRows], cl[kStRows];
+  // what the CTAs of a cluster send this one: its share of the rows' vectors, and what they are relative to (reference, sum of weights)
+  float4 in_o[8 * NT * (D / 4) + 8];
+  float2 in_ml[8 * NT * (D / 4) + 8];
+  int per, by_per;      // vectors of each CTA, at most; at / per is at * by_per >> 20 for all of them (at * (by_per * per - 2^20) is at most 2^18)
 };
 
 // The key of a block of codes that is row r (of 8) of S^T.  Keys' codes are 64 bytes apart (128 channels), so that a product's operands come from shared memory without
 // two lanes of a phase at one bank where neighbouring rows, and rows two apart, alternate between even and odd keys.
 __device__ __forceinline__ int stream_key(int r) { return r ^ ((r >> 1) & 1); }
 
-// The keys of a warp, where they are codes: pairs of blocks of 16 (one piece of memory of 4.6 KB each of K and V, with pages of 32 and more), from block `blk` on, every
-// `step`-th.  Rows as in the kernel below.  A block takes some 310 instructions, 3 for each pair of values, of which half are the ALU's (two cycles each), where its bytes take
-// 100 cycles of the SM's share of HBM: what counts is how many are issued.  Hence two blocks side by side, for each of which the other's latencies are filled; the rows'
-// maxima looked at by every lane for itself, and brought together only where one has outgrown its reference; sums and exponents two at a time.  (64 x 8 x 2048 keys,
-// 151 MB, us: one block at a time 73, two 60, with the masks' constant in a register 51, and one CTA an item 44; 32 x 8 x 16 rows x 2048 keys, 75 MB, 32.)
-template <int D, int NT, class Smem>
-__device__ __forceinline__ void stream_codes(const PrefixCodes& src, const PrefixParams& p, Smem& sm, const int32_t* pages, int hk, int blk, int step, int b1, int k1,
-                                             int rel_min, const int (&see)[NT][2], const uint4 (&q)[NT][D / 32], float (&o)[NT][D / 16][4], float (&m)[NT][2],
-                                             float (&l)[NT][2], int item) {
-  constexpr unsigned FULLM = 0xffffffffu;
-  constexpr int STAGES = Smem::kStages, BLOCK = Smem::kBlock, G = D / kQ4Group;
-  const PrefixShape& S = p.s;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, c = lane & 3, block_shift = S.page_shift - 4;
-  const uint32_t ring = smem_u32(&sm.ring[warp][0][0]), full = smem_u32(&sm.full[warp][0]);
-  const uint32_t sixteen = src.k.sixteen;
-  const bool single = block_shift == 0;      // a page is one block: pairs are two pages
-  const uint8_t* const k_head = src.k.ptr + hk * src.k.stride_head;
-  const uint8_t* const v_head = src.v.ptr + hk * src.v.stride_head;
-  auto page_of = [&](int at) { return at < b1 ? pages[at >> block_shift] : -1; };
-  auto exists = [&](int page) { return static_cast<unsigned>(page) < static_cast<unsigned>(S.pages); };
-  auto load = [&](int at, int page0, int page1, int stage) {
-    if (at >= b1) return;
+// The pages of a warp's first 8 blocks of 16 keys, `step` apart (PAIRS: and of the one behind each), by one load, a lane each, which asks for them before the sequence's
+// length is known where it can.  (One at a time, each asked for when the one before had come, the six stages of a ring took 2 us to fill.)
+template <bool PAIRS>
+struct FirstPages {
+  const int32_t* row;
+  int step, id0 = 0, id1 = 0;
+  __device__ __forceinline__ FirstPages(const PrefixParams& p, int slot, int step_) : row(p.table + static_cast<int64_t>(max(slot, 0)) * p.s.width), step(step_) {}
+  __device__ __forceinline__ void look_up(const PrefixShape& S, int blk) {
+    const int mine = blk + static_cast<int>(threadIdx.x & 7) * step, last = S.width - 1;
+    id0 = row[min(mine >> (S.page_shift - 4), last)];
+    if (PAIRS && S.page_shift == 4) id1 = row[min(mine + 1, last)];
+  }
+  __device__ __forceinline__ int page(int k) const { return __shfl_sync(0xffffffffu, id0, k); }
+  __device__ __forceinline__ int page_behind(const PrefixShape& S, int k) const { return __shfl_sync(0xffffffffu, PAIRS && S.page_shift == 4 ? id1 : id0, k); }
+};
+
+// The ring of a warp whose keys are codes: a stage has a pair of blocks of 16 keys (one piece of memory of 4.6 KB each of K and V, with pages of 32 and more).
+template <int D, class Smem>
+struct CodePairs {
+  static constexpr int BLOCK = Smem::kBlock;
+  const PrefixCodes& src;
+  Smem& sm;
+  const PrefixShape& S;
+  const int32_t* row;
+  int b1, step, at, next0, next1, warp, lane;
+  uint32_t ring, full;
+  const uint8_t *k_head, *v_head;
+  __device__ __forceinline__ CodePairs(const PrefixCodes& src_, const PrefixShape& S_, Smem& sm_, const FirstPages<true>& ids, int hk, int blk, int b1_)
+      : src(src_), sm(sm_), S(S_), row(ids.row), b1(b1_), step(ids.step), at(blk), warp(threadIdx.x >> 5), lane(threadIdx.x & 31),
+        ring(smem_u32(&sm_.ring[threadIdx.x >> 5][0][0])), full(smem_u32(&sm_.full[threadIdx.x >> 5][0])), k_head(src_.k.ptr + hk * src_.k.stride_head),
+        v_head(src_.v.ptr + hk * src_.v.stride_head) {
+    static_assert(Smem::kStages < 8, "the pages of a ring and the next one");
+#pragma unroll 1
+    for (int k = 0; k < Smem::kStages; k++) {
+      load(at, ids.page(k), ids.page_behind(S, k), k);
+      at += step;
+    }
+    next0 = ids.page(Smem::kStages);
+    next1 = ids.page_behind(S, Smem::kStages);
+  }
+  __device__ __forceinline__ bool single() const { return S.page_shift == 4; }      // a page is one block: pairs are two pages
+  __device__ __forceinline__ bool exists(int page) const { return static_cast<unsigned>(page) < static_cast<unsigned>(S.pages); }
+  __device__ __forceinline__ int page_of(int blk) const { return blk < b1 ? row[blk >> (S.page_shift - 4)] : -1; }
+  __device__ __forceinline__ void load_next(int stage) {
+    const int blk = at, page0 = next0, page1 = next1;
+    at += step;
+    next0 = page_of(at);
+    next1 = single() ? page_of(at + 1) : next0;
+    load(blk, page0, page1, stage);
+  }
+  __device__ __forceinline__ void load(int blk, int page0, int page1, int stage) {
+    if (blk >= b1) return;
     const uint32_t bar = full + stage * 8, dst = ring + stage * Smem::kStage;
     const bool has0 = exists(page0), has1 = exists(page1);
-    if (!(has0 && (has1 || at + 1 >= b1))) {
+    if (!(has0 && (has1 || blk + 1 >= b1))) {
       // a page that does not exist reads as zeros: scales of zero, the codes may be anything
       for (int h = 0; h < 2; h++)
         if (!(h == 0 ? has0 : has1))
@@ -211,13 +240,13 @@ __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const Prefi
       __syncwarp();
     }
     if (lane == 0) {
-      if (!single && has0) {
-        const int64_t in = page0 * src.k.stride_page + static_cast<int64_t>(at & ((1 << block_shift) - 1)) * BLOCK;
-        const int64_t in_v = page0 * src.v.stride_page + static_cast<int64_t>(at & ((1 << block_shift) - 1)) * BLOCK;
+      if (!single() && has0) {
+        const int64_t in = page0 * src.k.stride_page + static_cast<int64_t>(blk & ((1 << (S.page_shift - 4)) - 1)) * BLOCK;
+        const int64_t in_v = page0 * src.v.stride_page + static_cast<int64_t>(blk & ((1 << (S.page_shift - 4)) - 1)) * BLOCK;
         mbar_expect_tx(bar, 4 * BLOCK);
         bulk_load_1d(dst, k_head + in, 2 * BLOCK, bar);
         bulk_load_1d(dst + 2 * BLOCK, v_head + in_v, 2 * BLOCK, bar);
-      } else if (single && (has0 || has1)) {
+      } else if (single() && (has0 || has1)) {
         mbar_expect_tx(bar, ((has0 ? 2 : 0) + (has1 ? 2 : 0)) * BLOCK);
         if (has0) {
           bulk_load_1d(dst, k_head + page0 * src.k.stride_page, BLOCK, bar);
@@ -231,17 +260,30 @@ __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const Prefi
         mbar_arrive(bar);
       }
     }
-  };
-  int ahead = blk, next0 = page_of(ahead), next1 = single ? page_of(ahead + 1) : next0;
-  auto load_next = [&](int stage) {
-    const int page0 = next0, page1 = next1;
-    next0 = page_of(ahead + step);
-    next1 = single ? page_of(ahead + step + 1) : next0;
-    load(ahead, page0, page1, stage);
-    ahead += step;
-  };
-#pragma unroll 1
-  for (int k = 0; k < STAGES; k++) load_next(k);
+  }
+  __device__ __forceinline__ bool wait(int stage, int round) const { return __all_sync(0xffffffffu, mbar_wait(full + stage * 8, round & 1)); }
+  // a load never came: the status says so, the rows lack this warp's keys from there on, and what is under way lands before this memory is given away
+  __device__ __forceinline__ void give_up(const PrefixParams& p, int item, int blk, int stage, int round) const {
+    report_logged(p.status, p.log, AVSA_ERR_TIMEOUT, kPxKFull, item, blk);
+    for (int k = 0; k < Smem::kStages; k++) mbar_wait(full + k * 8, (round + (k < stage ? 1 : 0)) & 1);
+  }
+};
+
+// The keys of a warp, where they are codes: pairs of blocks of 16 (one piece of memory of 4.6 KB each of K and V, with pages of 32 and more), from block `blk` on, every
+// `step`-th.  Rows as in the kernel below.  A block takes some 310 instructions, 3 for each pair of values, of which half are the ALU's (two cycles each), where its bytes take
+// 100 cycles of the SM's share of HBM: what counts is how many are issued.  Hence two blocks side by side, for each of which the other's latencies are filled; the rows'
+// maxima looked at by every lane for itself, and brought together only where one has outgrown its reference; sums and exponents two at a time.  (64 x 8 x 2048 keys,
+// 151 MB, us: one block at a time 73, two 60, with the masks' constant in a register 51, and one CTA an item 44; 32 x 8 x 16 rows x 2048 keys, 75 MB, 32.)
+template <int D, int NT, class Smem>
+__device__ __forceinline__ void stream_codes(const PrefixCodes& src, const PrefixParams& p, Smem& sm, const FirstPages<true>& ids, int hk, int blk, int b1, int k1,
+                                             int rel_min, const int (&see)[NT][2], const uint4 (&q)[NT][D / 32], float (&o)[NT][D / 16][4], float (&m)[NT][2],
+                                             float (&l)[NT][2], int item) {
+  constexpr unsigned FULLM = 0xffffffffu;
+  constexpr int STAGES = Smem::kStages, BLOCK = Smem::kBlock, G = D / kQ4Group;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, c = lane & 3;
+  const uint32_t sixteen = src.k.sixteen;
+  const int step = ids.step;
+  CodePairs<D, Smem> pairs(src, p.s, sm, ids, hk, blk, b1);
   const int key = stream_key(n), key0 = stream_key(2 * c), key1 = stream_key(2 * c + 1);      // as an operand's rows; as its columns
   const float inv_scale = 1.0f / p.scale_log2;
   const uint64_t scale2 = pack_f32x2(p.scale_log2, p.scale_log2);
@@ -252,7 +294,7 @@ __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const Prefi
   bool ok = true;
 #pragma unroll 1
   for (; blk < b1; blk += step) {
-    if (!__all_sync(FULLM, mbar_wait(full + stage * 8, round & 1))) {
+    if (!pairs.wait(stage, round)) {
       ok = false;
       break;
     }
@@ -394,17 +436,13 @@ __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const Prefi
       }
     }
     __syncwarp();      // all lanes have read the stage
-    load_next(stage);
+    pairs.load_next(stage);
     if (++stage == STAGES) {
       stage = 0;
       round++;
     }
   }
-  if (!ok) {
-    // a load never came: the status says so, the rows lack this warp's keys from there on, and what is under way lands before this memory is given away
-    report_logged(p.status, p.log, AVSA_ERR_TIMEOUT, kPxKFull, item, blk);
-    for (int k = 0; k < STAGES; k++) mbar_wait(full + k * 8, (round + (k < stage ? 1 : 0)) & 1);
-  }
+  if (!ok) pairs.give_up(p, item, blk, stage, round);
 }
 
 // Where the parts of the beginning of stacked row rho are: `n` of them, `step` rows apart.
@@ -489,6 +527,7 @@ prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__
     }
     id--;
   }
+  if (ctas > 1) cluster_begun();
   // ---- the item: rows, keys
   const int split = t.splits > 1 ? id % t.splits : 0;
   if (t.splits > 1) id /= t.splits;
@@ -506,6 +545,14 @@ prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__
     k0 = S.k0;
     k1 = prefix_sequence(p, entry, slot, bad);
   }
+  if (ctas > 1 && threadIdx.x == 0) {
+    sm.per = (rows * (D / 4) + ctas - 1) / ctas;
+    sm.by_per = (1 << 20) / sm.per + 1;
+  }
+  constexpr int PER = Q4 ? 2 : 1;      // blocks that a warp takes at a time
+  FirstPages<Q4> ids(p, slot, PER * ctas * kStWarps);
+  const int ahead = PER * (rank * kStWarps + warp);
+  if (t.splits <= 1) ids.look_up(S, (k0 >> 4) + ahead);
   // Lane r: how far row r sees.  The thread's columns are rows 8x + 2c and 8x + 2c + 1 of S^T and O^T; as an operand, Q is row 8x + n.
   auto row_of = [&](int r, int& b, int& i, int& head, int& len) {
     int rr = row0 + r;
@@ -550,6 +597,7 @@ prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__
     if (Q4) per = (per + 1) & ~1;      // (pairs of blocks)
     b0 = min(b1, b0 + split * per);
     b1 = min(b1, b0 + per);
+    ids.look_up(S, b0 + ahead);
   }
   float o[NT][D / 16][4];       // product 4j + y: {channel 64j + 8n + 2y (of codes (D/8)n + 8j + 2y), the next} x {row 2c, the next}, as [2 * channel + row]
 #pragma unroll
@@ -559,9 +607,8 @@ prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__
   float m[NT][2], l[NT][2];
 #pragma unroll
   for (int x = 0; x < NT; x++) m[x][0] = m[x][1] = -INFINITY, l[x][0] = l[x][1] = 0.f;
-  const int32_t* const pages = p.table + static_cast<int64_t>(max(slot, 0)) * S.width;
   if constexpr (Q4) {
-    stream_codes<D, NT>(src, p, sm, pages, hk, b0 + 2 * (rank * kStWarps + warp), 2 * ctas * kStWarps, b1, k1, rel_min, see, q, o, m, l, item);
+    stream_codes<D, NT>(src, p, sm, ids, hk, b0 + ahead, b1, k1, rel_min, see, q, o, m, l, item);
   } else {
     const int step = ctas * kStWarps;
     const int block_shift = S.page_shift - 4;
@@ -581,17 +628,15 @@ prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__
     auto vec = [&](int stage, int panel, int key, int chunk) {
       return *reinterpret_cast<const uint4*>(&sm.ring[warp][stage][panel * PANEL + key * 128 + ((chunk ^ (key & 7)) << 4)]);
     };
-    auto page_of = [&](int blk) { return blk < b1 ? pages[blk >> block_shift] : -1; };
+    auto page_of = [&](int blk) { return blk < b1 ? ids.row[blk >> block_shift] : -1; };
 
-    int blk = b0 + rank * kStWarps + warp, ahead = blk;
-    int next = page_of(ahead);
+    int blk = b0 + ahead, at = blk;
 #pragma unroll
     for (int k = 0; k < STAGES; k++) {
-      const int page = next;
-      next = page_of(ahead + step);
-      load(ahead, page, k);
-      ahead += step;
+      load(at, ids.page(k), k);
+      at += step;
     }
+    int next = ids.page(STAGES);
     int stage = 0, round = 0;
     bool ok = true;
 #pragma unroll 1
@@ -682,9 +727,9 @@ prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__
       __syncwarp();      // all lanes have read the stage
       {
         const int page = next;
-        next = page_of(ahead + step);
-        load(ahead, page, stage);
-        ahead += step;
+        next = page_of(at + step);
+        load(at, page, stage);
+        at += step;
       }
       if (++stage == STAGES) {
         stage = 0;
@@ -700,6 +745,8 @@ prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__
   __syncthreads();      // the ring is the warps' rows from here on
 
   // ---- the warps of the CTA
+  // (the vectors of a row change places by its number: lanes of four rows write at a time, whose distance is a multiple of all banks; 16 rows took 1.5 us here)
+  auto turned = [](int r) { return Q4 && D == 128 ? (r >> 1) & 3 : ((r >> 1) & 1) | (r & 4); };
 #pragma unroll
   for (int x = 0; x < NT; x++)
 #pragma unroll
@@ -714,7 +761,7 @@ prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__
         }
 #pragma unroll
         for (int y = 0; y < D / 16; y += 2)
-          sm.o[warp][r][((y >> 2) * (Q4 ? 8 : 64) + (Q4 ? D / 8 : 8) * n + 2 * (y & 3)) / 4] = make_float4(o[x][y][e], o[x][y][2 + e], o[x][y + 1][e], o[x][y + 1][2 + e]);
+          sm.o[warp][r][(((y >> 2) * (Q4 ? 8 : 64) + (Q4 ? D / 8 : 8) * n + 2 * (y & 3)) / 4) ^ turned(r)] = make_float4(o[x][y][e], o[x][y][2 + e], o[x][y + 1][e], o[x][y + 1][2 + e]);
       }
     }
   __syncthreads();
@@ -724,10 +771,9 @@ prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__
   }
   constexpr int V = D / 4;       // vectors of a row
   const int total = rows * V;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  float M = -INFINITY, L = 0.f;
-  for (int at = threadIdx.x; at < total; at += kStThreads) {
-    const int r = at / V, x = at % V;
+  float4 acc;
+  float M, L;
+  auto of_warps = [&](int r, int x) {
     M = -INFINITY;
 #pragma unroll
     for (int w = 0; w < kStWarps; w++) M = fmaxf(M, sm.m[w][r]);
@@ -736,46 +782,56 @@ prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__
 #pragma unroll
     for (int w = 0; w < kStWarps; w++) {
       const float f = sm.m[w][r] == -INFINITY ? 0.f : fast_exp2(sm.m[w][r] - M);
-      const float4 v = sm.o[w][r][x];
+      const float4 v = sm.o[w][r][x ^ turned(r)];
       L += f * sm.l[w][r];
       acc.x += f * v.x;
       acc.y += f * v.y;
       acc.z += f * v.z;
       acc.w += f * v.w;
     }
-    if (ctas > 1) {
-      // (every vector is read by the one thread that replaces it)
-      sm.o[0][r][x] = acc;
-      if (x == 0) {
-        sm.cm[r] = M;
-        sm.cl[r] = L;
-      }
-    } else {
-      stream_finish<D>(p, t, item, split, hk, entry, row0, r, x, acc, M, L);
+  };
+  if (ctas == 1) {
+    for (int at = threadIdx.x; at < total; at += kStThreads) {
+      of_warps(at / V, at % V);
+      stream_finish<D>(p, t, item, split, hk, entry, row0, at / V, at % V, acc, M, L);
     }
-  }
-  if (ctas > 1) {
+  } else {
+    const int per = sm.per, by_per = sm.by_per;
+    cluster_all_begun();
+    // each vector to the CTA that has it among its own: it then reads its own memory, and nobody waits until it has (each reading the others' instead, behind one barrier and
+    // before another: 24 heads of 300 keys, codes, us in a row, 5.8, now 5.2; 21 rows x 5 x 8 x 1300 keys of 64 channels 10.7 and 9.3)
+    for (int at = threadIdx.x; at < total; at += kStThreads) {
+      of_warps(at / V, at % V);
+      const int to = at * by_per >> 20;
+      const uint32_t place = rank * per + at - to * per;
+      cluster_store_f32x4(cluster_addr(smem_u32(&sm.in_o[place]), to), acc);
+      cluster_store_f32x2(cluster_addr(smem_u32(&sm.in_ml[place]), to), M, L);
+    }
     cluster_sync_all();
-    for (int at = rank * kStThreads + threadIdx.x; at < total; at += ctas * kStThreads) {
-      const int r = at / V, x = at % V;
+    for (int i = threadIdx.x; i < per && rank * per + i < total; i += kStThreads) {
+      const int at = rank * per + i;
+      float2 ml[8];
       M = -INFINITY;
-      for (int k = 0; k < ctas; k++) M = fmaxf(M, load_cluster_f(cluster_addr(smem_u32(&sm.cm[r]), k)));
+#pragma unroll
+      for (int k = 0; k < 8; k++) {
+        ml[k] = k < ctas ? sm.in_ml[k * per + i] : make_float2(-INFINITY, 0.f);
+        M = fmaxf(M, ml[k].x);
+      }
       L = 0.f;
       acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-      for (int k = 0; k < ctas; k++) {
-        const float mk = load_cluster_f(cluster_addr(smem_u32(&sm.cm[r]), k));
-        const float f = mk == -INFINITY ? 0.f : fast_exp2(mk - M);
-        const float4 v = load_cluster_f4(cluster_addr(smem_u32(&sm.o[0][r][x]), k));
-        L += f * load_cluster_f(cluster_addr(smem_u32(&sm.cl[r]), k));
+#pragma unroll
+      for (int k = 0; k < 8; k++) {
+        if (k >= ctas) break;
+        const float f = ml[k].x == -INFINITY ? 0.f : fast_exp2(ml[k].x - M);
+        const float4 v = sm.in_o[k * per + i];
+        L += f * ml[k].y;
         acc.x += f * v.x;
         acc.y += f * v.y;
         acc.z += f * v.z;
         acc.w += f * v.w;
       }
-      stream_finish<D>(p, t, item, split, hk, entry, row0, r, x, acc, M, L);
+      stream_finish<D>(p, t, item, split, hk, entry, row0, at / V, at % V, acc, M, L);
     }
-    cluster_sync_all();      // nobody leaves while its memory is read
   }
 }
 
