@@ -119,9 +119,11 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     const long long fit = slots * 9ll / 10 / (y.own.items + 1ll), by_keys = keys / 64;
     long long ctas = fit < by_keys ? fit : by_keys;
     ctas = ctas < 1 ? 1 : ctas > 8 ? 8 : ctas;
-    // (codes, whose CTAs are longer at their start and end than at 128 keys: no second CTA for items that fill three quarters of the slots by themselves; 64 x 8 items of 2048
-    // keys of 128 channels 47 and 44, of 64 34 and 28, of 100 to 2048 keys 37 both ways)
-    const long long most_keys = codes > 0 && 4ll * y.own.items >= 3ll * slots ? 2048 : 1024;
+    // (Codes: no second CTA for items that fill three quarters of the slots by themselves and whose start and end weigh more, being half as long or, with 16 rows, twice as
+    // many. us, 1024 and 2048 keys a CTA: 64 channels, 64 x 8 items of 2048 keys 30 and 27, of 1000 to 2048 27 and 25, of up to 2048 23 and 23; 128 channels and 16 rows, 32 x 8
+    // of 2048 keys 36 and 31, of up to 6000 85 and 65; but one product, 64 x 8 of 2048 keys 44 and 42, of 100 to 2048 34 and 36, 20 x 24 of up to 2000 32 and 36.)
+    const bool short_items = codes > 0 && (d == 64 || stream_products(R) == 2) && 4ll * y.own.items >= 3ll * slots;
+    const long long most_keys = short_items ? 2048 : 1024;
     while (ctas < 8 && y.own.items < (1 << 27) && keys > most_keys * ctas) ctas = 2 * ctas < 8 ? 2 * ctas : 8;
     y.own_cluster = static_cast<int>(ctas);
     y.own.splits = 1;
