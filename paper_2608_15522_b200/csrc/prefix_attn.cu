@@ -15,15 +15,15 @@ constexpr int kChunk = 8;        // row tiles that go through the beginning side
 
 constexpr int kStreamRows = 32;      // query rows of a batch entry and key head that the stream kernel takes, at most; of the stacked rows as well
 
-// The same for so many keys (of all heads and sequences).  Codes: the stream kernel widens each of them again for every 16 rows, the tile kernel once for 128, but starts later:
-// 17 to 32 rows against 16 x 8 x 6000 keys of 128 channels, us, by either 78 to 83 and 60 to 62, 64 x 8 x 700 45 to 50 and 47 to 48, 8 x 8 x 2000 20 and 25.
-constexpr long long kManyCodes = 512 * 1024;
-static int stream_rows(bool codes, long long keys) { return codes && keys > kManyCodes ? kStRows : kStreamRows; }
+// The same where many keys (of all heads and sequences) are codes: the stream kernel makes each of them bf16 for every item, the tile kernel once for 128 rows, but starts
+// later.  128 channels, us, by either: 17 to 24 rows (one item) 8 x 8 x 2000 14 and 25, 64 x 8 x 700 33 and 47, 16 x 8 x 6000 63 and 59; up to 32 rows (two) 20 and 25, 47 and
+// 48, 83 and 62.
+static int stream_rows(bool codes, long long keys) { return !codes || keys <= 512 * 1024 ? kStreamRows : keys <= 704 * 1024 ? 24 : 16; }
 
 constexpr int kWidenTiles = 6;       // row tiles that read a tile of codes, beyond which it is made bf16 once for all of them
 
-// Products of 8 columns for so many query rows: with 8 or less the second one's would be empty.
-static int stream_products(long long rows) { return rows <= 8 ? 1 : 2; }
+// Products of 8 columns for so many query rows: with 8 or less the second one's would be empty; three of codes, which then become bf16 once instead of twice.
+static int stream_products(bool codes, long long rows) { return rows <= 8 ? 1 : codes && rows > 16 && rows <= 24 ? 3 : 2; }
 
 struct PrefixLayout {
   PrefixShape s;
@@ -89,15 +89,16 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     y.pre.stacked = 1;
     y.pre.first = 1;
     y.pre.begin = 1;
-    y.pre.tiles = static_cast<int>((RS + kStRows - 1) / kStRows);
+    y.pre.rows = stream_item_rows(stream_products(codes > 0, RS));
+    y.pre.tiles = static_cast<int>((RS + y.pre.rows - 1) / y.pre.rows);
     y.pre.items = y.pre.tiles * Hkv;
-    const int slots = sms * stream_ctas(stream_products(RS), codes > 0);      // CTAs of the stream kernel that the SMs hold
+    const int slots = sms * stream_ctas(stream_products(codes > 0, RS), codes > 0);      // CTAs of the stream kernel that the SMs hold
     const long long by_keys = PT / 2;      // 256 keys a CTA at least: four blocks a warp
     y.pre.splits = static_cast<int>(slots / y.pre.items < by_keys ? slots / y.pre.items : by_keys);
     // The kernel behind joins a row's parts eight at a time, 0.7 us each, so with few heads fewer and longer parts end earlier (4 heads x 60000 keys, us: 111 parts 35.8, 70 31.7).
     while (y.pre.splits > 8 && 12ll * y.pre.splits * y.pre.splits > s.k0) y.pre.splits--;
     if (y.pre.splits < 1) y.pre.splits = 1;
-    rows += static_cast<size_t>(y.pre.items) * y.pre.splits * kStRows;
+    rows += static_cast<size_t>(y.pre.items) * y.pre.splits * y.pre.rows;
   } else if (s.stack) {
     rows += (static_cast<size_t>(y.n_cta) + static_cast<size_t>(Hkv) * s.nrc * s.chunk) * 128;
   }
@@ -107,11 +108,13 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     y.own.join = !s.stack ? 0 : y.pre_stream ? kStJoinStream : kStJoinTile;
     y.own.join_tiles = y.pre.tiles;
     y.own.join_splits = y.pre.splits;
-    y.own.tiles = static_cast<int>((R + kStRows - 1) / kStRows);
+    y.own.join_rows = y.pre.rows;
+    y.own.rows = stream_item_rows(stream_products(codes > 0, R));
+    y.own.tiles = static_cast<int>((R + y.own.rows - 1) / y.own.rows);
     y.own.items = y.own.tiles * Hkv * B;
     y.own.out0 = static_cast<int>(own0);
     const long long keys = static_cast<long long>(width) * page - s.k0;      // at most
-    const int slots = sms * stream_ctas(stream_products(R), codes > 0);
+    const int slots = sms * stream_ctas(stream_products(codes > 0, R), codes > 0);
     // An item's keys over a cluster, 64 keys a CTA at least (a block a warp), as many CTAs as the SMs hold side by side: nine tenths of the slots, since a cluster takes its
     // own from one GPC and what does not fit waits for a whole item (us, filled to the last slot and like this: 96 items of 500 keys of 64 channels 14.4 and 9.7, 72
     // of 900 keys of 128 channels 16.4 and 10.3, 144 of 800 17.5 and 13.0).  No CTA has more than 1024 keys while others may have none (30 x 8 items of 1 to 1500
@@ -122,7 +125,7 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     // (Codes: no second CTA for items that fill three quarters of the slots by themselves and whose start and end weigh more, being half as long or, with 16 rows, twice as
     // many. us, 1024 and 2048 keys a CTA: 64 channels, 64 x 8 items of 2048 keys 30 and 27, of 1000 to 2048 27 and 25, of up to 2048 23 and 23; 128 channels and 16 rows, 32 x 8
     // of 2048 keys 36 and 31, of up to 6000 85 and 65; but one product, 64 x 8 of 2048 keys 44 and 42, of 100 to 2048 34 and 36, 20 x 24 of up to 2000 32 and 36.)
-    const bool short_items = codes > 0 && (d == 64 || stream_products(R) == 2) && 4ll * y.own.items >= 3ll * slots;
+    const bool short_items = codes > 0 && (d == 64 || R > 8) && 4ll * y.own.items >= 3ll * slots;
     const long long most_keys = short_items ? 2048 : 1024;
     while (ctas < 8 && y.own.items < (1 << 27) && keys > most_keys * ctas) ctas = 2 * ctas < 8 ? 2 * ctas : 8;
     y.own_cluster = static_cast<int>(ctas);
@@ -132,7 +135,7 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
       y.own_cluster = 1;
       y.own.splits = (slots - 1) / y.own.items;      // (one slot for the check of the tables)
       if (codes > 0 && keys / 256 < y.own.splits) y.own.splits = static_cast<int>(keys / 256);
-      rows += static_cast<size_t>(y.own.items) * y.own.splits * kStRows;
+      rows += static_cast<size_t>(y.own.items) * y.own.splits * y.own.rows;
     }
     y.own.check = 1;
     y.own.begin = !y.pre_stream;
@@ -200,8 +203,10 @@ static int launch_stream_of(const Source& src, const PrefixParams& p, const Stre
 }
 template <int D, class Source>
 static int launch_stream(const Source& src, const PrefixParams& p, const StreamParams& t, int cluster, cudaStream_t st) {
-  return stream_products(t.stacked ? static_cast<long long>(p.s.B) * p.s.R : p.s.R) == 1 ? launch_stream_of<D, 1>(src, p, t, cluster, st)
-                                                                                          : launch_stream_of<D, 2>(src, p, t, cluster, st);
+  const int products = stream_products(Source::kQ4, t.stacked ? static_cast<long long>(p.s.B) * p.s.R : p.s.R);
+  if constexpr (Source::kQ4)
+    if (products == 3) return launch_stream_of<D, 3>(src, p, t, cluster, st);
+  return products == 1 ? launch_stream_of<D, 1>(src, p, t, cluster, st) : launch_stream_of<D, 2>(src, p, t, cluster, st);
 }
 
 // `src`: of pages, where it is bf16.

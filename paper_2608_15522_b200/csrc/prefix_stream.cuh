@@ -23,19 +23,20 @@
 namespace avsa {
 
 constexpr int kStWarps = 4, kStThreads = 32 * kStWarps;
-constexpr int kStRows = 16;            // of an item, at most: two products' columns
+// Query rows of an item, at most, by its products of 8 columns; where there are three, all rows are one item.
+constexpr int stream_item_rows(int NT) { return NT == 3 ? 24 : 16; }
 
 // What a launch of the kernel below works on.
 struct StreamParams {
   int stacked;         // items are row tiles of the beginning (row tile, key head), else of the sequences (row tile, key head, batch entry)
-  int tiles;           // row tiles of an item's key head
+  int tiles, rows;     // row tiles of an item's key head, and their rows
   int items;
   int splits;          // parts that an item's keys are cut into, each of them a cluster; with more than one, or stacked, the rows are parts
   int first;           // no kernel of this call in front of it
   int begin;           // the first CTA clears the status record
   int check;           // the first cluster looks for what is out of range
   int join;            // 0, or the beginning's parts are in kStJoinStream's or kStJoinTile's places
-  int join_tiles, join_splits;
+  int join_tiles, join_rows, join_splits;
   int out0;            // first partial row
 };
 enum { kStJoinStream = 1, kStJoinTile = 2 };
@@ -149,21 +150,22 @@ __device__ __forceinline__ void prefix_check_begin(const PrefixParams& p) {
 }
 
 // CTAs that an SM holds, by shared memory: with one product's columns three of two stages (of 8 KB; 64 sequences of 100 to 2048 keys, us: 55.4, two of three stages 58.7),
-// with two products' the warps take longer and want more ahead (32 sequences x 8 x 2048 keys, 16 rows: 71.5 and 58.0).  Codes: by registers, 128 and 233 a thread (32 x 8 items of
+// with two products' the warps take longer and want more ahead (32 sequences x 8 x 2048 keys, 16 rows: 71.5 and 58.0).  Codes: by registers, 128, 233 and 248 a thread (32 x 8 items of
 // 2048 keys, 16 rows, us, with two, three and four CTAs of them: 33, 46, 39); two stages (of 4.6 KB) are as good as three.
 constexpr int stream_ctas(int NT, bool q4) { return q4 ? (NT == 1 ? 4 : 2) : NT == 1 ? 3 : 2; }
 
 template <int D, int NT, bool Q4>
 struct StreamSmem {
+  static constexpr int kRows = stream_item_rows(NT);
   static constexpr int kPanel = 16 * 128, kBlock = q4_block_bytes(D);
-  static constexpr int kStages = Q4 ? (NT == 1 ? 2 : 3) * (128 / D) : (NT == 1 ? 2 : 3) * (128 / D);
+  static constexpr int kStages = (NT == 1 ? 2 : 3) * (128 / D);
   static constexpr int kStage = Q4 ? 4 * kBlock : 2 * (D / 64) * kPanel;      // a stage: panels of K, panels of V, or two blocks of each
   union {
     uint8_t ring[kStWarps][kStages][kStage];      // 128-byte swizzled
-    float4 o[kStWarps][kStRows][D / 4];           // behind the keys
+    float4 o[kStWarps][kRows][D / 4];           // behind the keys
   };
   uint64_t full[kStWarps][kStages];
-  float m[kStWarps][kStRows], l[kStWarps][kStRows];
+  float m[kStWarps][kRows], l[kStWarps][kRows];
   // what the CTAs of a cluster send this one: its share of the rows' vectors, and what they are relative to (reference, sum of weights)
   float4 in_o[8 * NT * (D / 4) + 8];
   float2 in_ml[8 * NT * (D / 4) + 8];
@@ -273,13 +275,16 @@ struct CodePairs {
 // `step`-th.  Rows as in the kernel below.  A block takes some 310 instructions, 3 for each pair of values, of which half are the ALU's (two cycles each), where its bytes take
 // 100 cycles of the SM's share of HBM: what counts is how many are issued.  Hence two blocks side by side, for each of which the other's latencies are filled; the rows'
 // maxima looked at by every lane for itself, and brought together only where one has outgrown its reference; sums and exponents two at a time.  (64 x 8 x 2048 keys,
-// 151 MB, us: one block at a time 73, two 60, with the masks' constant in a register 51, and one CTA an item 44; 32 x 8 x 16 rows x 2048 keys, 75 MB, 32.)
+// 151 MB, us: one block at a time 73, two 60, with the masks' constant in a register 51, and one CTA an item 44; 32 x 8 x 16 rows x 2048 keys, 75 MB, 31.)
+// Three products, 17 to 24 rows, on the same operands instead of two items (us): 64 x 8 x 700 keys 45 and 33, 8 x 8 x 2000 17.4 and 14.5, of 64 channels 12.9 and 10.3; of 128
+// channels one block after the other then.
 template <int D, int NT, class Smem>
 __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const PrefixParams& p, Smem& sm, const FirstPages<true>& ids, int hk, int blk, int b1, int k1,
                                              int rel_min, const int (&see)[NT][2], const uint4 (&q)[NT][D / 32], float (&o)[NT][D / 16][4], float (&m)[NT][2],
                                              float (&l)[NT][2], int item) {
   constexpr unsigned FULLM = 0xffffffffu;
   constexpr int STAGES = Smem::kStages, BLOCK = Smem::kBlock, G = D / kQ4Group;
+  constexpr int H = NT == 3 && D == 128 ? 1 : 2;      // blocks side by side (registers)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, c = lane & 3;
   const uint32_t sixteen = src.k.sixteen;
   const int step = ids.step;
@@ -298,140 +303,144 @@ __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const Prefi
       ok = false;
       break;
     }
-    const uint8_t* const tile = &sm.ring[warp][stage][0];
-    // ---- S^T: lane (n, c) has a quarter of the channels of keys `key` and `key` + 8, in whole words
-    float s[2][NT][4];
+#pragma unroll 1
+    for (int h0 = 0; h0 < 2; h0 += H) {
+      const uint8_t* const tile = &sm.ring[warp][stage][h0 * BLOCK];
+      const int first = (blk + h0) * 16;
+      // ---- S^T: lane (n, c) has a quarter of the channels of keys `key` and `key` + 8, in whole words
+      float s[H][NT][4];
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
-      constexpr int W = D / 32;
-      const uint8_t* const k = tile + h * BLOCK;
-      uint32_t ka[W], kb[W];
-      if constexpr (W == 4) {
-        *reinterpret_cast<uint4*>(ka) = *reinterpret_cast<const uint4*>(k + key * (D / 2) + 16 * c);
-        *reinterpret_cast<uint4*>(kb) = *reinterpret_cast<const uint4*>(k + (key + 8) * (D / 2) + 16 * c);
-      } else {
-        *reinterpret_cast<uint2*>(ka) = *reinterpret_cast<const uint2*>(k + key * (D / 2) + 8 * c);
-        *reinterpret_cast<uint2*>(kb) = *reinterpret_cast<const uint2*>(k + (key + 8) * (D / 2) + 8 * c);
-      }
-      const uint16_t* const scales = reinterpret_cast<const uint16_t*>(k + q4_scales_at(D)) + c * (D / 4) / kQ4Group;
-      uint32_t sa = scales[key * G], sb = scales[(key + 8) * G];
-      sa |= sa << 16;
-      sb |= sb << 16;
-      const uint32_t oa = q4_offset(sa), ob = q4_offset(sb);
+      for (int h = 0; h < H; h++) {
+        constexpr int W = D / 32;
+        const uint8_t* const k = tile + h * BLOCK;
+        uint32_t ka[W], kb[W];
+        if constexpr (W == 4) {
+          *reinterpret_cast<uint4*>(ka) = *reinterpret_cast<const uint4*>(k + key * (D / 2) + 16 * c);
+          *reinterpret_cast<uint4*>(kb) = *reinterpret_cast<const uint4*>(k + (key + 8) * (D / 2) + 16 * c);
+        } else {
+          *reinterpret_cast<uint2*>(ka) = *reinterpret_cast<const uint2*>(k + key * (D / 2) + 8 * c);
+          *reinterpret_cast<uint2*>(kb) = *reinterpret_cast<const uint2*>(k + (key + 8) * (D / 2) + 8 * c);
+        }
+        const uint16_t* const scales = reinterpret_cast<const uint16_t*>(k + q4_scales_at(D)) + c * (D / 4) / kQ4Group;
+        uint32_t sa = scales[key * G], sb = scales[(key + 8) * G];
+        sa |= sa << 16;
+        sb |= sb << 16;
+        const uint32_t oa = q4_offset(sa), ob = q4_offset(sb);
 #pragma unroll
-      for (int j = 0; j < W; j++) {
-        uint32_t a[4], b[4];
+        for (int j = 0; j < W; j++) {
+          uint32_t a[4], b[4];
 #pragma unroll
-        for (int i = 0; i < 4; i++) a[i] = q4_pair(ka[j], i, sa, oa, sixteen), b[i] = q4_pair(kb[j], i, sb, ob, sixteen);
+          for (int i = 0; i < 4; i++) a[i] = q4_pair(ka[j], i, sa, oa, sixteen), b[i] = q4_pair(kb[j], i, sb, ob, sixteen);
 #pragma unroll
-        for (int x = 0; x < NT; x++) {
-          if (j == 0)
-            mma_16816_first(s[h][x], a[0], b[0], a[1], b[1], q[x][j].x, q[x][j].y);
-          else
-            mma_16816(s[h][x], a[0], b[0], a[1], b[1], q[x][j].x, q[x][j].y);
-          mma_16816(s[h][x], a[2], b[2], a[3], b[3], q[x][j].z, q[x][j].w);
+          for (int x = 0; x < NT; x++) {
+            if (j == 0)
+              mma_16816_first(s[h][x], a[0], b[0], a[1], b[1], q[x][j].x, q[x][j].y);
+            else
+              mma_16816(s[h][x], a[0], b[0], a[1], b[1], q[x][j].x, q[x][j].y);
+            mma_16816(s[h][x], a[2], b[2], a[3], b[3], q[x][j].z, q[x][j].w);
+          }
         }
       }
-    }
-    if (blk * 16 + 32 > rel_min || blk * 16 + 32 > k1) {
+      if (first + 16 * H > rel_min || first + 16 * H > k1) {
 #pragma unroll
-      for (int h = 0; h < 2; h++)
+        for (int h = 0; h < H; h++)
 #pragma unroll
-        for (int x = 0; x < NT; x++)
+          for (int x = 0; x < NT; x++)
 #pragma unroll
-          for (int e = 0; e < 4; e++)
-            if ((blk + h) * 16 + key + 8 * (e >> 1) >= min(see[x][e & 1], k1)) s[h][x][e] = -INFINITY;
-    }
-    // ---- maxima
-    float top[NT][2];
-    bool grown = false;
-#pragma unroll
-    for (int x = 0; x < NT; x++)
-#pragma unroll
-      for (int e = 0; e < 2; e++) {
-        top[x][e] = fmaxf(max3f(s[0][x][e], s[0][x][2 + e], s[1][x][e]), s[1][x][2 + e]);
-        grown = grown || top[x][e] > limit[x][e];
+            for (int e = 0; e < 4; e++)
+              if (first + 16 * h + key + 8 * (e >> 1) >= min(see[x][e & 1], k1)) s[h][x][e] = -INFINITY;
       }
-    if (__any_sync(FULLM, grown)) {
+      // ---- maxima
+      float top[NT][2];
+      bool grown = false;
 #pragma unroll
       for (int x = 0; x < NT; x++)
 #pragma unroll
         for (int e = 0; e < 2; e++) {
-          float up = top[x][e];
+          top[x][e] = H == 2 ? fmaxf(max3f(s[0][x][e], s[0][x][2 + e], s[H - 1][x][e]), s[H - 1][x][2 + e]) : fmaxf(s[0][x][e], s[0][x][2 + e]);
+          grown = grown || top[x][e] > limit[x][e];
+        }
+      if (__any_sync(FULLM, grown)) {
 #pragma unroll
-          for (int d = 4; d < 32; d <<= 1) up = fmaxf(up, __shfl_xor_sync(FULLM, up, d));
-          up = fmaxf(m[x][e], up * p.scale_log2);
-          const float f = m[x][e] == -INFINITY ? 0.f : fast_exp2(m[x][e] - up);
-          m[x][e] = up;
-          limit[x][e] = (up + 8.f) * inv_scale;
-          ref[x][e] = up == -INFINITY ? 0.f : up;
-          l[x][e] *= f;
+        for (int x = 0; x < NT; x++)
 #pragma unroll
-          for (int y = 0; y < D / 16; y++) {
-            o[x][y][e] *= f;
-            o[x][y][2 + e] *= f;
+          for (int e = 0; e < 2; e++) {
+            float up = top[x][e];
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) up = fmaxf(up, __shfl_xor_sync(FULLM, up, d));
+            up = fmaxf(m[x][e], up * p.scale_log2);
+            const float f = m[x][e] == -INFINITY ? 0.f : fast_exp2(m[x][e] - up);
+            m[x][e] = up;
+            limit[x][e] = (up + 8.f) * inv_scale;
+            ref[x][e] = up == -INFINITY ? 0.f : up;
+            l[x][e] *= f;
+#pragma unroll
+            for (int y = 0; y < D / 16; y++) {
+              o[x][y][e] *= f;
+              o[x][y][2 + e] *= f;
+            }
           }
-        }
-    }
-    // ---- P^T
-    uint32_t pt[2][NT][2];
-#pragma unroll
-    for (int h = 0; h < 2; h++)
-#pragma unroll
-      for (int x = 0; x < NT; x++) {
-        float w[4];
-        const uint64_t no_ref = pack_f32x2(-ref[x][0], -ref[x][1]);
-        uint64_t sum = pack_f32x2(l[x][0], l[x][1]);
-#pragma unroll
-        for (int e = 0; e < 4; e += 2) {
-          unpack_f32x2(fma_f32x2(pack_f32x2(s[h][x][e], s[h][x][e + 1]), scale2, no_ref), w[e], w[e + 1]);
-          w[e] = fast_exp2(w[e]);
-          w[e + 1] = fast_exp2(w[e + 1]);
-          sum = add_f32x2(sum, pack_f32x2(w[e], w[e + 1]));
-        }
-        unpack_f32x2(sum, l[x][0], l[x][1]);
-        pt[h][x][0] = transpose_8x8(pack_bf16x2(w[0], w[1]));
-        pt[h][x][1] = transpose_8x8(pack_bf16x2(w[2], w[3]));
       }
-    // ---- O^T: lane (n, c) has an eighth of the channels of the keys that are rows 2c, 2c + 1, 2c + 8 and 2c + 9 of S^T
+      // ---- P^T
+      uint32_t pt[H][NT][2];
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
-      constexpr int W = D / 64;
-      const uint8_t* const v = tile + (2 + h) * BLOCK;
-      uint32_t w0[W], w1[W], w2[W], w3[W];
-      auto codes = [&](int at, uint32_t (&w)[W]) {
-        if constexpr (W == 2) {
-          *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(v + at * (D / 2) + 8 * n);
-        } else {
-          w[0] = *reinterpret_cast<const uint32_t*>(v + at * (D / 2) + 4 * n);
+      for (int h = 0; h < H; h++)
+#pragma unroll
+        for (int x = 0; x < NT; x++) {
+          float w[4];
+          const uint64_t no_ref = pack_f32x2(-ref[x][0], -ref[x][1]);
+          uint64_t sum = pack_f32x2(l[x][0], l[x][1]);
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            unpack_f32x2(fma_f32x2(pack_f32x2(s[h][x][e], s[h][x][e + 1]), scale2, no_ref), w[e], w[e + 1]);
+            w[e] = fast_exp2(w[e]);
+            w[e + 1] = fast_exp2(w[e + 1]);
+            sum = add_f32x2(sum, pack_f32x2(w[e], w[e + 1]));
+          }
+          unpack_f32x2(sum, l[x][0], l[x][1]);
+          pt[h][x][0] = transpose_8x8(pack_bf16x2(w[0], w[1]));
+          pt[h][x][1] = transpose_8x8(pack_bf16x2(w[2], w[3]));
         }
-      };
-      codes(key0, w0);
-      codes(key1, w1);
-      codes(key0 + 8, w2);
-      codes(key1 + 8, w3);
-      const uint16_t* const scales = reinterpret_cast<const uint16_t*>(v + q4_scales_at(D)) + n * (D / 8) / kQ4Group;
-      uint32_t s0 = scales[key0 * G], s1 = scales[key1 * G], s2 = scales[(key0 + 8) * G], s3 = scales[(key1 + 8) * G];
-      if (blk * 16 + 32 > k1) {
-        // behind the last token its page may hold anything; P is zero there, and 0 * NaN is not
-        const int left = k1 - (blk + h) * 16;
-        if (key0 >= left) s0 = 0u;
-        if (key1 >= left) s1 = 0u;
-        if (key0 + 8 >= left) s2 = 0u;
-        if (key1 + 8 >= left) s3 = 0u;
-      }
-      s0 |= s1 << 16;
-      s2 |= s3 << 16;
-      const uint32_t o0 = q4_offset(s0), o2 = q4_offset(s2);
+      // ---- O^T: lane (n, c) has an eighth of the channels of the keys that are rows 2c, 2c + 1, 2c + 8 and 2c + 9 of S^T
 #pragma unroll
-      for (int j = 0; j < W; j++) {
-        const uint32_t e0 = __byte_perm(w0[j], w1[j], 0x5410), d0 = __byte_perm(w0[j], w1[j], 0x7632);      // even channels of both keys, odd ones
-        const uint32_t e2 = __byte_perm(w2[j], w3[j], 0x5410), d2 = __byte_perm(w2[j], w3[j], 0x7632);
+      for (int h = 0; h < H; h++) {
+        constexpr int W = D / 64;
+        const uint8_t* const v = tile + (2 + h) * BLOCK;
+        uint32_t w0[W], w1[W], w2[W], w3[W];
+        auto codes = [&](int at, uint32_t (&w)[W]) {
+          if constexpr (W == 2) {
+            *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(v + at * (D / 2) + 8 * n);
+          } else {
+            w[0] = *reinterpret_cast<const uint32_t*>(v + at * (D / 2) + 4 * n);
+          }
+        };
+        codes(key0, w0);
+        codes(key1, w1);
+        codes(key0 + 8, w2);
+        codes(key1 + 8, w3);
+        const uint16_t* const scales = reinterpret_cast<const uint16_t*>(v + q4_scales_at(D)) + n * (D / 8) / kQ4Group;
+        uint32_t s0 = scales[key0 * G], s1 = scales[key1 * G], s2 = scales[(key0 + 8) * G], s3 = scales[(key1 + 8) * G];
+        if (first + 16 * H > k1) {
+          // behind the last token its page may hold anything; P is zero there, and 0 * NaN is not
+          const int left = k1 - first - 16 * h;
+          if (key0 >= left) s0 = 0u;
+          if (key1 >= left) s1 = 0u;
+          if (key0 + 8 >= left) s2 = 0u;
+          if (key1 + 8 >= left) s3 = 0u;
+        }
+        s0 |= s1 << 16;
+        s2 |= s3 << 16;
+        const uint32_t o0 = q4_offset(s0), o2 = q4_offset(s2);
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const uint32_t a0 = q4_pair(e0, i, s0, o0, sixteen), a1 = q4_pair(d0, i, s0, o0, sixteen), a2 = q4_pair(e2, i, s2, o2, sixteen), a3 = q4_pair(d2, i, s2, o2, sixteen);
+        for (int j = 0; j < W; j++) {
+          const uint32_t e0 = __byte_perm(w0[j], w1[j], 0x5410), d0 = __byte_perm(w0[j], w1[j], 0x7632);      // even channels of both keys, odd ones
+          const uint32_t e2 = __byte_perm(w2[j], w3[j], 0x5410), d2 = __byte_perm(w2[j], w3[j], 0x7632);
 #pragma unroll
-          for (int x = 0; x < NT; x++) mma_16816(o[x][4 * j + i], a0, a1, a2, a3, pt[h][x][0], pt[h][x][1]);
+          for (int i = 0; i < 4; i++) {
+            const uint32_t a0 = q4_pair(e0, i, s0, o0, sixteen), a1 = q4_pair(d0, i, s0, o0, sixteen), a2 = q4_pair(e2, i, s2, o2, sixteen), a3 = q4_pair(d2, i, s2, o2, sixteen);
+#pragma unroll
+            for (int x = 0; x < NT; x++) mma_16816(o[x][4 * j + i], a0, a1, a2, a3, pt[h][x][0], pt[h][x][1]);
+          }
         }
       }
     }
@@ -449,9 +458,10 @@ __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const Prefi
 __device__ __forceinline__ void prefix_parts(const PrefixParams& p, const StreamParams& t, int hk, int rho, int& first, int& step, int& n) {
   const PrefixShape& S = p.s;
   if (t.join == kStJoinStream) {
-    step = kStRows;
+    const int tile = t.join_tiles > 1 ? rho >> 4 : 0;
+    step = t.join_rows;
     n = t.join_splits;
-    first = (hk * t.join_tiles + (rho >> 4)) * n * kStRows + (rho & 15);
+    first = (hk * t.join_tiles + tile) * n * step + rho - 16 * tile;
     return;
   }
   const int PT = (S.k0 + 127) >> 7;
@@ -469,7 +479,7 @@ __device__ __forceinline__ void stream_finish(const PrefixParams& p, const Strea
   const PrefixShape& S = p.s;
   float lse2 = L != 0.f ? M + log2f(L) : -INFINITY, inv = L > 0.f || L != L ? 1.0f / L : 0.f;
   if (t.stacked || t.splits > 1) {
-    const int64_t at = t.out0 + (static_cast<int64_t>(item) * t.splits + split) * kStRows + r;
+    const int64_t at = t.out0 + (static_cast<int64_t>(item) * t.splits + split) * t.rows + r;
     *reinterpret_cast<float4*>(p.part_o + at * D + 4 * x) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
     if (x == 0) p.part_lse2[at] = lse2;
     return;
@@ -488,7 +498,7 @@ __device__ __forceinline__ void stream_finish(const PrefixParams& p, const Strea
   if (x == 0 && p.lse != nullptr) p.lse[(static_cast<int64_t>(entry) * S.Hkv * S.G + head) * S.L + i] = lse2 * 0.6931471805599453f;
 }
 
-// NT: products of 8 query rows, 1 or 2.
+// NT: products of 8 query rows, 1 or 2 (of codes up to 3).
 template <int D, int NT, class Source>
 __global__ void __launch_bounds__(kStThreads, stream_ctas(NT, Source::kQ4))
 prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__ PrefixParams p, const StreamParams t) {
@@ -534,7 +544,7 @@ prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__
   const int item = id, tile = t.tiles > 1 ? id % t.tiles : 0;
   if (t.tiles > 1) id /= t.tiles;
   const int hk = id % S.Hkv, entry = id / S.Hkv;
-  const int row0 = tile * kStRows, n_rows = t.stacked ? S.B * S.R : S.R, rows = min(kStRows, n_rows - row0);
+  const int row0 = tile * L_::kRows, n_rows = t.stacked ? S.B * S.R : S.R, rows = min(L_::kRows, n_rows - row0);
   int slot, bad, k0, k1;
   if (t.stacked) {
     int most, who;
@@ -850,10 +860,11 @@ __global__ void __launch_bounds__(kPxMergeThreads) prefix_join_kernel(const __gr
   const int i = S.by_G.div(rr), g = rr - i * S.G;
   PrefixRow row = {};
   if (t.join != 0) prefix_parts(p, t, hk, entry * S.R + rr, row.first, row.step, row.n_first);
-  row.second = t.out0 + (pair * t.tiles + (rr >> 4)) * t.splits * kStRows + (rr & 15);
+  const int tile = t.tiles > 1 ? rr >> 4 : 0;
+  row.second = t.out0 + (pair * t.tiles + tile) * t.splits * t.rows + rr - 16 * tile;
   row.n_second = t.splits;
-  row.next = row.second + kStRows;
-  row.second_step = kStRows;
+  row.next = row.second + t.rows;
+  row.second_step = t.rows;
   const int n = row.n_first + row.n_second, per = (n + GROUPS - 1) / GROUPS, k0 = min(n, group * per);
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   float M = 0.f, L = 0.f;

@@ -340,6 +340,26 @@ def test_attention_ways_of_cutting(B, L, H, Hkv, width, lengths, d):
 
 
 @gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,L,H,Hkv,page,shared,lengths", [
+    (1, 17, 3, 3, 16, 0, (11000,)),                      # parts of three items
+    (2, 6, 12, 3, 16, 0, (1200, 0)),                     # 24 rows of a cluster's CTAs
+    (3, 7, 24, 8, 32, 0, (6, 23, 2049)),
+    (60, 3, 48, 8, 64, 0, tuple(range(1, 1500, 25))),
+    (20, 1, 4, 4, 64, 40, tuple(range(2560, 2580))),     # stacked to 20 rows, or to 24, 22 and 17 in front of own ones of 8, 11 and 17
+    (3, 8, 8, 8, 64, 160, (10240, 10300, 10999)),
+    (2, 11, 2, 2, 128, 600, (76800, 76900)),
+    (1, 17, 8, 8, 64, 160, (10700,)),
+    (9, 20, 8, 8, 128, 0, (10200,) + (300,) * 8)])       # 20 rows of a table with room for many keys
+def test_attention_of_17_to_24_rows(B, L, H, Hkv, page, shared, lengths, d):
+    case = held_case(B, H, Hkv, L, d, page, list(lengths), shared=shared, seed=B + d)
+    for causal in (False, True):
+        first = check(*case, "rows", prefix_pages=shared, causal=causal)
+        again = check(*case, "rows", prefix_pages=shared, causal=causal)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+@gpu
 @pytest.mark.parametrize("L", [1, 40])
 def test_attention_of_chosen_sequences_counts_and_scales(L):
     case, values = held_case(5, 4, 2, L, 64, 16, [140, 177, 0, 230, 116, 99, 164], seed=5)
