@@ -17,13 +17,17 @@ constexpr int kStreamRows = 32;      // query rows of a batch entry and key head
 
 // The same where many keys (of all heads and sequences) are codes: the stream kernel makes each of them bf16 for every item, the tile kernel once for 128 rows, but starts
 // later.  128 channels, us, by either: 17 to 24 rows (one item) 8 x 8 x 2000 14 and 25, 64 x 8 x 700 33 and 47, 16 x 8 x 6000 63 and 59; up to 32 rows (two) 20 and 25, 47 and
-// 48, 83 and 62.
+// 48, 83 and 62; 64 channels, up to 32 rows (one) 12 x 8 x 6000 40 and 37.
 static int stream_rows(bool codes, long long keys) { return !codes || keys <= 512 * 1024 ? kStreamRows : keys <= 704 * 1024 ? 24 : 16; }
 
 constexpr int kWidenTiles = 6;       // row tiles that read a tile of codes, beyond which it is made bf16 once for all of them
 
-// Products of 8 columns for so many query rows: with 8 or less the second one's would be empty; three of codes, which then become bf16 once instead of twice.
-static int stream_products(bool codes, long long rows) { return rows <= 8 ? 1 : codes && rows > 16 && rows <= 24 ? 3 : 2; }
+// Products of 8 columns for so many query rows: with 8 or less the second one's would be empty; three or four of codes, which then become bf16 once instead of twice
+// (as many as there are registers for).
+static int stream_products(bool codes, int d, long long rows) {
+  if (rows <= 16 || !codes || rows > (d == 64 ? 32 : 24)) return rows <= 8 ? 1 : 2;
+  return rows <= 24 ? 3 : 4;
+}
 
 struct PrefixLayout {
   PrefixShape s;
@@ -89,10 +93,10 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     y.pre.stacked = 1;
     y.pre.first = 1;
     y.pre.begin = 1;
-    y.pre.rows = stream_item_rows(stream_products(codes > 0, RS));
+    y.pre.rows = stream_item_rows(stream_products(codes > 0, d, RS));
     y.pre.tiles = static_cast<int>((RS + y.pre.rows - 1) / y.pre.rows);
     y.pre.items = y.pre.tiles * Hkv;
-    const int slots = sms * stream_ctas(stream_products(codes > 0, RS), codes > 0);      // CTAs of the stream kernel that the SMs hold
+    const int slots = sms * stream_ctas(stream_products(codes > 0, d, RS), codes > 0);      // CTAs of the stream kernel that the SMs hold
     const long long by_keys = PT / 2;      // 256 keys a CTA at least: four blocks a warp
     y.pre.splits = static_cast<int>(slots / y.pre.items < by_keys ? slots / y.pre.items : by_keys);
     // The kernel behind joins a row's parts eight at a time, 0.7 us each, so with few heads fewer and longer parts end earlier (4 heads x 60000 keys, us: 111 parts 35.8, 70 31.7).
@@ -109,12 +113,12 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     y.own.join_tiles = y.pre.tiles;
     y.own.join_splits = y.pre.splits;
     y.own.join_rows = y.pre.rows;
-    y.own.rows = stream_item_rows(stream_products(codes > 0, R));
+    y.own.rows = stream_item_rows(stream_products(codes > 0, d, R));
     y.own.tiles = static_cast<int>((R + y.own.rows - 1) / y.own.rows);
     y.own.items = y.own.tiles * Hkv * B;
     y.own.out0 = static_cast<int>(own0);
     const long long keys = static_cast<long long>(width) * page - s.k0;      // at most
-    const int slots = sms * stream_ctas(stream_products(codes > 0, R), codes > 0);
+    const int slots = sms * stream_ctas(stream_products(codes > 0, d, R), codes > 0);
     // An item's keys over a cluster, 64 keys a CTA at least (a block a warp), as many CTAs as the SMs hold side by side: nine tenths of the slots, since a cluster takes its
     // own from one GPC and what does not fit waits for a whole item (us, filled to the last slot and like this: 96 items of 500 keys of 64 channels 14.4 and 9.7, 72
     // of 900 keys of 128 channels 16.4 and 10.3, 144 of 800 17.5 and 13.0).  No CTA has more than 1024 keys while others may have none (30 x 8 items of 1 to 1500
@@ -203,9 +207,11 @@ static int launch_stream_of(const Source& src, const PrefixParams& p, const Stre
 }
 template <int D, class Source>
 static int launch_stream(const Source& src, const PrefixParams& p, const StreamParams& t, int cluster, cudaStream_t st) {
-  const int products = stream_products(Source::kQ4, t.stacked ? static_cast<long long>(p.s.B) * p.s.R : p.s.R);
+  const int products = stream_products(Source::kQ4, D, t.stacked ? static_cast<long long>(p.s.B) * p.s.R : p.s.R);
   if constexpr (Source::kQ4)
     if (products == 3) return launch_stream_of<D, 3>(src, p, t, cluster, st);
+  if constexpr (Source::kQ4 && D == 64)
+    if (products == 4) return launch_stream_of<D, 4>(src, p, t, cluster, st);
   return products == 1 ? launch_stream_of<D, 1>(src, p, t, cluster, st) : launch_stream_of<D, 2>(src, p, t, cluster, st);
 }
 

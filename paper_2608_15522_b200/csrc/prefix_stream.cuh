@@ -23,8 +23,8 @@
 namespace avsa {
 
 constexpr int kStWarps = 4, kStThreads = 32 * kStWarps;
-// Query rows of an item, at most, by its products of 8 columns; where there are three, all rows are one item.
-constexpr int stream_item_rows(int NT) { return NT == 3 ? 24 : 16; }
+// Query rows of an item, at most, by its products of 8 columns; where there are more than two, all rows are one item.
+constexpr int stream_item_rows(int NT) { return NT > 2 ? 8 * NT : 16; }
 
 // What a launch of the kernel below works on.
 struct StreamParams {
@@ -277,14 +277,14 @@ struct CodePairs {
 // maxima looked at by every lane for itself, and brought together only where one has outgrown its reference; sums and exponents two at a time.  (64 x 8 x 2048 keys,
 // 151 MB, us: one block at a time 73, two 60, with the masks' constant in a register 51, and one CTA an item 44; 32 x 8 x 16 rows x 2048 keys, 75 MB, 31.)
 // Three products, 17 to 24 rows, on the same operands instead of two items (us): 64 x 8 x 700 keys 45 and 33, 8 x 8 x 2000 17.4 and 14.5, of 64 channels 12.9 and 10.3; of 128
-// channels one block after the other then.
+// channels one block after the other then.  Four, up to 32 rows of 64 channels: 64 x 8 x 700 32.4 and 25.3, 8 x 8 x 2000 13.0 and 11.6.
 template <int D, int NT, class Smem>
 __device__ __forceinline__ void stream_codes(const PrefixCodes& src, const PrefixParams& p, Smem& sm, const FirstPages<true>& ids, int hk, int blk, int b1, int k1,
                                              int rel_min, const int (&see)[NT][2], const uint4 (&q)[NT][D / 32], float (&o)[NT][D / 16][4], float (&m)[NT][2],
                                              float (&l)[NT][2], int item) {
   constexpr unsigned FULLM = 0xffffffffu;
   constexpr int STAGES = Smem::kStages, BLOCK = Smem::kBlock, G = D / kQ4Group;
-  constexpr int H = NT == 3 && D == 128 ? 1 : 2;      // blocks side by side (registers)
+  constexpr int H = NT * D > 256 ? 1 : 2;      // blocks side by side (registers)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, c = lane & 3;
   const uint32_t sixteen = src.k.sixteen;
   const int step = ids.step;
@@ -498,7 +498,7 @@ __device__ __forceinline__ void stream_finish(const PrefixParams& p, const Strea
   if (x == 0 && p.lse != nullptr) p.lse[(static_cast<int64_t>(entry) * S.Hkv * S.G + head) * S.L + i] = lse2 * 0.6931471805599453f;
 }
 
-// NT: products of 8 query rows, 1 or 2 (of codes up to 3).
+// NT: products of 8 query rows, 1 or 2 (of codes up to 3, or, with 64 channels, 4).
 template <int D, int NT, class Source>
 __global__ void __launch_bounds__(kStThreads, stream_ctas(NT, Source::kQ4))
 prefix_stream_kernel(const __grid_constant__ Source src, const __grid_constant__ PrefixParams p, const StreamParams t) {

@@ -350,8 +350,13 @@ def test_attention_ways_of_cutting(B, L, H, Hkv, width, lengths, d):
     (3, 8, 8, 8, 64, 160, (10240, 10300, 10999)),
     (2, 11, 2, 2, 128, 600, (76800, 76900)),
     (1, 17, 8, 8, 64, 160, (10700,)),
+    (1, 26, 3, 3, 16, 0, (11000,)),
+    (2, 8, 12, 3, 16, 0, (1200, 0)),
+    (60, 1, 108, 4, 64, 0, tuple(range(1, 1500, 25))),
+    (4, 8, 8, 8, 64, 160, (10240, 10300, 10999, 10247)),
+    (28, 1, 4, 4, 64, 40, tuple(range(2560, 2588))),
     (9, 20, 8, 8, 128, 0, (10200,) + (300,) * 8)])       # 20 rows of a table with room for many keys
-def test_attention_of_17_to_24_rows(B, L, H, Hkv, page, shared, lengths, d):
+def test_attention_of_17_to_32_rows(B, L, H, Hkv, page, shared, lengths, d):
     case = held_case(B, H, Hkv, L, d, page, list(lengths), shared=shared, seed=B + d)
     for causal in (False, True):
         first = check(*case, "rows", prefix_pages=shared, causal=causal)
