@@ -80,6 +80,7 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     const int columns = Hkv * s.nrc * ((s.k0 + 127) / 128), most_groups = y.n_cta / s.chunk, by_piece = (columns + kPxMinPiece - 1) / kPxMinPiece;
     const int groups = most_groups < by_piece ? most_groups : by_piece;
     s.cg = (columns + groups - 1) / groups;
+    s.groups = (columns + s.cg - 1) / s.cg;
   }
   // Query rows as a box of a tensor map: (G heads, tokens, batch entries) that are the item's rows in their order.
   if (128 % s.G == 0) s.own_box = 128;

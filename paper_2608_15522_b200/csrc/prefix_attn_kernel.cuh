@@ -94,7 +94,7 @@ struct PrefixShape {
   int rows;            // rows of an own item's partial result: min(128, R)
   int queue;           // whole items off a queue
   int own_off;         // the beginning alone: the own items are another kernel's
-  int cg;              // columns of a group then (as if all sequences had the whole beginning)
+  int cg, groups;      // columns of a group then (as if all sequences had the whole beginning), and groups
   int pre_box, own_box;        // rows of the TMA box that holds the query rows of an item; 0: they are gathered
   int nb_max;          // B pieces at most
   int page, page_shift, pages, seqs, width;
@@ -732,7 +732,31 @@ prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ C
     PrefixPlan P = {};
     int n_pre = 0;
     bool queue = S.queue != 0;
-    {
+    if (S.own_off) {
+      // the beginning alone: cut by sizes alone (a shorter one's last tiles read as zeros, and nobody sees them), so that only the longest sequence is looked for
+      int most = 0, at = 0;
+#pragma unroll 1
+      for (int b0 = lane; b0 < S.B; b0 += 128) {
+        int slot[4], n[4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) slot[u] = b0 + 32 * u >= S.B ? -1 : p.seq != nullptr ? p.seq[b0 + 32 * u] : b0 + 32 * u;
+#pragma unroll
+        for (int u = 0; u < 4; u++) n[u] = slot[u] >= 0 && slot[u] < S.seqs ? p.length[slot[u]] : 0;
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+          const int len = min(n[u], S.width << S.page_shift);
+          if (len > most) most = len, at = slot[u];
+        }
+      }
+      const int top = __reduce_max_sync(FULLM, most);
+      P.donor = __shfl_sync(FULLM, at, __ffs(__ballot_sync(FULLM, most == top)) - 1);
+      P.PE = min(S.k0, top);
+      P.PT = (S.k0 + 127) >> 7;
+      P.cg = S.cg;
+      P.groups = S.groups;
+      P.sB = 1;
+      n_pre = P.groups * S.chunk;
+    } else {
       int most = 0, at = 0, W = 0, tiles = 0;
 #pragma unroll 1
       for (int f0 = 0; f0 < S.F; f0 += 32) {
@@ -753,14 +777,9 @@ prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ C
         P.donor = __shfl_sync(FULLM, at, __ffs(__ballot_sync(FULLM, most == top)) - 1);
         P.PE = min(S.k0, top);
         P.PT = (P.PE + 127) >> 7;
-        if (S.own_off) P.PT = (S.k0 + 127) >> 7;      // (a shorter one's last tiles read as zeros, and nobody sees them)
       }
       const int T = P.W * S.Hkv, columns = S.Hkv * S.nrc * P.PT;
-      if (S.own_off) {
-        P.cg = S.cg;
-        P.groups = float_div(columns + P.cg - 1, P.cg);
-        n_pre = P.groups * S.chunk;
-      } else if (columns > 0) {
+      if (columns > 0) {
         const float share = static_cast<float>(S.Hkv) * S.TP * P.PT;
         // (with a queue rather one more than one less: who is done early takes more off it; 400 queries of
         // 16 sequences behind 30000 tokens, us: the nearest number 2555, the next one 2411; elsewhere within 2 %)
