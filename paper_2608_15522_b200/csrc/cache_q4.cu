@@ -1,7 +1,7 @@
 // A paged cache held in 4 bits: new tokens into the pages, tokens out of them again, and the pages of an attention call as bf16.
 //
 // All three are bound by HBM (2.56 bytes a value, 2 outside and 4.5 bits inside; 49152 tokens of 8 heads of 128 channels read, 258 MB, 41.7 us, 6.2 TB/s; 6018 tokens of 24 heads
-// written, 95 MB, 18.4 us, of which three are the length, the page and the launch before the first token is asked for).  A thread has the 32 channels of a scale, so a group's maximum needs no other thread, and
+// written, 95 MB, 17.9 us, of which three are the length, the page and the launch before the first token is asked for).  A thread has the 32 channels of a scale, so a group's maximum needs no other thread, and
 // its codes are one 16-byte access.  Neighbouring threads have a token's groups, then the tokens of a head: the codes of a warp's eight tokens (128 channels) are
 // 512 contiguous bytes.
 #include "prefix_stream.cuh"
@@ -103,18 +103,22 @@ __global__ void __launch_bounds__(kQ4Threads, 8) tokens_q4_kernel(const __grid_c
   for (int i = threadIdx.x; i < G << (a.token_shift + a.head_shift); i += kQ4Threads) {
     const int group = i % G, r = i / G, t = t0 + (r & ((1 << a.token_shift) - 1)), h = h0 + (r >> a.token_shift);
     if (h >= a.Hkv || t >= a.T) continue;
+    __nv_bfloat16* const k = static_cast<__nv_bfloat16*>(const_cast<void*>(a.k.ptr)) + e * a.k.stride_b + h * a.k.stride_h + t * a.k.stride_n + group * kQ4Group;
+    __nv_bfloat16* const v = static_cast<__nv_bfloat16*>(const_cast<void*>(a.v.ptr)) + e * a.v.stride_b + h * a.v.stride_h + t * a.v.stride_n + group * kQ4Group;
+    uint32_t x[16], y[16];
+    if (!READ && t < count) {      // (asked for beside the page, which hardly a token lacks: 18.4 us behind it)
+      load_group<WIDE>(k, x);
+      load_group<WIDE>(v, y);
+    }
     const long long pos = start + t;
     int page = -1;
     if (t < count && pos >= 0 && (pos >> a.page_shift) < a.width) page = row[pos >> a.page_shift];
     const bool there = page >= 0 && page < a.pages;
     const int in = static_cast<int>(pos & ((1 << a.page_shift) - 1));
-    __nv_bfloat16* const k = static_cast<__nv_bfloat16*>(const_cast<void*>(a.k.ptr)) + e * a.k.stride_b + h * a.k.stride_h + t * a.k.stride_n + group * kQ4Group;
-    __nv_bfloat16* const v = static_cast<__nv_bfloat16*>(const_cast<void*>(a.v.ptr)) + e * a.v.stride_b + h * a.v.stride_h + t * a.v.stride_n + group * kQ4Group;
     uint8_t *k_codes, *v_codes;
     uint16_t *k_scale, *v_scale;
     q4_places<D>(a.k_pool, there ? page : 0, h, in, group, k_codes, k_scale);
     q4_places<D>(a.v_pool, there ? page : 0, h, in, group, v_codes, v_scale);
-    uint32_t x[16], y[16];
     if constexpr (READ) {
       uint4 kc = make_uint4(0u, 0u, 0u, 0u), vc = kc;
       uint32_t ks = 0, vs = 0;
@@ -129,8 +133,6 @@ __global__ void __launch_bounds__(kQ4Threads, 8) tokens_q4_kernel(const __grid_c
       store_group<WIDE>(k, x);
       store_group<WIDE>(v, y);
     } else if (there) {
-      load_group<WIDE>(k, x);
-      load_group<WIDE>(v, y);
       uint32_t ks, vs;
       const uint4 kc = quantise(x, ks), vc = quantise(y, vs);
       *reinterpret_cast<uint4*>(k_codes) = kc;
