@@ -327,7 +327,7 @@ prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ C
     mbar_init(BAR(DONE), 1);
     for (int r = 0; r < L_::kRS; r++) {
       mbar_init(BAR(RAW_FULL + r), 1);
-      mbar_init(BAR(RAW_EMPTY + r), kPxCodeWarps);
+      mbar_init(BAR(RAW_EMPTY + r), 2 * kPxCodeWarps);
     }
     for (int i = kPxStop; i < kPxWords; i++) misc[i] = 0;
     fence_mbar_init();
@@ -614,9 +614,16 @@ prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ C
       const uint32_t raws = smem_u32(smem + L_::kRaws), tiles = smem_u32(smem + (is_k ? L_::kK : L_::kV));
       const int* const there = reinterpret_cast<const int*>(smem + L_::kThere);
       int raw = 0, raw_round = 0, stage = 0, round = 0;
-      auto pass_raw = [&](int n) {      // at most kRS of them
-        raw += n;
-        if (raw >= L_::kRS) raw -= L_::kRS, raw_round ^= 1;
+      auto next_raw = [&]() {
+        if (++raw == L_::kRS) raw = 0, raw_round ^= 1;
+      };
+      // The other kind's codes.  Both kinds of warps wait for every load, in order, and say so before its place is filled again: a wait knows a load by its parity alone, and
+      // who had left out one that was still under way would take its place's next load for there.
+      auto pass_raw = [&]() -> bool {
+        if (!wait_all(RAW_FULL + raw, raw_round, where_full)) return false;
+        if (lane == 0) mbar_arrive(BAR(RAW_EMPTY + raw));
+        next_raw();
+        return true;
       };
 #pragma unroll 1
       for (int n = 0; ok; n++) {
@@ -627,7 +634,7 @@ prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ C
         int left = it.kv_end - it.pos0 - r;                 // the lane has a key of the tile where it is above 0
 #pragma unroll 1
         for (int t = 0; t < it.cnt && ok; t++, left -= 128) {
-          if (!is_k) pass_raw(1);
+          if (!is_k && !(ok = pass_raw())) break;
           if (is_k || kinds == 2) {
             if (round > 0) ok = __all_sync(FULLM, wait_idly(EMPTY + stage, (round - 1) & 1, where_empty));
             if (ok) ok = wait_all(RAW_FULL + raw, raw_round, where_full);
@@ -640,8 +647,9 @@ prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ C
               mbar_arrive(BAR(FULL + stage));
             }
             if (++stage == STAGES) stage = 0, round++;
-            pass_raw(is_k ? kinds : 1);
+            next_raw();
           }
+          if (is_k && kinds == 2) ok = pass_raw();
         }
         if (ok) item_done(n);
       }

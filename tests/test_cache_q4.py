@@ -441,6 +441,23 @@ def test_attention_reproduces_and_ignores_old_memory(B, L, H, Hkv, shared):
 
 
 @gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,L,H,Hkv,page,shared,most", [(4, 64, 64, 8, 128, 3, 1400), (8, 33, 48, 3, 64, 6, 1500), (2, 200, 8, 8, 16, 0, 3000)])
+def test_attention_of_codes_that_land_in_any_order(B, L, H, Hkv, page, shared, most, d):
+    """The tile kernel with nothing in L2: values may be there before the keys in front of them, and the other way round."""
+    draw = random.Random(d + B)
+    flush = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    for seed in range(8):
+        case = held_case(B, H, Hkv, L, d, page, [shared * page + draw.randint(0, most) for _ in range(B)], shared=shared, seed=seed)
+        flush.zero_()
+        first = check(*case, "cold")
+        for _ in range(2):
+            flush.zero_()
+            again = check(*case, "cold again")
+            assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+@gpu
 @pytest.mark.parametrize("L", [1, 33, 400])
 def test_outputs_of_a_call_lie_apart(L):
     """The outputs and the workspace of one call overlap nowhere, begin on 512 bytes, and keep no more memory than they need; q's strides go over to o."""
