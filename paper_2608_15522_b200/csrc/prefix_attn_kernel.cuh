@@ -471,7 +471,7 @@ prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ C
               }
             }
           }
-          if (next < 0 || next > S.pages) {
+          if (e < e1 && (next < 0 || next >= S.pages)) {      // (not where it was read, so that the load is under way during the copies above)
             report(AVSA_ERR_BAD_TABLE, kPrefixPage, it.slot, e);
             next = S.pages;
           }
@@ -537,7 +537,7 @@ prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ C
               round++;
             }
           }
-          if (next < 0 || next > S.pages) {
+          if (e < e1 && (next < 0 || next >= S.pages)) {      // (not where it was read, so that the load is under way during the copies above)
             report(AVSA_ERR_BAD_TABLE, kPrefixPage, it.slot, e);
             next = S.pages;
           }
