@@ -302,7 +302,8 @@ AVSA_API int avsa_build_block_mask_static(int B, int H, int N, int d, int blk, a
  *   k_pool, v_pool  [pages,Hkv,page,d]: stride_b is the distance of pages, stride_h of heads, stride_n of tokens
  *   prefix_pages    the first prefix_pages pages of all sequences of the batch are the same ones (of a shorter
  *                   sequence: all it has).  Where it costs less they are read once for the whole batch, all its queries stacked on
- *                   each other; the longest sequence's row of the table then says which pages they are.  0: nothing is shared.
+ *                   each other; the longest sequence's row of the table (of several the first batch entry's) then says which pages they are.  0: nothing is
+ *                   shared.
  *
  * What pages hold behind the last token of the longest sequence that has them is never used (it may be anything, NaN too).  Values of tokens that some rows
  * of a call see and others must not have to be finite (their weight is 0, and 0 times an infinity is no number): those behind a causal row's limit, and those in

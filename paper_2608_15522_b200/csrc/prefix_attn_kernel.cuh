@@ -198,6 +198,16 @@ __device__ __forceinline__ int prefix_own_tiles(const PrefixParams& p, int b, in
   return s.stack ? t : max(t, 1);      // (without a beginning of its own every row tile is written by somebody)
 }
 
+// The longest sequence of the batch, of several the one of the first batch entry: its row of the page table names the shared pages, so whoever asks has to find the same one.
+// A warp, a candidate a lane: its tokens, batch entry (of those that the lane has seen with so many the first) and row of the table.
+__device__ __forceinline__ int first_longest(int most, int& entry, int& slot) {
+  const int top = __reduce_max_sync(0xffffffffu, most);
+  const int first = __reduce_min_sync(0xffffffffu, most == top ? entry : 0x7fffffff);
+  slot = __shfl_sync(0xffffffffu, slot, __ffs(__ballot_sync(0xffffffffu, most == top && entry == first)) - 1);
+  entry = first;
+  return top;
+}
+
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)) : "memory");
 }
@@ -742,7 +752,7 @@ prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ C
     bool queue = S.queue != 0;
     if (S.own_off) {
       // the beginning alone: cut by sizes alone (a shorter one's last tiles read as zeros, and nobody sees them), so that only the longest sequence is looked for
-      int most = 0, at = 0;
+      int most = 0, who = 0;
 #pragma unroll 1
       for (int b0 = lane; b0 < S.B; b0 += 128) {
         int slot[4], n[4];
@@ -753,19 +763,17 @@ prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ C
 #pragma unroll
         for (int u = 0; u < 4; u++) {
           const int len = min(n[u], S.width << S.page_shift);
-          if (len > most) most = len, at = slot[u];
+          if (len > most) most = len, who = b0 + 32 * u, P.donor = slot[u];
         }
       }
-      const int top = __reduce_max_sync(FULLM, most);
-      P.donor = __shfl_sync(FULLM, at, __ffs(__ballot_sync(FULLM, most == top)) - 1);
-      P.PE = min(S.k0, top);
+      P.PE = min(S.k0, first_longest(most, who, P.donor));
       P.PT = (S.k0 + 127) >> 7;
       P.cg = S.cg;
       P.groups = S.groups;
       P.sB = 1;
       n_pre = P.groups * S.chunk;
     } else {
-      int most = 0, at = 0, W = 0, tiles = 0;
+      int most = 0, who = 0, W = 0, tiles = 0;
 #pragma unroll 1
       for (int f0 = 0; f0 < S.F; f0 += 32) {
         int nt, len, slot;
@@ -773,7 +781,7 @@ prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ C
         if (f0 == 0) nt0 = nt, len0 = len, slot0 = slot;
         W += units(nt);
         tiles += nt;
-        if (len > most) most = len, at = slot;
+        if (len > most) most = len, who = S.by_TO.div(f0 + lane), P.donor = slot;
       }
       P.W = __reduce_add_sync(FULLM, W);
       // keys and values that stay in L2 need no CTAs that work on the same ones (us, with them and without: the sequences of kPxItemUnits, 64 MB at most, 126 and 82;
@@ -781,9 +789,7 @@ prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ C
       const float bytes = static_cast<float>(__reduce_add_sync(FULLM, tiles)) * S.Hkv * (128.f * D * 4.f);
       queue = queue && bytes > static_cast<float>(kL2KeepBytes) * S.TO;
       if (S.stack) {
-        const int top = __reduce_max_sync(FULLM, most);
-        P.donor = __shfl_sync(FULLM, at, __ffs(__ballot_sync(FULLM, most == top)) - 1);
-        P.PE = min(S.k0, top);
+        P.PE = min(S.k0, first_longest(most, who, P.donor));
         P.PT = (P.PE + 127) >> 7;
       }
       const int T = P.W * S.Hkv, columns = S.Hkv * S.nrc * P.PT;

@@ -75,19 +75,16 @@ __device__ __forceinline__ uint32_t stream_cluster_size() {
   return r;
 }
 
-// The longest sequence of the batch: its row of the page table names the shared pages.  A warp.
+// The longest sequence of the batch.  A warp.
 __device__ __forceinline__ void longest_sequence(const PrefixParams& p, int& slot, int& tokens, int& entry) {
-  const int lane = threadIdx.x & 31;
-  int top = 0, at = 0, who = 0;
-  for (int b = lane; b < p.s.B; b += 32) {
+  int top = 0;
+  slot = entry = 0;
+  for (int b = threadIdx.x & 31; b < p.s.B; b += 32) {
     int s, bad;
     const int len = prefix_sequence(p, b, s, bad);
-    if (len > top) top = len, at = s, who = b;
+    if (len > top) top = len, slot = s, entry = b;
   }
-  tokens = __reduce_max_sync(0xffffffffu, top);
-  const int from = __ffs(__ballot_sync(0xffffffffu, top == tokens)) - 1;
-  slot = __shfl_sync(0xffffffffu, at, from);
-  entry = __shfl_sync(0xffffffffu, who, from);
+  tokens = first_longest(top, entry, slot);
 }
 
 // The call's status: what is out of range in the sequences of the batch, else the first error of a CTA of the tile kernel in front (`wait`: nothing has waited for it

@@ -45,3 +45,42 @@ def test_the_first_page_number_out_of_range(way, B, L, Hkv):
             x[table[row, at]] = old
         assert torch.equal(o, want), at
         assert torch.equal(o[:row], good[:row])
+
+
+@gpu
+@pytest.mark.parametrize("way", ["bf16", "codes"])
+@pytest.mark.parametrize("L,Hkv", [(40, 1), (1, 4)])
+def test_of_equally_long_sequences_the_first_names_the_shared_pages(L, Hkv, way):
+    """The longest sequence's row says which pages are shared; of several the first one's, for everything that the call does.
+
+    Rows that differ are malformed.  What the first one lacks reads as zeros and is reported, whatever the workspace held; what another one lacks is not looked at.
+    With forty queries the pages of codes are made bf16 before the products, and a sequence has two row tiles."""
+    B, group, page, shared = 20, 4, 16, 1024
+    lengths = [shared * page + (90 if b in (1, 16, 19) else 1 + 3 * b) for b in range(B)]
+    q, k, v, table, length = attention_case(B, group * Hkv, Hkv, L, 64, page, lengths, shared=shared, seed=2, poison=False)
+    call, query = av.avsa_prefix_attn, av.avsa_prefix_attn_workspace_bytes(B, group * Hkv, Hkv, L, 64, page, table.shape[1], shared)
+    if way == "codes":
+        (k, _), (v, _) = held(k), held(v)
+        call, query = av.avsa_prefix_attn_q4, av.avsa_prefix_attn_q4_workspace_bytes(B, group * Hkv, Hkv, L, 64, page, k.shape[0], table.shape[1], shared)
+    n = cu(length)
+
+    def run(t, k=k, v=v):
+        ws = torch.full((query,), 255, dtype=torch.uint8, device="cuda")      # (as bf16 or fp32: NaN)
+        o, lse, _ = call(q, k, v, cu(t), n, prefix_pages=shared, want_lse=True, ws=ws)
+        return o, lse, status(ws)
+
+    good = run(table)
+    assert good[2] == av.AVSA_OK and torch.isfinite(good[0].float()).all()
+    for at in (5, 700):
+        bad = table.copy()
+        bad[16, at] = -1 if at == 5 else k.shape[0]
+        o, lse, st = run(bad)
+        assert st == av.AVSA_OK and torch.equal(o, good[0]) and torch.equal(lse, good[1])
+        bad = table.copy()
+        bad[1, at] = -1 if at == 5 else k.shape[0]
+        o, lse, st = run(bad)
+        zero = [x.clone() for x in (k, v)]
+        for x in zero:
+            x[table[1, at]] = 0
+        want = run(table, *zero)
+        assert st == av.AVSA_ERR_BAD_TABLE and torch.equal(o, want[0]) and torch.equal(lse, want[1])
