@@ -374,8 +374,9 @@ AVSA_API size_t avsa_cache_workspace_bytes(int seqs, int pages, int n);
  * avsa_cache_read_q4  the last count[k] tokens of sequence seq[k] (count NULL: T of them) become the first count[k] (0..T) tokens of k and v [n,Hkv,T,d], exactly.
  *                     Tokens that there are not (behind count[k], in front of the sequence's first, without a page) are zeros.
  * avsa_prefix_attn_q4 attention on the values that the pages stand for.  Where many query rows read the same keys (more than 6 x 128 of a sequence and key head, or
- *                     stacked ones) the pages that the batch reads are first made bf16 in the workspace, which then has room for a layer's
- *                     (2 * pages * Hkv * page * d of bf16); it may be the same one for all layers.
+ *                     stacked ones) the pages that the batch reads are first made bf16 in the workspace, which then has room for these: as many as the
+ *                     rows can name, N = prefix_pages + B * (width - prefix_pages), or all that the pool has where these are fewer (2 * Hkv * page * d of bf16 each).
+ *                     The query's answer grows with its `pages`; a call needs no more than for min(pages, N) of them.  It may be the same workspace for all layers.
  *
  * Neither a write nor a read needs a workspace or leaves a status.
  */

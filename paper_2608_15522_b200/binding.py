@@ -597,6 +597,7 @@ def avsa_cache_read_q4(k_pool, v_pool, table, length, tokens, seq=None, count=No
 
 
 def avsa_prefix_attn_q4_workspace_bytes(B, H, Hkv, L, d, page, pages, width, prefix_pages) -> int:
+    """Of a pool with more pages than the rows of the batch can name, ask with that number, prefix_pages + B * (width - prefix_pages): the call needs no more."""
     return int(load_library().avsa_prefix_attn_q4_workspace_bytes(B, H, Hkv, L, d, page, pages, width, prefix_pages))
 
 

@@ -144,8 +144,9 @@ __global__ void __launch_bounds__(kQ4Threads, 8) tokens_q4_kernel(const __grid_c
 }
 
 // The pages that the batch of an attention call reads, as bf16: those of batch entry `entry` behind the shared ones, or, of the entry behind the last one, the beginning, as
-// the longest sequence's row of the table has it.  Entries whose neighbour in front has the same page at the same place leave it to that one (branches of one
-// parent; of others that share a page several write the same values).  2.56 bytes a value, and the copy is read from L2 or HBM once more by the tile kernel.
+// the longest sequence's row of the table has it.  Laid out by page numbers, entries whose neighbour in front has the same page at the same place leave it to that one (branches of
+// one parent; of others that share a page several write the same values); by places, each entry has its own, and what the beginning lacks is zeros (the tile kernel goes by
+// the rows of its items).  2.56 bytes a value, and the copy is read from L2 or HBM once more by the tile kernel.
 template <int D>
 __global__ void __launch_bounds__(kQ4Threads) widen_pages_kernel(const __grid_constant__ PrefixParams p, Q4Pool k4, Q4Pool v4, __nv_bfloat16* k, __nv_bfloat16* v,
                                                                  int chunks, int first) {
@@ -153,11 +154,13 @@ __global__ void __launch_bounds__(kQ4Threads) widen_pages_kernel(const __grid_co
   pdl_launch();
   constexpr int G = D / kQ4Group, GS = G == 4 ? 2 : 1;
   const PrefixShape& S = p.s;
-  const int entry = blockIdx.x / chunks, chunk = blockIdx.x - entry * chunks, b = first + entry, h = blockIdx.y, shared = S.k0 >> S.page_shift;
+  const int entry = blockIdx.x / chunks, chunk = blockIdx.x - entry * chunks, b = first + entry, h = blockIdx.y;
+  const bool by_place = S.places > 0;
+  const int shared = by_place || S.stack ? S.shared : 0;
   int slot, bad, e0 = shared, e1 = 0, before = -1, before_e1 = 0;
   if (b < S.B) {
     e1 = (prefix_sequence(p, b, slot, bad) + S.page - 1) >> S.page_shift;
-    if (b > 0) before_e1 = (prefix_sequence(p, b - 1, before, bad) + S.page - 1) >> S.page_shift;
+    if (b > 0 && !by_place) before_e1 = (prefix_sequence(p, b - 1, before, bad) + S.page - 1) >> S.page_shift;
   } else {
     int tokens, who;
     longest_sequence(p, slot, tokens, who);
@@ -169,15 +172,17 @@ __global__ void __launch_bounds__(kQ4Threads) widen_pages_kernel(const __grid_co
   for (long long u = static_cast<long long>(chunk) * kQ4Threads + threadIdx.x; u < n; u += static_cast<long long>(chunks) * kQ4Threads) {
     const int e = e0 + static_cast<int>(u >> shift), i = static_cast<int>(u & ((1 << shift) - 1)), in = i / G, group = i % G;
     const int page = p.table[static_cast<int64_t>(slot) * S.width + e];
-    if (page < 0 || page >= S.pages) continue;
+    const bool there = page >= 0 && page < S.pages;
+    if (!there && !by_place) continue;
     if (e < before_e1 && p.table[static_cast<int64_t>(before) * S.width + e] == page) continue;
     uint8_t *k_codes, *v_codes;
     uint16_t *k_scale, *v_scale;
-    q4_places<D>(k4, page, h, in, group, k_codes, k_scale);
-    q4_places<D>(v4, page, h, in, group, v_codes, v_scale);
+    q4_places<D>(k4, there ? page : 0, h, in, group, k_codes, k_scale);
+    q4_places<D>(v4, there ? page : 0, h, in, group, v_codes, v_scale);
     const uint4 kc = *reinterpret_cast<const uint4*>(k_codes), vc = *reinterpret_cast<const uint4*>(v_codes);
-    const uint32_t ks = *k_scale, vs = *v_scale;
-    const int64_t to = ((static_cast<int64_t>(page) * S.Hkv + h) * S.page + in) * D + group * kQ4Group;
+    const uint32_t ks = there ? *k_scale : 0u, vs = there ? *v_scale : 0u;
+    const int64_t at = by_place ? prefix_place(S, e, b < S.B ? b : 0) : page;
+    const int64_t to = ((at * S.Hkv + h) * S.page + in) * D + group * kQ4Group;
     uint32_t x[16];
     widen(kc, ks, k4.sixteen, x);
     store_group<true>(k + to, x);
@@ -189,9 +194,10 @@ __global__ void __launch_bounds__(kQ4Threads) widen_pages_kernel(const __grid_co
 int launch_widen(const PrefixParams& p, Q4Pool k4, Q4Pool v4, void* k, void* v, bool own, int d, cudaStream_t st) {
   const PrefixShape& s = p.s;
   const int first = own ? 0 : s.B;
-  const long long entries = static_cast<long long>(s.B) - first + (s.stack ? 1 : 0);
+  const long long entries = static_cast<long long>(s.B) - first + (s.stack || (s.places > 0 && s.shared > 0) ? 1 : 0);
   const long long most = static_cast<long long>(s.width) * s.page * (d / kQ4Group) / kQ4Threads + 1;      // CTAs that the longest row could use
-  long long chunks = persistent_grid(1 << 30) * 16ll / (entries * s.Hkv) + 1;
+  // As many CTAs to an entry whatever it has: a beginning is most of all pages, so four times what the SMs hold (a frame of 4 candidates by places, us: 16 CTAs an SM 1067, 32 1054, 64 1049).
+  long long chunks = persistent_grid(1 << 30) * 64ll / (entries * s.Hkv) + 1;
   if (chunks > most) chunks = most;
   const dim3 grid(static_cast<unsigned>(chunks * entries), static_cast<unsigned>(s.Hkv));
   auto kernel = d == 128 ? widen_pages_kernel<128> : widen_pages_kernel<64>;

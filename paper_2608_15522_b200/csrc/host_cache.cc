@@ -333,8 +333,12 @@ PyObject* attn(PyObject* const* a, Py_ssize_t n) {
     Outputs made(c);
     made.add(o);
     if (want_lse) made.add(lse, at::kFloat, {B, H, L});
-    if (!ws.there())
-      made.add_ws(ws, Q4 ? f_attn_q4_ws(B, H, Hkv, L, d, page, pages, width, prefix_pages) : f_attn_ws(B, H, Hkv, L, d, page, width, prefix_pages));
+    if (!ws.there()) {
+      // (of a larger pool the call reads no more pages than its rows can name)
+      int64_t named = pages;
+      if (prefix_pages >= 0 && prefix_pages <= width) named = std::min<int64_t>(named, prefix_pages + (static_cast<int64_t>(width) - prefix_pages) * B);
+      made.add_ws(ws, Q4 ? f_attn_q4_ws(B, H, Hkv, L, d, page, static_cast<int>(named), width, prefix_pages) : f_attn_ws(B, H, Hkv, L, d, page, width, prefix_pages));
+    }
     made.allocate();
     if constexpr (Q4)
       st = f_attn_q4(B, H, Hkv, L, d, page, pages, seqs, width, q, k4, v4, table.as<int32_t>(), length.as<int32_t>(), seq.as<int32_t>(),

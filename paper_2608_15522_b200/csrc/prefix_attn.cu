@@ -40,6 +40,7 @@ struct PrefixLayout {
   int own_row0, cut_row0;
   size_t plan, cta_err, own_rec, cut_rec, redo, lse, o, wide, total;       // offsets in the workspace
   size_t wide_pool;             // bytes of the keys as bf16, and of the values, where pages of codes become that before the tile kernel; else 0
+  size_t room;                  // what the query says: of a call that names as many pages as the pool has
 };
 
 // False: more units, or key positions rounded up to a tile, than 32 bits count.  `codes`: pages of a pool held in 4 bits, or 0.
@@ -59,6 +60,8 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   s.rows = R < 128 ? s.R : 128;
   s.causal = causal;
   s.page = page;
+  s.width = width;
+  s.shared = prefix_pages;
   s.page_shift = page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7;
   const int sms = persistent_grid(1 << 30);
   // Stacked, the beginning's key tiles are walked TP times a head instead of F times, but every row goes through the merge, which costs a key
@@ -175,14 +178,20 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   y.o = at;
   y.total = at + y.rows * d * 4;
   y.wide = y.wide_pool = 0;
+  y.room = y.total;
   // Pages of codes become tiles in the tile kernel, or, where a key tile meets many row tiles (each of which would do it again), bf16 pages in the workspace first.
   // 2 x 16 heads x 12000 keys of 128 channels, us, in the kernel and before it, by row tiles: two 76 and 130, four 134 and 188, five 157 and 162, six 182 and 181, eight 250
   // and 217, twelve 365 and 292 (of 64 channels: six 140 and 147, eight 194 and 191); 12800 shared ones: two 54 and 72, six 125 and 124, twelve 240 and 207.
   const long long own = y.own_stream ? 0 : s.stack ? most - PT : most, shared = s.stack ? PT : 0;
   if (codes > 0 && y.tile && TP * shared + F * own > kWidenTiles * (shared + B * own)) {
+    // Room for the pages that the rows can name, which is what the copy is laid out by where the pool has more.
+    const long long named = prefix_pages + (y.own_stream ? 0ll : (static_cast<long long>(width) - prefix_pages) * B);
+    const size_t bytes = static_cast<size_t>(Hkv) * page * d * 2;
+    if (named < codes) s.places = static_cast<int>(named);
     y.wide = align_up(y.total, 256);
-    y.wide_pool = static_cast<size_t>(codes) * Hkv * page * d * 2;      // (below 2^62)
+    y.wide_pool = (s.places > 0 ? s.places : codes) * bytes;      // (below 2^62)
     y.total = y.wide + 2 * y.wide_pool;
+    y.room = y.own_stream ? y.total : y.wide + 2 * (codes * bytes);
   }
   return true;
 }
@@ -271,9 +280,9 @@ static int launch_kernels(const PrefixLayout& y, const Source& src, const TileSo
 
 // Tensor maps of a bf16 pool, `rows` keys each.
 template <int D>
-static bool encode_tiles(PrefixTiles& t, const PrefixShape& s, const avsa_bf16_4d& k, const avsa_bf16_4d& v, int rows) {
-  return encode_bf16_tile_map(&t.k, k.ptr, s.pages, s.Hkv, s.page, D, k.stride_b, k.stride_h, k.stride_n, rows) &&
-         encode_bf16_tile_map(&t.v, v.ptr, s.pages, s.Hkv, s.page, D, v.stride_b, v.stride_h, v.stride_n, rows);
+static bool encode_tiles(PrefixTiles& t, const PrefixShape& s, int pages, const avsa_bf16_4d& k, const avsa_bf16_4d& v, int rows) {
+  return encode_bf16_tile_map(&t.k, k.ptr, pages, s.Hkv, s.page, D, k.stride_b, k.stride_h, k.stride_n, rows) &&
+         encode_bf16_tile_map(&t.v, v.ptr, pages, s.Hkv, s.page, D, v.stride_b, v.stride_h, v.stride_n, rows);
 }
 
 template <int D>
@@ -285,12 +294,12 @@ static int launch_prefix(const PrefixLayout& y, const PrefixPools& pools, const 
     avsa_bf16_4d k = {ws + y.wide, static_cast<int64_t>(s.Hkv) * s.page * D, static_cast<int64_t>(s.page) * D, D}, v = k;
     v.ptr = ws + y.wide + y.wide_pool;
     PrefixTiles wide;
-    if (!encode_tiles<D>(wide, s, k, v, s.page)) return AVSA_ERR_CUDA;
+    if (!encode_tiles<D>(wide, s, s.places > 0 ? s.places : s.pages, k, v, s.page)) return AVSA_ERR_CUDA;
     const int r = launch_widen(p, src.k, src.v, ws + y.wide, ws + y.wide + y.wide_pool, !y.own_stream, D, st);
     return r != AVSA_OK ? r : launch_kernels<D>(y, src, wide, p, st);
   }
   PrefixTiles few = {}, tiles = {};
-  if ((y.own_stream && !encode_tiles<D>(few, s, pools.k, pools.v, 16)) || (y.tile && !encode_tiles<D>(tiles, s, pools.k, pools.v, s.page))) return AVSA_ERR_CUDA;
+  if ((y.own_stream && !encode_tiles<D>(few, s, s.pages, pools.k, pools.v, 16)) || (y.tile && !encode_tiles<D>(tiles, s, s.pages, pools.k, pools.v, s.page))) return AVSA_ERR_CUDA;
   return launch_kernels<D>(y, few, tiles, p, st);
 }
 
@@ -317,7 +326,7 @@ extern "C" size_t avsa_prefix_attn_workspace_bytes(int B, int H, int Hkv, int L,
 extern "C" size_t avsa_prefix_attn_q4_workspace_bytes(int B, int H, int Hkv, int L, int d, int page, int pages, int width, int prefix_pages) {
   PrefixLayout y;
   if (pages <= 0 || !prefix_sizes_ok(B, H, Hkv, L, d, page, width, prefix_pages) || !prefix_layout(B, H, Hkv, L, d, page, width, prefix_pages, 0, pages, y)) return 0;
-  return y.total;
+  return y.room;
 }
 
 static int prefix_attn(int B, int H, int Hkv, int L, int d, int page, int pages, int seqs, int width, avsa_bf16_4d q, const PrefixPools& pools, const int32_t* table,
@@ -347,7 +356,6 @@ static int prefix_attn(int B, int H, int Hkv, int L, int d, int page, int pages,
   uint8_t* w = static_cast<uint8_t*>(ws);
   y.s.pages = pages;
   y.s.seqs = seqs;
-  y.s.width = width;
   PrefixParams p = {};
   p.s = y.s;
   p.q = q;

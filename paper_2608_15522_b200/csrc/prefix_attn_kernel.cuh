@@ -98,6 +98,8 @@ struct PrefixShape {
   int pre_box, own_box;        // rows of the TMA box that holds the query rows of an item; 0: they are gathered
   int nb_max;          // B pieces at most
   int page, page_shift, pages, seqs, width;
+  int shared;          // pages that all sequences begin with
+  int places;          // pages of a bf16 copy that is laid out by places of the rows (prefix_place), or 0: whatever is read is laid out by page numbers
   int causal;
   Divisor by_R, by_G, by_TO, by_F, by_chunk, by_nrc, by_cg;
 };
@@ -197,6 +199,9 @@ __device__ __forceinline__ int prefix_own_tiles(const PrefixParams& p, int b, in
   const int t = x > 0 ? (x + 127) >> 7 : 0;
   return s.stack ? t : max(t, 1);      // (without a beginning of its own every row tile is written by somebody)
 }
+
+// Where a copy of the pages that a call reads has the one at place e of batch entry b's row: the shared ones once, then each entry's own.
+__device__ __forceinline__ int prefix_place(const PrefixShape& s, int e, int b) { return e < s.shared ? e : e + b * (s.width - s.shared); }
 
 // The longest sequence of the batch, of several the one of the first batch entry: its row of the page table names the shared pages, so whoever asks has to find the same one.
 // A warp, a candidate a lane: its tokens, batch entry (of those that the lane has seen with so many the first) and row of the table.
@@ -547,9 +552,13 @@ prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ C
               round++;
             }
           }
-          if (e < e1 && (next < 0 || next >= S.pages)) {      // (not where it was read, so that the load is under way during the copies above)
-            report(AVSA_ERR_BAD_TABLE, kPrefixPage, it.slot, e);
-            next = S.pages;
+          if (e < e1) {      // (not where it was read, so that the load is under way during the copies above)
+            if (next < 0 || next >= S.pages) {
+              report(AVSA_ERR_BAD_TABLE, kPrefixPage, it.slot, e);
+              next = S.pages;
+            } else if (S.places > 0) {
+              next = prefix_place(S, e, it.b);
+            }
           }
           mine = next;
         }
@@ -693,6 +702,8 @@ prefix_attn_kernel(const __grid_constant__ Source src, const __grid_constant__ C
         if (page < 0 || page >= S.pages) {
           report(AVSA_ERR_BAD_TABLE, kPrefixPage, it.slot, e);
           page = S.pages;
+        } else if (!Q4 && S.places > 0) {
+          page = prefix_place(S, e, it.b);
         }
       }
       if (m >= kPxRing && !wait_all(ITEM_EMPTY + slot, ((m / kPxRing) - 1) & 1, kPxItemEmpty)) return false;

@@ -61,7 +61,8 @@ inline bool q4_pool_ok(const avsa_q4_pool& p, int pages, int Hkv, int page, int 
   return true;
 }
 
-// The pages that the batch of an attention call reads (`own`: not only the beginning's), as bf16: page p of head h at ((p*Hkv + h)*page)*d of `k` and `v`.
+// The pages that the batch of an attention call reads (`own`: not only the beginning's), as bf16: of head h at ((p*Hkv + h)*page)*d of `k` and `v`, with p the page's number or
+// (with p.s.places) its place.
 struct PrefixParams;
 int launch_widen(const PrefixParams& p, Q4Pool k4, Q4Pool v4, void* k, void* v, bool own, int d, cudaStream_t st);
 
