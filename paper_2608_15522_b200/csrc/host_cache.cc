@@ -172,8 +172,8 @@ void same_pools(const PoolQ4& k, const PoolQ4& v) {
 }
 
 // What a call allocates: its outputs are parts of one allocation, each at a multiple of 512 bytes, since an allocation takes 0.8 us of a call's 5 to 8 on the host.
-// Above 16 MB the device takes longer than that, and each is its own, so that who keeps one output does not keep the others' memory; for the same reason a
-// workspace is among them only up to 64 KB.  (Measured, us of host time apart and together: attention of one token 7.65 and 6.2, read of two short sequences 6.5
+// Who keeps one of them keeps the memory of all, so this is done up to 2 MB only, what the caching allocator takes from the device for small tensors, of which any one keeps all
+// as well; a workspace is among them up to 64 KB.  (Measured, us of host time apart and together: attention of one token 7.65 and 6.2, read of two short sequences 6.5
 // and 5.6.)
 class Outputs {
  public:
@@ -218,7 +218,7 @@ class Outputs {
   }
 
  private:
-  static constexpr int64_t kTogether = 16 << 20;
+  static constexpr int64_t kTogether = 2 << 20;
   static constexpr size_t kWorkspaceWithin = 64 << 10;
   struct Wanted {
     Arg* out;

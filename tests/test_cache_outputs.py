@@ -1,0 +1,29 @@
+"""What a call's outputs keep alive."""
+import pytest
+import torch
+
+from paper_2608_15522_b200 import binding as av
+from test_paged_cache import attention_case, cu
+
+gpu = pytest.mark.gpu
+
+MOST = 2 << 20      # what the outputs of one call may share
+
+
+@gpu
+@pytest.mark.parametrize("L", [1, 200, 700])
+def test_one_output_keeps_little_of_the_others(L):
+    """Outputs of a call share memory only where all of it is little: who keeps one keeps 2 MB more at most."""
+    q, k, v, table, length = attention_case(2, 16, 4, L, 128, 64, [900, 800], seed=1)
+    for o in av.avsa_prefix_attn(q, k, v, cu(table), cu(length), want_lse=True):
+        assert o.untyped_storage().nbytes() <= max(MOST, o.numel() * o.element_size() + 512)
+
+
+@gpu
+@pytest.mark.parametrize("N", [1, 333, 1009])
+def test_keys_that_are_kept_do_not_keep_the_queries(N):
+    q, k = torch.randn((1, 32, N, 128), device="cuda").bfloat16(), torch.randn((1, 8, N, 128), device="cuda").bfloat16()
+    sections = (22, 21, 21)
+    pos = torch.arange(3 * N, dtype=torch.int32, device="cuda").view(N, 3)
+    for x in av.avsa_rope(q, k, pos, av.avsa_rope_frequencies(sections), sections):
+        assert x.untyped_storage().nbytes() <= max(MOST, x.numel() * x.element_size() + 512)
