@@ -15,9 +15,15 @@ constexpr int kChunk = 8;        // row tiles that go through the beginning side
 
 constexpr int kStreamRows = 32;      // query rows of a batch entry and key head that the stream kernel takes, at most; of the stacked rows as well
 
-// The same where many keys (of all heads and sequences) are codes: the stream kernel makes each of them bf16 for every item, the tile kernel once for 128 rows, but starts
-// later.  128 channels, us, by either: 17 to 24 rows (one item) 8 x 8 x 2000 14 and 25, 64 x 8 x 700 33 and 47, 16 x 8 x 6000 63 and 59; up to 32 rows (two) 20 and 25, 47 and
-// 48, 83 and 62; 64 channels, up to 32 rows (one) 12 x 8 x 6000 40 and 37.
+// The same of codes, by the keys of all heads and sequences that the table has room for: the stream kernel makes each of them bf16 for every item, the tile kernel once for 128
+// rows, but starts later, and does not mind room that no sequence uses.  us, stream and tile kernel, sequences x heads x keys:
+//                              8 x 8 x 2000   64 x 8 x 800   12 x 8 x 6000   16 x 8 x 6000   64 x 24 x 600
+//   128 channels, 20 rows         15, 26         37, 58          63, 58          84, 74         87, 114      one item
+//                 30 rows         18, 27         57, 59          96, 59          91, 74        129, 114      two
+//    64 channels, 20 rows         10, 21         25, 47          44, 45          57, 55         59, 93       one
+//                 30 rows         12, 21         29, 48          48, 45          61, 56         68, 93       one
+// and with room for 16384 keys, 64 x 8 x 700, 128 channels: 20 rows 127, 53; 30 rows 214, 54.  A sum of keys tells few long sequences from many short ones no better than
+// this: 64 x 24 x 600 go to the slower one, and of two items 4 x 8 x 8000 (48, 33).
 static int stream_rows(bool codes, long long keys) { return !codes || keys <= 512 * 1024 ? kStreamRows : keys <= 704 * 1024 ? 24 : 16; }
 
 constexpr int kWidenTiles = 6;       // row tiles that read a tile of codes, beyond which it is made bf16 once for all of them
@@ -130,9 +136,14 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
     const long long fit = slots * 9ll / 10 / (y.own.items + 1ll), by_keys = keys / 64;
     long long ctas = fit < by_keys ? fit : by_keys;
     ctas = ctas < 1 ? 1 : ctas > 8 ? 8 : ctas;
-    // (Codes: no second CTA for items that fill three quarters of the slots by themselves and whose start and end weigh more, being half as long or, with 16 rows, twice as
-    // many. us, 1024 and 2048 keys a CTA: 64 channels, 64 x 8 items of 2048 keys 30 and 27, of 1000 to 2048 27 and 25, of up to 2048 23 and 23; 128 channels and 16 rows, 32 x 8
-    // of 2048 keys 36 and 31, of up to 6000 85 and 65; but one product, 64 x 8 of 2048 keys 44 and 42, of 100 to 2048 34 and 36, 20 x 24 of up to 2000 32 and 36.)
+    // (Codes: no second CTA up to 2048 keys for items that fill three quarters of the slots by themselves and whose start and end weigh more, being half as long or, with
+    // 16 rows, twice as many.  us, 1024 and 2048 keys a CTA, sequences x heads of so many keys:
+    //                            64 x 8 of 2048   1000 to 2048   100 to 2048   20 x 24 of 1 to 2000
+    //   64 channels, one row        27, 26           26, 25         23, 23           22, 22
+    //                16 rows        49, 40           43, 36         36, 32           34, 31
+    //   128 channels, 16 rows       69, 58           61, 52         49, 45           47, 44
+    //                 one row       44, 42           39, 39         32, 36           30, 34      (not taken)
+    // )
     const bool short_items = codes > 0 && (d == 64 || R > 8) && 4ll * y.own.items >= 3ll * slots;
     const long long most_keys = short_items ? 2048 : 1024;
     while (ctas < 8 && y.own.items < (1 << 27) && keys > most_keys * ctas) ctas = 2 * ctas < 8 ? 2 * ctas : 8;
@@ -180,8 +191,12 @@ static bool prefix_layout(int B, int H, int Hkv, int L, int d, int page, int wid
   y.wide = y.wide_pool = 0;
   y.room = y.total;
   // Pages of codes become tiles in the tile kernel, or, where a key tile meets many row tiles (each of which would do it again), bf16 pages in the workspace first.
-  // 2 x 16 heads x 12000 keys of 128 channels, us, in the kernel and before it, by row tiles: two 76 and 130, four 134 and 188, five 157 and 162, six 182 and 181, eight 250
-  // and 217, twelve 365 and 292 (of 64 channels: six 140 and 147, eight 194 and 191); 12800 shared ones: two 54 and 72, six 125 and 124, twelve 240 and 207.
+  // us, in the kernel and before it, by row tiles:
+  //                                             two        four        six         seven       eight       twelve
+  //   2 x 16 heads x 12000 keys, 128 channels   74, 125    134, 197    185, 206    255, 235    252, 238    393, 351
+  //                               64 channels   56, 73     98, 111     141, 147    194, 191    194, 191    285, 272
+  //   8 heads x 12800 shared keys, 128          31, 49     47, 64      70, 88                  86, 79      121, 106
+  //                                 64          26, 30     37, 40      55, 57                  66, 66      91, 88
   const long long own = y.own_stream ? 0 : s.stack ? most - PT : most, shared = s.stack ? PT : 0;
   if (codes > 0 && y.tile && TP * shared + F * own > kWidenTiles * (shared + B * own)) {
     // Room for the pages that the rows can name, which is what the copy is laid out by where the pool has more.

@@ -147,7 +147,7 @@ __device__ __forceinline__ void prefix_check_begin(const PrefixParams& p) {
 }
 
 // CTAs that an SM holds, by shared memory: with one product's columns three of two stages (of 8 KB; 64 sequences of 100 to 2048 keys, us: 55.4, two of three stages 58.7),
-// with two products' the warps take longer and want more ahead (32 sequences x 8 x 2048 keys, 16 rows: 71.5 and 58.0).  Codes: by registers, 128, 233 and 248 a thread (32 x 8 items of
+// with two products' the warps take longer and want more ahead (32 sequences x 8 x 2048 keys, 16 rows: 71.5 and 58.0).  Codes: by registers, 128 a thread, 234, 250 and 254 (32 x 8 items of
 // 2048 keys, 16 rows, us, with two, three and four CTAs of them: 33, 46, 39); two stages (of 4.6 KB) are as good as three.
 constexpr int stream_ctas(int NT, bool q4) { return q4 ? (NT == 1 ? 4 : 2) : NT == 1 ? 3 : 2; }
 
