@@ -239,10 +239,11 @@ class Outputs {
       w.size[k] = sizes[k];
       w.stride[k] = strides[k];
       none = none || sizes[k] == 0;
-      last += (sizes[k] - 1) * strides[k];
+      int64_t reach;
+      if (__builtin_mul_overflow(sizes[k] - 1, strides[k], &reach) || __builtin_add_overflow(last, reach, &last)) last = INT64_MAX, none = true;
     }
     w.at = total_;
-    if (none || total_ > kTogether || last > kTogether) {      // (nothing to save, and no sum to overflow)
+    if (none || total_ > kTogether || last > kTogether) {      // (nothing to save; of more than 63 bits nothing to be had, which the allocation says)
       total_ = kTogether + 1;
     } else {
       total_ += ((last + 1) * item + 511) / 512 * 512;

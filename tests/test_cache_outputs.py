@@ -27,3 +27,12 @@ def test_keys_that_are_kept_do_not_keep_the_queries(N):
     pos = torch.arange(3 * N, dtype=torch.int32, device="cuda").view(N, 3)
     for x in av.avsa_rope(q, k, pos, av.avsa_rope_frequencies(sections), sections):
         assert x.untyped_storage().nbytes() <= max(MOST, x.numel() * x.element_size() + 512)
+
+
+@gpu
+def test_more_tokens_than_63_bits_count_are_refused():
+    """32768 sequences x 32768 heads x 2^30 tokens x 64 channels are 2^66 values: no size that wrapped around is allocated, and nothing runs."""
+    pool = torch.zeros((1, 32768, 16, 36), dtype=torch.uint8, device="cuda")
+    table, length = torch.zeros((32768, 1), dtype=torch.int32, device="cuda"), torch.zeros(32768, dtype=torch.int32, device="cuda")
+    with pytest.raises(RuntimeError):
+        av.avsa_cache_read_q4(pool, pool, table, length, 1 << 30)
