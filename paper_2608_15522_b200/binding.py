@@ -7,8 +7,9 @@ PyTorch appears here for device memory and the current stream; every step of the
 library's CUDA kernels.  There is no CPU fallback: without the built library, or on a machine
 without a CUDA device, the calls raise.
 
-Outputs that the calls of the paged cache and ``avsa_rope`` allocate are, up to 2 MB, parts of one allocation: tensors of their own in all but the
-storage, so that one which is kept keeps the others' memory and ``torch.save`` writes all of it.  A clone, or an output of the caller's, stands alone.
+Outputs that one of the calls of the paged cache or ``avsa_rope`` allocates may be parts of one allocation: tensors of their own in all but the storage,
+so that one which is kept keeps the others' memory, and ``torch.save`` writes it (2 MB at most, or as much again as the output itself has, up to 16 MB
+in all).  A clone, or an output of the caller's, stands alone.
 """
 from __future__ import annotations
 
@@ -514,7 +515,7 @@ def avsa_prefix_attn(q, k_pool, v_pool, table, length, prefix_pages=0, seq=None,
 
     k_pool/v_pool [pages,Hkv,page,d] bf16, table [seqs,width] and length [seqs] int32.  causal: the queries are the last L tokens of
     their sequence, or with count int32 [B] the first count[b] of them its last count[b] tokens, and the rows behind are empty.  Returns (o, lse or None, ws), which may share
-    an allocation of up to 2 MB."""
+    an allocation."""
     done = (_cache_module or _cache()).attn(q, k_pool, v_pool, table, length, prefix_pages, seq, causal, softmax_scale, want_lse, o, lse, ws, count, log)
     if done[0] != AVSA_OK:
         raise AvsaError(done[0], "avsa_prefix_attn")
@@ -593,7 +594,7 @@ def avsa_cache_write_q4(k_new, v_new, k_pool, v_pool, table, length, seq=None, c
 def avsa_cache_read_q4(k_pool, v_pool, table, length, tokens, seq=None, count=None, k=None, v=None):
     """The last count[k] (None: ``tokens``) tokens of sequence seq[k] (None: of every sequence) as the pages have them, exactly.
 
-    Returns (k, v) bf16 [n,Hkv,tokens,d], which may share an allocation of up to 2 MB; tokens that there are not are zeros."""
+    Returns (k, v) bf16 [n,Hkv,tokens,d], which may share an allocation; tokens that there are not are zeros."""
     done = (_cache_module or _cache()).read_q4(k_pool, v_pool, table, length, tokens, seq, count, k, v)
     if done[0] != AVSA_OK:
         raise AvsaError(done[0], "avsa_cache_read_q4")
@@ -628,7 +629,7 @@ def avsa_rope(q, k, pos, freq, sections, halves=False, inverse=False, q_out=None
 
     pos int32 [B,N,axes] or [N,axes], freq fp64 [d/2] (avsa_rope_frequencies), sections the pairs of each axis.  Pairs are channels (2i, 2i + 1), with halves
     (i, i + d/2).  inverse turns back; as a rotation's transpose that is its gradient too.  q_out and k_out may be q and k.  Returns (q_out, k_out or None),
-    which, where the call allocates both, may share an allocation of up to 2 MB."""
+    which may share an allocation where the call makes both."""
     done = (_cache_module or _cache()).rope(q, k, pos, freq, tuple(sections), halves, inverse, q_out, k_out)
     if done[0] != AVSA_OK:
         raise AvsaError(done[0], "avsa_rope")

@@ -172,9 +172,9 @@ void same_pools(const PoolQ4& k, const PoolQ4& v) {
 }
 
 // What a call allocates: its outputs are parts of one allocation, each at a multiple of 512 bytes, since an allocation takes 0.8 us of a call's 5 to 8 on the host.
-// Who keeps one of them keeps the memory of all, so this is done up to 2 MB only, what the caching allocator takes from the device for small tensors, of which any one keeps all
-// as well; a workspace is among them up to 64 KB.  (Measured, us of host time apart and together: attention of one token 7.65 and 6.2, read of two short sequences 6.5
-// and 5.6.)
+// Who keeps one of them keeps the memory of all, so they are apart where that is more than as much again and more than 2 MB (what the caching allocator takes from the device for
+// small tensors, of which any one keeps all as well), and above 16 MB, where the device takes longer than that; a workspace is among them up to 64 KB.  (Measured, us of host time
+// apart and together: attention of one token 7.65 and 6.2, read of two short sequences 6.5 and 5.6.)
 class Outputs {
  public:
   explicit Outputs(const Call& c) : c_(c) {}
@@ -200,7 +200,7 @@ class Outputs {
   void allocate() {
     const auto options = at::TensorOptions().device(c_.device);
     at::Tensor all;
-    if (n_ > 1 && total_ <= kTogether) all = at::empty({total_}, options.dtype(at::kByte));
+    if (n_ > 1 && total_ <= kTogether && total_ - least_ <= std::max(least_, kKept)) all = at::empty({total_}, options.dtype(at::kByte));
     for (int k = 0; k < n_; k++) {
       const Wanted& w = wanted_[k];
       const at::IntArrayRef sizes(w.size, w.dims), strides(w.stride, w.dims);
@@ -218,7 +218,7 @@ class Outputs {
   }
 
  private:
-  static constexpr int64_t kTogether = 2 << 20;
+  static constexpr int64_t kTogether = 16 << 20, kKept = 2 << 20;
   static constexpr size_t kWorkspaceWithin = 64 << 10;
   struct Wanted {
     Arg* out;
@@ -246,13 +246,15 @@ class Outputs {
     if (none || total_ > kTogether || last > kTogether) {      // (nothing to save; of more than 63 bits nothing to be had, which the allocation says)
       total_ = kTogether + 1;
     } else {
-      total_ += ((last + 1) * item + 511) / 512 * 512;
+      const int64_t bytes = ((last + 1) * item + 511) / 512 * 512;
+      total_ += bytes;
+      least_ = std::min(least_, bytes);
     }
   }
   const Call& c_;
   Wanted wanted_[3];
   int n_ = 0;
-  int64_t total_ = 0;
+  int64_t total_ = 0, least_ = INT64_MAX;
 };
 
 PyObject* result(int status, std::initializer_list<PyObject*> items) {

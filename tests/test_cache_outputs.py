@@ -13,7 +13,7 @@ MOST = 2 << 20      # what the outputs of one call may share
 @gpu
 @pytest.mark.parametrize("L", [1, 200, 700])
 def test_one_output_keeps_little_of_the_others(L):
-    """Outputs of a call share memory only where all of it is little: who keeps one keeps 2 MB more at most."""
+    """An lse does not keep a large o, nor o a large workspace: who keeps an output keeps 2 MB in all, or what it has itself."""
     q, k, v, table, length = attention_case(2, 16, 4, L, 128, 64, [900, 800], seed=1)
     for o in av.avsa_prefix_attn(q, k, v, cu(table), cu(length), want_lse=True):
         assert o.untyped_storage().nbytes() <= max(MOST, o.numel() * o.element_size() + 512)
@@ -36,3 +36,14 @@ def test_more_tokens_than_63_bits_count_are_refused():
     table, length = torch.zeros((32768, 1), dtype=torch.int32, device="cuda"), torch.zeros(32768, dtype=torch.int32, device="cuda")
     with pytest.raises(RuntimeError):
         av.avsa_cache_read_q4(pool, pool, table, length, 1 << 30)
+
+
+@gpu
+@pytest.mark.parametrize("tokens", [1, 300, 3000])
+def test_keys_that_are_kept_keep_no_more_than_the_values(tokens):
+    """Two outputs of one size: as much again at most, and nothing of the other one's beyond 16 MB."""
+    pool = torch.zeros((400, 8, 16, 72), dtype=torch.uint8, device="cuda")
+    table, length = torch.arange(400, dtype=torch.int32, device="cuda").view(2, 200), torch.full((2,), 3000, dtype=torch.int32, device="cuda")
+    for x in av.avsa_cache_read_q4(pool, pool, table, length, tokens):
+        own = x.numel() * x.element_size()
+        assert x.untyped_storage().nbytes() <= (own if 2 * own > 16 << 20 else 2 * own) + 1024
