@@ -377,6 +377,7 @@ AVSA_API size_t avsa_cache_workspace_bytes(int seqs, int pages, int n);
  *                     stacked ones) the pages that the batch reads are first made bf16 in the workspace, which then has room for these: as many as the
  *                     rows can name, N = prefix_pages + B * (width - prefix_pages), or all that the pool has where these are fewer (2 * Hkv * page * d of bf16 each).
  *                     The query's answer grows with its `pages`; a call needs no more than for min(pages, N) of them.  It may be the same workspace for all layers.
+ *                     The shared pages are then read by the longest sequence's row, as where they are stacked.
  *
  * Neither a write nor a read needs a workspace or leaves a status.
  */

@@ -85,3 +85,36 @@ def test_large_pool_of_chosen_sequences():
     assert torch.equal(torch.isinf(lse), ~seen) and (o[~seen] == 0).all()
     close_o(o.double()[seen].cpu().numpy(), want[seen].cpu().numpy(), "chosen")
     close_lse(lse.double()[seen].cpu().numpy(), want_lse[seen].cpu().numpy(), "chosen")
+
+
+@gpu
+@pytest.mark.parametrize("row", [0, 1, 2])
+def test_large_pool_with_a_bad_page(row):
+    """A page out of range in any row: reported, zeros, and nothing that the workspace held; sequence 1 is the longest, whose row the shared pages are read by."""
+    B, page, shared = 3, 16, 40
+    (q, k, v, table, length), values = held_case(B, 2, 2, 900, 64, page, [1000, 1300, 900], shared=shared, seed=4)
+    pages = 6 * (shared + B * table.shape[1])
+    far = [torch.zeros((pages, *x.shape[1:]), dtype=torch.uint8, device="cuda") for x in (k, v)]
+    for x, y in zip(far, (k, v)):
+        x[pages - y.shape[0]:] = y
+    moved = np.where(table >= 0, table + pages - k.shape[0], -1).astype(np.int32)
+    call = lambda t, ws=None: av.avsa_prefix_attn_q4(q, *far, cu(t), cu(length), prefix_pages=shared, want_lse=True, ws=ws)
+    good = call(moved)
+    assert status(good[2]) == av.AVSA_OK
+    for at, bad in ((7, -1), (39, pages), (50, 1 << 30)):      # two shared ones and one of its own
+        t = moved.copy()
+        t[row, at] = bad
+        o, lse, ws = call(t, torch.full_like(good[2], 255))
+        assert status(ws) == av.AVSA_ERR_BAD_TABLE and torch.isfinite(o.float()).all() and torch.isfinite(lse).all()
+        # without that page: zeros for whoever goes by it
+        hit = [b for b in range(B) if b == row or (at < shared and row == 1)]
+        zero = [x.clone() for x in values[1:3]]
+        for x in zero:
+            x[table[row, at]] = 0.0
+        want, want_lse = exact_on_gpu(values[0], *zero, table, length)
+        for b in range(B):
+            if b not in hit:
+                assert torch.equal(o[b], good[0][b]) and torch.equal(lse[b], good[1][b])
+            else:
+                close_o(o[b].double().cpu().numpy(), want[b].cpu().numpy(), "zeros")
+                close_lse(lse[b].double().cpu().numpy(), want_lse[b].cpu().numpy(), "zeros")
